@@ -19,6 +19,13 @@
  *                                                closed masks onto the grid
  *   front end (Sec. 3.1)   rs3_seed_from_masks -- seed box of Eq. 1 from
  *                                                pixel masks, down_s
+ * and, for banks of hundreds of frames (no counterpart in the paper),
+ *   rs3_qk_norm_rope       -- RMS norm of query and key heads, rotated (Eq. 7)
+ *   rs3_bank_copy          -- units copied, forked and compacted
+ *   rs3_bank_drop_frames   -- ring frames given up at either end
+ *   rs3_bank_digest, rs3_block_select, rs3_sparse_readout
+ *                          -- the readout over the blocks of the bank that
+ *                             score highest for each query
  *
  * Vocabulary.  A *unit* is one (stream, object) pair: it owns one keep-set,
  * one memory bank and one output grid.  A *group* is the set of units that
@@ -268,6 +275,46 @@ rs3_status rs3_bank_set_pointers(const rs3_bank *bank, const void *k_ptr, const 
  * movement. */
 rs3_status rs3_bank_reset(const rs3_bank *bank, int unit, rs3_stream_t stream);
 
+/* Gives up ring frames of every unit: the n_oldest[u] oldest (room for commits
+ * to an unbounded bank) and the n_newest[u] newest (a frame that was committed
+ * on trial).  Counters only, no data movement.
+ *   n_oldest, n_newest  device int32 [U], each may be NULL (none)
+ * A negative number, or more frames than the unit holds, latches RS3_EINVAL
+ * into *status and leaves the unit as it is. */
+rs3_status rs3_bank_drop_frames(const rs3_bank *bank, const int32_t *n_oldest,
+                                const int32_t *n_newest, int32_t *status, rs3_stream_t stream);
+
+/* Bytes of device workspace rs3_bank_copy needs for U destination units and mask
+ * rows of keep_stride bytes (0 without a mask). */
+size_t rs3_bank_copy_workspace_bytes(int U, int64_t keep_stride);
+
+/*
+ * Copies units of `src` into units of `dst`: destination unit u becomes the kept
+ * rows of source unit parent[u], in logical order (pinned, ring frames oldest
+ * first, pointers).  With parents that repeat this forks a unit, with `keep` it
+ * compacts it, and a `dst` with a larger ring lets it grow.
+ *   parent  device int32 [dst->U]; -1 leaves the unit as it is
+ *   keep    device uint8 [dst->U][keep_stride] or NULL (all rows): row u, byte i
+ *           nonzero keeps logical row i of the parent; keep_stride is at least
+ *           the parent's length (bytes past it are not read).  Frames keep their
+ *           order and number, with the rows that are left of them (maybe none)
+ *   workspace device, >= rs3_bank_copy_workspace_bytes(dst->U, keep_stride)
+ *           bytes, 16-byte aligned; NULL is allowed without `keep`
+ * The rows are laid from the first pinned, ring and pointer row of the
+ * destination; its other rows keep their bits.  Values are copied bit for bit.
+ * Both banks have the same H, d, dtype and mn (else RS3_EINVAL); their pinned,
+ * ring, frame and pointer capacities may differ.  Status: RS3_EINVAL for a parent
+ * outside [-1, src->U) or a mask row shorter than the parent, RS3_ECAPACITY for
+ * rows or frames that do not fit; such a unit is left as it is, others proceed.
+ * `dst` may be `src` itself: unit u with parent[u] = u then stays as it is (with
+ * `keep`: RS3_EINVAL), and a parent p of another unit must itself stay as it is
+ * (parent[p] = -1, or p without `keep`), else that unit latches RS3_EINVAL.
+ * Banks whose storage overlaps otherwise are refused (RS3_EINVAL).
+ */
+rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, const int32_t *parent,
+                         const uint8_t *keep, int64_t keep_stride, void *workspace,
+                         size_t workspace_bytes, int32_t *status, rs3_stream_t stream);
+
 /* Copies the per-unit counters to host memory and SYNCHRONISES `stream`
  * (tests and tools only).  host_out: int64 [U][8] =
  * {head, tail, cond_len, n_frames, oldest, n_cond_frames, ptr_len, length}
@@ -391,6 +438,124 @@ rs3_status rs3_memory_readout_run(const void *q, rs3_dtype dtype, int G, int mn,
                                   const float *rope, const void *residual, void *out, float scale,
                                   void *workspace, size_t workspace_bytes, int32_t *status,
                                   rs3_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Read side over chosen blocks of a long bank                               */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Blocks.  Block b of a unit is its storage rows [b*block, (b+1)*block), of which
+ * the live ones count (a block may lie across the end of a region or of the ring).
+ * `block` is 32, 64 or 128.  rs3_bank_blocks gives the number of blocks of a
+ * unit's storage (-1 for an uninitialised bank).
+ *
+ * 8-bit vectors.  A vector x is held as whole numbers t with |t| <= 127 and a step:
+ *   e = floor(log2 max|x|), t = rint(x 2^(6-e)) cut to [-127, 127], step 2^(e-6);
+ * a vector with max|x| < 2^-100 is t = 0, step 0.  t . t' * step is exact in fp32.
+ */
+int64_t rs3_bank_blocks(const rs3_bank *bank, int block);
+
+/*
+ * Digest of a block, per head: the mean of its live keys in 8 bits.
+ *   refresh  -1: all blocks; n >= 0: the blocks of the n newest ring frames' rows,
+ *            and those of the ring's oldest and newest rows and of its two ends.
+ *            After a ring commit refresh = 1 brings the digests up to date, after
+ *            rs3_bank_drop_frames refresh = 0; after commits of conditioning
+ *            frames, pointer rows, rs3_bank_copy and rs3_bank_reset take -1
+ *   digest   device int8 [U][H][blocks][d], 16-byte aligned
+ *   step     device fp32 [U][H][blocks], 16-byte aligned
+ * A block without live rows that is visited gets zeros.  The sums are fp32 in one
+ * fixed order: partial sum p (0..7) takes rows p, p+8, ... of the block ascending,
+ * then ((0+4)+(2+6)) + ((1+5)+(3+7)), divided by the number of live rows.
+ * d: a power of two in [16, 256] (else RS3_EUNSUPPORTED).
+ */
+rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refresh, int8_t *digest,
+                           float *step, int32_t *status, rs3_stream_t stream);
+
+/* Bytes of device workspace rs3_block_select needs; never falls as U, H, k_max or
+ * n_blocks grows. */
+size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int n_blocks);
+
+/*
+ * For every unit u, kept query j < count[u] at cell i = idx[u][j] and head h, the
+ * n_top blocks with the highest scores, ascending:
+ *   t_q   = q[g][i]'s head h in 8 bits, rotated before by rope[i] when given (each
+ *           product and each sum rounded to fp32)
+ *   score = (t_q . digest[u][h][b]) * step[u][h][b]     (the query's own step is
+ *           the same for all blocks and left out)
+ * over the blocks that hold a live row; equal scores go to the lower block.
+ *   q .. k_max, bank, rope  as for rs3_memory_readout
+ *   digest, step  as rs3_bank_digest wrote them for this bank and block
+ *   sel   device int32 [U][H][k_max][n_top]; entries past the blocks that there
+ *         are become -1; rows at or past count[u] are left as they were
+ *   workspace device, >= rs3_block_select_workspace_bytes(U, H, k_max, blocks)
+ *         bytes, 16-byte aligned; one call at a time
+ * Limits: d a power of two in [16, 256], n_top <= 1024, k_max <= mn, at most 49152
+ * blocks per unit, else RS3_EUNSUPPORTED (RS3_EINVAL for k_max).  A unit with a
+ * count outside [0, k_max] or a group outside [0, G) latches RS3_EINVAL and is
+ * skipped; a cell outside [0, mn) latches it and that query gets some blocks.
+ */
+rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
+                            const int32_t *unit_group, const int32_t *idx, const int32_t *count,
+                            int k_max, const rs3_bank *bank, int block, const int8_t *digest,
+                            const float *step, const float *rope, int n_top, int32_t *sel,
+                            void *workspace, size_t workspace_bytes, int32_t *status,
+                            rs3_stream_t stream);
+
+/* Bytes of device workspace rs3_sparse_readout needs; never falls as U, H, k_max,
+ * n_top or n_blocks grows. */
+size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks,
+                                          rs3_dtype dtype);
+
+/*
+ * rs3_memory_readout where each query attends to the live rows of its own blocks:
+ * those that sel[u][h][j][0..n_top) lists (as rs3_block_select writes it; entries
+ * below 0 are skipped, one at or past the number of blocks latches RS3_EINVAL and
+ * is skipped, a block listed twice counts twice).  A query whose blocks hold no
+ * live row reads A = 0.  Arguments and results otherwise as rs3_memory_readout;
+ * idx holds distinct cells; a cell outside [0, mn) latches RS3_EINVAL and is
+ * skipped, a count outside [0, k_max] latches it and the unit is skipped.
+ *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, 16-byte
+ *         aligned; one call at a time
+ * Limits: those of rs3_block_select, without one on the blocks.
+ */
+rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
+                              const int32_t *unit_group, const int32_t *idx, const int32_t *count,
+                              int k_max, const rs3_bank *bank, int block, const int32_t *sel,
+                              int n_top, const float *rope, const void *residual, void *out,
+                              float scale, void *workspace, size_t workspace_bytes,
+                              int32_t *status, rs3_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Query and key heads: RMS norm with the position rotation (Eq. 7)          */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * For every row r of x (queries: q, keys: k; either may be NULL with 0 rows) and
+ * every head: y = x / sqrt(mean(x^2) + eps) * weight over the head's d elements,
+ * then elements (2p, 2p+1) become (y0 cos - y1 sin, y0 sin + y1 cos) with
+ * (cos, sin) = rope[r mod mn][p], the row's own cell.  fp32, rounded once.
+ *   q, k         device [rows] rows of H*d elements, `stride` elements apart (a
+ *                projection that holds queries, keys and values side by side is
+ *                read in place)
+ *   q_out, k_out device rows `out_stride` elements apart; may be the input itself
+ *                with the same stride, and may not overlap it otherwise
+ *   weight       device fp32 [d] or NULL (ones); 16-byte aligned
+ *   keep         device uint8 [rows] or NULL: rows with 0 are neither read nor
+ *                written (keys that no commit will store)
+ *   rope         device fp32 [mn][d/2][2] or NULL (no rotation), 16-byte aligned
+ *   eps          >= 0; a head of zeros gives zeros where eps > 0
+ * With the normed keys a bank takes rs3_bank_commit (they are rotated already),
+ * and the readouts take the normed queries with rope = NULL.
+ * Limits: d * sizeof(elem) a multiple of 16 (else RS3_EINVAL), d <= 256, mn <=
+ * 16384; strides (in bytes) multiples of 16.
+ */
+rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_stride, int Hq,
+                            const float *q_weight, const uint8_t *q_keep, void *q_out,
+                            int64_t q_out_stride, const void *k, int64_t k_rows, int64_t k_stride,
+                            int Hk, const float *k_weight, const uint8_t *k_keep, void *k_out,
+                            int64_t k_out_stride, rs3_dtype dtype, int mn, int d, float eps,
+                            const float *rope, rs3_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Write side: keep-set (Sec. 3.2; Eq. 8)                                    */

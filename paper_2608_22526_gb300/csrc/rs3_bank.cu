@@ -6,34 +6,12 @@
 // accesses, the first rows' loads in flight while the unit's counts and the
 // capacity decision are made; the last CTA of each unit publishes the new
 // counters.
-#include "rs3_internal.cuh"
+#include "rs3_bank.cuh"
 
 #include <cstdlib>
 #include <cstring>
 
 namespace {
-
-struct BankDev {
-    int64_t *meta;
-    int64_t stride_words;
-    int32_t max_frames, window, n_cond, n_ptr;
-    int64_t pinned_cap, ring_cap, rows_per_unit;
-};
-
-BankDev bank_dev(const rs3_bank *b)
-{
-    BankDev v;
-    v.meta = static_cast<int64_t *>(b->meta);
-    v.stride_words = b->meta_stride / 8;
-    v.max_frames = b->max_frames;
-    v.window = b->window;
-    v.n_cond = b->n_cond;
-    v.n_ptr = b->n_ptr;
-    v.pinned_cap = b->pinned_cap;
-    v.ring_cap = b->ring_cap;
-    v.rows_per_unit = b->rows_per_unit;
-    return v;
-}
 
 // Copies `nvec` 16-byte words of one row (one warp).
 __device__ __forceinline__ void copy_row(uint4 *__restrict__ dk, uint4 *__restrict__ dv,
@@ -348,13 +326,6 @@ __global__ void k_bank_reset(BankDev bk, int unit, int U)
         for (int w = threadIdx.x; w < BM_HEADER_WORDS; w += blockDim.x) mu[w] = 0;
     }
 }
-
-bool bank_ok(const rs3_bank *b)
-{
-    return b && b->magic == RS3_BANK_MAGIC && b->meta && b->k_store && b->v_store && b->U >= 1;
-}
-
-size_t elem_bytes(int dtype) { return dtype == RS3_BF16 ? 2 : 4; }
 
 }  // namespace
 

@@ -1,0 +1,213 @@
+// rs3_norm.cu -- RMS norm of every query and key head with the position rotation
+// (Sec. 3.1, Eq. 7) in the same pass.
+//
+//   y = x / sqrt(mean(x^2) + eps) * w,  then each pair (y0, y1) of the row's cell becomes
+//   (y0 cos - y1 sin, y0 sin + y1 cos)
+//
+// in fp32, rounded once to the stored type.  A head is read once into the registers of a
+// group of lanes (16 bytes each), so the sum of squares, the scaling and the rotation cost no
+// second read: the call is bound by the bytes of x and y.
+#include "rs3_internal.cuh"
+
+namespace {
+
+// One of the call's two tensors (queries or keys).
+struct NormSide {
+    const uint8_t *x;
+    uint8_t *y;
+    const float *weight;       // [d] or NULL
+    const uint8_t *keep;       // [rows] or NULL
+    int64_t rows, x_stride, y_stride;      // strides in bytes
+    int32_t H, turns;          // heads; rows of one cell: ceil(rows / mn)
+    int32_t per_cta;           // turns that one CTA takes
+    int32_t ctas;              // CTAs of this side: cell blocks x turn blocks
+    int32_t cell_blocks;
+};
+
+constexpr int NORM_THREADS = 256;
+constexpr int NORM_FLIGHT = 4;             // rows in flight per lane group
+
+template <typename T>
+struct Piece;                              // 16 bytes of a row
+template <>
+struct Piece<uint16_t> {
+    static constexpr int N = 8;
+    __device__ static __forceinline__ void widen(uint4 v, float *f)
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    __device__ static __forceinline__ uint4 narrow(const float *f)
+    {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <>
+struct Piece<float> {
+    static constexpr int N = 4;
+    __device__ static __forceinline__ void widen(uint4 v, float *f)
+    {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y);
+        f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+    __device__ static __forceinline__ uint4 narrow(const float *f)
+    {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+
+// A group of L lanes (a power of two) holds one head, ITEMS pieces each; it takes the rows of
+// one (cell, head) through the grids that share the cell, so the cell's angles are loaded once.
+template <typename T, int ITEMS>
+__global__ void __launch_bounds__(NORM_THREADS)
+k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float *__restrict__ rope)
+{
+    constexpr int N = Piece<T>::N;
+    pdl_wait();
+    const bool is_q = (int)blockIdx.x < q.ctas;
+    const NormSide &s = is_q ? q : k;
+    const int b = is_q ? (int)blockIdx.x : (int)blockIdx.x - q.ctas;
+    const int cb = b % s.cell_blocks, tb = b / s.cell_blocks;
+    const int groups = NORM_THREADS / L, lane = threadIdx.x & (L - 1);
+    const int64_t g = (int64_t)cb * groups + threadIdx.x / L;      // (cell, head)
+    const int pieces = d / N;
+    const bool here = g < (int64_t)mn * s.H;
+    const int cell = here ? (int)(g / s.H) : 0, head = here ? (int)(g % s.H) : 0;
+    // what the cell's rows share: the head's weights and the cell's angles
+    float w[ITEMS][N], cs[ITEMS][N];                               // (cos, sin) pairs
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int p = lane + i * L;
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            float4 a = make_float4(1.f, 1.f, 1.f, 1.f), c = make_float4(1.f, 0.f, 1.f, 0.f);
+            if (p < pieces && s.weight) a = __ldg(reinterpret_cast<const float4 *>(s.weight + p * N + e));
+            if (p < pieces && rope) c = __ldg(reinterpret_cast<const float4 *>(rope + (int64_t)cell * d + p * N + e));
+            w[i][e] = a.x; w[i][e + 1] = a.y; w[i][e + 2] = a.z; w[i][e + 3] = a.w;
+            cs[i][e] = c.x; cs[i][e + 1] = c.y; cs[i][e + 2] = c.z; cs[i][e + 3] = c.w;
+        }
+    }
+    const int t1 = min(s.turns, (tb + 1) * s.per_cta);
+    for (int t0 = tb * s.per_cta; t0 < t1; t0 += NORM_FLIGHT) {
+        uint4 v[NORM_FLIGHT][ITEMS];
+        bool take[NORM_FLIGHT];
+#pragma unroll
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            const int64_t row = (int64_t)(t0 + f) * mn + cell;
+            take[f] = here && t0 + f < t1 && row < s.rows && (!s.keep || s.keep[row] != 0);
+        }
+#pragma unroll
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            const int64_t row = (int64_t)(t0 + f) * mn + cell;
+            const uint4 *src = reinterpret_cast<const uint4 *>(s.x + row * s.x_stride) + head * pieces;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int p = lane + i * L;
+                v[f][i] = take[f] && p < pieces ? __ldcs(src + p) : make_uint4(0, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            float x[ITEMS][N], sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                Piece<T>::widen(v[f][i], x[i]);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum = fmaf(x[i][e], x[i][e], sum);
+            }
+            for (int o = L >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const float r = rsqrtf(sum / (float)d + eps);
+            if (!take[f]) continue;
+            const int64_t row = (int64_t)(t0 + f) * mn + cell;
+            uint4 *dst = reinterpret_cast<uint4 *>(s.y + row * s.y_stride) + head * pieces;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int p = lane + i * L;
+                float y[N];
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const float y0 = x[i][e] * r * w[i][e], y1 = x[i][e + 1] * r * w[i][e + 1];
+                    y[e] = y0 * cs[i][e] - y1 * cs[i][e + 1];
+                    y[e + 1] = y0 * cs[i][e + 1] + y1 * cs[i][e];
+                }
+                if (p < pieces) dst[p] = Piece<T>::narrow(y);
+            }
+        }
+    }
+}
+
+// Fills one side; false when its arguments are not what the header asks for.
+bool norm_side(NormSide &s, const void *x, int64_t rows, int64_t stride, int H, const float *weight, const uint8_t *keep,
+               void *y, int64_t y_stride, int esz, int d)
+{
+    s = {};
+    s.cell_blocks = 1;
+    if (rows == 0 && !x && !y) return true;
+    if (!x || !y || rows < 0 || H < 1) return false;
+    if (!rs3_aligned16(x) || !rs3_aligned16(y) || (weight && !rs3_aligned16(weight))) return false;
+    const int64_t width = (int64_t)H * d;
+    if (stride < width || y_stride < width || stride * esz % 16 != 0 || y_stride * esz % 16 != 0) return false;
+    if (x == y && stride != y_stride) return false;          // in place: every row over itself
+    s.x = static_cast<const uint8_t *>(x);
+    s.y = static_cast<uint8_t *>(y);
+    s.weight = weight;
+    s.keep = keep;
+    s.rows = rows;
+    s.x_stride = stride * esz;
+    s.y_stride = y_stride * esz;
+    s.H = H;
+    return true;
+}
+
+}  // namespace
+
+extern "C" rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_stride, int Hq, const float *q_weight,
+                                       const uint8_t *q_keep, void *q_out, int64_t q_out_stride, const void *k,
+                                       int64_t k_rows, int64_t k_stride, int Hk, const float *k_weight,
+                                       const uint8_t *k_keep, void *k_out, int64_t k_out_stride, rs3_dtype dtype, int mn,
+                                       int d, float eps, const float *rope, rs3_stream_t stream)
+{
+    if (dtype != RS3_F32 && dtype != RS3_BF16) return RS3_EINVAL;
+    if (mn < 1 || d < 1 || !(eps >= 0.f) || (rope && !rs3_aligned16(rope))) return RS3_EINVAL;
+    const int esz = dtype == RS3_BF16 ? 2 : 4;
+    if (d * esz % 16 != 0) return RS3_EINVAL;
+    if (d > 256 || mn > RS3_MAX_MN) return RS3_EUNSUPPORTED;
+    NormSide s[2];
+    if (!norm_side(s[0], q, q_rows, q_stride, Hq, q_weight, q_keep, q_out, q_out_stride, esz, d) ||
+        !norm_side(s[1], k, k_rows, k_stride, Hk, k_weight, k_keep, k_out, k_out_stride, esz, d))
+        return RS3_EINVAL;
+    const int pieces = d * esz / 16, items = pieces > 32 ? 2 : 1;
+    int L = 1;
+    while (L * items < pieces) L <<= 1;
+    const int groups = NORM_THREADS / L;
+    int64_t total = 0;
+    for (NormSide &t : s) {
+        if (t.rows == 0) continue;
+        const int64_t turns = (t.rows + mn - 1) / mn, cells = t.rows < mn ? t.rows : mn;
+        const int64_t cb = (cells * t.H + groups - 1) / groups;
+        // a CTA takes 16 rows of its cells, fewer where that leaves SMs idle
+        int64_t per = 16;
+        while (per > 1 && cb * ((turns + per - 1) / per) < 4ll * rs3_sm_count()) per >>= 1;
+        const int64_t ctas = cb * ((turns + per - 1) / per);
+        if (turns > INT32_MAX || ctas > INT32_MAX) return RS3_EUNSUPPORTED;
+        t.turns = (int32_t)turns;
+        t.per_cta = (int32_t)per;
+        t.cell_blocks = (int32_t)cb;
+        t.ctas = (int32_t)ctas;
+        total += ctas;
+    }
+    if (total == 0) return RS3_OK;
+    if (total > INT32_MAX) return RS3_EUNSUPPORTED;
+    void (*kern)(NormSide, NormSide, int, int, int, float, const float *) =
+        dtype == RS3_BF16 ? k_norm_rope<uint16_t, 1> : items == 1 ? k_norm_rope<float, 1> : k_norm_rope<float, 2>;
+    launch_pdl(kern, dim3((unsigned)total), dim3(NORM_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), s[0], s[1], mn, d, L,
+               eps, rope);
+    return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+}

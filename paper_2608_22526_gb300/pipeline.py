@@ -116,6 +116,67 @@ class Pipeline:
     def set_pointers(self, kp: torch.Tensor, vp: torch.Tensor):
         rs3.rs3_bank_set_pointers(self.bank, kp, vp, self.status, self.stream)
 
+    # -- long banks ------------------------------------------------------------
+    def norm(self, q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
+             k_out: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+             k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, rope: Optional[torch.Tensor] = None,
+             k_keep: Optional[torch.Tensor] = None):
+        """RMS norm of the frame's query and key heads, rotated by their own cells: what
+        readout() and commit() then take without a table.  k_keep: the commit's mask."""
+        w = self.w
+        rs3.rs3_qk_norm_rope(q, q_out, k, k_out, w.dtype, w.mn, w.H, w.H, w.d, q_weight, k_weight, eps, rope,
+                             k_keep=k_keep, stream=self.stream)
+
+    def use_blocks(self, block: int, n_top: int):
+        """Buffers for reading the bank by blocks: digests, the chosen blocks and workspaces."""
+        w, dev, nb = self.w, self.device, self.bank.blocks(block)
+        self.block, self.n_top = block, n_top
+        self.block_digest = torch.zeros((w.U, w.H, nb, w.d), dtype=torch.int8, device=dev)
+        self.block_step = torch.zeros((w.U, w.H, nb), dtype=torch.float32, device=dev)
+        self.block_sel = torch.full((w.U, w.H, max(self.k_max, 1), n_top), -1, dtype=torch.int32, device=dev)
+        self.ws_blocks = torch.empty(rs3.rs3_block_select_workspace_bytes(w.U, w.H, self.k_max, nb), dtype=torch.uint8,
+                                     device=dev)
+        self.ws_sparse = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(w.U, w.H, w.d, self.k_max, n_top, nb, w.dtype),
+                                     dtype=torch.uint8, device=dev)
+
+    def digest(self, refresh: int = 1):
+        """Brings the digests up to date: 1 after a ring commit, -1 after anything else."""
+        rs3.rs3_bank_digest(self.bank, self.block, refresh, self.block_digest, self.block_step, self.status, self.stream)
+
+    def select_blocks(self, q: torch.Tensor, rope: Optional[torch.Tensor] = None):
+        """The blocks that score highest for each kept query and head (block_sel)."""
+        w = self.w
+        rs3.rs3_block_select(q, w.dtype, w.G, w.mn, w.H, w.d, self.unit_group, self.idx, self.count, self.k_max, self.bank,
+                             self.block, self.block_digest, self.block_step, rope, self.n_top, self.block_sel,
+                             self.ws_blocks, self.status, self.stream)
+
+    def readout_blocks(self, q: torch.Tensor, residual: Optional[torch.Tensor], out: torch.Tensor,
+                       rope: Optional[torch.Tensor] = None, scale: float = 0.0):
+        """readout() over the blocks of block_sel."""
+        w = self.w
+        rs3.rs3_sparse_readout(q, w.dtype, w.G, w.mn, w.H, w.d, self.unit_group, self.idx, self.count, self.k_max,
+                               self.bank, self.block, self.block_sel, self.n_top, rope, residual, out, scale,
+                               self.ws_sparse, self.status, self.stream)
+
+    def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
+        """A pipeline (`into`, or a new one with this one's sizes) whose unit u holds the rows
+        of this one's unit parent[u], those that keep[u] leaves, and its tracker."""
+        if into is None:
+            into = Pipeline(self.w, self.device, self.dense, int(self.bank.ring_cap), self.params, self.stream)
+            if hasattr(self, "block"):
+                into.use_blocks(self.block, self.n_top)
+        stride = 0 if keep is None else keep.shape[1]
+        ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
+        rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
+        with torch.cuda.stream(self.stream):
+            chosen = self.track[parent.clamp(min=0).long()]
+            into.track.copy_(torch.where((parent >= 0)[:, None], chosen, into.track))
+        return into
+
+    def drop_frames(self, n_oldest: Optional[torch.Tensor], n_newest: Optional[torch.Tensor] = None):
+        """Gives up ring frames at either end; digest(0) follows."""
+        rs3.rs3_bank_drop_frames(self.bank, n_oldest, n_newest, self.status, self.stream)
+
     def reset(self):
         rs3.rs3_bank_reset(self.bank, -1, self.stream)
         self.track.zero_()

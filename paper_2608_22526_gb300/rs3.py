@@ -66,6 +66,18 @@ SIGNATURES = {
     "rs3_bank_set_pointers": (_I, [_P, _P, _P, _P, _P]),
     "rs3_bank_reset": (_I, [_P, _I, _P]),
     "rs3_bank_read_meta": (_I, [_P, _P, _P, _P]),
+    "rs3_bank_drop_frames": (_I, [_P, _P, _P, _P, _P]),
+    "rs3_bank_copy_workspace_bytes": (_SZ, [_I, _I64]),
+    "rs3_bank_copy": (_I, [_P, _P, _P, _P, _I64, _P, _SZ, _P, _P]),
+    "rs3_bank_blocks": (_I64, [_P, _I]),
+    "rs3_bank_digest": (_I, [_P, _I, _I, _P, _P, _P, _P]),
+    "rs3_block_select_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
+    "rs3_block_select": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _P, _P, _SZ, _P, _P]),
+    "rs3_sparse_readout_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "rs3_sparse_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _I, _P, _P, _P,
+                                ctypes.c_float, _P, _SZ, _P, _P]),
+    "rs3_qk_norm_rope": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64,
+                              _I, _I, _I, ctypes.c_float, _P, _P]),
     "rs3_readout_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
     "rs3_memory_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P,
                                 ctypes.c_float, _P, _SZ, _P, _P]),
@@ -120,6 +132,22 @@ def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _bytes(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _want(name: str, t: Optional[torch.Tensor], dtype, numel: int, optional: bool = False):
+    """A tensor of at least `numel` elements of this type on the current device."""
+    if t is None:
+        if not optional:
+            raise ValueError(f"{name} is missing")
+        return
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current CUDA device")
+    if t.dtype != dtype or t.numel() < numel:
+        raise ValueError(f"{name}: at least {numel} elements of {dtype} wanted, got {tuple(t.shape)} of {t.dtype}")
 
 
 # ---------------------------------------------------------------------------
@@ -255,6 +283,16 @@ class Bank:
         _check(rc, "rs3_bank_init")
 
     @property
+    def counters(self) -> torch.Tensor:
+        """Per unit, on the device: {head, tail, cond_len, n_frames, oldest,
+        n_cond_frames, ptr_len}, int64 [U, 7], a view of the bank's own."""
+        return self.meta.view(self.U, -1)[:, :7]
+
+    def blocks(self, block: int) -> int:
+        """Blocks of `block` storage rows of a unit (rs3_bank_blocks)."""
+        return int(lib.rs3_bank_blocks(ctypes.byref(self.desc), int(block)))
+
+    @property
     def pinned_cap(self):
         return self.desc.pinned_cap
 
@@ -290,6 +328,36 @@ def rs3_bank_reset(bank: Bank, unit: int = -1, stream=None):
     _check(rc, "rs3_bank_reset")
 
 
+def rs3_bank_drop_frames(bank: Bank, n_oldest, n_newest, status, stream=None):
+    """Gives up the n_oldest[u] oldest and n_newest[u] newest ring frames of every unit."""
+    _want("n_oldest", n_oldest, torch.int32, bank.U, optional=True)
+    _want("n_newest", n_newest, torch.int32, bank.U, optional=True)
+    _want("status", status, torch.int32, 1)
+    rc = lib.rs3_bank_drop_frames(ctypes.byref(bank.desc), _ptr(n_oldest), _ptr(n_newest), _ptr(status),
+                                  _stream(stream))
+    _check(rc, "rs3_bank_drop_frames")
+
+
+def rs3_bank_copy_workspace_bytes(U: int, keep_stride: int) -> int:
+    return int(lib.rs3_bank_copy_workspace_bytes(U, keep_stride))
+
+
+def rs3_bank_copy(dst: Bank, src: Bank, parent, keep, workspace, status, stream=None):
+    """Unit u of dst becomes the kept rows of unit parent[u] of src (-1: left as it
+    is); keep: uint8 [dst.U, at least the parents' length] over logical rows, or None."""
+    _want("parent", parent, torch.int32, dst.U)
+    _want("status", status, torch.int32, 1)
+    stride = 0
+    if keep is not None:
+        if keep.dim() != 2 or keep.shape[0] != dst.U:
+            raise ValueError("keep: one row per destination unit")
+        _want("keep", keep, torch.uint8, dst.U)
+        stride = keep.shape[1]
+    rc = lib.rs3_bank_copy(ctypes.byref(dst.desc), ctypes.byref(src.desc), _ptr(parent), _ptr(keep), stride,
+                           _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
+    _check(rc, "rs3_bank_copy")
+
+
 def rs3_bank_read_meta(bank: Bank, stream=None):
     """(counters int64 [U, 8], frames int64 [U, max_frames, 2]); synchronises."""
     import numpy as np
@@ -299,6 +367,115 @@ def rs3_bank_read_meta(bank: Bank, stream=None):
                                 fr.ctypes.data_as(ctypes.c_void_p), _stream(stream))
     _check(rc, "rs3_bank_read_meta")
     return out, fr
+
+
+# ---------------------------------------------------------------------------
+# read side over chosen blocks of a long bank
+# ---------------------------------------------------------------------------
+
+def rs3_bank_digest(bank: Bank, block: int, refresh: int, digest, step, status, stream=None):
+    """Digests (int8 [U, H, blocks, d] and their steps fp32 [U, H, blocks]) of the
+    blocks of the `refresh` newest ring frames, or of all blocks (-1)."""
+    n = bank.U * bank.H * max(0, bank.blocks(block) if block > 0 else 0)
+    _want("digest", digest, torch.int8, n * bank.d)
+    _want("step", step, torch.float32, n)
+    _want("status", status, torch.int32, 1)
+    rc = lib.rs3_bank_digest(ctypes.byref(bank.desc), block, refresh, _ptr(digest), _ptr(step), _ptr(status),
+                             _stream(stream))
+    _check(rc, "rs3_bank_digest")
+
+
+def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status):
+    _want("q", q, TORCH_DTYPES[dtype], G * mn * H * d)
+    _want("unit_group", unit_group, torch.int32, bank.U)
+    _want("idx", idx, torch.int32, bank.U * k_max)
+    _want("count", count, torch.int32, bank.U)
+    _want("rope", rope, torch.float32, mn * d, optional=True)
+    _want("status", status, torch.int32, 1)
+
+
+def rs3_block_select_workspace_bytes(U: int, H: int, k_max: int, n_blocks: int) -> int:
+    return int(lib.rs3_block_select_workspace_bytes(U, H, k_max, n_blocks))
+
+
+def rs3_block_select(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int,
+                     bank: "Bank", block: int, digest, step, rope, n_top: int, sel, workspace, status,
+                     stream=None):
+    """The n_top blocks whose digests score highest for each kept query and head:
+    sel int32 [U, H, k_max, n_top], ascending, -1 where there are fewer."""
+    _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    n = bank.U * bank.H * max(0, bank.blocks(block) if block > 0 else 0)
+    _want("digest", digest, torch.int8, n * bank.d)
+    _want("step", step, torch.float32, n)
+    _want("sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    rc = lib.rs3_block_select(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
+                              ctypes.byref(bank.desc), block, _ptr(digest), _ptr(step), _ptr(rope), n_top, _ptr(sel),
+                              _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
+    _check(rc, "rs3_block_select")
+
+
+def rs3_sparse_readout_workspace_bytes(U: int, H: int, d: int, k_max: int, n_top: int, n_blocks: int,
+                                       dtype: str) -> int:
+    return int(lib.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, n_blocks, DTYPES[dtype]))
+
+
+def rs3_sparse_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int,
+                       bank: "Bank", block: int, sel, n_top: int, rope, residual, out, scale: float,
+                       workspace, status, stream=None):
+    """rs3_memory_readout over the blocks that sel lists for each query and head."""
+    _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    _want("sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    _want("residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d, optional=True)
+    _want("out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    rc = lib.rs3_sparse_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count),
+                                k_max, ctypes.byref(bank.desc), block, _ptr(sel), n_top, _ptr(rope), _ptr(residual),
+                                _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status),
+                                _stream(stream))
+    _check(rc, "rs3_sparse_readout")
+
+
+# ---------------------------------------------------------------------------
+# query and key heads: RMS norm with the position rotation
+# ---------------------------------------------------------------------------
+
+def _rows_of(name: str, t: torch.Tensor, width: int):
+    """(rows, elements between rows) of a tensor [..., width] whose rows are evenly spaced."""
+    if t.dim() < 1 or t.shape[-1] != width or (width > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: rows of {width} adjacent elements wanted, got {tuple(t.shape)}")
+    rows, step, reach = 1, None, None
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n != 1 and rows != 0:
+            if step is None:
+                step, reach = st, st
+            if st != reach:
+                raise ValueError(f"{name}: its rows are not evenly spaced")
+            reach = st * n
+        rows *= n
+    return rows, (width if step is None else step)
+
+
+def rs3_qk_norm_rope(q, q_out, k, k_out, dtype: str, mn: int, Hq: int, Hk: int, d: int, q_weight=None,
+                     k_weight=None, eps: float = 1e-6, rope=None, q_keep=None, k_keep=None, stream=None):
+    """RMS norm of every head of q [..., Hq*d] and k [..., Hk*d] (either may be None),
+    rotated by the row's own cell, row r being cell r mod mn.  Rows may be evenly
+    spaced parts of a wider tensor; out may be the input."""
+    sides = []
+    for name, x, y, H, w, keep in (("q", q, q_out, Hq, q_weight, q_keep), ("k", k, k_out, Hk, k_weight, k_keep)):
+        if x is None and y is None:
+            sides += [None, 0, 0, 0, None, None, None, 0]
+            continue
+        for what, t in ((name, x), (name + "_out", y)):
+            _want(what, t, TORCH_DTYPES[dtype], 0)
+        (rows, stride), (rows_out, out_stride) = _rows_of(name, x, H * d), _rows_of(name + "_out", y, H * d)
+        if rows != rows_out:
+            raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
+        _want(name + "_weight", w, torch.float32, d, optional=True)
+        _want(name + "_keep", keep, torch.uint8, rows, optional=True)
+        sides += [ctypes.c_void_p(x.data_ptr()), rows, stride, H, _ptr(w), _ptr(keep), ctypes.c_void_p(y.data_ptr()),
+                  out_stride]
+    _want("rope", rope, torch.float32, mn * d, optional=True)
+    rc = lib.rs3_qk_norm_rope(*sides, DTYPES[dtype], mn, d, float(eps), _ptr(rope), _stream(stream))
+    _check(rc, "rs3_qk_norm_rope")
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,721 @@
+"""The calls for long banks against plain implementations in 64 bits: norms of query and
+key heads, copies of banks, block digests, block selection, and the readout over chosen blocks."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}              # a rounding to the stored type, relative
+
+
+@pytest.fixture(scope="module")
+def rs3():
+    from paper_2608_22526_gb300 import rs3
+    return rs3
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def status():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def rope_table(mn, d, seed=1):
+    a = torch.rand((mn, d // 2), generator=gen(seed), device="cuda", dtype=torch.float64) * 6.3
+    return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def turned(x, d, table):
+    """x [..., mn, D] in 64 bits with every head's pairs turned by their cell's angles."""
+    z = torch.view_as_complex(x.unflatten(-1, (-1, d // 2, 2)).contiguous())
+    return torch.view_as_real(z * torch.view_as_complex(table.double().contiguous())[:, None]).flatten(-3)
+
+
+# ---------------------------------------------------------------------------
+# norms
+# ---------------------------------------------------------------------------
+def norm_ref(x, d, w, table, mn, eps):
+    """(value, size of its terms) in 64 bits; x [rows, H*d]."""
+    h = x.double().unflatten(-1, (-1, d))
+    h = h / (h.square().mean(-1, keepdim=True) + eps).sqrt()
+    h = h * (1.0 if w is None else w.double())
+    y = h.flatten(-2)
+    if table is None:
+        return y, y.abs()
+    cell = torch.arange(x.shape[0], device="cuda") % mn
+    t = table.double()[cell]
+    p = h.unflatten(-1, (d // 2, 2))
+    c, s = t[:, None, :, 0], t[:, None, :, 1]
+    out = torch.stack([p[..., 0] * c - p[..., 1] * s, p[..., 0] * s + p[..., 1] * c], -1)
+    size = torch.stack([(p[..., 0] * c).abs() + (p[..., 1] * s).abs(), (p[..., 0] * s).abs() + (p[..., 1] * c).abs()], -1)
+    return out.flatten(-3), size.flatten(-3)
+
+
+def check_norm(got, ref, size, dtype):
+    # one rounding to the stored type, and in fp32: the sum of at most 256 squares (16 adds in a
+    # chain and a tree of five, 21 half-steps of 2^-24, half of it after the root), the mean, the
+    # reciprocal root (2 steps = 4 half-steps), three products and a sum: under 32 half-steps of the terms
+    tol = HALF[dtype] * ref.abs() + 32 * 2.0 ** -24 * size * (1 + HALF[dtype])
+    err = (got.double() - ref).abs()
+    assert (err <= tol + 1e-42).all(), float((err - tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 16, 24, 64, 80, 128, 248, 256])
+@pytest.mark.parametrize("rows,mn,Hq,Hk", [(1, 1, 1, 1), (1, 35, 3, 1), (35, 35, 2, 5), (3 * 35, 35, 1, 2), (71, 35, 4, 4)])
+def test_norm_matches_64_bits(rs3, dtype, d, rows, mn, Hq, Hk):
+    g = gen(d + rows)
+    q = (torch.randn((rows, Hq * d), generator=g, device="cuda") * 3).to(DT[dtype])
+    k = torch.randn((2 * rows, Hk * d), generator=g, device="cuda").to(DT[dtype])
+    w = [1 + torch.randn(d, generator=g, device="cuda") * 0.3, None]
+    table = rope_table(mn, d) if rows % 2 else None
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    rs3.rs3_qk_norm_rope(q, qo, k, ko, dtype, mn, Hq, Hk, d, w[0], w[1], 1e-5, table)
+    check_norm(qo, *norm_ref(q, d, w[0], table, mn, 1e-5), dtype)
+    check_norm(ko, *norm_ref(k, d, w[1], table, mn, 1e-5), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_packed_in_place_with_masks(rs3, dtype):
+    """Queries, keys and values side by side; in place; rows that the mask leaves hold NaN."""
+    G, mn, H, d = 3, 20, 2, 64
+    x = torch.randn((G, mn, 3 * H * d), generator=gen(5), device="cuda").to(DT[dtype])
+    keep = (torch.rand((G, mn), generator=gen(6), device="cuda") < 0.5).to(torch.uint8)
+    keep[1] = 0                                            # a grid without any kept row
+    x[keep == 0, H * d:2 * H * d] = math.nan
+    before = x.clone()
+    q, k = x[..., :H * d], x[..., H * d:2 * H * d]
+    table = rope_table(mn, d)
+    rs3.rs3_qk_norm_rope(q, q, k, k, dtype, mn, H, H, d, eps=1e-6, rope=table, k_keep=keep)
+    flat = before.view(-1, 3 * H * d)
+    check_norm(q.reshape(-1, H * d), *norm_ref(flat[:, :H * d], d, None, table, mn, 1e-6), dtype)
+    on = keep.view(-1) != 0
+    ref, size = norm_ref(flat[:, H * d:2 * H * d], d, None, table, mn, 1e-6)
+    check_norm(k.reshape(-1, H * d)[on], ref[on], size[on], dtype)
+    same = torch.ones_like(x, dtype=torch.bool)
+    same[..., :H * d] = False
+    same[..., H * d:2 * H * d] = (keep == 0)[..., None]
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(x.view(bits)[same], before.view(bits)[same])
+
+
+def test_norm_one_side_zero_rows_and_zero_heads(rs3):
+    x = torch.zeros((4, 64), device="cuda")
+    x[1:] = torch.randn((3, 64), generator=gen(1), device="cuda") * 1e-3
+    y = torch.full_like(x, 7.0)
+    rs3.rs3_qk_norm_rope(None, None, x, y, "f32", 2, 0, 1, 64, eps=1e-6)
+    assert torch.equal(y[0], torch.zeros(64, device="cuda"))     # a head of zeros
+    check_norm(y, *norm_ref(x, 64, None, None, 2, 1e-6), "f32")
+    e = x[:0]
+    rs3.rs3_qk_norm_rope(e, e, x, y, "f32", 2, 1, 1, 64)
+    with pytest.raises(ValueError):
+        rs3.rs3_qk_norm_rope(x, y[:3], None, None, "f32", 2, 1, 1, 64)
+    with pytest.raises(ValueError):
+        rs3.rs3_qk_norm_rope(x.bfloat16(), y, None, None, "f32", 2, 1, 1, 64)
+
+
+# ---------------------------------------------------------------------------
+# banks with known contents
+# ---------------------------------------------------------------------------
+class Built:
+    """A bank filled through commits, and its logical rows as read back from its counters."""
+
+    def __init__(self, rs3, U=3, H=2, d=16, dtype="bf16", m=5, n=7, n_cond=1, window=3, ring_frames=3, commits=5, n_ptr=4, seed=0,
+                 density=0.5, empty=(), ring=None, scale=1.0):
+        self.rs3, self.U, self.H, self.d, self.D, self.dtype, self.mn = rs3, U, H, d, H * d, dtype, m * n
+        g = gen(seed)
+        ring = (window * self.mn if window > 0 else ring_frames * self.mn) if ring is None else ring
+        self.bank = rs3.Bank(U, H, d, dtype, self.mn, n_cond, window, ring, window if window > 0 else ring_frames, n_ptr)
+        # rows that are not live hold NaN: nothing may come of them
+        self.bank.k_store.fill_(math.nan)
+        self.bank.v_store.fill_(math.nan)
+        self.st = status()
+        for f in range(n_cond + commits):
+            self.commit(g, int(f < n_cond), density, empty, scale)
+        if n_ptr:
+            kp, vp = (torch.randn((U, n_ptr, self.D), generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+            rs3.rs3_bank_set_pointers(self.bank, kp, vp, self.st)
+        assert int(self.st) == 0
+
+    def commit(self, g, is_cond=0, density=0.5, empty=(), scale=1.0):
+        shape = (self.U, self.mn, self.D)
+        k, v = (torch.randn(shape, generator=g, device="cuda") * s for s in (scale, 1.0))
+        mask = (torch.rand(shape[:2], generator=g, device="cuda") < density).to(torch.uint8)
+        for u in empty:
+            mask[u] = 0
+        self.rs3.rs3_bank_commit(self.bank, k.to(DT[self.dtype]), v.to(DT[self.dtype]), mask, is_cond, self.st)
+
+    def places(self, u, bank=None):
+        """Storage rows of unit u in logical order, and its frames' lengths."""
+        bank = self.bank if bank is None else bank
+        meta, frames = self.rs3.rs3_bank_read_meta(bank)
+        head, tail, cond, nf, _, _, ptr, length = meta[u]
+        ring = [bank.pinned_cap + p % max(1, bank.ring_cap) for p in range(head, tail)]
+        rows = list(range(cond)) + ring + [bank.pinned_cap + bank.ring_cap + i for i in range(ptr)]
+        assert len(rows) == length
+        lens = [int(x) for x in frames[u, :nf, 1]]
+        assert sum(lens) == tail - head and [int(x) for x in frames[u, :nf, 0]] == list(head + np.cumsum([0] + lens[:-1]))[:nf]
+        return np.array(rows, dtype=np.int64), lens, (int(cond), int(tail - head), int(ptr))
+
+
+def rows_of(bank, u, rows):
+    i = torch.from_numpy(rows).cuda()
+    return bank.k_store[u][i], bank.v_store[u][i]
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+
+# ---------------------------------------------------------------------------
+# copies
+# ---------------------------------------------------------------------------
+LAYOUTS = [dict(window=3, commits=5), dict(window=3, commits=2), dict(window=-1, ring_frames=9, commits=8),
+           dict(window=2, commits=4, n_cond=0, n_ptr=0), dict(window=1, commits=0, n_cond=2), dict(window=-1, ring_frames=400, commits=330, m=2, n=3)]
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("keep", [None, 0.0, 0.4, 1.0])
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 1, 8), ("f32", 3, 20)])
+def test_copy_takes_the_kept_rows(rs3, layout, keep, dtype, H, d):
+    s = Built(rs3, U=4, H=H, d=d, dtype=dtype, empty=(2,), seed=3, **layout)
+    t = Built(rs3, U=5, H=H, d=d, dtype=dtype, seed=4, **layout)
+    parent = [3, -1, 0, 3, 2]
+    before_k, before_v = t.bank.k_store.clone(), t.bank.v_store.clone()
+    meta0, _ = rs3.rs3_bank_read_meta(t.bank)
+    most = max(len(s.places(u)[0]) for u in range(4))
+    mask = None
+    if keep is not None:
+        mask = (torch.rand((5, most + 3), generator=gen(9), device="cuda") < keep).to(torch.uint8) * 3
+    st = status()
+    ws = torch.full((rs3.rs3_bank_copy_workspace_bytes(5, most + 3),), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(2):                                     # the second call finds the first's workspace and counters
+        rs3.rs3_bank_copy(t.bank, s.bank, torch.tensor(parent, dtype=torch.int32, device="cuda"), mask, ws, st)
+    assert int(st) == 0
+    meta, _ = rs3.rs3_bank_read_meta(t.bank)
+    assert np.array_equal(meta[1], meta0[1])
+    for u, p in enumerate(parent):
+        if p < 0:
+            assert torch.equal(bits(t.bank.k_store[u]), bits(before_k[u])) and torch.equal(bits(t.bank.v_store[u]), bits(before_v[u]))
+            continue
+        rows, lens, (cond, ring, ptr) = s.places(p)
+        on = np.ones(len(rows), bool) if mask is None else mask[u, :len(rows)].cpu().numpy() != 0
+        got, got_lens, got_n = t.places(u)
+        want_n = (int(on[:cond].sum()), int(on[cond:cond + ring].sum()), int(on[cond + ring:].sum()))
+        assert got_n == want_n
+        ends = cond + np.cumsum([0] + lens)
+        assert got_lens == [int(on[a:b].sum()) for a, b in zip(ends[:-1], ends[1:])]
+        assert meta[u, 0] == 0 and meta[u, 5] == rs3.rs3_bank_read_meta(s.bank)[0][p, 5]
+        for a, b, old in zip(rows_of(s.bank, p, rows[on]), rows_of(t.bank, u, got), (before_k, before_v)):
+            assert torch.equal(bits(a), bits(b))
+        other = np.setdiff1d(np.arange(t.bank.rows_per_unit), got)
+        assert torch.equal(bits(t.bank.k_store[u][other]), bits(before_k[u][other]))
+    # the copy takes commits and drops as any bank does
+    t.commit(gen(11))
+    if layout["window"] > 0:
+        assert int(t.st) == 0
+    [t.places(u) for u in range(5)]
+
+
+def test_copy_into_a_larger_ring_and_what_does_not_fit(rs3):
+    s = Built(rs3, window=-1, ring_frames=6, commits=6, density=1.0, seed=1)
+    big = rs3.Bank(3, s.H, s.d, s.dtype, s.mn, 2, -1, 20 * s.mn, 30, 9)
+    st = status()
+    same = torch.arange(3, dtype=torch.int32, device="cuda")
+    rs3.rs3_bank_copy(big, s.bank, same, None, None, st)
+    assert int(st) == 0
+    for u in range(3):
+        a, b = rows_of(s.bank, u, s.places(u)[0]), rows_of(big, u, s.places(u, big)[0])
+        assert torch.equal(bits(a[0]), bits(b[0])) and torch.equal(bits(a[1]), bits(b[1]))
+    for over in (dict(n_cond=0), dict(ring=5 * s.mn), dict(max_frames=5), dict(n_ptr=3)):
+        a = dict(n_cond=2, ring=20 * s.mn, max_frames=30, n_ptr=9)
+        a.update(over)
+        small = rs3.Bank(3, s.H, s.d, s.dtype, s.mn, a["n_cond"], -1, a["ring"], a["max_frames"], a["n_ptr"])
+        for keep in (None, torch.ones((3, 7 * s.mn + 4), dtype=torch.uint8, device="cuda")):
+            st = status()
+            ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(3, 7 * s.mn + 4), dtype=torch.uint8, device="cuda")
+            rs3.rs3_bank_copy(small, s.bank, same, keep, ws, st)
+            assert int(st) == rs3.RS3_ECAPACITY, over
+            assert (rs3.rs3_bank_read_meta(small)[0] == 0).all() and not small.k_store.any()
+    # rows that are left fit again
+    keep = torch.zeros((3, 7 * s.mn + 4), dtype=torch.uint8, device="cuda")
+    keep[:, s.mn:3 * s.mn + 1] = 1
+    small = rs3.Bank(3, s.H, s.d, s.dtype, s.mn, 1, -1, 2 * s.mn + 1, 6, 4)
+    st = status()
+    rs3.rs3_bank_copy(small, s.bank, same, keep, ws, st)
+    assert int(st) == 0 and s.places(0, small)[1] == [s.mn, s.mn, 1, 0, 0, 0]
+
+
+def test_copy_refuses_units_on_the_device(rs3):
+    s = Built(rs3, seed=2)
+    t = Built(rs3, seed=5)
+    length = max(len(s.places(u)[0]) for u in range(3))
+
+    def run(dst, parent, keep=None):
+        st = status()
+        stride = 1 if keep is None else keep.shape[1]
+        ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(3, stride), dtype=torch.uint8, device="cuda")
+        m0 = rs3.rs3_bank_read_meta(dst.bank)[0]
+        rs3.rs3_bank_copy(dst.bank, s.bank, torch.tensor(parent, dtype=torch.int32, device="cuda"), keep, ws, st)
+        m1 = rs3.rs3_bank_read_meta(dst.bank)[0]
+        return int(st), [bool((m0[u] == m1[u]).all()) for u in range(3)]
+
+    assert run(t, [3, -1, -1]) == (rs3.RS3_EINVAL, [True] * 3)
+    assert run(t, [-2, -1, -1]) == (rs3.RS3_EINVAL, [True] * 3)
+    code, same = run(t, [5, 1, 1])
+    assert code == rs3.RS3_EINVAL and same[0] and not same[1] and not same[2]      # the others proceed
+    short = torch.ones((3, length - 1), dtype=torch.uint8, device="cuda")
+    assert run(t, [0, 1, 2], short)[0] == rs3.RS3_EINVAL
+    # one bank: a source stays as it is
+    assert run(s, [0, 1, 2])[0] == 0
+    assert run(s, [1, 2, -1])[0] == rs3.RS3_EINVAL
+    ones = torch.ones((3, length), dtype=torch.uint8, device="cuda")
+    assert run(s, [0, -1, -1], ones)[0] == rs3.RS3_EINVAL
+    s = Built(rs3, seed=2)
+    want = [rows_of(s.bank, 0, s.places(0)[0])[i].clone() for i in range(2)]
+    assert run(s, [-1, 0, 0]) == (0, [True, False, False])
+    for u in range(3):
+        got = rows_of(s.bank, u, s.places(u)[0])
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("layout", LAYOUTS[:5])
+def test_drop_frames(rs3, layout):
+    s = Built(rs3, seed=7, **layout)
+    before = [s.places(u) for u in range(3)]
+    nf = [len(x[1]) for x in before]
+    old, new = [min(1, n) for n in nf], [max(0, n - 2) for n in nf]
+    old[2], new[2] = nf[2], 0                              # all of them
+    st = status()
+    rs3.rs3_bank_drop_frames(s.bank, torch.tensor(old, dtype=torch.int32, device="cuda"),
+                             torch.tensor(new, dtype=torch.int32, device="cuda"), st)
+    assert int(st) == 0
+    for u in range(3):
+        rows, lens, (cond, ring, ptr) = before[u]
+        a, b = sum(lens[:old[u]]), sum(lens[nf[u] - new[u]:])
+        got, got_lens, _ = s.places(u)
+        assert got_lens == lens[old[u]:nf[u] - new[u]]
+        assert np.array_equal(got, np.concatenate([rows[:cond], rows[cond + a:cond + ring - b], rows[cond + ring:]]))
+    s.commit(gen(8))
+    assert int(s.st) == 0
+    [s.places(u) for u in range(3)]
+    meta = rs3.rs3_bank_read_meta(s.bank)[0]
+    for bad in ([-1, 0, 0], [99, 0, 0]):
+        for side in (0, 1):
+            st = status()
+            arg = [None, None]
+            arg[side] = torch.tensor(bad, dtype=torch.int32, device="cuda")
+            rs3.rs3_bank_drop_frames(s.bank, *arg, st)
+            assert int(st) == rs3.RS3_EINVAL
+    assert np.array_equal(meta, rs3.rs3_bank_read_meta(s.bank)[0])
+
+
+# ---------------------------------------------------------------------------
+# digests
+# ---------------------------------------------------------------------------
+def eight_bits(x):
+    """[..., d] fp32 on the CPU -> whole numbers, steps (np.float32)."""
+    a = np.abs(x).max(-1)
+    e = np.frexp(a)[1] - 1
+    some = a >= np.float32(2.0 ** -100)
+    t = np.clip(np.rint(np.ldexp(x.astype(np.float64), (6 - e)[..., None])), -127, 127)
+    return np.where(some[..., None], t, 0), np.where(some, np.ldexp(1.0, e - 6), 0.0)
+
+
+def digest_ref(b, u, bs, nb):
+    rows = b.places(u)[0]
+    k = b.bank.k_store[u].float().cpu().numpy()
+    x = np.zeros((nb * bs, b.D), np.float32)
+    x[rows] = k[rows]
+    n = np.bincount(rows // bs, minlength=nb)
+    x = x.reshape(nb, bs // 8, 8, b.D)
+    p = x[:, 0].copy()
+    for i in range(1, bs // 8):
+        p = p + x[:, i]
+    s = ((p[:, 0] + p[:, 4]) + (p[:, 2] + p[:, 6])) + ((p[:, 1] + p[:, 5]) + (p[:, 3] + p[:, 7]))
+    mean = (s / np.maximum(n, 1)[:, None].astype(np.float32)).reshape(nb, b.H, b.d)
+    t, step = eight_bits(mean)
+    return t.transpose(1, 0, 2), step.T, n
+
+
+def make_digest(b, block, fill=None):
+    nb = b.bank.blocks(block)
+    dig = torch.full((b.U, b.H, nb, b.d), 77, dtype=torch.int8, device="cuda")
+    step = torch.full((b.U, b.H, nb), 0.5, device="cuda")
+    return dig, step, nb
+
+
+HEADS = [("bf16", 1, 16), ("bf16", 5, 64), ("bf16", 3, 256), ("f32", 1, 32), ("f32", 3, 64), ("f32", 2, 256), ("f32", 3, 16)]
+
+
+@pytest.mark.parametrize("dtype,H,d", HEADS)
+@pytest.mark.parametrize("block", [32, 64, 128])
+def test_digest_of_all_blocks(rs3, dtype, H, d, block):
+    b = Built(rs3, H=H, d=d, dtype=dtype, m=9, n=11, window=3, commits=5, empty=(1,), seed=block)
+    b.bank.k_store[0, :block] *= 1e-36 if dtype == "f32" else 1.0      # a block below 2^-100
+    dig, step, nb = make_digest(b, block)
+    rs3.rs3_bank_digest(b.bank, block, -1, dig, step, b.st)
+    assert int(b.st) == 0
+    for u in range(b.U):
+        t, s, n = digest_ref(b, u, block, nb)
+        assert np.array_equal(step[u].cpu().numpy(), s.astype(np.float32))
+        assert np.array_equal(dig[u].cpu().numpy(), t.astype(np.int8))
+        assert (s[:, n == 0] == 0).all()
+
+
+@pytest.mark.parametrize("window,n_ptr", [(3, 4), (-1, 0), (2, 5)])
+@pytest.mark.parametrize("block", [32, 64])
+def test_digest_refresh_follows_commits_and_drops(rs3, window, n_ptr, block):
+    """After every commit refresh = 1, after a drop refresh = 0: every block with a live row is up to date."""
+    b = Built(rs3, m=6, n=7, window=window, ring_frames=12, commits=1, n_ptr=n_ptr, seed=13)
+    dig, step, nb = make_digest(b, block)
+    rs3.rs3_bank_digest(b.bank, block, -1, dig, step, b.st)
+    g = gen(17)
+
+    def same():
+        for u in range(b.U):
+            t, s, n = digest_ref(b, u, block, nb)
+            on = n > 0
+            assert np.array_equal(step[u].cpu().numpy()[:, on], s.astype(np.float32)[:, on])
+            assert np.array_equal(dig[u].cpu().numpy()[:, on], t.astype(np.int8)[:, on])
+
+    for i in range(9):
+        b.commit(g, density=[0.5, 1.0, 0.1][i % 3], empty=(i % 3,))
+        rs3.rs3_bank_digest(b.bank, block, 1, dig, step, b.st)
+        same()
+        if i % 3 == 2:
+            one = torch.ones(3, dtype=torch.int32, device="cuda")
+            rs3.rs3_bank_drop_frames(b.bank, one, None, b.st)
+            rs3.rs3_bank_digest(b.bank, block, 0, dig, step, b.st)
+            same()
+            rs3.rs3_bank_drop_frames(b.bank, None, one, b.st)
+            rs3.rs3_bank_digest(b.bank, block, 0, dig, step, b.st)
+            same()
+            b.commit(g)
+            b.commit(g)
+            rs3.rs3_bank_digest(b.bank, block, 2, dig, step, b.st)
+            same()
+    assert int(b.st) == 0
+
+
+# ---------------------------------------------------------------------------
+# selection
+# ---------------------------------------------------------------------------
+def queries(b, G, k_max, counts, seed=21, scale=1.0):
+    g = gen(seed)
+    q = (torch.randn((G, b.mn, b.D), generator=g, device="cuda") * scale).to(DT[b.dtype])
+    idx = torch.full((b.U, max(1, k_max)), -9, dtype=torch.int32, device="cuda")
+    for u, n in enumerate(counts):
+        idx[u, :n] = torch.randperm(b.mn, generator=g, device="cuda")[:n].sort().values.to(torch.int32)
+    group = torch.arange(b.U, dtype=torch.int32, device="cuda") % G
+    return q, idx[:, :k_max].contiguous(), torch.tensor(counts, dtype=torch.int32, device="cuda"), group
+
+
+def select_ref(b, q, idx, counts, group, dig, step, table, block, nb, n_top, sel):
+    sel = sel.copy()
+    qf = q.float().cpu().numpy()
+    if table is not None:
+        t = table.cpu().numpy()
+        p = qf.reshape(qf.shape[0], b.mn, b.H, b.d // 2, 2)
+        c, s = t[:, None, :, 0], t[:, None, :, 1]
+        qf = np.stack([p[..., 0] * c - p[..., 1] * s, p[..., 0] * s + p[..., 1] * c], -1).astype(np.float32).reshape(qf.shape)
+    dig, step = dig.cpu().numpy().astype(np.int64), step.cpu().numpy().astype(np.float64)
+    for u, n in enumerate(counts):
+        live = np.bincount(b.places(u)[0] // block, minlength=nb) > 0
+        for j in range(n):
+            x = qf[int(group[u]), int(idx[u, j])].reshape(b.H, b.d)
+            tq, _ = eight_bits(x)
+            for h in range(b.H):
+                score = (dig[u, h] @ tq[h].astype(np.int64)) * step[u, h]
+                order = [i for i in np.argsort(-score, kind="stable") if live[i]][:n_top]
+                sel[u, h, j] = sorted(order) + [-1] * (n_top - len(order))
+    return sel
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 1, 16), ("bf16", 3, 64), ("bf16", 2, 256), ("bf16", 1, 128), ("bf16", 4, 32), ("f32", 2, 64),
+                                       ("f32", 1, 256), ("f32", 3, 16)])
+@pytest.mark.parametrize("n_top,block,commits,rope", [(1, 32, 9, False), (5, 32, 40, True), (16, 64, 40, False), (200, 32, 9, True)])
+def test_select_is_exact(rs3, dtype, H, d, n_top, block, commits, rope):
+    b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=8, n=9, window=-1, ring_frames=commits, commits=commits, empty=(1,), n_ptr=0, n_cond=1,
+              seed=n_top, ring=commits * 50)
+    dig, step, nb = make_digest(b, block)
+    rs3.rs3_bank_digest(b.bank, block, -1, dig, step, b.st)
+    counts = [21, 5, 0]
+    q, idx, count, group = queries(b, 2, 21, counts)
+    table = rope_table(b.mn, d) if rope else None
+    q[1] = 0                                               # scores all zero: ties everywhere
+    sel = torch.full((b.U, H, 21, n_top), -5, dtype=torch.int32, device="cuda")
+    want = select_ref(b, q, idx, counts, group, dig, step, table, block, nb, n_top, sel.cpu().numpy())
+    ws = torch.full((rs3.rs3_block_select_workspace_bytes(b.U, H, 21, nb),), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        rs3.rs3_block_select(q, dtype, 2, b.mn, H, d, group, idx, count, 21, b.bank, block, dig, step, table, n_top, sel, ws, b.st)
+        assert int(b.st) == 0
+        assert np.array_equal(sel.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("rows,n_top,block", [(70_000, 32, 64), (260_000, 7, 32), (400_000, 64, 32), (49_152 * 32 - 64, 3, 32), (300, 1024, 32)])
+def test_select_over_many_blocks(rs3, rows, n_top, block):
+    """Thousands of blocks, digests and steps given: few different scores, so most choices are ties."""
+    d, H, mn = 16, 1, 64
+    bank = rs3.Bank(1, H, d, "bf16", mn, 1, -1, rows, 4, 0)
+    st = status()
+    k = torch.randn((1, mn, d), generator=gen(1), device="cuda").bfloat16()
+    rs3.rs3_bank_commit(bank, k, k, None, 1, st)
+    bank.counters[0, 1] = rows - 100                       # as if the ring had been filled
+    nb = bank.blocks(block)
+    g = gen(2)
+    dig = torch.randint(-3, 4, (1, H, nb, d), generator=g, device="cuda").to(torch.int8)
+    step = torch.randint(1, 3, (1, H, nb), generator=g, device="cuda").float() / 64
+    q = torch.randint(-2, 3, (1, mn, d), generator=g, device="cuda").bfloat16()
+    q[..., 0] = 2                                          # every query has the same step: t = 32 q
+    n = 20
+    idx = torch.arange(n, dtype=torch.int32, device="cuda").view(1, n)
+    sel = torch.full((1, H, n, n_top), -5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(1, H, n, nb), dtype=torch.uint8, device="cuda")
+    one = torch.tensor([n], dtype=torch.int32, device="cuda")
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rs3.rs3_block_select(q, "bf16", 1, mn, H, d, zero, idx, one, n, bank, block, dig, step, None, n_top, sel, ws, st)
+    assert int(st) == 0
+    score = (q[0, :n].double() @ dig[0, 0].double().T) * step[0, 0].double()
+    live = torch.arange(nb, device="cuda") * block < mn + rows - 100
+    score[:, ~live] = -math.inf
+    order = score.argsort(dim=1, descending=True, stable=True)[:, :n_top]
+    m = min(n_top, int(live.sum()))
+    want = torch.full((n, n_top), -1, device="cuda", dtype=torch.int32)
+    want[:, :m] = order[:, :m].sort(1).values.to(torch.int32)
+    assert torch.equal(sel[0, 0], want)
+
+
+# ---------------------------------------------------------------------------
+# the readout over chosen blocks
+# ---------------------------------------------------------------------------
+def readout_ref(b, q, idx, counts, group, sel, table, block, scale, res, out0):
+    """(out, tolerance) in 64 bits: out starts as out0 outside the kept cells."""
+    bf = b.dtype == "bf16"
+    half = HALF[b.dtype]
+    out = (out0 if res is None else res).double().clone()
+    tol = torch.zeros_like(out)
+    qd = q.double()
+    if table is not None:
+        qd = turned(qd, b.d, table)
+    for u, n in enumerate(counts):
+        rows = torch.from_numpy(b.places(u)[0]).cuda()
+        k, v = (x[u][rows].double() for x in (b.bank.k_store, b.bank.v_store))
+        blk = rows // block
+        for j in range(n):
+            cell = int(idx[u, j])
+            for h in range(b.H):
+                col = slice(h * b.d, (h + 1) * b.d)
+                times = torch.zeros(b.bank.blocks(block), device="cuda", dtype=torch.float64)
+                for e in sel[u, h, j].tolist():
+                    if 0 <= e < times.numel():
+                        times[e] += 1
+                w = times[blk] if rows.numel() else times[:0]
+                A = torch.zeros(b.d, device="cuda", dtype=torch.float64)
+                size = A.clone()
+                s_abs = 0.0
+                if float(w.sum()) > 0:
+                    x = k[:, col] @ qd[int(group[u]), cell, col] * scale
+                    x[w == 0] = -math.inf
+                    p = torch.exp(x - x.max()) * w
+                    p = p / p.sum()
+                    A, size = p @ v[:, col], p @ v[:, col].abs()
+                    s_abs = float(((k[:, col].abs() @ qd[int(group[u]), cell, col].abs()) * scale)[w > 0].max())
+                r = torch.zeros_like(A) if res is None else res[u, cell, col].double()
+                out[u, cell, col] = r + A
+                # fp32 sums of scores, weights and values: under 300 half-steps; bf16: the weights are rounded
+                # once (2^-8 of each), a rotated query too (its scores off by 2^-8 of their terms, a weight by
+                # twice that beside its neighbours), and the result
+                e_s = s_abs * (2.0 ** -24 * 300 + (half if bf and table is not None else 0.0))
+                tol[u, cell, col] = half * (r + A).abs() + size * (math.expm1(2 * e_s) + 300 * 2.0 ** -24 + (half if bf else 0.0)) * 1.01 + 1e-30
+    return out, tol
+
+
+def run_readout(rs3, b, q, idx, count, group, sel, table, block, scale, res, out, G):
+    nb, k_max, n_top = b.bank.blocks(block), sel.shape[2], sel.shape[3]
+    ws = torch.full((rs3.rs3_sparse_readout_workspace_bytes(b.U, b.H, b.d, k_max, n_top, nb, b.dtype),), 255, dtype=torch.uint8,
+                    device="cuda")
+    rs3.rs3_sparse_readout(q, b.dtype, G, b.mn, b.H, b.d, group, idx, count, k_max, b.bank, block, sel, n_top, table, res, out, scale,
+                           ws, b.st)
+    return ws
+
+
+SHAPES = [("bf16", 1, 16), ("bf16", 2, 32), ("bf16", 3, 64), ("bf16", 2, 128), ("bf16", 1, 256), ("f32", 2, 16), ("f32", 3, 64),
+          ("f32", 1, 128), ("f32", 2, 256)]
+
+
+@pytest.mark.parametrize("dtype,H,d", SHAPES)
+@pytest.mark.parametrize("n_top,block,residual,rope", [(1, 32, "none", False), (4, 64, "inplace", True), (7, 32, "other", False),
+                                                       (3, 128, "inplace", False)])
+@pytest.mark.parametrize("counts", [[1, 0, 3], [40, 17, 33]])
+def test_sparse_readout_matches_64_bits(rs3, dtype, H, d, n_top, block, residual, rope, counts):
+    """Lists with gaps, a unit without rows, wrapped rings, blocks across region ends, NaN in dead rows."""
+    b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=8, n=9, window=4, commits=7, n_ptr=5, empty=(1,), seed=n_top, scale=1.5)
+    if counts[1]:
+        rs3.rs3_bank_reset(b.bank, 1)                      # unit 1: not even pointers
+    nb = b.bank.blocks(block)
+    q, idx, count, group = queries(b, 2, 40, counts, scale=1.2)
+    g = gen(31)
+    sel = torch.rand((b.U, H, 40, nb), generator=g, device="cuda").argsort(-1)[..., :n_top].to(torch.int32)
+    if sel.shape[-1] < n_top:
+        sel = torch.nn.functional.pad(sel, (0, n_top - sel.shape[-1]), value=-1)
+    sel = torch.where(torch.rand(sel.shape, generator=g, device="cuda") < 0.2, -1, sel).contiguous()
+    sel[0, :, 0] = -1                                      # a query without blocks
+    table = rope_table(b.mn, d) if rope else None
+    x = torch.randn((b.U, b.mn, b.D), generator=g, device="cuda").to(DT[dtype])
+    res = None if residual == "none" else x.clone()
+    out = res if residual == "inplace" else torch.full_like(x, math.nan)
+    want, tol = readout_ref(b, q, idx, counts, group, sel, table, block, 0.11 if rope else d ** -0.5, None if res is None else x,
+                            torch.zeros_like(x))
+    run_readout(rs3, b, q, idx, count, group, sel, table, block, 0.11 if rope else 0.0, res, out, 2)
+    assert int(b.st) == 0
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 256), ("f32", 1, 64)])
+@pytest.mark.parametrize("same_blocks", [False, True])
+def test_sparse_readout_over_all_blocks_is_the_memory_readout(rs3, dtype, H, d, same_blocks):
+    """Many queries, every block listed: what rs3_memory_readout gives, within both calls' roundings."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=20, n=20, window=-1, ring_frames=6, commits=6, n_ptr=3, seed=5)
+    k_max = 400
+    q, idx, count, group = queries(b, 1, k_max, [400, 131])
+    nb = b.bank.blocks(64)
+    if same_blocks:
+        sel = torch.arange(nb, dtype=torch.int32, device="cuda").expand(2, H, k_max, nb).contiguous()
+    else:
+        sel = torch.rand((2, H, k_max, nb), generator=gen(1), device="cuda").argsort(-1).to(torch.int32)
+    outs = [torch.zeros((2, b.mn, b.D), dtype=DT[dtype], device="cuda") for _ in range(2)]
+    run_readout(rs3, b, q, idx, count, group, sel, None, 64, 0.0, None, outs[0], 1)
+    ws = torch.empty(rs3.rs3_readout_workspace_bytes(2, H, d, k_max, dtype), dtype=torch.uint8, device="cuda")
+    b.bank.k_store.nan_to_num_(0)
+    b.bank.v_store.nan_to_num_(0)
+    rs3.rs3_memory_readout(q, dtype, 1, b.mn, H, d, group, idx, count, k_max, b.bank, None, None, outs[1], 0.0, ws, b.st)
+    assert int(b.st) == 0
+    # |A| <= sum p |v| <= max |v|: two roundings of the weights and two of the result (bf16), fp32 sums of scores
+    vmax = float(b.bank.v_store.float().abs().max())
+    tol = vmax * (4 * 2.0 ** -8 if dtype == "bf16" else 2.0 ** -14)
+    assert float((outs[0].float() - outs[1].float()).abs().max()) <= tol
+
+
+def test_one_block_chosen_by_everybody_and_scores_far_apart(rs3):
+    """Skewed lists, and scores so far apart that all but one weight vanish."""
+    b = Built(rs3, U=1, H=1, d=64, dtype="bf16", m=20, n=20, window=-1, ring_frames=8, commits=8, n_ptr=0, density=0.9, seed=6, scale=6.0)
+    q, idx, count, group = queries(b, 1, 300, [300], scale=6.0)
+    sel = torch.full((1, 1, 300, 3), -1, dtype=torch.int32, device="cuda")
+    sel[..., 0] = 2
+    sel[:, :, ::7, 1] = 11
+    out = torch.zeros((1, b.mn, 64), dtype=torch.bfloat16, device="cuda")
+    want, tol = readout_ref(b, q, idx, [300], group, sel, None, 64, 1.0, None, torch.zeros_like(out))
+    run_readout(rs3, b, q, idx, count, group, sel, None, 64, 1.0, None, out, 1)
+    err = (out.double() - want).abs()
+    assert int(b.st) == 0 and (err <= tol).all(), float((err - tol).max())
+
+
+def test_sparse_calls_latch_what_the_device_finds(rs3):
+    b = Built(rs3, U=3, H=1, d=64, m=8, n=8, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
+    nb = b.bank.blocks(32)
+    dig, step, _ = make_digest(b, 32)
+    rs3.rs3_bank_digest(b.bank, 32, -1, dig, step, b.st)
+    q, idx, count, group = queries(b, 1, 10, [10, 10, 10])
+    group.zero_()
+    sel0 = torch.zeros((3, 1, 10, 2), dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(3, 1, 10, nb), dtype=torch.uint8, device="cuda")
+
+    def both(idx=idx, count=count, group=group, sel=sel0):
+        codes = []
+        st, s = status(), torch.full_like(sel0, -5)
+        rs3.rs3_block_select(q, "bf16", 1, b.mn, 1, 64, group, idx, count, 10, b.bank, 32, dig, step, None, 2, s, ws, st)
+        codes.append(int(st))
+        b.st.zero_()
+        out = torch.zeros((3, b.mn, 64), dtype=torch.bfloat16, device="cuda")
+        run_readout(rs3, b, q, idx, count, group, sel, None, 32, 0.0, None, out, 1)
+        codes.append(int(b.st))
+        return codes, s, out
+
+    codes, s, good = both()
+    assert codes == [0, 0] and (s >= 0).all()
+    E = rs3.RS3_EINVAL
+    for bad in (-1, 11):
+        c = count.clone()
+        c[1] = bad
+        codes, s, out = both(count=c)
+        assert codes == [E, E] and (s[1] == -5).all() and not out[1].any()
+        assert torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+    for bad in (-1, 1):
+        gr = group.clone()
+        gr[2] = bad
+        codes, s, out = both(group=gr)
+        assert codes == [E, E] and (s[2] == -5).all() and not out[2].any() and torch.equal(out[0], good[0])
+    for bad in (-1, b.mn):
+        i = idx.clone()
+        i[0, 3] = bad
+        codes, s, out = both(idx=i)
+        assert codes == [E, E] and torch.equal(out[1], good[1])
+    for bad in (nb, 1 << 30):
+        sel = sel0.clone()
+        sel[0, 0, 4, 1] = bad
+        codes, _, out = both(sel=sel)
+        assert codes == [0, E] and torch.equal(out[1], good[1])
+        sel[0, 0, 4, 1] = -1
+        assert torch.equal(out, both(sel=sel)[2])
+
+
+def test_reading_a_long_bank_frame_by_frame(rs3):
+    """Norm, commit, digest, select and readout as a frame makes them, captured in a graph on a stream of its own, then a
+    branch: the fork reads as its parent did."""
+    from paper_2608_22526_gb300 import synth
+    from paper_2608_22526_gb300.pipeline import Pipeline
+    w = synth.Workload("t", 0, 12, 12, 2, 64, "bf16", 1, 2, 6, 0.2, 0.4, 1, -1, 0)
+    pipe = Pipeline(w, ring_cap=20 * w.mn)
+    pipe.use_blocks(32, 3)
+    g = gen(3)
+    mask = torch.zeros((2, w.mn), dtype=torch.uint8, device="cuda")
+    mask[:, 30:90] = 1
+    z = torch.randn((1, w.mn, w.D), generator=g, device="cuda").bfloat16()
+    kv = [torch.randn((2, w.mn, w.D), generator=g, device="cuda").bfloat16() for _ in range(2)]
+    table = rope_table(w.mn, 64)
+    qn, kn = torch.zeros_like(z), torch.zeros_like(kv[0])
+    x = torch.zeros((2, w.mn, w.D), dtype=torch.bfloat16, device="cuda")
+    pipe.norm(z, qn, kv[0], kn, rope=table, k_keep=mask)
+    pipe.commit(kn, kv[1], mask, 1)
+    pipe.digest(-1)
+
+    def frame():
+        pipe.norm(z, qn, kv[0], kn, rope=table, k_keep=mask)
+        pipe.select(z, mask)
+        pipe.select_blocks(qn)
+        pipe.readout_blocks(qn, None, x)
+        pipe.commit(kn, kv[1], mask, 0)
+        pipe.digest(1)
+
+    frame()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        frame()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert pipe.status_code() == 0
+    assert rs3.rs3_bank_read_meta(pipe.bank)[0][0, 3] == 4
+    before = x.clone()
+    # the same frame again, read from a fork of unit 0
+    pipe.select_blocks(qn)
+    pipe.readout_blocks(qn, None, x)
+    fork = pipe.fork(torch.tensor([0, 0], dtype=torch.int32, device="cuda"))
+    y = torch.zeros_like(x)
+    fork.digest(-1)
+    fork.idx.copy_(pipe.idx[:1].expand_as(pipe.idx))
+    fork.count.copy_(pipe.count[:1].expand_as(pipe.count))
+    fork.select_blocks(qn)
+    fork.readout_blocks(qn, None, y)
+    assert pipe.status_code() == 0 and fork.status_code() == 0
+    assert torch.equal(y[0], x[0]) and torch.equal(y[1], x[0]) and before.shape == x.shape
