@@ -9,7 +9,8 @@
 //              partial results of a query's blocks are joined by their log-sum-exp (k_join_blocks)
 #include "rs3_sparse.cuh"
 
-#include "rs3_readout_common.cuh"
+#include "rs3_tc_host.cuh"
+#include "rs3_tc_ptx.cuh"
 
 #include <cmath>
 
@@ -227,72 +228,100 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 // by block
 // ---------------------------------------------------------------------------
 constexpr int TILE = 64;                   // queries of an item
-constexpr int LIST_THREADS = 512;
+constexpr int LIST_THREADS = 1024;
 constexpr int LIST_BINS = 8192;            // blocks that a CTA counts
 constexpr int MAX_SEGMENTS = 1024;         // (unit, head, segment) triples that a CTA of the attention holds at a time
+constexpr int CHUNK_ITEMS = 64;            // items whose records it holds
 
-// A block and up to TILE of the queries that chose it.
+// Part of a block (its 32 or 64 rows, half of its 128) and up to TILE of the queries that chose it.
 struct BlockItem {
-    int32_t uh, b, first, n;               // unit * H + head, block, first list entry, entries
-    uint32_t live[4];                      // its live rows
+    int32_t uh, part, first, n;            // unit * H + head, storage rows / rows of a part, first list entry, entries
+    uint32_t live[2];                      // its live rows
+    int32_t pad[2];
 };
 
 struct BlockWork {                         // in the workspace
     int32_t *n_items, *first_item;         // [U * H][segments]
     BlockItem *items;                      // [U * H][max_items]
     int2 *list;                            // [U * H][k_max * n_top]: (query * n_top + entry, cell)
-    float2 *ml;                            // [U * H][k_max][n_top]: (max in the log2 domain, sum)
-    float *o;                              // [U * H][k_max][n_top][d]
-    int32_t segments, bins;
+    float2 *ml;                            // [U * H][k_max][n_top][parts]: (max in the log2 domain, sum)
+    float *o;                              // [U * H][k_max][n_top][parts][d]
+    int32_t segments, bins, parts, list_ctas;
     int64_t max_items;
+    uint64_t wait_ns;                      // limit of each wait
 };
+
+// f(i, list[i]) for i < n, by the CTA's threads, four entries to a load where the alignment allows
+template <typename F>
+__device__ __forceinline__ void each_entry(const int32_t *list, int n, F f)
+{
+    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(list) & 15)) >> 2 & 3));
+    const int vecs = (n - head) >> 2, tail = head + 4 * vecs;
+    if ((int)threadIdx.x < head) f((int)threadIdx.x, __ldg(list + threadIdx.x));
+    const int4 *v = reinterpret_cast<const int4 *>(list + head);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < vecs; i += LIST_THREADS) {
+        const int4 x = __ldg(v + i);
+        const int e = head + 4 * i;
+        f(e, x.x);
+        f(e + 1, x.y);
+        f(e + 2, x.z);
+        f(e + 3, x.w);
+    }
+    if (tail + (int)threadIdx.x < n) f(tail + (int)threadIdx.x, __ldg(list + tail + threadIdx.x));
+}
 
 // The queries of every block: CTA (segment, unit * H + head) counts the lists' entries for its
 // blocks, gives every block a run of list entries and its items, and fills them in.  Entries of one block
-// come in any order; each is computed by itself, so the result does not depend on it.
-__global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, BlockWork w)
+// come in any order; each is computed by itself, so the result does not depend on it.  Out of place the
+// launch's other CTAs write out = residual (or zeros) on every cell.
+__global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
-    extern __shared__ int32_t s_bin[];                 // [bins + 1] counts, then first entries
-    __shared__ int32_t s_part[LIST_THREADS / 32], s_items[LIST_THREADS / 32], s_before;
+    if ((int)blockIdx.x >= w.list_ctas) {
+        const uint4 *res = static_cast<const uint4 *>(a.residual);
+        uint4 *out = static_cast<uint4 *>(a.out);
+        for (int64_t i = (int64_t)((int)blockIdx.x - w.list_ctas) * LIST_THREADS + threadIdx.x; i < nvec;
+             i += (int64_t)((int)gridDim.x - w.list_ctas) * LIST_THREADS)
+            out[i] = res ? __ldcs(res + i) : make_uint4(0, 0, 0, 0);
+        return;
+    }
+    extern __shared__ int32_t s_bin[];                 // [bins] counts, then first entries
+    __shared__ int32_t s_part[LIST_THREADS / 32], s_items[LIST_THREADS / 32];
     const SparseArgs &s = a.s;
-    const int uh = blockIdx.y, u = uh / s.H, seg = blockIdx.x;
+    const int uh = blockIdx.x / w.segments, seg = blockIdx.x - uh * w.segments, u = uh / s.H;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int lo = seg * w.bins, hi = min(s.nb, lo + w.bins), n_bins = hi - lo;
     int cnt, g;
     LiveRows rows;
     const bool work = sparse_unit(s, u, threadIdx.x == 0 && seg == 0 && uh == u * s.H, cnt, g, rows) && n_bins > 0;
     if (!work) {
-        if (threadIdx.x == 0) w.n_items[uh * w.segments + seg] = 0;
+        if (threadIdx.x == 0) w.n_items[blockIdx.x] = 0;
         return;
     }
-    for (int i = threadIdx.x; i <= n_bins; i += LIST_THREADS) s_bin[i] = 0;
-    __syncthreads();
+    for (int i = threadIdx.x; i < n_bins; i += LIST_THREADS) s_bin[i] = 0;
+    const int32_t *idx = s.idx + (int64_t)u * s.k_max;
+    bool bad = false;                                  // some query's cell is not on the grid: it is in no list
+    for (int j = threadIdx.x; j < cnt; j += LIST_THREADS) bad |= (uint32_t)idx[j] >= (uint32_t)s.mn;
+    if (bad && seg == 0) latch_status(s.status, RS3_EINVAL);
+    const bool check = __syncthreads_or(bad);
     const int64_t base = (int64_t)uh * s.k_max * s.n_top;
-    const int32_t *sel = a.sel + base, *idx = s.idx + (int64_t)u * s.k_max;
     const int pairs = cnt * s.n_top;
+    const auto listed = [&](int i) { return !check || (uint32_t)idx[i / s.n_top] < (uint32_t)s.mn; };
     int before = 0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < pairs; i += LIST_THREADS) {
-        const int b = __ldg(sel + i);
-        const int cell = __ldg(idx + i / s.n_top);
-        if (b >= s.nb || cell < 0 || cell >= s.mn) {   // such an entry is in no list
-            if (seg == 0) latch_status(s.status, RS3_EINVAL);
-            continue;
-        }
-        if (b >= lo && b < hi) atomicAdd(&s_bin[b - lo], 1);
-        before += b >= 0 && b < lo;
-    }
+    each_entry(a.sel + base, pairs, [&](int i, int b) {
+        if (b >= s.nb && seg == 0) latch_status(s.status, RS3_EINVAL);
+        if (b < 0 || b >= hi || !listed(i)) return;
+        if (b >= lo) atomicAdd(&s_bin[b - lo], 1);
+        before += b < lo;
+    });
     before = __reduce_add_sync(0xffffffffu, before);
     if (lane == 0) s_part[warp] = before;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int t = 0;
-        for (int i = 0; i < LIST_THREADS / 32; ++i) t += s_part[i];
-        s_before = t;
-    }
+    before = 0;
+#pragma unroll
+    for (int i = 0; i < LIST_THREADS / 32; ++i) before += s_part[i];
     __syncthreads();
-    before = s_before;
     // entries and items before each bin: a run of bins per thread
     const int per = (n_bins + LIST_THREADS - 1) / LIST_THREADS;
     const int b0 = min(n_bins, (int)threadIdx.x * per), b1 = min(n_bins, b0 + per);
@@ -319,28 +348,26 @@ __global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, Bloc
     // the segments before this one have at most an item per block or entry, and one more per TILE entries
     const int item0 = min(lo, before) + before / TILE;
     if (threadIdx.x == 0) {
-        w.n_items[uh * w.segments + seg] = n_items;
-        w.first_item[uh * w.segments + seg] = item0;
+        w.n_items[blockIdx.x] = n_items * w.parts;
+        w.first_item[blockIdx.x] = item0 * w.parts;
     }
     int first = before + e_sum - entries;
-    BlockItem *out = w.items + uh * w.max_items + item0 + i_sum - items;
+    BlockItem *out = w.items + uh * w.max_items + (int64_t)(item0 + i_sum - items) * w.parts;
+    const int pr = s.bs / w.parts;                     // rows of a part
     for (int b = b0; b < b1; ++b) {
         const int n = s_bin[b];
         s_bin[b] = first;
-        if (n > 0) {
-            const int64_t r0 = (int64_t)(lo + b) * s.bs;
-            BlockItem it;
+        for (int p = 0; n > 0 && p < w.parts; ++p) {
+            BlockItem it = {};
             it.uh = uh;
-            it.b = lo + b;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) it.live[i] = i * 32 < s.bs ? 0xffffffffu : 0u;
-            if (rows.count(r0, r0 + s.bs) < s.bs)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t m = 0;
-                    for (int r = 0; r < 32 && i * 32 < s.bs; ++r) m |= (uint32_t)rows.holds(r0 + i * 32 + r) << r;
-                    it.live[i] = m;
-                }
+            it.part = (lo + b) * w.parts + p;
+            const int64_t r0 = (int64_t)it.part * pr;
+            it.live[0] = 0xffffffffu;
+            it.live[1] = pr > 32 ? 0xffffffffu : 0u;
+            if (rows.count(r0, r0 + pr) < pr) {
+                it.live[0] = it.live[1] = 0u;
+                for (int r = 0; r < pr; ++r) it.live[r >> 5] |= (uint32_t)rows.holds(r0 + r) << (r & 31);
+            }
             for (int e = 0; e < n; e += TILE) {
                 it.first = first + e;
                 it.n = min(TILE, n - e);
@@ -351,30 +378,16 @@ __global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, Bloc
     }
     __syncthreads();
     int2 *list = w.list + base;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < pairs; i += LIST_THREADS) {
-        const int b = __ldg(sel + i);
-        const int cell = __ldg(idx + i / s.n_top);
-        if (b >= lo && b < hi && cell >= 0 && cell < s.mn) list[atomicAdd(&s_bin[b - lo], 1)] = make_int2(i, cell);
-    }
+    each_entry(a.sel + base, pairs, [&](int i, int b) {
+        if (b >= lo && b < hi && listed(i)) list[atomicAdd(&s_bin[b - lo], 1)] = make_int2(i, idx[i / s.n_top]);
+    });
 }
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool some)
+__device__ __forceinline__ uint4 lds128(uint32_t addr)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
-}
-
-__device__ __forceinline__ void ld_matrix4(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-
-__device__ __forceinline__ void ld_matrix2(uint32_t (&r)[2], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 __device__ __forceinline__ void ld_matrix4_t(uint32_t (&r)[4], uint32_t addr)
@@ -384,51 +397,64 @@ __device__ __forceinline__ void ld_matrix4_t(uint32_t (&r)[4], uint32_t addr)
 }
 
 // c (16 x 8, fp32) += a (16 x 16, bf16) b (16 x 8, bf16)
-__device__ __forceinline__ void mma_16x8x16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int D, int BS>
+template <int D, int TR>
 struct BlockTile {
-    static constexpr int NW = D == 64 ? 4 : 8;         // warps
-    static constexpr int ROW = 2 * D + 16;             // bytes of a K, V or Q row: 8 rows at 16-byte steps hit all banks
-    static constexpr int PROW = 2 * BS + 16;
-    static constexpr int KEYS = BS / NW < 8 ? 8 : BS / NW;     // keys of a warp's scores
-    static constexpr int SW = BS / KEYS;               // warps with scores
-    static constexpr int COLS = D / NW;                // columns of a warp's values
-    static constexpr int M = 32;                       // queries of a pass
-    static constexpr int K0 = 0, V0 = BS * ROW, Q0 = 2 * BS * ROW, P0 = Q0 + M * ROW, MAX0 = P0 + M * PROW, SUM0 = MAX0 + 4 * M * NW,
-                         LIST0 = SUM0 + 4 * M * NW, BYTES = LIST0 + 8 * TILE;
+    static constexpr int CONSUMERS = 8, THREADS = 32 * (CONSUMERS + 1);
+    static constexpr int CTAS = D == 256 ? 1 : 2;      // per SM
+    static constexpr int HALF = TR * D * 2, STAGE = 2 * HALF;      // bytes of a part's keys; keys and values
+    static constexpr int FIT = (D == 256 ? 196608 : 98304) / STAGE, STAGES = FIT > 8 ? 8 : FIT;
+    static constexpr int SMEM = STAGES * STAGE + 1024;             // stages begin at a multiple of 1 KB
 };
 
-// Persistent CTAs walk the items.  Per item the block's K and V rows come by cp.async (dead rows as
-// zeros), and up to 64 queries pass in tiles of 32: S = Q K^T with the keys shared out to the warps, the
-// rows' maxima and sums exchanged through shared memory, P as bf16, O = P V with the columns shared
-// out, and (m, l, O) stored for k_join_blocks.  mma.sync: a block of a long bank has some 20 queries, so the
-// call is bound by the bytes of K and V and tiles of 128 rows would be four fifths empty.
-template <int D, int BS>
-__global__ void __launch_bounds__(32 * BlockTile<D, BS>::NW) k_attend_blocks(AttendArgs a, BlockWork w)
+// Persistent CTAs walk the items.  A producer thread brings the parts' keys and values by TMA (128-byte
+// swizzle) into a ring of stages; every consumer warp takes tiles of 16 queries by itself, item after item:
+// S = Q K^T from query fragments that it loads straight from the grid (the columns of a 64-column box
+// are taken in the order in which adjacent lanes can load 16 bytes of a row), the softmax of its rows in
+// registers, O = P V from those, and (m, l, O) stored for k_join_blocks.  No warp waits for another.
+// mma.sync: a block of a long bank has some 20 queries, so the call is bound by the bytes of K and V, and
+// tiles of 128 rows would be four fifths empty.
+template <int D, int TR>
+__global__ void __launch_bounds__(BlockTile<D, TR>::THREADS, BlockTile<D, TR>::CTAS)
+k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
 {
-    using X = BlockTile<D, BS>;
-    constexpr int THREADS = 32 * X::NW, PIECES = D / 8;
-    pdl_wait();
-    extern __shared__ __align__(16) uint8_t smem[];
+    using X = BlockTile<D, TR>;
+    using namespace tc;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_bars[2 * X::STAGES];
     __shared__ int32_t s_first[MAX_SEGMENTS + 1];
+    __shared__ BlockItem s_item[CHUNK_ITEMS];
+    __shared__ int32_t s_tile0[CHUNK_ITEMS];
+    __shared__ int s_abort;
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    const uint32_t full = smem_u32(s_bars), empty = full + 8u * X::STAGES;
+    volatile int *abort_flag = &s_abort;
     const SparseArgs &s = a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float *s_max = reinterpret_cast<float *>(smem + X::MAX0), *s_sum = reinterpret_cast<float *>(smem + X::SUM0);
-    int2 *s_list = reinterpret_cast<int2 *>(smem + X::LIST0);
-    const uint32_t sk = smem_addr(smem + X::K0), sv = smem_addr(smem + X::V0), sq = smem_addr(smem + X::Q0), sp = smem_addr(smem + X::P0);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < X::STAGES; ++i) {
+            mbar_init(full + 8u * i, 1);
+            mbar_init(empty + 8u * i, X::CONSUMERS);
+        }
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    pdl_wait();
     const int n_seg = s.U * s.H * w.segments;
     const int64_t row_elems = (int64_t)s.H * D;
-    int next = blockIdx.x;
+    uint32_t cnt = 0, issued = 0;                      // parts gone through: stage cnt % STAGES, phase cnt / STAGES; the producer's
+    int next = blockIdx.x, turn = 0;                   // this CTA's next item; tiles before the chunk
     for (int g0 = 0; g0 < n_seg; g0 += MAX_SEGMENTS) {
         const int n = min(MAX_SEGMENTS, n_seg - g0);
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += THREADS) s_first[i + 1] = w.n_items[g0 + i];
+        for (int i = threadIdx.x; i < n; i += X::THREADS) s_first[i + 1] = w.n_items[g0 + i];
         __syncthreads();
         if (warp == 0) {                               // items before each segment
             int run = 0;
@@ -446,248 +472,276 @@ __global__ void __launch_bounds__(32 * BlockTile<D, BS>::NW) k_attend_blocks(Att
         }
         __syncthreads();
         const int total = s_first[n];
-        for (; next < total; next += gridDim.x) {
-            int x = 0, y = n;                          // the last segment whose items begin at or before `next`
-            while (y - x > 1) {
-                const int mid = (x + y) >> 1;
-                if (s_first[mid] <= next) x = mid; else y = mid;
-            }
-            const int uh0 = (g0 + x) / w.segments;
-            const BlockItem *ip = w.items + uh0 * w.max_items + w.first_item[g0 + x] + (next - s_first[x]);
-            const int4 head = __ldg(reinterpret_cast<const int4 *>(ip));
-            const uint4 live4 = __ldg(reinterpret_cast<const uint4 *>(ip) + 1);
-            const uint32_t live[4] = {live4.x, live4.y, live4.z, live4.w};
-            const int u = head.x / s.H, h = head.x - u * s.H, nq = head.w;
-            // the block's rows
-            const int64_t off = ((int64_t)u * s.bank.rows_per_unit + (int64_t)head.y * BS) * row_elems + h * D;
-            const uint16_t *K = reinterpret_cast<const uint16_t *>(a.k_store) + off;
-            const uint16_t *V = reinterpret_cast<const uint16_t *>(a.v_store) + off;
-            for (int v = 0; v < 2; ++v) {
-                const uint16_t *src = v ? V : K;
-                const uint32_t dst = v ? sv : sk;
-#pragma unroll 4
-                for (int i = threadIdx.x; i < BS * PIECES; i += THREADS) {
-                    const int r = i / PIECES, p = i - r * PIECES;
-                    const bool on = (live[BS > 32 ? r >> 5 : 0] >> (r & 31)) & 1u;
-                    copy16(dst + r * X::ROW + p * 16, on ? src + r * row_elems + p * 8 : K, on);
+        while (next < total) {
+            // the records of this CTA's next items
+            const int chunk = min(CHUNK_ITEMS, (total - next + (int)gridDim.x - 1) / (int)gridDim.x);
+            if ((int)threadIdx.x < chunk) {
+                const int at = next + threadIdx.x * gridDim.x;
+                int x = 0, y = n;                      // the last segment whose items begin at or before `at`
+                while (y - x > 1) {
+                    const int mid = (x + y) >> 1;
+                    if (s_first[mid] <= at) x = mid; else y = mid;
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
+                s_item[threadIdx.x] = w.items[(g0 + x) / w.segments * w.max_items + w.first_item[g0 + x] + (at - s_first[x])];
             }
-            const int64_t base = (int64_t)head.x * s.k_max * s.n_top;
-            for (int i = threadIdx.x; i < nq; i += THREADS) s_list[i] = w.list[base + head.z + i];
             __syncthreads();
-            const uint16_t *Q = static_cast<const uint16_t *>(s.q) + (int64_t)s.unit_group[u] * s.mn * row_elems + h * D;
-            for (int q0 = 0; q0 < nq; q0 += X::M) {
-                const int m = min(X::M, nq - q0), tiles = m > 16 ? 2 : 1;
-                // query rows, rotated and rounded as the memory readout's; rows past the last are zeros
-                for (int i = threadIdx.x; i < tiles * 16 * PIECES; i += THREADS) {
-                    const int r = i / PIECES, p = i - r * PIECES;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (r < m) {
-                        const int cell = s_list[q0 + r].y;
-                        v = __ldg(reinterpret_cast<const uint4 *>(Q + cell * row_elems) + p);
-                        if (s.rope) v = rotate_q_piece(v, s.rope + (int64_t)cell * D + p * 8);
+            if (warp == 0) {                           // tiles before each item
+                int run = turn;
+                for (int c0 = 0; c0 < chunk; c0 += 32) {
+                    const int tiles = c0 + lane < chunk ? (s_item[c0 + lane].n + 15) >> 4 : 0;
+                    int v = tiles;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int t = __shfl_up_sync(0xffffffffu, v, o);
+                        if (lane >= o) v += t;
                     }
-                    *reinterpret_cast<uint4 *>(smem + X::Q0 + r * X::ROW + p * 16) = v;
+                    if (c0 + lane < chunk) s_tile0[c0 + lane] = run + v - tiles;
+                    run += __shfl_sync(0xffffffffu, v, 31);
                 }
-                if (q0 == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
-                __syncthreads();
-                float c[2][X::KEYS / 8][4];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < X::KEYS / 8; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[t][i][e] = 0.f;
-                float top[2][2];
-                if (warp < X::SW) {
-#pragma unroll 4
-                    for (int k = 0; k < D / 16; ++k) {
-                        uint32_t qa[2][4];
-                        ld_matrix4(qa[0], sq + (lane & 15) * X::ROW + k * 32 + (lane >> 4) * 16);
-                        if (tiles == 2) ld_matrix4(qa[1], sq + (16 + (lane & 15)) * X::ROW + k * 32 + (lane >> 4) * 16);
-                        if (X::KEYS == 8) {
-                            uint32_t kb[2];
-                            ld_matrix2(kb, sk + (warp * 8 + (lane & 7)) * X::ROW + k * 32 + ((lane >> 3) & 1) * 16);
-                            mma_16x8x16(c[0][0], qa[0], kb[0], kb[1]);
-                            if (tiles == 2) mma_16x8x16(c[1][0], qa[1], kb[0], kb[1]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < X::KEYS / 16; ++i) {
-                                uint32_t kb[4];
-                                ld_matrix4(kb, sk + (warp * X::KEYS + i * 16 + (lane & 7) + ((lane >> 4) << 3)) * X::ROW + k * 32 +
-                                                   ((lane >> 3) & 1) * 16);
-#pragma unroll
-                                for (int t = 0; t < 2; ++t) {
-                                    if (t == 1 && tiles == 1) break;
-                                    mma_16x8x16(c[t][(2 * i) % (X::KEYS / 8)], qa[t], kb[0], kb[1]);
-                                    mma_16x8x16(c[t][(2 * i + 1) % (X::KEYS / 8)], qa[t], kb[2], kb[3]);
-                                }
-                            }
-                        }
-                    }
-                    // this lane holds columns 2 (lane % 4), + 1 of rows lane / 4 and + 8
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            float mx = -INFINITY;
-#pragma unroll
-                            for (int i = 0; i < X::KEYS / 8; ++i)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const int key = warp * X::KEYS + i * 8 + (lane & 3) * 2 + e;
-                                    const bool on = (live[BS > 32 ? key >> 5 : 0] >> (key & 31)) & 1u;
-                                    float &v = c[t][i][2 * r + e];
-                                    v = on ? v * a.scale_log2 : -INFINITY;
-                                    mx = fmaxf(mx, v);
-                                }
-                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                            if ((lane & 3) == 0) s_max[warp * X::M + t * 16 + r * 8 + (lane >> 2)] = mx;
-                        }
-                }
-                __syncthreads();
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float mx = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < X::SW; ++i) mx = fmaxf(mx, s_max[i * X::M + t * 16 + r * 8 + (lane >> 2)]);
-                        top[t][r] = mx;
-                    }
-                if (warp < X::SW) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (t == 1 && tiles == 1) break;
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float ref = top[t][r] == -INFINITY ? 0.f : top[t][r];
-                            const int row = t * 16 + r * 8 + (lane >> 2);
-                            float sum = 0.f;
-#pragma unroll
-                            for (int i = 0; i < X::KEYS / 8; ++i) {
-                                const float p0 = exp2f(c[t][i][2 * r] - ref), p1 = exp2f(c[t][i][2 * r + 1] - ref);
-                                sum += p0 + p1;
-                                *reinterpret_cast<uint32_t *>(smem + X::P0 + row * X::PROW + (warp * X::KEYS + i * 8 + (lane & 3) * 2) * 2) =
-                                    pack_bf16x2(p0, p1);
-                            }
-                            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                            if ((lane & 3) == 0) s_sum[warp * X::M + row] = sum;
-                        }
-                    }
-                }
-                if (q0 == 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
-                __syncthreads();
-                float o[2][X::COLS / 8][4];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < X::COLS / 8; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < BS / 16; ++k) {
-                    uint32_t pa[2][4];
-                    ld_matrix4(pa[0], sp + (lane & 15) * X::PROW + k * 32 + (lane >> 4) * 16);
-                    if (tiles == 2) ld_matrix4(pa[1], sp + (16 + (lane & 15)) * X::PROW + k * 32 + (lane >> 4) * 16);
-#pragma unroll
-                    for (int i = 0; i < X::COLS / 16; ++i) {
-                        uint32_t vb[4];
-                        ld_matrix4_t(vb, sv + (k * 16 + (lane & 15)) * X::ROW + (warp * X::COLS + i * 16 + (lane >> 4) * 8) * 2);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            if (t == 1 && tiles == 1) break;
-                            mma_16x8x16(o[t][2 * i], pa[t], vb[0], vb[1]);
-                            mma_16x8x16(o[t][2 * i + 1], pa[t], vb[2], vb[3]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int row = t * 16 + r * 8 + (lane >> 2);
-                        if (row >= m) continue;
-                        const int64_t slot = base + s_list[q0 + row].x;
-                        if (warp == 0 && (lane & 3) == 0) {
-                            float l = 0.f;
-#pragma unroll
-                            for (int i = 0; i < X::SW; ++i) l += s_sum[i * X::M + row];
-                            w.ml[slot] = make_float2(top[t][r], l);
-                        }
-                        float *dst = w.o + slot * D + warp * X::COLS + (lane & 3) * 2;
-#pragma unroll
-                        for (int i = 0; i < X::COLS / 8; ++i)
-                            *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(o[t][i][2 * r], o[t][i][2 * r + 1]);
-                    }
-                __syncthreads();                       // P, Q and the sums are free; after the last pass K, V and the list too
             }
+            __syncthreads();
+            if (warp == X::CONSUMERS) {
+                if (lane == 0) {
+                    uint32_t k = cnt;
+                    for (int i = 0; i < chunk; ++i, ++k) {
+                        const uint32_t st = k % X::STAGES;
+                        if (!mbar_wait(empty + 8u * st, (k / X::STAGES & 1u) ^ 1u, abort_flag, w.wait_ns)) break;
+                        const int u = s_item[i].uh / s.H, h = s_item[i].uh - u * s.H;
+                        const int y = (int)(u * s.bank.rows_per_unit + (int64_t)s_item[i].part * TR);
+                        const uint32_t dst = base + st * X::STAGE, bar = full + 8u * st;
+                        mbar_expect_tx(bar, X::STAGE);
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c) tma_load_2d(dst + c * (TR * 128), &tmk, bar, h * D + c * 64, y);
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c) tma_load_2d(dst + X::HALF + c * (TR * 128), &tmv, bar, h * D + c * 64, y);
+                    }
+                    issued = k;
+                }
+                __syncwarp();
+            } else {
+                bool ok = true;
+                for (int i = 0; i < chunk && ok; ++i) {
+                    const uint32_t k = cnt + i, st = k % X::STAGES;
+                    const int tile = (warp - s_tile0[i]) & (X::CONSUMERS - 1);
+                    const int m = s_item[i].n - tile * 16;     // queries of this warp's tile
+                    if (m <= 0) {                      // the others'
+                        ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
+                        if (ok && lane == 0) mbar_arrive(empty + 8u * st);
+                        continue;
+                    }
+                    const int uh = s_item[i].uh, u = uh / s.H, h = uh - u * s.H;
+                    const int64_t pair0 = (int64_t)uh * s.k_max * s.n_top;
+                    const int2 *list = w.list + pair0 + s_item[i].first + tile * 16;
+                    // this lane's rows: lane / 4 and + 8; of 64 columns the pieces 2 (lane % 4) and + 1
+                    const int r = lane >> 2, t = lane & 3;
+                    int2 e[2];
+                    uint4 q[2][D / 32];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) e[x] = r + 8 * x < m ? __ldg(list + r + 8 * x) : make_int2(-1, -1);
+                    const uint16_t *Q = static_cast<const uint16_t *>(s.q) + (int64_t)__ldg(s.unit_group + u) * s.mn * row_elems + h * D;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            q[x][c] = make_uint4(0, 0, 0, 0);
+                            if (e[x].y >= 0)
+                                q[x][c] = __ldg(reinterpret_cast<const uint4 *>(Q + e[x].y * row_elems) + (c >> 1) * 8 + 2 * t + (c & 1));
+                        }
+                    if (s.rope)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+#pragma unroll
+                            for (int c = 0; c < D / 32; ++c)
+                                if (e[x].y >= 0)
+                                    q[x][c] = rotate_q_piece(q[x][c], s.rope + (int64_t)e[x].y * D + ((c >> 1) * 8 + 2 * t + (c & 1)) * 8);
+                    ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
+                    if (!ok) break;
+                    const uint32_t sk = base + st * X::STAGE, sv = sk + X::HALF;
+                    const uint32_t live[2] = {s_item[i].live[0], s_item[i].live[1]};
+                    const bool whole = live[0] == 0xffffffffu && (TR == 32 || live[1] == 0xffffffffu);
+                    float c[TR / 8][4];
+#pragma unroll
+                    for (int x = 0; x < TR / 8; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
+#pragma unroll
+                    for (int b = 0; b < D / 32; ++b) {
+                        const uint32_t col = sk + (b >> 1) * (TR * 128) + (((2 * t + (b & 1)) ^ r) << 4);
+#pragma unroll
+                        for (int x = 0; x < TR / 8; ++x) {
+                            const uint4 y = lds128(col + (x * 8 + r) * 128);
+                            mma_16x8x16(c[x], q[0][b].x, q[1][b].x, q[0][b].y, q[1][b].y, y.x, y.y);
+                            mma_16x8x16(c[x], q[0][b].z, q[1][b].z, q[0][b].w, q[1][b].w, y.z, y.w);
+                        }
+                    }
+                    // this lane holds keys 8 x + 2 t, + 1 of its two rows
+                    if (!whole) {
+#pragma unroll
+                        for (int x = 0; x < TR / 8; ++x)
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                if (!(live[x >> 2] >> ((x & 3) * 8 + 2 * t + (y & 1)) & 1u)) c[x][y] = -INFINITY;
+                    }
+                    float mx[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, ref[2];
+#pragma unroll
+                    for (int x = 0; x < TR / 8; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) mx[y >> 1] = fmaxf(mx[y >> 1], c[x][y]);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
+                        mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2)) * a.scale_log2;
+                        ref[y] = mx[y] == -INFINITY ? 0.f : -mx[y];
+                    }
+                    uint32_t p[TR / 8][2];
+#pragma unroll
+                    for (int x = 0; x < TR / 8; ++x)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float p0 = ex2_approx(fmaf(c[x][2 * y], a.scale_log2, ref[y]));
+                            const float p1 = ex2_approx(fmaf(c[x][2 * y + 1], a.scale_log2, ref[y]));
+                            sum[y] += p0 + p1;
+                            p[x][y] = pack_bf16x2(p0, p1);
+                        }
+                    if (!whole) {                      // dead rows may hold anything: as values they are zeros
+                        for (int row = 0; row < TR; ++row)
+                            if (!(live[row >> 5] >> (row & 31) & 1u) && lane < D / 8)
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};"
+                                             ::"r"(sv + (lane >> 3) * (TR * 128) + row * 128 + (lane & 7) * 16), "r"(0) : "memory");
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
+                    float o[D / 8][4];
+#pragma unroll
+                    for (int x = 0; x < D / 8; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) o[x][y] = 0.f;
+#pragma unroll
+                    for (int b = 0; b < TR / 16; ++b) {
+                        const uint32_t row = sv + (b * 16 + (lane & 15)) * 128;
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) {
+                            uint32_t v[4];
+                            ld_matrix4_t(v, row + (x >> 2) * (TR * 128) + ((((x & 3) * 2 + (lane >> 4)) ^ (lane & 7)) << 4));
+                            mma_16x8x16(o[2 * x], p[2 * b][0], p[2 * b][1], p[2 * b + 1][0], p[2 * b + 1][1], v[0], v[1]);
+                            mma_16x8x16(o[2 * x + 1], p[2 * b][0], p[2 * b][1], p[2 * b + 1][0], p[2 * b + 1][1], v[2], v[3]);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(empty + 8u * st);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
+                        sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
+                        if (e[y].x < 0) continue;
+                        const int64_t slot = (pair0 + e[y].x) * w.parts + s_item[i].part % w.parts;
+                        if (t == 0) w.ml[slot] = make_float2(mx[y], sum[y]);
+                        float *dst = w.o + slot * D + 2 * t;
+#pragma unroll
+                        for (int x = 0; x < D / 8; ++x)
+                            *reinterpret_cast<float2 *>(dst + 8 * x) = make_float2(o[x][2 * y], o[x][2 * y + 1]);
+                    }
+                    __syncwarp();
+                }
+            }
+            __syncthreads();                           // the records are read
+            if (*abort_flag) {                         // the same for all threads: it is set before the barrier
+                if (threadIdx.x == 0) latch_status(s.status, RS3_ETIMEOUT);
+                // copies in flight land before the CTA ends (only the producer's thread has issued any)
+                for (uint32_t d = issued > X::STAGES ? issued - X::STAGES : 0; d < issued; ++d)
+                    mbar_drain(full + 8u * (d % X::STAGES), d / X::STAGES & 1u);
+                return;
+            }
+            cnt += chunk;
+            next += chunk * (int)gridDim.x;
+            turn = (s_tile0[chunk - 1] + ((s_item[chunk - 1].n + 15) >> 4)) & (X::CONSUMERS - 1);
+            __syncthreads();
         }
         next -= total;
     }
 }
 
-// Lanes of D / 4 (at most 32) take a (unit, head, query): out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
+// Groups of D / 4 (at most 64) lanes, four to a (unit, head, query): each joins a quarter of the blocks'
+// results by their running maximum, then the four are joined:
+//   out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
+// A quarter each because the loads of one after another would wait for one another.
+constexpr int JOIN_THREADS = 256;
+
 template <int D>
-__global__ void __launch_bounds__(256) k_join_blocks(AttendArgs a, BlockWork w)
+__global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, BlockWork w)
 {
-    constexpr int L = D / 4 < 32 ? D / 4 : 32, ITEMS = D / 4 / L;
+    constexpr int L = D / 4, PER = JOIN_THREADS / (4 * L);
     pdl_wait();
+    __shared__ float4 s_y[JOIN_THREADS];
+    __shared__ float2 s_ml[JOIN_THREADS / L];
     const SparseArgs &s = a.s;
-    const int u = blockIdx.y, sub = threadIdx.x % L;
-    const int64_t jh = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int u = blockIdx.y, sub = threadIdx.x % L, part = threadIdx.x / L;
+    const int64_t jh = (int64_t)blockIdx.x * PER + part / 4;
     const int j = (int)(jh / s.H), h = (int)(jh - (int64_t)j * s.H);
     const int cnt = s.count[u], g = s.unit_group[u];
-    if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || j >= cnt) return;
-    const int cell = s.idx[(int64_t)u * s.k_max + j];
-    if (cell < 0 || cell >= s.mn) return;
+    if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || (int64_t)blockIdx.x * PER >= (int64_t)cnt * s.H) return;
+    const int cell = j < cnt ? s.idx[(int64_t)u * s.k_max + j] : -1;
+    const bool here = cell >= 0 && cell < s.mn;
     const int64_t base = (((int64_t)u * s.H + h) * s.k_max + j) * s.n_top;
-    float top = -INFINITY;
-    for (int t = sub; t < s.n_top; t += L) {
-        const int b = a.sel[base + t];
-        if (b >= 0 && b < s.nb) top = fmaxf(top, w.ml[base + t].x);
-    }
-    const uint32_t group = L == 32 ? 0xffffffffu : ((1u << L) - 1u) << ((threadIdx.x & 31) / L * L);
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    const int n = here ? s.n_top * w.parts : 0;
+    constexpr int F = 8;                               // results in flight
+    for (int t0 = part & 3; t0 < n; t0 += 4 * F) {
+        float2 ml[F];
+        float4 v[F];
 #pragma unroll
-    for (int o = L >> 1; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(group, top, o));
-    float4 y[ITEMS];
-    float l = 0.f;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (top > -INFINITY) {
-#pragma unroll 4
-        for (int t = 0; t < s.n_top; ++t) {
-            const int b = __ldg(a.sel + base + t);
-            if (b < 0 || b >= s.nb) continue;
-            const float2 ml = w.ml[base + t];
-            const float f = exp2f(ml.x - top);
-            l = fmaf(f, ml.y, l);
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const float4 v = __ldcs(reinterpret_cast<const float4 *>(w.o + (base + t) * D) + sub + L * i);
-                y[i].x = fmaf(f, v.x, y[i].x);
-                y[i].y = fmaf(f, v.y, y[i].y);
-                y[i].z = fmaf(f, v.z, y[i].z);
-                y[i].w = fmaf(f, v.w, y[i].w);
+        for (int f = 0; f < F; ++f) {
+            const int t = t0 + 4 * f;
+            const int b = t < n ? __ldg(a.sel + base + (w.parts == 2 ? t >> 1 : t)) : -1;
+            ml[f] = make_float2(-INFINITY, 0.f);
+            v[f] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (b >= 0 && b < s.nb) {
+                ml[f] = w.ml[base * w.parts + t];
+                v[f] = __ldcs(reinterpret_cast<const float4 *>(w.o + (base * w.parts + t) * D) + sub);
             }
         }
-        const float inv = 1.f / l;
+        float top = m;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) y[i] = make_float4(y[i].x * inv, y[i].y * inv, y[i].z * inv, y[i].w * inv);
-    }
-    const int64_t at = ((int64_t)u * s.mn + cell) * ((int64_t)s.H * D) + h * D;
+        for (int f = 0; f < F; ++f) top = fmaxf(top, ml[f].x);
+        if (top == -INFINITY) continue;
+        const float keep = exp2f(m - top);
+        m = top;
+        l *= keep;
+        y = make_float4(y.x * keep, y.y * keep, y.z * keep, y.w * keep);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int64_t x = at + (sub + L * i) * 4;
-        if (a.residual) {
-            const float4 r = load4(static_cast<const uint16_t *>(a.residual) + x);
-            y[i] = make_float4(y[i].x + r.x, y[i].y + r.y, y[i].z + r.z, y[i].w + r.w);
+        for (int f = 0; f < F; ++f) {
+            const float e = exp2f(ml[f].x - top);
+            l = fmaf(e, ml[f].y, l);
+            y = make_float4(fmaf(e, v[f].x, y.x), fmaf(e, v[f].y, y.y), fmaf(e, v[f].z, y.z), fmaf(e, v[f].w, y.w));
         }
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + x) = make_uint2(pack_bf16x2(y[i].x, y[i].y), pack_bf16x2(y[i].z, y[i].w));
     }
+    s_y[threadIdx.x] = y;
+    if (sub == 0) s_ml[part] = make_float2(m, l);
+    __syncthreads();
+    if ((part & 3) != 0 || !here) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top = fmaxf(top, s_ml[part + x].x);
+    y = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (top > -INFINITY) {
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float e = exp2f(s_ml[part + x].x - top);
+            const float4 v = s_y[threadIdx.x + x * L];
+            l = fmaf(e, s_ml[part + x].y, l);
+            y = make_float4(fmaf(e, v.x, y.x), fmaf(e, v.y, y.y), fmaf(e, v.z, y.z), fmaf(e, v.w, y.w));
+        }
+        const float inv = 1.f / l;
+        y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+    }
+    const int64_t at = ((int64_t)u * s.mn + cell) * ((int64_t)s.H * D) + h * D + sub * 4;
+    if (a.residual) {
+        const float4 r = load4(static_cast<const uint16_t *>(a.residual) + at);
+        y = make_float4(y.x + r.x, y.y + r.y, y.z + r.z, y.w + r.w);
+    }
+    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
 }
 
 // Where the parts of a by-block call lie in its workspace.
@@ -696,7 +750,7 @@ struct WorkLayout {
     size_t n_items, first_item, items, list, ml, o, total;
 };
 
-WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top, int64_t nb)
+WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top, int64_t nb, int64_t parts)
 {
     WorkLayout l = {};
     const int64_t uh = U * H, pairs = k_max * n_top;
@@ -705,7 +759,7 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
     l.segments = least;
     while (uh * l.segments < 256 && nb / (2 * l.segments) >= 64) l.segments *= 2;
     l.bins = (nb + l.segments - 1) / l.segments;
-    l.max_items = (nb < pairs ? nb : pairs) + pairs / TILE + 1;
+    l.max_items = ((nb < pairs ? nb : pairs) + pairs / TILE + 1) * parts;
     size_t at = 0;
     const auto part = [&](size_t bytes) {
         const size_t x = at;
@@ -716,8 +770,8 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
     l.first_item = part((size_t)(uh * least + 512) * 4);
     l.items = part((size_t)(uh * l.max_items) * sizeof(BlockItem));
     l.list = part((size_t)(uh * pairs) * 8);
-    l.ml = part((size_t)(uh * pairs) * 8);
-    l.o = part((size_t)(uh * pairs) * (size_t)d * 4);
+    l.ml = part((size_t)(uh * pairs * parts) * 8);
+    l.o = part((size_t)(uh * pairs * parts) * (size_t)d * 4);
     l.total = at;
     return l;
 }
@@ -728,26 +782,32 @@ bool sized_by_blocks(rs3_dtype dtype, int64_t U, int64_t H, int64_t d, int64_t k
     return dtype == RS3_BF16 && d >= 64 && U * H * k_max * n_top >= 4096;
 }
 
-bool by_blocks(rs3_dtype dtype, int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top)
+// Beyond the sizes that the lists' and the tensor maps' 32-bit numbers hold it is by query.
+bool by_blocks(const SparseArgs &s, rs3_dtype dtype)
 {
-    return sized_by_blocks(dtype, U, H, d, k_max, n_top) && k_max * n_top < (1ll << 30) && U * H < 65536;
+    return sized_by_blocks(dtype, s.U, s.H, s.d, s.k_max, s.n_top) && (int64_t)s.k_max * s.n_top < (1ll << 28) &&
+           (int64_t)s.U * s.H * work_layout(s.U, s.H, s.d, s.k_max, s.n_top, s.nb, 2).max_items < (1ll << 30) &&
+           s.U * s.bank.rows_per_unit < (1ll << 31) - 128;
 }
 
-template <int D, int BS>
+template <int D, int TR>
 rs3_status launch_attend(const AttendArgs &a, const BlockWork &w, cudaStream_t st)
 {
-    using X = BlockTile<D, BS>;
-    const rs3_status r = rs3_kernel_smem((const void *)k_attend_blocks<D, BS>, X::BYTES);
+    using X = BlockTile<D, TR>;
+    const rs3_status r = rs3_kernel_smem((const void *)k_attend_blocks<D, TR>, X::SMEM);
     if (r != RS3_OK) return r;
-    const int per_sm = 225 * 1024 / (X::BYTES + 6 * 1024);
-    launch_pdl(k_attend_blocks<D, BS>, dim3((unsigned)(rs3_sm_count() * (per_sm > 8 ? 8 : per_sm))), dim3(32 * X::NW), X::BYTES, st, a, w);
+    CUtensorMap mk, mv;
+    const int64_t rows = a.s.U * a.s.bank.rows_per_unit, width = (int64_t)a.s.H * D;
+    if (!tc::make_kv_map(&mk, a.k_store, width, rows, TR) || !tc::make_kv_map(&mv, a.v_store, width, rows, TR)) return RS3_ECUDA;
+    launch_pdl(k_attend_blocks<D, TR>, dim3((unsigned)(rs3_sm_count() * X::CTAS)), dim3(X::THREADS), X::SMEM, st, a, w, mk, mv);
     return RS3_OK;
 }
 
 rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t st)
 {
     const SparseArgs &s = a.s;
-    const WorkLayout l = work_layout(s.U, s.H, s.d, s.k_max, s.n_top, s.nb);
+    const int parts = s.bs > 64 ? 2 : 1;
+    const WorkLayout l = work_layout(s.U, s.H, s.d, s.k_max, s.n_top, s.nb, parts);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     BlockWork w = {};
     w.n_items = reinterpret_cast<int32_t *>(ws + l.n_items);
@@ -758,16 +818,26 @@ rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t s
     w.o = reinterpret_cast<float *>(ws + l.o);
     w.segments = (int32_t)l.segments;
     w.bins = (int32_t)l.bins;
+    w.parts = parts;
+    w.list_ctas = (int32_t)(s.U * s.H * l.segments);
     w.max_items = l.max_items;
-    launch_pdl(k_block_lists, dim3((unsigned)l.segments, (unsigned)(s.U * s.H)), dim3(LIST_THREADS), (size_t)(l.bins + 1) * 4, st, a, w);
+    w.wait_ns = rs3_get_wait_limit_ns();
+    int64_t nvec = 0, pass = 0;
+    if (a.out != a.residual) {
+        nvec = (int64_t)s.U * s.mn * s.H * s.d / 8;
+        pass = (nvec + 4 * LIST_THREADS - 1) / (4 * LIST_THREADS);
+        if (pass > 2 * rs3_sm_count()) pass = 2 * rs3_sm_count();
+    }
+    launch_pdl(k_block_lists, dim3((unsigned)(w.list_ctas + pass)), dim3(LIST_THREADS), (size_t)l.bins * 4, st, a, w, nvec);
     rs3_status r = RS3_EINTERNAL;
-    if (s.d == 64) r = s.bs == 32 ? launch_attend<64, 32>(a, w, st) : s.bs == 64 ? launch_attend<64, 64>(a, w, st) : launch_attend<64, 128>(a, w, st);
-    if (s.d == 128) r = s.bs == 32 ? launch_attend<128, 32>(a, w, st) : s.bs == 64 ? launch_attend<128, 64>(a, w, st) : launch_attend<128, 128>(a, w, st);
-    if (s.d == 256) r = s.bs == 32 ? launch_attend<256, 32>(a, w, st) : s.bs == 64 ? launch_attend<256, 64>(a, w, st) : launch_attend<256, 128>(a, w, st);
+    const bool half = s.bs == 32;
+    if (s.d == 64) r = half ? launch_attend<64, 32>(a, w, st) : launch_attend<64, 64>(a, w, st);
+    if (s.d == 128) r = half ? launch_attend<128, 32>(a, w, st) : launch_attend<128, 64>(a, w, st);
+    if (s.d == 256) r = half ? launch_attend<256, 32>(a, w, st) : launch_attend<256, 64>(a, w, st);
     if (r != RS3_OK) return r;
     void (*join)(AttendArgs, BlockWork) = s.d == 64 ? k_join_blocks<64> : s.d == 128 ? k_join_blocks<128> : k_join_blocks<256>;
-    const int per = 256 / (s.d / 4 < 32 ? s.d / 4 : 32);
-    launch_pdl(join, dim3((unsigned)(((int64_t)s.k_max * s.H + per - 1) / per), (unsigned)s.U), dim3(256), 0, st, a, w);
+    const int per = JOIN_THREADS / s.d;
+    launch_pdl(join, dim3((unsigned)(((int64_t)s.k_max * s.H + per - 1) / per), (unsigned)s.U), dim3(JOIN_THREADS), 0, st, a, w);
     return RS3_OK;
 }
 
@@ -777,7 +847,7 @@ extern "C" size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_
 {
     if (U < 1 || H < 1 || d < 1 || k_max < 0 || n_top < 1 || n_blocks < 0) return 0;
     if (dtype != RS3_F32 && dtype != RS3_BF16) return 0;
-    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(U, H, d, k_max, n_top, n_blocks).total : 0);
+    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(U, H, d, k_max, n_top, n_blocks, 2).total : 0);
 }
 
 extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -792,7 +862,7 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
     if (!sel || !out || !workspace || !(scale >= 0.f) || std::isinf(scale)) return RS3_EINVAL;
     if (!rs3_aligned16(out) || !rs3_aligned16(workspace) || (residual && !rs3_aligned16(residual))) return RS3_EINVAL;
     if (workspace_bytes < rs3_sparse_readout_workspace_bytes(a.s.U, H, d, k_max, n_top, a.s.nb, dtype)) return RS3_ECAPACITY;
-    const bool blocks = a.s.nb > 0 && by_blocks(dtype, a.s.U, H, d, k_max, n_top);
+    const bool blocks = a.s.nb > 0 && by_blocks(a.s, dtype);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     a.k_store = static_cast<const uint8_t *>(bank->k_store);
     a.v_store = static_cast<const uint8_t *>(bank->v_store);
@@ -800,7 +870,7 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
     a.residual = residual;
     a.out = out;
     a.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)d) : scale) * 1.4426950408889634f;
-    if (out != residual) {
+    if (out != residual && !blocks) {
         const int64_t nvec = (int64_t)a.s.U * mn * H * d * (int64_t)elem_bytes(dtype) / 16;
         const int64_t ctas = (nvec + 1023) / 1024, most = 8ll * rs3_sm_count();
         launch_pdl(k_pass_through, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st,

@@ -580,6 +580,71 @@ def test_sparse_readout_matches_64_bits(rs3, dtype, H, d, n_top, block, residual
     assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
 
 
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 64), ("bf16", 1, 128), ("bf16", 3, 256), ("f32", 1, 64)])
+@pytest.mark.parametrize("block,n_top", [(32, 19), (64, 11), (128, 6)])
+@pytest.mark.parametrize("residual,rope", [("none", True), ("inplace", False), ("other", True)])
+def test_sparse_readout_of_many_queries(rs3, dtype, H, d, block, n_top, residual, rope):
+    """Enough queries that a block's go together; half of them choose among a few blocks, others have gaps; NaN in
+    dead rows, a unit without rows, one without queries, a wrapped ring."""
+    counts = [143, 90, 0, 131]
+    b = Built(rs3, U=4, H=H, d=d, dtype=dtype, m=12, n=12, window=5, commits=8, n_ptr=5, empty=(1,), seed=n_top)
+    rs3.rs3_bank_reset(b.bank, 1)
+    nb = b.bank.blocks(block)
+    k_max = 143
+    q, idx, count, group = queries(b, 2, k_max, counts)
+    g = gen(33)
+    key = torch.rand((b.U, H, k_max, nb), generator=g, device="cuda")
+    key[:, :, ::2, n_top + 1:] += 1.0
+    sel = key.argsort(-1)[..., :n_top].to(torch.int32)
+    if nb < n_top:
+        sel = torch.nn.functional.pad(sel, (0, n_top - nb), value=-1)
+    sel = torch.where(torch.rand(sel.shape, generator=g, device="cuda") < 0.1, -1, sel).contiguous()
+    sel[0, :, 5] = -1
+    table = rope_table(b.mn, d) if rope else None
+    x = torch.randn((b.U, b.mn, b.D), generator=g, device="cuda").to(DT[dtype])
+    res = None if residual == "none" else x.clone()
+    out = res if residual == "inplace" else torch.full_like(x, math.nan)
+    some = list(range(0, 143, 9)) + [1, 142]
+    part = idx[:, some].contiguous()
+    counts_of = [sum(i < n for i in some) for n in counts]
+    order = [sorted((i >= n, i) for i in some) for n in counts]
+    for u in range(b.U):                                   # the checked queries of a unit: those that are kept
+        part[u] = idx[u, [i for _, i in order[u]]]
+    sub = torch.stack([sel[u][:, [i for _, i in order[u]]] for u in range(b.U)])
+    want, tol = readout_ref(b, q, part, counts_of, group, sub, table, block, d ** -0.5, None if res is None else x, torch.zeros_like(x))
+    run_readout(rs3, b, q, idx, count, group, sel, table, block, 0.0, res, out, 2)
+    assert int(b.st) == 0
+    checked = torch.zeros((b.U, b.mn), dtype=torch.bool, device="cuda")
+    for u, n in enumerate(counts):
+        checked[u] = True
+        checked[u, idx[u, :n].long()] = False              # cells that are not kept pass through
+        checked[u, part[u, :counts_of[u]].long()] = True
+    err = (out.double() - want).abs()
+    assert (err <= tol)[checked].all(), float((err - tol)[checked].max())
+    assert not out.isnan().any()
+
+
+def test_sparse_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3):
+    b = Built(rs3, U=1, H=1, d=64, m=20, n=20, window=-1, ring_frames=8, commits=8, n_ptr=0, seed=6)
+    q, idx, count, group = queries(b, 1, 400, [400])
+    nb = b.bank.blocks(64)
+    sel = torch.arange(nb, dtype=torch.int32, device="cuda").expand(1, 1, 400, nb).contiguous()
+    outs = [torch.zeros((1, b.mn, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    run_readout(rs3, b, q, idx, count, group, sel, None, 64, 0.0, None, outs[0], 1)
+    torch.cuda.synchronize()
+    assert int(b.st) == 0
+    rs3.rs3_set_wait_limit_ns(0)
+    try:
+        run_readout(rs3, b, q, idx, count, group, sel, None, 64, 0.0, None, outs[1], 1)
+        torch.cuda.synchronize()
+    finally:
+        rs3.rs3_set_wait_limit_ns(10 ** 9)
+    assert int(b.st) == rs3.RS3_ETIMEOUT
+    b.st.zero_()
+    run_readout(rs3, b, q, idx, count, group, sel, None, 64, 0.0, None, outs[1], 1)
+    assert int(b.st) == 0 and torch.equal(outs[0], outs[1])
+
+
 @pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 256), ("f32", 1, 64)])
 @pytest.mark.parametrize("same_blocks", [False, True])
 def test_sparse_readout_over_all_blocks_is_the_memory_readout(rs3, dtype, H, d, same_blocks):
