@@ -62,12 +62,17 @@ struct LiveRows {
         return true;
     }
 
-    __device__ __forceinline__ bool holds(int64_t row) const
+    // the storage rows [a, a + 64) that live, a bit each
+    __device__ __forceinline__ uint64_t mask64(int64_t a) const
     {
-        bool in = false;
+        uint64_t m = 0;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) in |= row >= start[r] && row - start[r] < len[r];
-        return in;
+        for (int r = 0; r < 4; ++r) {
+            const int lo = (int)max((int64_t)0, min((int64_t)64, start[r] - a));
+            const int hi = (int)max((int64_t)0, min((int64_t)64, start[r] + len[r] - a));
+            if (hi > lo) m |= (hi - lo == 64 ? ~0ull : (1ull << (hi - lo)) - 1ull) << lo;
+        }
+        return m;
     }
 
     // live rows among the storage rows [a, b)

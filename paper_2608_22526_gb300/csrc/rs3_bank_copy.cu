@@ -3,20 +3,20 @@
 //
 // A copy moves the kept rows of a source unit, in logical order, to the first pinned, ring
 // and pointer rows of a destination unit.  It is bound by the bytes of those rows, each read
-// once per destination and written once.  Chunks of 256 logical rows of all units form one
+// once per destination and written once.  Chunks of 64 logical rows of all units form one
 // axis that the CTAs walk in strides, because only the device knows the banks' lengths.
 //
-// With a keep mask the rows' places depend on the kept rows before them: k_keep_count counts
-// each chunk over all SMs, and the last CTA of a unit to arrive turns the counts into places and
-// the unit's new counters; k_bank_copy then moves the rows.  Without one the places are known
-// and the copy is the only launch.
+// With a keep mask the rows' places depend on the kept rows before them: k_keep_count turns the
+// mask into words of 64 rows and their counts over all SMs, and the last CTA of a unit to arrive turns
+// the counts into places and the unit's new counters; k_bank_copy then moves the rows.  Without one the
+// places are known and the copy is the only launch.
 #include "rs3_bank.cuh"
 
 #include <initializer_list>
 
 namespace {
 
-constexpr int COPY_CHUNK = 256;            // logical rows of a chunk, one per thread
+constexpr int COPY_CHUNK = 64;             // logical rows of a chunk: a word of the mask
 constexpr int COPY_THREADS = 256;
 constexpr int COPY_FLIGHT = 4;             // pieces of K and of V in flight per thread
 constexpr int COPY_UNITS = 1024;           // units whose chunk counts a CTA holds at a time
@@ -29,6 +29,7 @@ struct CopyArgs {
     const uint8_t *keep;
     int64_t keep_stride;
     int64_t *place;            // [U][chunks + 2]: kept rows before each chunk, of the pinned rows, of pinned + ring
+    uint64_t *words;           // [U][chunks]: the kept rows of each
     int64_t chunks;            // of a mask row
     int64_t row_bytes;
     int32_t U, U_src;
@@ -106,8 +107,8 @@ __device__ int64_t cta_sums(int64_t v)
 }
 
 // The destination's counters for a copy of source unit p with `cond`, `ring` and `ptr` kept
-// rows.  By the whole CTA; `before(r0, r1)` gives each thread the kept ring rows before the
-// ring rows r0 and r1 of its frame (CTA-wide calls inside are allowed).
+// rows.  By the whole CTA; `before(r0, r1)` turns the ring rows r0 and r1 where a frame begins and
+// ends into the kept ring rows before them.
 template <typename F>
 __device__ void publish(const CopyArgs &a, int u, int p, int64_t live, int64_t cond, int64_t ring, int64_t ptr, F before)
 {
@@ -143,44 +144,47 @@ __device__ void publish(const CopyArgs &a, int u, int p, int64_t live, int64_t c
     }
 }
 
-// kept rows among the mask row's [a, b), by the whole CTA; every thread gets the sum
-__device__ int64_t kept_in(const uint8_t *m, int64_t lo, int64_t hi)
-{
-    __shared__ int s_sum[COPY_THREADS / 32];
-    int n = 0;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += COPY_THREADS) n += m[i] != 0;
-    n = __reduce_add_sync(0xffffffffu, n);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = n;
-    __syncthreads();
-    int64_t t = 0;
-#pragma unroll
-    for (int w = 0; w < COPY_THREADS / 32; ++w) t += s_sum[w];
-    return t;
-}
-
-// Kept rows of each chunk (a CTA per chunk and unit, in strides); the last CTA of a unit
-// to arrive sums them up, decides whether they fit and publishes the unit's counters.
+// The mask's words and their counts: a thread takes 16 rows, four threads a chunk; the last CTA of a
+// unit to arrive sums the counts up, decides whether the rows fit and publishes the unit's counters.
 __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
 {
     pdl_wait();
     const int u = blockIdx.y;
     const CopyUnit c = copy_unit(a, u, blockIdx.x == 0 && threadIdx.x == 0);
     int64_t *place = a.place + (int64_t)u * (a.chunks + 2);
+    uint64_t *words = a.words + (int64_t)u * a.chunks;
     if (c.p < 0) {
         if (blockIdx.x == 0 && threadIdx.x == 0) place[a.chunks] = -1;
         return;
     }
     const uint8_t *m = a.keep + (int64_t)u * a.keep_stride;
+    const bool wide = (reinterpret_cast<uintptr_t>(m) & 15u) == 0;
     const int64_t n_chunks = (c.length + COPY_CHUNK - 1) / COPY_CHUNK;
-    for (int64_t ch = blockIdx.x; ch < n_chunks; ch += gridDim.x) {
-        const int64_t n = kept_in(m, ch * COPY_CHUNK, min(c.length, (ch + 1) * COPY_CHUNK));
-        if (threadIdx.x == 0) place[ch] = n;
+    for (int64_t r0 = (int64_t)blockIdx.x * (16 * COPY_THREADS); r0 < c.length; r0 += (int64_t)gridDim.x * (16 * COPY_THREADS)) {
+        const int64_t r = r0 + 16 * threadIdx.x;
+        uint32_t bits = 0;
+        if (wide && r + 16 <= c.length) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(m + r));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                    // a bit per byte, then the four side by side
+                bits |= (((__vcmpne4(w[i], 0u) & 0x08040201u) * 0x01010101u) >> 24) << (4 * i);
+        } else {
+            for (int i = 0; i < 16; ++i)
+                if (r + i < c.length) bits |= (uint32_t)(m[r + i] != 0) << i;
+        }
+        uint64_t word = (uint64_t)bits << (16 * (threadIdx.x & 3));
+        word |= __shfl_xor_sync(0xffffffffu, word, 1);
+        word |= __shfl_xor_sync(0xffffffffu, word, 2);
+        if ((threadIdx.x & 3) == 0 && r < c.length) {
+            words[r / COPY_CHUNK] = word;
+            place[r / COPY_CHUNK] = __popcll(word);
+        }
     }
     __shared__ bool s_last;
+    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
-        __threadfence();
         int64_t *arrive = a.dst.meta + (int64_t)u * a.dst.stride_words + BM_ARRIVE;
         s_last = atomicAdd(reinterpret_cast<unsigned long long *>(arrive), 1ull) == gridDim.x - 1;
         if (s_last) *arrive = 0;
@@ -188,34 +192,26 @@ __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    // exclusive sums over the chunks, a warp's 32 at a time
-    __shared__ int64_t s_total;
-    if (threadIdx.x < 32) {
-        int64_t run = 0;
-        for (int64_t c0 = 0; c0 < n_chunks; c0 += 32) {
-            const int64_t ch = c0 + threadIdx.x;
-            const int64_t v = ch < n_chunks ? __ldcg(place + ch) : 0;
-            int64_t s = v;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t t = __shfl_up_sync(0xffffffffu, s, o);
-                if (threadIdx.x >= o) s += t;
-            }
-            if (ch < n_chunks) place[ch] = run + s - v;
-            run += __shfl_sync(0xffffffffu, s, 31);
-        }
-        if (threadIdx.x == 0) s_total = run;
+    // exclusive sums over the chunks
+    __shared__ int64_t s_run;
+    int64_t run = 0;
+    for (int64_t c0 = 0; c0 < n_chunks; c0 += COPY_THREADS) {
+        const int64_t ch = c0 + threadIdx.x;
+        const int64_t v = ch < n_chunks ? __ldcg(place + ch) : 0, end = run + cta_sums(v);
+        if (ch < n_chunks) place[ch] = end - v;
+        __syncthreads();
+        if (threadIdx.x == COPY_THREADS - 1) s_run = end;
+        __syncthreads();
+        run = s_run;
     }
     __syncthreads();
     // kept rows before logical row r
     const auto before = [&](int64_t r) -> int64_t {
-        if (r >= c.length) return s_total;
         const int64_t ch = r / COPY_CHUNK;
-        return place[ch] + kept_in(m, ch * COPY_CHUNK, r);
+        return ch < n_chunks ? place[ch] + __popcll(__ldcg(words + ch) & ((1ull << (r % COPY_CHUNK)) - 1ull)) : run;
     };
-    const int64_t cond = before(c.rows.len[0]);
     const int64_t ring_end = c.rows.len[0] + c.rows.len[1] + c.rows.len[2];
-    const int64_t ring = before(ring_end) - cond, ptr = s_total - cond - ring;
+    const int64_t cond = before(c.rows.len[0]), ring = before(ring_end) - cond, ptr = run - cond - ring;
     const bool fits = cond <= a.dst.pinned_cap && ring <= a.dst.ring_cap && ptr <= a.dst.n_ptr;
     if (threadIdx.x == 0) {
         if (!fits) latch_status(a.status, RS3_ECAPACITY);
@@ -224,43 +220,32 @@ __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
     }
     if (!fits) return;
     publish(a, u, c.p, ring_end - c.rows.len[0], cond, ring, ptr, [&](int64_t &r0, int64_t &r1) {
-        // a frame's kept rows begin behind those before its first row: the whole chunks', then the rest
-        // of its chunk's, counted by a warp for each of its lanes in turn
-        const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            int64_t &r = e ? r1 : r0;
-            const int64_t x = c.rows.len[0] + r;
-            int mine = 0;
-            for (int l = 0; l < 32; ++l) {
-                const int64_t y = __shfl_sync(0xffffffffu, x, l);
-                int n = 0;
-                for (int64_t i = y / COPY_CHUNK * COPY_CHUNK + lane; i < y; i += 32) n += m[i] != 0;
-                n = __reduce_add_sync(0xffffffffu, n);
-                if (lane == l) mine = n;
-            }
-            const int64_t ch = x / COPY_CHUNK;
-            r = (ch < n_chunks ? place[ch] + mine : s_total) - cond;
-        }
+        r0 = before(c.rows.len[0] + r0) - cond;
+        r1 = before(c.rows.len[0] + r1) - cond;
     });
 }
 
 template <bool KEEP>
-__global__ void __launch_bounds__(COPY_THREADS) k_bank_copy(CopyArgs a)
+__global__ void __launch_bounds__(COPY_THREADS, 3) k_bank_copy(CopyArgs a)
 {
     pdl_wait();
     __shared__ int64_t s_first[COPY_UNITS + 1];       // chunks before each unit of the round
     __shared__ int64_t s_from[COPY_CHUNK], s_to[COPY_CHUNK];
-    __shared__ int s_wc[COPY_THREADS / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // a thread's piece of 16 bytes and its rows of a chunk: rows t / nvec, + step, ... (rows of more than
+    // 256 pieces: every row, pieces t, + 256, ...)
     const int nvec = (int)(a.row_bytes / 16);
+    const int step = nvec < COPY_THREADS ? COPY_THREADS / nvec : 1;
+    const int row0 = nvec < COPY_THREADS ? (int)threadIdx.x / nvec : 0, piece0 = (int)threadIdx.x - row0 * nvec;
     int64_t next = blockIdx.x;                        // this CTA's next chunk, counted from the round's first
+    int last = -1;                                    // the unit that c describes
+    CopyUnit c;
     for (int u0 = 0; u0 < a.U; u0 += COPY_UNITS) {
         const int n_units = min(COPY_UNITS, a.U - u0);
         __syncthreads();
         for (int i = threadIdx.x; i < n_units; i += COPY_THREADS) {
-            const CopyUnit c = copy_unit(a, u0 + i, !KEEP && blockIdx.x == 0);
-            int64_t n = (c.length + COPY_CHUNK - 1) / COPY_CHUNK;
+            const CopyUnit x = copy_unit(a, u0 + i, !KEEP && blockIdx.x == 0);
+            int64_t n = (x.length + COPY_CHUNK - 1) / COPY_CHUNK;
             if (KEEP && n > 0 && a.place[(int64_t)(u0 + i) * (a.chunks + 2) + a.chunks] < 0) n = 0;   // does not fit
             s_first[i + 1] = n;
         }
@@ -289,25 +274,19 @@ __global__ void __launch_bounds__(COPY_THREADS) k_bank_copy(CopyArgs a)
                 if (s_first[mid] <= next) lo = mid; else hi = mid;
             }
             const int u = u0 + lo;
-            const int64_t ch = next - s_first[lo], r = ch * COPY_CHUNK + threadIdx.x;
-            const CopyUnit c = copy_unit(a, u, false);
-            // a row per thread: whether it is kept, where it lies and where it goes
+            const int64_t ch = next - s_first[lo];
             const int64_t *place = a.place + (int64_t)u * (a.chunks + 2);
-            const bool mine = r < c.length && (!KEEP || a.keep[(int64_t)u * a.keep_stride + r] != 0);
-            const uint32_t bal = __ballot_sync(0xffffffffu, mine);
-            if (lane == 0) s_wc[warp] = __popc(bal);
-            __syncthreads();
-            int off = 0, n = 0;
-#pragma unroll
-            for (int w = 0; w < COPY_THREADS / 32; ++w) {
-                off += w < warp ? s_wc[w] : 0;
-                n += s_wc[w];
-            }
-            if (mine) {
-                uint32_t lm;
-                asm("mov.u32 %0, %%lanemask_lt;" : "=r"(lm));
-                const int at = off + __popc(bal & lm);
-                int64_t from = 0, x = r;
+            const uint64_t word = KEEP ? a.words[(int64_t)u * a.chunks + ch] : 0;
+            const int64_t first = KEEP ? place[ch] : ch * COPY_CHUNK;
+            if (u != last) c = copy_unit(a, u, false);
+            last = u;
+            const int64_t left = c.length - ch * COPY_CHUNK;
+            const uint64_t kept = KEEP ? word : left >= COPY_CHUNK ? ~0ull : (1ull << left) - 1ull;
+            const int n = __popcll(kept);
+            // a row per thread: where it lies and where it goes
+            if (threadIdx.x < COPY_CHUNK && (kept >> threadIdx.x & 1ull)) {
+                const int at = __popcll(kept & ((1ull << threadIdx.x) - 1ull));
+                int64_t from = 0, x = ch * COPY_CHUNK + threadIdx.x;
                 int region = 0;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -316,38 +295,38 @@ __global__ void __launch_bounds__(COPY_THREADS) k_bank_copy(CopyArgs a)
                 }
                 const int64_t n_cond = KEEP ? place[a.chunks] : c.rows.len[0];
                 const int64_t n_ring = KEEP ? place[a.chunks + 1] : n_cond + c.rows.len[1] + c.rows.len[2];
-                const int64_t rank = KEEP ? place[ch] + at : r;
-                s_from[at] = from;
-                s_to[at] = region == 0 ? rank : region < 3 ? a.dst.pinned_cap + rank - n_cond
-                                                           : a.dst.pinned_cap + a.dst.ring_cap + rank - n_ring;
+                const int64_t rank = first + at;
+                s_from[at] = from * a.row_bytes;
+                s_to[at] = (region == 0 ? rank : region < 3 ? a.dst.pinned_cap + rank - n_cond
+                                                            : a.dst.pinned_cap + a.dst.ring_cap + rank - n_ring) * a.row_bytes;
             }
             __syncthreads();
             const uint8_t *ks = a.k_src + (int64_t)c.p * a.src.rows_per_unit * a.row_bytes;
             const uint8_t *vs = a.v_src + (int64_t)c.p * a.src.rows_per_unit * a.row_bytes;
             uint8_t *kd = a.k_dst + (int64_t)u * a.dst.rows_per_unit * a.row_bytes;
             uint8_t *vd = a.v_dst + (int64_t)u * a.dst.rows_per_unit * a.row_bytes;
-            const int pieces = n * nvec;              // at most 256 rows of at most 2^20 bytes
-            for (int e0 = threadIdx.x; e0 < pieces; e0 += COPY_THREADS * COPY_FLIGHT) {
-                uint4 kv[COPY_FLIGHT], vv[COPY_FLIGHT];
+            for (int p = row0 < step ? piece0 : nvec; p < nvec; p += COPY_THREADS)
+                for (int r0 = row0; r0 < n; r0 += step * COPY_FLIGHT) {
+                    uint4 kv[COPY_FLIGHT], vv[COPY_FLIGHT];
 #pragma unroll
-                for (int f = 0; f < COPY_FLIGHT; ++f) {
-                    const int e = e0 + f * COPY_THREADS;
-                    if (e < pieces) {
-                        const int64_t at = s_from[e / nvec] * a.row_bytes + 16 * (e % nvec);
-                        kv[f] = __ldcs(reinterpret_cast<const uint4 *>(ks + at));
-                        vv[f] = __ldcs(reinterpret_cast<const uint4 *>(vs + at));
+                    for (int f = 0; f < COPY_FLIGHT; ++f) {
+                        const int r = r0 + f * step;
+                        if (r < n) {
+                            const int64_t at = s_from[r] + 16 * p;
+                            kv[f] = __ldcs(reinterpret_cast<const uint4 *>(ks + at));
+                            vv[f] = __ldcs(reinterpret_cast<const uint4 *>(vs + at));
+                        }
+                    }
+#pragma unroll
+                    for (int f = 0; f < COPY_FLIGHT; ++f) {
+                        const int r = r0 + f * step;
+                        if (r < n) {
+                            const int64_t at = s_to[r] + 16 * p;
+                            *reinterpret_cast<uint4 *>(kd + at) = kv[f];
+                            *reinterpret_cast<uint4 *>(vd + at) = vv[f];
+                        }
                     }
                 }
-#pragma unroll
-                for (int f = 0; f < COPY_FLIGHT; ++f) {
-                    const int e = e0 + f * COPY_THREADS;
-                    if (e < pieces) {
-                        const int64_t at = s_to[e / nvec] * a.row_bytes + 16 * (e % nvec);
-                        *reinterpret_cast<uint4 *>(kd + at) = kv[f];
-                        *reinterpret_cast<uint4 *>(vd + at) = vv[f];
-                    }
-                }
-            }
             __syncthreads();
         }
         next -= total;
@@ -403,7 +382,7 @@ bool overlap(const void *a, int64_t n, const void *b, int64_t m)
 extern "C" size_t rs3_bank_copy_workspace_bytes(int U, int64_t keep_stride)
 {
     if (U < 1 || keep_stride < 1) return 0;
-    return (size_t)U * (size_t)(copy_chunks(keep_stride) + 2) * 8;
+    return (size_t)U * (size_t)(2 * copy_chunks(keep_stride) + 2) * 8;
 }
 
 extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, const int32_t *parent, const uint8_t *keep,
@@ -425,6 +404,8 @@ extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, co
     if (!same && overlap(dst->meta, dst->U * dst->meta_stride, src->meta, src->U * src->meta_stride)) return RS3_EINVAL;
     if (row_bytes > (1 << 20)) return RS3_EUNSUPPORTED;
     CopyArgs a = {};
+    a.U = dst->U;
+    a.U_src = src->U;
     a.src = bank_dev(src);
     a.dst = bank_dev(dst);
     a.k_src = static_cast<const uint8_t *>(src->k_store);
@@ -436,19 +417,18 @@ extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, co
     a.keep_stride = keep_stride;
     a.place = static_cast<int64_t *>(workspace);
     a.chunks = keep ? copy_chunks(keep_stride) : 0;
+    a.words = reinterpret_cast<uint64_t *>(a.place + a.U * (a.chunks + 2));
     a.row_bytes = row_bytes;
-    a.U = dst->U;
-    a.U_src = src->U;
     a.same = same;
     a.status = status;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     // no more CTAs than chunks that full banks would have
     const int64_t most = keep ? a.chunks : (src->rows_per_unit + COPY_CHUNK - 1) / COPY_CHUNK;
-    int64_t ctas = 4ll * rs3_sm_count();
+    int64_t ctas = 3ll * rs3_sm_count();
     if (most * a.U < ctas) ctas = most * a.U > 0 ? most * a.U : 1;
     if (keep) {
-        int64_t per = (8ll * rs3_sm_count() + a.U - 1) / a.U;
-        if (per > most) per = most;
+        int64_t per = (2ll * rs3_sm_count() + a.U - 1) / a.U;
+        if (per > (most + COPY_THREADS / 4 - 1) / (COPY_THREADS / 4)) per = (most + COPY_THREADS / 4 - 1) / (COPY_THREADS / 4);
         launch_pdl(k_keep_count, dim3((unsigned)per, (unsigned)a.U), dim3(COPY_THREADS), 0, st, a);
         launch_pdl(k_bank_copy<true>, dim3((unsigned)ctas), dim3(COPY_THREADS), 0, st, a);
     } else {

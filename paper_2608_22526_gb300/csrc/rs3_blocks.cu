@@ -56,7 +56,7 @@ __device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int6
 
 // A CTA digests 32 x ITEMS pieces (16 bytes each: whole heads) of one block: thread (piece, p)
 // sums rows p, p + 8, ... of its piece, then the eight partial sums of a channel are joined
-// as ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)).  Dead rows are not read.
+// as ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)).
 template <typename T, int ITEMS>
 __global__ void __launch_bounds__(DIGEST_THREADS) k_digest(DigestArgs a)
 {
@@ -67,43 +67,65 @@ __global__ void __launch_bounds__(DIGEST_THREADS) k_digest(DigestArgs a)
     __shared__ int64_t s_block;
     const int64_t u = blockIdx.z;
     LiveRows rows;
-    if (!rows.load(a.bank, u)) {
-        if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
-        return;
-    }
     int64_t b = blockIdx.x;
     if (a.refresh >= 0) {
+        const bool sane = rows.load(a.bank, u);
+        if (!sane && threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
+        if (!sane) return;
         if (threadIdx.x == 0) s_block = refresh_block(a, rows, u, b);
         __syncthreads();
         b = s_block;
         if (b < 0) return;
     }
     const int64_t r0 = b * a.bs;
-    const int64_t n_live = rows.count(r0, r0 + a.bs);
     const int piece = threadIdx.x & 31, p = threadIdx.x >> 5;
     const int nvec = (int)(a.row_bytes / 16), v0 = blockIdx.y * 32 * ITEMS;
     const uint8_t *src = a.k_store + (u * a.bank.rows_per_unit + r0) * a.row_bytes;
+    // the rows are loaded beside the unit's counters, which then say which of them count
+    constexpr int F = 8 / ITEMS;
+    uint4 w[F][ITEMS];
+    const auto load = [&](int first) {
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            const int r = p + 8 * (first + f);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int v = v0 + piece + 32 * i;
+                w[f][i] = make_uint4(0, 0, 0, 0);
+                if (r < a.bs && r0 + r < a.bank.rows_per_unit && v < nvec)
+                    w[f][i] = __ldg(reinterpret_cast<const uint4 *>(src + r * a.row_bytes) + v);
+            }
+        }
+    };
+    load(0);
+    if (a.refresh < 0 && !rows.load(a.bank, u)) {
+        if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
+        return;
+    }
+    const uint64_t live[2] = {rows.mask64(r0) & (a.bs == 32 ? 0xffffffffull : ~0ull), a.bs > 64 ? rows.mask64(r0 + 64) : 0ull};
+    const int n_live = __popcll(live[0]) + __popcll(live[1]);
     float sum[ITEMS][N];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[i][e] = 0.f;
-#pragma unroll 4
-    for (int r = p; r < a.bs; r += 8) {
-        const bool live = rows.holds(r0 + r);
+    for (int first = 0; 8 * first < a.bs; first += F) {
+        if (first > 0) load(first);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int v = v0 + piece + 32 * i;
-            if (!live || v >= nvec) continue;
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src + r * a.row_bytes) + v);
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        for (int f = 0; f < F; ++f) {
+            const int r = p + 8 * (first + f);
+            const bool on = r < a.bs && ((r < 64 ? live[0] : live[1]) >> (r & 63) & 1ull);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (N == 8) {
-                    sum[i][2 * e] += __uint_as_float(x[e] << 16);
-                    sum[i][2 * e + 1] += __uint_as_float(x[e] & 0xffff0000u);
-                } else {
-                    sum[i][e] += __uint_as_float(x[e]);
+            for (int i = 0; i < ITEMS; ++i) {
+                const uint32_t x[4] = {w[f][i].x, w[f][i].y, w[f][i].z, w[f][i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (N == 8) {
+                        sum[i][2 * e] += on ? __uint_as_float(x[e] << 16) : 0.f;
+                        sum[i][2 * e + 1] += on ? __uint_as_float(x[e] & 0xffff0000u) : 0.f;
+                    } else {
+                        sum[i][e] += on ? __uint_as_float(x[e]) : 0.f;
+                    }
                 }
             }
         }
@@ -282,6 +304,375 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
     for (int i = want + lane; i < s.n_top; i += 32) out[i] = -1;
 }
 
+// The same on the tensor cores, for what most calls are: up to 1024 blocks in one piece, or more in
+// pieces (`splits`) of up to 1024 whose choices k_merge_blocks joins.
+//
+// A CTA scores 16 queries against its blocks: whole numbers of at most 127 are exact in bf16, and their
+// products' sums stay below 2^22, exact in the fp32 accumulators.  A lane's 16 bytes of a digest are
+// spread over four steps of the matrix instruction, and the queries' columns are taken in the same order.
+// Then a warp per query holds the scores in registers (32 per lane at most).  Of n <= 32 wanted, the n-th
+// largest of the lanes' maxima is a lower bound for the n-th largest score that leaves few more than n
+// candidates; those are compacted and cut exactly.
+constexpr int TC_ROWS = 16;                // queries of a CTA
+constexpr int TC_THREADS = 256;
+constexpr int TC_BLOCKS = 1024;            // blocks of a piece
+constexpr int TC_TOP = 64;                 // choices of a piece that the workspace has room for
+constexpr int TC_PAIRS = 3072;             // candidates of a query that are joined in shared memory
+constexpr size_t TC_SMS = 256;             // SMs that pieces are cut for, at most
+
+struct PickArgs {
+    SelectArgs a;
+    int2 *cand;                // [rows][splits][take]: (ordered score, block)
+    int32_t *n_cand;           // [rows][splits]
+    int32_t splits, piece;     // pieces of a query's blocks, blocks of a piece (a multiple of 32)
+    int32_t take;              // room for a piece's choices
+};
+
+// four bytes (signed) of w to two bf16 pairs: 128 + low seven bits, less 128 or (negative) 256
+__device__ __forceinline__ void bytes_to_bf16(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    const uint32_t x = __byte_perm(w, 0, 0x4140), y = __byte_perm(w, 0, 0x4342);    // bytes 0, 1 and 2, 3 in 16 bits each
+    asm("{\n\t.reg .b32 a, b;\n\t"
+        "lop3.b32 a, %1, 0x007f007f, 0x43004300, 0xea;\n\t"
+        "lop3.b32 b, %1, 0x00800080, 0x43004300, 0xea;\n\t"
+        "sub.rn.bf16x2 %0, a, b;\n\t}" : "=r"(lo) : "r"(x));
+    asm("{\n\t.reg .b32 a, b;\n\t"
+        "lop3.b32 a, %1, 0x007f007f, 0x43004300, 0xea;\n\t"
+        "lop3.b32 b, %1, 0x00800080, 0x43004300, 0xea;\n\t"
+        "sub.rn.bf16x2 %0, a, b;\n\t}" : "=r"(hi) : "r"(y));
+}
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t lanes_below()
+{
+    uint32_t m;
+    asm("mov.u32 %0, %%lanemask_lt;" : "=r"(m));
+    return m;
+}
+
+// The `want`-th largest of a warp's keys, bit by bit, n_at_least(x) being how many are x or more (the same
+// for all lanes); a smaller number that cuts them alike where one is found sooner.  At least `want` keys lie
+// in [least, most], so the bits that these share need no step.
+template <typename F>
+__device__ __forceinline__ uint32_t cut_at(int want, uint32_t least, uint32_t most, F n_at_least)
+{
+    const int shared = __clz(least ^ most);
+    uint32_t low = shared == 0 ? 0u : most & ~(0xffffffffu >> shared);
+    if (shared == 32) return most;
+    for (uint32_t bit = 0x80000000u >> shared; bit != 0u; bit >>= 1) {
+        const int n = n_at_least(low | bit);
+        if (n >= want) low |= bit;
+        if (n == want) return low;
+    }
+    return low;
+}
+
+// Where the choices of a query go: the list itself, or a piece's candidates.
+struct Choice {
+    int32_t *sel;
+    int2 *cand;
+    __device__ __forceinline__ void put(int at, uint32_t key, int block) const
+    {
+        if (cand) cand[at] = make_int2((int)key, block);
+        else sel[at] = block;
+    }
+};
+
+// The `want` first of n (key, block) pairs in ascending block order, by (key desc, block asc); key 0 is none,
+// and at least `want` are not.  The first 32 * HELD keys are held in registers.
+template <int HELD, typename Load>
+__device__ __forceinline__ void choose(int n, int want, const Choice &out, Load load)
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t k[HELD], least = 0xffffffffu, most = 0u;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        k[i] = 32 * i + lane < n ? (uint32_t)load(32 * i + lane).x : 0u;
+        most = max(most, k[i]);
+        least = k[i] > 0u ? min(least, k[i]) : least;
+    }
+    for (int i = 32 * HELD + lane; i < n; i += 32) {
+        const uint32_t x = (uint32_t)load(i).x;
+        most = max(most, x);
+        least = x > 0u ? min(least, x) : least;
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    least = __reduce_min_sync(0xffffffffu, least);
+    const auto n_at_least = [&](uint32_t x) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) c += k[i] >= x;
+        for (int i = 32 * HELD + lane; i < n; i += 32) c += (uint32_t)load(i).x >= x;
+        return (int)__reduce_add_sync(0xffffffffu, c);
+    };
+    const uint32_t cut = n > want ? cut_at(want, least, most, n_at_least) : 0u;
+    int equal = n > want ? want - (cut == 0xffffffffu ? 0 : n_at_least(cut + 1u)) : n, at = 0;
+    for (int i0 = 0; i0 < n && at < want; i0 += 32) {
+        const int i = i0 + lane;
+        const int2 e = i < n ? load(i) : make_int2(0, 0);
+        const uint32_t x = (uint32_t)e.x, same = __ballot_sync(0xffffffffu, x > 0 && x == cut);
+        const bool take = x > 0 && (x > cut || (x == cut && __popc(same & lanes_below()) < equal));
+        const uint32_t bal = __ballot_sync(0xffffffffu, take);
+        if (take) out.put(at + __popc(bal & lanes_below()), x, e.y);
+        at += __popc(bal);
+        equal -= min(equal, __popc(same));
+    }
+}
+
+__global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
+{
+    pdl_wait();
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ uint32_t s_live[TC_BLOCKS / 32];
+    const SparseArgs &s = p.a.s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int tiles = (s.k_max + TC_ROWS - 1) / TC_ROWS;
+    const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles, h = blockIdx.y, u = blockIdx.z;
+    int cnt, g;
+    LiveRows rows;
+    if (!sparse_unit(s, u, threadIdx.x == 0, cnt, g, rows)) return;
+    const int j0 = tile * TC_ROWS, nq = min(TC_ROWS, cnt - j0);
+    if (nq <= 0) return;
+    const int lo = split * p.piece, n = min(p.piece, s.nb - lo);           // this piece's blocks
+    const int stride = p.piece + 8;                                        // of a query's keys
+    uint32_t *s_keys = reinterpret_cast<uint32_t *>(smem);
+    const int width = s.d < 64 ? 64 : s.d, q_row = 2 * width + 16;         // columns, bytes of a query
+    uint8_t *s_q = smem + TC_ROWS * stride * 4;
+    // this warp's steps: 16 blocks, then 64 columns after 64; a step's digests are loaded one step ahead
+    const int r = lane >> 2, t = lane & 3;
+    const int64_t dig = ((int64_t)u * s.H + h) * s.nb + lo;
+    int b0 = warp * 16, k0 = 0;
+    uint4 w[2];
+    const auto load_step = [&](uint4 (&v)[2], int b, int k) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            v[x] = make_uint4(0, 0, 0, 0);
+            if (b + 8 * x + r < n && k + 16 * t < s.d)
+                v[x] = __ldg(reinterpret_cast<const uint4 *>(p.a.digest + (dig + b + 8 * x + r) * s.d + k + 16 * t));
+        }
+    };
+    load_step(w, b0, k0);
+    // which blocks hold a live row
+    for (int b = threadIdx.x; b < p.piece; b += TC_THREADS) {
+        const int64_t r0 = (int64_t)(lo + b) * s.bs;
+        const uint32_t bal = __ballot_sync(0xffffffffu, b < n && rows.count(r0, r0 + s.bs) > 0);
+        if (lane == 0) s_live[b >> 5] = bal;
+    }
+    // the queries in 8 bits, held as bf16; a warp takes two
+    for (int r = warp; r < TC_ROWS; r += TC_THREADS / 32) {
+        const int cell = r < nq ? s.idx[(int64_t)u * s.k_max + j0 + r] : 0;
+        const bool ok = r < nq && cell >= 0 && cell < s.mn;
+        if (r < nq && !ok && lane == 0) latch_status(s.status, RS3_EINVAL);
+        float x[8], m = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 32 * i;
+            float x0 = 0.f, x1 = 0.f;
+            if (ok && 2 * c < s.d) {
+                const int64_t at = ((int64_t)g * s.mn + cell) * (s.H * s.d) + h * s.d + 2 * c;
+                if (p.a.bf16) {
+                    const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(static_cast<const uint16_t *>(s.q) + at));
+                    x0 = __uint_as_float(w << 16);
+                    x1 = __uint_as_float(w & 0xffff0000u);
+                } else {
+                    const float2 w = __ldg(reinterpret_cast<const float2 *>(static_cast<const float *>(s.q) + at));
+                    x0 = w.x;
+                    x1 = w.y;
+                }
+                if (s.rope) {
+                    const float2 f = __ldg(reinterpret_cast<const float2 *>(s.rope + (int64_t)cell * s.d) + c);
+                    const float y0 = __fsub_rn(__fmul_rn(x0, f.x), __fmul_rn(x1, f.y));
+                    x1 = __fadd_rn(__fmul_rn(x0, f.y), __fmul_rn(x1, f.x));
+                    x0 = y0;
+                }
+            }
+            x[2 * i] = x0;
+            x[2 * i + 1] = x1;
+            m = fmaxf(m, fmaxf(fabsf(x0), fabsf(x1)));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const EightBits e(m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = lane + 32 * i;
+            if (2 * c < width) {
+                uint32_t w;
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"((float)e(x[2 * i + 1])), "f"((float)e(x[2 * i])));
+                *reinterpret_cast<uint32_t *>(s_q + r * q_row + 4 * c) = w;
+            }
+        }
+    }
+    __syncthreads();
+    float c[2][4], st[2][2];
+    for (; b0 < p.piece;) {
+        if (k0 == 0) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int b = b0 + 8 * x + 2 * t + y;
+                    st[x][y] = b < n ? __ldg(p.a.step + dig + b) : 0.f;
+                }
+            }
+        }
+        const int b1 = k0 + 64 < width ? b0 : b0 + TC_THREADS / 2, k1 = k0 + 64 < width ? k0 + 64 : 0;
+        uint4 w1[2];
+        load_step(w1, b1, k1);
+        const uint8_t *qa = s_q + r * q_row + 2 * (k0 + 16 * t);
+        uint4 qv[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) qv[x][y] = *reinterpret_cast<const uint4 *>(qa + 8 * x * q_row + 16 * y);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            uint32_t b[4][2];
+            bytes_to_bf16(w[x].x, b[0][0], b[0][1]);
+            bytes_to_bf16(w[x].y, b[1][0], b[1][1]);
+            bytes_to_bf16(w[x].z, b[2][0], b[2][1]);
+            bytes_to_bf16(w[x].w, b[3][0], b[3][1]);
+            mma_bf16(c[x], qv[0][0].x, qv[1][0].x, qv[0][0].y, qv[1][0].y, b[0][0], b[0][1]);
+            mma_bf16(c[x], qv[0][0].z, qv[1][0].z, qv[0][0].w, qv[1][0].w, b[1][0], b[1][1]);
+            mma_bf16(c[x], qv[0][1].x, qv[1][1].x, qv[0][1].y, qv[1][1].y, b[2][0], b[2][1]);
+            mma_bf16(c[x], qv[0][1].z, qv[1][1].z, qv[0][1].w, qv[1][1].w, b[3][0], b[3][1]);
+        }
+        if (k1 == 0) {
+            // this lane holds blocks 8 x + 2 t, + 1 of queries r and r + 8
+            const uint32_t live = s_live[b0 >> 5] >> (b0 & 31);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const bool on0 = live >> (8 * x + 2 * t) & 1u, on1 = live >> (8 * x + 2 * t + 1) & 1u;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint2 key = make_uint2(on0 ? order_bits(c[x][2 * y] * st[x][0]) : 0u, on1 ? order_bits(c[x][2 * y + 1] * st[x][1]) : 0u);
+                    *reinterpret_cast<uint2 *>(s_keys + (r + 8 * y) * stride + b0 + 8 * x + 2 * t) = key;
+                }
+            }
+        }
+        b0 = b1;
+        k0 = k1;
+        w[0] = w1[0];
+        w[1] = w1[1];
+    }
+    __syncthreads();
+    int n_live = 0;
+    for (int i = lane; i < p.piece / 32; i += 32) n_live += __popc(s_live[i]);
+    n_live = __reduce_add_sync(0xffffffffu, n_live);
+    const int want = min(s.n_top, n_live);
+    for (int q = warp; q < nq; q += TC_THREADS / 32) {
+        const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j0 + q;
+        const Choice out = {p.a.sel + row * s.n_top, p.splits > 1 ? p.cand + (row * p.splits + split) * p.take : nullptr};
+        uint32_t *key = s_keys + q * stride;
+        uint32_t k[TC_BLOCKS / 32], top = 0u;
+#pragma unroll
+        for (int i = 0; i < TC_BLOCKS / 32; ++i) {
+            k[i] = 32 * i < p.piece ? key[32 * i + lane] : 0u;
+            top = max(top, k[i]);
+        }
+        const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+        bool done = false;
+        if (want > 0 && want <= 32) {
+            // the want-th largest of the lanes' maxima, or 1 where fewer lanes hold a live block
+            uint32_t bound = 1u;
+            if (__popc(__ballot_sync(0xffffffffu, top > 0u)) >= want)
+                bound = max(1u, cut_at(want, __reduce_min_sync(0xffffffffu, top), most,
+                                       [&](uint32_t x) { return __popc(__ballot_sync(0xffffffffu, top >= x)); }));
+            __syncwarp();
+            int2 *pair = reinterpret_cast<int2 *>(key);    // room for half as many (key, block) pairs in the query's own row
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < TC_BLOCKS / 32; ++i) {
+                const uint32_t bal = __ballot_sync(0xffffffffu, k[i] >= bound);
+                if (bal != 0u) {
+                    const int to = at + __popc(bal & lanes_below());
+                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)k[i], lo + 32 * i + lane);
+                    at += __popc(bal);
+                }
+            }
+            __syncwarp();
+            done = 2 * at <= p.piece;
+            if (done) choose<4>(at, want, out, [&](int i) { return pair[i]; });
+        }
+        if (!done && want > 0) {
+            const auto n_at_least = [&](uint32_t x) {
+                int c = 0;
+#pragma unroll
+                for (int i = 0; i < TC_BLOCKS / 32; ++i) c += k[i] >= x;
+                return (int)__reduce_add_sync(0xffffffffu, c);
+            };
+            const uint32_t cut = cut_at(want, 1u, most, n_at_least);
+            int equal = want - (cut == 0xffffffffu ? 0 : n_at_least(cut + 1u)), at = 0;
+#pragma unroll
+            for (int i = 0; i < TC_BLOCKS / 32; ++i) {
+                const uint32_t same = __ballot_sync(0xffffffffu, k[i] == cut && k[i] > 0);
+                const bool take = k[i] > cut || (k[i] == cut && k[i] > 0 && __popc(same & lanes_below()) < equal);
+                const uint32_t bal = __ballot_sync(0xffffffffu, take);
+                if (take) out.put(at + __popc(bal & lanes_below()), k[i], lo + 32 * i + lane);
+                at += __popc(bal);
+                equal -= min(equal, __popc(same));
+            }
+        }
+        if (p.splits > 1) {
+            if (lane == 0) p.n_cand[row * p.splits + split] = want;
+        } else {
+            for (int i = want + lane; i < s.n_top; i += 32) out.sel[i] = -1;
+        }
+    }
+}
+
+// The choices of a query's pieces joined: a warp per query.  The pieces follow one another, so their
+// candidates are in ascending block order.
+__global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
+{
+    pdl_wait();
+    extern __shared__ int2 s_pairs[];                      // [4][room]
+    const SparseArgs &s = p.a.s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int j = blockIdx.x * 4 + warp, h = blockIdx.y, u = blockIdx.z;
+    const int cnt = s.count[u], g = s.unit_group[u];
+    if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || j >= cnt) return;
+    LiveRows rows;
+    if (!rows.load(s.bank, u)) return;
+    const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j;
+    int2 *pair = s_pairs + warp * room;
+    // places without a candidate hold key 0
+    const int n = p.splits * p.take;
+    int some = 0;
+#pragma unroll 4
+    for (int i = lane; i < n; i += 32) {
+        const int x = i / p.take;
+        const bool on = i - x * p.take < p.n_cand[row * p.splits + x];
+        const int2 e = p.cand[row * p.splits * p.take + i];
+        pair[i] = on ? e : make_int2(0, 0);
+        some += on;
+    }
+    some = __reduce_add_sync(0xffffffffu, some);
+    __syncwarp();
+    const int want = min(s.n_top, some);
+    const Choice out = {p.a.sel + row * s.n_top, nullptr};
+    if (want > 0) choose<12>(n, want, out, [&](int i) { return pair[i]; });
+    for (int i = want + lane; i < s.n_top; i += 32) out.sel[i] = -1;
+}
+
+// Pieces of a query's blocks: as many as their size needs, more where that leaves SMs idle.
+int64_t select_splits(int64_t U, int64_t H, int64_t k_max, int64_t nb, int64_t n_top, int64_t sms)
+{
+    const int64_t tiles = U * H * ((k_max + TC_ROWS - 1) / TC_ROWS), least = (nb + TC_BLOCKS - 1) / TC_BLOCKS;
+    int64_t n = tiles > 0 ? (2 * sms + tiles - 1) / tiles : 1;
+    if (n > nb / 256) n = nb / 256;
+    if (n > TC_PAIRS / n_top) n = TC_PAIRS / n_top;        // 48 x 64 at the most blocks and choices
+    return n > least ? n : least > 0 ? least : 1;
+}
+
 }  // namespace
 
 extern "C" int64_t rs3_bank_blocks(const rs3_bank *bank, int block)
@@ -329,7 +720,10 @@ extern "C" rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refre
 extern "C" size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int n_blocks)
 {
     if (U < 1 || H < 1 || k_max < 0 || n_blocks < 0) return 0;
-    return 16;
+    // rows x pieces: beyond what the blocks need, pieces only fill up two CTAs of 16 rows per SM
+    const size_t rows = (size_t)U * (size_t)H * (size_t)k_max, least = ((size_t)n_blocks + TC_BLOCKS - 1) / TC_BLOCKS;
+    const size_t pieces = 4 * TC_SMS * TC_ROWS + (least > 1 ? rows * (least + 1) : 0);
+    return 256 + align_up(pieces * 4, 256) + pieces * TC_TOP * sizeof(int2);
 }
 
 extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -346,16 +740,44 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     if (a.s.nb > SELECT_MAX_BLOCKS) return RS3_EUNSUPPORTED;
     if (workspace_bytes < rs3_block_select_workspace_bytes(a.s.U, H, k_max, a.s.nb)) return RS3_ECAPACITY;
     if (k_max == 0) return RS3_OK;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     a.digest = digest;
     a.step = step;
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
+    const int sms = rs3_sm_count() < (int)TC_SMS ? rs3_sm_count() : (int)TC_SMS;
+    int64_t splits = select_splits(a.s.U, H, k_max, a.s.nb, n_top, sms);
+    if (n_top > TC_TOP && a.s.nb <= TC_BLOCKS) splits = 1;
+    if (splits == 1 || n_top <= TC_TOP) {
+        PickArgs p = {};
+        p.a = a;
+        p.splits = (int32_t)splits;
+        p.piece = (int32_t)align_up((size_t)(a.s.nb + splits - 1) / splits, 32);
+        if (p.piece == 0) p.piece = 32;
+        p.take = n_top < p.piece ? n_top : p.piece;
+        const int64_t pieces = (int64_t)a.s.U * H * k_max * splits;
+        p.n_cand = static_cast<int32_t *>(workspace);
+        p.cand = reinterpret_cast<int2 *>(static_cast<uint8_t *>(workspace) + align_up((size_t)pieces * 4, 256));
+        const size_t smem = (size_t)TC_ROWS * ((size_t)(p.piece + 8) * 4 + 2 * (d < 64 ? 64 : d) + 16);
+        rs3_status r = rs3_kernel_smem((const void *)k_score_blocks, smem);
+        if (r != RS3_OK) return r;
+        const dim3 grid((unsigned)((k_max + TC_ROWS - 1) / TC_ROWS * splits), (unsigned)H, (unsigned)a.s.U);
+        launch_pdl(k_score_blocks, grid, dim3(TC_THREADS), smem, st, p);
+        if (splits > 1) {
+            const int room = p.splits * p.take;
+            const size_t bytes = 4 * (size_t)room * sizeof(int2);
+            r = rs3_kernel_smem((const void *)k_merge_blocks, bytes);
+            if (r != RS3_OK) return r;
+            launch_pdl(k_merge_blocks, dim3((unsigned)((k_max + 3) / 4), (unsigned)H, (unsigned)a.s.U), dim3(128), bytes, st, p, room);
+        }
+        return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+    }
     a.qt = 8;
     while (a.qt > 1 && (int64_t)a.qt * a.s.nb * 4 > SELECT_KEYS_BYTES) a.qt >>= 1;
     const size_t smem = (size_t)a.qt * (size_t)a.s.nb * 4;
     const rs3_status r = rs3_kernel_smem((const void *)k_block_select, smem);
     if (r != RS3_OK) return r;
     const dim3 grid((unsigned)((k_max + a.qt - 1) / a.qt), (unsigned)H, (unsigned)a.s.U);
-    launch_pdl(k_block_select, grid, dim3(SELECT_THREADS), smem, reinterpret_cast<cudaStream_t>(stream), a);
+    launch_pdl(k_block_select, grid, dim3(SELECT_THREADS), smem, st, a);
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }

@@ -69,16 +69,13 @@ struct Row<float> {
     }
 };
 
-constexpr int GATHER_WARPS = 4;
-constexpr int GATHER_FLIGHT = 4;           // rows in flight per lane group
-
 // A CTA per (query, head): its warps take the listed blocks in turn.  L lanes hold a row (ITEMS
 // pieces of 16 bytes each), so a warp reads 32 / L rows at once; scores are summed over the L lanes,
 // the softmax runs online per warp in the log2 domain, and the warps' results are joined at the end.
-template <typename T, int ITEMS>
+template <typename T, int ITEMS, int GATHER_WARPS>
 __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs a, int L)
 {
-    constexpr int N = Row<T>::N;
+    constexpr int N = Row<T>::N, GATHER_FLIGHT = 8 / ITEMS;    // rows in flight per lane group
     pdl_wait();
     __shared__ float s_o[GATHER_WARPS][256];
     __shared__ float s_m[GATHER_WARPS], s_l[GATHER_WARPS];
@@ -129,6 +126,8 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
             if (lane == 0) latch_status(s.status, RS3_EINVAL);
             continue;
         }
+        const int64_t row0 = (int64_t)b * s.bs;
+        const uint64_t on[2] = {rows.mask64(row0) & (s.bs == 32 ? 0xffffffffull : ~0ull), s.bs > 64 ? rows.mask64(row0 + 64) : 0ull};
         for (int r0 = 0; r0 < s.bs; r0 += groups * GATHER_FLIGHT) {
             bool live[GATHER_FLIGHT];
             float x[GATHER_FLIGHT], top = -INFINITY;
@@ -136,8 +135,8 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 #pragma unroll
             for (int f = 0; f < GATHER_FLIGHT; ++f) {
                 const int r = r0 + f * groups + group;
-                const int64_t row = (int64_t)b * s.bs + r;
-                live[f] = r < s.bs && rows.holds(row);
+                const int64_t row = row0 + r;
+                live[f] = r < s.bs && ((r < 64 ? on[0] : on[1]) >> (r & 63) & 1ull);
 #pragma unroll
                 for (int i = 0; i < ITEMS; ++i) {
                     const int64_t at = row * D + (sub + L * i) * N;
@@ -228,7 +227,7 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 // by block
 // ---------------------------------------------------------------------------
 constexpr int TILE = 64;                   // queries of an item
-constexpr int LIST_THREADS = 1024;
+constexpr int LIST_THREADS = 512;
 constexpr int LIST_BINS = 8192;            // blocks that a CTA counts
 constexpr int MAX_SEGMENTS = 1024;         // (unit, head, segment) triples that a CTA of the attention holds at a time
 constexpr int CHUNK_ITEMS = 64;            // items whose records it holds
@@ -275,7 +274,7 @@ __device__ __forceinline__ void each_entry(const int32_t *list, int n, F f)
 // blocks, gives every block a run of list entries and its items, and fills them in.  Entries of one block
 // come in any order; each is computed by itself, so the result does not depend on it.  Out of place the
 // launch's other CTAs write out = residual (or zeros) on every cell.
-__global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
+__global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
     if ((int)blockIdx.x >= w.list_ctas) {
@@ -362,12 +361,9 @@ __global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, Bloc
             it.uh = uh;
             it.part = (lo + b) * w.parts + p;
             const int64_t r0 = (int64_t)it.part * pr;
-            it.live[0] = 0xffffffffu;
-            it.live[1] = pr > 32 ? 0xffffffffu : 0u;
-            if (rows.count(r0, r0 + pr) < pr) {
-                it.live[0] = it.live[1] = 0u;
-                for (int r = 0; r < pr; ++r) it.live[r >> 5] |= (uint32_t)rows.holds(r0 + r) << (r & 31);
-            }
+            const uint64_t live = rows.mask64(r0);
+            it.live[0] = (uint32_t)live;
+            it.live[1] = pr > 32 ? (uint32_t)(live >> 32) : 0u;
             for (int e = 0; e < n; e += TILE) {
                 it.first = first + e;
                 it.n = min(TILE, n - e);
@@ -685,22 +681,26 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
     const int64_t base = (((int64_t)u * s.H + h) * s.k_max + j) * s.n_top;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
-    const int n = here ? s.n_top * w.parts : 0;
-    constexpr int F = 8;                               // results in flight
+    // all of a query's loads go out together: what an entry without a block left in its place is not used
+    const int n = j < cnt ? s.n_top * w.parts : 0;
+    constexpr int F = 4;                               // results in flight
     for (int t0 = part & 3; t0 < n; t0 += 4 * F) {
         float2 ml[F];
         float4 v[F];
+        int b[F];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            const int t = t0 + 4 * f;
-            const int b = t < n ? __ldg(a.sel + base + (w.parts == 2 ? t >> 1 : t)) : -1;
-            ml[f] = make_float2(-INFINITY, 0.f);
-            v[f] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (b >= 0 && b < s.nb) {
-                ml[f] = w.ml[base * w.parts + t];
-                v[f] = __ldcs(reinterpret_cast<const float4 *>(w.o + (base * w.parts + t) * D) + sub);
-            }
+            const int t = min(t0 + 4 * f, n - 1);
+            b[f] = __ldg(a.sel + base + (w.parts == 2 ? t >> 1 : t));
+            ml[f] = __ldg(w.ml + base * w.parts + t);
+            v[f] = __ldcs(reinterpret_cast<const float4 *>(w.o + (base * w.parts + t) * D) + sub);
         }
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+            if (!here || t0 + 4 * f >= n || b[f] < 0 || b[f] >= s.nb) {
+                ml[f] = make_float2(-INFINITY, 0.f);
+                v[f] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
         float top = m;
 #pragma unroll
         for (int f = 0; f < F; ++f) top = fmaxf(top, ml[f].x);
@@ -755,9 +755,9 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
     WorkLayout l = {};
     const int64_t uh = U * H, pairs = k_max * n_top;
     const int64_t least = nb > LIST_BINS ? (nb + LIST_BINS - 1) / LIST_BINS : 1;
-    // lists are made by about two CTAs per SM, of no fewer than 64 blocks each
+    // lists are made by about a CTA per SM, of no fewer than 64 blocks each
     l.segments = least;
-    while (uh * l.segments < 256 && nb / (2 * l.segments) >= 64) l.segments *= 2;
+    while (uh * l.segments < 128 && nb / (2 * l.segments) >= 64) l.segments *= 2;
     l.bins = (nb + l.segments - 1) / l.segments;
     l.max_items = ((nb < pairs ? nb : pairs) + pairs / TILE + 1) * parts;
     size_t at = 0;
@@ -882,9 +882,17 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
     } else if (k_max > 0) {
         const int pieces = d * (int)elem_bytes(dtype) / 16;
         const dim3 grid((unsigned)k_max, (unsigned)H, (unsigned)a.s.U);
-        void (*kern)(AttendArgs, int) = dtype == RS3_BF16 ? k_attend_gather<uint16_t, 1>
-                                        : pieces > 32     ? k_attend_gather<float, 2> : k_attend_gather<float, 1>;
-        launch_pdl(kern, grid, dim3(32 * GATHER_WARPS), 0, st, a, pieces > 32 ? 32 : pieces);
+        // the fewer the queries, the more warps share a query's blocks
+        const int64_t ctas = (int64_t)k_max * H * a.s.U;
+        const int warps = ctas <= rs3_sm_count() ? 16 : ctas <= 4ll * rs3_sm_count() ? 8 : 4;
+        void (*kern)(AttendArgs, int);
+        if (dtype == RS3_BF16)
+            kern = warps == 16 ? k_attend_gather<uint16_t, 1, 16> : warps == 8 ? k_attend_gather<uint16_t, 1, 8> : k_attend_gather<uint16_t, 1, 4>;
+        else if (pieces <= 32)
+            kern = warps == 16 ? k_attend_gather<float, 1, 16> : warps == 8 ? k_attend_gather<float, 1, 8> : k_attend_gather<float, 1, 4>;
+        else
+            kern = warps == 16 ? k_attend_gather<float, 2, 16> : warps == 8 ? k_attend_gather<float, 2, 8> : k_attend_gather<float, 2, 4>;
+        launch_pdl(kern, grid, dim3(32 * warps), 0, st, a, pieces > 32 ? 32 : pieces);
     }
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }

@@ -460,7 +460,9 @@ def test_select_is_exact(rs3, dtype, H, d, n_top, block, commits, rope):
         assert np.array_equal(sel.cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("rows,n_top,block", [(70_000, 32, 64), (260_000, 7, 32), (400_000, 64, 32), (49_152 * 32 - 64, 3, 32), (300, 1024, 32)])
+@pytest.mark.parametrize("rows,n_top,block", [(70_000, 32, 64), (260_000, 7, 32), (400_000, 64, 32), (49_152 * 32 - 64, 3, 32), (300, 1024, 32),
+                                              (49_152 * 32 - 64, 64, 32), (32_700, 40, 32), (32_700, 1024, 32), (33_000, 65, 32),
+                                              (200_000, 65, 32), (200_000, 1024, 64)])
 def test_select_over_many_blocks(rs3, rows, n_top, block):
     """Thousands of blocks, digests and steps given: few different scores, so most choices are ties."""
     d, H, mn = 16, 1, 64
