@@ -192,14 +192,24 @@ __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    // exclusive sums over the chunks
+    // exclusive sums over the chunks, 16 in a row per thread
     __shared__ int64_t s_run;
+    constexpr int PER = 16;
     int64_t run = 0;
-    for (int64_t c0 = 0; c0 < n_chunks; c0 += COPY_THREADS) {
-        const int64_t ch = c0 + threadIdx.x;
-        const int64_t v = ch < n_chunks ? __ldcg(place + ch) : 0, end = run + cta_sums(v);
-        if (ch < n_chunks) place[ch] = end - v;
-        __syncthreads();
+    for (int64_t c0 = 0; c0 < n_chunks; c0 += PER * COPY_THREADS) {
+        const int64_t ch = c0 + PER * threadIdx.x;
+        int32_t v[PER], n = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = ch + i < n_chunks ? (int32_t)__ldcg(place + ch + i) : 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) n += v[i];
+        const int64_t end = run + cta_sums(n);
+        int64_t at = end - n;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (ch + i < n_chunks) place[ch + i] = at;
+            at += v[i];
+        }
         if (threadIdx.x == COPY_THREADS - 1) s_run = end;
         __syncthreads();
         run = s_run;

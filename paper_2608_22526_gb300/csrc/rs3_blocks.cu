@@ -19,27 +19,38 @@ struct DigestArgs {
     int8_t *digest;
     float *step;
     int32_t *status;
-    int64_t row_bytes;
+    int64_t row_bytes, visits; // blocks to visit
     int32_t H, d, bs, nb, refresh;
 };
 
-// Blocks that a refresh of the newest frames visits: those of the frames' rows (two runs when
-// the ring wraps), then those of the ring's oldest and newest rows and of its two ends.  Frames
-// given up or overwritten since leave dead rows beside live ones only there.
-__device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int64_t u, int64_t t)
+// Rows of the newest `refresh` ring frames; by a whole warp.
+__device__ int64_t fresh_rows(const DigestArgs &a, int64_t u)
 {
     const int64_t *mu = a.bank.meta + u * a.bank.stride_words;
     const int64_t *fl = mu + BM_HEADER_WORDS + a.bank.max_frames;
-    const int64_t nf = mu[BM_NFRAMES], oldest = mu[BM_OLDEST];
-    const int64_t live = rows.len[1] + rows.len[2];
-    int64_t fresh = 0;
-    for (int64_t i = 0; i < a.refresh && i < nf; ++i) fresh += fl[(oldest + nf - 1 - i) % a.bank.max_frames];
-    fresh = min(live, max((int64_t)0, fresh));
-    const int64_t cap = a.bank.ring_cap, base = a.bank.pinned_cap;
+    const int64_t nf = min(mu[BM_NFRAMES], (int64_t)a.bank.max_frames), oldest = mu[BM_OLDEST];
+    int64_t n = 0;
+    for (int64_t i = threadIdx.x & 31; i < a.refresh && i < nf; i += 32) {
+        int64_t slot = oldest + nf - 1 - i;
+        if (slot >= a.bank.max_frames) slot -= a.bank.max_frames;
+        n += fl[slot];
+    }
+    return warp_sum(n);
+}
+
+// Blocks that a refresh of the newest frames visits: those of the frames' `fresh` rows (two runs when
+// the ring wraps), then those of the ring's two ends and of its oldest and newest rows.  Frames
+// given up or overwritten since leave dead rows beside live ones only there.  -1 behind the last.
+__device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int64_t fresh, int64_t t)
+{
+    const int64_t live = rows.len[1] + rows.len[2], cap = a.bank.ring_cap, base = a.bank.pinned_cap;
     if (cap == 0) return -1;
-    const int64_t tail = live > 0 ? (rows.start[1] - base + live) % cap : 0;      // one past the newest row
-    const int64_t from = live > 0 ? (tail - fresh + cap) % cap : 0;
-    int64_t runs[2][2] = {{from, min(from + fresh, cap)}, {0, from + fresh - cap}};
+    fresh = min(live, max((int64_t)0, fresh));
+    // one past the newest row, and the first fresh one
+    int64_t tail = live > 0 ? rows.start[1] - base + live : 0;
+    tail -= tail >= cap ? cap : 0;
+    const int64_t from = tail - fresh + (tail < fresh ? cap : 0);
+    const int64_t runs[2][2] = {{from, min(from + fresh, cap)}, {0, from + fresh - cap}};
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         if (runs[r][1] <= runs[r][0]) continue;
@@ -50,119 +61,133 @@ __device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int6
     if (t == 0) return base / a.bs;
     if (t == 1) return (base + cap - 1) / a.bs;
     if (live > 0 && t == 2) return rows.start[1] / a.bs;
-    if (live > 0 && t == 3) return (base + (tail + cap - 1) % cap) / a.bs;
+    if (live > 0 && t == 3) return (base + (tail == 0 ? cap : tail) - 1) / a.bs;
     return -1;
 }
 
-// A CTA digests 32 x ITEMS pieces (16 bytes each: whole heads) of one block: thread (piece, p)
-// sums rows p, p + 8, ... of its piece, then the eight partial sums of a channel are joined
-// as ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)).
+// A CTA digests 32 x ITEMS pieces (16 bytes each: whole heads) of blocks of a unit, one after another: thread
+// (piece, p) sums rows p, p + 8, ... of its piece, then the eight partial sums of a channel are joined
+// as ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)).  The next block's rows are loaded while one is joined, and which
+// rows live is worked out for 32 blocks at a time, a thread each: per block and thread that arithmetic took
+// half of the kernel's instructions (all blocks of eight banks: 112 us).
+constexpr int DIGEST_BLOCKS = 32;
+
 template <typename T, int ITEMS>
-__global__ void __launch_bounds__(DIGEST_THREADS) k_digest(DigestArgs a)
+__global__ void __launch_bounds__(DIGEST_THREADS, 3) k_digest(DigestArgs a)
 {
-    constexpr int N = 16 / sizeof(T), COLS = 32 * ITEMS * N;
+    constexpr int N = 16 / sizeof(T), COLS = 32 * ITEMS * N, F = 8 / ITEMS;
     pdl_wait();
     __shared__ float s_sum[8][COLS];
     __shared__ float s_max[DIGEST_THREADS / 32];
-    __shared__ int64_t s_block;
+    __shared__ int32_t s_block[DIGEST_BLOCKS];
+    __shared__ uint64_t s_live[DIGEST_BLOCKS][2];
     const int64_t u = blockIdx.z;
     LiveRows rows;
-    int64_t b = blockIdx.x;
-    if (a.refresh >= 0) {
-        const bool sane = rows.load(a.bank, u);
-        if (!sane && threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
-        if (!sane) return;
-        if (threadIdx.x == 0) s_block = refresh_block(a, rows, u, b);
-        __syncthreads();
-        b = s_block;
-        if (b < 0) return;
+    int64_t fresh = 0;                                         // (the first warp's)
+    if (threadIdx.x < DIGEST_BLOCKS && a.refresh > 0) fresh = fresh_rows(a, u);
+    if (threadIdx.x < DIGEST_BLOCKS && !rows.load(a.bank, u)) {
+        if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
+        rows.start[0] = -1;                                    // no block is visited
     }
-    const int64_t r0 = b * a.bs;
+    const bool sane = !(threadIdx.x < DIGEST_BLOCKS && rows.start[0] < 0);
+    if (!__syncthreads_and(sane)) return;
     const int piece = threadIdx.x & 31, p = threadIdx.x >> 5;
     const int nvec = (int)(a.row_bytes / 16), v0 = blockIdx.y * 32 * ITEMS;
-    const uint8_t *src = a.k_store + (u * a.bank.rows_per_unit + r0) * a.row_bytes;
-    // the rows are loaded beside the unit's counters, which then say which of them count
-    constexpr int F = 8 / ITEMS;
-    uint4 w[F][ITEMS];
-    const auto load = [&](int first) {
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            const int r = p + 8 * (first + f);
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int v = v0 + piece + 32 * i;
-                w[f][i] = make_uint4(0, 0, 0, 0);
-                if (r < a.bs && r0 + r < a.bank.rows_per_unit && v < nvec)
-                    w[f][i] = __ldg(reinterpret_cast<const uint4 *>(src + r * a.row_bytes) + v);
-            }
+    const uint8_t *unit = a.k_store + u * a.bank.rows_per_unit * a.row_bytes;
+    for (int64_t t0 = blockIdx.x; t0 < a.visits; t0 += (int64_t)gridDim.x * DIGEST_BLOCKS) {
+        // this CTA's next 32 blocks
+        if (threadIdx.x < DIGEST_BLOCKS) {
+            const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
+            const int64_t b = t >= a.visits ? -1 : a.refresh < 0 ? t : refresh_block(a, rows, fresh, t);
+            s_block[threadIdx.x] = (int32_t)b;
+            s_live[threadIdx.x][0] = b < 0 ? 0ull : rows.mask64(b * a.bs) & (a.bs == 32 ? 0xffffffffull : ~0ull);
+            s_live[threadIdx.x][1] = b < 0 || a.bs <= 64 ? 0ull : rows.mask64(b * a.bs + 64);
         }
-    };
-    load(0);
-    if (a.refresh < 0 && !rows.load(a.bank, u)) {
-        if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
-        return;
-    }
-    const uint64_t live[2] = {rows.mask64(r0) & (a.bs == 32 ? 0xffffffffull : ~0ull), a.bs > 64 ? rows.mask64(r0 + 64) : 0ull};
-    const int n_live = __popcll(live[0]) + __popcll(live[1]);
-    float sum[ITEMS][N];
+        __syncthreads();
+        uint4 w[F][ITEMS];
+        // rows p + 8 first, ... of the i-th block, those that live
+        const auto load = [&](int i, int first) {
+            const uint64_t live = s_live[i][first >= 8 ? 1 : 0];
+            const uint8_t *src = unit + (int64_t)s_block[i] * a.bs * a.row_bytes;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
+            for (int f = 0; f < F; ++f) {
+                const int r = p + 8 * (first + f);
+                const bool on = live >> (r & 63) & 1ull;
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum[i][e] = 0.f;
-    for (int first = 0; 8 * first < a.bs; first += F) {
-        if (first > 0) load(first);
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            const int r = p + 8 * (first + f);
-            const bool on = r < a.bs && ((r < 64 ? live[0] : live[1]) >> (r & 63) & 1ull);
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const uint32_t x[4] = {w[f][i].x, w[f][i].y, w[f][i].z, w[f][i].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (N == 8) {
-                        sum[i][2 * e] += on ? __uint_as_float(x[e] << 16) : 0.f;
-                        sum[i][2 * e + 1] += on ? __uint_as_float(x[e] & 0xffff0000u) : 0.f;
-                    } else {
-                        sum[i][e] += on ? __uint_as_float(x[e]) : 0.f;
-                    }
+                for (int x = 0; x < ITEMS; ++x) {
+                    const int v = v0 + piece + 32 * x;
+                    w[f][x] = make_uint4(0, 0, 0, 0);
+                    if (on && v < nvec) w[f][x] = __ldg(reinterpret_cast<const uint4 *>(src + r * a.row_bytes) + v);
                 }
             }
-        }
-    }
+        };
+        load(0, 0);
+        for (int i = 0; i < DIGEST_BLOCKS && s_block[i] >= 0; ++i) {
+            float sum[ITEMS][N];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
+            for (int x = 0; x < ITEMS; ++x)
 #pragma unroll
-        for (int e = 0; e < N; ++e) s_sum[p][(piece + 32 * i) * N + e] = sum[i][e];
-    __syncthreads();
-    // a channel per thread and round; a head is a run of d threads
-    const float n = (float)(n_live > 0 ? n_live : 1);
-    for (int c0 = 0; c0 < COLS; c0 += DIGEST_THREADS) {
-        const int c = c0 + threadIdx.x;                       // COLS <= 256, or a multiple of it
-        const bool in = c < COLS && v0 * N + c < a.H * a.d;
-        float x = 0.f;
-        if (c < COLS) {
-            x = ((s_sum[0][c] + s_sum[4][c]) + (s_sum[2][c] + s_sum[6][c])) +
-                ((s_sum[1][c] + s_sum[5][c]) + (s_sum[3][c] + s_sum[7][c]));
-            x = __fdiv_rn(x, n);
-        }
-        float m = fabsf(x);
+                for (int e = 0; e < N; ++e) sum[x][e] = 0.f;
+            for (int first = 0; 8 * first < a.bs; first += F) {
+                if (first > 0) load(i, first);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1)
-            if (o < a.d) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (a.d > 32) {
+                for (int f = 0; f < F; ++f)
+#pragma unroll
+                    for (int x = 0; x < ITEMS; ++x) {
+                        const uint32_t y[4] = {w[f][x].x, w[f][x].y, w[f][x].z, w[f][x].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (N == 8) {
+                                sum[x][2 * e] += __uint_as_float(y[e] << 16);
+                                sum[x][2 * e + 1] += __uint_as_float(y[e] & 0xffff0000u);
+                            } else {
+                                sum[x][e] += __uint_as_float(y[e]);
+                            }
+                        }
+                    }
+            }
+            const int64_t b = s_block[i];
+            const int n_live = __popcll(s_live[i][0]) + __popcll(s_live[i][1]);
+            if (i + 1 < DIGEST_BLOCKS && s_block[i + 1] >= 0) load(i + 1, 0);
+#pragma unroll
+            for (int x = 0; x < ITEMS; ++x)
+#pragma unroll
+                for (int e = 0; e < N; e += 4)
+                    *reinterpret_cast<float4 *>(&s_sum[p][(piece + 32 * x) * N + e]) =
+                        make_float4(sum[x][e], sum[x][e + 1], sum[x][e + 2], sum[x][e + 3]);
             __syncthreads();
-            if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+            // a channel per thread and round; a head is a run of d threads
+            for (int c0 = 0; c0 < COLS; c0 += DIGEST_THREADS) {
+                const int c = c0 + threadIdx.x;                // COLS <= 256, or a multiple of it
+                const bool in = c < COLS && v0 * N + c < a.H * a.d;
+                float x = 0.f;
+                if (c < COLS) {
+                    x = ((s_sum[0][c] + s_sum[4][c]) + (s_sum[2][c] + s_sum[6][c])) +
+                        ((s_sum[1][c] + s_sum[5][c]) + (s_sum[3][c] + s_sum[7][c]));
+                    // dividing by a power of two is exact either way
+                    x = (n_live & (n_live - 1)) == 0 ? x * (1.f / (float)max(1, n_live)) : __fdiv_rn(x, (float)n_live);
+                }
+                float m = fabsf(x);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (o < a.d) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                if (a.d > 32) {
+                    __syncthreads();
+                    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+                    __syncthreads();
+                    const int w0 = (threadIdx.x >> 5) / (a.d >> 5) * (a.d >> 5);
+                    for (int k = 0; k < a.d >> 5; ++k) m = fmaxf(m, s_max[w0 + k]);
+                }
+                if (!in) continue;                             // no barrier is skipped by it
+                const EightBits q(m);
+                const int col = v0 * N + c, h = col / a.d, e = col - h * a.d;
+                const int64_t at = (u * a.H + h) * a.nb + b;
+                a.digest[at * a.d + e] = (int8_t)q(x);
+                if (e == 0) a.step[at] = q.step;
+            }
             __syncthreads();
-            const int w0 = (threadIdx.x >> 5) / (a.d >> 5) * (a.d >> 5);
-            for (int w = 0; w < a.d >> 5; ++w) m = fmaxf(m, s_max[w0 + w]);
         }
-        if (!in) continue;                                    // uniform over a head; no barrier follows for these
-        const EightBits q(m);
-        const int col = v0 * N + c, h = col / a.d, e = col - h * a.d;
-        const int64_t at = (u * a.H + h) * a.nb + b;
-        a.digest[at * a.d + e] = (int8_t)q(x);
-        if (e == 0) a.step[at] = q.step;
+        __syncthreads();
     }
 }
 
@@ -324,9 +349,48 @@ struct PickArgs {
     SelectArgs a;
     int2 *cand;                // [rows][splits][take]: (ordered score, block)
     int32_t *n_cand;           // [rows][splits]
-    int32_t splits, piece;     // pieces of a query's blocks, blocks of a piece (a multiple of 32)
+    int32_t splits, piece;     // most pieces of a query's blocks, blocks of a piece (a multiple of 32)
+    int32_t wanted;            // pieces that keep the SMs busy
     int32_t take;              // room for a piece's choices
 };
+
+// The words (32 blocks each) of a unit that hold a live row, as four runs in ascending order; the others
+// are never looked at.
+struct LiveWords {
+    int32_t first[4], n[4], total;
+    __device__ __forceinline__ LiveWords(const LiveRows &rows, int bs)
+    {
+        const int sh = 31 - __clz(32 * bs);
+        int end = 0;                                       // one past the last word so far
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i == 1 ? 2 : i == 2 ? 1 : i;     // pinned, the ring's wrapped piece, its other, pointers
+            const int lo = max(end, (int)(rows.start[r] >> sh)), hi = (int)((rows.start[r] + rows.len[r] - 1) >> sh) + 1;
+            first[i] = lo;
+            n[i] = rows.len[r] > 0 ? max(0, hi - lo) : 0;
+            if (rows.len[r] > 0) end = max(end, hi);
+            total += n[i];
+        }
+    }
+    __device__ __forceinline__ int at(int i) const         // the i-th of them
+    {
+        int w = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (i >= 0 && i < n[r]) w = first[r] + i;
+            i -= n[r];
+        }
+        return w;
+    }
+};
+
+// Words of a piece: what the pieces that are wanted leave for each, at most TC_BLOCKS.
+__device__ __forceinline__ int piece_words(const PickArgs &p, int total)
+{
+    const int pieces = max(p.wanted, (total + TC_BLOCKS / 32 - 1) / (TC_BLOCKS / 32));
+    return max(1, (total + pieces - 1) / pieces);
+}
 
 // four bytes (signed) of w to two bf16 pairs: 128 + low seven bits, less 128 or (negative) 256
 __device__ __forceinline__ void bytes_to_bf16(uint32_t w, uint32_t &lo, uint32_t &hi)
@@ -430,40 +494,52 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ uint32_t s_live[TC_BLOCKS / 32];
+    __shared__ int32_t s_word[TC_BLOCKS / 32];
+    __shared__ int32_t s_size[2];                                          // words of this piece, whether there are others
     const SparseArgs &s = p.a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = (s.k_max + TC_ROWS - 1) / TC_ROWS;
     const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles, h = blockIdx.y, u = blockIdx.z;
-    int cnt, g;
-    LiveRows rows;
-    if (!sparse_unit(s, u, threadIdx.x == 0, cnt, g, rows)) return;
+    const int cnt = s.count[u], g = s.unit_group[u];
+    if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G) {
+        if (threadIdx.x == 0) latch_status(s.status, RS3_EINVAL);
+        return;
+    }
     const int j0 = tile * TC_ROWS, nq = min(TC_ROWS, cnt - j0);
     if (nq <= 0) return;
-    const int lo = split * p.piece, n = min(p.piece, s.nb - lo);           // this piece's blocks
+    // the piece's words and the live blocks of each, by one warp (a word per lane)
+    if (warp == TC_THREADS / 32 - 1) {
+        LiveRows rows;
+        const bool sane = rows.load(s.bank, u);
+        if (!sane && lane == 0) latch_status(s.status, RS3_EINTERNAL);
+        const LiveWords words(rows, s.bs);
+        const int per = piece_words(p, words.total);
+        const int n = sane ? max(0, min(per, words.total - split * per)) : -1;
+        const int word = words.at(split * per + lane);
+        if (lane < n) {
+            const int sh = 31 - __clz(s.bs);
+            uint64_t live = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {                                  // blocks of the word that the run reaches
+                if (rows.len[r] == 0) continue;
+                const int lo = max(0, (int)(rows.start[r] >> sh) - 32 * word);
+                const int hi = min(31, (int)((rows.start[r] + rows.len[r] - 1) >> sh) - 32 * word);
+                if (lo <= hi) live |= (2ull << hi) - (1ull << lo);
+            }
+            s_word[lane] = word;
+            s_live[lane] = (uint32_t)live;
+        }
+        if (lane == 0) {
+            s_size[0] = n;
+            s_size[1] = words.total > per;
+        }
+    }
     const int stride = p.piece + 8;                                        // of a query's keys
     uint32_t *s_keys = reinterpret_cast<uint32_t *>(smem);
     const int width = s.d < 64 ? 64 : s.d, q_row = 2 * width + 16;         // columns, bytes of a query
     uint8_t *s_q = smem + TC_ROWS * stride * 4;
-    // this warp's steps: 16 blocks, then 64 columns after 64; a step's digests are loaded one step ahead
     const int r = lane >> 2, t = lane & 3;
-    const int64_t dig = ((int64_t)u * s.H + h) * s.nb + lo;
-    int b0 = warp * 16, k0 = 0;
-    uint4 w[2];
-    const auto load_step = [&](uint4 (&v)[2], int b, int k) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            v[x] = make_uint4(0, 0, 0, 0);
-            if (b + 8 * x + r < n && k + 16 * t < s.d)
-                v[x] = __ldg(reinterpret_cast<const uint4 *>(p.a.digest + (dig + b + 8 * x + r) * s.d + k + 16 * t));
-        }
-    };
-    load_step(w, b0, k0);
-    // which blocks hold a live row
-    for (int b = threadIdx.x; b < p.piece; b += TC_THREADS) {
-        const int64_t r0 = (int64_t)(lo + b) * s.bs;
-        const uint32_t bal = __ballot_sync(0xffffffffu, b < n && rows.count(r0, r0 + s.bs) > 0);
-        if (lane == 0) s_live[b >> 5] = bal;
-    }
+    const int64_t dig = ((int64_t)u * s.H + h) * s.nb;
     // the queries in 8 bits, held as bf16; a warp takes two
     for (int r = warp; r < TC_ROWS; r += TC_THREADS / 32) {
         const int cell = r < nq ? s.idx[(int64_t)u * s.k_max + j0 + r] : 0;
@@ -510,18 +586,32 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         }
     }
     __syncthreads();
+    if (s_size[0] < 0) return;
+    const int n = 32 * s_size[0];                                          // places: blocks of the words, 32 each
+    const bool alone = !s_size[1];
+    // this warp's steps: 16 places, then 64 columns after 64; a step's digests are loaded one step ahead
+    int b0 = warp * 16, k0 = 0;
+    uint4 w[2];
+    const auto load_step = [&](uint4 (&v)[2], int place, int k) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            v[x] = make_uint4(0, 0, 0, 0);
+            const int b = place < n ? s_word[place >> 5] * 32 + (place & 31) + 8 * x + r : s.nb;
+            if (b < s.nb && k + 16 * t < s.d)
+                v[x] = __ldg(reinterpret_cast<const uint4 *>(p.a.digest + (dig + b) * s.d + k + 16 * t));
+        }
+    };
+    load_step(w, b0, k0);
     float c[2][4], st[2][2];
-    for (; b0 < p.piece;) {
+    while (b0 < n) {
         if (k0 == 0) {
+            const int b = s_word[b0 >> 5] * 32 + (b0 & 31) + 2 * t;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int b = b0 + 8 * x + 2 * t + y;
-                    st[x][y] = b < n ? __ldg(p.a.step + dig + b) : 0.f;
-                }
+                for (int y = 0; y < 2; ++y) st[x][y] = b + 8 * x + y < s.nb ? __ldg(p.a.step + dig + b + 8 * x + y) : 0.f;
             }
         }
         const int b1 = k0 + 64 < width ? b0 : b0 + TC_THREADS / 2, k1 = k0 + 64 < width ? k0 + 64 : 0;
@@ -546,7 +636,7 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             mma_bf16(c[x], qv[0][1].z, qv[1][1].z, qv[0][1].w, qv[1][1].w, b[3][0], b[3][1]);
         }
         if (k1 == 0) {
-            // this lane holds blocks 8 x + 2 t, + 1 of queries r and r + 8
+            // this lane holds places 8 x + 2 t, + 1 of queries r and r + 8
             const uint32_t live = s_live[b0 >> 5] >> (b0 & 31);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -564,18 +654,17 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         w[1] = w1[1];
     }
     __syncthreads();
-    int n_live = 0;
-    for (int i = lane; i < p.piece / 32; i += 32) n_live += __popc(s_live[i]);
-    n_live = __reduce_add_sync(0xffffffffu, n_live);
-    const int want = min(s.n_top, n_live);
+    // the first 32 places of the words: one word's blocks per lane
+    const int n_live = __reduce_add_sync(0xffffffffu, lane < s_size[0] ? __popc(s_live[lane]) : 0);
+    const int want = min(s.n_top, n_live), word = lane < s_size[0] ? 32 * s_word[lane] : 0;
     for (int q = warp; q < nq; q += TC_THREADS / 32) {
         const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j0 + q;
-        const Choice out = {p.a.sel + row * s.n_top, p.splits > 1 ? p.cand + (row * p.splits + split) * p.take : nullptr};
+        const Choice out = {p.a.sel + row * s.n_top, alone ? nullptr : p.cand + (row * p.splits + split) * p.take};
         uint32_t *key = s_keys + q * stride;
         uint32_t k[TC_BLOCKS / 32], top = 0u;
 #pragma unroll
         for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-            k[i] = 32 * i < p.piece ? key[32 * i + lane] : 0u;
+            k[i] = 32 * i < n ? key[32 * i + lane] : 0u;
             top = max(top, k[i]);
         }
         const uint32_t most = __reduce_max_sync(0xffffffffu, top);
@@ -593,8 +682,8 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             for (int i = 0; i < TC_BLOCKS / 32; ++i) {
                 const uint32_t bal = __ballot_sync(0xffffffffu, k[i] >= bound);
                 if (bal != 0u) {
-                    const int to = at + __popc(bal & lanes_below());
-                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)k[i], lo + 32 * i + lane);
+                    const int to = at + __popc(bal & lanes_below()), b = __shfl_sync(0xffffffffu, word, i) + lane;
+                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)k[i], b);
                     at += __popc(bal);
                 }
             }
@@ -616,14 +705,15 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
                 const uint32_t same = __ballot_sync(0xffffffffu, k[i] == cut && k[i] > 0);
                 const bool take = k[i] > cut || (k[i] == cut && k[i] > 0 && __popc(same & lanes_below()) < equal);
                 const uint32_t bal = __ballot_sync(0xffffffffu, take);
-                if (take) out.put(at + __popc(bal & lanes_below()), k[i], lo + 32 * i + lane);
+                const int b = __shfl_sync(0xffffffffu, word, i) + lane;
+                if (take) out.put(at + __popc(bal & lanes_below()), k[i], b);
                 at += __popc(bal);
                 equal -= min(equal, __popc(same));
             }
         }
-        if (p.splits > 1) {
+        if (!alone) {
             if (lane == 0) p.n_cand[row * p.splits + split] = want;
-        } else {
+        } else if (split == 0) {                           // no piece but this one
             for (int i = want + lane; i < s.n_top; i += 32) out.sel[i] = -1;
         }
     }
@@ -642,10 +732,12 @@ __global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
     if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || j >= cnt) return;
     LiveRows rows;
     if (!rows.load(s.bank, u)) return;
+    const int total = LiveWords(rows, s.bs).total, per = piece_words(p, total);
+    if (total <= per) return;                              // one piece: its choices are the list
     const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j;
     int2 *pair = s_pairs + warp * room;
     // places without a candidate hold key 0
-    const int n = p.splits * p.take;
+    const int n = (total + per - 1) / per * p.take;
     int some = 0;
 #pragma unroll 4
     for (int i = lane; i < n; i += 32) {
@@ -664,13 +756,14 @@ __global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
 }
 
 // Pieces of a query's blocks: as many as their size needs, more where that leaves SMs idle.
-int64_t select_splits(int64_t U, int64_t H, int64_t k_max, int64_t nb, int64_t n_top, int64_t sms)
+int64_t select_splits(int64_t U, int64_t H, int64_t k_max, int64_t nb, int64_t n_top, int64_t sms, int64_t &wanted)
 {
     const int64_t tiles = U * H * ((k_max + TC_ROWS - 1) / TC_ROWS), least = (nb + TC_BLOCKS - 1) / TC_BLOCKS;
-    int64_t n = tiles > 0 ? (2 * sms + tiles - 1) / tiles : 1;
-    if (n > nb / 256) n = nb / 256;
-    if (n > TC_PAIRS / n_top) n = TC_PAIRS / n_top;        // 48 x 64 at the most blocks and choices
-    return n > least ? n : least > 0 ? least : 1;
+    wanted = tiles > 0 ? (4 * sms + tiles - 1) / tiles : 1;
+    if (wanted > nb / 256) wanted = nb / 256;
+    if (wanted > TC_PAIRS / n_top) wanted = TC_PAIRS / n_top;      // 48 x 64 at the most blocks and choices
+    if (wanted < 1) wanted = 1;
+    return wanted > least ? wanted : least > 0 ? least : 1;
 }
 
 }  // namespace
@@ -706,11 +799,14 @@ extern "C" rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refre
     a.refresh = refresh;
     // blocks of the frames' rows in two runs, and the four single ones
     const int64_t most = (int64_t)refresh * bank->mn / block + 8;
-    const int64_t x = refresh < 0 || most > nb + 8 ? nb + (refresh < 0 ? 0 : 8) : most;
+    a.visits = refresh < 0 ? nb : most > nb + 8 ? nb + 8 : most;
     const bool wide = bank->dtype == RS3_F32 && d == 256;
     const int pieces = wide ? 64 : 32;
     const int64_t slabs = (a.row_bytes / 16 + pieces - 1) / pieces;
     if (slabs > 65535) return RS3_EUNSUPPORTED;
+    // about three CTAs per SM in all, each with a run of blocks
+    int64_t x = (3ll * rs3_sm_count() + slabs * bank->U - 1) / (slabs * bank->U);
+    if (x > a.visits) x = a.visits;
     const dim3 grid((unsigned)x, (unsigned)slabs, (unsigned)bank->U);
     void (*kern)(DigestArgs) = bank->dtype == RS3_BF16 ? k_digest<uint16_t, 1> : wide ? k_digest<float, 2> : k_digest<float, 1>;
     launch_pdl(kern, grid, dim3(DIGEST_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), a);
@@ -720,9 +816,9 @@ extern "C" rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refre
 extern "C" size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int n_blocks)
 {
     if (U < 1 || H < 1 || k_max < 0 || n_blocks < 0) return 0;
-    // rows x pieces: beyond what the blocks need, pieces only fill up two CTAs of 16 rows per SM
+    // rows x pieces: beyond what the blocks need, pieces only fill up four CTAs of 16 rows per SM
     const size_t rows = (size_t)U * (size_t)H * (size_t)k_max, least = ((size_t)n_blocks + TC_BLOCKS - 1) / TC_BLOCKS;
-    const size_t pieces = 4 * TC_SMS * TC_ROWS + (least > 1 ? rows * (least + 1) : 0);
+    const size_t pieces = 8 * TC_SMS * TC_ROWS + (least > 1 ? rows * (least + 1) : 0);
     return 256 + align_up(pieces * 4, 256) + pieces * TC_TOP * sizeof(int2);
 }
 
@@ -746,14 +842,16 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
     const int sms = rs3_sm_count() < (int)TC_SMS ? rs3_sm_count() : (int)TC_SMS;
-    int64_t splits = select_splits(a.s.U, H, k_max, a.s.nb, n_top, sms);
-    if (n_top > TC_TOP && a.s.nb <= TC_BLOCKS) splits = 1;
+    int64_t wanted, splits = select_splits(a.s.U, H, k_max, a.s.nb, n_top, sms, wanted);
+    if (n_top > TC_TOP && a.s.nb <= TC_BLOCKS) splits = wanted = 1;
     if (splits == 1 || n_top <= TC_TOP) {
         PickArgs p = {};
         p.a = a;
         p.splits = (int32_t)splits;
-        p.piece = (int32_t)align_up((size_t)(a.s.nb + splits - 1) / splits, 32);
-        if (p.piece == 0) p.piece = 32;
+        p.wanted = (int32_t)wanted;
+        // blocks of the largest piece that piece_words() can ask for
+        const int64_t words = (a.s.nb + 31) / 32, per = (words + wanted - 1) / wanted;
+        p.piece = (int32_t)(32 * (per < 1 ? 1 : per < TC_BLOCKS / 32 ? per : TC_BLOCKS / 32));
         p.take = n_top < p.piece ? n_top : p.piece;
         const int64_t pieces = (int64_t)a.s.U * H * k_max * splits;
         p.n_cand = static_cast<int32_t *>(workspace);

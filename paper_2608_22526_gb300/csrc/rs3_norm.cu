@@ -80,64 +80,76 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
     const int pieces = d / N;
     const bool here = g < (int64_t)mn * s.H;
     const int cell = here ? (int)(g / s.H) : 0, head = here ? (int)(g % s.H) : 0;
-    // what the cell's rows share: the head's weights and the cell's angles
-    float w[ITEMS][N], cs[ITEMS][N];                               // (cos, sin) pairs
+    // what the cell's rows share, the weights times the angles: with u = x / norm a pair becomes
+    // (u0 wc0 - u1 ws1, u0 ws0 + u1 wc1), (wc, ws) = (w cos, w sin)
+    float co[ITEMS][N], si[ITEMS][N];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int p = lane + i * L;
 #pragma unroll
         for (int e = 0; e < N; e += 4) {
-            float4 a = make_float4(1.f, 1.f, 1.f, 1.f), c = make_float4(1.f, 0.f, 1.f, 0.f);
-            if (p < pieces && s.weight) a = __ldg(reinterpret_cast<const float4 *>(s.weight + p * N + e));
+            float4 w = make_float4(1.f, 1.f, 1.f, 1.f), c = make_float4(1.f, 0.f, 1.f, 0.f);
+            if (p < pieces && s.weight) w = __ldg(reinterpret_cast<const float4 *>(s.weight + p * N + e));
             if (p < pieces && rope) c = __ldg(reinterpret_cast<const float4 *>(rope + (int64_t)cell * d + p * N + e));
-            w[i][e] = a.x; w[i][e + 1] = a.y; w[i][e + 2] = a.z; w[i][e + 3] = a.w;
-            cs[i][e] = c.x; cs[i][e + 1] = c.y; cs[i][e + 2] = c.z; cs[i][e + 3] = c.w;
+            co[i][e] = w.x * c.x; si[i][e] = w.x * c.y;
+            co[i][e + 1] = w.y * c.x; si[i][e + 1] = w.y * c.y;
+            co[i][e + 2] = w.z * c.z; si[i][e + 2] = w.z * c.w;
+            co[i][e + 3] = w.w * c.z; si[i][e + 3] = w.w * c.w;
         }
     }
-    const int t1 = min(s.turns, (tb + 1) * s.per_cta);
-    for (int t0 = tb * s.per_cta; t0 < t1; t0 += NORM_FLIGHT) {
-        uint4 v[NORM_FLIGHT][ITEMS];
-        bool take[NORM_FLIGHT];
-#pragma unroll
-        for (int f = 0; f < NORM_FLIGHT; ++f) {
-            const int64_t row = (int64_t)(t0 + f) * mn + cell;
-            take[f] = here && t0 + f < t1 && row < s.rows && (!s.keep || s.keep[row] != 0);
+    const float inv_d = 1.f / (float)d;
+    const int t0 = tb * s.per_cta, t1 = min(s.turns, t0 + s.per_cta);
+    const int64_t row0 = (int64_t)t0 * mn + cell;
+    const uint8_t *src = s.x + row0 * s.x_stride + (head * pieces + lane) * 16;
+    uint8_t *dst = s.y + row0 * s.y_stride + (head * pieces + lane) * 16;
+    const int64_t x_turn = s.x_stride * mn, y_turn = s.y_stride * mn;
+    // the rows that are kept, a bit for each of the next 32 turns
+    for (int t = t0; t < t1; t += 32) {
+        uint32_t kept = 0;
+#pragma unroll 8
+        for (int f = 0; f < 32; ++f) {
+            if (t + f >= t1) break;
+            const int64_t row = (int64_t)(t + f) * mn + cell;
+            kept |= (uint32_t)(here && row < s.rows && (!s.keep || s.keep[row] != 0)) << f;
         }
+        // a warp goes from one turn to the next that any of its lanes keeps
+        uint32_t todo = __reduce_or_sync(0xffffffffu, kept);
+        while (todo != 0u) {
+            uint4 v[NORM_FLIGHT][ITEMS];
+            int turn[NORM_FLIGHT];
 #pragma unroll
-        for (int f = 0; f < NORM_FLIGHT; ++f) {
-            const int64_t row = (int64_t)(t0 + f) * mn + cell;
-            const uint4 *src = reinterpret_cast<const uint4 *>(s.x + row * s.x_stride) + head * pieces;
+            for (int f = 0; f < NORM_FLIGHT; ++f) {
+                turn[f] = todo != 0u ? __ffs(todo) - 1 : -1;
+                todo &= todo - 1u;
+                const bool take = turn[f] >= 0 && (kept >> turn[f] & 1u);
+                const uint4 *x = reinterpret_cast<const uint4 *>(src + (int64_t)(t - t0 + turn[f]) * x_turn);
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int p = lane + i * L;
-                v[f][i] = take[f] && p < pieces ? __ldcs(src + p) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < ITEMS; ++i) v[f][i] = take && lane + i * L < pieces ? __ldcs(x + i * L) : make_uint4(0, 0, 0, 0);
             }
-        }
 #pragma unroll
-        for (int f = 0; f < NORM_FLIGHT; ++f) {
-            float x[ITEMS][N], sum = 0.f;
+            for (int f = 0; f < NORM_FLIGHT; ++f) {
+                if (turn[f] < 0) break;
+                float x[ITEMS][N], sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                Piece<T>::widen(v[f][i], x[i]);
+                for (int i = 0; i < ITEMS; ++i) {
+                    Piece<T>::widen(v[f][i], x[i]);
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-            }
-            for (int o = L >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float r = rsqrtf(sum / (float)d + eps);
-            if (!take[f]) continue;
-            const int64_t row = (int64_t)(t0 + f) * mn + cell;
-            uint4 *dst = reinterpret_cast<uint4 *>(s.y + row * s.y_stride) + head * pieces;
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int p = lane + i * L;
-                float y[N];
-#pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    const float y0 = x[i][e] * r * w[i][e], y1 = x[i][e + 1] * r * w[i][e + 1];
-                    y[e] = y0 * cs[i][e] - y1 * cs[i][e + 1];
-                    y[e + 1] = y0 * cs[i][e + 1] + y1 * cs[i][e];
+                    for (int e = 0; e < N; ++e) sum = fmaf(x[i][e], x[i][e], sum);
                 }
-                if (p < pieces) dst[p] = Piece<T>::narrow(y);
+                for (int o = L >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                const float r = rsqrtf(fmaf(sum, inv_d, eps));
+                uint4 *y = reinterpret_cast<uint4 *>(dst + (int64_t)(t - t0 + turn[f]) * y_turn);
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    float z[N];
+#pragma unroll
+                    for (int e = 0; e < N; e += 2) {
+                        const float u0 = x[i][e] * r, u1 = x[i][e + 1] * r;
+                        z[e] = fmaf(u0, co[i][e], -(u1 * si[i][e + 1]));
+                        z[e + 1] = fmaf(u0, si[i][e], u1 * co[i][e + 1]);
+                    }
+                    if ((kept >> turn[f] & 1u) && lane + i * L < pieces) y[i * L] = Piece<T>::narrow(z);
+                }
             }
         }
     }

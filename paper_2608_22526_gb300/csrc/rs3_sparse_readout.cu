@@ -227,7 +227,8 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 // by block
 // ---------------------------------------------------------------------------
 constexpr int TILE = 64;                   // queries of an item
-constexpr int LIST_THREADS = 512;
+constexpr int LIST_THREADS = 1024;
+constexpr int LIST_HELD = 6;               // fours of list entries that a thread holds
 constexpr int LIST_BINS = 8192;            // blocks that a CTA counts
 constexpr int MAX_SEGMENTS = 1024;         // (unit, head, segment) triples that a CTA of the attention holds at a time
 constexpr int CHUNK_ITEMS = 64;            // items whose records it holds
@@ -250,31 +251,11 @@ struct BlockWork {                         // in the workspace
     uint64_t wait_ns;                      // limit of each wait
 };
 
-// f(i, list[i]) for i < n, by the CTA's threads, four entries to a load where the alignment allows
-template <typename F>
-__device__ __forceinline__ void each_entry(const int32_t *list, int n, F f)
-{
-    const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(list) & 15)) >> 2 & 3));
-    const int vecs = (n - head) >> 2, tail = head + 4 * vecs;
-    if ((int)threadIdx.x < head) f((int)threadIdx.x, __ldg(list + threadIdx.x));
-    const int4 *v = reinterpret_cast<const int4 *>(list + head);
-#pragma unroll 4
-    for (int i = threadIdx.x; i < vecs; i += LIST_THREADS) {
-        const int4 x = __ldg(v + i);
-        const int e = head + 4 * i;
-        f(e, x.x);
-        f(e + 1, x.y);
-        f(e + 2, x.z);
-        f(e + 3, x.w);
-    }
-    if (tail + (int)threadIdx.x < n) f(tail + (int)threadIdx.x, __ldg(list + tail + threadIdx.x));
-}
-
 // The queries of every block: CTA (segment, unit * H + head) counts the lists' entries for its
 // blocks, gives every block a run of list entries and its items, and fills them in.  Entries of one block
 // come in any order; each is computed by itself, so the result does not depend on it.  Out of place the
 // launch's other CTAs write out = residual (or zeros) on every cell.
-__global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
+__global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
     if ((int)blockIdx.x >= w.list_ctas) {
@@ -291,6 +272,26 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
     const int uh = blockIdx.x / w.segments, seg = blockIdx.x - uh * w.segments, u = uh / s.H;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int lo = seg * w.bins, hi = min(s.nb, lo + w.bins), n_bins = hi - lo;
+    // the first lists' entries are on their way while the unit's counters are read; both passes use them
+    const int64_t base = (int64_t)uh * s.k_max * s.n_top;
+    const int32_t *sel = a.sel + base, *idx = s.idx + (int64_t)u * s.k_max;
+    const int most = s.k_max * s.n_top;
+    const int first_four = (int)((16 - (reinterpret_cast<uintptr_t>(sel) & 15)) >> 2 & 3);     // where 16-byte loads begin
+    const auto fours = [&](int e) {                    // entries e .. e + 3; -1 past the end
+        int4 x = make_int4(-1, -1, -1, -1);
+        if (e + 4 <= most) x = __ldg(reinterpret_cast<const int4 *>(sel + e));
+        else {
+            if (e < most) x.x = __ldg(sel + e);
+            if (e + 1 < most) x.y = __ldg(sel + e + 1);
+            if (e + 2 < most) x.z = __ldg(sel + e + 2);
+        }
+        return x;
+    };
+    int4 held[LIST_HELD];
+#pragma unroll
+    for (int i = 0; i < LIST_HELD; ++i) held[i] = fours(first_four + 4 * (threadIdx.x + i * LIST_THREADS));
+    const int head = (int)threadIdx.x < first_four && (int)threadIdx.x < most ? __ldg(sel + threadIdx.x) : -1;
+    bool bad = false;                                  // some query's cell is not on the grid: it is in no list
     int cnt, g;
     LiveRows rows;
     const bool work = sparse_unit(s, u, threadIdx.x == 0 && seg == 0 && uh == u * s.H, cnt, g, rows) && n_bins > 0;
@@ -299,21 +300,41 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
         return;
     }
     for (int i = threadIdx.x; i < n_bins; i += LIST_THREADS) s_bin[i] = 0;
-    const int32_t *idx = s.idx + (int64_t)u * s.k_max;
-    bool bad = false;                                  // some query's cell is not on the grid: it is in no list
     for (int j = threadIdx.x; j < cnt; j += LIST_THREADS) bad |= (uint32_t)idx[j] >= (uint32_t)s.mn;
     if (bad && seg == 0) latch_status(s.status, RS3_EINVAL);
     const bool check = __syncthreads_or(bad);
-    const int64_t base = (int64_t)uh * s.k_max * s.n_top;
     const int pairs = cnt * s.n_top;
-    const auto listed = [&](int i) { return !check || (uint32_t)idx[i / s.n_top] < (uint32_t)s.mn; };
+    const auto listed = [&](int i) { return i < pairs && (!check || (uint32_t)idx[i / s.n_top] < (uint32_t)s.mn); };
+    // f(entry, block) for every entry of the lists that is a block's
+    bool over = false;                                 // some is past the last block
+    const auto each = [&](auto f) {
+        const auto one = [&](int e, int b) {
+            over |= b >= s.nb && e < pairs;
+            if (b >= 0 && b < hi && listed(e)) f(e, b);
+        };
+        one(threadIdx.x, head);
+        int e = first_four + 4 * threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < LIST_HELD; ++i, e += 4 * LIST_THREADS) {
+            one(e, held[i].x);
+            one(e + 1, held[i].y);
+            one(e + 2, held[i].z);
+            one(e + 3, held[i].w);
+        }
+        for (; e < pairs; e += 4 * LIST_THREADS) {
+            const int4 x = fours(e);
+            one(e, x.x);
+            one(e + 1, x.y);
+            one(e + 2, x.z);
+            one(e + 3, x.w);
+        }
+    };
     int before = 0;
-    each_entry(a.sel + base, pairs, [&](int i, int b) {
-        if (b >= s.nb && seg == 0) latch_status(s.status, RS3_EINVAL);
-        if (b < 0 || b >= hi || !listed(i)) return;
+    each([&](int, int b) {
         if (b >= lo) atomicAdd(&s_bin[b - lo], 1);
         before += b < lo;
     });
+    if (over && seg == 0) latch_status(s.status, RS3_EINVAL);
     before = __reduce_add_sync(0xffffffffu, before);
     if (lane == 0) s_part[warp] = before;
     __syncthreads();
@@ -374,8 +395,8 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
     }
     __syncthreads();
     int2 *list = w.list + base;
-    each_entry(a.sel + base, pairs, [&](int i, int b) {
-        if (b >= lo && b < hi && listed(i)) list[atomicAdd(&s_bin[b - lo], 1)] = make_int2(i, idx[i / s.n_top]);
+    each([&](int i, int b) {
+        if (b >= lo) list[atomicAdd(&s_bin[b - lo], 1)] = make_int2(i, idx[i / s.n_top]);
     });
 }
 
@@ -516,6 +537,22 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                 __syncwarp();
             } else {
                 bool ok = true;
+                const int r = lane >> 2, t = lane & 3;
+                // list entries of this warp's next tile, at or behind item i: rows lane / 4 and + 8
+                int2 ahead[2];
+                const auto look_ahead = [&](int i) {
+                    ahead[0] = ahead[1] = make_int2(-1, -1);
+                    for (; i < chunk; ++i) {
+                        const int tile = (warp - s_tile0[i]) & (X::CONSUMERS - 1), m = s_item[i].n - tile * 16;
+                        if (m <= 0) continue;
+                        const int2 *list = w.list + (int64_t)s_item[i].uh * s.k_max * s.n_top + s_item[i].first + tile * 16;
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            if (r + 8 * x < m) ahead[x] = __ldg(list + r + 8 * x);
+                        break;
+                    }
+                };
+                look_ahead(0);
                 for (int i = 0; i < chunk && ok; ++i) {
                     const uint32_t k = cnt + i, st = k % X::STAGES;
                     const int tile = (warp - s_tile0[i]) & (X::CONSUMERS - 1);
@@ -527,13 +564,9 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                     }
                     const int uh = s_item[i].uh, u = uh / s.H, h = uh - u * s.H;
                     const int64_t pair0 = (int64_t)uh * s.k_max * s.n_top;
-                    const int2 *list = w.list + pair0 + s_item[i].first + tile * 16;
-                    // this lane's rows: lane / 4 and + 8; of 64 columns the pieces 2 (lane % 4) and + 1
-                    const int r = lane >> 2, t = lane & 3;
-                    int2 e[2];
+                    // of 64 columns this lane holds the pieces 2 (lane % 4) and + 1
+                    const int2 e[2] = {ahead[0], ahead[1]};
                     uint4 q[2][D / 32];
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) e[x] = r + 8 * x < m ? __ldg(list + r + 8 * x) : make_int2(-1, -1);
                     const uint16_t *Q = static_cast<const uint16_t *>(s.q) + (int64_t)__ldg(s.unit_group + u) * s.mn * row_elems + h * D;
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
@@ -550,6 +583,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                             for (int c = 0; c < D / 32; ++c)
                                 if (e[x].y >= 0)
                                     q[x][c] = rotate_q_piece(q[x][c], s.rope + (int64_t)e[x].y * D + ((c >> 1) * 8 + 2 * t + (c & 1)) * 8);
+                    look_ahead(i + 1);
                     ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
                     if (!ok) break;
                     const uint32_t sk = base + st * X::STAGE, sv = sk + X::HALF;
@@ -657,22 +691,23 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
     }
 }
 
-// Groups of D / 4 (at most 64) lanes, four to a (unit, head, query): each joins a quarter of the blocks'
-// results by their running maximum, then the four are joined:
+// Groups of D / 4 lanes, G = D / 64 to a (unit, head, query): each joins its share of the blocks' results by
+// their running maximum, eight loads at a time, then the groups are joined:
 //   out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
-// A quarter each because the loads of one after another would wait for one another.
+// Wide heads have few queries and much to load for each; for heads of 64 four groups a query took 33 us where
+// one took XX (23 700 queries of 16 blocks).
 constexpr int JOIN_THREADS = 256;
 
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, BlockWork w)
 {
-    constexpr int L = D / 4, PER = JOIN_THREADS / (4 * L);
+    constexpr int L = D / 4, G = D / 64, PER = JOIN_THREADS / (G * L);
     pdl_wait();
     __shared__ float4 s_y[JOIN_THREADS];
     __shared__ float2 s_ml[JOIN_THREADS / L];
     const SparseArgs &s = a.s;
     const int u = blockIdx.y, sub = threadIdx.x % L, part = threadIdx.x / L;
-    const int64_t jh = (int64_t)blockIdx.x * PER + part / 4;
+    const int64_t jh = (int64_t)blockIdx.x * PER + part / G;
     const int j = (int)(jh / s.H), h = (int)(jh - (int64_t)j * s.H);
     const int cnt = s.count[u], g = s.unit_group[u];
     if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || (int64_t)blockIdx.x * PER >= (int64_t)cnt * s.H) return;
@@ -683,21 +718,21 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
     float m = -INFINITY, l = 0.f;
     // all of a query's loads go out together: what an entry without a block left in its place is not used
     const int n = j < cnt ? s.n_top * w.parts : 0;
-    constexpr int F = 4;                               // results in flight
-    for (int t0 = part & 3; t0 < n; t0 += 4 * F) {
+    constexpr int F = 8;                               // results in flight
+    for (int t0 = part % G; t0 < n; t0 += G * F) {
         float2 ml[F];
         float4 v[F];
         int b[F];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            const int t = min(t0 + 4 * f, n - 1);
+            const int t = min(t0 + G * f, n - 1);
             b[f] = __ldg(a.sel + base + (w.parts == 2 ? t >> 1 : t));
             ml[f] = __ldg(w.ml + base * w.parts + t);
             v[f] = __ldcs(reinterpret_cast<const float4 *>(w.o + (base * w.parts + t) * D) + sub);
         }
 #pragma unroll
         for (int f = 0; f < F; ++f)
-            if (!here || t0 + 4 * f >= n || b[f] < 0 || b[f] >= s.nb) {
+            if (!here || t0 + G * f >= n || b[f] < 0 || b[f] >= s.nb) {
                 ml[f] = make_float2(-INFINITY, 0.f);
                 v[f] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
@@ -716,23 +751,26 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
             y = make_float4(fmaf(e, v[f].x, y.x), fmaf(e, v[f].y, y.y), fmaf(e, v[f].z, y.z), fmaf(e, v[f].w, y.w));
         }
     }
-    s_y[threadIdx.x] = y;
-    if (sub == 0) s_ml[part] = make_float2(m, l);
-    __syncthreads();
-    if ((part & 3) != 0 || !here) return;
-    float top = -INFINITY;
+    if (G > 1) {
+        s_y[threadIdx.x] = y;
+        if (sub == 0) s_ml[part] = make_float2(m, l);
+        __syncthreads();
+        if (part % G != 0) return;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) top = fmaxf(top, s_ml[part + x].x);
-    y = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (top > -INFINITY) {
+        for (int x = 1; x < G; ++x) m = fmaxf(m, s_ml[part + x].x);
+        y = make_float4(0.f, 0.f, 0.f, 0.f);
         l = 0.f;
+        if (m > -INFINITY)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const float e = exp2f(s_ml[part + x].x - top);
-            const float4 v = s_y[threadIdx.x + x * L];
-            l = fmaf(e, s_ml[part + x].y, l);
-            y = make_float4(fmaf(e, v.x, y.x), fmaf(e, v.y, y.y), fmaf(e, v.z, y.z), fmaf(e, v.w, y.w));
-        }
+            for (int x = 0; x < G; ++x) {
+                const float e = exp2f(s_ml[part + x].x - m);
+                const float4 v = s_y[threadIdx.x + x * L];
+                l = fmaf(e, s_ml[part + x].y, l);
+                y = make_float4(fmaf(e, v.x, y.x), fmaf(e, v.y, y.y), fmaf(e, v.z, y.z), fmaf(e, v.w, y.w));
+            }
+    }
+    if (!here) return;
+    if (m > -INFINITY) {
         const float inv = 1.f / l;
         y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     }
@@ -836,7 +874,7 @@ rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t s
     if (s.d == 256) r = half ? launch_attend<256, 32>(a, w, st) : launch_attend<256, 64>(a, w, st);
     if (r != RS3_OK) return r;
     void (*join)(AttendArgs, BlockWork) = s.d == 64 ? k_join_blocks<64> : s.d == 128 ? k_join_blocks<128> : k_join_blocks<256>;
-    const int per = JOIN_THREADS / s.d;
+    const int per = JOIN_THREADS * 256 / (s.d * s.d);      // queries of a CTA: G * L lanes each
     launch_pdl(join, dim3((unsigned)(((int64_t)s.k_max * s.H + per - 1) / per), (unsigned)s.U), dim3(JOIN_THREADS), 0, st, a, w);
     return RS3_OK;
 }
