@@ -6,6 +6,8 @@
 // a power of two: exact, hence the same whatever order they are summed in.
 #include "rs3_sparse.cuh"
 
+#include <cfloat>
+
 namespace {
 
 // ---------------------------------------------------------------------------
@@ -219,6 +221,12 @@ __device__ __forceinline__ uint32_t order_bits(float s)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
+// the score of a number of order_bits()
+__device__ __forceinline__ float score_of(uint32_t key)
+{
+    return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
+
 __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
 {
     pdl_wait();
@@ -332,7 +340,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
 // The same on the tensor cores, for what most calls are: up to 1024 blocks in one piece, or more in
 // pieces (`splits`) of up to 1024 whose choices k_merge_blocks joins.
 //
-// A CTA scores 16 queries against its blocks: whole numbers of at most 127 are exact in bf16, and their
+// A CTA scores 16 queries against its blocks: whole numbers of at most 127 are exact in fp16, and their
 // products' sums stay below 2^22, exact in the fp32 accumulators.  A lane's 16 bytes of a digest are
 // spread over four steps of the matrix instruction, and the queries' columns are taken in the same order.
 // Then a warp per query holds the scores in registers (32 per lane at most).  Of n <= 32 wanted, the n-th
@@ -392,23 +400,17 @@ __device__ __forceinline__ int piece_words(const PickArgs &p, int total)
     return max(1, (total + pieces - 1) / pieces);
 }
 
-// four bytes (signed) of w to two bf16 pairs: 128 + low seven bits, less 128 or (negative) 256
-__device__ __forceinline__ void bytes_to_bf16(uint32_t w, uint32_t &lo, uint32_t &hi)
+// Four signed bytes of w as two fp16 pairs: a byte u on top of 0x6400 is 1024 + u exactly, u = x + 128.
+__device__ __forceinline__ void bytes_to_fp16(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    const uint32_t x = __byte_perm(w, 0, 0x4140), y = __byte_perm(w, 0, 0x4342);    // bytes 0, 1 and 2, 3 in 16 bits each
-    asm("{\n\t.reg .b32 a, b;\n\t"
-        "lop3.b32 a, %1, 0x007f007f, 0x43004300, 0xea;\n\t"
-        "lop3.b32 b, %1, 0x00800080, 0x43004300, 0xea;\n\t"
-        "sub.rn.bf16x2 %0, a, b;\n\t}" : "=r"(lo) : "r"(x));
-    asm("{\n\t.reg .b32 a, b;\n\t"
-        "lop3.b32 a, %1, 0x007f007f, 0x43004300, 0xea;\n\t"
-        "lop3.b32 b, %1, 0x00800080, 0x43004300, 0xea;\n\t"
-        "sub.rn.bf16x2 %0, a, b;\n\t}" : "=r"(hi) : "r"(y));
+    w ^= 0x80808080u;
+    asm("{\n\t.reg .b32 a;\n\tprmt.b32 a, %1, 0x64646464, 0x4140;\n\tsub.rn.f16x2 %0, a, %2;\n\t}" : "=r"(lo) : "r"(w), "r"(0x64806480u));
+    asm("{\n\t.reg .b32 a;\n\tprmt.b32 a, %1, 0x64646464, 0x4342;\n\tsub.rn.f16x2 %0, a, %2;\n\t}" : "=r"(hi) : "r"(w), "r"(0x64806480u));
 }
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma_fp16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -534,13 +536,13 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             s_size[1] = words.total > per;
         }
     }
-    const int stride = p.piece + 8;                                        // of a query's keys
-    uint32_t *s_keys = reinterpret_cast<uint32_t *>(smem);
+    const int stride = p.piece + 8;                                        // of a query's scores
+    float *s_score = reinterpret_cast<float *>(smem);
     const int width = s.d < 64 ? 64 : s.d, q_row = 2 * width + 16;         // columns, bytes of a query
     uint8_t *s_q = smem + TC_ROWS * stride * 4;
     const int r = lane >> 2, t = lane & 3;
     const int64_t dig = ((int64_t)u * s.H + h) * s.nb;
-    // the queries in 8 bits, held as bf16; a warp takes two
+    // the queries in 8 bits, held as fp16; a warp takes two
     for (int r = warp; r < TC_ROWS; r += TC_THREADS / 32) {
         const int cell = r < nq ? s.idx[(int64_t)u * s.k_max + j0 + r] : 0;
         const bool ok = r < nq && cell >= 0 && cell < s.mn;
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             const int c = lane + 32 * i;
             if (2 * c < width) {
                 uint32_t w;
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"((float)e(x[2 * i + 1])), "f"((float)e(x[2 * i])));
+                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"((float)e(x[2 * i + 1])), "f"((float)e(x[2 * i])));
                 *reinterpret_cast<uint32_t *>(s_q + r * q_row + 4 * c) = w;
             }
         }
@@ -626,14 +628,14 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             uint32_t b[4][2];
-            bytes_to_bf16(w[x].x, b[0][0], b[0][1]);
-            bytes_to_bf16(w[x].y, b[1][0], b[1][1]);
-            bytes_to_bf16(w[x].z, b[2][0], b[2][1]);
-            bytes_to_bf16(w[x].w, b[3][0], b[3][1]);
-            mma_bf16(c[x], qv[0][0].x, qv[1][0].x, qv[0][0].y, qv[1][0].y, b[0][0], b[0][1]);
-            mma_bf16(c[x], qv[0][0].z, qv[1][0].z, qv[0][0].w, qv[1][0].w, b[1][0], b[1][1]);
-            mma_bf16(c[x], qv[0][1].x, qv[1][1].x, qv[0][1].y, qv[1][1].y, b[2][0], b[2][1]);
-            mma_bf16(c[x], qv[0][1].z, qv[1][1].z, qv[0][1].w, qv[1][1].w, b[3][0], b[3][1]);
+            bytes_to_fp16(w[x].x, b[0][0], b[0][1]);
+            bytes_to_fp16(w[x].y, b[1][0], b[1][1]);
+            bytes_to_fp16(w[x].z, b[2][0], b[2][1]);
+            bytes_to_fp16(w[x].w, b[3][0], b[3][1]);
+            mma_fp16(c[x], qv[0][0].x, qv[1][0].x, qv[0][0].y, qv[1][0].y, b[0][0], b[0][1]);
+            mma_fp16(c[x], qv[0][0].z, qv[1][0].z, qv[0][0].w, qv[1][0].w, b[1][0], b[1][1]);
+            mma_fp16(c[x], qv[0][1].x, qv[1][1].x, qv[0][1].y, qv[1][1].y, b[2][0], b[2][1]);
+            mma_fp16(c[x], qv[0][1].z, qv[1][1].z, qv[0][1].w, qv[1][1].w, b[3][0], b[3][1]);
         }
         if (k1 == 0) {
             // this lane holds places 8 x + 2 t, + 1 of queries r and r + 8
@@ -643,8 +645,8 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
                 const bool on0 = live >> (8 * x + 2 * t) & 1u, on1 = live >> (8 * x + 2 * t + 1) & 1u;
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const uint2 key = make_uint2(on0 ? order_bits(c[x][2 * y] * st[x][0]) : 0u, on1 ? order_bits(c[x][2 * y + 1] * st[x][1]) : 0u);
-                    *reinterpret_cast<uint2 *>(s_keys + (r + 8 * y) * stride + b0 + 8 * x + 2 * t) = key;
+                    const float2 score = make_float2(on0 ? c[x][2 * y] * st[x][0] : -INFINITY, on1 ? c[x][2 * y + 1] * st[x][1] : -INFINITY);
+                    *reinterpret_cast<float2 *>(s_score + (r + 8 * y) * stride + b0 + 8 * x + 2 * t) = score;
                 }
             }
         }
@@ -660,30 +662,34 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     for (int q = warp; q < nq; q += TC_THREADS / 32) {
         const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j0 + q;
         const Choice out = {p.a.sel + row * s.n_top, alone ? nullptr : p.cand + (row * p.splits + split) * p.take};
-        uint32_t *key = s_keys + q * stride;
-        uint32_t k[TC_BLOCKS / 32], top = 0u;
+        float *score = s_score + q * stride;
+        float k[TC_BLOCKS / 32], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-            k[i] = 32 * i < n ? key[32 * i + lane] : 0u;
-            top = max(top, k[i]);
+            k[i] = 32 * i < n ? score[32 * i + lane] : -INFINITY;
+            top = fmaxf(top, k[i]);
         }
-        const uint32_t most = __reduce_max_sync(0xffffffffu, top);
         bool done = false;
         if (want > 0 && want <= 32) {
-            // the want-th largest of the lanes' maxima, or 1 where fewer lanes hold a live block
-            uint32_t bound = 1u;
-            if (__popc(__ballot_sync(0xffffffffu, top > 0u)) >= want)
-                bound = max(1u, cut_at(want, __reduce_min_sync(0xffffffffu, top), most,
-                                       [&](uint32_t x) { return __popc(__ballot_sync(0xffffffffu, top >= x)); }));
+            // the want-th largest of the lanes' maxima, or all that live where fewer lanes hold one
+            const uint32_t mine = top > -INFINITY ? order_bits(top) : 0u;
+            uint32_t least = mine;
+            if (want < 32) {
+                const uint32_t cut = cut_at(want, __reduce_min_sync(0xffffffffu, mine), __reduce_max_sync(0xffffffffu, mine),
+                                            [&](uint32_t x) { return __popc(__ballot_sync(0xffffffffu, mine >= x)); });
+                least = mine >= cut ? mine : 0xffffffffu;
+            }
+            least = __reduce_min_sync(0xffffffffu, least);
+            const float bound = least > 0u ? score_of(least) : -FLT_MAX;
             __syncwarp();
-            int2 *pair = reinterpret_cast<int2 *>(key);    // room for half as many (key, block) pairs in the query's own row
+            int2 *pair = reinterpret_cast<int2 *>(score);  // room for half as many (key, block) pairs in the query's own row
             int at = 0;
 #pragma unroll
             for (int i = 0; i < TC_BLOCKS / 32; ++i) {
                 const uint32_t bal = __ballot_sync(0xffffffffu, k[i] >= bound);
                 if (bal != 0u) {
                     const int to = at + __popc(bal & lanes_below()), b = __shfl_sync(0xffffffffu, word, i) + lane;
-                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)k[i], b);
+                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)order_bits(k[i]), b);
                     at += __popc(bal);
                 }
             }
@@ -692,21 +698,24 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             if (done) choose<4>(at, want, out, [&](int i) { return pair[i]; });
         }
         if (!done && want > 0) {
+            uint32_t key[TC_BLOCKS / 32];
+#pragma unroll
+            for (int i = 0; i < TC_BLOCKS / 32; ++i) key[i] = k[i] > -INFINITY ? order_bits(k[i]) : 0u;
             const auto n_at_least = [&](uint32_t x) {
                 int c = 0;
 #pragma unroll
-                for (int i = 0; i < TC_BLOCKS / 32; ++i) c += k[i] >= x;
+                for (int i = 0; i < TC_BLOCKS / 32; ++i) c += key[i] >= x;
                 return (int)__reduce_add_sync(0xffffffffu, c);
             };
-            const uint32_t cut = cut_at(want, 1u, most, n_at_least);
+            const uint32_t cut = cut_at(want, 1u, __reduce_max_sync(0xffffffffu, top > -INFINITY ? order_bits(top) : 0u), n_at_least);
             int equal = want - (cut == 0xffffffffu ? 0 : n_at_least(cut + 1u)), at = 0;
 #pragma unroll
             for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-                const uint32_t same = __ballot_sync(0xffffffffu, k[i] == cut && k[i] > 0);
-                const bool take = k[i] > cut || (k[i] == cut && k[i] > 0 && __popc(same & lanes_below()) < equal);
+                const uint32_t same = __ballot_sync(0xffffffffu, key[i] == cut && key[i] > 0);
+                const bool take = key[i] > cut || (key[i] == cut && key[i] > 0 && __popc(same & lanes_below()) < equal);
                 const uint32_t bal = __ballot_sync(0xffffffffu, take);
                 const int b = __shfl_sync(0xffffffffu, word, i) + lane;
-                if (take) out.put(at + __popc(bal & lanes_below()), k[i], b);
+                if (take) out.put(at + __popc(bal & lanes_below()), key[i], b);
                 at += __popc(bal);
                 equal -= min(equal, __popc(same));
             }
