@@ -6,6 +6,9 @@
 // a power of two: exact, hence the same whatever order they are summed in.
 #include "rs3_sparse.cuh"
 
+#include "rs3_tc_host.cuh"
+#include "rs3_tc_ptx.cuh"
+
 #include <cfloat>
 
 namespace {
@@ -13,8 +16,6 @@ namespace {
 // ---------------------------------------------------------------------------
 // digests
 // ---------------------------------------------------------------------------
-constexpr int DIGEST_THREADS = 256;        // 32 pieces x 8 partial sums
-
 struct DigestArgs {
     BankDev bank;
     const uint8_t *k_store;
@@ -23,6 +24,7 @@ struct DigestArgs {
     int32_t *status;
     int64_t row_bytes, visits; // blocks to visit
     int32_t H, d, bs, nb, refresh;
+    uint64_t wait_ns;          // limit of each wait
 };
 
 // Rows of the newest `refresh` ring frames; by a whole warp.
@@ -67,129 +69,161 @@ __device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int6
     return -1;
 }
 
-// A CTA digests 32 x ITEMS pieces (16 bytes each: whole heads) of blocks of a unit, one after another: thread
-// (piece, p) sums rows p, p + 8, ... of its piece, then the eight partial sums of a channel are joined
-// as ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)).  The next block's rows are loaded while one is joined, and which
-// rows live is worked out for 32 blocks at a time, a thread each: per block and thread that arithmetic took
-// half of the kernel's instructions (all blocks of eight banks: 112 us).
-constexpr int DIGEST_BLOCKS = 32;
+// A warp digests 32 x ITEMS pieces (16 bytes each: whole heads) of one block after another, by itself: its first
+// lane brings the rows by TMA, 16 at a time (8 of 1 KB), into one of the warp's two buffers while the other's are added.  A
+// lane adds its pieces' rows up in the eight partial sums, which it then joins as
+// ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)): no barrier among warps.  Which rows live is worked out for 32 blocks at
+// a time, one per lane; pieces without a live row are not read.  192 KB in flight per SM: with the rows loaded
+// into registers (64 KB) all blocks of eight banks took 64 us, XX so.
+constexpr int DIGEST_WARPS = 12;
 
 template <typename T, int ITEMS>
-__global__ void __launch_bounds__(DIGEST_THREADS, 3) k_digest(DigestArgs a)
+__global__ void __launch_bounds__(32 * DIGEST_WARPS, 1) k_digest(DigestArgs a, const __grid_constant__ CUtensorMap map)
 {
-    constexpr int N = 16 / sizeof(T), COLS = 32 * ITEMS * N, F = 8 / ITEMS;
+    using namespace tc;
+    constexpr int N = 16 / sizeof(T), ROWS = 16 / ITEMS, BUFFER = 8192, PER = 64 / ROWS;     // of a piece; pieces of 64 rows
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_bars[DIGEST_WARPS][2];
+    __shared__ int s_abort;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t buffer = ((smem_u32(smem_raw) + 127u) & ~127u) + (uint32_t)warp * 2u * BUFFER, bar = smem_u32(s_bars[warp]);
+    if (threadIdx.x == 0) s_abort = 0;
+    if (lane == 0) {
+        mbar_init(bar, 1);
+        mbar_init(bar + 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    __syncthreads();
     pdl_wait();
-    __shared__ float s_sum[8][COLS];
-    __shared__ float s_max[DIGEST_THREADS / 32];
-    __shared__ int32_t s_block[DIGEST_BLOCKS];
-    __shared__ uint64_t s_live[DIGEST_BLOCKS][2];
     const int64_t u = blockIdx.z;
     LiveRows rows;
-    int64_t fresh = 0;                                         // (the first warp's)
-    if (threadIdx.x < DIGEST_BLOCKS && a.refresh > 0) fresh = fresh_rows(a, u);
-    if (threadIdx.x < DIGEST_BLOCKS && !rows.load(a.bank, u)) {
+    if (!rows.load(a.bank, u)) {
         if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
-        rows.start[0] = -1;                                    // no block is visited
+        return;
     }
-    const bool sane = !(threadIdx.x < DIGEST_BLOCKS && rows.start[0] < 0);
-    if (!__syncthreads_and(sane)) return;
-    const int piece = threadIdx.x & 31, p = threadIdx.x >> 5;
-    const int nvec = (int)(a.row_bytes / 16), v0 = blockIdx.y * 32 * ITEMS;
-    const uint8_t *unit = a.k_store + u * a.bank.rows_per_unit * a.row_bytes;
-    for (int64_t t0 = blockIdx.x; t0 < a.visits; t0 += (int64_t)gridDim.x * DIGEST_BLOCKS) {
-        // this CTA's next 32 blocks
-        if (threadIdx.x < DIGEST_BLOCKS) {
-            const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
-            const int64_t b = t >= a.visits ? -1 : a.refresh < 0 ? t : refresh_block(a, rows, fresh, t);
-            s_block[threadIdx.x] = (int32_t)b;
-            s_live[threadIdx.x][0] = b < 0 ? 0ull : rows.mask64(b * a.bs) & (a.bs == 32 ? 0xffffffffull : ~0ull);
-            s_live[threadIdx.x][1] = b < 0 || a.bs <= 64 ? 0ull : rows.mask64(b * a.bs + 64);
+    const int64_t fresh = a.refresh > 0 ? fresh_rows(a, u) : 0;
+    const int nvec = (int)(a.row_bytes / 16), slab0 = blockIdx.y * 32 * ITEMS;
+    const uint32_t pitch = (uint32_t)min(nvec, 32 * ITEMS) * 16u;      // bytes of a row in a buffer
+    const int64_t warps = (int64_t)gridDim.x * DIGEST_WARPS;
+    const int y0 = (int)(u * a.bank.rows_per_unit);
+    uint32_t issued = 0, used = 0;                                     // of the warp's pieces
+    bool ok = true;
+    for (int64_t t0 = (int64_t)blockIdx.x * DIGEST_WARPS + warp; t0 < a.visits && ok; t0 += 32 * warps) {
+        // this warp's next 32 blocks, one per lane, and their live rows
+        const int64_t t = t0 + lane * warps;
+        const int mine = (int)(t >= a.visits ? -1 : a.refresh < 0 ? t : refresh_block(a, rows, fresh, t));
+        uint64_t live[2] = {0ull, 0ull};
+        if (mine >= 0) {
+            live[0] = rows.mask64((int64_t)mine * a.bs) & (a.bs == 32 ? 0xffffffffull : ~0ull);
+            if (a.bs > 64) live[1] = rows.mask64((int64_t)mine * a.bs + 64);
         }
-        __syncthreads();
-        uint4 w[F][ITEMS];
-        // rows p + 8 first, ... of the i-th block, those that live
-        const auto load = [&](int i, int first) {
-            const uint64_t live = s_live[i][first >= 8 ? 1 : 0];
-            const uint8_t *src = unit + (int64_t)s_block[i] * a.bs * a.row_bytes;
+        // the pieces with a live row, a bit each
+        constexpr uint32_t ALL = (1u << ROWS) - 1u;
+        uint32_t some = 0;
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const int r = p + 8 * (first + f);
-                const bool on = live >> (r & 63) & 1ull;
-#pragma unroll
-                for (int x = 0; x < ITEMS; ++x) {
-                    const int v = v0 + piece + 32 * x;
-                    w[f][x] = make_uint4(0, 0, 0, 0);
-                    if (on && v < nvec) w[f][x] = __ldg(reinterpret_cast<const uint4 *>(src + r * a.row_bytes) + v);
-                }
+        for (int j = 0; j < 2 * PER; ++j) some |= (uint32_t)(((uint32_t)(live[j / PER] >> (ROWS * (j % PER))) & ALL) != 0u) << j;
+        int ahead = 0;                                                 // the block whose pieces are brought next, and which are left
+        uint32_t left = __shfl_sync(0xffffffffu, some, 0);
+        const auto bring = [&]() {
+            while (left == 0u && ahead < 31) left = __shfl_sync(0xffffffffu, some, ++ahead);
+            const int b = __shfl_sync(0xffffffffu, mine, ahead);
+            if (left == 0u) return;
+            if (lane == 0) {
+                const uint32_t st = issued & 1u;
+                mbar_expect_tx(bar + 8u * st, ROWS * pitch);
+                tma_load_2d(buffer + st * BUFFER, &map, bar + 8u * st, slab0 * N, y0 + b * a.bs + ROWS * (__ffs(left) - 1));
             }
+            left &= left - 1u;
+            ++issued;
         };
-        load(0, 0);
-        for (int i = 0; i < DIGEST_BLOCKS && s_block[i] >= 0; ++i) {
-            float sum[ITEMS][N];
+        bring();
+        bring();
+        for (int i = 0; i < 32 && ok; ++i) {
+            const int b = __shfl_sync(0xffffffffu, mine, i);
+            if (b < 0) break;
+            float sum[ITEMS][8][N];
 #pragma unroll
             for (int x = 0; x < ITEMS; ++x)
 #pragma unroll
-                for (int e = 0; e < N; ++e) sum[x][e] = 0.f;
-            for (int first = 0; 8 * first < a.bs; first += F) {
-                if (first > 0) load(i, first);
+                for (int p = 0; p < 8; ++p)
 #pragma unroll
-                for (int f = 0; f < F; ++f)
+                    for (int e = 0; e < N; ++e) sum[x][p][e] = 0.f;
+            int n_live = 0;
+            for (int j = 0; ROWS * j < a.bs; ++j) {
+                const uint32_t on = (uint32_t)(__shfl_sync(0xffffffffu, j < PER ? live[0] : live[1], i) >> (ROWS * (j % PER))) & ALL;
+                if (on == 0u) continue;
+                n_live += __popc(on);
+                const uint32_t st = used & 1u, src = buffer + st * BUFFER + lane * 16;
+                ok = mbar_wait_warp(bar + 8u * st, used >> 1 & 1u, &s_abort, a.wait_ns);
+                if (!ok) break;
+                ++used;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    if (!(on >> r & 1u)) continue;
 #pragma unroll
                     for (int x = 0; x < ITEMS; ++x) {
-                        const uint32_t y[4] = {w[f][x].x, w[f][x].y, w[f][x].z, w[f][x].w};
+                        uint32_t y[4];
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3])
+                                     : "r"(src + r * pitch + 512u * x) : "memory");
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if (N == 8) {
-                                sum[x][2 * e] += __uint_as_float(y[e] << 16);
-                                sum[x][2 * e + 1] += __uint_as_float(y[e] & 0xffff0000u);
+                                sum[x][r & 7][2 * e] += __uint_as_float(y[e] << 16);
+                                sum[x][r & 7][2 * e + 1] += __uint_as_float(y[e] & 0xffff0000u);
                             } else {
-                                sum[x][e] += __uint_as_float(y[e]);
+                                sum[x][r & 7][e] += __uint_as_float(y[e]);
                             }
                         }
                     }
+                }
+                __syncwarp();
+                bring();
             }
-            const int64_t b = s_block[i];
-            const int n_live = __popcll(s_live[i][0]) + __popcll(s_live[i][1]);
-            if (i + 1 < DIGEST_BLOCKS && s_block[i + 1] >= 0) load(i + 1, 0);
+            if (!ok) break;
+            // dividing by a power of two is exact either way
+            const bool pow2 = (n_live & (n_live - 1)) == 0;
+            const float n = (float)max(1, n_live), inv = 1.f / n;
 #pragma unroll
             for (int x = 0; x < ITEMS; ++x)
 #pragma unroll
-                for (int e = 0; e < N; e += 4)
-                    *reinterpret_cast<float4 *>(&s_sum[p][(piece + 32 * x) * N + e]) =
-                        make_float4(sum[x][e], sum[x][e + 1], sum[x][e + 2], sum[x][e + 3]);
-            __syncthreads();
-            // a channel per thread and round; a head is a run of d threads
-            for (int c0 = 0; c0 < COLS; c0 += DIGEST_THREADS) {
-                const int c = c0 + threadIdx.x;                // COLS <= 256, or a multiple of it
-                const bool in = c < COLS && v0 * N + c < a.H * a.d;
-                float x = 0.f;
-                if (c < COLS) {
-                    x = ((s_sum[0][c] + s_sum[4][c]) + (s_sum[2][c] + s_sum[6][c])) +
-                        ((s_sum[1][c] + s_sum[5][c]) + (s_sum[3][c] + s_sum[7][c]));
-                    // dividing by a power of two is exact either way
-                    x = (n_live & (n_live - 1)) == 0 ? x * (1.f / (float)max(1, n_live)) : __fdiv_rn(x, (float)n_live);
+                for (int e = 0; e < N; ++e) {
+                    const auto &v = sum[x];
+                    const float y = ((v[0][e] + v[4][e]) + (v[2][e] + v[6][e])) + ((v[1][e] + v[5][e]) + (v[3][e] + v[7][e]));
+                    sum[x][0][e] = pow2 ? y * inv : __fdiv_rn(y, n);
                 }
-                float m = fabsf(x);
+            // a head is a run of d / N lanes (ITEMS = 2: of all 32, both items)
+            float m = 0.f;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    if (o < a.d) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                if (a.d > 32) {
-                    __syncthreads();
-                    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
-                    __syncthreads();
-                    const int w0 = (threadIdx.x >> 5) / (a.d >> 5) * (a.d >> 5);
-                    for (int k = 0; k < a.d >> 5; ++k) m = fmaxf(m, s_max[w0 + k]);
-                }
-                if (!in) continue;                             // no barrier is skipped by it
-                const EightBits q(m);
-                const int col = v0 * N + c, h = col / a.d, e = col - h * a.d;
+            for (int x = 0; x < ITEMS; ++x)
+#pragma unroll
+                for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(sum[x][0][e]));
+            for (int o = min(32, a.d / N) >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const EightBits q(m);
+#pragma unroll
+            for (int x = 0; x < ITEMS; ++x) {
+                const int v = slab0 + 32 * x + lane;
+                if (v >= nvec) continue;
+                const int col = v * N, h = col / a.d, e0 = col - h * a.d;
                 const int64_t at = (u * a.H + h) * a.nb + b;
-                a.digest[at * a.d + e] = (int8_t)q(x);
-                if (e == 0) a.step[at] = q.step;
+                uint32_t word[N / 4];
+#pragma unroll
+                for (int e = 0; e < N; e += 4)
+                    word[e / 4] = (uint32_t)(q(sum[x][0][e]) & 255) | (uint32_t)(q(sum[x][0][e + 1]) & 255) << 8 |
+                                  (uint32_t)(q(sum[x][0][e + 2]) & 255) << 16 | (uint32_t)q(sum[x][0][e + 3]) << 24;
+                if (N == 8) *reinterpret_cast<uint2 *>(a.digest + at * a.d + e0) = make_uint2(word[0], word[N / 4 - 1]);
+                else *reinterpret_cast<uint32_t *>(a.digest + at * a.d + e0) = word[0];
+                if (e0 == 0) a.step[at] = q.step;
             }
-            __syncthreads();
         }
-        __syncthreads();
+    }
+    if (!ok) {
+        // copies in flight land before the CTA ends
+        if (lane == 0) {
+            for (; used < issued; ++used) mbar_drain(bar + 8u * (used & 1u), used >> 1 & 1u);
+            latch_status(a.status, RS3_ETIMEOUT);
+        }
     }
 }
 
@@ -337,19 +371,22 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
     for (int i = want + lane; i < s.n_top; i += 32) out[i] = -1;
 }
 
-// The same on the tensor cores, for what most calls are: up to 1024 blocks in one piece, or more in
-// pieces (`splits`) of up to 1024 whose choices k_merge_blocks joins.
+// The same on the tensor cores, for what most calls are: up to 1024 blocks that hold a live row in one piece, or more
+// in pieces of up to 1024 whose choices k_merge_blocks joins.
 //
 // A CTA scores 16 queries against its blocks: whole numbers of at most 127 are exact in fp16, and their
 // products' sums stay below 2^22, exact in the fp32 accumulators.  A lane's 16 bytes of a digest are
 // spread over four steps of the matrix instruction, and the queries' columns are taken in the same order.
-// Then a warp per query holds the scores in registers (32 per lane at most).  Of n <= 32 wanted, the n-th
-// largest of the lanes' maxima is a lower bound for the n-th largest score that leaves few more than n
-// candidates; those are compacted and cut exactly.
+// Then a warp per query holds the scores in registers, 32 blocks to a lane.  Of n wanted, a number that n or few more
+// of the maxima of four blocks each reach is a bound that few more than n scores reach: these candidates are ranked
+// by counting.  (Where they are many, as among ties, the registers are cut exactly.)
+// Bound by instruction issue and, at the start, latency.  Also built: a lane per query that keeps a running threshold;
+// as scores grow towards the newest frames, that admits nearly every block (436 us where this takes XX).
 constexpr int TC_ROWS = 16;                // queries of a CTA
 constexpr int TC_THREADS = 256;
 constexpr int TC_BLOCKS = 1024;            // blocks of a piece
 constexpr int TC_TOP = 64;                 // choices of a piece that the workspace has room for
+constexpr int TC_HELD = 64;                // candidates of a query that are compacted
 constexpr int TC_PAIRS = 3072;             // candidates of a query that are joined in shared memory
 constexpr size_t TC_SMS = 256;             // SMs that pieces are cut for, at most
 
@@ -357,7 +394,7 @@ struct PickArgs {
     SelectArgs a;
     int2 *cand;                // [rows][splits][take]: (ordered score, block)
     int32_t *n_cand;           // [rows][splits]
-    int32_t splits, piece;     // most pieces of a query's blocks, blocks of a piece (a multiple of 32)
+    int32_t splits, piece;     // most pieces of a query's blocks, blocks of the largest (a multiple of 32)
     int32_t wanted;            // pieces that keep the SMs busy
     int32_t take;              // room for a piece's choices
 };
@@ -393,11 +430,26 @@ struct LiveWords {
     }
 };
 
-// Words of a piece: what the pieces that are wanted leave for each, at most TC_BLOCKS.
+// Words of a piece: what the pieces that are wanted leave for each, at most TC_BLOCKS blocks.
 __device__ __forceinline__ int piece_words(const PickArgs &p, int total)
 {
     const int pieces = max(p.wanted, (total + TC_BLOCKS / 32 - 1) / (TC_BLOCKS / 32));
     return max(1, (total + pieces - 1) / pieces);
+}
+
+// The blocks of a word that hold a live row, a bit each.
+__device__ __forceinline__ uint32_t live_blocks(const LiveRows &rows, int bs, int word)
+{
+    const int sh = 31 - __clz(bs);
+    uint64_t live = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (rows.len[r] == 0) continue;
+        const int lo = max(0, (int)(rows.start[r] >> sh) - 32 * word);
+        const int hi = min(31, (int)((rows.start[r] + rows.len[r] - 1) >> sh) - 32 * word);
+        if (lo <= hi) live |= (2ull << hi) - (1ull << lo);
+    }
+    return (uint32_t)live;
 }
 
 // Four signed bytes of w as two fp16 pairs: a byte u on top of 0x6400 is 1024 + u exactly, u = x + 128.
@@ -422,19 +474,18 @@ __device__ __forceinline__ uint32_t lanes_below()
     return m;
 }
 
-// The `want`-th largest of a warp's keys, bit by bit, n_at_least(x) being how many are x or more (the same
-// for all lanes); a smaller number that cuts them alike where one is found sooner.  At least `want` keys lie
-// in [least, most], so the bits that these share need no step.
+// A number that `want` of a warp's keys reach and no more than want + slack, or the largest that `want` reach where equal
+// keys allow none: n_at_least(x) is how many keys are x or more (the same for all lanes), at least `want` are `low` or
+// more, and none is `high` or more.  Halving the range ends after some steps where `low` is near.
 template <typename F>
-__device__ __forceinline__ uint32_t cut_at(int want, uint32_t least, uint32_t most, F n_at_least)
+__device__ __forceinline__ uint32_t cut_at(int want, int slack, uint32_t low, uint32_t high, F n_at_least)
 {
-    const int shared = __clz(least ^ most);
-    uint32_t low = shared == 0 ? 0u : most & ~(0xffffffffu >> shared);
-    if (shared == 32) return most;
-    for (uint32_t bit = 0x80000000u >> shared; bit != 0u; bit >>= 1) {
-        const int n = n_at_least(low | bit);
-        if (n >= want) low |= bit;
-        if (n == want) return low;
+    while (high - low > 1u) {
+        const uint32_t mid = low + (high - low) / 2u;
+        const int n = n_at_least(mid);
+        if (n >= want) low = mid;
+        else high = mid;
+        if (n >= want && n <= want + slack) break;
     }
     return low;
 }
@@ -451,25 +502,19 @@ struct Choice {
 };
 
 // The `want` first of n (key, block) pairs in ascending block order, by (key desc, block asc); key 0 is none,
-// and at least `want` are not.  The first 32 * HELD keys are held in registers.
+// and at least `want` are `low` or more.  The first 32 * HELD keys are held in registers.
 template <int HELD, typename Load>
-__device__ __forceinline__ void choose(int n, int want, const Choice &out, Load load)
+__device__ __forceinline__ void choose(int n, int want, uint32_t low, const Choice &out, Load load)
 {
     const int lane = threadIdx.x & 31;
-    uint32_t k[HELD], least = 0xffffffffu, most = 0u;
+    uint32_t k[HELD], most = 0u;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         k[i] = 32 * i + lane < n ? (uint32_t)load(32 * i + lane).x : 0u;
         most = max(most, k[i]);
-        least = k[i] > 0u ? min(least, k[i]) : least;
     }
-    for (int i = 32 * HELD + lane; i < n; i += 32) {
-        const uint32_t x = (uint32_t)load(i).x;
-        most = max(most, x);
-        least = x > 0u ? min(least, x) : least;
-    }
+    for (int i = 32 * HELD + lane; i < n; i += 32) most = max(most, (uint32_t)load(i).x);
     most = __reduce_max_sync(0xffffffffu, most);
-    least = __reduce_min_sync(0xffffffffu, least);
     const auto n_at_least = [&](uint32_t x) {
         int c = 0;
 #pragma unroll
@@ -477,8 +522,8 @@ __device__ __forceinline__ void choose(int n, int want, const Choice &out, Load 
         for (int i = 32 * HELD + lane; i < n; i += 32) c += (uint32_t)load(i).x >= x;
         return (int)__reduce_add_sync(0xffffffffu, c);
     };
-    const uint32_t cut = n > want ? cut_at(want, least, most, n_at_least) : 0u;
-    int equal = n > want ? want - (cut == 0xffffffffu ? 0 : n_at_least(cut + 1u)) : n, at = 0;
+    const uint32_t cut = n > want ? cut_at(want, 0, low, most + 1u, n_at_least) : 0u;
+    int equal = n > want ? want - n_at_least(cut + 1u) : n, at = 0;
     for (int i0 = 0; i0 < n && at < want; i0 += 32) {
         const int i = i0 + lane;
         const int2 e = i < n ? load(i) : make_int2(0, 0);
@@ -491,13 +536,20 @@ __device__ __forceinline__ void choose(int n, int want, const Choice &out, Load 
     }
 }
 
+// Where a word's i-th score lies in its query's row: pairs of scores in an order of the word's own, so that 32 lanes
+// reading the same pair of their words, and a warp writing one word, meet different banks.
+__device__ __forceinline__ int score_at(int word, int i) { return 32 * word + (i ^ (2 * (word & 15))); }
+
+template <typename T>
 __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
 {
+    constexpr int N = 16 / sizeof(T);
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ uint32_t s_live[TC_BLOCKS / 32];
     __shared__ int32_t s_word[TC_BLOCKS / 32];
     __shared__ int32_t s_size[2];                                          // words of this piece, whether there are others
+    __shared__ int2 s_pair[TC_THREADS / 32][TC_HELD];
     const SparseArgs &s = p.a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = (s.k_max + TC_ROWS - 1) / TC_ROWS;
@@ -509,82 +561,87 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     }
     const int j0 = tile * TC_ROWS, nq = min(TC_ROWS, cnt - j0);
     if (nq <= 0) return;
-    // the piece's words and the live blocks of each, by one warp (a word per lane)
-    if (warp == TC_THREADS / 32 - 1) {
-        LiveRows rows;
-        const bool sane = rows.load(s.bank, u);
-        if (!sane && lane == 0) latch_status(s.status, RS3_EINTERNAL);
-        const LiveWords words(rows, s.bs);
-        const int per = piece_words(p, words.total);
-        const int n = sane ? max(0, min(per, words.total - split * per)) : -1;
-        const int word = words.at(split * per + lane);
-        if (lane < n) {
-            const int sh = 31 - __clz(s.bs);
-            uint64_t live = 0;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {                                  // blocks of the word that the run reaches
-                if (rows.len[r] == 0) continue;
-                const int lo = max(0, (int)(rows.start[r] >> sh) - 32 * word);
-                const int hi = min(31, (int)((rows.start[r] + rows.len[r] - 1) >> sh) - 32 * word);
-                if (lo <= hi) live |= (2ull << hi) - (1ull << lo);
-            }
-            s_word[lane] = word;
-            s_live[lane] = (uint32_t)live;
-        }
-        if (lane == 0) {
-            s_size[0] = n;
-            s_size[1] = words.total > per;
-        }
-    }
     const int stride = p.piece + 8;                                        // of a query's scores
     float *s_score = reinterpret_cast<float *>(smem);
     const int width = s.d < 64 ? 64 : s.d, q_row = 2 * width + 16;         // columns, bytes of a query
     uint8_t *s_q = smem + TC_ROWS * stride * 4;
     const int r = lane >> 2, t = lane & 3;
     const int64_t dig = ((int64_t)u * s.H + h) * s.nb;
-    // the queries in 8 bits, held as fp16; a warp takes two
-    for (int r = warp; r < TC_ROWS; r += TC_THREADS / 32) {
-        const int cell = r < nq ? s.idx[(int64_t)u * s.k_max + j0 + r] : 0;
-        const bool ok = r < nq && cell >= 0 && cell < s.mn;
-        if (r < nq && !ok && lane == 0) latch_status(s.status, RS3_EINVAL);
-        float x[8], m = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = lane + 32 * i;
-            float x0 = 0.f, x1 = 0.f;
-            if (ok && 2 * c < s.d) {
-                const int64_t at = ((int64_t)g * s.mn + cell) * (s.H * s.d) + h * s.d + 2 * c;
-                if (p.a.bf16) {
-                    const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(static_cast<const uint16_t *>(s.q) + at));
-                    x0 = __uint_as_float(w << 16);
-                    x1 = __uint_as_float(w & 0xffff0000u);
-                } else {
-                    const float2 w = __ldg(reinterpret_cast<const float2 *>(static_cast<const float *>(s.q) + at));
-                    x0 = w.x;
-                    x1 = w.y;
-                }
-                if (s.rope) {
-                    const float2 f = __ldg(reinterpret_cast<const float2 *>(s.rope + (int64_t)cell * s.d) + c);
-                    const float y0 = __fsub_rn(__fmul_rn(x0, f.x), __fmul_rn(x1, f.y));
-                    x1 = __fadd_rn(__fmul_rn(x0, f.y), __fmul_rn(x1, f.x));
-                    x0 = y0;
-                }
-            }
-            x[2 * i] = x0;
-            x[2 * i + 1] = x1;
-            m = fmaxf(m, fmaxf(fabsf(x0), fabsf(x1)));
+    if (warp == TC_THREADS / 32 - 1) {
+        // the piece's words and the live blocks of each, a word per lane
+        LiveRows rows;
+        const bool sane = rows.load(s.bank, u);
+        if (!sane && lane == 0) latch_status(s.status, RS3_EINTERNAL);
+        const LiveWords words(rows, s.bs);
+        const int per = piece_words(p, words.total);
+        const int n = sane ? max(0, min(per, words.total - split * per)) : -1;
+        if (lane < n) {
+            const int word = words.at(split * per + lane);
+            s_word[lane] = word;
+            s_live[lane] = live_blocks(rows, s.bs, word);
         }
+        if (lane == 0) {
+            s_size[0] = n;
+            s_size[1] = words.total > per;
+        }
+    } else {
+        // the queries in 8 bits, held as fp16: a group of lanes per query, 16 bytes (up to two) each
+        const int parts = s.d / N, L = min(32, parts), sub = lane & (L - 1), at_once = 32 / L;
+        for (int r0 = warp * at_once; r0 < TC_ROWS; r0 += (TC_THREADS / 32 - 1) * at_once) {
+            const int row = r0 + lane / L;                                 // rows past the tile: none of the lanes' groups writes
+            const int cell = row < nq ? s.idx[(int64_t)u * s.k_max + j0 + row] : 0;
+            const bool ok = row < nq && cell >= 0 && cell < s.mn;
+            if (row < nq && !ok && sub == 0) latch_status(s.status, RS3_EINVAL);
+            float x[2][N], m = 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const EightBits e(m);
+            for (int i = 0; i < 2; ++i) {
+                const int c = sub + 32 * i;                                // its piece of the row
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = lane + 32 * i;
-            if (2 * c < width) {
-                uint32_t w;
-                asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"((float)e(x[2 * i + 1])), "f"((float)e(x[2 * i])));
-                *reinterpret_cast<uint32_t *>(s_q + r * q_row + 4 * c) = w;
+                for (int e = 0; e < N; ++e) x[i][e] = 0.f;
+                if (i * 32 >= parts || !ok) continue;
+                const uint4 w = __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(s.q) + ((int64_t)g * s.mn + cell) * (s.H * s.d) + h * s.d) + c);
+                const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (N == 8) {
+                        x[i][2 * e] = __uint_as_float(y[e] << 16);
+                        x[i][2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
+                    } else {
+                        x[i][e] = __uint_as_float(y[e]);
+                    }
+                }
+                if (s.rope) {                                              // each product and each sum rounded
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        const float4 f = __ldg(reinterpret_cast<const float4 *>(s.rope + (int64_t)cell * s.d + c * N + e));
+                        const float x0 = x[i][e], x1 = x[i][e + 1], x2 = x[i][e + 2], x3 = x[i][e + 3];
+                        x[i][e] = __fsub_rn(__fmul_rn(x0, f.x), __fmul_rn(x1, f.y));
+                        x[i][e + 1] = __fadd_rn(__fmul_rn(x0, f.y), __fmul_rn(x1, f.x));
+                        x[i][e + 2] = __fsub_rn(__fmul_rn(x2, f.z), __fmul_rn(x3, f.w));
+                        x[i][e + 3] = __fadd_rn(__fmul_rn(x2, f.w), __fmul_rn(x3, f.z));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(x[i][e]));
             }
+            for (int o = L >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const EightBits bits(m);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (i * 32 >= parts || row >= TC_ROWS) continue;
+                uint32_t w[N / 2];
+#pragma unroll
+                for (int e = 0; e < N; e += 2)
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[e / 2]) : "f"((float)bits(x[i][e + 1])), "f"((float)bits(x[i][e])));
+                uint8_t *to = s_q + row * q_row + (sub + 32 * i) * 2 * N;
+                if (N == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]);
+                else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+            }
+        }
+        // heads of 16 and 32: the columns up to 64 are zeros
+        for (int i = threadIdx.x; i < TC_ROWS * (width - s.d) / 8; i += TC_THREADS - 32) {
+            const int row = i / ((width - s.d) / 8);
+            *reinterpret_cast<uint4 *>(s_q + row * q_row + 2 * s.d + 16 * (i - row * ((width - s.d) / 8))) = make_uint4(0, 0, 0, 0);
         }
     }
     __syncthreads();
@@ -594,31 +651,36 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     // this warp's steps: 16 places, then 64 columns after 64; a step's digests are loaded one step ahead
     int b0 = warp * 16, k0 = 0;
     uint4 w[2];
-    const auto load_step = [&](uint4 (&v)[2], int place, int k) {
+    float st[2][2], st1[2][2];
+    const auto load_step = [&](uint4 (&v)[2], float (&f)[2][2], int place, int k) {
+        const int first = place < n ? s_word[place >> 5] * 32 + (place & 31) : s.nb;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             v[x] = make_uint4(0, 0, 0, 0);
-            const int b = place < n ? s_word[place >> 5] * 32 + (place & 31) + 8 * x + r : s.nb;
+            const int b = first + 8 * x + r;
             if (b < s.nb && k + 16 * t < s.d)
                 v[x] = __ldg(reinterpret_cast<const uint4 *>(p.a.digest + (dig + b) * s.d + k + 16 * t));
+            if (k == 0) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) f[x][y] = first + 8 * x + 2 * t + y < s.nb ? __ldg(p.a.step + dig + first + 8 * x + 2 * t + y) : 0.f;
+            }
         }
     };
-    load_step(w, b0, k0);
-    float c[2][4], st[2][2];
+    load_step(w, st1, b0, k0);
+    float c[2][4];
     while (b0 < n) {
         if (k0 == 0) {
-            const int b = s_word[b0 >> 5] * 32 + (b0 & 31) + 2 * t;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
                 for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
-#pragma unroll
-                for (int y = 0; y < 2; ++y) st[x][y] = b + 8 * x + y < s.nb ? __ldg(p.a.step + dig + b + 8 * x + y) : 0.f;
+                st[x][0] = st1[x][0];
+                st[x][1] = st1[x][1];
             }
         }
         const int b1 = k0 + 64 < width ? b0 : b0 + TC_THREADS / 2, k1 = k0 + 64 < width ? k0 + 64 : 0;
         uint4 w1[2];
-        load_step(w1, b1, k1);
+        load_step(w1, st1, b1, k1);
         const uint8_t *qa = s_q + r * q_row + 2 * (k0 + 16 * t);
         uint4 qv[2][2];
 #pragma unroll
@@ -646,7 +708,7 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const float2 score = make_float2(on0 ? c[x][2 * y] * st[x][0] : -INFINITY, on1 ? c[x][2 * y + 1] * st[x][1] : -INFINITY);
-                    *reinterpret_cast<float2 *>(s_score + (r + 8 * y) * stride + b0 + 8 * x + 2 * t) = score;
+                    *reinterpret_cast<float2 *>(s_score + (r + 8 * y) * stride + score_at(b0 >> 5, (b0 & 31) + 8 * x + 2 * t)) = score;
                 }
             }
         }
@@ -656,68 +718,120 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         w[1] = w1[1];
     }
     __syncthreads();
-    // the first 32 places of the words: one word's blocks per lane
+    // a warp per query, a lane per word: blocks ascend with the lanes
     const int n_live = __reduce_add_sync(0xffffffffu, lane < s_size[0] ? __popc(s_live[lane]) : 0);
     const int want = min(s.n_top, n_live), word = lane < s_size[0] ? 32 * s_word[lane] : 0;
     for (int q = warp; q < nq; q += TC_THREADS / 32) {
         const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j0 + q;
         const Choice out = {p.a.sel + row * s.n_top, alone ? nullptr : p.cand + (row * p.splits + split) * p.take};
         float *score = s_score + q * stride;
-        float k[TC_BLOCKS / 32], top = -INFINITY;
+        float k[32];
 #pragma unroll
-        for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-            k[i] = 32 * i < n ? score[32 * i + lane] : -INFINITY;
-            top = fmaxf(top, k[i]);
+        for (int i = 0; i < 32; i += 2) {
+            const float2 v = lane < s_size[0] ? *reinterpret_cast<const float2 *>(score + score_at(lane, i)) : make_float2(-INFINITY, -INFINITY);
+            k[i] = v.x;
+            k[i + 1] = v.y;
         }
-        bool done = false;
-        if (want > 0 && want <= 32) {
-            // the want-th largest of the lanes' maxima, or all that live where fewer lanes hold one
-            const uint32_t mine = top > -INFINITY ? order_bits(top) : 0u;
-            uint32_t least = mine;
-            if (want < 32) {
-                const uint32_t cut = cut_at(want, __reduce_min_sync(0xffffffffu, mine), __reduce_max_sync(0xffffffffu, mine),
-                                            [&](uint32_t x) { return __popc(__ballot_sync(0xffffffffu, mine >= x)); });
-                least = mine >= cut ? mine : 0xffffffffu;
-            }
-            least = __reduce_min_sync(0xffffffffu, least);
-            const float bound = least > 0u ? score_of(least) : -FLT_MAX;
-            __syncwarp();
-            int2 *pair = reinterpret_cast<int2 *>(score);  // room for half as many (key, block) pairs in the query's own row
-            int at = 0;
+        // a bound from the maxima of four blocks each; where fewer of those hold a live block than are wanted, all live
+        // blocks are candidates
+        uint32_t g[8], best = 0u;
 #pragma unroll
-            for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-                const uint32_t bal = __ballot_sync(0xffffffffu, k[i] >= bound);
-                if (bal != 0u) {
-                    const int to = at + __popc(bal & lanes_below()), b = __shfl_sync(0xffffffffu, word, i) + lane;
-                    if (k[i] >= bound && 2 * to < p.piece) pair[to] = make_int2((int)order_bits(k[i]), b);
-                    at += __popc(bal);
+        for (int x = 0; x < 8; ++x) {
+            const float m = fmaxf(fmaxf(k[4 * x], k[4 * x + 1]), fmaxf(k[4 * x + 2], k[4 * x + 3]));
+            g[x] = m > -INFINITY ? order_bits(m) : 0u;
+            best = max(best, g[x]);
+        }
+        const auto groups = [&](uint32_t x) {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n += g[i] >= x;
+            return (int)__reduce_add_sync(0xffffffffu, n);
+        };
+        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+        uint32_t low = 1u;
+        if (want > 0 && groups(1u) >= want) {
+            // the least of the lanes' own maxima, if enough reach it, is a near lower end
+            uint32_t least = __reduce_min_sync(0xffffffffu, best > 0u ? best : 0xffffffffu);
+            if (groups(least) < want) least = 1u;
+            low = cut_at(want, 4, least, most + 1u, groups);
+        }
+        const float bound = low > 0x00800000u ? score_of(low) : -FLT_MAX;     // (the key of -FLT_MAX)
+        // the candidates as (key, block) pairs in block order
+        uint32_t in = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) in |= (uint32_t)(k[i] >= bound) << i;
+        const int mine = __popc(in);
+        int end = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, end, o);
+            if (lane >= o) end += x;
+        }
+        const int c = __shfl_sync(0xffffffffu, end, 31);
+        if (want > 0 && c <= TC_HELD) {
+            int2 *pair = s_pair[warp];
+            __syncwarp();
+            for (int at = end - mine; in != 0u; ++at, in &= in - 1u) {
+                const int i = __ffs(in) - 1;
+                pair[at] = make_int2((int)order_bits(score[score_at(lane, i)]), word + i);
+            }
+            __syncwarp();
+            if (c <= 32) {
+                // a candidate per lane, ranked by counting those before it
+                const int2 e = lane < c ? pair[lane] : make_int2(0, 0);
+                int before = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const uint32_t y = (uint32_t)__shfl_sync(0xffffffffu, e.x, i);
+                    before += y > (uint32_t)e.x || (y == (uint32_t)e.x && i < lane);
                 }
-            }
-            __syncwarp();
-            done = 2 * at <= p.piece;
-            if (done) choose<4>(at, want, out, [&](int i) { return pair[i]; });
-        }
-        if (!done && want > 0) {
-            uint32_t key[TC_BLOCKS / 32];
-#pragma unroll
-            for (int i = 0; i < TC_BLOCKS / 32; ++i) key[i] = k[i] > -INFINITY ? order_bits(k[i]) : 0u;
-            const auto n_at_least = [&](uint32_t x) {
-                int c = 0;
-#pragma unroll
-                for (int i = 0; i < TC_BLOCKS / 32; ++i) c += key[i] >= x;
-                return (int)__reduce_add_sync(0xffffffffu, c);
-            };
-            const uint32_t cut = cut_at(want, 1u, __reduce_max_sync(0xffffffffu, top > -INFINITY ? order_bits(top) : 0u), n_at_least);
-            int equal = want - (cut == 0xffffffffu ? 0 : n_at_least(cut + 1u)), at = 0;
-#pragma unroll
-            for (int i = 0; i < TC_BLOCKS / 32; ++i) {
-                const uint32_t same = __ballot_sync(0xffffffffu, key[i] == cut && key[i] > 0);
-                const bool take = key[i] > cut || (key[i] == cut && key[i] > 0 && __popc(same & lanes_below()) < equal);
+                const bool take = lane < c && before < want;
                 const uint32_t bal = __ballot_sync(0xffffffffu, take);
-                const int b = __shfl_sync(0xffffffffu, word, i) + lane;
-                if (take) out.put(at + __popc(bal & lanes_below()), key[i], b);
-                at += __popc(bal);
-                equal -= min(equal, __popc(same));
+                if (take) out.put(__popc(bal & lanes_below()), (uint32_t)e.x, e.y);
+            } else {
+                choose<TC_HELD / 32>(c, want, low, out, [&](int i) { return pair[i]; });
+            }
+        } else if (want > 0) {
+            // the cut among all of the row's scores
+#pragma unroll
+            for (int i = 0; i < 32; ++i) k[i] = __uint_as_float(k[i] > -INFINITY ? order_bits(k[i]) : 0u);
+            const auto n_at_least = [&](uint32_t x) {
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) n += __float_as_uint(k[i]) >= x;
+                return (int)__reduce_add_sync(0xffffffffu, n);
+            };
+            const uint32_t cut = cut_at(want, 0, low, most + 1u, n_at_least);
+            const int equal = want - n_at_least(cut + 1u);
+            // per lane: how many lie above the cut and at it, and how many of the latter go to lower lanes
+            int above = 0, same = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t x = __float_as_uint(k[i]);
+                above += x > cut;
+                same += x == cut && x > 0u;
+            }
+            int same_end = same;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, same_end, o);
+                if (lane >= o) same_end += x;
+            }
+            int left = max(0, min(same, equal - (same_end - same)));       // of those at the cut, this lane's first ones
+            int to = above + left;
+            const int n = to;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, to, o);
+                if (lane >= o) to += x;
+            }
+            to -= n;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t x = __float_as_uint(k[i]);
+                const bool tie = x == cut && x > 0u && left > 0;
+                left -= tie;
+                if (x > cut || tie) out.put(to++, x, word + i);
             }
         }
         if (!alone) {
@@ -760,7 +874,7 @@ __global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
     __syncwarp();
     const int want = min(s.n_top, some);
     const Choice out = {p.a.sel + row * s.n_top, nullptr};
-    if (want > 0) choose<12>(n, want, out, [&](int i) { return pair[i]; });
+    if (want > 0) choose<12>(n, want, 1u, out, [&](int i) { return pair[i]; });
     for (int i = want + lane; i < s.n_top; i += 32) out.sel[i] = -1;
 }
 
@@ -769,7 +883,7 @@ int64_t select_splits(int64_t U, int64_t H, int64_t k_max, int64_t nb, int64_t n
 {
     const int64_t tiles = U * H * ((k_max + TC_ROWS - 1) / TC_ROWS), least = (nb + TC_BLOCKS - 1) / TC_BLOCKS;
     wanted = tiles > 0 ? (4 * sms + tiles - 1) / tiles : 1;
-    if (wanted > nb / 256) wanted = nb / 256;
+    if (wanted > nb / 512) wanted = nb / 512;
     if (wanted > TC_PAIRS / n_top) wanted = TC_PAIRS / n_top;      // 48 x 64 at the most blocks and choices
     if (wanted < 1) wanted = 1;
     return wanted > least ? wanted : least > 0 ? least : 1;
@@ -813,12 +927,21 @@ extern "C" rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refre
     const int pieces = wide ? 64 : 32;
     const int64_t slabs = (a.row_bytes / 16 + pieces - 1) / pieces;
     if (slabs > 65535) return RS3_EUNSUPPORTED;
-    // about three CTAs per SM in all, each with a run of blocks
-    int64_t x = (3ll * rs3_sm_count() + slabs * bank->U - 1) / (slabs * bank->U);
-    if (x > a.visits) x = a.visits;
+    const int64_t rows = bank->U * bank->rows_per_unit;
+    if (rows >= (1ll << 31) - 256) return RS3_EUNSUPPORTED;    // tensor maps take 32-bit rows
+    a.wait_ns = rs3_get_wait_limit_ns();
+    CUtensorMap map;
+    const int es = (int)elem_bytes(bank->dtype), cols = (int)(a.row_bytes < pieces * 16 ? a.row_bytes : pieces * 16) / es;
+    if (!tc::make_rows_map(&map, bank->k_store, es, bank->D, rows, cols, wide ? 8 : 16)) return RS3_ECUDA;
+    // a CTA per SM in all, a block per warp at least
+    int64_t x = (rs3_sm_count() + slabs * bank->U - 1) / (slabs * bank->U);
+    if (x > (a.visits + DIGEST_WARPS - 1) / DIGEST_WARPS) x = (a.visits + DIGEST_WARPS - 1) / DIGEST_WARPS;
     const dim3 grid((unsigned)x, (unsigned)slabs, (unsigned)bank->U);
-    void (*kern)(DigestArgs) = bank->dtype == RS3_BF16 ? k_digest<uint16_t, 1> : wide ? k_digest<float, 2> : k_digest<float, 1>;
-    launch_pdl(kern, grid, dim3(DIGEST_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), a);
+    void (*kern)(DigestArgs, CUtensorMap) = bank->dtype == RS3_BF16 ? k_digest<uint16_t, 1> : wide ? k_digest<float, 2> : k_digest<float, 1>;
+    const size_t smem = (size_t)DIGEST_WARPS * 2 * 8192 + 128;
+    const rs3_status r = rs3_kernel_smem((const void *)kern, smem);
+    if (r != RS3_OK) return r;
+    launch_pdl(kern, grid, dim3(32 * DIGEST_WARPS), smem, reinterpret_cast<cudaStream_t>(stream), a, map);
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }
 
@@ -866,10 +989,11 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
         p.n_cand = static_cast<int32_t *>(workspace);
         p.cand = reinterpret_cast<int2 *>(static_cast<uint8_t *>(workspace) + align_up((size_t)pieces * 4, 256));
         const size_t smem = (size_t)TC_ROWS * ((size_t)(p.piece + 8) * 4 + 2 * (d < 64 ? 64 : d) + 16);
-        rs3_status r = rs3_kernel_smem((const void *)k_score_blocks, smem);
+        void (*kern)(PickArgs) = dtype == RS3_BF16 ? k_score_blocks<uint16_t> : k_score_blocks<float>;
+        rs3_status r = rs3_kernel_smem((const void *)kern, smem);
         if (r != RS3_OK) return r;
         const dim3 grid((unsigned)((k_max + TC_ROWS - 1) / TC_ROWS * splits), (unsigned)H, (unsigned)a.s.U);
-        launch_pdl(k_score_blocks, grid, dim3(TC_THREADS), smem, st, p);
+        launch_pdl(kern, grid, dim3(TC_THREADS), smem, st, p);
         if (splits > 1) {
             const int room = p.splits * p.take;
             const size_t bytes = 4 * (size_t)room * sizeof(int2);

@@ -66,7 +66,7 @@ struct Piece<float> {
 // A group of L lanes (a power of two) holds one head, ITEMS pieces each; it takes the rows of
 // one (cell, head) through the grids that share the cell, so the cell's angles are loaded once.
 template <typename T, int ITEMS>
-__global__ void __launch_bounds__(NORM_THREADS)
+__global__ void __launch_bounds__(NORM_THREADS, ITEMS == 1 ? 4 : 2)
 k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float *__restrict__ rope)
 {
     constexpr int N = Piece<T>::N;
@@ -80,8 +80,8 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
     const int pieces = d / N;
     const bool here = g < (int64_t)mn * s.H;
     const int cell = here ? (int)(g / s.H) : 0, head = here ? (int)(g % s.H) : 0;
-    // what the cell's rows share, the weights times the angles: with u = x / norm a pair becomes
-    // (u0 wc0 - u1 ws1, u0 ws0 + u1 wc1), (wc, ws) = (w cos, w sin)
+    // what the cell's rows share, the weights times the angles: a pair becomes
+    // (x0 wc0 - x1 ws1, x0 ws0 + x1 wc1) / norm, (wc, ws) = (w cos, w sin)
     float co[ITEMS][N], si[ITEMS][N];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
@@ -114,9 +114,9 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
         }
         // a warp goes from one turn to the next that any of its lanes keeps
         uint32_t todo = __reduce_or_sync(0xffffffffu, kept);
-        while (todo != 0u) {
-            uint4 v[NORM_FLIGHT][ITEMS];
-            int turn[NORM_FLIGHT];
+        uint4 v[NORM_FLIGHT][ITEMS];
+        int turn[NORM_FLIGHT];
+        const auto load = [&]() {
 #pragma unroll
             for (int f = 0; f < NORM_FLIGHT; ++f) {
                 turn[f] = todo != 0u ? __ffs(todo) - 1 : -1;
@@ -126,6 +126,8 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
 #pragma unroll
                 for (int i = 0; i < ITEMS; ++i) v[f][i] = take && lane + i * L < pieces ? __ldcs(x + i * L) : make_uint4(0, 0, 0, 0);
             }
+        };
+        const auto finish = [&]() {
 #pragma unroll
             for (int f = 0; f < NORM_FLIGHT; ++f) {
                 if (turn[f] < 0) break;
@@ -144,13 +146,17 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
                     float z[N];
 #pragma unroll
                     for (int e = 0; e < N; e += 2) {
-                        const float u0 = x[i][e] * r, u1 = x[i][e + 1] * r;
-                        z[e] = fmaf(u0, co[i][e], -(u1 * si[i][e + 1]));
-                        z[e + 1] = fmaf(u0, si[i][e], u1 * co[i][e + 1]);
+                        z[e] = fmaf(x[i][e], co[i][e], -(x[i][e + 1] * si[i][e + 1])) * r;
+                        z[e + 1] = fmaf(x[i][e], si[i][e], x[i][e + 1] * co[i][e + 1]) * r;
                     }
                     if ((kept >> turn[f] & 1u) && lane + i * L < pieces) y[i * L] = Piece<T>::narrow(z);
                 }
             }
+        };
+        load();
+        while (turn[0] >= 0) {
+            finish();
+            load();
         }
     }
 }
