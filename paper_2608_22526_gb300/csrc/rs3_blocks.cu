@@ -371,8 +371,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
     for (int i = want + lane; i < s.n_top; i += 32) out[i] = -1;
 }
 
-// The same on the tensor cores, for what most calls are: up to 1024 blocks that hold a live row in one piece, or more
-// in pieces of up to 1024 whose choices k_merge_blocks joins.
+// The same on the tensor cores, for what most calls are: up to 992 blocks that hold a live row in one piece, or more
+// in pieces of up to 992 whose choices k_merge_blocks joins.
 //
 // A CTA scores 16 queries against its blocks: whole numbers of at most 127 are exact in fp16, and their
 // products' sums stay below 2^22, exact in the fp32 accumulators.  A lane's 16 bytes of a digest are
@@ -384,16 +384,17 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
 // as scores grow towards the newest frames, that admits nearly every block (436 us where this takes XX).
 constexpr int TC_ROWS = 16;                // queries of a CTA
 constexpr int TC_THREADS = 256;
-constexpr int TC_BLOCKS = 1024;            // blocks of a piece
+constexpr int TC_BLOCKS = 992;             // blocks of a piece: three CTAs per SM
 constexpr int TC_TOP = 64;                 // choices of a piece that the workspace has room for
 constexpr int TC_HELD = 64;                // candidates of a query that are compacted
-constexpr int TC_PAIRS = 3072;             // candidates of a query that are joined in shared memory
+constexpr int TC_PAIRS = 3264;             // candidates of a query that are joined in shared memory
 constexpr size_t TC_SMS = 256;             // SMs that pieces are cut for, at most
 
 struct PickArgs {
     SelectArgs a;
     int2 *cand;                // [rows][splits][take]: (ordered score, block)
     int32_t *n_cand;           // [rows][splits]
+    int32_t *n_pieces;         // [U]: pieces of a unit's queries
     int32_t splits, piece;     // most pieces of a query's blocks, blocks of the largest (a multiple of 32)
     int32_t wanted;            // pieces that keep the SMs busy
     int32_t take;              // room for a piece's choices
@@ -490,6 +491,8 @@ __device__ __forceinline__ uint32_t cut_at(int want, int slack, uint32_t low, ui
     return low;
 }
 
+constexpr uint32_t LEAST_KEY = 0x00800000u;                // of -FLT_MAX: every live block's score reaches it
+
 // Where the choices of a query go: the list itself, or a piece's candidates.
 struct Choice {
     int32_t *sel;
@@ -500,6 +503,25 @@ struct Choice {
         else sel[at] = block;
     }
 };
+
+// The `want` first of up to 64 (key, block) pairs in ascending block order, by (key desc, block asc): two to a lane,
+// counted by ballots.  At least `want` keys are `low` or more, none is above `most`; key 0 is none.
+__device__ __forceinline__ void choose_64(const int2 *pair, int n, int want, uint32_t low, uint32_t most, const Choice &out)
+{
+    const int lane = threadIdx.x & 31;
+    const int2 e0 = lane < n ? pair[lane] : make_int2(0, 0), e1 = lane + 32 < n ? pair[lane + 32] : make_int2(0, 0);
+    const uint32_t k0 = (uint32_t)e0.x, k1 = (uint32_t)e1.x;
+    const auto ballots = [&](bool a, bool b) { return __popc(__ballot_sync(0xffffffffu, a)) + (n > 32 ? __popc(__ballot_sync(0xffffffffu, b)) : 0); };
+    const uint32_t cut = n > want ? cut_at(want, 0, low, most + 1u, [&](uint32_t x) { return ballots(k0 >= x, k1 >= x); }) : 0u;
+    // of those at the cut, the first
+    const int ties = cut > 0u ? want - ballots(k0 > cut, k1 > cut) : 0;
+    const uint32_t same0 = __ballot_sync(0xffffffffu, k0 == cut), same1 = __ballot_sync(0xffffffffu, k1 == cut);
+    const bool take0 = k0 > cut || (k0 == cut && __popc(same0 & lanes_below()) < ties);
+    const bool take1 = k1 > cut || (k1 == cut && __popc(same0) + __popc(same1 & lanes_below()) < ties);
+    const uint32_t all0 = __ballot_sync(0xffffffffu, take0), all1 = __ballot_sync(0xffffffffu, take1);
+    if (take0) out.put(__popc(all0 & lanes_below()), k0, e0.y);
+    if (take1) out.put(__popc(all0) + __popc(all1 & lanes_below()), k1, e1.y);
+}
 
 // The `want` first of n (key, block) pairs in ascending block order, by (key desc, block asc); key 0 is none,
 // and at least `want` are `low` or more.  The first 32 * HELD keys are held in registers.
@@ -536,9 +558,9 @@ __device__ __forceinline__ void choose(int n, int want, uint32_t low, const Choi
     }
 }
 
-// Where a word's i-th score lies in its query's row: pairs of scores in an order of the word's own, so that 32 lanes
-// reading the same pair of their words, and a warp writing one word, meet different banks.
-__device__ __forceinline__ int score_at(int word, int i) { return 32 * word + (i ^ (2 * (word & 15))); }
+// Where a word's i-th score lies in its query's row: fours of scores in an order of the word's own, so that lanes
+// reading the same four of their words meet different banks.
+__device__ __forceinline__ int score_at(int word, int i) { return 32 * word + (i ^ (4 * (word & 7))); }
 
 template <typename T>
 __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
@@ -550,6 +572,7 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     __shared__ int32_t s_word[TC_BLOCKS / 32];
     __shared__ int32_t s_size[2];                                          // words of this piece, whether there are others
     __shared__ int2 s_pair[TC_THREADS / 32][TC_HELD];
+    __shared__ __align__(8) float s_step[TC_BLOCKS];                       // of the piece's blocks; NaN: no live row, it scores NaN
     const SparseArgs &s = p.a.s;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = (s.k_max + TC_ROWS - 1) / TC_ROWS;
@@ -583,6 +606,12 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         if (lane == 0) {
             s_size[0] = n;
             s_size[1] = words.total > per;
+            if (p.splits > 1 && tile == 0 && split == 0 && h == 0) p.n_pieces[u] = sane ? (words.total + per - 1) / per : 0;
+        }
+        __syncwarp();
+        for (int i = 0; i < n; ++i) {
+            const bool live = s_live[i] >> lane & 1u;
+            s_step[32 * i + lane] = live ? __ldg(p.a.step + dig + 32 * s_word[i] + lane) : __int_as_float(0x7fffffff);
         }
     } else {
         // the queries in 8 bits, held as fp16: a group of lanes per query, 16 bytes (up to two) each
@@ -651,36 +680,27 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     // this warp's steps: 16 places, then 64 columns after 64; a step's digests are loaded one step ahead
     int b0 = warp * 16, k0 = 0;
     uint4 w[2];
-    float st[2][2], st1[2][2];
-    const auto load_step = [&](uint4 (&v)[2], float (&f)[2][2], int place, int k) {
+    const uint8_t *digests = reinterpret_cast<const uint8_t *>(p.a.digest) + (dig * s.d + r * s.d + 16 * t);
+    const auto load_step = [&](uint4 (&v)[2], int place, int k) {
         const int first = place < n ? s_word[place >> 5] * 32 + (place & 31) : s.nb;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             v[x] = make_uint4(0, 0, 0, 0);
-            const int b = first + 8 * x + r;
-            if (b < s.nb && k + 16 * t < s.d)
-                v[x] = __ldg(reinterpret_cast<const uint4 *>(p.a.digest + (dig + b) * s.d + k + 16 * t));
-            if (k == 0) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) f[x][y] = first + 8 * x + 2 * t + y < s.nb ? __ldg(p.a.step + dig + first + 8 * x + 2 * t + y) : 0.f;
-            }
+            if (first + 8 * x + r < s.nb && k + 16 * t < s.d) v[x] = __ldg(reinterpret_cast<const uint4 *>(digests + (int64_t)(first + 8 * x) * s.d + k));
         }
     };
-    load_step(w, st1, b0, k0);
+    load_step(w, b0, k0);
     float c[2][4];
     while (b0 < n) {
         if (k0 == 0) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
-                st[x][0] = st1[x][0];
-                st[x][1] = st1[x][1];
-            }
         }
         const int b1 = k0 + 64 < width ? b0 : b0 + TC_THREADS / 2, k1 = k0 + 64 < width ? k0 + 64 : 0;
         uint4 w1[2];
-        load_step(w1, st1, b1, k1);
+        load_step(w1, b1, k1);
         const uint8_t *qa = s_q + r * q_row + 2 * (k0 + 16 * t);
         uint4 qv[2][2];
 #pragma unroll
@@ -701,15 +721,12 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         }
         if (k1 == 0) {
             // this lane holds places 8 x + 2 t, + 1 of queries r and r + 8
-            const uint32_t live = s_live[b0 >> 5] >> (b0 & 31);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const bool on0 = live >> (8 * x + 2 * t) & 1u, on1 = live >> (8 * x + 2 * t + 1) & 1u;
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const float2 score = make_float2(on0 ? c[x][2 * y] * st[x][0] : -INFINITY, on1 ? c[x][2 * y + 1] * st[x][1] : -INFINITY);
-                    *reinterpret_cast<float2 *>(s_score + (r + 8 * y) * stride + score_at(b0 >> 5, (b0 & 31) + 8 * x + 2 * t)) = score;
-                }
+                const float2 f = *reinterpret_cast<const float2 *>(s_step + b0 + 8 * x + 2 * t);
+                float *to = s_score + r * stride + score_at(b0 >> 5, (b0 & 31) + 8 * x + 2 * t);
+                *reinterpret_cast<float2 *>(to) = make_float2(c[x][0] * f.x, c[x][1] * f.y);
+                *reinterpret_cast<float2 *>(to + 8 * stride) = make_float2(c[x][2] * f.x, c[x][3] * f.y);
             }
         }
         b0 = b1;
@@ -727,39 +744,39 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         float *score = s_score + q * stride;
         float k[32];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            const float2 v = lane < s_size[0] ? *reinterpret_cast<const float2 *>(score + score_at(lane, i)) : make_float2(-INFINITY, -INFINITY);
-            k[i] = v.x;
-            k[i + 1] = v.y;
+        for (int i = 0; i < 32; i += 4) {
+            const float4 v = lane < s_size[0] ? *reinterpret_cast<const float4 *>(score + score_at(lane, i)) : make_float4(NAN, NAN, NAN, NAN);
+            k[i] = v.x; k[i + 1] = v.y; k[i + 2] = v.z; k[i + 3] = v.w;
         }
-        // a bound from the maxima of four blocks each; where fewer of those hold a live block than are wanted, all live
-        // blocks are candidates
-        uint32_t g[8], best = 0u;
+        // a bound from the maxima of four blocks each (a NaN is passed over); where fewer of those hold a live block than are
+        // wanted, all live blocks are candidates
+        float g[8], best = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            const float m = fmaxf(fmaxf(k[4 * x], k[4 * x + 1]), fmaxf(k[4 * x + 2], k[4 * x + 3]));
-            g[x] = m > -INFINITY ? order_bits(m) : 0u;
-            best = max(best, g[x]);
+            g[x] = fmaxf(fmaxf(k[4 * x], k[4 * x + 1]), fmaxf(k[4 * x + 2], k[4 * x + 3]));
+            best = fmaxf(best, g[x]);
         }
         const auto groups = [&](uint32_t x) {
+            const float f = score_of(x);
             int n = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) n += g[i] >= x;
+            for (int i = 0; i < 8; ++i) n += g[i] >= f;
             return (int)__reduce_add_sync(0xffffffffu, n);
         };
-        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
-        uint32_t low = 1u;
-        if (want > 0 && groups(1u) >= want) {
+        const uint32_t most = __reduce_max_sync(0xffffffffu, best > -INFINITY ? order_bits(best) : 0u);
+        uint32_t low = LEAST_KEY;
+        if (want > 0) {
             // the least of the lanes' own maxima, if enough reach it, is a near lower end
-            uint32_t least = __reduce_min_sync(0xffffffffu, best > 0u ? best : 0xffffffffu);
-            if (groups(least) < want) least = 1u;
-            low = cut_at(want, 4, least, most + 1u, groups);
+            const uint32_t least = __reduce_min_sync(0xffffffffu, best > -INFINITY ? order_bits(best) : 0xffffffffu);
+            if (groups(least) >= want) low = cut_at(want, 4, least, most + 1u, groups);
+            else if (groups(LEAST_KEY) >= want) low = cut_at(want, 4, LEAST_KEY, least, groups);
         }
-        const float bound = low > 0x00800000u ? score_of(low) : -FLT_MAX;     // (the key of -FLT_MAX)
+        const float bound = score_of(low);
         // the candidates as (key, block) pairs in block order
         uint32_t in = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) in |= (uint32_t)(k[i] >= bound) << i;
+        for (int i = 0; i < 32; ++i)
+            asm("{\n\t.reg .pred p;\n\tsetp.ge.f32 p, %1, %2;\n\t@p or.b32 %0, %0, %3;\n\t}" : "+r"(in) : "f"(k[i]), "f"(bound), "r"(1u << i));
         const int mine = __popc(in);
         int end = mine;
 #pragma unroll
@@ -776,25 +793,11 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
                 pair[at] = make_int2((int)order_bits(score[score_at(lane, i)]), word + i);
             }
             __syncwarp();
-            if (c <= 32) {
-                // a candidate per lane, ranked by counting those before it
-                const int2 e = lane < c ? pair[lane] : make_int2(0, 0);
-                int before = 0;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const uint32_t y = (uint32_t)__shfl_sync(0xffffffffu, e.x, i);
-                    before += y > (uint32_t)e.x || (y == (uint32_t)e.x && i < lane);
-                }
-                const bool take = lane < c && before < want;
-                const uint32_t bal = __ballot_sync(0xffffffffu, take);
-                if (take) out.put(__popc(bal & lanes_below()), (uint32_t)e.x, e.y);
-            } else {
-                choose<TC_HELD / 32>(c, want, low, out, [&](int i) { return pair[i]; });
-            }
+            choose_64(pair, c, want, low, most, out);
         } else if (want > 0) {
             // the cut among all of the row's scores
 #pragma unroll
-            for (int i = 0; i < 32; ++i) k[i] = __uint_as_float(k[i] > -INFINITY ? order_bits(k[i]) : 0u);
+            for (int i = 0; i < 32; ++i) k[i] = __uint_as_float(k[i] > -INFINITY ? order_bits(k[i]) : 0u);     // (NaN: 0)
             const auto n_at_least = [&](uint32_t x) {
                 int n = 0;
 #pragma unroll
@@ -853,14 +856,12 @@ __global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
     const int j = blockIdx.x * 4 + warp, h = blockIdx.y, u = blockIdx.z;
     const int cnt = s.count[u], g = s.unit_group[u];
     if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G || j >= cnt) return;
-    LiveRows rows;
-    if (!rows.load(s.bank, u)) return;
-    const int total = LiveWords(rows, s.bs).total, per = piece_words(p, total);
-    if (total <= per) return;                              // one piece: its choices are the list
     const int64_t row = ((int64_t)u * s.H + h) * s.k_max + j;
+    const int pieces = p.n_pieces[u];
+    if (pieces <= 1) return;                               // (its choices are the list; or the unit was refused)
     int2 *pair = s_pairs + warp * room;
     // places without a candidate hold key 0
-    const int n = (total + per - 1) / per * p.take;
+    const int n = pieces * p.take;
     int some = 0;
 #pragma unroll 4
     for (int i = lane; i < n; i += 32) {
@@ -874,8 +875,545 @@ __global__ void __launch_bounds__(128) k_merge_blocks(PickArgs p, int room)
     __syncwarp();
     const int want = min(s.n_top, some);
     const Choice out = {p.a.sel + row * s.n_top, nullptr};
-    if (want > 0) choose<12>(n, want, 1u, out, [&](int i) { return pair[i]; });
+    if (want > 0 && n <= 64) choose_64(pair, n, want, 1u, 0xfffffffeu, out);
+    else if (want > 0) choose<12>(n, want, 1u, out, [&](int i) { return pair[i]; });
     for (int i = want + lane; i < s.n_top; i += 32) out.sel[i] = -1;
+}
+
+// ---------------------------------------------------------------------------
+// selection for many queries
+// ---------------------------------------------------------------------------
+constexpr int TILE_ROWS = 128;             // queries of a CTA
+constexpr int TILE_THREADS = 256;          // a warp per 32 queries, three for the digests, one that issues
+constexpr int TILE_COLS = 64;              // blocks of a tile: two words
+constexpr int TILE_TOP = 32;               // most blocks per query
+constexpr int TILE_WORDS = 512;            // most words of a unit
+
+struct TileArgs {
+    SelectArgs a;
+    int32_t cap;               // room for a query's candidates: n_top + 33 at least
+    uint64_t wait_ns;          // limit of each wait
+};
+
+// The blocks that hold a live row, as four runs.
+struct LiveBlocks {
+    int32_t first[4], last[4];
+    __device__ __forceinline__ LiveBlocks(const LiveRows &rows, int bs)
+    {
+        const int sh = 31 - __clz(bs);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            first[r] = rows.len[r] > 0 ? (int)(rows.start[r] >> sh) : 0;
+            last[r] = rows.len[r] > 0 ? (int)((rows.start[r] + rows.len[r] - 1) >> sh) : -1;
+        }
+    }
+    __device__ __forceinline__ bool holds(int b) const
+    {
+        bool in = false;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) in |= b >= first[r] && b <= last[r];
+        return in;
+    }
+};
+
+// A lane's run of floats in shared memory, -infinity behind the last; runs begin an odd number of 16 bytes apart, so
+// lanes that read the same four of theirs meet different banks.
+struct Column {
+    float *v;
+
+    __device__ __forceinline__ void clear(int from, int to) const
+    {
+        for (; from < to && (from & 3) != 0; ++from) v[from] = -INFINITY;
+        for (; from < to; from += 4) *reinterpret_cast<float4 *>(v + from) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    }
+
+    // how many are x or more, among the first `most` (the same for the warp)
+    __device__ __forceinline__ int at_least(float x, int most) const
+    {
+        int c[4] = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 0; i < most; i += 4) {
+            const float4 y = *reinterpret_cast<const float4 *>(v + i);
+            c[0] += y.x >= x;
+            c[1] += y.y >= x;
+            c[2] += y.z >= x;
+            c[3] += y.w >= x;
+        }
+        return (c[0] + c[1]) + (c[2] + c[3]);
+    }
+};
+
+// Bitonic networks in registers, without a branch: a full sort of 32, and the merge of a bitonic run, descending.
+__device__ __forceinline__ void merge_down_32(float (&x)[32])
+{
+#pragma unroll
+    for (int lj = 4; lj >= 0; --lj)
+#pragma unroll
+        for (int n = 0; n < 16; ++n) {
+            const int i = (n >> lj) << (lj + 1) | (n & ((1 << lj) - 1)), j = i + (1 << lj);
+            const float hi = fmaxf(x[i], x[j]), lo = fminf(x[i], x[j]);
+            x[i] = hi;
+            x[j] = lo;
+        }
+}
+
+__device__ __forceinline__ void sort_32(float (&x)[32])
+{
+#pragma unroll
+    for (int lk = 1; lk <= 5; ++lk)
+#pragma unroll
+        for (int lj = lk - 1; lj >= 0; --lj)
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+                // the n-th pair 2^lj apart, descending where bit lk of the first is 0
+                const int i = (n >> lj) << (lj + 1) | (n & ((1 << lj) - 1)), j = i + (1 << lj);
+                const float hi = fmaxf(x[i], x[j]), lo = fminf(x[i], x[j]);
+                x[i] = (i >> lk & 1) == 0 ? hi : lo;
+                x[j] = (i >> lk & 1) == 0 ? lo : hi;
+            }
+}
+
+// The want-th largest (from 1, at most 32) of the first `most` of a column: 32 after 32 are sorted and merged into the 32
+// largest so far, some 21 instructions for each of 32 queries' entries.  A search by halving, which goes on
+// for the slowest lane, took five times as long.
+__device__ __forceinline__ float nth_largest(const Column &c, int most, int want)
+{
+    float top[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top[i] = -INFINITY;
+    for (int i0 = 0; i0 < most; i0 += 32) {
+        float x[32];
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {                  // (a column ends at a multiple of four)
+            const float4 t = i0 + i < most ? *reinterpret_cast<const float4 *>(c.v + i0 + i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            x[i] = t.x; x[i + 1] = t.y; x[i + 2] = t.z; x[i + 3] = t.w;
+        }
+        sort_32(x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) top[i] = fmaxf(top[i], x[31 - i]);
+        merge_down_32(top);
+    }
+    float y = top[0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i)                           // (chosen like this, the array stays in registers)
+        asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %2, %3;\n\t@p mov.f32 %0, %1;\n\t}" : "+f"(y) : "f"(top[i]), "r"(want), "r"(i + 1));
+    return y;
+}
+
+// Candidates of a lane's query in block order.
+struct Candidates {
+    Column score;
+    uint16_t *block;
+    int n;
+
+    // Cuts down the lanes that hold more than `want` to the best by (score desc, block asc); for those the key of the
+    // want-th, else `low`.
+    __device__ __forceinline__ uint32_t cut(int want, uint32_t low)
+    {
+        const bool over = n > want;
+        const int most = __reduce_max_sync(0xffffffffu, over ? n : 0);
+        if (most == 0) return low;
+        const uint32_t key = order_bits(nth_largest(score, most, want));
+        const float x = score_of(key);
+        // of those that equal it, the first stay
+        int ties = want - score.at_least(score_of(key + 1u), most);
+        // four at a time, predicated: what stays moves down, in order
+        const uint32_t first = static_cast<uint32_t>(__cvta_generic_to_shared(score.v));
+        uint32_t at = first, at_block = static_cast<uint32_t>(__cvta_generic_to_shared(block));
+        for (int i = 0; i < most; i += 4) {
+            const float4 t = *reinterpret_cast<const float4 *>(score.v + i);
+            const float y[4] = {t.x, t.y, t.z, t.w};
+            const uint2 b = *reinterpret_cast<const uint2 *>(block + i);
+            const uint16_t id[4] = {(uint16_t)b.x, (uint16_t)(b.x >> 16), (uint16_t)b.y, (uint16_t)(b.y >> 16)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool tie = y[e] == x, in = over && (y[e] > x || (tie && ties > 0));
+                ties -= tie;
+                asm volatile("{\n\t.reg .pred p;\n\t"
+                             "setp.ne.s32 p, %2, 0;\n\t"
+                             "@p st.shared.f32 [%0], %3;\n\t"
+                             "@p st.shared.u16 [%1], %4;\n\t"
+                             "@p add.u32 %0, %0, 4;\n\t"
+                             "@p add.u32 %1, %1, 2;\n\t}"
+                             : "+r"(at), "+r"(at_block) : "r"((int)in), "f"(y[e]), "h"(id[e]) : "memory");
+            }
+        }
+        const int to = (int)(at - first) >> 2;
+        if (!over) return low;
+        score.clear(to, n);
+        n = to;
+        return key;
+    }
+};
+
+// A CTA takes 128 queries of a head and its blocks in tiles of 64, twice; tcgen05 gives the scores, a query per lane of
+// tensor memory, and a thread goes through its query's scores by itself.
+//   first pass   the maxima of groups of blocks (8 or more).  The n_top-th largest of them is a bound that n_top scores or
+//                few more reach, whatever the blocks' order.
+//   second pass  the scores that reach the bound, in block order, as candidates in shared memory; where they are too
+//                many (ties, or fewer groups than choices), they are cut down and the bound rises.
+// Then the candidates are cut to n_top.  Three warps spread the digests (fp16, 128-byte swizzle) a tile ahead, one issues
+// the products.  Per query this takes a third of k_score_blocks' instructions, but a CTA goes through all of the
+// blocks twice, so it is for calls whose queries fill the SMs: 23 700 queries over 987 blocks 70 us against 117, 757 over
+// 4 700 the other way round (74 against 47).
+template <typename T>
+__global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
+{
+    using namespace tc;
+    constexpr int N = 16 / sizeof(T), ISSUER = 7;           // warps 0 to 3: queries, 4 to 6: digests
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t s_bars[9];
+    __shared__ __align__(16) float s_step[2][TILE_COLS];
+    __shared__ int32_t s_word[TILE_WORDS + 4];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    const SparseArgs &s = p.a.s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_wait();
+    const int h = blockIdx.y, u = blockIdx.z;
+    int cnt, g;
+    LiveRows rows;
+    if (!sparse_unit(s, u, threadIdx.x == 0, cnt, g, rows)) return;
+    const int j0 = blockIdx.x * TILE_ROWS, nq = min(TILE_ROWS, cnt - j0);
+    if (nq <= 0) return;
+    const LiveWords words(rows, s.bs);
+    const int n_words = words.total;
+    if (n_words == 0) {                                    // nothing to choose from
+        const int64_t row0 = ((int64_t)u * s.H + h) * s.k_max + j0;
+        for (int i = threadIdx.x; i < nq * s.n_top; i += TILE_THREADS) p.a.sel[row0 * s.n_top + i] = -1;
+        return;
+    }
+    const int n_tiles = (n_words + 1) / 2;
+
+    // shared memory: queries [128] and two tiles' digests [64], fp16, in 64-column blocks; then the candidates
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - raw);
+    const int width = s.d < 64 ? 64 : s.d, q_bytes = TILE_ROWS * 2 * width, b_bytes = TILE_COLS * 2 * width;
+    uint8_t *s_b = smem + q_bytes;
+    const int cap = p.cap;
+    float *s_cand = reinterpret_cast<float *>(s_b + 2 * b_bytes) + (threadIdx.x & 127) * cap;
+    uint16_t *s_block = reinterpret_cast<uint16_t *>(s_b + 2 * b_bytes + TILE_ROWS * cap * 4) + (threadIdx.x & 127) * cap;
+    const uint32_t bars = smem_u32(s_bars);
+    const uint32_t SFULL = bars, SFREE = bars + 16, BFULL = bars + 32, BFREE = bars + 48, DRAIN = bars + 64;
+    volatile int *abort_flag = &s_abort;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(SFULL + 8 * i, 2);                   // the commit, and the issuing thread for the steps
+            mbar_init(SFREE + 8 * i, 4);
+            mbar_init(BFULL + 8 * i, 3);
+            mbar_init(BFREE + 8 * i, 1);
+        }
+        mbar_init(DRAIN, 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    if (warp == ISSUER) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(2 * TILE_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // the words; none behind the last
+    for (int i = threadIdx.x; i < 2 * n_tiles; i += TILE_THREADS) s_word[i] = i < n_words ? 32 * words.at(i) : -1;
+    if (s.d < 64)                                          // the columns up to 64 are zeros
+        for (int i = threadIdx.x; i < (TILE_ROWS + 2 * TILE_COLS) * 8; i += TILE_THREADS) *reinterpret_cast<uint4 *>(smem + 16 * i) = make_uint4(0, 0, 0, 0);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+
+    {
+        // the queries in 8 bits, 16 per warp: a group of lanes per query, 16 bytes each; four groups' rows
+        // are loaded together
+        const int parts = s.d / N, L = min(32, parts), sub = lane & (L - 1), at_once = 32 / L, first = 16 * warp;
+        const int my_cell = (lane < 16 && first + lane < nq) ? s.idx[(int64_t)u * s.k_max + j0 + first + lane] : -1;
+        if (lane < 16 && first + lane < nq && (my_cell < 0 || my_cell >= s.mn)) latch_status(s.status, RS3_EINVAL);
+        const T *grid = static_cast<const T *>(s.q) + (int64_t)g * s.mn * (s.H * s.d) + h * s.d;
+        constexpr int F = 4;
+        for (int r0 = 0; r0 < 16; r0 += F * at_once) {
+            uint4 v[F][1];
+            float4 f[F][1][N / 4];
+            int cells[F];
+#pragma unroll
+            for (int x = 0; x < F; ++x) {
+                const int row = r0 + x * at_once + lane / L, cell = __shfl_sync(0xffffffffu, my_cell, row & 15);
+                cells[x] = row < 16 && cell >= 0 && cell < s.mn ? cell : -1;
+#pragma unroll
+                for (int i = 0; i < 1; ++i) {
+                    const int c = sub + 32 * i;            // its piece of the row
+                    v[x][i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < N / 4; ++e) f[x][i][e] = make_float4(1.f, 0.f, 1.f, 0.f);
+                    if (i * 32 >= parts || cells[x] < 0) continue;
+                    v[x][i] = __ldg(reinterpret_cast<const uint4 *>(grid + (int64_t)cells[x] * (s.H * s.d)) + c);
+                    if (s.rope)
+#pragma unroll
+                        for (int e = 0; e < N / 4; ++e) f[x][i][e] = __ldg(reinterpret_cast<const float4 *>(s.rope + (int64_t)cells[x] * s.d + c * N) + e);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < F; ++x) {
+                const int row = r0 + x * at_once + lane / L;
+                float z[1][N], m = 0.f;
+#pragma unroll
+                for (int i = 0; i < 1; ++i) {
+                    const uint32_t y[4] = {v[x][i].x, v[x][i].y, v[x][i].z, v[x][i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (N == 8) {
+                            z[i][2 * e] = __uint_as_float(y[e] << 16);
+                            z[i][2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
+                        } else {
+                            z[i][e] = __uint_as_float(y[e]);
+                        }
+                    }
+                    if (s.rope) {                          // each product and each sum rounded
+#pragma unroll
+                        for (int e = 0; e < N; e += 4) {
+                            const float4 t = f[x][i][e / 4];
+                            const float x0 = z[i][e], x1 = z[i][e + 1], x2 = z[i][e + 2], x3 = z[i][e + 3];
+                            z[i][e] = __fsub_rn(__fmul_rn(x0, t.x), __fmul_rn(x1, t.y));
+                            z[i][e + 1] = __fadd_rn(__fmul_rn(x0, t.y), __fmul_rn(x1, t.x));
+                            z[i][e + 2] = __fsub_rn(__fmul_rn(x2, t.z), __fmul_rn(x3, t.w));
+                            z[i][e + 3] = __fadd_rn(__fmul_rn(x2, t.w), __fmul_rn(x3, t.z));
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(z[i][e]));
+                }
+                for (int o = L >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const EightBits bits(m);
+#pragma unroll
+                for (int i = 0; i < 1; ++i) {
+                    if (i * 32 >= parts || row >= 16) continue;
+                    uint32_t w[N / 2];
+#pragma unroll
+                    for (int e = 0; e < N; e += 2)
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[e / 2]) : "f"((float)bits(z[i][e + 1])), "f"((float)bits(z[i][e])));
+                    const int c = sub + 32 * i;            // N fp16 columns: a chunk of 8, or half of one
+                    uint8_t *to = smem + sw128_offset(TILE_ROWS, first + row, c * N / 8) + (N == 8 ? 0 : (c & 1) * 8);
+                    if (N == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]);
+                    else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+                }
+            }
+        }
+        fence_proxy_async();
+    }
+    __syncthreads();
+
+    // step k: tile k mod n_tiles, scores and digests in buffer k mod 2
+    if (warp >= 4 && warp < ISSUER) {
+        // digests: pieces of 16 bytes, a word's 2 d after the other's, loaded a step ahead
+        constexpr int CONVERT = 96, MOST = (4 * 128 + CONVERT - 1) / CONVERT;
+        const int pt = threadIdx.x - 128, n_pieces = 4 * s.d, sh = 31 - __clz(s.d / 16), n_x = (n_pieces + CONVERT - 1) / CONVERT;
+        const uint8_t *digests = reinterpret_cast<const uint8_t *>(p.a.digest) + ((int64_t)u * s.H + h) * s.nb * s.d;
+        uint4 v[MOST];
+        const auto load_tile = [&](int i) {
+            const int word[2] = {s_word[2 * i], s_word[2 * i + 1]};
+#pragma unroll
+            for (int x = 0; x < MOST; ++x) {
+                if (x >= n_x) break;
+                const int e = pt + CONVERT * x, second = e >= 2 * s.d;
+                const int first = second ? word[1] : word[0], b = first + ((e >> sh) & 31);
+                v[x] = make_uint4(0, 0, 0, 0);
+                if (e < n_pieces && first >= 0 && b < s.nb)
+                    v[x] = __ldg(reinterpret_cast<const uint4 *>(digests + (int64_t)first * s.d + 16 * (e - (second ? 2 * s.d : 0))));
+            }
+        };
+        load_tile(0);
+        for (int k = 0, i = 0; k < 2 * n_tiles; ++k) {
+            const uint32_t buf = k & 1, ph = k >> 1 & 1;
+            if (!mbar_wait_warp(BFREE + 8 * buf, ph ^ 1u, abort_flag, p.wait_ns)) break;
+#pragma unroll
+            for (int x = 0; x < MOST; ++x) {
+                const int e = pt + CONVERT * x;
+                if (x >= n_x) break;
+                if (e >= n_pieces) continue;
+                const int row = e >> sh, ch = 2 * (e & ((1 << sh) - 1));
+                uint32_t w[8];
+                bytes_to_fp16(v[x].x, w[0], w[1]);
+                bytes_to_fp16(v[x].y, w[2], w[3]);
+                bytes_to_fp16(v[x].z, w[4], w[5]);
+                bytes_to_fp16(v[x].w, w[6], w[7]);
+                *reinterpret_cast<uint4 *>(s_b + buf * b_bytes + sw128_offset(TILE_COLS, row, ch)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(s_b + buf * b_bytes + sw128_offset(TILE_COLS, row, ch + 1)) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+            i = i + 1 == n_tiles ? 0 : i + 1;
+            if (k + 1 < 2 * n_tiles) load_tile(i);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BFULL + 8 * buf);
+        }
+    } else if (warp == ISSUER) {
+        // steps of the tile's blocks (a block without a live row scores NaN: it reaches nothing), and the products
+        const LiveBlocks live(rows, s.bs);
+        const float *steps = p.a.step + ((int64_t)u * s.H + h) * s.nb;
+        const auto step_of = [&](int word) {
+            const int b = word + lane;
+            return word >= 0 && b < s.nb && live.holds(b) ? __ldg(steps + b) : __int_as_float(0x7fffffff);
+        };
+        float step[2] = {step_of(s_word[0]), step_of(s_word[1])};
+        constexpr uint32_t ID = (1u << 4) | ((uint32_t)(TILE_COLS >> 3) << 17) | ((uint32_t)(TILE_ROWS >> 4) << 24);   // fp16 in, fp32 out
+        const uint64_t dq = desc_sw128((uint32_t)uniform((int)base), 16, 1024);
+        const uint32_t tm = (uint32_t)uniform((int)tmem);
+        for (int k = 0, i = 0; k < 2 * n_tiles; ++k) {
+            const uint32_t buf = k & 1, ph = k >> 1 & 1;
+            // the buffer's last scores have been read, and with them its steps
+            if (!mbar_wait_warp(SFREE + 8 * buf, ph ^ 1u, abort_flag, p.wait_ns)) break;
+            s_step[buf][lane] = step[0];
+            s_step[buf][lane + 32] = step[1];
+            i = i + 1 == n_tiles ? 0 : i + 1;
+            if (k + 1 < 2 * n_tiles) {
+                step[0] = step_of(s_word[2 * i]);
+                step[1] = step_of(s_word[2 * i + 1]);
+            }
+            __syncwarp();
+            if (!mbar_wait_warp(BFULL + 8 * buf, ph, abort_flag, p.wait_ns)) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t db = desc_sw128(base + (uint32_t)q_bytes + buf * (uint32_t)b_bytes, 16, 1024);
+#pragma unroll 4
+                for (int kk = 0; kk < width / 16; ++kk) {
+                    const uint32_t oq = (uint32_t)((kk >> 2) * (TILE_ROWS * 128) + (kk & 3) * 32), ob = (uint32_t)((kk >> 2) * (TILE_COLS * 128) + (kk & 3) * 32);
+                    tc_mma(tm + TILE_COLS * buf, dq + (oq >> 4), db + (ob >> 4), ID, kk > 0 ? 1u : 0u);
+                }
+                tc_commit(SFULL + 8 * buf);
+                tc_commit(BFREE + 8 * buf);
+                mbar_arrive(SFULL + 8 * buf);
+            }
+            __syncwarp();
+        }
+        if (elect_one()) {                                 // every product is done before the tensor memory goes
+            tc_commit(DRAIN);
+            mbar_drain(DRAIN, 0);
+        }
+        __syncwarp();
+    } else {
+        const int q = threadIdx.x;
+        const bool mine = q < nq, busy = (q & ~31) < nq;
+        const uint32_t tl = tmem + ((uint32_t)(q & ~31) << 16);
+        const int places = TILE_COLS * n_tiles;
+        int blocks = 8;                                    // blocks of a maximum
+        while (places > blocks * cap) blocks *= 2;
+        const int n_maxima = (places + blocks - 1) / blocks;
+        Candidates c = {{s_cand}, s_block, 0};
+        c.score.clear(0, cap);
+        // waits for the next scores and loads them, times their blocks' steps
+        uint32_t x[TILE_COLS];
+        int k = 0;
+        const auto next = [&]() {
+            const uint32_t buf = k & 1, ph = k >> 1 & 1;
+            ++k;
+            if (!mbar_wait_warp(SFULL + 8 * buf, ph, abort_flag, p.wait_ns)) return false;
+            tc_fence_after();
+            if (busy) {
+                tmem_ld_cols<TILE_COLS>(tl + TILE_COLS * buf, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int b = 0; b < TILE_COLS; b += 4) {
+                    const float4 f = *reinterpret_cast<const float4 *>(&s_step[buf][b]);
+                    x[b] = __float_as_uint(__uint_as_float(x[b]) * f.x);
+                    x[b + 1] = __float_as_uint(__uint_as_float(x[b + 1]) * f.y);
+                    x[b + 2] = __float_as_uint(__uint_as_float(x[b + 2]) * f.z);
+                    x[b + 3] = __float_as_uint(__uint_as_float(x[b + 3]) * f.w);
+                }
+                tc_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(SFREE + 8 * buf);
+            return true;
+        };
+        // first pass: the maxima (fmaxf passes over NaN)
+        bool ok = true;
+        float top = -INFINITY;
+        int at_max = 0;
+        for (int i = 0; i < n_tiles && ok; ++i) {
+            ok = next();
+            if (!ok || !busy) continue;
+#pragma unroll
+            for (int b = 0; b < TILE_COLS; b += 8) {
+                float m[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m[e] = fmaxf(__uint_as_float(x[b + e]), __uint_as_float(x[b + 4 + e]));
+                top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+                if (((TILE_COLS * i + b + 8) & (blocks - 1)) == 0) {
+                    c.score.v[at_max++] = top;
+                    top = -INFINITY;
+                }
+            }
+        }
+        if (busy && (places & (blocks - 1)) != 0) c.score.v[at_max] = top;
+        // the bound: the n_top-th largest of the maxima, which n_top scores reach; where fewer maxima hold a live block, every
+        // live one's score
+        float bound = INFINITY;
+        uint32_t low = LEAST_KEY;
+        if (ok && busy) {
+            const float nth = nth_largest(c.score, n_maxima, s.n_top);
+            if (nth > -INFINITY) low = order_bits(nth);
+            if (mine) bound = score_of(low);
+            c.score.clear(0, cap);
+        }
+        // second pass: the candidates
+        uint32_t at = smem_u32(s_cand), at_block = smem_u32(s_block);
+        for (int i = 0; i < n_tiles && ok; ++i) {
+            ok = next();
+            if (!ok || !busy) continue;
+#pragma unroll
+            for (int word = 0; word < TILE_COLS / 32; ++word) {
+                const uint32_t first = (uint32_t)s_word[2 * i + word];
+#pragma unroll
+                for (int b = 0; b < 32; ++b) {
+                    // predicated, as a branch per score would cost more than the stores
+                    const uint16_t block = (uint16_t)(first + b);
+                    asm volatile("{\n\t.reg .pred p;\n\t"
+                                 "setp.ge.f32 p, %2, %3;\n\t"
+                                 "@p st.shared.f32 [%0], %2;\n\t"
+                                 "@p st.shared.u16 [%1], %4;\n\t"
+                                 "@p add.u32 %0, %0, 4;\n\t"
+                                 "@p add.u32 %1, %1, 2;\n\t}"
+                                 : "+r"(at), "+r"(at_block) : "f"(__uint_as_float(x[32 * word + b])), "f"(bound), "h"(block) : "memory");
+                }
+                c.n = (int)(at - smem_u32(s_cand)) >> 2;
+                if (__any_sync(0xffffffffu, c.n > cap - 32)) {
+                    const bool over = c.n > s.n_top;
+                    low = c.cut(s.n_top, low);
+                    if (over) bound = score_of(low + 1u);  // later blocks have to be better
+                    at = smem_u32(s_cand) + 4u * c.n;
+                    at_block = smem_u32(s_block) + 2u * c.n;
+                }
+            }
+        }
+        if (ok && busy) {
+            // the choices: the candidates above the n_top-th largest, and of those that equal it the first
+            const int most = __reduce_max_sync(0xffffffffu, c.n);
+            float cut = -FLT_MAX;
+            int ties = c.n;
+            if (most > s.n_top) {
+                const uint32_t key = order_bits(nth_largest(c.score, most, s.n_top));
+                const int above = c.score.at_least(score_of(key + 1u), most);
+                if (c.n > s.n_top) {
+                    cut = score_of(key);
+                    ties = s.n_top - above;
+                }
+            }
+            if (mine) {
+                int32_t *out = p.a.sel + (((int64_t)u * s.H + h) * s.k_max + j0 + q) * s.n_top;
+                int to = 0;
+#pragma unroll 4
+                for (int e = 0; e < c.n; ++e) {
+                    const float y = s_cand[e];
+                    const bool tie = y == cut, take = y > cut || (tie && ties > 0);
+                    ties -= tie;
+                    if (take) out[to++] = s_block[e];
+                }
+                for (; to < s.n_top; ++to) out[to] = -1;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == ISSUER) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * TILE_COLS));
+    if (threadIdx.x == 0 && *abort_flag) latch_status(s.status, RS3_ETIMEOUT);
 }
 
 // Pieces of a query's blocks: as many as their size needs, more where that leaves SMs idle.
@@ -884,7 +1422,7 @@ int64_t select_splits(int64_t U, int64_t H, int64_t k_max, int64_t nb, int64_t n
     const int64_t tiles = U * H * ((k_max + TC_ROWS - 1) / TC_ROWS), least = (nb + TC_BLOCKS - 1) / TC_BLOCKS;
     wanted = tiles > 0 ? (4 * sms + tiles - 1) / tiles : 1;
     if (wanted > nb / 512) wanted = nb / 512;
-    if (wanted > TC_PAIRS / n_top) wanted = TC_PAIRS / n_top;      // 48 x 64 at the most blocks and choices
+    if (wanted > TC_PAIRS / n_top) wanted = TC_PAIRS / n_top;      // 50 x 64 at the most blocks and choices
     if (wanted < 1) wanted = 1;
     return wanted > least ? wanted : least > 0 ? least : 1;
 }
@@ -951,7 +1489,7 @@ extern "C" size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int 
     // rows x pieces: beyond what the blocks need, pieces only fill up four CTAs of 16 rows per SM
     const size_t rows = (size_t)U * (size_t)H * (size_t)k_max, least = ((size_t)n_blocks + TC_BLOCKS - 1) / TC_BLOCKS;
     const size_t pieces = 8 * TC_SMS * TC_ROWS + (least > 1 ? rows * (least + 1) : 0);
-    return 256 + align_up(pieces * 4, 256) + pieces * TC_TOP * sizeof(int2);
+    return 256 + align_up((pieces + (size_t)U) * 4, 256) + pieces * TC_TOP * sizeof(int2);
 }
 
 extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -973,6 +1511,19 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.step = step;
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
+    // Two CTAs of 128 queries per SM, where the queries fill the SMs and their candidates have room
+    const int fixed = (TILE_ROWS + 2 * TILE_COLS) * 2 * (d < 64 ? 64 : d) + 1024, each = TILE_ROWS * 6;
+    const int cap = (((106 * 1024 - fixed) / each / 4 - 1) | 1) * 4;       // an odd number of 16 bytes
+    if ((int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS) >= rs3_sm_count() && n_top <= TILE_TOP && cap >= n_top + 48 &&
+        a.s.nb <= 32 * TILE_WORDS) {
+        TileArgs p = {a, cap, rs3_get_wait_limit_ns()};
+        const size_t smem = (size_t)fixed + (size_t)cap * each;
+        void (*kern)(TileArgs) = dtype == RS3_BF16 ? k_score_tiles<uint16_t> : k_score_tiles<float>;
+        const rs3_status r = rs3_kernel_smem((const void *)kern, smem);
+        if (r != RS3_OK) return r;
+        launch_pdl(kern, dim3((unsigned)((k_max + TILE_ROWS - 1) / TILE_ROWS), (unsigned)H, (unsigned)a.s.U), dim3(TILE_THREADS), smem, st, p);
+        return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+    }
     const int sms = rs3_sm_count() < (int)TC_SMS ? rs3_sm_count() : (int)TC_SMS;
     int64_t wanted, splits = select_splits(a.s.U, H, k_max, a.s.nb, n_top, sms, wanted);
     if (n_top > TC_TOP && a.s.nb <= TC_BLOCKS) splits = wanted = 1;
@@ -987,10 +1538,11 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
         p.take = n_top < p.piece ? n_top : p.piece;
         const int64_t pieces = (int64_t)a.s.U * H * k_max * splits;
         p.n_cand = static_cast<int32_t *>(workspace);
-        p.cand = reinterpret_cast<int2 *>(static_cast<uint8_t *>(workspace) + align_up((size_t)pieces * 4, 256));
+        p.n_pieces = p.n_cand + pieces;
+        p.cand = reinterpret_cast<int2 *>(static_cast<uint8_t *>(workspace) + align_up((size_t)(pieces + a.s.U) * 4, 256));
         const size_t smem = (size_t)TC_ROWS * ((size_t)(p.piece + 8) * 4 + 2 * (d < 64 ? 64 : d) + 16);
         void (*kern)(PickArgs) = dtype == RS3_BF16 ? k_score_blocks<uint16_t> : k_score_blocks<float>;
-        rs3_status r = rs3_kernel_smem((const void *)kern, smem);
+        rs3_status r = rs3_kernel_smem((const void *)kern, smem + 16 * 1024);      // (its own static arrays count too)
         if (r != RS3_OK) return r;
         const dim3 grid((unsigned)((k_max + TC_ROWS - 1) / TC_ROWS * splits), (unsigned)H, (unsigned)a.s.U);
         launch_pdl(kern, grid, dim3(TC_THREADS), smem, st, p);
@@ -1006,7 +1558,7 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.qt = 8;
     while (a.qt > 1 && (int64_t)a.qt * a.s.nb * 4 > SELECT_KEYS_BYTES) a.qt >>= 1;
     const size_t smem = (size_t)a.qt * (size_t)a.s.nb * 4;
-    const rs3_status r = rs3_kernel_smem((const void *)k_block_select, smem);
+    const rs3_status r = rs3_kernel_smem((const void *)k_block_select, smem + 4 * 1024);   // (its own static arrays count too)
     if (r != RS3_OK) return r;
     const dim3 grid((unsigned)((k_max + a.qt - 1) / a.qt), (unsigned)H, (unsigned)a.s.U);
     launch_pdl(k_block_select, grid, dim3(SELECT_THREADS), smem, st, a);

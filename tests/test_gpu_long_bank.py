@@ -495,6 +495,102 @@ def test_select_over_many_blocks(rs3, rows, n_top, block):
     assert torch.equal(sel[0, 0], want)
 
 
+@pytest.mark.parametrize("dtype,H,d,U,k_max,n_top,rows,spread,rope", [
+    ("bf16", 4, 64, 40, 21, 16, 900, 127, True), ("bf16", 1, 16, 160, 130, 5, 3_000, 2, False), ("bf16", 2, 32, 80, 40, 32, 70_000, 127, False),
+    ("f32", 2, 64, 80, 33, 7, 2_000, 1, True), ("f32", 1, 32, 80, 250, 32, 9_000, 2, False), ("bf16", 1, 64, 160, 9, 20, 300_000, 0, False),
+    ("bf16", 1, 64, 160, 9, 1, 40, 9, False), ("bf16", 2, 64, 40, 250, 30, 40_000, 40, False)])
+def test_select_for_many_queries(rs3, dtype, H, d, U, k_max, n_top, rows, spread, rope):
+    """Enough queries to fill the SMs; digests given: `spread` 127 is random, small ones are full of ties, 0 is nothing but
+    them; units of every length from none to all rows; scores that grow with the blocks."""
+    mn = 256
+    bank = rs3.Bank(U, H, d, dtype, mn, 1, -1, rows, 4, 3)
+    st = status()
+    g = gen(rows)
+    # counters as if the rings had been filled and turned over
+    counters = bank.counters.cpu()
+    for u in range(U):
+        live = rows * (u % 7) // 6
+        head = (u * 37) % max(1, rows)
+        counters[u] = torch.tensor([head, head + live, [0, 5, mn][u % 3], int(live > 0), 0, int(u % 3 > 0), [3, 0, 1][u % 3]])
+    bank.counters.copy_(counters)
+    nb = bank.blocks(32)
+    shape = (U, H, nb, d)
+    dig = torch.randint(-max(1, spread), max(1, spread) + 1, shape, generator=g, device="cuda") * (spread > 0)
+    if U == 80:
+        dig[..., 0] = torch.arange(nb, device="cuda") * 127 // nb
+    dig = dig.to(torch.int8)
+    step = torch.randint(1, 3, shape[:3], generator=g, device="cuda").float() / 64
+    q = torch.randn((2, mn, H * d), generator=g, device="cuda").to(DT[dtype])
+    if U == 80:
+        q.view(2, mn, H, d)[..., 0] = 3.0
+    counts = [(k_max * (5 + u) // 7) % (k_max + 1) for u in range(U)]
+    idx = torch.stack([torch.randperm(mn, generator=g, device="cuda")[:k_max].sort().values for _ in range(U)]).to(torch.int32)
+    count = torch.tensor(counts, dtype=torch.int32, device="cuda")
+    group = (torch.arange(U, device="cuda") % 2).to(torch.int32)
+    table = rope_table(mn, d) if rope else None
+    sel = torch.full((U, H, k_max, n_top), -5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(U, H, k_max, nb), dtype=torch.uint8, device="cuda")
+    rs3.rs3_block_select(q, dtype, 2, mn, H, d, group, idx, count, k_max, bank, 32, dig, step, table, n_top, sel, ws, st)
+    assert int(st) == 0
+    x = q.float().cpu()
+    if rope:
+        p, t = x.view(2, mn, H, d // 2, 2), table.cpu()[:, None]
+        x = torch.stack([p[..., 0] * t[..., 0] - p[..., 1] * t[..., 1], p[..., 0] * t[..., 1] + p[..., 1] * t[..., 0]], -1).view(2, mn, H * d)
+    tq = torch.from_numpy(eight_bits(x.view(2, mn, H, d).numpy())[0]).cuda()
+    for u in range(U):
+        head, tail, cond, _, _, _, ptr = counters[u].tolist()
+        at = torch.arange(tail - head, device="cuda")
+        places = torch.cat([torch.arange(cond, device="cuda"), mn + (head + at) % rows, mn + rows + torch.arange(ptr, device="cuda")])
+        live = torch.zeros(nb, dtype=torch.bool, device="cuda")
+        live[places // 32] = True
+        n = counts[u]
+        assert (sel[u, :, n:] == -5).all()
+        if n == 0:
+            continue
+        score = torch.einsum("jhd,hbd->hjb", tq[u % 2, idx[u, :n].long()], dig[u].double()) * step[u].double()[:, None]
+        score.masked_fill_(~live, -math.inf)
+        m = min(n_top, int(live.sum()))
+        best = score.argsort(dim=-1, descending=True, stable=True)[..., :m].sort(-1).values
+        assert torch.equal(sel[u, :, :n, :m].long(), best), u
+        assert (sel[u, :, :n, m:] == -1).all()
+
+
+def test_select_wait_limit_runs_out_and_the_context_stays_usable(rs3):
+    U, H, d, mn, k_max = 160, 1, 64, 64, 5
+    bank = rs3.Bank(U, H, d, "bf16", mn, 1, -1, 640, 4, 0)
+    st = status()
+    k = torch.randn((U, mn, d), generator=gen(1), device="cuda").bfloat16()
+    rs3.rs3_bank_commit(bank, k, k, None, 1, st)
+    bank.counters[:, 1] = 640                              # as if the ring had been filled
+    nb = bank.blocks(32)
+    dig = torch.zeros((U, H, nb, d), dtype=torch.int8, device="cuda")
+    step = torch.zeros((U, H, nb), device="cuda")
+    idx = torch.arange(k_max, dtype=torch.int32, device="cuda").expand(U, k_max).contiguous()
+    count = torch.full((U,), k_max, dtype=torch.int32, device="cuda")
+    zero = torch.zeros(U, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(U, H, k_max, nb), dtype=torch.uint8, device="cuda")
+    codes, sels, digs = [], [], []
+    for limit in (10 ** 9, 0, 10 ** 9):
+        st = status()
+        sel = torch.zeros((U, H, k_max, 2), dtype=torch.int32, device="cuda")
+        rs3.rs3_set_wait_limit_ns(limit)
+        try:
+            rs3.rs3_bank_digest(bank, 32, -1, dig, step, st)
+            torch.cuda.synchronize()
+            codes.append(int(st))
+            st.zero_()
+            rs3.rs3_block_select(k[:1], "bf16", 1, mn, H, d, zero, idx, count, k_max, bank, 32, dig, step, None, 2, sel, ws, st)
+            torch.cuda.synchronize()
+        finally:
+            rs3.rs3_set_wait_limit_ns(10 ** 9)
+        codes.append(int(st))
+        sels.append(sel)
+        digs.append(dig.clone())
+    T = rs3.RS3_ETIMEOUT
+    assert codes == [0, 0, T, T, 0, 0]
+    assert torch.equal(sels[0], sels[2]) and torch.equal(digs[0], digs[2])
+
+
 # ---------------------------------------------------------------------------
 # the readout over chosen blocks
 # ---------------------------------------------------------------------------
