@@ -125,26 +125,24 @@ def _ptr(t: Optional[torch.Tensor]):
         return None
     if not t.is_contiguous():
         raise ValueError("tensors passed to librs3 must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+def _stream(stream):
+    if stream is None:                 # the current stream's handle, without a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _bytes(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
-def _want(name: str, t: Optional[torch.Tensor], dtype, numel: int, optional: bool = False):
-    """A tensor of at least `numel` elements of this type on the current device."""
+def _want(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int):
+    """A tensor of at least `numel` elements of this type on device `dev`, the current one."""
     if t is None:
-        if not optional:
-            raise ValueError(f"{name} is missing")
-        return
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is missing")
+    if t.get_device() != dev:
         raise ValueError(f"{name} is not on the current CUDA device")
     if t.dtype != dtype or t.numel() < numel:
         raise ValueError(f"{name}: at least {numel} elements of {dtype} wanted, got {tuple(t.shape)} of {t.dtype}")
@@ -281,12 +279,9 @@ class Bank:
                                ring_cap, max_frames, n_ptr, _ptr(self.k_store), _ptr(self.v_store),
                                _ptr(self.meta), _stream(stream))
         _check(rc, "rs3_bank_init")
-
-    @property
-    def counters(self) -> torch.Tensor:
-        """Per unit, on the device: {head, tail, cond_len, n_frames, oldest,
-        n_cond_frames, ptr_len}, int64 [U, 7], a view of the bank's own."""
-        return self.meta.view(self.U, -1)[:, :7]
+        # per unit, on the device: {head, tail, cond_len, n_frames, oldest, n_cond_frames, ptr_len},
+        # int64 [U, 7], a view of the bank's own
+        self.counters = self.meta.view(U, -1)[:, :7]
 
     def blocks(self, block: int) -> int:
         """Blocks of `block` storage rows of a unit (rs3_bank_blocks)."""
@@ -330,9 +325,12 @@ def rs3_bank_reset(bank: Bank, unit: int = -1, stream=None):
 
 def rs3_bank_drop_frames(bank: Bank, n_oldest, n_newest, status, stream=None):
     """Gives up the n_oldest[u] oldest and n_newest[u] newest ring frames of every unit."""
-    _want("n_oldest", n_oldest, torch.int32, bank.U, optional=True)
-    _want("n_newest", n_newest, torch.int32, bank.U, optional=True)
-    _want("status", status, torch.int32, 1)
+    dev = torch.cuda.current_device()
+    if n_oldest is not None:
+        _want(dev, "n_oldest", n_oldest, torch.int32, bank.U)
+    if n_newest is not None:
+        _want(dev, "n_newest", n_newest, torch.int32, bank.U)
+    _want(dev, "status", status, torch.int32, 1)
     rc = lib.rs3_bank_drop_frames(ctypes.byref(bank.desc), _ptr(n_oldest), _ptr(n_newest), _ptr(status),
                                   _stream(stream))
     _check(rc, "rs3_bank_drop_frames")
@@ -345,13 +343,14 @@ def rs3_bank_copy_workspace_bytes(U: int, keep_stride: int) -> int:
 def rs3_bank_copy(dst: Bank, src: Bank, parent, keep, workspace, status, stream=None):
     """Unit u of dst becomes the kept rows of unit parent[u] of src (-1: left as it
     is); keep: uint8 [dst.U, at least the parents' length] over logical rows, or None."""
-    _want("parent", parent, torch.int32, dst.U)
-    _want("status", status, torch.int32, 1)
+    dev = torch.cuda.current_device()
+    _want(dev, "parent", parent, torch.int32, dst.U)
+    _want(dev, "status", status, torch.int32, 1)
     stride = 0
     if keep is not None:
         if keep.dim() != 2 or keep.shape[0] != dst.U:
             raise ValueError("keep: one row per destination unit")
-        _want("keep", keep, torch.uint8, dst.U)
+        _want(dev, "keep", keep, torch.uint8, dst.U)
         stride = keep.shape[1]
     rc = lib.rs3_bank_copy(ctypes.byref(dst.desc), ctypes.byref(src.desc), _ptr(parent), _ptr(keep), stride,
                            _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
@@ -373,25 +372,32 @@ def rs3_bank_read_meta(bank: Bank, stream=None):
 # read side over chosen blocks of a long bank
 # ---------------------------------------------------------------------------
 
+def _block_heads(bank: Bank, block: int) -> int:
+    return bank.U * bank.H * (-(-bank.rows_per_unit // block) if block > 0 else 0)
+
+
 def rs3_bank_digest(bank: Bank, block: int, refresh: int, digest, step, status, stream=None):
     """Digests (int8 [U, H, blocks, d] and their steps fp32 [U, H, blocks]) of the
     blocks of the `refresh` newest ring frames, or of all blocks (-1)."""
-    n = bank.U * bank.H * max(0, bank.blocks(block) if block > 0 else 0)
-    _want("digest", digest, torch.int8, n * bank.d)
-    _want("step", step, torch.float32, n)
-    _want("status", status, torch.int32, 1)
+    dev, n = torch.cuda.current_device(), _block_heads(bank, block)
+    _want(dev, "digest", digest, torch.int8, n * bank.d)
+    _want(dev, "step", step, torch.float32, n)
+    _want(dev, "status", status, torch.int32, 1)
     rc = lib.rs3_bank_digest(ctypes.byref(bank.desc), block, refresh, _ptr(digest), _ptr(step), _ptr(status),
                              _stream(stream))
     _check(rc, "rs3_bank_digest")
 
 
 def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status):
-    _want("q", q, TORCH_DTYPES[dtype], G * mn * H * d)
-    _want("unit_group", unit_group, torch.int32, bank.U)
-    _want("idx", idx, torch.int32, bank.U * k_max)
-    _want("count", count, torch.int32, bank.U)
-    _want("rope", rope, torch.float32, mn * d, optional=True)
-    _want("status", status, torch.int32, 1)
+    dev = torch.cuda.current_device()
+    _want(dev, "q", q, TORCH_DTYPES[dtype], G * mn * H * d)
+    _want(dev, "unit_group", unit_group, torch.int32, bank.U)
+    _want(dev, "idx", idx, torch.int32, bank.U * k_max)
+    _want(dev, "count", count, torch.int32, bank.U)
+    if rope is not None:
+        _want(dev, "rope", rope, torch.float32, mn * d)
+    _want(dev, "status", status, torch.int32, 1)
+    return dev
 
 
 def rs3_block_select_workspace_bytes(U: int, H: int, k_max: int, n_blocks: int) -> int:
@@ -403,11 +409,11 @@ def rs3_block_select(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group,
                      stream=None):
     """The n_top blocks whose digests score highest for each kept query and head:
     sel int32 [U, H, k_max, n_top], ascending, -1 where there are fewer."""
-    _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
-    n = bank.U * bank.H * max(0, bank.blocks(block) if block > 0 else 0)
-    _want("digest", digest, torch.int8, n * bank.d)
-    _want("step", step, torch.float32, n)
-    _want("sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    n = _block_heads(bank, block)
+    _want(dev, "digest", digest, torch.int8, n * bank.d)
+    _want(dev, "step", step, torch.float32, n)
+    _want(dev, "sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
     rc = lib.rs3_block_select(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
                               ctypes.byref(bank.desc), block, _ptr(digest), _ptr(step), _ptr(rope), n_top, _ptr(sel),
                               _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
@@ -423,10 +429,11 @@ def rs3_sparse_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
                        bank: "Bank", block: int, sel, n_top: int, rope, residual, out, scale: float,
                        workspace, status, stream=None):
     """rs3_memory_readout over the blocks that sel lists for each query and head."""
-    _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
-    _want("sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
-    _want("residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d, optional=True)
-    _want("out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    _want(dev, "sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    if residual is not None:
+        _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
     rc = lib.rs3_sparse_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count),
                                 k_max, ctypes.byref(bank.desc), block, _ptr(sel), n_top, _ptr(rope), _ptr(residual),
                                 _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status),
@@ -440,6 +447,8 @@ def rs3_sparse_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
 
 def _rows_of(name: str, t: torch.Tensor, width: int):
     """(rows, elements between rows) of a tensor [..., width] whose rows are evenly spaced."""
+    if t.dim() >= 1 and t.shape[-1] == width and t.is_contiguous():
+        return t.numel() // width, width
     if t.dim() < 1 or t.shape[-1] != width or (width > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name}: rows of {width} adjacent elements wanted, got {tuple(t.shape)}")
     rows, step, reach = 1, None, None
@@ -459,21 +468,23 @@ def rs3_qk_norm_rope(q, q_out, k, k_out, dtype: str, mn: int, Hq: int, Hk: int, 
     """RMS norm of every head of q [..., Hq*d] and k [..., Hk*d] (either may be None),
     rotated by the row's own cell, row r being cell r mod mn.  Rows may be evenly
     spaced parts of a wider tensor; out may be the input."""
-    sides = []
+    dev, dt, sides = torch.cuda.current_device(), TORCH_DTYPES[dtype], []
     for name, x, y, H, w, keep in (("q", q, q_out, Hq, q_weight, q_keep), ("k", k, k_out, Hk, k_weight, k_keep)):
         if x is None and y is None:
             sides += [None, 0, 0, 0, None, None, None, 0]
             continue
-        for what, t in ((name, x), (name + "_out", y)):
-            _want(what, t, TORCH_DTYPES[dtype], 0)
+        _want(dev, name, x, dt, 0)
+        _want(dev, name + "_out", y, dt, 0)
         (rows, stride), (rows_out, out_stride) = _rows_of(name, x, H * d), _rows_of(name + "_out", y, H * d)
         if rows != rows_out:
             raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
-        _want(name + "_weight", w, torch.float32, d, optional=True)
-        _want(name + "_keep", keep, torch.uint8, rows, optional=True)
-        sides += [ctypes.c_void_p(x.data_ptr()), rows, stride, H, _ptr(w), _ptr(keep), ctypes.c_void_p(y.data_ptr()),
-                  out_stride]
-    _want("rope", rope, torch.float32, mn * d, optional=True)
+        if w is not None:
+            _want(dev, name + "_weight", w, torch.float32, d)
+        if keep is not None:
+            _want(dev, name + "_keep", keep, torch.uint8, rows)
+        sides += [x.data_ptr(), rows, stride, H, _ptr(w), _ptr(keep), y.data_ptr(), out_stride]
+    if rope is not None:
+        _want(dev, "rope", rope, torch.float32, mn * d)
     rc = lib.rs3_qk_norm_rope(*sides, DTYPES[dtype], mn, d, float(eps), _ptr(rope), _stream(stream))
     _check(rc, "rs3_qk_norm_rope")
 

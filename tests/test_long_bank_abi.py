@@ -152,8 +152,13 @@ def test_workspace_sizes_never_fall(b):
 
 def test_binding_refuses_tensors_that_are_not_what_the_call_reads(b):
     x = torch.zeros(64, 256, dtype=torch.bfloat16)
-    with pytest.raises(ValueError, match="current CUDA device"):
-        b.rs3_qk_norm_rope(x, x, None, None, "bf16", 64, 4, 4, 64)
+    for dev, t, dtype, n in ((0, x, torch.bfloat16, 1), (0, None, torch.bfloat16, 1), (-1, x, torch.float32, 1),
+                             (-1, x, torch.bfloat16, 64 * 256 + 1)):
+        with pytest.raises(ValueError):
+            b._want(dev, "x", t, dtype, n)
+    b._want(-1, "x", x, torch.bfloat16, 64 * 256)          # (a CPU tensor's device is -1)
+    with pytest.raises(ValueError):
+        b._ptr(x.T)
     assert b._rows_of("q", torch.zeros(3, 5, 7, 16)[..., :8], 8) == (105, 16)
     assert b._rows_of("q", torch.zeros(1, 5, 24)[..., 8:16], 8) == (5, 24)
     assert b._rows_of("q", torch.zeros(8), 8) == (1, 8)
