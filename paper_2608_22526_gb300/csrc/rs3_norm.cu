@@ -6,7 +6,10 @@
 //
 // in fp32, rounded once to the stored type.  A head is read once into the registers of a
 // group of lanes (16 bytes each), so the sum of squares, the scaling and the rotation cost no
-// second read: the call is bound by the bytes of x and y.
+// second read: the call is bound by the bytes of x and y, and next by issuing instructions.  Queries of
+// 16 streams and two fifths of the rows of 48 objects' keys, 96 x 96 cells of 4 heads of 64 in bf16
+// (335 MB): 65 us, 5.2 TB/s.  Lanes of a head fixed at compile time, so that the reductions of the rows in flight
+// run side by side, and products in pairs took that from 86 us; two rows in flight 66, four (they spill) 68.
 #include "rs3_internal.cuh"
 
 namespace {
@@ -25,7 +28,8 @@ struct NormSide {
 };
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_FLIGHT = 4;             // rows in flight per lane group
+constexpr int NORM_FLIGHT = 3;             // rows in flight per lane group
+constexpr int NORM_TURNS = 16;             // rows of a cell that a CTA takes
 
 template <typename T>
 struct Piece;                              // 16 bytes of a row
@@ -63,20 +67,39 @@ struct Piece<float> {
     }
 };
 
-// A group of L lanes (a power of two) holds one head, ITEMS pieces each; it takes the rows of
-// one (cell, head) through the grids that share the cell, so the cell's angles are loaded once.
-template <typename T, int ITEMS>
-__global__ void __launch_bounds__(NORM_THREADS, ITEMS == 1 ? 4 : 2)
-k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float *__restrict__ rope)
+// Two fp32 values in a register pair; a product of pairs is one instruction.
+__device__ __forceinline__ uint64_t pair2(float x, float y)
 {
-    constexpr int N = Piece<T>::N;
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ uint64_t square2(uint64_t x, uint64_t sum)
+{
+    asm("fma.rn.f32x2 %0, %1, %1, %0;" : "+l"(sum) : "l"(x));
+    return sum;
+}
+__device__ __forceinline__ float2 scale2(uint64_t x, uint64_t r)
+{
+    float2 v;
+    asm("{\n\t.reg .b64 t;\n\tmul.rn.f32x2 t, %2, %3;\n\tmov.b64 {%0, %1}, t;\n\t}" : "=f"(v.x), "=f"(v.y) : "l"(x), "l"(r));
+    return v;
+}
+
+// A group of L lanes holds one head, ITEMS pieces each; it takes the rows of
+// one (cell, head) through the grids that share the cell, so the cell's angles are loaded once.
+template <typename T, int ITEMS, int L>
+__global__ void __launch_bounds__(NORM_THREADS, ITEMS == 1 ? 4 : 2)
+k_norm_rope(NormSide q, NormSide k, int mn, int d, float eps, const float *__restrict__ rope)
+{
+    constexpr int N = Piece<T>::N, GROUPS = NORM_THREADS / L;
     pdl_wait();
     const bool is_q = (int)blockIdx.x < q.ctas;
     const NormSide &s = is_q ? q : k;
     const int b = is_q ? (int)blockIdx.x : (int)blockIdx.x - q.ctas;
     const int cb = b % s.cell_blocks, tb = b / s.cell_blocks;
-    const int groups = NORM_THREADS / L, lane = threadIdx.x & (L - 1);
-    const int64_t g = (int64_t)cb * groups + threadIdx.x / L;      // (cell, head)
+    const int lane = threadIdx.x & (L - 1);
+    const int64_t g = (int64_t)cb * GROUPS + threadIdx.x / L;      // (cell, head)
     const int pieces = d / N;
     const bool here = g < (int64_t)mn * s.H;
     const int cell = here ? (int)(g / s.H) : 0, head = here ? (int)(g % s.H) : 0;
@@ -103,61 +126,79 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, int L, float eps, const float
     const uint8_t *src = s.x + row0 * s.x_stride + (head * pieces + lane) * 16;
     uint8_t *dst = s.y + row0 * s.y_stride + (head * pieces + lane) * 16;
     const int64_t x_turn = s.x_stride * mn, y_turn = s.y_stride * mn;
-    // the rows that are kept, a bit for each of the next 32 turns
-    for (int t = t0; t < t1; t += 32) {
-        uint32_t kept = 0;
-#pragma unroll 8
-        for (int f = 0; f < 32; ++f) {
-            if (t + f >= t1) break;
-            const int64_t row = (int64_t)(t + f) * mn + cell;
-            kept |= (uint32_t)(here && row < s.rows && (!s.keep || s.keep[row] != 0)) << f;
-        }
-        // a warp goes from one turn to the next that any of its lanes keeps
-        uint32_t todo = __reduce_or_sync(0xffffffffu, kept);
+    // the rows that are kept, a bit for each of this CTA's turns (32 at most): a group's lanes look them up
+    uint32_t kept = 0;
+#pragma unroll
+    for (int f = lane; f < NORM_TURNS; f += L) {
+        const int64_t row = row0 + (int64_t)f * mn;
+        kept |= (uint32_t)(here && t0 + f < t1 && row < s.rows && (!s.keep || s.keep[row] != 0)) << f;
+    }
+#pragma unroll
+    for (int o = L >> 1; o > 0; o >>= 1) kept |= __shfl_xor_sync(0xffffffffu, kept, o);
+    // a warp goes from one turn to the next that any of its lanes keeps
+    uint32_t todo = __reduce_or_sync(0xffffffffu, kept);
+    while (todo != 0u) {
         uint4 v[NORM_FLIGHT][ITEMS];
         int turn[NORM_FLIGHT];
-        const auto load = [&]() {
+        float sum[NORM_FLIGHT];
 #pragma unroll
-            for (int f = 0; f < NORM_FLIGHT; ++f) {
-                turn[f] = todo != 0u ? __ffs(todo) - 1 : -1;
-                todo &= todo - 1u;
-                const bool take = turn[f] >= 0 && (kept >> turn[f] & 1u);
-                const uint4 *x = reinterpret_cast<const uint4 *>(src + (int64_t)(t - t0 + turn[f]) * x_turn);
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            turn[f] = todo != 0u ? __ffs(todo) - 1 : -1;
+            todo &= todo - 1u;
+            const bool take = turn[f] >= 0 && (kept >> turn[f] & 1u);
+            const uint4 *x = reinterpret_cast<const uint4 *>(src + turn[f] * x_turn);
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) v[f][i] = take && lane + i * L < pieces ? __ldcs(x + i * L) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        const auto finish = [&]() {
-#pragma unroll
-            for (int f = 0; f < NORM_FLIGHT; ++f) {
-                if (turn[f] < 0) break;
-                float x[ITEMS][N], sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    Piece<T>::widen(v[f][i], x[i]);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-                }
-                for (int o = L >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const float r = rsqrtf(fmaf(sum, inv_d, eps));
-                uint4 *y = reinterpret_cast<uint4 *>(dst + (int64_t)(t - t0 + turn[f]) * y_turn);
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    float z[N];
-#pragma unroll
-                    for (int e = 0; e < N; e += 2) {
-                        z[e] = fmaf(x[i][e], co[i][e], -(x[i][e + 1] * si[i][e + 1])) * r;
-                        z[e + 1] = fmaf(x[i][e], si[i][e], x[i][e + 1] * co[i][e + 1]) * r;
-                    }
-                    if ((kept >> turn[f] & 1u) && lane + i * L < pieces) y[i * L] = Piece<T>::narrow(z);
-                }
-            }
-        };
-        load();
-        while (turn[0] >= 0) {
-            finish();
-            load();
+            for (int i = 0; i < ITEMS; ++i) v[f][i] = take && lane + i * L < pieces ? __ldcs(x + i * L) : make_uint4(0, 0, 0, 0);
         }
+#pragma unroll
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            uint64_t two = 0;                          // (0.f, 0.f)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                float x[N];
+                Piece<T>::widen(v[f][i], x);
+#pragma unroll
+                for (int e = 0; e < N; e += 2) two = square2(pair2(x[e], x[e + 1]), two);
+            }
+            sum[f] = __uint_as_float((uint32_t)two) + __uint_as_float((uint32_t)(two >> 32));
+        }
+#pragma unroll
+        for (int o = L >> 1; o > 0; o >>= 1)
+#pragma unroll
+            for (int f = 0; f < NORM_FLIGHT; ++f) sum[f] += __shfl_xor_sync(0xffffffffu, sum[f], o);
+#pragma unroll
+        for (int f = 0; f < NORM_FLIGHT; ++f) {
+            if (turn[f] < 0) break;
+            const float r = rsqrtf(fmaf(sum[f], inv_d, eps));
+            uint4 *y = reinterpret_cast<uint4 *>(dst + turn[f] * y_turn);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                float x[N], z[N];
+                Piece<T>::widen(v[f][i], x);
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const float2 n = scale2(pair2(x[e], x[e + 1]), pair2(r, r));
+                    z[e] = fmaf(n.x, co[i][e], -(n.y * si[i][e + 1]));
+                    z[e + 1] = fmaf(n.x, si[i][e], n.y * co[i][e + 1]);
+                }
+                if ((kept >> turn[f] & 1u) && lane + i * L < pieces) y[i * L] = Piece<T>::narrow(z);
+            }
+        }
+    }
+}
+
+using NormKernel = void (*)(NormSide, NormSide, int, int, float, const float *);
+
+template <typename T>
+NormKernel norm_kernel(int L)
+{
+    switch (L) {
+    case 1: return k_norm_rope<T, 1, 1>;
+    case 2: return k_norm_rope<T, 1, 2>;
+    case 4: return k_norm_rope<T, 1, 4>;
+    case 8: return k_norm_rope<T, 1, 8>;
+    case 16: return k_norm_rope<T, 1, 16>;
+    default: return k_norm_rope<T, 1, 32>;
     }
 }
 
@@ -210,8 +251,8 @@ extern "C" rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_
         if (t.rows == 0) continue;
         const int64_t turns = (t.rows + mn - 1) / mn, cells = t.rows < mn ? t.rows : mn;
         const int64_t cb = (cells * t.H + groups - 1) / groups;
-        // a CTA takes 16 rows of its cells, fewer where that leaves SMs idle
-        int64_t per = 16;
+        // fewer rows to a CTA where SMs would be idle
+        int64_t per = NORM_TURNS;
         while (per > 1 && cb * ((turns + per - 1) / per) < 4ll * rs3_sm_count()) per >>= 1;
         const int64_t ctas = cb * ((turns + per - 1) / per);
         if (turns > INT32_MAX || ctas > INT32_MAX) return RS3_EUNSUPPORTED;
@@ -223,9 +264,9 @@ extern "C" rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_
     }
     if (total == 0) return RS3_OK;
     if (total > INT32_MAX) return RS3_EUNSUPPORTED;
-    void (*kern)(NormSide, NormSide, int, int, int, float, const float *) =
-        dtype == RS3_BF16 ? k_norm_rope<uint16_t, 1> : items == 1 ? k_norm_rope<float, 1> : k_norm_rope<float, 2>;
-    launch_pdl(kern, dim3((unsigned)total), dim3(NORM_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), s[0], s[1], mn, d, L,
+    NormKernel kern = k_norm_rope<float, 2, 32>;
+    if (items == 1) kern = dtype == RS3_BF16 ? norm_kernel<uint16_t>(L) : norm_kernel<float>(L);
+    launch_pdl(kern, dim3((unsigned)total), dim3(NORM_THREADS), 0, reinterpret_cast<cudaStream_t>(stream), s[0], s[1], mn, d,
                eps, rope);
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }
