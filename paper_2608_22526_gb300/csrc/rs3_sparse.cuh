@@ -28,11 +28,12 @@ __device__ __forceinline__ bool sparse_unit(const SparseArgs &a, int u, bool lat
 {
     cnt = a.count[u];
     g = a.unit_group[u];
+    const bool sound = rows.load(a.bank, u);               // (before the checks: all loads go out together)
     if (cnt < 0 || cnt > a.k_max || g < 0 || g >= a.G) {
         if (latch) latch_status(a.status, RS3_EINVAL);
         return false;
     }
-    if (!rows.load(a.bank, u)) {
+    if (!sound) {
         if (latch) latch_status(a.status, RS3_EINTERNAL);
         return false;
     }

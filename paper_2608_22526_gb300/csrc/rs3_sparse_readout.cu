@@ -9,6 +9,7 @@
 //              partial results of a query's blocks are joined by their log-sum-exp (k_join_blocks)
 #include "rs3_sparse.cuh"
 
+#include "rs3_cluster.cuh"
 #include "rs3_tc_host.cuh"
 #include "rs3_tc_ptx.cuh"
 
@@ -227,177 +228,199 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 // by block
 // ---------------------------------------------------------------------------
 constexpr int TILE = 64;                   // queries of an item
-constexpr int LIST_THREADS = 1024;
-constexpr int LIST_HELD = 6;               // fours of list entries that a thread holds
-constexpr int LIST_BINS = 8192;            // blocks that a CTA counts
-constexpr int MAX_SEGMENTS = 1024;         // (unit, head, segment) triples that a CTA of the attention holds at a time
+constexpr int LIST_THREADS = 512;
+constexpr int LIST_HELD = 8;               // list entries that a thread holds
+constexpr int LIST_BINS = 8192;            // blocks that are counted at a time
+constexpr int LIST_CTAS = 8;               // largest cluster of a (unit, head)
+constexpr int MAX_HEADS = 1024;            // (unit, head) pairs whose item counts a CTA of the attention holds at a time
 constexpr int CHUNK_ITEMS = 64;            // items whose records it holds
 
 // Part of a block (its 32 or 64 rows, half of its 128) and up to TILE of the queries that chose it.
 struct BlockItem {
     int32_t uh, part, first, n;            // unit * H + head, storage rows / rows of a part, first list entry, entries
     uint32_t live[2];                      // its live rows
-    int32_t pad[2];
+    int64_t q;                             // element of its unit's and head's first query row (k_attend_blocks)
 };
 
 struct BlockWork {                         // in the workspace
-    int32_t *n_items, *first_item;         // [U * H][segments]
+    int32_t *n_items;                      // [U * H]
     BlockItem *items;                      // [U * H][max_items]
-    int2 *list;                            // [U * H][k_max * n_top]: (query * n_top + entry, cell)
+    int2 *list;                            // [U * H][k_max * n_top]: (query * n_top + entry, row of the query)
+    uint4 *q;                              // [U][k_max][H * d]: the kept queries, rotated (calls with angles)
     float2 *ml;                            // [U * H][k_max][n_top][parts]: (max in the log2 domain, sum)
     float *o;                              // [U * H][k_max][n_top][parts][d]
-    int32_t segments, bins, parts, list_ctas;
+    int32_t cluster, bins, parts, list_ctas, pass_ctas;
     int64_t max_items;
     uint64_t wait_ns;                      // limit of each wait
+    uint32_t per_top, per_top_shift;       // x / n_top = x * per_top >> per_top_shift for x < 2^28
 };
 
-// The queries of every block: CTA (segment, unit * H + head) counts the lists' entries for its
-// blocks, gives every block a run of list entries and its items, and fills them in.  Entries of one block
-// come in any order; each is computed by itself, so the result does not depend on it.  Out of place the
-// launch's other CTAs write out = residual (or zeros) on every cell.
-__global__ void __launch_bounds__(LIST_THREADS) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
+// The queries of every block, a counting sort: the CTAs of a cluster share the list entries of one (unit, head).
+// Each counts its entries per block in shared memory; then each owns some of the blocks, adds up their counts
+// through distributed shared memory, gives every block a run of the sorted list and its items, and
+// tells every CTA where its entries of the block go.  Entries of one block come in any order; each
+// is computed by itself, so the result does not depend on it.  Out of place the launch's other CTAs
+// write out = residual (or zeros) on every cell, and with angles a further few rotate the kept queries once for all
+// of their blocks (in fp32, rounded to bf16 for the tensor cores).
+__global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
     if ((int)blockIdx.x >= w.list_ctas) {
         const uint4 *res = static_cast<const uint4 *>(a.residual);
         uint4 *out = static_cast<uint4 *>(a.out);
-        for (int64_t i = (int64_t)((int)blockIdx.x - w.list_ctas) * LIST_THREADS + threadIdx.x; i < nvec;
-             i += (int64_t)((int)gridDim.x - w.list_ctas) * LIST_THREADS)
-            out[i] = res ? __ldcs(res + i) : make_uint4(0, 0, 0, 0);
+        const int64_t first = (int64_t)((int)blockIdx.x - w.list_ctas) * LIST_THREADS + threadIdx.x;
+        const int64_t pass = (int64_t)w.pass_ctas * LIST_THREADS;
+        if (first < pass) {
+            for (int64_t i = first; i < nvec; i += 4 * pass) {
+                uint4 v[4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) v[f] = res && i + f * pass < nvec ? __ldcs(res + i + f * pass) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                    if (i + f * pass < nvec) out[i + f * pass] = v[f];
+            }
+            return;
+        }
+        const SparseArgs &s = a.s;
+        if (!s.rope) return;                           // (the grid is whole clusters)
+        const int width = s.H * s.d / 8;               // 16-byte pieces of a query row
+        const int64_t i = first - pass;
+        const int u = (int)(i / ((int64_t)s.k_max * width)), r = (int)(i - (int64_t)u * s.k_max * width), j = r / width, c = r - j * width;
+        if (u >= s.U) return;
+        const int cnt = s.count[u], g = s.unit_group[u];
+        if (cnt > s.k_max || j >= cnt || g < 0 || g >= s.G) return;
+        const int cell = s.idx[(int64_t)u * s.k_max + j];
+        if (cell < 0 || cell >= s.mn) return;
+        w.q[i] = rotate_q_piece(__ldg(static_cast<const uint4 *>(s.q) + ((int64_t)g * s.mn + cell) * width + c),
+                                s.rope + (int64_t)cell * s.d + (c * 8 & (s.d - 1)));
         return;
     }
-    extern __shared__ int32_t s_bin[];                 // [bins] counts, then first entries
-    __shared__ int32_t s_part[LIST_THREADS / 32], s_items[LIST_THREADS / 32];
+    extern __shared__ int32_t s_bin[];                 // [bins] counts, then next places
+    __shared__ int32_t s_part[2][LIST_THREADS / 32], s_total[LIST_CTAS][2];
     const SparseArgs &s = a.s;
-    const int uh = blockIdx.x / w.segments, seg = blockIdx.x - uh * w.segments, u = uh / s.H;
+    const int C = w.cluster, rank = (int)cluster_rank(), uh = (int)blockIdx.x / C, u = uh / s.H;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int lo = seg * w.bins, hi = min(s.nb, lo + w.bins), n_bins = hi - lo;
-    // the first lists' entries are on their way while the unit's counters are read; both passes use them
     const int64_t base = (int64_t)uh * s.k_max * s.n_top;
     const int32_t *sel = a.sel + base, *idx = s.idx + (int64_t)u * s.k_max;
-    const int most = s.k_max * s.n_top;
-    const int first_four = (int)((16 - (reinterpret_cast<uintptr_t>(sel) & 15)) >> 2 & 3);     // where 16-byte loads begin
-    const auto fours = [&](int e) {                    // entries e .. e + 3; -1 past the end
-        int4 x = make_int4(-1, -1, -1, -1);
-        if (e + 4 <= most) x = __ldg(reinterpret_cast<const int4 *>(sel + e));
-        else {
-            if (e < most) x.x = __ldg(sel + e);
-            if (e + 1 < most) x.y = __ldg(sel + e + 1);
-            if (e + 2 < most) x.z = __ldg(sel + e + 2);
-        }
-        return x;
-    };
-    int4 held[LIST_HELD];
+    const int first = rank * LIST_THREADS + (int)threadIdx.x, step = C * LIST_THREADS, most = s.k_max * s.n_top;
+    const auto query_of = [&](int e) { return (int)((uint64_t)(uint32_t)e * w.per_top >> w.per_top_shift); };     // e / n_top
+    // the first entries and their queries' cells are on their way while the unit's counters are read
+    int held[LIST_HELD], row[LIST_HELD];               // blocks; rows of their queries, -1 for none
 #pragma unroll
-    for (int i = 0; i < LIST_HELD; ++i) held[i] = fours(first_four + 4 * (threadIdx.x + i * LIST_THREADS));
-    const int head = (int)threadIdx.x < first_four && (int)threadIdx.x < most ? __ldg(sel + threadIdx.x) : -1;
-    bool bad = false;                                  // some query's cell is not on the grid: it is in no list
+    for (int i = 0; i < LIST_HELD; ++i) {
+        const int e = first + i * step;
+        held[i] = e < most ? __ldg(sel + e) : -1;
+        row[i] = e < most ? __ldg(idx + query_of(e)) : 0;
+    }
     int cnt, g;
     LiveRows rows;
-    const bool work = sparse_unit(s, u, threadIdx.x == 0 && seg == 0 && uh == u * s.H, cnt, g, rows) && n_bins > 0;
-    if (!work) {
-        if (threadIdx.x == 0) w.n_items[blockIdx.x] = 0;
+    // (the same for the whole cluster)
+    if (!sparse_unit(s, u, threadIdx.x == 0 && rank == 0 && uh == u * s.H, cnt, g, rows)) {
+        if (threadIdx.x == 0 && rank == 0) w.n_items[uh] = 0;
         return;
     }
-    for (int i = threadIdx.x; i < n_bins; i += LIST_THREADS) s_bin[i] = 0;
-    for (int j = threadIdx.x; j < cnt; j += LIST_THREADS) bad |= (uint32_t)idx[j] >= (uint32_t)s.mn;
-    if (bad && seg == 0) latch_status(s.status, RS3_EINVAL);
-    const bool check = __syncthreads_or(bad);
     const int pairs = cnt * s.n_top;
-    const auto listed = [&](int i) { return i < pairs && (!check || (uint32_t)idx[i / s.n_top] < (uint32_t)s.mn); };
-    // f(entry, block) for every entry of the lists that is a block's
-    bool over = false;                                 // some is past the last block
-    const auto each = [&](auto f) {
-        const auto one = [&](int e, int b) {
-            over |= b >= s.nb && e < pairs;
-            if (b >= 0 && b < hi && listed(e)) f(e, b);
-        };
-        one(threadIdx.x, head);
-        int e = first_four + 4 * threadIdx.x;
-#pragma unroll
-        for (int i = 0; i < LIST_HELD; ++i, e += 4 * LIST_THREADS) {
-            one(e, held[i].x);
-            one(e + 1, held[i].y);
-            one(e + 2, held[i].z);
-            one(e + 3, held[i].w);
-        }
-        for (; e < pairs; e += 4 * LIST_THREADS) {
-            const int4 x = fours(e);
-            one(e, x.x);
-            one(e + 1, x.y);
-            one(e + 2, x.z);
-            one(e + 3, x.w);
-        }
+    bool bad = false;                                  // a query off the grid (it is in no list), a block past the last
+    const auto row_of = [&](int e, int b, int cell) {
+        if (e >= pairs) return -1;
+        const bool off = (uint32_t)cell >= (uint32_t)s.mn;
+        bad |= off || b >= s.nb;
+        return off || b >= s.nb ? -1 : s.rope ? query_of(e) : cell;
     };
-    int before = 0;
-    each([&](int, int b) {
-        if (b >= lo) atomicAdd(&s_bin[b - lo], 1);
-        before += b < lo;
-    });
-    if (over && seg == 0) latch_status(s.status, RS3_EINVAL);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (lane == 0) s_part[warp] = before;
-    __syncthreads();
-    before = 0;
 #pragma unroll
-    for (int i = 0; i < LIST_THREADS / 32; ++i) before += s_part[i];
-    __syncthreads();
-    // entries and items before each bin: a run of bins per thread
-    const int per = (n_bins + LIST_THREADS - 1) / LIST_THREADS;
-    const int b0 = min(n_bins, (int)threadIdx.x * per), b1 = min(n_bins, b0 + per);
-    int entries = 0, items = 0;
-    for (int b = b0; b < b1; ++b) {
-        entries += s_bin[b];
-        items += (s_bin[b] + TILE - 1) / TILE;
-    }
-    int e_sum = entries, i_sum = items;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, e_sum, o), y = __shfl_up_sync(0xffffffffu, i_sum, o);
-        if (lane >= o) { e_sum += x; i_sum += y; }
-    }
-    if (lane == 31) { s_part[warp] = e_sum; s_items[warp] = i_sum; }
-    __syncthreads();
-    int n_items = 0;
-#pragma unroll
-    for (int i = 0; i < LIST_THREADS / 32; ++i) {
-        e_sum += i < warp ? s_part[i] : 0;
-        i_sum += i < warp ? s_items[i] : 0;
-        n_items += s_items[i];
-    }
-    // the segments before this one have at most an item per block or entry, and one more per TILE entries
-    const int item0 = min(lo, before) + before / TILE;
-    if (threadIdx.x == 0) {
-        w.n_items[blockIdx.x] = n_items * w.parts;
-        w.first_item[blockIdx.x] = item0 * w.parts;
-    }
-    int first = before + e_sum - entries;
-    BlockItem *out = w.items + uh * w.max_items + (int64_t)(item0 + i_sum - items) * w.parts;
+    for (int i = 0; i < LIST_HELD; ++i) row[i] = row_of(first + i * step, held[i], row[i]);
     const int pr = s.bs / w.parts;                     // rows of a part
-    for (int b = b0; b < b1; ++b) {
-        const int n = s_bin[b];
-        s_bin[b] = first;
-        for (int p = 0; n > 0 && p < w.parts; ++p) {
-            BlockItem it = {};
-            it.uh = uh;
-            it.part = (lo + b) * w.parts + p;
-            const int64_t r0 = (int64_t)it.part * pr;
-            const uint64_t live = rows.mask64(r0);
-            it.live[0] = (uint32_t)live;
-            it.live[1] = pr > 32 ? (uint32_t)(live >> 32) : 0u;
-            for (int e = 0; e < n; e += TILE) {
-                it.first = first + e;
-                it.n = min(TILE, n - e);
-                *out++ = it;
+    int entry0 = 0, item0 = 0;                         // of this window of blocks
+    for (int lo = 0; lo < s.nb; lo += w.bins) {
+        const int n_bins = min(w.bins, s.nb - lo);
+        for (int i = threadIdx.x; i < n_bins; i += LIST_THREADS) s_bin[i] = 0;
+        __syncthreads();
+        const auto each = [&](auto f) {                // f(entry, block of the window, row of its query)
+#pragma unroll
+            for (int i = 0; i < LIST_HELD; ++i)
+                if (row[i] >= 0 && (uint32_t)(held[i] - lo) < (uint32_t)n_bins) f(first + i * step, held[i] - lo, row[i]);
+            for (int e = first + LIST_HELD * step; e < pairs; e += step) {
+                const int b = __ldg(sel + e), r = row_of(e, b, __ldg(idx + query_of(e)));
+                if (r >= 0 && (uint32_t)(b - lo) < (uint32_t)n_bins) f(e, b - lo, r);
+            }
+        };
+        each([&](int, int b, int) { atomicAdd(&s_bin[b], 1); });
+        cluster_barrier();
+        // a run of blocks for each thread
+        const int own = (n_bins + C - 1) / C, per = (own + LIST_THREADS - 1) / LIST_THREADS;
+        const int end = min(n_bins, (rank + 1) * own);
+        const int b0 = min(end, rank * own + (int)threadIdx.x * per), b1 = min(end, b0 + per);
+        int entries = 0, items = 0, c[LIST_CTAS];      // the CTAs' entries of one block
+        const auto counts = [&](int b) {
+            int n = 0;
+#pragma unroll
+            for (int r = 0; r < LIST_CTAS; ++r) c[r] = r < C ? (int)dsmem_ld_u32(dsmem_addr(s_bin + b, r)) : 0;
+#pragma unroll
+            for (int r = 0; r < LIST_CTAS; ++r) n += c[r];
+            return n;
+        };
+        for (int b = b0; b < b1; ++b) {
+            const int n = counts(b);
+            entries += n;
+            items += (n + TILE - 1) / TILE;
+        }
+        int e_sum = entries, i_sum = items;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, e_sum, o), y = __shfl_up_sync(0xffffffffu, i_sum, o);
+            if (lane >= o) { e_sum += x; i_sum += y; }
+        }
+        if (lane == 31) { s_part[0][warp] = e_sum; s_part[1][warp] = i_sum; }
+        __syncthreads();
+        int e_all = 0, i_all = 0;
+#pragma unroll
+        for (int i = 0; i < LIST_THREADS / 32; ++i) {
+            if (i == warp) { e_sum += e_all; i_sum += i_all; }
+            e_all += s_part[0][i];
+            i_all += s_part[1][i];
+        }
+        if ((int)threadIdx.x < C) {
+            dsmem_st_u32(dsmem_addr(&s_total[rank][0], threadIdx.x), (uint32_t)e_all);
+            dsmem_st_u32(dsmem_addr(&s_total[rank][1], threadIdx.x), (uint32_t)i_all);
+        }
+        cluster_barrier();
+        int next = entry0 + e_sum - entries, item = item0 + i_sum - items;
+        for (int r = 0; r < C; ++r) {
+            if (r < rank) { next += s_total[r][0]; item += s_total[r][1]; }
+            entry0 += s_total[r][0];
+            item0 += s_total[r][1];
+        }
+        BlockItem *out = w.items + uh * w.max_items + (int64_t)item * w.parts;
+        for (int b = b0; b < b1; ++b) {
+            const int from = next;
+            if (per > 1) counts(b);                    // (else they are at hand)
+#pragma unroll
+            for (int r = 0; r < LIST_CTAS; ++r)
+                if (r < C) {
+                    dsmem_st_u32(dsmem_addr(s_bin + b, r), (uint32_t)next);
+                    next += c[r];
+                }
+            for (int p = 0; next > from && p < w.parts; ++p) {
+                BlockItem it = {};
+                it.uh = uh;
+                it.part = (lo + b) * w.parts + p;
+                const uint64_t live = rows.mask64((int64_t)it.part * pr);
+                it.live[0] = (uint32_t)live;
+                it.live[1] = pr > 32 ? (uint32_t)(live >> 32) : 0u;
+                for (int e = from; e < next; e += TILE) {
+                    it.first = e;
+                    it.n = min(TILE, next - e);
+                    *out++ = it;
+                }
             }
         }
-        first += n;
+        cluster_barrier();                             // (the last use of another CTA's shared memory)
+        int2 *list = w.list + base;
+        each([&](int e, int b, int r) { list[atomicAdd(&s_bin[b], 1)] = make_int2(e, r); });
+        __syncthreads();
     }
-    __syncthreads();
-    int2 *list = w.list + base;
-    each([&](int i, int b) {
-        if (b >= lo) list[atomicAdd(&s_bin[b - lo], 1)] = make_int2(i, idx[i / s.n_top]);
-    });
+    if (threadIdx.x == 0 && rank == 0) w.n_items[uh] = item0 * w.parts;
+    if (bad) latch_status(s.status, RS3_EINVAL);
 }
 
 __device__ __forceinline__ uint4 lds128(uint32_t addr)
@@ -423,11 +446,12 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t
 
 template <int D, int TR>
 struct BlockTile {
-    static constexpr int CONSUMERS = 8, THREADS = 32 * (CONSUMERS + 1);
+    static constexpr int CONSUMERS = 7, THREADS = 32 * (CONSUMERS + 1);
     static constexpr int CTAS = D == 256 ? 1 : 2;      // per SM
     static constexpr int HALF = TR * D * 2, STAGE = 2 * HALF;      // bytes of a part's keys; keys and values
     static constexpr int FIT = (D == 256 ? 196608 : 98304) / STAGE, STAGES = FIT > 8 ? 8 : FIT;
     static constexpr int SMEM = STAGES * STAGE + 1024;             // stages begin at a multiple of 1 KB
+    static constexpr bool EARLY = true;             // registers hold a tile's queries while the one before goes on
 };
 
 // Persistent CTAs walk the items.  A producer thread brings the parts' keys and values by TMA (128-byte
@@ -445,9 +469,9 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
     using namespace tc;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_bars[2 * X::STAGES];
-    __shared__ int32_t s_first[MAX_SEGMENTS + 1];
+    __shared__ int32_t s_first[MAX_HEADS + 1];
     __shared__ BlockItem s_item[CHUNK_ITEMS];
-    __shared__ int32_t s_tile0[CHUNK_ITEMS];
+    __shared__ int32_t s_tile0[CHUNK_ITEMS];           // the warp that takes an item's first tile
     __shared__ int s_abort;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t full = smem_u32(s_bars), empty = full + 8u * X::STAGES;
@@ -464,16 +488,16 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
         fence_proxy_async();
     }
     pdl_wait();
-    const int n_seg = s.U * s.H * w.segments;
+    const int heads = s.U * s.H;
     const int64_t row_elems = (int64_t)s.H * D;
     uint32_t cnt = 0, issued = 0;                      // parts gone through: stage cnt % STAGES, phase cnt / STAGES; the producer's
     int next = blockIdx.x, turn = 0;                   // this CTA's next item; tiles before the chunk
-    for (int g0 = 0; g0 < n_seg; g0 += MAX_SEGMENTS) {
-        const int n = min(MAX_SEGMENTS, n_seg - g0);
+    for (int g0 = 0; g0 < heads; g0 += MAX_HEADS) {
+        const int n = min(MAX_HEADS, heads - g0);
         __syncthreads();
         for (int i = threadIdx.x; i < n; i += X::THREADS) s_first[i + 1] = w.n_items[g0 + i];
         __syncthreads();
-        if (warp == 0) {                               // items before each segment
+        if (warp == 0) {                               // items before each (unit, head)
             int run = 0;
             for (int c0 = 0; c0 < n; c0 += 32) {
                 int v = c0 + lane < n ? s_first[c0 + lane + 1] : 0;
@@ -494,15 +518,18 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             const int chunk = min(CHUNK_ITEMS, (total - next + (int)gridDim.x - 1) / (int)gridDim.x);
             if ((int)threadIdx.x < chunk) {
                 const int at = next + threadIdx.x * gridDim.x;
-                int x = 0, y = n;                      // the last segment whose items begin at or before `at`
+                int x = 0, y = n;                      // the last one whose items begin at or before `at`
                 while (y - x > 1) {
                     const int mid = (x + y) >> 1;
                     if (s_first[mid] <= at) x = mid; else y = mid;
                 }
-                s_item[threadIdx.x] = w.items[(g0 + x) / w.segments * w.max_items + w.first_item[g0 + x] + (at - s_first[x])];
+                BlockItem it = w.items[(g0 + x) * w.max_items + (at - s_first[x])];
+                const int u = it.uh / s.H;
+                it.q = ((s.rope ? (int64_t)u * s.k_max : (int64_t)__ldg(s.unit_group + u) * s.mn) * s.H + (it.uh - u * s.H)) * D;
+                s_item[threadIdx.x] = it;
             }
             __syncthreads();
-            if (warp == 0) {                           // tiles before each item
+            if (warp == 0) {                           // the warps take the items' tiles in turn
                 int run = turn;
                 for (int c0 = 0; c0 < chunk; c0 += 32) {
                     const int tiles = c0 + lane < chunk ? (s_item[c0 + lane].n + 15) >> 4 : 0;
@@ -512,7 +539,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                         const int t = __shfl_up_sync(0xffffffffu, v, o);
                         if (lane >= o) v += t;
                     }
-                    if (c0 + lane < chunk) s_tile0[c0 + lane] = run + v - tiles;
+                    if (c0 + lane < chunk) s_tile0[c0 + lane] = (run + v - tiles) % X::CONSUMERS;
                     run += __shfl_sync(0xffffffffu, v, 31);
                 }
             }
@@ -538,51 +565,50 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             } else {
                 bool ok = true;
                 const int r = lane >> 2, t = lane & 3;
-                // list entries of this warp's next tile, at or behind item i: rows lane / 4 and + 8
+                // list entries of this warp's next tile, at or behind item i (rows lane / 4 and + 8), and its queries:
+                // of 64 columns this lane holds the pieces 2 (lane % 4) and + 1
                 int2 ahead[2];
+                int64_t ahead_q = 0;
                 const auto look_ahead = [&](int i) {
                     ahead[0] = ahead[1] = make_int2(-1, -1);
                     for (; i < chunk; ++i) {
-                        const int tile = (warp - s_tile0[i]) & (X::CONSUMERS - 1), m = s_item[i].n - tile * 16;
+                        const int tile = warp - s_tile0[i] + (warp < s_tile0[i] ? X::CONSUMERS : 0), m = s_item[i].n - tile * 16;
                         if (m <= 0) continue;
                         const int2 *list = w.list + (int64_t)s_item[i].uh * s.k_max * s.n_top + s_item[i].first + tile * 16;
 #pragma unroll
                         for (int x = 0; x < 2; ++x)
                             if (r + 8 * x < m) ahead[x] = __ldg(list + r + 8 * x);
+                        ahead_q = s_item[i].q;
                         break;
                     }
                 };
+                const uint16_t *rotated = reinterpret_cast<const uint16_t *>(w.q);
+                const uint16_t *Q = s.rope ? rotated : static_cast<const uint16_t *>(s.q);
+                uint4 q[2][D / 32];
+                const auto load_q = [&]() {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            q[x][c] = make_uint4(0, 0, 0, 0);
+                            if (ahead[x].y >= 0)
+                                q[x][c] = __ldg(reinterpret_cast<const uint4 *>(Q + ahead_q + ahead[x].y * row_elems) + (c >> 1) * 8 + 2 * t + (c & 1));
+                        }
+                };
                 look_ahead(0);
+                if (X::EARLY) load_q();
                 for (int i = 0; i < chunk && ok; ++i) {
                     const uint32_t k = cnt + i, st = k % X::STAGES;
-                    const int tile = (warp - s_tile0[i]) & (X::CONSUMERS - 1);
+                    const int tile = warp - s_tile0[i] + (warp < s_tile0[i] ? X::CONSUMERS : 0);
                     const int m = s_item[i].n - tile * 16;     // queries of this warp's tile
                     if (m <= 0) {                      // the others'
                         ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
                         if (ok && lane == 0) mbar_arrive(empty + 8u * st);
                         continue;
                     }
-                    const int uh = s_item[i].uh, u = uh / s.H, h = uh - u * s.H;
-                    const int64_t pair0 = (int64_t)uh * s.k_max * s.n_top;
-                    // of 64 columns this lane holds the pieces 2 (lane % 4) and + 1
-                    const int2 e[2] = {ahead[0], ahead[1]};
-                    uint4 q[2][D / 32];
-                    const uint16_t *Q = static_cast<const uint16_t *>(s.q) + (int64_t)__ldg(s.unit_group + u) * s.mn * row_elems + h * D;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            q[x][c] = make_uint4(0, 0, 0, 0);
-                            if (e[x].y >= 0)
-                                q[x][c] = __ldg(reinterpret_cast<const uint4 *>(Q + e[x].y * row_elems) + (c >> 1) * 8 + 2 * t + (c & 1));
-                        }
-                    if (s.rope)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int c = 0; c < D / 32; ++c)
-                                if (e[x].y >= 0)
-                                    q[x][c] = rotate_q_piece(q[x][c], s.rope + (int64_t)e[x].y * D + ((c >> 1) * 8 + 2 * t + (c & 1)) * 8);
+                    const int64_t pair0 = (int64_t)s_item[i].uh * s.k_max * s.n_top;
+                    const int entry[2] = {ahead[0].x, ahead[1].x};
+                    if (!X::EARLY) load_q();
                     look_ahead(i + 1);
                     ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
                     if (!ok) break;
@@ -604,6 +630,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                             mma_16x8x16(c[x], q[0][b].z, q[1][b].z, q[0][b].w, q[1][b].w, y.z, y.w);
                         }
                     }
+                    if (X::EARLY) load_q();            // the next tile's, while this one goes on
                     // this lane holds keys 8 x + 2 t, + 1 of its two rows
                     if (!whole) {
 #pragma unroll
@@ -663,8 +690,8 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                     for (int y = 0; y < 2; ++y) {
                         sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
                         sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
-                        if (e[y].x < 0) continue;
-                        const int64_t slot = (pair0 + e[y].x) * w.parts + s_item[i].part % w.parts;
+                        if (entry[y] < 0) continue;
+                        const int64_t slot = (pair0 + entry[y]) * w.parts + s_item[i].part % w.parts;
                         if (t == 0) w.ml[slot] = make_float2(mx[y], sum[y]);
                         float *dst = w.o + slot * D + 2 * t;
 #pragma unroll
@@ -684,7 +711,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             }
             cnt += chunk;
             next += chunk * (int)gridDim.x;
-            turn = (s_tile0[chunk - 1] + ((s_item[chunk - 1].n + 15) >> 4)) & (X::CONSUMERS - 1);
+            turn = (s_tile0[chunk - 1] + ((s_item[chunk - 1].n + 15) >> 4)) % X::CONSUMERS;
             __syncthreads();
         }
         next -= total;
@@ -784,19 +811,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
 
 // Where the parts of a by-block call lie in its workspace.
 struct WorkLayout {
-    int64_t segments, bins, max_items;
-    size_t n_items, first_item, items, list, ml, o, total;
+    int64_t max_items;
+    size_t n_items, items, list, q, ml, o, total;
 };
 
 WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top, int64_t nb, int64_t parts)
 {
     WorkLayout l = {};
     const int64_t uh = U * H, pairs = k_max * n_top;
-    const int64_t least = nb > LIST_BINS ? (nb + LIST_BINS - 1) / LIST_BINS : 1;
-    // lists are made by about a CTA per SM, of no fewer than 64 blocks each
-    l.segments = least;
-    while (uh * l.segments < 128 && nb / (2 * l.segments) >= 64) l.segments *= 2;
-    l.bins = (nb + l.segments - 1) / l.segments;
     l.max_items = ((nb < pairs ? nb : pairs) + pairs / TILE + 1) * parts;
     size_t at = 0;
     const auto part = [&](size_t bytes) {
@@ -804,10 +826,10 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
         at = align_up(at + bytes, 256);
         return x;
     };
-    l.n_items = part((size_t)(uh * least + 512) * 4);      // at least uh * segments, and never falling
-    l.first_item = part((size_t)(uh * least + 512) * 4);
+    l.n_items = part((size_t)uh * 4);
     l.items = part((size_t)(uh * l.max_items) * sizeof(BlockItem));
     l.list = part((size_t)(uh * pairs) * 8);
+    l.q = part((size_t)(uh * k_max * d) * 2);
     l.ml = part((size_t)(uh * pairs * parts) * 8);
     l.o = part((size_t)(uh * pairs * parts) * (size_t)d * 4);
     l.total = at;
@@ -849,15 +871,22 @@ rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t s
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     BlockWork w = {};
     w.n_items = reinterpret_cast<int32_t *>(ws + l.n_items);
-    w.first_item = reinterpret_cast<int32_t *>(ws + l.first_item);
     w.items = reinterpret_cast<BlockItem *>(ws + l.items);
     w.list = reinterpret_cast<int2 *>(ws + l.list);
+    w.q = reinterpret_cast<uint4 *>(ws + l.q);
     w.ml = reinterpret_cast<float2 *>(ws + l.ml);
     w.o = reinterpret_cast<float *>(ws + l.o);
-    w.segments = (int32_t)l.segments;
-    w.bins = (int32_t)l.bins;
+    w.bins = s.nb < LIST_BINS ? s.nb : LIST_BINS;
+    // with 2^t >= n_top and M = ceil(2^(28 + t) / n_top): x M / 2^(28 + t) is above x / n_top by less than 2^-t <= 1 / n_top
+    uint32_t t = 0;
+    while ((1 << t) < s.n_top) ++t;
+    w.per_top_shift = 28 + t;
+    w.per_top = (uint32_t)(((1ull << w.per_top_shift) + s.n_top - 1) / s.n_top);
+    // the largest cluster whose CTAs are on the SMs at once
+    w.cluster = LIST_CTAS;
+    while (w.cluster > 1 && (int64_t)s.U * s.H * w.cluster > rs3_sm_count()) w.cluster /= 2;
     w.parts = parts;
-    w.list_ctas = (int32_t)(s.U * s.H * l.segments);
+    w.list_ctas = s.U * s.H * w.cluster;
     w.max_items = l.max_items;
     w.wait_ns = rs3_get_wait_limit_ns();
     int64_t nvec = 0, pass = 0;
@@ -866,7 +895,10 @@ rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t s
         pass = (nvec + 4 * LIST_THREADS - 1) / (4 * LIST_THREADS);
         if (pass > 2 * rs3_sm_count()) pass = 2 * rs3_sm_count();
     }
-    launch_pdl(k_block_lists, dim3((unsigned)(w.list_ctas + pass)), dim3(LIST_THREADS), (size_t)l.bins * 4, st, a, w, nvec);
+    w.pass_ctas = (int32_t)pass;
+    const int64_t turn = s.rope ? ((int64_t)s.U * s.k_max * s.H * s.d / 8 + LIST_THREADS - 1) / LIST_THREADS : 0;
+    const int64_t ctas = (w.list_ctas + pass + turn + w.cluster - 1) / w.cluster * w.cluster;     // whole clusters
+    launch_pdl_cluster(k_block_lists, w.cluster, dim3((unsigned)ctas), dim3(LIST_THREADS), (size_t)w.bins * 4, st, a, w, nvec);
     rs3_status r = RS3_EINTERNAL;
     const bool half = s.bs == 32;
     if (s.d == 64) r = half ? launch_attend<64, 32>(a, w, st) : launch_attend<64, 64>(a, w, st);

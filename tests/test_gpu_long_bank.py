@@ -782,6 +782,90 @@ def test_one_block_chosen_by_everybody_and_scores_far_apart(rs3):
     assert int(b.st) == 0 and (err <= tol).all(), float((err - tol).max())
 
 
+@pytest.mark.parametrize("block,dtype,H,d,n,n_top", [(32, "bf16", 2, 64, 300, 9), (32, "bf16", 1, 128, 1000, 40), (64, "f32", 1, 64, 20, 5)])
+def test_sparse_readout_over_many_blocks(rs3, block, dtype, H, d, n, n_top):
+    """A bank of thousands of blocks, all of its rows live; blocks chosen by one query, by many, twice by one."""
+    rows, mn = (600_000 if block == 64 else 300_000), 1024
+    bank = rs3.Bank(1, H, d, dtype, mn, 0, -1, rows, 4, 0)
+    g, st = gen(41), status()
+    for x in (bank.k_store, bank.v_store):
+        x.normal_(generator=g)
+    rs3.rs3_bank_commit(bank, bank.k_store[:, :mn].clone(), bank.v_store[:, :mn].clone(), None, 0, st)
+    bank.counters[0, 1] = rows                             # as if the ring had been filled
+    nb = bank.blocks(block)
+    assert nb > 8192
+    q = torch.randn((1, mn, H * d), generator=g, device="cuda").to(DT[dtype])
+    idx = torch.randperm(mn, generator=g, device="cuda")[:n].to(torch.int32).view(1, n).contiguous()
+    sel = torch.randint(0, rows // block, (1, H, n, n_top), generator=g, device="cuda").to(torch.int32)
+    sel[..., 0] = 8192                                     # everybody's
+    sel[:, :, ::5, 2] = sel[:, :, ::5, 3]
+    out = torch.zeros((1, mn, H * d), dtype=DT[dtype], device="cuda")
+    ws = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(1, H, d, n, n_top, nb, dtype), dtype=torch.uint8, device="cuda")
+    one, zero = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    rs3.rs3_sparse_readout(q, dtype, 1, mn, H, d, zero, idx, one, n, bank, block, sel, n_top, None, None, out, 0.0, ws, st)
+    assert int(st) == 0
+    want, tol = torch.zeros_like(out, dtype=torch.float64), torch.zeros_like(out, dtype=torch.float64)
+    bf, half = dtype == "bf16", HALF[dtype]
+    for h in range(H):
+        col = slice(h * d, (h + 1) * d)
+        for j0 in range(0, n, 50):
+            cells = idx[0, j0:j0 + 50].long()
+            r = (sel[0, h, j0:j0 + 50].long()[..., None] * block + torch.arange(block, device="cuda")).flatten(1)
+            k, v, x = bank.k_store[0, :, col][r].double(), bank.v_store[0, :, col][r].double(), q[0, cells, col].double()
+            p = torch.softmax(torch.einsum("nrd,nd->nr", k, x) * d ** -0.5, 1)
+            A, size = torch.einsum("nr,nrd->nd", p, v), torch.einsum("nr,nrd->nd", p, v.abs())
+            s_abs = (torch.einsum("nrd,nd->nr", k.abs(), x.abs()) * d ** -0.5).max(1).values[:, None]
+            want[0, cells, col] = A                        # (the bounds of readout_ref)
+            tol[0, cells, col] = half * A.abs() + size * (torch.expm1(2 * s_abs * 2.0 ** -24 * 300) + 300 * 2.0 ** -24 + (half if bf else 0.0)) * 1.01
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), float((err - tol).max())
+
+
+def test_sparse_readout_by_block_latches_what_the_device_finds(rs3):
+    """As below, for a call large enough to go by block; a bad entry leaves the others' results as they are."""
+    U, H, n, n_top = 3, 2, 150, 6
+    b = Built(rs3, U=U, H=H, d=64, m=13, n=13, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
+    nb = b.bank.blocks(32)
+    q, idx, count, group = queries(b, 1, n, [n, n, n])
+    group.zero_()
+    sel0 = torch.randint(0, nb, (U, H, n, n_top), generator=gen(3), device="cuda").to(torch.int32)
+
+    def read(idx=idx, count=count, group=group, sel=sel0):
+        b.st.zero_()
+        out = torch.zeros((U, b.mn, H * 64), dtype=torch.bfloat16, device="cuda")
+        run_readout(rs3, b, q, idx, count, group, sel, None, 32, 0.0, None, out, 1)
+        return int(b.st), out
+
+    code, good = read()
+    assert code == 0
+    E = rs3.RS3_EINVAL
+    for bad in (-1, n + 1, -(1 << 31), (1 << 31) - 1):
+        c = count.clone()
+        c[1] = bad
+        code, out = read(count=c)
+        assert code == E and not out[1].any() and torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+    for bad in (-1, 1):
+        gr = group.clone()
+        gr[2] = bad
+        code, out = read(group=gr)
+        assert code == E and not out[2].any() and torch.equal(out[:2], good[:2])
+    for bad in (-1, b.mn, -(1 << 31), (1 << 31) - 1):
+        i = idx.clone()
+        i[0, 3] = bad
+        code, out = read(idx=i)
+        left = torch.ones(b.mn, dtype=torch.bool, device="cuda")
+        left[int(idx[0, 3])] = False
+        assert code == E and torch.equal(out[1:], good[1:]) and torch.equal(out[0, left], good[0, left])
+    for bad in (nb, 1 << 30, (1 << 31) - 1):
+        sel = sel0.clone()
+        sel[0, 0, 4, 1] = bad
+        code, out = read(sel=sel)
+        assert code == E and torch.equal(out[1:], good[1:])
+        sel[0, 0, 4, 1] = -1
+        code, same = read(sel=sel)
+        assert code == 0 and torch.equal(out, same)
+
+
 def test_sparse_calls_latch_what_the_device_finds(rs3):
     b = Built(rs3, U=3, H=1, d=64, m=8, n=8, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
     nb = b.bank.blocks(32)
