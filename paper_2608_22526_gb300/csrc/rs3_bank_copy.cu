@@ -7,9 +7,9 @@
 // axis that the CTAs walk in strides, because only the device knows the banks' lengths.
 //
 // With a keep mask the rows' places depend on the kept rows before them: k_keep_count turns the
-// mask into words of 64 rows and their counts over all SMs, and the last CTA of a unit to arrive turns
-// the counts into places and the unit's new counters; k_bank_copy then moves the rows.  Without one the
-// places are known and the copy is the only launch.
+// mask into words of 64 rows and counts the kept rows over all SMs, and the last CTA of a unit to arrive sums the
+// counts up; k_bank_copy then moves the rows and publishes the counters.  Without one the places are known and the
+// copy is the only launch.
 #include "rs3_bank.cuh"
 
 #include <initializer_list>
@@ -19,6 +19,7 @@ namespace {
 constexpr int COPY_CHUNK = 64;             // logical rows of a chunk: a word of the mask
 constexpr int COPY_THREADS = 256;
 constexpr int COPY_FLIGHT = 4;             // pieces of K and of V in flight per thread
+constexpr int SLOT_CHUNKS = 64;            // chunks that a CTA counts together
 constexpr int COPY_UNITS = 1024;           // units whose chunk counts a CTA holds at a time
 
 struct CopyArgs {
@@ -28,8 +29,11 @@ struct CopyArgs {
     const int32_t *parent;
     const uint8_t *keep;
     int64_t keep_stride;
-    int64_t *place;            // [U][chunks + 2]: kept rows before each chunk, of the pinned rows, of pinned + ring
+    int64_t *place;            // [U][chunks + 3]: kept rows of its slot before each chunk; of the pinned rows (-1: they do
+                               // not fit), of pinned + ring, of all
     uint64_t *words;           // [U][chunks]: the kept rows of each
+    int64_t *before;           // [U][slots]: kept rows before each slot
+    int64_t slots;
     int64_t chunks;            // of a mask row
     int64_t row_bytes;
     int32_t U, U_src;
@@ -144,24 +148,34 @@ __device__ void publish(const CopyArgs &a, int u, int p, int64_t live, int64_t c
     }
 }
 
-// The mask's words and their counts: a thread takes 16 rows, four threads a chunk; the last CTA of a
-// unit to arrive sums the counts up, decides whether the rows fit and publishes the unit's counters.
+// Kept rows of unit u before its logical row r, of n in all.
+__device__ __forceinline__ int64_t kept_before(const CopyArgs &a, int u, int64_t r, int64_t length)
+{
+    const int64_t *place = a.place + (int64_t)u * (a.chunks + 3);
+    if (r >= length) return __ldcg(place + a.chunks + 2);
+    const int64_t ch = r / COPY_CHUNK;
+    return __ldcg(a.before + u * a.slots + ch / SLOT_CHUNKS) + __ldcg(place + ch) +
+           __popcll(__ldcg(a.words + u * a.chunks + ch) & ((1ull << (r % COPY_CHUNK)) - 1ull));
+}
+
+// The mask's words and their counts: a thread takes 16 rows, four threads a chunk, a CTA a slot; the last CTA of a
+// unit to arrive sums the slots up and decides whether the rows fit.
 __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
 {
+    static_assert(SLOT_CHUNKS * COPY_CHUNK == 16 * COPY_THREADS, "a CTA's rows are a slot");
     pdl_wait();
     const int u = blockIdx.y;
     const CopyUnit c = copy_unit(a, u, blockIdx.x == 0 && threadIdx.x == 0);
-    int64_t *place = a.place + (int64_t)u * (a.chunks + 2);
-    uint64_t *words = a.words + (int64_t)u * a.chunks;
+    int64_t *place = a.place + (int64_t)u * (a.chunks + 3);
     if (c.p < 0) {
         if (blockIdx.x == 0 && threadIdx.x == 0) place[a.chunks] = -1;
         return;
     }
     const uint8_t *m = a.keep + (int64_t)u * a.keep_stride;
     const bool wide = (reinterpret_cast<uintptr_t>(m) & 15u) == 0;
-    const int64_t n_chunks = (c.length + COPY_CHUNK - 1) / COPY_CHUNK;
-    for (int64_t r0 = (int64_t)blockIdx.x * (16 * COPY_THREADS); r0 < c.length; r0 += (int64_t)gridDim.x * (16 * COPY_THREADS)) {
-        const int64_t r = r0 + 16 * threadIdx.x;
+    const int64_t n_slots = (c.length + 16 * COPY_THREADS - 1) / (16 * COPY_THREADS);
+    for (int64_t slot = blockIdx.x; slot < n_slots; slot += gridDim.x) {
+        const int64_t r = slot * (16 * COPY_THREADS) + 16 * threadIdx.x;
         uint32_t bits = 0;
         if (wide && r + 16 <= c.length) {
             const uint4 v = __ldg(reinterpret_cast<const uint4 *>(m + r));
@@ -176,10 +190,12 @@ __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
         uint64_t word = (uint64_t)bits << (16 * (threadIdx.x & 3));
         word |= __shfl_xor_sync(0xffffffffu, word, 1);
         word |= __shfl_xor_sync(0xffffffffu, word, 2);
+        const int64_t end = cta_sums(__popc(bits));
         if ((threadIdx.x & 3) == 0 && r < c.length) {
-            words[r / COPY_CHUNK] = word;
-            place[r / COPY_CHUNK] = __popcll(word);
+            a.words[u * a.chunks + r / COPY_CHUNK] = word;
+            place[r / COPY_CHUNK] = end - __popc(bits);
         }
+        if (threadIdx.x == COPY_THREADS - 1) a.before[u * a.slots + slot] = end;
     }
     __shared__ bool s_last;
     __threadfence();
@@ -192,47 +208,27 @@ __global__ void __launch_bounds__(COPY_THREADS) k_keep_count(CopyArgs a)
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    // exclusive sums over the chunks, 16 in a row per thread
+    // exclusive sums over the slots
     __shared__ int64_t s_run;
-    constexpr int PER = 16;
     int64_t run = 0;
-    for (int64_t c0 = 0; c0 < n_chunks; c0 += PER * COPY_THREADS) {
-        const int64_t ch = c0 + PER * threadIdx.x;
-        int32_t v[PER], n = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] = ch + i < n_chunks ? (int32_t)__ldcg(place + ch + i) : 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) n += v[i];
+    for (int64_t s0 = 0; s0 < n_slots; s0 += COPY_THREADS) {
+        const int64_t slot = s0 + threadIdx.x;
+        const int64_t n = slot < n_slots ? __ldcg(a.before + u * a.slots + slot) : 0;
         const int64_t end = run + cta_sums(n);
-        int64_t at = end - n;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (ch + i < n_chunks) place[ch + i] = at;
-            at += v[i];
-        }
+        if (slot < n_slots) a.before[u * a.slots + slot] = end - n;
         if (threadIdx.x == COPY_THREADS - 1) s_run = end;
         __syncthreads();
         run = s_run;
     }
+    if (threadIdx.x == 0) place[a.chunks + 2] = run;
     __syncthreads();
-    // kept rows before logical row r
-    const auto before = [&](int64_t r) -> int64_t {
-        const int64_t ch = r / COPY_CHUNK;
-        return ch < n_chunks ? place[ch] + __popcll(__ldcg(words + ch) & ((1ull << (r % COPY_CHUNK)) - 1ull)) : run;
-    };
-    const int64_t ring_end = c.rows.len[0] + c.rows.len[1] + c.rows.len[2];
-    const int64_t cond = before(c.rows.len[0]), ring = before(ring_end) - cond, ptr = run - cond - ring;
-    const bool fits = cond <= a.dst.pinned_cap && ring <= a.dst.ring_cap && ptr <= a.dst.n_ptr;
-    if (threadIdx.x == 0) {
-        if (!fits) latch_status(a.status, RS3_ECAPACITY);
-        place[a.chunks] = fits ? cond : -1;
-        place[a.chunks + 1] = cond + ring;
-    }
-    if (!fits) return;
-    publish(a, u, c.p, ring_end - c.rows.len[0], cond, ring, ptr, [&](int64_t &r0, int64_t &r1) {
-        r0 = before(c.rows.len[0] + r0) - cond;
-        r1 = before(c.rows.len[0] + r1) - cond;
-    });
+    if (threadIdx.x != 0) return;
+    const int64_t cond = kept_before(a, u, c.rows.len[0], c.length);
+    const int64_t ring = kept_before(a, u, c.rows.len[0] + c.rows.len[1] + c.rows.len[2], c.length) - cond;
+    const bool fits = cond <= a.dst.pinned_cap && ring <= a.dst.ring_cap && run - cond - ring <= a.dst.n_ptr;
+    if (!fits) latch_status(a.status, RS3_ECAPACITY);
+    place[a.chunks] = fits ? cond : -1;
+    place[a.chunks + 1] = cond + ring;
 }
 
 template <bool KEEP>
@@ -256,7 +252,7 @@ __global__ void __launch_bounds__(COPY_THREADS, 3) k_bank_copy(CopyArgs a)
         for (int i = threadIdx.x; i < n_units; i += COPY_THREADS) {
             const CopyUnit x = copy_unit(a, u0 + i, !KEEP && blockIdx.x == 0);
             int64_t n = (x.length + COPY_CHUNK - 1) / COPY_CHUNK;
-            if (KEEP && n > 0 && a.place[(int64_t)(u0 + i) * (a.chunks + 2) + a.chunks] < 0) n = 0;   // does not fit
+            if (KEEP && n > 0 && a.place[(int64_t)(u0 + i) * (a.chunks + 3) + a.chunks] < 0) n = 0;   // does not fit
             s_first[i + 1] = n;
         }
         __syncthreads();
@@ -285,9 +281,9 @@ __global__ void __launch_bounds__(COPY_THREADS, 3) k_bank_copy(CopyArgs a)
             }
             const int u = u0 + lo;
             const int64_t ch = next - s_first[lo];
-            const int64_t *place = a.place + (int64_t)u * (a.chunks + 2);
-            const uint64_t word = KEEP ? a.words[(int64_t)u * a.chunks + ch] : 0;
-            const int64_t first = KEEP ? place[ch] : ch * COPY_CHUNK;
+            const int64_t *place = a.place + (int64_t)u * (a.chunks + 3);
+            const uint64_t word = KEEP ? a.words[u * a.chunks + ch] : 0;
+            const int64_t first = KEEP ? a.before[u * a.slots + ch / SLOT_CHUNKS] + place[ch] : ch * COPY_CHUNK;
             if (u != last) c = copy_unit(a, u, false);
             last = u;
             const int64_t left = c.length - ch * COPY_CHUNK;
@@ -341,13 +337,24 @@ __global__ void __launch_bounds__(COPY_THREADS, 3) k_bank_copy(CopyArgs a)
         }
         next -= total;
     }
-    if (!KEEP)                                        // the counters, a unit per CTA (a source's are never written)
-        for (int u = blockIdx.x; u < a.U; u += gridDim.x) {
-            const CopyUnit c = copy_unit(a, u, false);
-            if (c.p < 0) continue;
-            const int64_t live = c.rows.len[1] + c.rows.len[2];
-            publish(a, u, c.p, live, c.rows.len[0], live, c.rows.len[3], [](int64_t &, int64_t &) {});
+    // the counters, a unit per CTA, from the last one on, which has no more chunks than the others (a source's counters
+    // are never written)
+    for (int64_t u = gridDim.x - 1 - blockIdx.x; u < a.U; u += gridDim.x) {
+        const CopyUnit x = copy_unit(a, (int)u, false);
+        if (x.p < 0) continue;
+        const int64_t ring0 = x.rows.len[0], ring1 = ring0 + x.rows.len[1] + x.rows.len[2];
+        if (!KEEP) {
+            publish(a, (int)u, x.p, ring1 - ring0, ring0, ring1 - ring0, x.rows.len[3], [](int64_t &, int64_t &) {});
+        } else {
+            const int64_t *place = a.place + u * (a.chunks + 3) + a.chunks;
+            const int64_t cond = place[0], both = place[1];
+            if (cond < 0) continue;
+            publish(a, (int)u, x.p, ring1 - ring0, cond, both - cond, place[2] - both, [&](int64_t &r0, int64_t &r1) {
+                r0 = kept_before(a, (int)u, ring0 + r0, x.length) - cond;
+                r1 = kept_before(a, (int)u, ring0 + r1, x.length) - cond;
+            });
         }
+    }
 }
 
 // A warp per unit: the frames given up at either end leave the counters.
@@ -379,6 +386,7 @@ __global__ void k_drop_frames(BankDev bk, int U, const int32_t *n_oldest, const 
 }
 
 int64_t copy_chunks(int64_t keep_stride) { return (keep_stride + COPY_CHUNK - 1) / COPY_CHUNK; }
+int64_t copy_slots(int64_t keep_stride) { return (copy_chunks(keep_stride) + SLOT_CHUNKS - 1) / SLOT_CHUNKS; }
 
 // Storage [a, a + n) and [b, b + m) share a byte.
 bool overlap(const void *a, int64_t n, const void *b, int64_t m)
@@ -392,7 +400,7 @@ bool overlap(const void *a, int64_t n, const void *b, int64_t m)
 extern "C" size_t rs3_bank_copy_workspace_bytes(int U, int64_t keep_stride)
 {
     if (U < 1 || keep_stride < 1) return 0;
-    return (size_t)U * (size_t)(2 * copy_chunks(keep_stride) + 2) * 8;
+    return (size_t)U * (size_t)(2 * copy_chunks(keep_stride) + 3 + copy_slots(keep_stride)) * 8;
 }
 
 extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, const int32_t *parent, const uint8_t *keep,
@@ -427,7 +435,9 @@ extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, co
     a.keep_stride = keep_stride;
     a.place = static_cast<int64_t *>(workspace);
     a.chunks = keep ? copy_chunks(keep_stride) : 0;
-    a.words = reinterpret_cast<uint64_t *>(a.place + a.U * (a.chunks + 2));
+    a.slots = keep ? copy_slots(keep_stride) : 0;
+    a.words = reinterpret_cast<uint64_t *>(a.place + a.U * (a.chunks + 3));
+    a.before = reinterpret_cast<int64_t *>(a.words + a.U * a.chunks);
     a.row_bytes = row_bytes;
     a.same = same;
     a.status = status;
@@ -438,7 +448,7 @@ extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, co
     if (most * a.U < ctas) ctas = most * a.U > 0 ? most * a.U : 1;
     if (keep) {
         int64_t per = (2ll * rs3_sm_count() + a.U - 1) / a.U;
-        if (per > (most + COPY_THREADS / 4 - 1) / (COPY_THREADS / 4)) per = (most + COPY_THREADS / 4 - 1) / (COPY_THREADS / 4);
+        if (per > a.slots) per = a.slots;
         launch_pdl(k_keep_count, dim3((unsigned)per, (unsigned)a.U), dim3(COPY_THREADS), 0, st, a);
         launch_pdl(k_bank_copy<true>, dim3((unsigned)ctas), dim3(COPY_THREADS), 0, st, a);
     } else {
