@@ -1511,10 +1511,12 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.step = step;
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
-    // Two CTAs of 128 queries per SM, where the queries fill the SMs and their candidates have room
+    // 128 queries to a CTA, where those keep half of the SMs busy and their candidates have room.  Over 990 blocks (a tile of
+    // queries / 16 of them to a CTA): 64 queries in 32 heads 43 / 19 us, 709 in 8 heads (48 tiles) 48 / 36, 256
+    // in 32 (64 tiles) 45 / 47, 709 in 32 (192 tiles) 70 / 113.
     const int fixed = (TILE_ROWS + 2 * TILE_COLS) * 2 * (d < 64 ? 64 : d) + 1024, each = TILE_ROWS * 6;
     const int cap = (((106 * 1024 - fixed) / each / 4 - 1) | 1) * 4;       // an odd number of 16 bytes
-    if ((int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS) >= rs3_sm_count() && n_top <= TILE_TOP && cap >= n_top + 48 &&
+    if (2 * (int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS) >= rs3_sm_count() && n_top <= TILE_TOP && cap >= n_top + 48 &&
         a.s.nb <= 32 * TILE_WORDS) {
         TileArgs p = {a, cap, rs3_get_wait_limit_ns()};
         const size_t smem = (size_t)fixed + (size_t)cap * each;

@@ -451,7 +451,9 @@ struct BlockTile {
     static constexpr int HALF = TR * D * 2, STAGE = 2 * HALF;      // bytes of a part's keys; keys and values
     static constexpr int FIT = (D == 256 ? 196608 : 98304) / STAGE, STAGES = FIT > 8 ? 8 : FIT;
     static constexpr int SMEM = STAGES * STAGE + 1024;             // stages begin at a multiple of 1 KB
-    static constexpr bool EARLY = true;             // registers hold a tile's queries while the one before goes on
+    // the next tile's queries are loaded while a tile goes on, where the registers have room (heads of 128: 98.6 us
+    // without it, 102.9 with, 4 100 queries of 16 blocks; heads of 64 took 121 us for 129)
+    static constexpr bool EARLY = D != 128;
 };
 
 // Persistent CTAs walk the items.  A producer thread brings the parts' keys and values by TMA (128-byte
@@ -471,7 +473,6 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
     __shared__ __align__(8) uint64_t s_bars[2 * X::STAGES];
     __shared__ int32_t s_first[MAX_HEADS + 1];
     __shared__ BlockItem s_item[CHUNK_ITEMS];
-    __shared__ int32_t s_tile0[CHUNK_ITEMS];           // the warp that takes an item's first tile
     __shared__ int s_abort;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t full = smem_u32(s_bars), empty = full + 8u * X::STAGES;
@@ -486,21 +487,20 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmk)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmv)) : "memory");
     }
     pdl_wait();
     const int heads = s.U * s.H;
     const int64_t row_elems = (int64_t)s.H * D;
     uint32_t cnt = 0, issued = 0;                      // parts gone through: stage cnt % STAGES, phase cnt / STAGES; the producer's
-    int next = blockIdx.x, turn = 0;                   // this CTA's next item; tiles before the chunk
+    int next = blockIdx.x, turn = 0;                   // this CTA's next item; the warp that takes the next tile
     for (int g0 = 0; g0 < heads; g0 += MAX_HEADS) {
         const int n = min(MAX_HEADS, heads - g0);
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += X::THREADS) s_first[i + 1] = w.n_items[g0 + i];
-        __syncthreads();
-        if (warp == 0) {                               // items before each (unit, head)
+        const auto before_each = [&]() {               // items before each (unit, head)
             int run = 0;
             for (int c0 = 0; c0 < n; c0 += 32) {
-                int v = c0 + lane < n ? s_first[c0 + lane + 1] : 0;
+                int v = c0 + lane < n ? w.n_items[g0 + c0 + lane] : 0;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const int t = __shfl_up_sync(0xffffffffu, v, o);
@@ -510,8 +510,15 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                 run += __shfl_sync(0xffffffffu, v, 31);
             }
             if (lane == 0) s_first[0] = 0;
+        };
+        if (heads <= 32) {                             // every warp for itself, the same values: no barrier
+            before_each();
+            __syncwarp();
+        } else {
+            __syncthreads();
+            if (warp == 0) before_each();
+            __syncthreads();
         }
-        __syncthreads();
         const int total = s_first[n];
         while (next < total) {
             // the records of this CTA's next items
@@ -529,23 +536,9 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                 s_item[threadIdx.x] = it;
             }
             __syncthreads();
-            if (warp == 0) {                           // the warps take the items' tiles in turn
-                int run = turn;
-                for (int c0 = 0; c0 < chunk; c0 += 32) {
-                    const int tiles = c0 + lane < chunk ? (s_item[c0 + lane].n + 15) >> 4 : 0;
-                    int v = tiles;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const int t = __shfl_up_sync(0xffffffffu, v, o);
-                        if (lane >= o) v += t;
-                    }
-                    if (c0 + lane < chunk) s_tile0[c0 + lane] = (run + v - tiles) % X::CONSUMERS;
-                    run += __shfl_sync(0xffffffffu, v, 31);
-                }
-            }
-            __syncthreads();
             if (warp == X::CONSUMERS) {
                 if (lane == 0) {
+                    const uint64_t once = l2_once();
                     uint32_t k = cnt;
                     for (int i = 0; i < chunk; ++i, ++k) {
                         const uint32_t st = k % X::STAGES;
@@ -555,9 +548,9 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                         const uint32_t dst = base + st * X::STAGE, bar = full + 8u * st;
                         mbar_expect_tx(bar, X::STAGE);
 #pragma unroll
-                        for (int c = 0; c < D / 64; ++c) tma_load_2d(dst + c * (TR * 128), &tmk, bar, h * D + c * 64, y);
+                        for (int c = 0; c < D / 64; ++c) tma_load_2d_once(dst + c * (TR * 128), &tmk, bar, h * D + c * 64, y, once);
 #pragma unroll
-                        for (int c = 0; c < D / 64; ++c) tma_load_2d(dst + X::HALF + c * (TR * 128), &tmv, bar, h * D + c * 64, y);
+                        for (int c = 0; c < D / 64; ++c) tma_load_2d_once(dst + X::HALF + c * (TR * 128), &tmv, bar, h * D + c * 64, y, once);
                     }
                     issued = k;
                 }
@@ -565,14 +558,19 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             } else {
                 bool ok = true;
                 const int r = lane >> 2, t = lane & 3;
+                // the warps take the items' tiles in turn (an item has four at most)
+                const auto next_turn = [](int turn, int n) {
+                    turn += (n + 15) >> 4;
+                    return turn >= X::CONSUMERS ? turn - X::CONSUMERS : turn;
+                };
                 // list entries of this warp's next tile, at or behind item i (rows lane / 4 and + 8), and its queries:
                 // of 64 columns this lane holds the pieces 2 (lane % 4) and + 1
                 int2 ahead[2];
                 int64_t ahead_q = 0;
-                const auto look_ahead = [&](int i) {
+                const auto look_ahead = [&](int i, int turn) {
                     ahead[0] = ahead[1] = make_int2(-1, -1);
-                    for (; i < chunk; ++i) {
-                        const int tile = warp - s_tile0[i] + (warp < s_tile0[i] ? X::CONSUMERS : 0), m = s_item[i].n - tile * 16;
+                    for (; i < chunk; turn = next_turn(turn, s_item[i].n), ++i) {
+                        const int tile = warp - turn + (warp < turn ? X::CONSUMERS : 0), m = s_item[i].n - tile * 16;
                         if (m <= 0) continue;
                         const int2 *list = w.list + (int64_t)s_item[i].uh * s.k_max * s.n_top + s_item[i].first + tile * 16;
 #pragma unroll
@@ -595,12 +593,13 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                                 q[x][c] = __ldg(reinterpret_cast<const uint4 *>(Q + ahead_q + ahead[x].y * row_elems) + (c >> 1) * 8 + 2 * t + (c & 1));
                         }
                 };
-                look_ahead(0);
+                look_ahead(0, turn);
                 if (X::EARLY) load_q();
                 for (int i = 0; i < chunk && ok; ++i) {
                     const uint32_t k = cnt + i, st = k % X::STAGES;
-                    const int tile = warp - s_tile0[i] + (warp < s_tile0[i] ? X::CONSUMERS : 0);
+                    const int tile = warp - turn + (warp < turn ? X::CONSUMERS : 0);
                     const int m = s_item[i].n - tile * 16;     // queries of this warp's tile
+                    turn = next_turn(turn, s_item[i].n);
                     if (m <= 0) {                      // the others'
                         ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
                         if (ok && lane == 0) mbar_arrive(empty + 8u * st);
@@ -609,7 +608,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                     const int64_t pair0 = (int64_t)s_item[i].uh * s.k_max * s.n_top;
                     const int entry[2] = {ahead[0].x, ahead[1].x};
                     if (!X::EARLY) load_q();
-                    look_ahead(i + 1);
+                    look_ahead(i + 1, turn);
                     ok = mbar_wait_warp(full + 8u * st, k / X::STAGES & 1u, abort_flag, w.wait_ns);
                     if (!ok) break;
                     const uint32_t sk = base + st * X::STAGE, sv = sk + X::HALF;
@@ -711,7 +710,6 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             }
             cnt += chunk;
             next += chunk * (int)gridDim.x;
-            turn = (s_tile0[chunk - 1] + ((s_item[chunk - 1].n + 15) >> 4)) % X::CONSUMERS;
             __syncthreads();
         }
         next -= total;
@@ -836,10 +834,13 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
     return l;
 }
 
-// Whether a call's path may be by block, for which its workspace is sized.
+// Whether a call's path may be by block, for which its workspace is sized.  Three launches against one, and every row
+// read once against once per query.  Of one bank of 200 frames, blocks of 64 (by block / by query): 4 heads of 64, 64
+// queries of 4 blocks 14.9 / 9.3 us, 128 of 4 15.5 / 15.4, 64 of 16 16.9 / 16.5, 128 of 16 18.5 / 30, 787 of 16
+// 29 / 129; one head of 256, 16 queries of 4 blocks 16.0 / 21, 64 of 4 17.0 / 22, 787 of 16 33 / 162.
 bool sized_by_blocks(rs3_dtype dtype, int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top)
 {
-    return dtype == RS3_BF16 && d >= 64 && U * H * k_max * n_top >= 4096;
+    return dtype == RS3_BF16 && d >= 64 && U * H * k_max * n_top * d * d * d >= (1ll << 30);
 }
 
 // Beyond the sizes that the lists' and the tensor maps' 32-bit numbers hold it is by query.
@@ -858,7 +859,10 @@ rs3_status launch_attend(const AttendArgs &a, const BlockWork &w, cudaStream_t s
     if (r != RS3_OK) return r;
     CUtensorMap mk, mv;
     const int64_t rows = a.s.U * a.s.bank.rows_per_unit, width = (int64_t)a.s.H * D;
-    if (!tc::make_kv_map(&mk, a.k_store, width, rows, TR) || !tc::make_kv_map(&mv, a.v_store, width, rows, TR)) return RS3_ECUDA;
+    // a head of 64 is 128 bytes of a row: no more is fetched of its neighbour, whose turn comes later
+    const CUtensorMapL2promotion grain = D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
+    if (!tc::make_kv_map(&mk, a.k_store, width, rows, TR, grain) || !tc::make_kv_map(&mv, a.v_store, width, rows, TR, grain))
+        return RS3_ECUDA;
     launch_pdl(k_attend_blocks<D, TR>, dim3((unsigned)(rs3_sm_count() * X::CTAS)), dim3(X::THREADS), X::SMEM, st, a, w, mk, mv);
     return RS3_OK;
 }
