@@ -74,7 +74,8 @@ __device__ int64_t refresh_block(const DigestArgs &a, const LiveRows &rows, int6
 // lane adds its pieces' rows up in the eight partial sums, which it then joins as
 // ((0 + 4) + (2 + 6)) + ((1 + 5) + (3 + 7)): no barrier among warps.  Which rows live is worked out for 32 blocks at
 // a time, one per lane; pieces without a live row are not read.  192 KB in flight per SM: with the rows loaded
-// into registers (64 KB) all blocks of eight banks took 64 us, XX so.
+// into registers (64 KB) all blocks of eight banks (252 MB) took 64 us, 51 to 59 so.  The blocks of a newest frame take
+// 10 us, the latency of the bank's counters, the frames' lengths, a copy and its sums one after another.
 constexpr int DIGEST_WARPS = 12;
 
 template <typename T, int ITEMS>
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) k_block_select(SelectArgs a)
 // of the maxima of four blocks each reach is a bound that few more than n scores reach: these candidates are ranked
 // by counting.  (Where they are many, as among ties, the registers are cut exactly.)
 // Bound by instruction issue and, at the start, latency.  Also built: a lane per query that keeps a running threshold;
-// as scores grow towards the newest frames, that admits nearly every block (436 us where this takes XX).
+// as scores grow towards the newest frames, that admits nearly every block and took several times as long.
 constexpr int TC_ROWS = 16;                // queries of a CTA
 constexpr int TC_THREADS = 256;
 constexpr int TC_BLOCKS = 992;             // blocks of a piece: three CTAs per SM

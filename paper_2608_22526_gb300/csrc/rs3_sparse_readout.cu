@@ -70,16 +70,19 @@ struct Row<float> {
     }
 };
 
+constexpr int GATHER_WARPS = 16;           // at most
+
 // A CTA per (query, head): its warps take the listed blocks in turn.  L lanes hold a row (ITEMS
 // pieces of 16 bytes each), so a warp reads 32 / L rows at once; scores are summed over the L lanes,
 // the softmax runs online per warp in the log2 domain, and the warps' results are joined at the end.
-template <typename T, int ITEMS, int GATHER_WARPS>
-__global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs a, int L)
+template <typename T, int ITEMS, int L>
+__global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs a)
 {
     constexpr int N = Row<T>::N, GATHER_FLIGHT = 8 / ITEMS;    // rows in flight per lane group
     pdl_wait();
     __shared__ float s_o[GATHER_WARPS][256];
     __shared__ float s_m[GATHER_WARPS], s_l[GATHER_WARPS];
+    const int n_warps = (int)blockDim.x >> 5;
     const SparseArgs &s = a.s;
     const int j = blockIdx.x, h = blockIdx.y, u = blockIdx.z;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -91,7 +94,8 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
         if (threadIdx.x == 0) latch_status(s.status, RS3_EINVAL);
         return;
     }
-    const int D = s.H * s.d, sub = lane & (L - 1), group = lane / L, groups = 32 / L;
+    const int D = s.H * s.d, sub = lane & (L - 1), group = lane / L;
+    constexpr int groups = 32 / L;
     // this lane's pieces of the query, rotated, times scale * log2 e
     float q[ITEMS][N];
 #pragma unroll
@@ -120,7 +124,7 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
     for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
         for (int e = 0; e < N; ++e) o[i][e] = 0.f;
-    for (int t = warp; t < s.n_top; t += GATHER_WARPS) {
+    for (int t = warp; t < s.n_top; t += n_warps) {
         const int b = sel[t];
         if (b < 0) continue;
         if (b >= s.nb) {
@@ -155,10 +159,17 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 #pragma unroll
                     for (int e = 0; e < N; ++e) x[f] = fmaf(q[i][e], w[e], x[f]);
                 }
-                for (int k = L >> 1; k > 0; k >>= 1) x[f] += __shfl_xor_sync(0xffffffffu, x[f], k);
+            }
+#pragma unroll
+            for (int k = L >> 1; k > 0; k >>= 1)
+#pragma unroll
+                for (int f = 0; f < GATHER_FLIGHT; ++f) x[f] += __shfl_xor_sync(0xffffffffu, x[f], k);
+#pragma unroll
+            for (int f = 0; f < GATHER_FLIGHT; ++f) {
                 if (!live[f]) x[f] = -INFINITY;
                 top = fmaxf(top, x[f]);
             }
+#pragma unroll
             for (int k = L; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
             if (top == -INFINITY) continue;                  // no live row (uniform)
             const float m1 = fmaxf(m, top), keep = exp2f(m - m1);
@@ -182,6 +193,7 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
             }
         }
     }
+#pragma unroll
     for (int k = L; k < 32; k <<= 1) {
         l += __shfl_xor_sync(0xffffffffu, l, k);
 #pragma unroll
@@ -199,13 +211,11 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
     __syncthreads();
     if (threadIdx.x >= s.d / N) return;
     float top = -INFINITY, total = 0.f, y[N];
-#pragma unroll
-    for (int w = 0; w < GATHER_WARPS; ++w) top = fmaxf(top, s_m[w]);
+    for (int w = 0; w < n_warps; ++w) top = fmaxf(top, s_m[w]);
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = 0.f;
     if (top > -INFINITY) {
-#pragma unroll
-        for (int w = 0; w < GATHER_WARPS; ++w) {
+        for (int w = 0; w < n_warps; ++w) {
             const float f = exp2f(s_m[w] - top);
             total = fmaf(f, s_l[w], total);
 #pragma unroll
@@ -222,6 +232,20 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
         for (int e = 0; e < N; ++e) y[e] += r[e];
     }
     *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + at) = Row<T>::narrow(y);
+}
+
+using GatherKernel = void (*)(AttendArgs);
+
+template <typename T>
+GatherKernel gather_kernel(int pieces)         // a power of two: of 2 (bf16) or 4 (fp32) to 32
+{
+    switch (pieces) {
+    case 2: return k_attend_gather<T, 1, 2>;
+    case 4: return k_attend_gather<T, 1, 4>;
+    case 8: return k_attend_gather<T, 1, 8>;
+    case 16: return k_attend_gather<T, 1, 16>;
+    default: return k_attend_gather<T, 1, 32>;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -720,7 +744,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
 // their running maximum, eight loads at a time, then the groups are joined:
 //   out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
 // Wide heads have few queries and much to load for each; for heads of 64 four groups a query took 33 us where
-// one took XX (23 700 queries of 16 blocks).
+// one took 21 (23 700 queries of 16 blocks; 18.5 since the attention leaves its results in L2).
 constexpr int JOIN_THREADS = 256;
 
 template <int D>
@@ -956,17 +980,15 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
     } else if (k_max > 0) {
         const int pieces = d * (int)elem_bytes(dtype) / 16;
         const dim3 grid((unsigned)k_max, (unsigned)H, (unsigned)a.s.U);
-        // the fewer the queries, the more warps share a query's blocks
+        // the fewer the queries, the more warps share a query's blocks, a block to a warp at least.  Of heads of 64 in fp32,
+        // 16 blocks of 32 rows (16 / 8 / 4 warps): 128 CTAs 9.8 / 11.3 / 15.4 us, 600 CTAs 30 / 24 / 21; of 256, 300 CTAs
+        // 27 / 23 / 28; 600 CTAs of 4 blocks 22 / 12.9 / 8.8
         const int64_t ctas = (int64_t)k_max * H * a.s.U;
-        const int warps = ctas <= rs3_sm_count() ? 16 : ctas <= 4ll * rs3_sm_count() ? 8 : 4;
-        void (*kern)(AttendArgs, int);
-        if (dtype == RS3_BF16)
-            kern = warps == 16 ? k_attend_gather<uint16_t, 1, 16> : warps == 8 ? k_attend_gather<uint16_t, 1, 8> : k_attend_gather<uint16_t, 1, 4>;
-        else if (pieces <= 32)
-            kern = warps == 16 ? k_attend_gather<float, 1, 16> : warps == 8 ? k_attend_gather<float, 1, 8> : k_attend_gather<float, 1, 4>;
-        else
-            kern = warps == 16 ? k_attend_gather<float, 2, 16> : warps == 8 ? k_attend_gather<float, 2, 8> : k_attend_gather<float, 2, 4>;
-        launch_pdl(kern, grid, dim3(32 * warps), 0, st, a, pieces > 32 ? 32 : pieces);
+        int warps = ctas <= rs3_sm_count() ? GATHER_WARPS : ctas <= 3ll * rs3_sm_count() ? GATHER_WARPS / 2 : GATHER_WARPS / 4;
+        while (warps > GATHER_WARPS / 4 && warps >= 2 * n_top) warps /= 2;
+        GatherKernel kern = k_attend_gather<float, 2, 32>;
+        if (pieces <= 32) kern = dtype == RS3_BF16 ? gather_kernel<uint16_t>(pieces) : gather_kernel<float>(pieces);
+        launch_pdl(kern, grid, dim3(32 * warps), 0, st, a);
     }
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }
