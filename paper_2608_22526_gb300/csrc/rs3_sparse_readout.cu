@@ -864,7 +864,7 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
 // 29 / 129; one head of 256, 16 queries of 4 blocks 16.0 / 21, 64 of 4 17.0 / 22, 787 of 16 33 / 162.
 bool sized_by_blocks(rs3_dtype dtype, int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top)
 {
-    return dtype == RS3_BF16 && d >= 64 && U * H * k_max * n_top * d * d * d >= (1ll << 30);
+    return dtype == RS3_BF16 && d >= 64 && (double)U * H * k_max * n_top * d * d * d >= 0x1p30;
 }
 
 // Beyond the sizes that the lists' and the tensor maps' 32-bit numbers hold it is by query.

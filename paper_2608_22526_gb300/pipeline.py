@@ -131,13 +131,14 @@ class Pipeline:
         """Buffers for reading the bank by blocks: digests, the chosen blocks and workspaces."""
         w, dev, nb = self.w, self.device, self.bank.blocks(block)
         self.block, self.n_top = block, n_top
-        self.block_digest = torch.zeros((w.U, w.H, nb, w.d), dtype=torch.int8, device=dev)
-        self.block_step = torch.zeros((w.U, w.H, nb), dtype=torch.float32, device=dev)
-        self.block_sel = torch.full((w.U, w.H, max(self.k_max, 1), n_top), -1, dtype=torch.int32, device=dev)
-        self.ws_blocks = torch.empty(rs3.rs3_block_select_workspace_bytes(w.U, w.H, self.k_max, nb), dtype=torch.uint8,
-                                     device=dev)
-        self.ws_sparse = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(w.U, w.H, w.d, self.k_max, n_top, nb, w.dtype),
-                                     dtype=torch.uint8, device=dev)
+        with torch.cuda.stream(self.stream):               # (filled in the order of the calls that use them)
+            self.block_digest = torch.zeros((w.U, w.H, nb, w.d), dtype=torch.int8, device=dev)
+            self.block_step = torch.zeros((w.U, w.H, nb), dtype=torch.float32, device=dev)
+            self.block_sel = torch.full((w.U, w.H, max(self.k_max, 1), n_top), -1, dtype=torch.int32, device=dev)
+            self.ws_blocks = torch.empty(rs3.rs3_block_select_workspace_bytes(w.U, w.H, self.k_max, nb), dtype=torch.uint8,
+                                         device=dev)
+            self.ws_sparse = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(w.U, w.H, w.d, self.k_max, n_top, nb, w.dtype),
+                                         dtype=torch.uint8, device=dev)
 
     def digest(self, refresh: int = 1):
         """Brings the digests up to date: 1 after a ring commit, -1 after anything else."""
@@ -161,14 +162,15 @@ class Pipeline:
     def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
         """A pipeline (`into`, or a new one with this one's sizes) whose unit u holds the rows
         of this one's unit parent[u], those that keep[u] leaves, and its tracker."""
-        if into is None:
-            into = Pipeline(self.w, self.device, self.dense, int(self.bank.ring_cap), self.params, self.stream)
-            if hasattr(self, "block"):
-                into.use_blocks(self.block, self.n_top)
-        stride = 0 if keep is None else keep.shape[1]
-        ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
-        rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
+        # the new buffers are filled, and the workspace comes and goes, in the order of this pipeline's stream
         with torch.cuda.stream(self.stream):
+            if into is None:
+                into = Pipeline(self.w, self.device, self.dense, int(self.bank.ring_cap), self.params, self.stream)
+                if hasattr(self, "block"):
+                    into.use_blocks(self.block, self.n_top)
+            stride = 0 if keep is None else keep.shape[1]
+            ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
+            rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
             chosen = self.track[parent.clamp(min=0).long()]
             into.track.copy_(torch.where((parent >= 0)[:, None], chosen, into.track))
         return into

@@ -966,3 +966,201 @@ def test_reading_a_long_bank_frame_by_frame(rs3):
     fork.readout_blocks(qn, None, y)
     assert pipe.status_code() == 0 and fork.status_code() == 0
     assert torch.equal(y[0], x[0]) and torch.equal(y[1], x[0]) and before.shape == x.shape
+
+
+def small_pipeline(stream=None):
+    """Two units of a few frames, ready to be read by blocks; its queries."""
+    from paper_2608_22526_gb300 import synth
+    from paper_2608_22526_gb300.pipeline import Pipeline
+    w = synth.Workload("t", 0, 12, 12, 2, 64, "bf16", 1, 2, 6, 0.2, 0.4, 1, -1, 0)
+    pipe = Pipeline(w, ring_cap=20 * w.mn, stream=stream)
+    g = gen(3)
+    mask = torch.zeros((2, w.mn), dtype=torch.uint8, device="cuda")
+    mask[:, 30:90] = 1
+    z = torch.randn((1, w.mn, w.D), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((2, w.mn, w.D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        pipe.commit(k, v, mask, 0)
+    return pipe, z, mask
+
+
+def test_pipeline_buffers_belong_to_its_stream(rs3):
+    """The current stream is busy while a pipeline on another makes its buffers, digests and forks."""
+    want, _, _ = small_pipeline()
+    want.use_blocks(32, 3)
+    want.digest(-1)
+    side = torch.cuda.Stream()
+    pipe, _, _ = small_pipeline(side)
+    parent = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)                         # some 50 ms on the current stream
+    pipe.use_blocks(32, 3)
+    pipe.digest(-1)
+    fork = pipe.fork(parent)
+    fork.digest(-1)
+    pipe.fork(parent, into=fork)
+    torch.cuda.synchronize()
+    assert pipe.status_code() == 0 and fork.status_code() == 0
+    assert want.block_digest.any() and torch.equal(pipe.block_digest, want.block_digest) and torch.equal(pipe.block_step, want.block_step)
+    assert torch.equal(fork.block_digest, want.block_digest.flip(0)) and torch.equal(fork.block_step, want.block_step.flip(0))
+    assert (rs3.rs3_bank_read_meta(fork.bank)[0][:, 7] == rs3.rs3_bank_read_meta(want.bank)[0][:, 7]).all()
+
+
+def test_two_reads_at_once_on_two_streams(rs3):
+    """One bank read by two calls at a time, each with workspaces of its own, on streams other than the current one."""
+    b = Built(rs3, U=3, H=2, d=64, m=12, n=12, window=-1, ring_frames=12, commits=12, n_ptr=5, seed=4)
+    nb, n, n_top = b.bank.blocks(32), 140, 7
+    dig, step, _ = make_digest(b, 32)
+    rs3.rs3_bank_digest(b.bank, 32, -1, dig, step, b.st)
+    q, idx, count, group = queries(b, 2, n, [n, 77, n])
+    x = [torch.randn((3, b.mn, b.D), generator=gen(9), device="cuda").bfloat16() for _ in range(2)]
+    table = rope_table(b.mn, 64)
+
+    def buffers():
+        return dict(sel=torch.zeros((3, 2, n, n_top), dtype=torch.int32, device="cuda"), st=status(),
+                    out=torch.zeros((3, b.mn, b.D), dtype=torch.bfloat16, device="cuda"),
+                    w1=torch.empty(rs3.rs3_block_select_workspace_bytes(3, 2, n, nb), dtype=torch.uint8, device="cuda"),
+                    w2=torch.empty(rs3.rs3_sparse_readout_workspace_bytes(3, 2, 64, n, n_top, nb, "bf16"), dtype=torch.uint8, device="cuda"))
+
+    def read(o, res, rope, stream=None):
+        rs3.rs3_block_select(q, "bf16", 2, b.mn, 2, 64, group, idx, count, n, b.bank, 32, dig, step, rope, n_top, o["sel"], o["w1"],
+                             o["st"], stream)
+        rs3.rs3_sparse_readout(q, "bf16", 2, b.mn, 2, 64, group, idx, count, n, b.bank, 32, o["sel"], n_top, rope, res, o["out"], 0.0,
+                               o["w2"], o["st"], stream)
+
+    want = [buffers(), buffers()]
+    for o, res, rope in zip(want, x, (None, table)):
+        read(o, res, rope)
+    got, streams = [buffers(), buffers()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for o, res, rope, s in zip(got, x, (None, table), streams):
+            read(o, res, rope, s)
+    torch.cuda.synchronize()
+    for o, p in zip(got, want):
+        assert int(o["st"]) == 0 and int(p["st"]) == 0
+        assert torch.equal(o["sel"], p["sel"]) and torch.equal(o["out"], p["out"])
+
+
+@pytest.mark.parametrize("n", [150, 6])
+def test_captured_reads_share_workspaces(rs3, n):
+    """Two captured graphs with one set of workspaces, replayed in turn with other queries, counts and rows (sizes
+    that go by block, and by query)."""
+    b = Built(rs3, U=2, H=2, d=64, m=13, n=13, window=-1, ring_frames=12, commits=6, n_ptr=0, seed=5)
+    nb, n_top = b.bank.blocks(64), 9
+    dig, step, _ = make_digest(b, 64)
+    q, idx, count, group = queries(b, 1, n, [n, n - 3])
+    group.zero_()
+    w1 = torch.empty(rs3.rs3_block_select_workspace_bytes(2, 2, n, nb), dtype=torch.uint8, device="cuda")
+    w2 = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(2, 2, 64, n, n_top, nb, "bf16"), dtype=torch.uint8, device="cuda")
+    sel = torch.zeros((2, 2, n, n_top), dtype=torch.int32, device="cuda")
+    outs = [torch.zeros((2, b.mn, b.D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+
+    def read(out):
+        rs3.rs3_bank_digest(b.bank, 64, -1, dig, step, b.st)
+        rs3.rs3_block_select(q, "bf16", 1, b.mn, 2, 64, group, idx, count, n, b.bank, 64, dig, step, None, n_top, sel, w1, b.st)
+        rs3.rs3_sparse_readout(q, "bf16", 1, b.mn, 2, 64, group, idx, count, n, b.bank, 64, sel, n_top, None, None, out, 0.0, w2, b.st)
+
+    graphs = []
+    for out in outs:
+        read(out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            read(out)
+        graphs.append(graph)
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, generator=gen(50 + i), device="cuda"))
+        count.copy_(torch.tensor([n - i, i], dtype=torch.int32))
+        b.commit(gen(60 + i), 0)
+        want = torch.zeros_like(outs[0])
+        graphs[i % 2].replay()
+        first = sel.clone()
+        read(want)
+        live = torch.arange(n, device="cuda")[None, :] < count[:, None]
+        assert int(b.st) == 0 and torch.equal(want, outs[i % 2])
+        assert torch.equal(first.transpose(1, 2)[live], sel.transpose(1, 2)[live])
+
+
+@pytest.mark.parametrize("k_max,n_top", [(8, 5), (2, 1), (0, 3)])
+def test_read_of_many_units(rs3, k_max, n_top):
+    """More (unit, head) pairs than a CTA keeps counts of; few queries of each, none of some, or none at all."""
+    U, H, d, mn = 400, 4, 64, 16
+    bank = rs3.Bank(U, H, d, "bf16", mn, 1, -1, 64, 4, 0)
+    st, g = status(), gen(71)
+    for f in range(4):
+        k, v = (torch.randn((U, mn, H * d), generator=g, device="cuda").bfloat16() for _ in range(2))
+        rs3.rs3_bank_commit(bank, k, v, None, int(f == 0), st)
+    nb = bank.blocks(32)                                    # 80 rows: two blocks and a half
+    dig, step = torch.zeros((U, H, nb, d), dtype=torch.int8, device="cuda"), torch.zeros((U, H, nb), device="cuda")
+    rs3.rs3_bank_digest(bank, 32, -1, dig, step, st)
+    q = torch.randn((1, mn, H * d), generator=g, device="cuda").bfloat16()
+    idx = torch.stack([torch.randperm(mn, generator=g, device="cuda")[:max(k_max, 1)] for _ in range(U)]).to(torch.int32)
+    count = (torch.arange(U, device="cuda") % (k_max + 1)).to(torch.int32)
+    group = torch.zeros(U, dtype=torch.int32, device="cuda")
+    sel = torch.full((U, H, max(k_max, 1), n_top), -5, dtype=torch.int32, device="cuda")
+    x = torch.randn((U, mn, H * d), generator=g, device="cuda").bfloat16()
+    out = torch.zeros_like(x)
+    w1 = torch.empty(rs3.rs3_block_select_workspace_bytes(U, H, k_max, nb), dtype=torch.uint8, device="cuda")
+    w2 = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, nb, "bf16"), dtype=torch.uint8, device="cuda")
+    rs3.rs3_block_select(q, "bf16", 1, mn, H, d, group, idx, count, k_max, bank, 32, dig, step, None, n_top, sel, w1, st)
+    rs3.rs3_sparse_readout(q, "bf16", 1, mn, H, d, group, idx, count, k_max, bank, 32, sel, n_top, None, x, out, 0.0, w2, st)
+    assert int(st) == 0
+    kept = torch.zeros((U, mn), dtype=torch.bool, device="cuda")
+    live = torch.arange(max(k_max, 1), device="cuda")[None, :] < count[:, None]
+    kept.scatter_(1, idx.long(), live)
+    assert torch.equal(out[~kept], x[~kept]) and (sel.transpose(1, 2)[~live] == -5).all()
+    if not k_max:
+        return
+    # all 64 live rows in 64 bits: blocks 0 and 1 are live, so a query of one block reads it, of more reads both
+    K, V = (t[:, :80].double().view(U, 80, H, d) for t in (bank.k_store, bank.v_store))
+    Q = q[0].double().view(mn, H, d)[idx.long()]            # [U, k_max, H, d]
+    s = torch.einsum("ujhd,urhd->ujhr", Q, K) * d ** -0.5
+    rows = torch.arange(80, device="cuda") // 32
+    sel_ = sel.transpose(1, 2)                              # [U, k_max, H, n_top]
+    chosen = torch.stack([(sel_ == b).any(-1) for b in range(nb)], -1)
+    length = torch.tensor(rs3.rs3_bank_read_meta(bank)[0][:, 7].tolist(), device="cuda")
+    assert (length == 64).all()                             # (the rows fill the storage from its start)
+    assert (chosen[live].sum(-1) == min(n_top, 2)).all() and not chosen[..., 2][live].any()
+    s = s.masked_fill(~chosen[..., rows.clamp(max=nb - 1)] | (torch.arange(80, device="cuda") >= 64), -math.inf)
+    A = torch.einsum("ujhr,urhd->ujhd", torch.softmax(s, -1).nan_to_num(0.0), V).flatten(2)
+    size = torch.einsum("ujhr,urhd->ujhd", torch.softmax(s, -1).nan_to_num(0.0), V.abs()).flatten(2)
+    want = x.double().gather(1, idx.long()[..., None].expand(-1, -1, H * d)) + A
+    got = out.double().gather(1, idx.long()[..., None].expand(-1, -1, H * d))
+    s_abs = (torch.einsum("ujhd,urhd->ujhr", Q.abs(), K.abs()) * d ** -0.5).amax(-1)[..., None].expand(-1, -1, -1, d).flatten(2)
+    half = HALF["bf16"]                                     # (the bounds of readout_ref)
+    tol = half * want.abs() + size * (torch.expm1(2 * s_abs * 2.0 ** -24 * 300) + 300 * 2.0 ** -24 + half) * 1.01 + 1e-30
+    assert ((got - want).abs() <= tol)[live].all(), float(((got - want).abs() - tol)[live].max())
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_copy_of_more_units_than_a_cta_counts(rs3, masked):
+    U, H, d, mn = 1100, 1, 16, 8
+    a, b = (rs3.Bank(U, H, d, "f32", mn, 1, -1, 40, 5, 0) for _ in range(2))
+    st, g = status(), gen(81)
+    for f in range(4):
+        k, v = (torch.randn((U, mn, d), generator=g, device="cuda") for _ in range(2))
+        mask = (torch.rand((U, mn), generator=g, device="cuda") < 0.6).to(torch.uint8)
+        rs3.rs3_bank_commit(a, k, v, mask, int(f == 0), st)
+    meta, frames = rs3.rs3_bank_read_meta(a)
+    parent = torch.randint(-1, U, (U,), generator=g, device="cuda").to(torch.int32)
+    keep = (torch.rand((U, 33), generator=g, device="cuda") < 0.5).to(torch.uint8) if masked else None
+    ws = torch.full((rs3.rs3_bank_copy_workspace_bytes(U, 33),), 255, dtype=torch.uint8, device="cuda") if masked else None
+    rs3.rs3_bank_copy(b, a, parent, keep, ws, st)
+    assert int(st) == 0
+    got, got_frames = rs3.rs3_bank_read_meta(b)
+    for u, p in enumerate(parent.tolist()):
+        if p < 0:
+            assert got[u, 7] == 0
+            continue
+        cond, ring = int(meta[p, 2]), int(meta[p, 1] - meta[p, 0])
+        rows = list(range(cond)) + [mn + int(meta[p, 0]) + i for i in range(ring)]
+        on = [True] * len(rows) if keep is None else keep[u, :len(rows)].bool().tolist()
+        from_cond = [r for r, k in zip(rows[:cond], on[:cond]) if k]
+        from_ring = [r for r, k in zip(rows[cond:], on[cond:]) if k]
+        assert (int(got[u, 2]), int(got[u, 1])) == (len(from_cond), len(from_ring)) and got[u, 3] == meta[p, 3]
+        to = list(range(len(from_cond))) + [mn + i for i in range(len(from_ring))]
+        if u % 50 == 0:
+            assert torch.equal(b.k_store[u][to], a.k_store[p][from_cond + from_ring])
+            assert torch.equal(b.v_store[u][to], a.v_store[p][from_cond + from_ring])
