@@ -766,7 +766,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = -INFINITY, l = 0.f;
     // all of a query's loads go out together: what an entry without a block left in its place is not used
-    const int n = j < cnt ? s.n_top * w.parts : 0;
+    // (a unit whose counters are unsound has no items: nothing was computed for it)
+    const int n = j < cnt && w.n_items[u * s.H + h] > 0 ? s.n_top * w.parts : 0;
     constexpr int F = 8;                               // results in flight
     for (int t0 = part % G; t0 < n; t0 += G * F) {
         float2 ml[F];

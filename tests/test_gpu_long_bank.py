@@ -866,6 +866,36 @@ def test_sparse_readout_by_block_latches_what_the_device_finds(rs3):
         assert code == 0 and torch.equal(out, same)
 
 
+@pytest.mark.parametrize("n", [150, 10])
+def test_reads_leave_out_units_whose_counters_are_unsound(rs3, n):
+    b = Built(rs3, U=3, H=2, d=64, m=13, n=13, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
+    nb, n_top = b.bank.blocks(32), 6
+    dig, step, _ = make_digest(b, 32)
+    rs3.rs3_bank_digest(b.bank, 32, -1, dig, step, b.st)
+    q, idx, count, group = queries(b, 1, n, [n, n, n])
+    group.zero_()
+    w1 = torch.empty(rs3.rs3_block_select_workspace_bytes(3, 2, n, nb), dtype=torch.uint8, device="cuda")
+
+    def read():
+        b.st.zero_()
+        st, sel = status(), torch.full((3, 2, n, n_top), 1, dtype=torch.int32, device="cuda")
+        rs3.rs3_block_select(q, "bf16", 1, b.mn, 2, 64, group, idx, count, n, b.bank, 32, dig, step, None, n_top, sel, w1, st)
+        out = torch.zeros((3, b.mn, 128), dtype=torch.bfloat16, device="cuda")
+        run_readout(rs3, b, q, idx, count, group, sel, None, 32, 0.0, None, out, 1)
+        return int(st), int(b.st), sel, out
+
+    good = read()
+    assert good[:2] == (0, 0)
+    for word, value in ((0, -1), (1, 1 << 40), (2, -5), (6, 7)):
+        was = int(b.bank.counters[1, word])
+        b.bank.counters[1, word] = value
+        bad = read()
+        b.bank.counters[1, word] = was
+        assert bad[:2] == (rs3.RS3_EINTERNAL, rs3.RS3_EINTERNAL) and not bad[3][1].any()
+        for i in (0, 2):
+            assert torch.equal(bad[2][i], good[2][i]) and torch.equal(bad[3][i], good[3][i])
+
+
 def test_sparse_calls_latch_what_the_device_finds(rs3):
     b = Built(rs3, U=3, H=1, d=64, m=8, n=8, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
     nb = b.bank.blocks(32)
