@@ -578,12 +578,19 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int tiles = (s.k_max + TC_ROWS - 1) / TC_ROWS;
     const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles, h = blockIdx.y, u = blockIdx.z;
-    const int cnt = s.count[u], g = s.unit_group[u];
+    // the first loads go out together: the unit's counts, the counters for the last warp, a cell for the others' lanes
+    const int cnt = s.count[u], g = s.unit_group[u], j0 = tile * TC_ROWS;
+    const int parts = s.d / N, L = min(32, parts), sub = lane & (L - 1), at_once = 32 / L, row0 = warp * at_once + lane / L;
+    LiveRows rows;
+    bool sane = true;
+    int first_cell = 0;
+    if (warp == TC_THREADS / 32 - 1) sane = rows.load(s.bank, u);
+    else if (row0 < TC_ROWS && j0 + row0 < s.k_max) first_cell = __ldg(s.idx + (int64_t)u * s.k_max + j0 + row0);
     if (cnt < 0 || cnt > s.k_max || g < 0 || g >= s.G) {
         if (threadIdx.x == 0) latch_status(s.status, RS3_EINVAL);
         return;
     }
-    const int j0 = tile * TC_ROWS, nq = min(TC_ROWS, cnt - j0);
+    const int nq = min(TC_ROWS, cnt - j0);
     if (nq <= 0) return;
     const int stride = p.piece + 8;                                        // of a query's scores
     float *s_score = reinterpret_cast<float *>(smem);
@@ -593,8 +600,6 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     const int64_t dig = ((int64_t)u * s.H + h) * s.nb;
     if (warp == TC_THREADS / 32 - 1) {
         // the piece's words and the live blocks of each, a word per lane
-        LiveRows rows;
-        const bool sane = rows.load(s.bank, u);
         if (!sane && lane == 0) latch_status(s.status, RS3_EINTERNAL);
         const LiveWords words(rows, s.bs);
         const int per = piece_words(p, words.total);
@@ -609,17 +614,11 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             s_size[1] = words.total > per;
             if (p.splits > 1 && tile == 0 && split == 0 && h == 0) p.n_pieces[u] = sane ? (words.total + per - 1) / per : 0;
         }
-        __syncwarp();
-        for (int i = 0; i < n; ++i) {
-            const bool live = s_live[i] >> lane & 1u;
-            s_step[32 * i + lane] = live ? __ldg(p.a.step + dig + 32 * s_word[i] + lane) : __int_as_float(0x7fffffff);
-        }
     } else {
         // the queries in 8 bits, held as fp16: a group of lanes per query, 16 bytes (up to two) each
-        const int parts = s.d / N, L = min(32, parts), sub = lane & (L - 1), at_once = 32 / L;
         for (int r0 = warp * at_once; r0 < TC_ROWS; r0 += (TC_THREADS / 32 - 1) * at_once) {
             const int row = r0 + lane / L;                                 // rows past the tile: none of the lanes' groups writes
-            const int cell = row < nq ? s.idx[(int64_t)u * s.k_max + j0 + row] : 0;
+            const int cell = row == row0 ? first_cell : row < nq ? s.idx[(int64_t)u * s.k_max + j0 + row] : 0;
             const bool ok = row < nq && cell >= 0 && cell < s.mn;
             if (row < nq && !ok && sub == 0) latch_status(s.status, RS3_EINVAL);
             float x[2][N], m = 0.f;
@@ -678,9 +677,9 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
     if (s_size[0] < 0) return;
     const int n = 32 * s_size[0];                                          // places: blocks of the words, 32 each
     const bool alone = !s_size[1];
-    // this warp's steps: 16 places, then 64 columns after 64; a step's digests are loaded one step ahead
+    // this warp's steps: 16 places, then 64 columns after 64; a step's digests are loaded two steps ahead
     int b0 = warp * 16, k0 = 0;
-    uint4 w[2];
+    uint4 w[2], w1[2];
     const uint8_t *digests = reinterpret_cast<const uint8_t *>(p.a.digest) + (dig * s.d + r * s.d + 16 * t);
     const auto load_step = [&](uint4 (&v)[2], int place, int k) {
         const int first = place < n ? s_word[place >> 5] * 32 + (place & 31) : s.nb;
@@ -690,7 +689,31 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
             if (first + 8 * x + r < s.nb && k + 16 * t < s.d) v[x] = __ldg(reinterpret_cast<const uint4 *>(digests + (int64_t)(first + 8 * x) * s.d + k));
         }
     };
+    const auto next_step = [&](int &b, int &k) {
+        const bool more = k + 64 < width;
+        b += more ? 0 : TC_THREADS / 2;
+        k = more ? k + 64 : 0;
+    };
     load_step(w, b0, k0);
+    int b1 = b0, k1 = k0;
+    next_step(b1, k1);
+    load_step(w1, b1, k1);
+    {
+        // its places' steps: 16 after 128, four to a lane
+        float f[TC_BLOCKS / 256 + 1];
+#pragma unroll
+        for (int i = 0; i < TC_BLOCKS / 256 + 1; ++i) {
+            const int place = b0 + 256 * i + 128 * (lane >> 4) + (lane & 15);
+            f[i] = place < n && (s_live[place >> 5] >> (place & 31) & 1u)
+                       ? __ldg(p.a.step + dig + 32 * s_word[place >> 5] + (place & 31)) : __int_as_float(0x7fffffff);
+        }
+#pragma unroll
+        for (int i = 0; i < TC_BLOCKS / 256 + 1; ++i) {
+            const int place = b0 + 256 * i + 128 * (lane >> 4) + (lane & 15);
+            if (place < n) s_step[place] = f[i];
+        }
+        __syncwarp();
+    }
     float c[2][4];
     while (b0 < n) {
         if (k0 == 0) {
@@ -699,9 +722,10 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) c[x][y] = 0.f;
         }
-        const int b1 = k0 + 64 < width ? b0 : b0 + TC_THREADS / 2, k1 = k0 + 64 < width ? k0 + 64 : 0;
-        uint4 w1[2];
-        load_step(w1, b1, k1);
+        int b2 = b1, k2 = k1;
+        next_step(b2, k2);
+        uint4 w2[2];
+        load_step(w2, b2, k2);
         const uint8_t *qa = s_q + r * q_row + 2 * (k0 + 16 * t);
         uint4 qv[2][2];
 #pragma unroll
@@ -732,8 +756,13 @@ __global__ void __launch_bounds__(TC_THREADS, 3) k_score_blocks(PickArgs p)
         }
         b0 = b1;
         k0 = k1;
-        w[0] = w1[0];
-        w[1] = w1[1];
+        b1 = b2;
+        k1 = k2;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            w[x] = w1[x];
+            w1[x] = w2[x];
+        }
     }
     __syncthreads();
     // a warp per query, a lane per word: blocks ascend with the lanes
