@@ -6,8 +6,7 @@
 // a power of two: exact, hence the same whatever order they are summed in.
 #include "rs3_sparse.cuh"
 
-#include "rs3_tc_host.cuh"
-#include "rs3_tc_ptx.cuh"
+#include "rs3_blocks_tma.cuh"
 
 #include <cfloat>
 

@@ -9,9 +9,8 @@
 //              partial results of a query's blocks are joined by their log-sum-exp (k_join_blocks)
 #include "rs3_sparse.cuh"
 
+#include "rs3_blocks_tma.cuh"
 #include "rs3_cluster.cuh"
-#include "rs3_tc_host.cuh"
-#include "rs3_tc_ptx.cuh"
 
 #include <cmath>
 
@@ -285,7 +284,9 @@ struct BlockWork {                         // in the workspace
 // tells every CTA where its entries of the block go.  Entries of one block come in any order; each
 // is computed by itself, so the result does not depend on it.  Out of place the launch's other CTAs
 // write out = residual (or zeros) on every cell, and with angles a further few rotate the kept queries once for all
-// of their blocks (in fp32, rounded to bf16 for the tensor cores).
+// of their blocks (in fp32, rounded to bf16 for the tensor cores).  Bound by latency: three cluster barriers and some
+// six dependent loads, 13 us for one head's 24 200 entries over 4 700 blocks and 16 for 32 heads' 379 000 over 990 with
+// 17 MB passed through; with every CTA going through all of a head's entries for its share of the blocks 18 and 22.
 __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
@@ -486,7 +487,10 @@ struct BlockTile {
 // are taken in the order in which adjacent lanes can load 16 bytes of a row), the softmax of its rows in
 // registers, O = P V from those, and (m, l, O) stored for k_join_blocks.  No warp waits for another.
 // mma.sync: a block of a long bank has some 20 queries, so the call is bound by the bytes of K and V, and
-// tiles of 128 rows would be four fifths empty.
+// tiles of 128 rows would be four fifths empty.  23 700 queries of 16 blocks in 32 heads of 64 (18 500 blocks, 303 MB read
+// and 97 MB of results): 75 us, 5.3 TB/s; the loads alone take 60.  757 queries of 32 blocks, one head of 256 (78 MB): 28 us,
+// 21 of them the loads with their start and end.  Seven warps and the producer leave 128 registers (255 at D = 256)
+// where eight and it left 96.
 template <int D, int TR>
 __global__ void __launch_bounds__(BlockTile<D, TR>::THREADS, BlockTile<D, TR>::CTAS)
 k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
@@ -562,7 +566,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
             __syncthreads();
             if (warp == X::CONSUMERS) {
                 if (lane == 0) {
-                    const uint64_t once = l2_once();
+                    const uint64_t once = l2_once();   // L2 keeps the results for k_join_blocks (21 -> 18.5 us there)
                     uint32_t k = cnt;
                     for (int i = 0; i < chunk; ++i, ++k) {
                         const uint32_t st = k % X::STAGES;
@@ -884,9 +888,10 @@ rs3_status launch_attend(const AttendArgs &a, const BlockWork &w, cudaStream_t s
     if (r != RS3_OK) return r;
     CUtensorMap mk, mv;
     const int64_t rows = a.s.U * a.s.bank.rows_per_unit, width = (int64_t)a.s.H * D;
-    // a head of 64 is 128 bytes of a row: no more is fetched of its neighbour, whose turn comes later
+    // a head of 64 is 128 bytes of a row: no more is fetched of its neighbour, whose turn comes later (78 -> 74 us)
     const CUtensorMapL2promotion grain = D == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
-    if (!tc::make_kv_map(&mk, a.k_store, width, rows, TR, grain) || !tc::make_kv_map(&mv, a.v_store, width, rows, TR, grain))
+    if (!tc::make_rows_map(&mk, a.k_store, 2, width, rows, 64, TR, true, grain) ||
+        !tc::make_rows_map(&mv, a.v_store, 2, width, rows, 64, TR, true, grain))
         return RS3_ECUDA;
     launch_pdl(k_attend_blocks<D, TR>, dim3((unsigned)(rs3_sm_count() * X::CTAS)), dim3(X::THREADS), X::SMEM, st, a, w, mk, mv);
     return RS3_OK;

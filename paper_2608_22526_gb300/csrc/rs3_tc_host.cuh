@@ -21,8 +21,7 @@ inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
     return fn;
 }
 
-inline bool make_kv_map(CUtensorMap *m, const void *store, int64_t D, int64_t rows, int box_rows,
-                        CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B)
+inline bool make_kv_map(CUtensorMap *m, const void *store, int64_t D, int64_t rows, int box_rows)
 {
     PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
     if (!enc) return false;
@@ -31,22 +30,7 @@ inline bool make_kv_map(CUtensorMap *m, const void *store, int64_t D, int64_t ro
     const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     const cuuint32_t es[2] = {1, 1};
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(store), dims, strides, box, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promotion,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// A tensor map of `rows` rows of D elements (2 bytes: bf16, 4: fp32) whose copies are `box_rows` rows of
-// `cols` columns as they lie.
-inline bool make_rows_map(CUtensorMap *m, const void *store, int elem_bytes, int64_t D, int64_t rows, int cols, int box_rows)
-{
-    PFN_cuTensorMapEncodeTiled_v12000 enc = encode_fn();
-    if (!enc) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)D * (cuuint64_t)elem_bytes};
-    const cuuint32_t box[2] = {(cuuint32_t)cols, (cuuint32_t)box_rows};
-    const cuuint32_t es[2] = {1, 1};
-    return enc(m, elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(store),
-               dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
