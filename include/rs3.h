@@ -372,8 +372,8 @@ rs3_status rs3_memory_readout(const void *q, rs3_dtype dtype, int G, int mn, int
                               rs3_stream_t stream);
 
 /*
- * Time limit of every wait inside the readout kernels launched after this
- * call, in nanoseconds of the GPU's global timer (default 1000000000, one
+ * Time limit of every wait inside the readout, digest and block-selection
+ * kernels launched after this call, in nanoseconds of the GPU's global timer (default 1000000000, one
  * second; 0 gives up at the first wait whose condition does not already
  * hold).  A kernel whose wait runs out stops issuing work, lets its copies
  * and matrix operations in flight complete, frees its tensor memory, latches
@@ -467,7 +467,8 @@ int64_t rs3_bank_blocks(const rs3_bank *bank, int block);
  * A block without live rows that is visited gets zeros.  The sums are fp32 in one
  * fixed order: partial sum p (0..7) takes rows p, p+8, ... of the block ascending,
  * then ((0+4)+(2+6)) + ((1+5)+(3+7)), divided by the number of live rows.
- * d: a power of two in [16, 256] (else RS3_EUNSUPPORTED).
+ * d: a power of two in [16, 256], U * rows_per_unit < 2^31 - 256 (else
+ * RS3_EUNSUPPORTED).  RS3_ETIMEOUT as for the readout (rs3_set_wait_limit_ns).
  */
 rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refresh, int8_t *digest,
                            float *step, int32_t *status, rs3_stream_t stream);
@@ -491,9 +492,10 @@ size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int n_blocks);
  *   workspace device, >= rs3_block_select_workspace_bytes(U, H, k_max, blocks)
  *         bytes, 16-byte aligned; one call at a time
  * Limits: d a power of two in [16, 256], n_top <= 1024, k_max <= mn, at most 49152
- * blocks per unit, else RS3_EUNSUPPORTED (RS3_EINVAL for k_max).  A unit with a
- * count outside [0, k_max] or a group outside [0, G) latches RS3_EINVAL and is
- * skipped; a cell outside [0, mn) latches it and that query gets some blocks.
+ * blocks per unit, else RS3_EUNSUPPORTED (RS3_EINVAL for k_max); block means below
+ * 2^111, so that no score passes the largest fp32 number.  A unit with a count * outside [0, k_max] or a group outside [0, G) latches RS3_EINVAL and is skipped; a
+ * cell outside [0, mn) latches it and that query gets some blocks.  RS3_ETIMEOUT as
+ * for the readout (rs3_set_wait_limit_ns).
  */
 rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
                             const int32_t *unit_group, const int32_t *idx, const int32_t *count,
@@ -517,7 +519,11 @@ size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_
  * skipped, a count outside [0, k_max] latches it and the unit is skipped.
  *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, 16-byte
  *         aligned; one call at a time
- * Limits: those of rs3_block_select, without one on the blocks.
+ * bf16 calls with many queries go block by block on the tensor cores: the softmax's
+ * weights are then rounded to bf16, and a query that is rotated here is too (a
+ * query rotated before, by rs3_qk_norm_rope, has been rounded already).
+ * Limits: those of rs3_block_select, without one on the blocks.  RS3_ETIMEOUT as for
+ * the readout (rs3_set_wait_limit_ns).
  */
 rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
                               const int32_t *unit_group, const int32_t *idx, const int32_t *count,
