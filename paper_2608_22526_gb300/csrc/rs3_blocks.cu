@@ -1159,70 +1159,58 @@ __global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
         const T *grid = static_cast<const T *>(s.q) + (int64_t)g * s.mn * (s.H * s.d) + h * s.d;
         constexpr int F = 4;
         for (int r0 = 0; r0 < 16; r0 += F * at_once) {
-            uint4 v[F][1];
-            float4 f[F][1][N / 4];
-            int cells[F];
+            uint4 v[F];
+            float4 f[F][N / 4];
 #pragma unroll
             for (int x = 0; x < F; ++x) {
                 const int row = r0 + x * at_once + lane / L, cell = __shfl_sync(0xffffffffu, my_cell, row & 15);
-                cells[x] = row < 16 && cell >= 0 && cell < s.mn ? cell : -1;
+                v[x] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 1; ++i) {
-                    const int c = sub + 32 * i;            // its piece of the row
-                    v[x][i] = make_uint4(0, 0, 0, 0);
+                for (int e = 0; e < N / 4; ++e) f[x][e] = make_float4(1.f, 0.f, 1.f, 0.f);
+                if (row >= 16 || cell < 0 || cell >= s.mn) continue;
+                v[x] = __ldg(reinterpret_cast<const uint4 *>(grid + (int64_t)cell * (s.H * s.d)) + sub);
+                if (s.rope)
 #pragma unroll
-                    for (int e = 0; e < N / 4; ++e) f[x][i][e] = make_float4(1.f, 0.f, 1.f, 0.f);
-                    if (i * 32 >= parts || cells[x] < 0) continue;
-                    v[x][i] = __ldg(reinterpret_cast<const uint4 *>(grid + (int64_t)cells[x] * (s.H * s.d)) + c);
-                    if (s.rope)
-#pragma unroll
-                        for (int e = 0; e < N / 4; ++e) f[x][i][e] = __ldg(reinterpret_cast<const float4 *>(s.rope + (int64_t)cells[x] * s.d + c * N) + e);
-                }
+                    for (int e = 0; e < N / 4; ++e) f[x][e] = __ldg(reinterpret_cast<const float4 *>(s.rope + (int64_t)cell * s.d + sub * N) + e);
             }
 #pragma unroll
             for (int x = 0; x < F; ++x) {
                 const int row = r0 + x * at_once + lane / L;
-                float z[1][N], m = 0.f;
+                const uint32_t y[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+                float z[N], m = 0.f;
 #pragma unroll
-                for (int i = 0; i < 1; ++i) {
-                    const uint32_t y[4] = {v[x][i].x, v[x][i].y, v[x][i].z, v[x][i].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (N == 8) {
-                            z[i][2 * e] = __uint_as_float(y[e] << 16);
-                            z[i][2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
-                        } else {
-                            z[i][e] = __uint_as_float(y[e]);
-                        }
+                for (int e = 0; e < 4; ++e) {
+                    if (N == 8) {
+                        z[2 * e] = __uint_as_float(y[e] << 16);
+                        z[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
+                    } else {
+                        z[e] = __uint_as_float(y[e]);
                     }
-                    if (s.rope) {                          // each product and each sum rounded
-#pragma unroll
-                        for (int e = 0; e < N; e += 4) {
-                            const float4 t = f[x][i][e / 4];
-                            const float x0 = z[i][e], x1 = z[i][e + 1], x2 = z[i][e + 2], x3 = z[i][e + 3];
-                            z[i][e] = __fsub_rn(__fmul_rn(x0, t.x), __fmul_rn(x1, t.y));
-                            z[i][e + 1] = __fadd_rn(__fmul_rn(x0, t.y), __fmul_rn(x1, t.x));
-                            z[i][e + 2] = __fsub_rn(__fmul_rn(x2, t.z), __fmul_rn(x3, t.w));
-                            z[i][e + 3] = __fadd_rn(__fmul_rn(x2, t.w), __fmul_rn(x3, t.z));
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(z[i][e]));
                 }
+                if (s.rope) {                              // each product and each sum rounded
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        const float4 t = f[x][e / 4];
+                        const float x0 = z[e], x1 = z[e + 1], x2 = z[e + 2], x3 = z[e + 3];
+                        z[e] = __fsub_rn(__fmul_rn(x0, t.x), __fmul_rn(x1, t.y));
+                        z[e + 1] = __fadd_rn(__fmul_rn(x0, t.y), __fmul_rn(x1, t.x));
+                        z[e + 2] = __fsub_rn(__fmul_rn(x2, t.z), __fmul_rn(x3, t.w));
+                        z[e + 3] = __fadd_rn(__fmul_rn(x2, t.w), __fmul_rn(x3, t.z));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(z[e]));
                 for (int o = L >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
                 const EightBits bits(m);
+                if (row >= 16) continue;
+                uint32_t w[N / 2];
 #pragma unroll
-                for (int i = 0; i < 1; ++i) {
-                    if (i * 32 >= parts || row >= 16) continue;
-                    uint32_t w[N / 2];
-#pragma unroll
-                    for (int e = 0; e < N; e += 2)
-                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[e / 2]) : "f"((float)bits(z[i][e + 1])), "f"((float)bits(z[i][e])));
-                    const int c = sub + 32 * i;            // N fp16 columns: a chunk of 8, or half of one
-                    uint8_t *to = smem + sw128_offset(TILE_ROWS, first + row, c * N / 8) + (N == 8 ? 0 : (c & 1) * 8);
-                    if (N == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]);
-                    else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-                }
+                for (int e = 0; e < N; e += 2)
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[e / 2]) : "f"((float)bits(z[e + 1])), "f"((float)bits(z[e])));
+                // N fp16 columns: a chunk of 8, or half of one
+                uint8_t *to = smem + sw128_offset(TILE_ROWS, first + row, sub * N / 8) + (N == 8 ? 0 : (sub & 1) * 8);
+                if (N == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[N / 2 - 2], w[N / 2 - 1]);
+                else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
             }
         }
         fence_proxy_async();
