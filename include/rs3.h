@@ -519,8 +519,8 @@ size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_
  * skipped, a count outside [0, k_max] latches it and the unit is skipped.
  *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, 16-byte
  *         aligned; one call at a time
- * bf16 calls with many queries go block by block on the tensor cores: the softmax's
- * weights are then rounded to bf16, and a query that is rotated here is too (a
+ * Calls with many queries go block by block, in bf16 on the tensor cores: there the
+ * softmax's weights are rounded to bf16, and a query that is rotated here is too (a
  * query rotated before, by rs3_qk_norm_rope, has been rounded already).
  * Limits: those of rs3_block_select, without one on the blocks.  RS3_ETIMEOUT as for
  * the readout (rs3_set_wait_limit_ns).

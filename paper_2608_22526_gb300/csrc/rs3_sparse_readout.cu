@@ -2,11 +2,12 @@
 // back to the grid (Sec. 3.1's readout, Eq. 6 and Eq. 7, over chosen blocks of the bank).
 //
 // Two paths (by_blocks() holds the rule):
-//   by query   a CTA per (query, head) reads the blocks of its list: few queries, fp32, narrow heads
+//   by query   a CTA per (query, head) reads the blocks of its list: few queries, narrow heads
 //   by block   a block that many queries chose is read once for all of them: the lists are turned
-//              into lists of queries per block (k_block_lists), a CTA per (block, up to 64 queries)
-//              computes their attention over the block on the tensor cores (k_attend_blocks), and the
-//              partial results of a query's blocks are joined by their log-sum-exp (k_join_blocks)
+//              into lists of queries per block (k_block_lists), a block and up to 64 of its queries make
+//              an item, whose attention is computed on the tensor cores (k_attend_blocks; fp32 on the CUDA
+//              cores, k_attend_blocks_fp32), and the partial results of a query's blocks are joined by
+//              their log-sum-exp (k_join_blocks)
 #include "rs3_sparse.cuh"
 
 #include "rs3_blocks_tma.cuh"
@@ -250,7 +251,7 @@ GatherKernel gather_kernel(int pieces)         // a power of two: of 2 (bf16) or
 // ---------------------------------------------------------------------------
 // by block
 // ---------------------------------------------------------------------------
-constexpr int TILE = 64;                   // queries of an item
+constexpr int TILE = 64, TILE_FP32 = 32;   // queries of an item: four tiles of 16, or eight warps' four each
 constexpr int LIST_THREADS = 512;
 constexpr int LIST_HELD = 8;               // list entries that a thread holds
 constexpr int LIST_BINS = 8192;            // blocks that are counted at a time
@@ -258,9 +259,9 @@ constexpr int LIST_CTAS = 8;               // largest cluster of a (unit, head)
 constexpr int MAX_HEADS = 1024;            // (unit, head) pairs whose item counts a CTA of the attention holds at a time
 constexpr int CHUNK_ITEMS = 64;            // items whose records it holds
 
-// Part of a block (its 32 or 64 rows, half of its 128) and up to TILE of the queries that chose it.
+// Part of a block (part_rows() of its rows) and up to TILE (TILE_FP32) of the queries that chose it.
 struct BlockItem {
-    int32_t uh, part, first, n;            // unit * H + head, storage rows / rows of a part, first list entry, entries
+    int32_t uh, part, first, n;            // unit * H + head, its rows in parts, first list entry, entries
     uint32_t live[2];                      // its live rows
     int64_t q;                             // element of its unit's and head's first query row (k_attend_blocks)
 };
@@ -272,11 +273,26 @@ struct BlockWork {                         // in the workspace
     uint4 *q;                              // [U][k_max][H * d]: the kept queries, rotated (calls with angles)
     float2 *ml;                            // [U * H][k_max][n_top][parts]: (max in the log2 domain, sum)
     float *o;                              // [U * H][k_max][n_top][parts][d]
-    int32_t cluster, bins, parts, list_ctas, pass_ctas;
+    int32_t cluster, bins, parts, parts_log2, tile, tile_log2, list_ctas, pass_ctas;
     int64_t max_items;
     uint64_t wait_ns;                      // limit of each wait
     uint32_t per_top, per_top_shift;       // x / n_top = x * per_top >> per_top_shift for x < 2^28
 };
+
+// 16 bytes of a query, rotated.
+template <typename T>
+__device__ __forceinline__ uint4 rotate_piece(uint4 v, const float *f)
+{
+    if (sizeof(T) == 2) return rotate_q_piece(v, f);
+    const float4 c = __ldg(reinterpret_cast<const float4 *>(f));
+    float x[4], y[4];
+    Row<float>::widen(v, x);
+    y[0] = x[0] * c.x - x[1] * c.y;
+    y[1] = x[0] * c.y + x[1] * c.x;
+    y[2] = x[2] * c.z - x[3] * c.w;
+    y[3] = x[2] * c.w + x[3] * c.z;
+    return Row<float>::narrow(y);
+}
 
 // The queries of every block, a counting sort: the CTAs of a cluster share the list entries of one (unit, head).
 // Each counts its entries per block in shared memory; then each owns some of the blocks, adds up their counts
@@ -284,9 +300,10 @@ struct BlockWork {                         // in the workspace
 // tells every CTA where its entries of the block go.  Entries of one block come in any order; each
 // is computed by itself, so the result does not depend on it.  Out of place the launch's other CTAs
 // write out = residual (or zeros) on every cell, and with angles a further few rotate the kept queries once for all
-// of their blocks (in fp32, rounded to bf16 for the tensor cores).  Bound by latency: three cluster barriers and some
+// of their blocks (in fp32; bf16 queries rounded to bf16 for the tensor cores).  Bound by latency: three cluster barriers and some
 // six dependent loads, 13 us for one head's 24 200 entries over 4 700 blocks and 16 for 32 heads' 379 000 over 990 with
 // 17 MB passed through; with every CTA going through all of a head's entries for its share of the blocks 18 and 22.
+template <typename T>
 __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
 {
     pdl_wait();
@@ -308,7 +325,8 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
         }
         const SparseArgs &s = a.s;
         if (!s.rope) return;                           // (the grid is whole clusters)
-        const int width = s.H * s.d / 8;               // 16-byte pieces of a query row
+        constexpr int N = Row<T>::N;
+        const int width = s.H * s.d / N;               // 16-byte pieces of a query row
         const int64_t i = first - pass;
         const int u = (int)(i / ((int64_t)s.k_max * width)), r = (int)(i - (int64_t)u * s.k_max * width), j = r / width, c = r - j * width;
         if (u >= s.U) return;
@@ -316,8 +334,8 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
         if (cnt > s.k_max || j >= cnt || g < 0 || g >= s.G) return;
         const int cell = s.idx[(int64_t)u * s.k_max + j];
         if (cell < 0 || cell >= s.mn) return;
-        w.q[i] = rotate_q_piece(__ldg(static_cast<const uint4 *>(s.q) + ((int64_t)g * s.mn + cell) * width + c),
-                                s.rope + (int64_t)cell * s.d + (c * 8 & (s.d - 1)));
+        const uint4 x = __ldg(static_cast<const uint4 *>(s.q) + ((int64_t)g * s.mn + cell) * width + c);
+        w.q[i] = rotate_piece<T>(x, s.rope + (int64_t)cell * s.d + (c * N & (s.d - 1)));
         return;
     }
     extern __shared__ int32_t s_bin[];                 // [bins] counts, then next places
@@ -387,7 +405,7 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
         for (int b = b0; b < b1; ++b) {
             const int n = counts(b);
             entries += n;
-            items += (n + TILE - 1) / TILE;
+            items += (n + w.tile - 1) >> w.tile_log2;
         }
         int e_sum = entries, i_sum = items;
 #pragma unroll
@@ -432,9 +450,9 @@ __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, B
                 const uint64_t live = rows.mask64((int64_t)it.part * pr);
                 it.live[0] = (uint32_t)live;
                 it.live[1] = pr > 32 ? (uint32_t)(live >> 32) : 0u;
-                for (int e = from; e < next; e += TILE) {
+                for (int e = from; e < next; e += w.tile) {
                     it.first = e;
-                    it.n = min(TILE, next - e);
+                    it.n = min(w.tile, next - e);
                     *out++ = it;
                 }
             }
@@ -744,6 +762,199 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
     }
 }
 
+// The same in fp32 on the CUDA cores.  A CTA brings a part's rows into shared memory and its warps take its queries, four
+// each: a lane holds the scores of a row (of two, where a part has 64), so that a key read once serves four queries, then
+// the columns that it adds up, a value read once for the four.  Four CTAs per SM (heads of 64) load while others compute.
+// Bound by the latency of an item (its load, its scores, its sums) and next by shared-memory reads.  9 500 queries of 16
+// blocks in 16 heads of 64: the call takes 206 us, by query 617; four warps with up to sixteen queries each 260, eight queries
+// to a warp 237.
+template <int D, int PR>
+struct Fp32Tile {
+    static constexpr int WARPS = 8, THREADS = 32 * WARPS, QUERIES = 4, PITCH = D + 4;     // floats of a key row: lanes meet different banks
+    static constexpr int KEYS = PR * PITCH, VALUES = PR * D, Q = QUERIES * D, P = PR * QUERIES;
+    static constexpr int SMEM = (KEYS + VALUES + WARPS * (Q + P)) * 4;
+};
+
+template <int D, int PR>
+__global__ void __launch_bounds__(Fp32Tile<D, PR>::THREADS) k_attend_blocks_fp32(AttendArgs a, BlockWork w)
+{
+    using X = Fp32Tile<D, PR>;
+    constexpr int M = X::QUERIES, S = PR / 32, V4 = D < 128 ? 1 : D / 128;      // score rows, column groups of a lane
+    extern __shared__ __align__(16) float s_mem[];
+    __shared__ int32_t s_first[MAX_HEADS + 1];
+    pdl_wait();
+    const SparseArgs &s = a.s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float *s_k = s_mem, *s_v = s_k + X::KEYS, *s_q = s_v + X::VALUES + warp * (X::Q + X::P), *s_p = s_q + X::Q;
+    const float *Q = s.rope ? reinterpret_cast<const float *>(w.q) : static_cast<const float *>(s.q);
+    const int heads = s.U * s.H;
+    const int64_t row_elems = (int64_t)s.H * D;
+    int next = blockIdx.x;
+    for (int g0 = 0; g0 < heads; g0 += MAX_HEADS) {
+        const int n = min(MAX_HEADS, heads - g0);
+        __syncthreads();
+        if (warp == 0) {                               // items before each (unit, head)
+            int run = 0;
+            for (int c0 = 0; c0 < n; c0 += 32) {
+                int v = c0 + lane < n ? w.n_items[g0 + c0 + lane] : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += t;
+                }
+                if (c0 + lane < n) s_first[c0 + lane + 1] = run + v;
+                run += __shfl_sync(0xffffffffu, v, 31);
+            }
+            if (lane == 0) s_first[0] = 0;
+        }
+        __syncthreads();
+        const int total = s_first[n];
+        for (; next < total; next += gridDim.x) {
+            int x = 0, y = n;                          // the last one whose items begin at or before `next`
+            while (y - x > 1) {
+                const int mid = (x + y) >> 1;
+                if (s_first[mid] <= next) x = mid; else y = mid;
+            }
+            const BlockItem it = w.items[(g0 + x) * w.max_items + (next - s_first[x])];
+            const int u = it.uh / s.H, h = it.uh - u * s.H;
+            const float *K = reinterpret_cast<const float *>(a.k_store) + (u * s.bank.rows_per_unit) * row_elems + h * D;
+            const float *V = reinterpret_cast<const float *>(a.v_store) + (u * s.bank.rows_per_unit) * row_elems + h * D;
+            const uint64_t live = (uint64_t)it.live[1] << 32 | it.live[0];
+            // dead rows may hold anything, or lie past the storage: they are zeros, and nothing is read
+            for (int i = threadIdx.x; i < PR * (D / 4); i += X::THREADS) {
+                const int r = i / (D / 4), c = 4 * (i % (D / 4)), bytes = (live >> r & 1u) ? 16 : 0;
+                const int64_t at = bytes ? ((int64_t)it.part * PR + r) * row_elems + c : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"((uint32_t)__cvta_generic_to_shared(s_k + r * X::PITCH + c)), "l"(K + at), "r"(bytes) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"((uint32_t)__cvta_generic_to_shared(s_v + r * D + c)), "l"(V + at), "r"(bytes) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            const float *q_rows = Q + ((s.rope ? (int64_t)u * s.k_max : (int64_t)__ldg(s.unit_group + u) * s.mn) * s.H + h) * D;
+            const int2 *list = w.list + (int64_t)it.uh * s.k_max * s.n_top + it.first;
+            int2 entry = make_int2(-1, -1);            // of the warp's four queries: lane i's the i-th
+            const auto load_q = [&](int q0) {
+                entry = make_int2(-1, -1);
+                if (lane < M && q0 + lane < it.n) entry = __ldg(list + q0 + lane);
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    const int row = __shfl_sync(0xffffffffu, entry.y, i);
+#pragma unroll
+                    for (int c = 4 * lane; c < D; c += 128)
+                        *reinterpret_cast<float4 *>(s_q + i * D + c) =
+                            row >= 0 ? __ldg(reinterpret_cast<const float4 *>(q_rows + row * row_elems + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                __syncwarp();
+            };
+            if (M * warp < it.n) load_q(M * warp);
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();
+            for (int q0 = M * warp; q0 < it.n; q0 += M * X::WARPS) {
+                if (q0 != M * warp) load_q(q0);
+                float c[S][M];
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+#pragma unroll
+                    for (int q = 0; q < M; ++q) c[i][q] = 0.f;
+#pragma unroll 4
+                for (int e = 0; e < D; e += 4) {
+                    float4 k[S];
+#pragma unroll
+                    for (int i = 0; i < S; ++i) k[i] = *reinterpret_cast<const float4 *>(s_k + (32 * i + lane) * X::PITCH + e);
+#pragma unroll
+                    for (int q = 0; q < M; ++q) {
+                        const float4 z = *reinterpret_cast<const float4 *>(s_q + q * D + e);
+#pragma unroll
+                        for (int i = 0; i < S; ++i)
+                            c[i][q] = fmaf(z.w, k[i].w, fmaf(z.z, k[i].z, fmaf(z.y, k[i].y, fmaf(z.x, k[i].x, c[i][q]))));
+                    }
+                }
+                float mx[M], sum[M];
+#pragma unroll
+                for (int q = 0; q < M; ++q) {
+                    mx[q] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < S; ++i) {
+                        if (!(live >> (32 * i + lane) & 1u)) c[i][q] = -INFINITY;
+                        mx[q] = fmaxf(mx[q], c[i][q]);
+                    }
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                    for (int q = 0; q < M; ++q) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xffffffffu, mx[q], o));
+#pragma unroll
+                for (int q = 0; q < M; ++q) {
+                    mx[q] *= a.scale_log2;
+                    const float ref = mx[q] == -INFINITY ? 0.f : -mx[q];
+                    sum[q] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < S; ++i) {
+                        c[i][q] = exp2f(fmaf(c[i][q], a.scale_log2, ref));
+                        sum[q] += c[i][q];
+                    }
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                    for (int q = 0; q < M; ++q) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
+#pragma unroll
+                for (int i = 0; i < S; ++i)
+#pragma unroll
+                    for (int q = 0; q < M; q += 4)
+                        *reinterpret_cast<float4 *>(s_p + (32 * i + lane) * M + q) = make_float4(c[i][q], c[i][q + 1], c[i][q + 2], c[i][q + 3]);
+                __syncwarp();
+                // columns 4 lane, 128 + 4 lane, ... (heads of 64: 2 lane)
+                constexpr int COLS = D < 128 ? 2 : 4;
+                float o[M][V4][COLS];
+#pragma unroll
+                for (int q = 0; q < M; ++q)
+#pragma unroll
+                    for (int v = 0; v < V4; ++v)
+#pragma unroll
+                        for (int e = 0; e < COLS; ++e) o[q][v][e] = 0.f;
+#pragma unroll 4
+                for (int r = 0; r < PR; ++r) {
+                    float pq[M];
+#pragma unroll
+                    for (int q = 0; q < M; q += 4) {
+                        const float4 p = *reinterpret_cast<const float4 *>(s_p + r * M + q);
+                        pq[q] = p.x; pq[q + 1] = p.y; pq[q + 2] = p.z; pq[q + 3] = p.w;
+                    }
+#pragma unroll
+                    for (int v = 0; v < V4; ++v) {
+                        const float *at = s_v + r * D + 128 * v + COLS * lane;
+                        float4 f;
+                        if (COLS == 4) f = *reinterpret_cast<const float4 *>(at);
+                        else f = make_float4(at[0], at[1], 0.f, 0.f);
+                        const float y[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                        for (int q = 0; q < M; ++q)
+#pragma unroll
+                            for (int e = 0; e < COLS; ++e) o[q][v][e] = fmaf(pq[q], y[e], o[q][v][e]);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < M; ++q) {
+                    const int e = __shfl_sync(0xffffffffu, entry.x, q);
+                    if (e < 0) continue;               // (the same for the warp)
+                    const int64_t slot = ((int64_t)it.uh * s.k_max * s.n_top + e) * w.parts + it.part % w.parts;
+                    if (lane == 0) w.ml[slot] = make_float2(mx[q], sum[q]);
+#pragma unroll
+                    for (int v = 0; v < V4; ++v) {
+                        float *dst = w.o + slot * D + 128 * v + COLS * lane;
+                        if (COLS == 2) *reinterpret_cast<float2 *>(dst) = make_float2(o[q][v][0], o[q][v][1]);
+                        else *reinterpret_cast<float4 *>(dst) = make_float4(o[q][v][0], o[q][v][1], o[q][v][COLS - 2], o[q][v][COLS - 1]);
+                    }
+                }
+                __syncwarp();                          // (the queries and weights are read)
+            }
+            __syncthreads();                           // the rows are read
+        }
+        next -= total;
+    }
+}
+
 // Groups of D / 4 lanes, G = D / 64 to a (unit, head, query): each joins its share of the blocks' results by
 // their running maximum, eight loads at a time, then the groups are joined:
 //   out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
@@ -751,7 +962,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
 // one took 21 (23 700 queries of 16 blocks; 18.5 since the attention leaves its results in L2).
 constexpr int JOIN_THREADS = 256;
 
-template <int D>
+template <typename T, int D>
 __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, BlockWork w)
 {
     constexpr int L = D / 4, G = D / 64, PER = JOIN_THREADS / (G * L);
@@ -780,7 +991,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const int t = min(t0 + G * f, n - 1);
-            b[f] = __ldg(a.sel + base + (w.parts == 2 ? t >> 1 : t));
+            b[f] = __ldg(a.sel + base + (t >> w.parts_log2));
             ml[f] = __ldg(w.ml + base * w.parts + t);
             v[f] = __ldcs(reinterpret_cast<const float4 *>(w.o + (base * w.parts + t) * D) + sub);
         }
@@ -830,10 +1041,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
     }
     const int64_t at = ((int64_t)u * s.mn + cell) * ((int64_t)s.H * D) + h * D + sub * 4;
     if (a.residual) {
-        const float4 r = load4(static_cast<const uint16_t *>(a.residual) + at);
+        const float4 r = load4(static_cast<const T *>(a.residual) + at);
         y = make_float4(y.x + r.x, y.y + r.y, y.z + r.z, y.w + r.w);
     }
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+    if (sizeof(T) == 4) *reinterpret_cast<float4 *>(static_cast<T *>(a.out) + at) = y;
+    else *reinterpret_cast<uint2 *>(static_cast<T *>(a.out) + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
 }
 
 // Where the parts of a by-block call lie in its workspace.
@@ -842,11 +1054,15 @@ struct WorkLayout {
     size_t n_items, items, list, q, ml, o, total;
 };
 
-WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top, int64_t nb, int64_t parts)
+// Rows of a block that an item takes: what the shared memory of the kernels holds several of.
+int part_rows(bool fp32, int64_t d, int64_t bs) { return bs == 32 || (fp32 && d > 64) ? 32 : 64; }
+int most_parts(bool fp32, int64_t d) { return 128 / part_rows(fp32, d, 128); }
+
+WorkLayout work_layout(bool fp32, int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top, int64_t nb, int64_t parts)
 {
     WorkLayout l = {};
     const int64_t uh = U * H, pairs = k_max * n_top;
-    l.max_items = ((nb < pairs ? nb : pairs) + pairs / TILE + 1) * parts;
+    l.max_items = ((nb < pairs ? nb : pairs) + pairs / (fp32 ? TILE_FP32 : TILE) + 1) * parts;
     size_t at = 0;
     const auto part = [&](size_t bytes) {
         const size_t x = at;
@@ -856,7 +1072,7 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
     l.n_items = part((size_t)uh * 4);
     l.items = part((size_t)(uh * l.max_items) * sizeof(BlockItem));
     l.list = part((size_t)(uh * pairs) * 8);
-    l.q = part((size_t)(uh * k_max * d) * 2);
+    l.q = part((size_t)(uh * k_max * d) * (fp32 ? 4 : 2));
     l.ml = part((size_t)(uh * pairs * parts) * 8);
     l.o = part((size_t)(uh * pairs * parts) * (size_t)d * 4);
     l.total = at;
@@ -864,19 +1080,25 @@ WorkLayout work_layout(int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n
 }
 
 // Whether a call's path may be by block, for which its workspace is sized.  Three launches against one, and every row
-// read once against once per query.  Of one bank of 200 frames, blocks of 64 (by block / by query): 4 heads of 64, 64
-// queries of 4 blocks 14.9 / 9.3 us, 128 of 4 15.5 / 15.4, 64 of 16 16.9 / 16.5, 128 of 16 18.5 / 30, 787 of 16
+// read once against once per query.  bf16, of one bank of 200 frames, blocks of 64 (by block / by query): 4 heads of 64,
+// 64 queries of 4 blocks 14.9 / 9.3 us, 128 of 4 15.5 / 15.4, 64 of 16 16.9 / 16.5, 128 of 16 18.5 / 30, 787 of 16
 // 29 / 129; one head of 256, 16 queries of 4 blocks 16.0 / 21, 64 of 4 17.0 / 22, 787 of 16 33 / 162.
 bool sized_by_blocks(rs3_dtype dtype, int64_t U, int64_t H, int64_t d, int64_t k_max, int64_t n_top)
 {
-    return dtype == RS3_BF16 && d >= 64 && (double)U * H * k_max * n_top * d * d * d >= 0x1p30;
+    const double pairs = (double)U * H * k_max * n_top;
+    return d >= 64 && (dtype == RS3_BF16 ? pairs * d * d * d >= 0x1p30 : pairs >= 4096);
 }
 
-// Beyond the sizes that the lists' and the tensor maps' 32-bit numbers hold it is by query.
+// fp32 by the rows too, 6 000 lists' entries of 64: 4 heads of 64 of a bank of 100 frames, 64 queries of 16 blocks
+// 22.9 / 20.6 us, 128 of 16 31 / 34, 300 of 4 28 / 22, 700 of 4 34 / 48, 700 of 16 68 / 163; one head of 256,
+// 300 of 16 44 / 38, 700 of 16 74 / 111.  Beyond the sizes that the lists' and the tensor maps' 32-bit numbers
+// hold it is by query.
 bool by_blocks(const SparseArgs &s, rs3_dtype dtype)
 {
+    const bool fp32 = dtype == RS3_F32;
     return sized_by_blocks(dtype, s.U, s.H, s.d, s.k_max, s.n_top) && (int64_t)s.k_max * s.n_top < (1ll << 28) &&
-           (int64_t)s.U * s.H * work_layout(s.U, s.H, s.d, s.k_max, s.n_top, s.nb, 2).max_items < (1ll << 30) &&
+           (!fp32 || (double)s.U * s.H * s.k_max * s.n_top * s.bs >= 0x1.8p18) &&
+           (int64_t)s.U * s.H * work_layout(fp32, s.U, s.H, s.d, s.k_max, s.n_top, s.nb, most_parts(fp32, s.d)).max_items < (1ll << 30) &&
            s.U * s.bank.rows_per_unit < (1ll << 31) - 128;
 }
 
@@ -897,11 +1119,22 @@ rs3_status launch_attend(const AttendArgs &a, const BlockWork &w, cudaStream_t s
     return RS3_OK;
 }
 
-rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t st)
+template <int D, int PR>
+rs3_status launch_attend_fp32(const AttendArgs &a, const BlockWork &w, cudaStream_t st)
+{
+    using X = Fp32Tile<D, PR>;
+    const rs3_status r = rs3_kernel_smem((const void *)k_attend_blocks_fp32<D, PR>, X::SMEM + 8 * 1024);   // (its static arrays count too)
+    if (r != RS3_OK) return r;
+    constexpr int CTAS = 220 * 1024 / (X::SMEM + 6 * 1024);
+    launch_pdl(k_attend_blocks_fp32<D, PR>, dim3((unsigned)(rs3_sm_count() * CTAS)), dim3(X::THREADS), X::SMEM, st, a, w);
+    return RS3_OK;
+}
+
+rs3_status launch_by_blocks(const AttendArgs &a, bool fp32, void *workspace, cudaStream_t st)
 {
     const SparseArgs &s = a.s;
-    const int parts = s.bs > 64 ? 2 : 1;
-    const WorkLayout l = work_layout(s.U, s.H, s.d, s.k_max, s.n_top, s.nb, parts);
+    const int parts = s.bs / part_rows(fp32, s.d, s.bs);
+    const WorkLayout l = work_layout(fp32, s.U, s.H, s.d, s.k_max, s.n_top, s.nb, parts);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     BlockWork w = {};
     w.n_items = reinterpret_cast<int32_t *>(ws + l.n_items);
@@ -920,26 +1153,37 @@ rs3_status launch_by_blocks(const AttendArgs &a, void *workspace, cudaStream_t s
     w.cluster = LIST_CTAS;
     while (w.cluster > 1 && (int64_t)s.U * s.H * w.cluster > rs3_sm_count()) w.cluster /= 2;
     w.parts = parts;
+    w.parts_log2 = parts == 4 ? 2 : parts - 1;
+    w.tile = fp32 ? TILE_FP32 : TILE;
+    w.tile_log2 = fp32 ? 5 : 6;
+    static_assert(TILE_FP32 == 1 << 5 && TILE == 1 << 6, "their logarithms");
     w.list_ctas = s.U * s.H * w.cluster;
     w.max_items = l.max_items;
     w.wait_ns = rs3_get_wait_limit_ns();
     int64_t nvec = 0, pass = 0;
     if (a.out != a.residual) {
-        nvec = (int64_t)s.U * s.mn * s.H * s.d / 8;
+        nvec = (int64_t)s.U * s.mn * s.H * s.d / (fp32 ? 4 : 8);
         pass = (nvec + 4 * LIST_THREADS - 1) / (4 * LIST_THREADS);
         if (pass > 2 * rs3_sm_count()) pass = 2 * rs3_sm_count();
     }
     w.pass_ctas = (int32_t)pass;
-    const int64_t turn = s.rope ? ((int64_t)s.U * s.k_max * s.H * s.d / 8 + LIST_THREADS - 1) / LIST_THREADS : 0;
+    const int64_t turn = s.rope ? ((int64_t)s.U * s.k_max * s.H * s.d / (fp32 ? 4 : 8) + LIST_THREADS - 1) / LIST_THREADS : 0;
     const int64_t ctas = (w.list_ctas + pass + turn + w.cluster - 1) / w.cluster * w.cluster;     // whole clusters
-    launch_pdl_cluster(k_block_lists, w.cluster, dim3((unsigned)ctas), dim3(LIST_THREADS), (size_t)w.bins * 4, st, a, w, nvec);
+    launch_pdl_cluster(fp32 ? k_block_lists<float> : k_block_lists<uint16_t>, w.cluster, dim3((unsigned)ctas), dim3(LIST_THREADS), (size_t)w.bins * 4, st, a, w, nvec);
     rs3_status r = RS3_EINTERNAL;
     const bool half = s.bs == 32;
-    if (s.d == 64) r = half ? launch_attend<64, 32>(a, w, st) : launch_attend<64, 64>(a, w, st);
-    if (s.d == 128) r = half ? launch_attend<128, 32>(a, w, st) : launch_attend<128, 64>(a, w, st);
-    if (s.d == 256) r = half ? launch_attend<256, 32>(a, w, st) : launch_attend<256, 64>(a, w, st);
+    if (fp32) {
+        if (s.d == 64) r = half ? launch_attend_fp32<64, 32>(a, w, st) : launch_attend_fp32<64, 64>(a, w, st);
+        if (s.d == 128) r = launch_attend_fp32<128, 32>(a, w, st);
+        if (s.d == 256) r = launch_attend_fp32<256, 32>(a, w, st);
+    } else {
+        if (s.d == 64) r = half ? launch_attend<64, 32>(a, w, st) : launch_attend<64, 64>(a, w, st);
+        if (s.d == 128) r = half ? launch_attend<128, 32>(a, w, st) : launch_attend<128, 64>(a, w, st);
+        if (s.d == 256) r = half ? launch_attend<256, 32>(a, w, st) : launch_attend<256, 64>(a, w, st);
+    }
     if (r != RS3_OK) return r;
-    void (*join)(AttendArgs, BlockWork) = s.d == 64 ? k_join_blocks<64> : s.d == 128 ? k_join_blocks<128> : k_join_blocks<256>;
+    void (*join)(AttendArgs, BlockWork) = s.d == 64 ? k_join_blocks<uint16_t, 64> : s.d == 128 ? k_join_blocks<uint16_t, 128> : k_join_blocks<uint16_t, 256>;
+    if (fp32) join = s.d == 64 ? k_join_blocks<float, 64> : s.d == 128 ? k_join_blocks<float, 128> : k_join_blocks<float, 256>;
     const int per = JOIN_THREADS * 256 / (s.d * s.d);      // queries of a CTA: G * L lanes each
     launch_pdl(join, dim3((unsigned)(((int64_t)s.k_max * s.H + per - 1) / per), (unsigned)s.U), dim3(JOIN_THREADS), 0, st, a, w);
     return RS3_OK;
@@ -951,7 +1195,7 @@ extern "C" size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_
 {
     if (U < 1 || H < 1 || d < 1 || k_max < 0 || n_top < 1 || n_blocks < 0) return 0;
     if (dtype != RS3_F32 && dtype != RS3_BF16) return 0;
-    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(U, H, d, k_max, n_top, n_blocks, 2).total : 0);
+    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(dtype == RS3_F32, U, H, d, k_max, n_top, n_blocks, most_parts(dtype == RS3_F32, d)).total : 0);
 }
 
 extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -981,7 +1225,7 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
                    static_cast<const uint4 *>(residual), static_cast<uint4 *>(out), nvec);
     }
     if (blocks) {
-        const rs3_status e = launch_by_blocks(a, workspace, st);
+        const rs3_status e = launch_by_blocks(a, dtype == RS3_F32, workspace, st);
         if (e != RS3_OK) return e;
     } else if (k_max > 0) {
         const int pieces = d * (int)elem_bytes(dtype) / 16;

@@ -678,7 +678,8 @@ def test_sparse_readout_matches_64_bits(rs3, dtype, H, d, n_top, block, residual
     assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
 
 
-@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 64), ("bf16", 1, 128), ("bf16", 3, 256), ("f32", 1, 64)])
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 64), ("bf16", 1, 128), ("bf16", 3, 256), ("f32", 1, 64), ("f32", 2, 64),
+                                       ("f32", 2, 128), ("f32", 1, 256)])
 @pytest.mark.parametrize("block,n_top", [(32, 19), (64, 11), (128, 6)])
 @pytest.mark.parametrize("residual,rope", [("none", True), ("inplace", False), ("other", True)])
 def test_sparse_readout_of_many_queries(rs3, dtype, H, d, block, n_top, residual, rope):
@@ -782,7 +783,7 @@ def test_one_block_chosen_by_everybody_and_scores_far_apart(rs3):
     assert int(b.st) == 0 and (err <= tol).all(), float((err - tol).max())
 
 
-@pytest.mark.parametrize("block,dtype,H,d,n,n_top", [(32, "bf16", 2, 64, 300, 9), (32, "bf16", 1, 128, 1000, 40), (64, "f32", 1, 64, 20, 5)])
+@pytest.mark.parametrize("block,dtype,H,d,n,n_top", [(32, "bf16", 2, 64, 300, 9), (32, "bf16", 1, 128, 1000, 40), (64, "f32", 1, 64, 20, 5), (64, "f32", 2, 64, 300, 9)])
 def test_sparse_readout_over_many_blocks(rs3, block, dtype, H, d, n, n_top):
     """A bank of thousands of blocks, all of its rows live; blocks chosen by one query, by many, twice by one."""
     rows, mn = (600_000 if block == 64 else 300_000), 1024
@@ -821,10 +822,11 @@ def test_sparse_readout_over_many_blocks(rs3, block, dtype, H, d, n, n_top):
     assert (err <= tol).all(), float((err - tol).max())
 
 
-def test_sparse_readout_by_block_latches_what_the_device_finds(rs3):
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sparse_readout_by_block_latches_what_the_device_finds(rs3, dtype):
     """As below, for a call large enough to go by block; a bad entry leaves the others' results as they are."""
-    U, H, n, n_top = 3, 2, 150, 6
-    b = Built(rs3, U=U, H=H, d=64, m=13, n=13, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
+    U, H, n, n_top = 3, 2, 150, 14
+    b = Built(rs3, U=U, H=H, d=64, dtype=dtype, m=13, n=13, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
     nb = b.bank.blocks(32)
     q, idx, count, group = queries(b, 1, n, [n, n, n])
     group.zero_()
@@ -832,7 +834,7 @@ def test_sparse_readout_by_block_latches_what_the_device_finds(rs3):
 
     def read(idx=idx, count=count, group=group, sel=sel0):
         b.st.zero_()
-        out = torch.zeros((U, b.mn, H * 64), dtype=torch.bfloat16, device="cuda")
+        out = torch.zeros((U, b.mn, H * 64), dtype=DT[dtype], device="cuda")
         run_readout(rs3, b, q, idx, count, group, sel, None, 32, 0.0, None, out, 1)
         return int(b.st), out
 
@@ -1113,29 +1115,30 @@ def test_captured_reads_share_workspaces(rs3, n):
         assert torch.equal(first.transpose(1, 2)[live], sel.transpose(1, 2)[live])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("k_max,n_top", [(8, 5), (2, 1), (0, 3)])
-def test_read_of_many_units(rs3, k_max, n_top):
+def test_read_of_many_units(rs3, k_max, n_top, dtype):
     """More (unit, head) pairs than a CTA keeps counts of; few queries of each, none of some, or none at all."""
     U, H, d, mn = 400, 4, 64, 16
-    bank = rs3.Bank(U, H, d, "bf16", mn, 1, -1, 64, 4, 0)
+    bank = rs3.Bank(U, H, d, dtype, mn, 1, -1, 64, 4, 0)
     st, g = status(), gen(71)
     for f in range(4):
-        k, v = (torch.randn((U, mn, H * d), generator=g, device="cuda").bfloat16() for _ in range(2))
+        k, v = (torch.randn((U, mn, H * d), generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
         rs3.rs3_bank_commit(bank, k, v, None, int(f == 0), st)
     nb = bank.blocks(32)                                    # 80 rows: two blocks and a half
     dig, step = torch.zeros((U, H, nb, d), dtype=torch.int8, device="cuda"), torch.zeros((U, H, nb), device="cuda")
     rs3.rs3_bank_digest(bank, 32, -1, dig, step, st)
-    q = torch.randn((1, mn, H * d), generator=g, device="cuda").bfloat16()
+    q = torch.randn((1, mn, H * d), generator=g, device="cuda").to(DT[dtype])
     idx = torch.stack([torch.randperm(mn, generator=g, device="cuda")[:max(k_max, 1)] for _ in range(U)]).to(torch.int32)
     count = (torch.arange(U, device="cuda") % (k_max + 1)).to(torch.int32)
     group = torch.zeros(U, dtype=torch.int32, device="cuda")
     sel = torch.full((U, H, max(k_max, 1), n_top), -5, dtype=torch.int32, device="cuda")
-    x = torch.randn((U, mn, H * d), generator=g, device="cuda").bfloat16()
+    x = torch.randn((U, mn, H * d), generator=g, device="cuda").to(DT[dtype])
     out = torch.zeros_like(x)
     w1 = torch.empty(rs3.rs3_block_select_workspace_bytes(U, H, k_max, nb), dtype=torch.uint8, device="cuda")
-    w2 = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, nb, "bf16"), dtype=torch.uint8, device="cuda")
-    rs3.rs3_block_select(q, "bf16", 1, mn, H, d, group, idx, count, k_max, bank, 32, dig, step, None, n_top, sel, w1, st)
-    rs3.rs3_sparse_readout(q, "bf16", 1, mn, H, d, group, idx, count, k_max, bank, 32, sel, n_top, None, x, out, 0.0, w2, st)
+    w2 = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, nb, dtype), dtype=torch.uint8, device="cuda")
+    rs3.rs3_block_select(q, dtype, 1, mn, H, d, group, idx, count, k_max, bank, 32, dig, step, None, n_top, sel, w1, st)
+    rs3.rs3_sparse_readout(q, dtype, 1, mn, H, d, group, idx, count, k_max, bank, 32, sel, n_top, None, x, out, 0.0, w2, st)
     assert int(st) == 0
     kept = torch.zeros((U, mn), dtype=torch.bool, device="cuda")
     live = torch.arange(max(k_max, 1), device="cuda")[None, :] < count[:, None]
@@ -1159,8 +1162,8 @@ def test_read_of_many_units(rs3, k_max, n_top):
     want = x.double().gather(1, idx.long()[..., None].expand(-1, -1, H * d)) + A
     got = out.double().gather(1, idx.long()[..., None].expand(-1, -1, H * d))
     s_abs = (torch.einsum("ujhd,urhd->ujhr", Q.abs(), K.abs()) * d ** -0.5).amax(-1)[..., None].expand(-1, -1, -1, d).flatten(2)
-    half = HALF["bf16"]                                     # (the bounds of readout_ref)
-    tol = half * want.abs() + size * (torch.expm1(2 * s_abs * 2.0 ** -24 * 300) + 300 * 2.0 ** -24 + half) * 1.01 + 1e-30
+    half = HALF[dtype]                                      # (the bounds of readout_ref)
+    tol = half * want.abs() + size * (torch.expm1(2 * s_abs * 2.0 ** -24 * 300) + 300 * 2.0 ** -24 + (half if dtype == "bf16" else 0.0)) * 1.01 + 1e-30
     assert ((got - want).abs() <= tol)[live].all(), float(((got - want).abs() - tol)[live].max())
 
 
