@@ -26,12 +26,13 @@ struct DigestArgs {
     uint64_t wait_ns;          // limit of each wait
 };
 
-// Rows of the newest `refresh` ring frames; by a whole warp.
+// Rows of the newest `refresh` ring frames, -1 where the counters are inconsistent; by a whole warp.
 __device__ int64_t fresh_rows(const DigestArgs &a, int64_t u)
 {
     const int64_t *mu = a.bank.meta + u * a.bank.stride_words;
     const int64_t *fl = mu + BM_HEADER_WORDS + a.bank.max_frames;
-    const int64_t nf = min(mu[BM_NFRAMES], (int64_t)a.bank.max_frames), oldest = mu[BM_OLDEST];
+    const int64_t nf = mu[BM_NFRAMES], oldest = mu[BM_OLDEST];
+    if (nf < 0 || nf > a.bank.max_frames || (nf > 0 && (oldest < 0 || oldest >= a.bank.max_frames))) return -1;
     int64_t n = 0;
     for (int64_t i = threadIdx.x & 31; i < a.refresh && i < nf; i += 32) {
         int64_t slot = oldest + nf - 1 - i;
@@ -98,11 +99,12 @@ __global__ void __launch_bounds__(32 * DIGEST_WARPS, 1) k_digest(DigestArgs a, c
     pdl_wait();
     const int64_t u = blockIdx.z;
     LiveRows rows;
-    if (!rows.load(a.bank, u)) {
+    const bool sane = rows.load(a.bank, u);
+    const int64_t fresh = a.refresh > 0 ? fresh_rows(a, u) : 0;
+    if (!sane || fresh < 0) {
         if (threadIdx.x == 0) latch_status(a.status, RS3_EINTERNAL);
         return;
     }
-    const int64_t fresh = a.refresh > 0 ? fresh_rows(a, u) : 0;
     const int nvec = (int)(a.row_bytes / 16), slab0 = blockIdx.y * 32 * ITEMS;
     const uint32_t pitch = (uint32_t)min(nvec, 32 * ITEMS) * 16u;      // bytes of a row in a buffer
     const int64_t warps = (int64_t)gridDim.x * DIGEST_WARPS;

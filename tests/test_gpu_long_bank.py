@@ -868,6 +868,23 @@ def test_sparse_readout_by_block_latches_what_the_device_finds(rs3, dtype):
         assert code == 0 and torch.equal(out, same)
 
 
+def test_digest_and_drop_leave_out_units_whose_frame_counters_are_unsound(rs3):
+    b = Built(rs3, U=3, H=1, d=64, m=8, n=8, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=9)
+    dig, step, _ = make_digest(b, 32)
+    one = torch.ones(3, dtype=torch.int32, device="cuda")
+    for word, value in ((3, -1), (3, 1 << 20), (4, -1), (4, b.bank.max_frames)):
+        was = b.bank.counters.clone()
+        b.bank.counters[1, word] = value
+        bad = b.bank.counters[1].clone()
+        st, d, s = status(), torch.full_like(dig, 9), torch.full_like(step, 9.0)
+        rs3.rs3_bank_digest(b.bank, 32, 1, d, s, st)
+        assert int(st) == rs3.RS3_EINTERNAL and (d[1] == 9).all() and (s[1] == 9.0).all() and (s[0] != 9.0).any()
+        st = status()
+        rs3.rs3_bank_drop_frames(b.bank, one, None, st)
+        assert int(st) == rs3.RS3_EINTERNAL and torch.equal(b.bank.counters[1], bad)
+        b.bank.counters.copy_(was)
+
+
 @pytest.mark.parametrize("n", [150, 10])
 def test_reads_leave_out_units_whose_counters_are_unsound(rs3, n):
     b = Built(rs3, U=3, H=2, d=64, m=13, n=13, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=8)
