@@ -1122,8 +1122,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
     const int width = s.d < 64 ? 64 : s.d, q_bytes = TILE_ROWS * 2 * width, b_bytes = TILE_COLS * 2 * width;
     uint8_t *s_b = smem + q_bytes;
     const int cap = p.cap;
-    float *s_cand = reinterpret_cast<float *>(s_b + 2 * b_bytes) + (threadIdx.x & 127) * cap;
-    uint16_t *s_block = reinterpret_cast<uint16_t *>(s_b + 2 * b_bytes + TILE_ROWS * cap * 4) + (threadIdx.x & 127) * cap;
+    // a query warp's part: its lanes' candidates, scores then blocks; before those the maxima, in longer runs
+    float *s_mine = reinterpret_cast<float *>(s_b + 2 * b_bytes + (warp & 3) * 32 * cap * 6), *s_cand = s_mine + lane * cap;
+    uint16_t *s_block = reinterpret_cast<uint16_t *>(s_mine + 32 * cap) + lane * cap;
     const uint32_t bars = smem_u32(s_bars);
     const uint32_t SFULL = bars, SFREE = bars + 16, BFULL = bars + 32, BFREE = bars + 48, DRAIN = bars + 64;
     volatile int *abort_flag = &s_abort;
@@ -1311,11 +1312,13 @@ __global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
         const bool mine = q < nq, busy = (q & ~31) < nq;
         const uint32_t tl = tmem + ((uint32_t)(q & ~31) << 16);
         const int places = TILE_COLS * n_tiles;
+        const int most_maxima = ((cap * 3 / 2 / 4 - 1) | 1) * 4;      // an odd number of 16 bytes
         int blocks = 8;                                    // blocks of a maximum
-        while (places > blocks * cap) blocks *= 2;
+        while (places > blocks * most_maxima) blocks *= 2;
         const int n_maxima = (places + blocks - 1) / blocks;
+        const Column maxima = {s_mine + lane * most_maxima};
         Candidates c = {{s_cand}, s_block, 0};
-        c.score.clear(0, cap);
+        maxima.clear(0, most_maxima);
         // waits for the next scores and loads them, times their blocks' steps
         uint32_t x[TILE_COLS];
         int k = 0;
@@ -1355,18 +1358,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
                 for (int e = 0; e < 4; ++e) m[e] = fmaxf(__uint_as_float(x[b + e]), __uint_as_float(x[b + 4 + e]));
                 top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
                 if (((TILE_COLS * i + b + 8) & (blocks - 1)) == 0) {
-                    c.score.v[at_max++] = top;
+                    maxima.v[at_max++] = top;
                     top = -INFINITY;
                 }
             }
         }
-        if (busy && (places & (blocks - 1)) != 0) c.score.v[at_max] = top;
+        if (busy && (places & (blocks - 1)) != 0) maxima.v[at_max] = top;
         // the bound: the n_top-th largest of the maxima, which n_top scores reach; where fewer maxima hold a live block, every
         // live one's score
         float bound = INFINITY;
         uint32_t low = LEAST_KEY;
         if (ok && busy) {
-            const float nth = nth_largest(c.score, n_maxima, s.n_top);
+            const float nth = nth_largest(maxima, n_maxima, s.n_top);
+            __syncwarp();                                  // (the lanes' maxima are read: candidates take their place)
             if (nth > -INFINITY) low = order_bits(nth);
             if (mine) bound = score_of(low);
             c.score.clear(0, cap);
