@@ -1085,8 +1085,11 @@ struct Candidates {
 //                many (ties, or fewer groups than choices), they are cut down and the bound rises.
 // Then the candidates are cut to n_top.  Three warps spread the digests (fp16, 128-byte swizzle) a tile ahead, one issues
 // the products.  Per query this takes a third of k_score_blocks' instructions, but a CTA goes through all of the
-// blocks twice, so it is for calls whose queries fill the SMs: 23 700 queries over 987 blocks 70 us against 117, 757 over
-// 4 700 the other way round (74 against 47).
+// blocks twice, so it is for calls whose queries fill the SMs: 23 700 queries over 990 blocks 65 us against 93, 757 over
+// 4 700 the other way round (74 against 46).  A step of 64 blocks takes some 1 600 cycles in the first pass and 2 100 in the
+// second, where a score's predicated stores fill the shared memory's pipe; the digests are there in time.  The maxima take
+// the whole of the warp's part of shared memory: in groups of 16 blocks where 8 have room, 16 choices took 70 us and
+// 32 took 163 instead of 92, as two of a group's blocks are often among the best.
 template <typename T>
 __global__ void __launch_bounds__(TILE_THREADS, 2) k_score_tiles(TileArgs p)
 {
@@ -1534,9 +1537,9 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.step = step;
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
-    // 128 queries to a CTA, where those keep half of the SMs busy and their candidates have room.  Over 990 blocks (a tile of
-    // queries / 16 of them to a CTA): 64 queries in 32 heads 43 / 19 us, 709 in 8 heads (48 tiles) 48 / 36, 256
-    // in 32 (64 tiles) 45 / 47, 709 in 32 (192 tiles) 70 / 113.
+    // 128 queries to a CTA, where those keep half of the SMs busy and their candidates have room.  Over 990 blocks, 16 choices
+    // (128 queries to a CTA / 16): 64 queries in 32 heads (32 tiles) 38 / 16 us, 709 in 8 heads (48) 40 / 31, 256 in 32
+    // (64) 43 / 40, 384 in 32 (96) 42 / 54, 709 in 32 (192) 57 / 95, with 32 choices 92 / 117.
     const int fixed = (TILE_ROWS + 2 * TILE_COLS) * 2 * (d < 64 ? 64 : d) + 1024, each = TILE_ROWS * 6;
     const int cap = (((106 * 1024 - fixed) / each / 4 - 1) | 1) * 4;       // an odd number of 16 bytes
     if (2 * (int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS) >= rs3_sm_count() && n_top <= TILE_TOP && cap >= n_top + 48 &&
