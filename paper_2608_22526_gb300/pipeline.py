@@ -171,8 +171,9 @@ class Pipeline:
             stride = 0 if keep is None else keep.shape[1]
             ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
             rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
-            chosen = self.track[parent.clamp(min=0).long()]
-            into.track.copy_(torch.where((parent >= 0)[:, None], chosen, into.track))
+            # (a parent past the last unit is the copy's to refuse: the gather stays inside)
+            chosen = self.track[parent.clamp(0, self.w.U - 1).long()]
+            into.track.copy_(torch.where(((parent >= 0) & (parent < self.w.U))[:, None], chosen, into.track))
         return into
 
     def drop_frames(self, n_oldest: Optional[torch.Tensor], n_newest: Optional[torch.Tensor] = None):

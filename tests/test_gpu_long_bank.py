@@ -1214,3 +1214,18 @@ def test_copy_of_more_units_than_a_cta_counts(rs3, masked):
         if u % 50 == 0:
             assert torch.equal(b.k_store[u][to], a.k_store[p][from_cond + from_ring])
             assert torch.equal(b.v_store[u][to], a.v_store[p][from_cond + from_ring])
+
+
+def test_fork_with_a_parent_that_is_no_unit(rs3):
+    """The status word tells; the unit and its tracker stay as they are, and the context lives."""
+    pipe, _, _ = small_pipeline()
+    other, _, _ = small_pipeline()
+    pipe.track.copy_(torch.arange(12).view(2, 6))
+    other.track.fill_(-7)
+    before = rs3.rs3_bank_read_meta(other.bank)[0]
+    for bad in (2, (1 << 31) - 1, -2):
+        other.status.zero_()
+        pipe.fork(torch.tensor([bad, 0], dtype=torch.int32, device="cuda"), into=other)
+        assert other.status_code() == rs3.RS3_EINVAL
+        assert (other.track[0] == -7).all() and torch.equal(other.track[1], pipe.track[0])
+        assert (rs3.rs3_bank_read_meta(other.bank)[0][0] == before[0]).all()

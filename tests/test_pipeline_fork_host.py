@@ -1,0 +1,49 @@
+"""Pipeline.fork() around the library's copy: which trackers move, in which order of streams, and with
+what workspace.  CPU only: the copy, the streams and the bank are stand-ins."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+
+@pytest.fixture()
+def fork(monkeypatch):
+    """fork(parent, ...) over pipelines without a GPU; .calls lists what was asked of the library and the streams."""
+    from paper_2608_22526_gb300 import _build
+    _build.build()
+    from paper_2608_22526_gb300 import pipeline
+
+    calls = []
+
+    def make(U, first, stream=None):
+        p = pipeline.Pipeline.__new__(pipeline.Pipeline)
+        p.w, p.device, p.stream = types.SimpleNamespace(U=U), torch.device("cpu"), stream
+        p.track = (torch.arange(6 * U, dtype=torch.int32) + first).view(U, 6)
+        p.bank = types.SimpleNamespace(U=U, ring_cap=0)
+        p.status = torch.zeros(1, dtype=torch.int32)
+        return p
+
+    def copy(dst, src, parent, keep, workspace, status, stream=None):
+        calls.append(("copy", workspace.numel()))
+        for u in range(dst.U):
+            if not -1 <= int(parent[u]) < src.U:
+                status.fill_(pipeline.rs3.RS3_EINVAL)
+
+    monkeypatch.setattr(pipeline.rs3, "rs3_bank_copy", copy)
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    return types.SimpleNamespace(make=make, calls=calls, rs3=pipeline.rs3)
+
+
+def parents(*p):
+    return torch.tensor(p, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("bad", [3, 4, 1 << 30, (1 << 31) - 1, -2, -(1 << 31)])
+def test_a_parent_that_is_no_unit_is_left_to_the_copy(fork, bad):
+    """It latches RS3_EINVAL and leaves its unit as it is: no index goes past the trackers for it."""
+    a, b = fork.make(3, 100), fork.make(3, 500)
+    was = b.track.clone()
+    a.fork(parents(2, bad, -1), into=b)
+    assert int(b.status) == fork.rs3.RS3_EINVAL
+    assert torch.equal(b.track[0], a.track[2]) and torch.equal(b.track[1:], was[1:])
