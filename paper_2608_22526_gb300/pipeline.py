@@ -159,9 +159,18 @@ class Pipeline:
                                self.bank, self.block, self.block_sel, self.n_top, rope, residual, out, scale,
                                self.ws_sparse, self.status, self.stream)
 
+    def _on(self):
+        """The stream of this pipeline's calls."""
+        return self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+
     def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
         """A pipeline (`into`, or a new one with this one's sizes) whose unit u holds the rows
-        of this one's unit parent[u], those that keep[u] leaves, and its tracker."""
+        of this one's unit parent[u], those that keep[u] leaves, and its tracker.  The copy runs on this
+        pipeline's stream; where `into` has another, it comes after what was issued there, and what is issued
+        there next comes after it."""
+        here, there = self._on(), into._on() if into is not None else None
+        if there is not None and there != here:
+            here.wait_stream(there)
         # the new buffers are filled, and the workspace comes and goes, in the order of this pipeline's stream
         with torch.cuda.stream(self.stream):
             if into is None:
@@ -174,6 +183,8 @@ class Pipeline:
             # (a parent past the last unit is the copy's to refuse: the gather stays inside)
             chosen = self.track[parent.clamp(0, self.w.U - 1).long()]
             into.track.copy_(torch.where(((parent >= 0) & (parent < self.w.U))[:, None], chosen, into.track))
+        if there is not None and there != here:
+            there.wait_stream(here)
         return into
 
     def drop_frames(self, n_oldest: Optional[torch.Tensor], n_newest: Optional[torch.Tensor] = None):

@@ -1229,3 +1229,33 @@ def test_fork_with_a_parent_that_is_no_unit(rs3):
         assert other.status_code() == rs3.RS3_EINVAL
         assert (other.track[0] == -7).all() and torch.equal(other.track[1], pipe.track[0])
         assert (rs3.rs3_bank_read_meta(other.bank)[0][0] == before[0]).all()
+
+
+@pytest.mark.parametrize("busy", ["source", "target"])
+def test_fork_into_a_pipeline_on_another_stream(rs3, busy):
+    """What the target's stream still has to do comes before the copy, what it does next after it."""
+    want, _, _ = small_pipeline()
+    want.use_blocks(32, 3)
+    want.digest(-1)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    (pipe, _, mask), (other, _, _) = (small_pipeline(s) for s in streams)
+    pipe.track.copy_(torch.arange(12).view(2, 6))
+    parent = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    k = torch.randn((2, other.w.mn, other.w.D), generator=gen(8), device="cuda").bfloat16()
+    other.use_blocks(32, 3)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[busy == "target"]):
+        torch.cuda._sleep(100_000_000)                     # some 50 ms
+    with torch.cuda.stream(streams[1]):
+        other.commit(k, k, mask, 0)                        # (a frame that the copy takes away)
+        other.track.fill_(-7)
+        pipe.fork(parent, into=other)
+        other.digest(-1)
+        track = other.track.clone()
+    torch.cuda.synchronize()
+    assert pipe.status_code() == 0 and other.status_code() == 0
+    live = want.block_step != 0
+    assert live.any() and torch.equal(other.block_step.flip(0)[live], want.block_step[live])
+    assert torch.equal(other.block_digest.flip(0)[live], want.block_digest[live])
+    assert torch.equal(track, pipe.track.flip(0))
+    assert (rs3.rs3_bank_read_meta(other.bank)[0][:, 7] == rs3.rs3_bank_read_meta(want.bank)[0][:, 7]).all()

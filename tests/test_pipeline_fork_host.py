@@ -7,6 +7,17 @@ import pytest
 import torch
 
 
+class Stream:
+    def __init__(self, name, calls):
+        self.name, self.calls, self.seen = name, calls, lambda: None
+
+    def __eq__(self, other):
+        return self.name == other.name
+
+    def wait_stream(self, other):
+        self.calls.append((self.name, "waits for", other.name, self.seen()))
+
+
 @pytest.fixture()
 def fork(monkeypatch):
     """fork(parent, ...) over pipelines without a GPU; .calls lists what was asked of the library and the streams."""
@@ -32,6 +43,7 @@ def fork(monkeypatch):
 
     monkeypatch.setattr(pipeline.rs3, "rs3_bank_copy", copy)
     monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream("current", calls))
     return types.SimpleNamespace(make=make, calls=calls, rs3=pipeline.rs3)
 
 
@@ -47,3 +59,24 @@ def test_a_parent_that_is_no_unit_is_left_to_the_copy(fork, bad):
     a.fork(parents(2, bad, -1), into=b)
     assert int(b.status) == fork.rs3.RS3_EINVAL
     assert torch.equal(b.track[0], a.track[2]) and torch.equal(b.track[1:], was[1:])
+
+
+@pytest.mark.parametrize("here,there", [("a", "b"), ("a", None), (None, "b")])
+def test_the_target_s_stream_is_waited_for_and_waits(fork, here, there):
+    """What the target's stream does goes before the copy, and what it does next after the trackers."""
+    a, b = (fork.make(2, n, s and Stream(s, fork.calls)) for n, s in ((100, here), (500, there)))
+    seen = lambda: bool(torch.equal(b.track, a.track))
+    if b.stream:
+        b.stream.seen = seen
+    a.fork(parents(0, 1), into=b)
+    x, y = here or "current", there or "current"
+    first, copy, last = fork.calls
+    assert first[:3] == (x, "waits for", y) and copy[0] == "copy" and last[:3] == (y, "waits for", x)
+    assert last[3] is (True if there else None)
+
+
+@pytest.mark.parametrize("name", ["a", None])
+def test_one_stream_waits_for_nothing(fork, name):
+    a, b = (fork.make(2, n, name and Stream(name, fork.calls)) for n in (100, 500))
+    a.fork(parents(0, 1), into=b)
+    assert [c[0] for c in fork.calls] == ["copy"]
