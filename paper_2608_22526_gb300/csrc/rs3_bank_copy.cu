@@ -145,6 +145,7 @@ __device__ void publish(const CopyArgs &a, int u, int p, int64_t live, int64_t c
         mu[BM_OLDEST] = 0;
         mu[BM_NCOND] = mp[BM_NCOND];
         mu[BM_PTRLEN] = ptr;
+        mu[BM_COPIES] += 1;                       // (what moves with the rows on the host's side goes by this)
     }
 }
 

@@ -25,6 +25,7 @@ enum {
     BM_NCOND = 5,       // pinned frames held
     BM_PTRLEN = 6,      // pointer rows held
     BM_ARRIVE = 8,      // CTAs of the running commit that have read the old counters
+    BM_COPIES = 9,      // copies that the unit has become (a copy that leaves the unit as it is does not count)
     BM_HEADER_WORDS = 16
 };
 // after the header: int64 foff[max_frames], int64 flen[max_frames]

@@ -165,7 +165,8 @@ class Pipeline:
 
     def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
         """A pipeline (`into`, or a new one with this one's sizes) whose unit u holds the rows
-        of this one's unit parent[u], those that keep[u] leaves, and its tracker.  The copy runs on this
+        of this one's unit parent[u], those that keep[u] leaves, and its tracker.  A unit that the copy
+        leaves as it is (`into`'s status tells why) keeps its tracker too.  The copy runs on this
         pipeline's stream; where `into` has another, it comes after what was issued there, and what is issued
         there next comes after it."""
         here, there = self._on(), into._on() if into is not None else None
@@ -179,10 +180,11 @@ class Pipeline:
                     into.use_blocks(self.block, self.n_top)
             stride = 0 if keep is None else keep.shape[1]
             ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
+            copies = into.bank.copies.clone()
             rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
-            # (a parent past the last unit is the copy's to refuse: the gather stays inside)
+            # the trackers of the units that the copy replaced (it refuses parents that are no unit: the gather stays inside)
             chosen = self.track[parent.clamp(0, self.w.U - 1).long()]
-            into.track.copy_(torch.where(((parent >= 0) & (parent < self.w.U))[:, None], chosen, into.track))
+            into.track.copy_(torch.where((into.bank.copies != copies)[:, None], chosen, into.track))
         if there is not None and there != here:
             there.wait_stream(here)
         return into

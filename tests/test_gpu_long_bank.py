@@ -1259,3 +1259,32 @@ def test_fork_into_a_pipeline_on_another_stream(rs3, busy):
     assert torch.equal(other.block_digest.flip(0)[live], want.block_digest[live])
     assert torch.equal(track, pipe.track.flip(0))
     assert (rs3.rs3_bank_read_meta(other.bank)[0][:, 7] == rs3.rs3_bank_read_meta(want.bank)[0][:, 7]).all()
+
+
+def test_fork_leaves_the_trackers_of_refused_units(rs3):
+    """No room, a mask shorter than the parent, a source that does not stay as it is: the unit's tracker stays with its bank."""
+    from paper_2608_22526_gb300.pipeline import Pipeline
+    pipe, _, _ = small_pipeline()
+    pipe.track.copy_(torch.arange(12).view(2, 6))
+    both = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    small = Pipeline(pipe.w, ring_cap=100)                 # three frames of 60 rows do not fit
+    small.track.fill_(-7)
+    pipe.fork(both, into=small)
+    assert small.status_code() == rs3.RS3_ECAPACITY and (small.track == -7).all()
+    keep = torch.ones((2, 180), dtype=torch.uint8, device="cuda")
+    keep[1] = 0
+    small.status.zero_()
+    pipe.fork(both, keep, into=small)                      # of unit 1 nothing is left, which fits
+    assert small.status_code() == rs3.RS3_ECAPACITY
+    assert (small.track[0] == -7).all() and torch.equal(small.track[1], pipe.track[0])
+    small.status.zero_()
+    small.track.fill_(-7)
+    pipe.fork(both, torch.zeros((2, 179), dtype=torch.uint8, device="cuda"), into=small)
+    assert small.status_code() == rs3.RS3_EINVAL and (small.track == -7).all()
+    pipe.fork(both, into=pipe)                             # each other's source
+    assert pipe.status_code() == rs3.RS3_EINVAL and torch.equal(pipe.track, torch.arange(12, dtype=torch.int32, device="cuda").view(2, 6))
+    pipe.status.zero_()
+    pipe.fork(torch.tensor([-1, 0], dtype=torch.int32, device="cuda"), into=pipe)
+    assert pipe.status_code() == 0 and torch.equal(pipe.track[1], pipe.track[0])
+    # the words count what became of the units, no more
+    assert pipe.bank.copies.tolist() == [0, 1] and small.bank.copies.tolist() == [0, 1]

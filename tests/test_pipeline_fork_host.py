@@ -31,7 +31,8 @@ def fork(monkeypatch):
         p = pipeline.Pipeline.__new__(pipeline.Pipeline)
         p.w, p.device, p.stream = types.SimpleNamespace(U=U), torch.device("cpu"), stream
         p.track = (torch.arange(6 * U, dtype=torch.int32) + first).view(U, 6)
-        p.bank = types.SimpleNamespace(U=U, ring_cap=0)
+        p.bank = types.SimpleNamespace(U=U, ring_cap=0, copies=torch.full((U,), 3, dtype=torch.int64))
+        p.bank.full = []                                   # units that a copy finds no room in
         p.status = torch.zeros(1, dtype=torch.int32)
         return p
 
@@ -40,6 +41,10 @@ def fork(monkeypatch):
         for u in range(dst.U):
             if not -1 <= int(parent[u]) < src.U:
                 status.fill_(pipeline.rs3.RS3_EINVAL)
+            elif u in dst.full:
+                status.fill_(pipeline.rs3.RS3_ECAPACITY)
+            elif int(parent[u]) >= 0:
+                dst.copies[u] += 1
 
     monkeypatch.setattr(pipeline.rs3, "rs3_bank_copy", copy)
     monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
@@ -80,3 +85,15 @@ def test_one_stream_waits_for_nothing(fork, name):
     a, b = (fork.make(2, n, name and Stream(name, fork.calls)) for n in (100, 500))
     a.fork(parents(0, 1), into=b)
     assert [c[0] for c in fork.calls] == ["copy"]
+
+
+def test_a_unit_that_the_copy_leaves_keeps_its_tracker(fork):
+    a, b = fork.make(3, 100), fork.make(3, 500)
+    b.bank.full = [1]
+    was = b.track.clone()
+    a.fork(parents(0, 2, -1), into=b)
+    assert int(b.status) == fork.rs3.RS3_ECAPACITY
+    assert torch.equal(b.track[0], a.track[0]) and torch.equal(b.track[1:], was[1:])
+    b.bank.full = []
+    a.fork(parents(-1, 2, -1), into=b)                     # (a copy counted before is not taken for this one's)
+    assert torch.equal(b.track[1], a.track[2]) and torch.equal(b.track[2], was[2])
