@@ -164,11 +164,14 @@ class Pipeline:
         return self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
 
     def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
-        """A pipeline (`into`, or a new one with this one's sizes) whose unit u holds the rows
+        """A pipeline (`into`, or a new one with this one's sizes; `into` may have another number of units) whose unit u holds the rows
         of this one's unit parent[u], those that keep[u] leaves, and its tracker.  A unit that the copy
         leaves as it is (`into`'s status tells why) keeps its tracker too.  The copy runs on this
         pipeline's stream; where `into` has another, it comes after what was issued there, and what is issued
         there next comes after it."""
+        U = self.w.U if into is None else into.w.U
+        if parent.shape != (U,):
+            raise ValueError(f"parent: one for each of the {U} units wanted, got {tuple(parent.shape)}")
         here, there = self._on(), into._on() if into is not None else None
         if there is not None and there != here:
             here.wait_stream(there)
@@ -179,7 +182,7 @@ class Pipeline:
                 if hasattr(self, "block"):
                     into.use_blocks(self.block, self.n_top)
             stride = 0 if keep is None else keep.shape[1]
-            ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(self.w.U, stride), dtype=torch.uint8, device=self.device)
+            ws = torch.empty(rs3.rs3_bank_copy_workspace_bytes(U, stride), dtype=torch.uint8, device=self.device)
             copies = into.bank.copies.clone()
             rs3.rs3_bank_copy(into.bank, self.bank, parent, keep, ws, into.status, self.stream)
             # the trackers of the units that the copy replaced (it refuses parents that are no unit: the gather stays inside)

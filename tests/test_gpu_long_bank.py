@@ -1288,3 +1288,24 @@ def test_fork_leaves_the_trackers_of_refused_units(rs3):
     assert pipe.status_code() == 0 and torch.equal(pipe.track[1], pipe.track[0])
     # the words count what became of the units, no more
     assert pipe.bank.copies.tolist() == [0, 1] and small.bank.copies.tolist() == [0, 1]
+
+
+def test_fork_into_a_pipeline_with_another_number_of_units(rs3):
+    import dataclasses
+    from paper_2608_22526_gb300.pipeline import Pipeline
+    pipe, _, _ = small_pipeline()
+    pipe.track.copy_(torch.arange(12).view(2, 6))
+    for parent in ([1], [1, -1, 0, 1, 1]):
+        wide = Pipeline(dataclasses.replace(pipe.w, units_per_group=len(parent)), ring_cap=20 * pipe.w.mn)
+        wide.track.fill_(-7)
+        keep = (torch.rand((len(parent), 180), generator=gen(2), device="cuda") < 0.5).to(torch.uint8)
+        pipe.fork(torch.tensor(parent, dtype=torch.int32, device="cuda"), keep, into=wide)
+        assert wide.status_code() == 0
+        length = rs3.rs3_bank_read_meta(wide.bank)[0][:, 7]
+        for u, p in enumerate(parent):
+            on = keep[u] != 0
+            assert length[u] == (0 if p < 0 else int(on.sum()))
+            assert torch.equal(wide.track[u], pipe.track[p]) if p >= 0 else (wide.track[u] == -7).all()
+            if p >= 0:
+                n, at = int(length[u]), pipe.w.n_cond * pipe.w.mn
+                assert torch.equal(bits(wide.bank.k_store[u, at:at + n]), bits(pipe.bank.k_store[p, at:at + 180][on]))

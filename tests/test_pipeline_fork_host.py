@@ -38,6 +38,8 @@ def fork(monkeypatch):
 
     def copy(dst, src, parent, keep, workspace, status, stream=None):
         calls.append(("copy", workspace.numel()))
+        assert parent.numel() == dst.U
+        assert keep is None or workspace.numel() >= pipeline.rs3.rs3_bank_copy_workspace_bytes(dst.U, keep.shape[1])
         for u in range(dst.U):
             if not -1 <= int(parent[u]) < src.U:
                 status.fill_(pipeline.rs3.RS3_EINVAL)
@@ -97,3 +99,18 @@ def test_a_unit_that_the_copy_leaves_keeps_its_tracker(fork):
     b.bank.full = []
     a.fork(parents(-1, 2, -1), into=b)                     # (a copy counted before is not taken for this one's)
     assert torch.equal(b.track[1], a.track[2]) and torch.equal(b.track[2], was[2])
+
+
+@pytest.mark.parametrize("U", [1, 2, 5])
+def test_a_target_with_another_number_of_units(fork, U):
+    """The workspace is the target's, a unit of its own each; trackers go by the parents."""
+    a, b = fork.make(3, 100), fork.make(U, 500)
+    p = parents(2, 0, -1, 2, 1)[:U]
+    was = b.track.clone()
+    a.fork(p, torch.ones((U, 5000), dtype=torch.uint8), into=b)
+    for u in range(U):
+        assert torch.equal(b.track[u], was[u] if p[u] < 0 else a.track[int(p[u])])
+    for bad in (p[:-1], torch.cat([p, p])):
+        with pytest.raises(ValueError):
+            a.fork(bad, into=b)
+    assert len(fork.calls) == 1                            # (nothing was copied)
