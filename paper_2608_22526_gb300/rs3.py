@@ -147,6 +147,11 @@ def _want(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int):
     if t.dtype != dtype or t.numel() < numel:
         raise ValueError(f"{name}: at least {numel} elements of {dtype} wanted, got {tuple(t.shape)} of {t.dtype}")
 
+def _want_workspace(dev: int, t: Optional[torch.Tensor]):
+    """A workspace on device `dev`, or none (its size is the library's to check)."""
+    if t is not None and t.get_device() != dev and t.numel():
+        raise ValueError("workspace is not on the current CUDA device")
+
 
 # ---------------------------------------------------------------------------
 # small helpers
@@ -354,6 +359,7 @@ def rs3_bank_copy(dst: Bank, src: Bank, parent, keep, workspace, status, stream=
             raise ValueError("keep: one row per destination unit")
         _want(dev, "keep", keep, torch.uint8, dst.U)
         stride = keep.shape[1]
+    _want_workspace(dev, workspace)
     rc = lib.rs3_bank_copy(ctypes.byref(dst.desc), ctypes.byref(src.desc), _ptr(parent), _ptr(keep), stride,
                            _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
     _check(rc, "rs3_bank_copy")
@@ -416,6 +422,7 @@ def rs3_block_select(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group,
     _want(dev, "digest", digest, torch.int8, n * bank.d)
     _want(dev, "step", step, torch.float32, n)
     _want(dev, "sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    _want_workspace(dev, workspace)
     rc = lib.rs3_block_select(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
                               ctypes.byref(bank.desc), block, _ptr(digest), _ptr(step), _ptr(rope), n_top, _ptr(sel),
                               _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
@@ -433,6 +440,7 @@ def rs3_sparse_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
     """rs3_memory_readout over the blocks that sel lists for each query and head."""
     dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
     _want(dev, "sel", sel, torch.int32, bank.U * bank.H * k_max * n_top)
+    _want_workspace(dev, workspace)
     if residual is not None:
         _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
     _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
