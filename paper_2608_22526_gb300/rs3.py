@@ -147,6 +147,12 @@ def _want(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int):
     if t.dtype != dtype or t.numel() < numel:
         raise ValueError(f"{name}: at least {numel} elements of {dtype} wanted, got {tuple(t.shape)} of {t.dtype}")
 
+def _want_bank(dev: int, bank: "Bank"):
+    """A bank whose storage is on device `dev`."""
+    if bank.k_store.get_device() != dev:
+        raise ValueError("the bank is not on the current CUDA device")
+
+
 def _want_workspace(dev: int, t: Optional[torch.Tensor]):
     """A workspace on device `dev`, or none (its size is the library's to check)."""
     if t is not None and t.get_device() != dev and t.numel():
@@ -333,6 +339,7 @@ def rs3_bank_reset(bank: Bank, unit: int = -1, stream=None):
 def rs3_bank_drop_frames(bank: Bank, n_oldest, n_newest, status, stream=None):
     """Gives up the n_oldest[u] oldest and n_newest[u] newest ring frames of every unit."""
     dev = torch.cuda.current_device()
+    _want_bank(dev, bank)
     if n_oldest is not None:
         _want(dev, "n_oldest", n_oldest, torch.int32, bank.U)
     if n_newest is not None:
@@ -351,6 +358,8 @@ def rs3_bank_copy(dst: Bank, src: Bank, parent, keep, workspace, status, stream=
     """Unit u of dst becomes the kept rows of unit parent[u] of src (-1: left as it
     is); keep: uint8 [dst.U, at least the parents' length] over logical rows, or None."""
     dev = torch.cuda.current_device()
+    _want_bank(dev, dst)
+    _want_bank(dev, src)
     _want(dev, "parent", parent, torch.int32, dst.U)
     _want(dev, "status", status, torch.int32, 1)
     stride = 0
@@ -388,6 +397,7 @@ def rs3_bank_digest(bank: Bank, block: int, refresh: int, digest, step, status, 
     """Digests (int8 [U, H, blocks, d] and their steps fp32 [U, H, blocks]) of the
     blocks of the `refresh` newest ring frames, or of all blocks (-1)."""
     dev, n = torch.cuda.current_device(), _block_heads(bank, block)
+    _want_bank(dev, bank)
     _want(dev, "digest", digest, torch.int8, n * bank.d)
     _want(dev, "step", step, torch.float32, n)
     _want(dev, "status", status, torch.int32, 1)
@@ -398,6 +408,7 @@ def rs3_bank_digest(bank: Bank, block: int, refresh: int, digest, step, status, 
 
 def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status):
     dev = torch.cuda.current_device()
+    _want_bank(dev, bank)
     _want(dev, "q", q, TORCH_DTYPES[dtype], G * mn * H * d)
     _want(dev, "unit_group", unit_group, torch.int32, bank.U)
     _want(dev, "idx", idx, torch.int32, bank.U * k_max)

@@ -76,3 +76,13 @@ def test_a_copy_without_a_mask_takes_an_empty_workspace_from_anywhere(calls):
     _, reached, make, _ = calls
     make.rs3_bank_copy(keep=None, ws=torch.zeros(0, dtype=torch.uint8))
     assert reached == ["rs3_bank_copy"]
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_a_bank_elsewhere_is_refused(calls, name):
+    _, reached, make, bank = calls
+    other = types.SimpleNamespace(**{**vars(bank), **{part: torch.zeros(4) for part in ("k_store", "v_store", "meta")}})
+    for args in ([dict(bank=other), dict(dst=other)] if name == "rs3_bank_copy" else [dict(bank=other)]):
+        with pytest.raises(ValueError, match="bank"):
+            getattr(make, name)(**args)
+    assert not reached
