@@ -450,8 +450,9 @@ rs3_status rs3_memory_readout_run(const void *q, rs3_dtype dtype, int G, int mn,
  * unit's storage (-1 for an uninitialised bank).
  *
  * 8-bit vectors.  A vector x is held as whole numbers t with |t| <= 127 and a step:
- *   e = floor(log2 max|x|), t = rint(x 2^(6-e)) cut to [-127, 127], step 2^(e-6);
- * a vector with max|x| < 2^-100 is t = 0, step 0.  t . t' * step is exact in fp32.
+ *   e = min(floor(log2 max|x|), 110), t = rint(x 2^(6-e)) cut to [-127, 127], step 2^(e-6);
+ * a vector with max|x| < 2^-100 is t = 0, step 0, and a NaN in it counts as 0.  t . t' * step
+ * is exact in fp32, and finite whatever the keys are.
  */
 int64_t rs3_bank_blocks(const rs3_bank *bank, int block);
 
@@ -492,8 +493,8 @@ size_t rs3_block_select_workspace_bytes(int U, int H, int k_max, int n_blocks);
  *   workspace device, >= rs3_block_select_workspace_bytes(U, H, k_max, blocks)
  *         bytes, 16-byte aligned; one call at a time
  * Limits: d a power of two in [16, 256], n_top <= 1024, k_max <= mn, at most 49152
- * blocks per unit, else RS3_EUNSUPPORTED (RS3_EINVAL for k_max); block means below
- * 2^111, so that no score passes the largest fp32 number.  A unit with a count * outside [0, k_max] or a group outside [0, G) latches RS3_EINVAL and is skipped; a
+ * blocks per unit, else RS3_EUNSUPPORTED (RS3_EINVAL for k_max).  A unit with a count
+ * outside [0, k_max] or a group outside [0, G) latches RS3_EINVAL and is skipped; a
  * cell outside [0, mn) latches it and that query gets some blocks.  RS3_ETIMEOUT as
  * for the readout (rs3_set_wait_limit_ns).
  */

@@ -41,15 +41,16 @@ __device__ __forceinline__ bool sparse_unit(const SparseArgs &a, int u, bool lat
 }
 
 // The 8-bit form of a vector whose largest element is `amax`: whole numbers t with
-// |t| <= 127, standing for t * step, step a power of two: e = floor(log2 amax),
+// |t| <= 127, standing for t * step, step a power of two: e = min(floor(log2 amax), 110),
 // t = rint(x 2^(6 - e)) cut to 127, step = 2^(e - 6).  Scaling by a power of two is exact, so a
 // score t . t' * step never rounds: |t . t'| <= 127^2 * 256 < 2^22, whatever the order of its
-// sums.  Vectors below 2^-100 are zeros with step 0.
+// sums, and with steps up to 2^104 it is finite: every live block has a rank.  Vectors below 2^-100 are
+// zeros with step 0.  A NaN is a 0 (maxima pass over it, and so does the conversion).
 struct EightBits {
     float up, step;
     __device__ __forceinline__ explicit EightBits(float amax)
     {
-        const int e = (int)(__float_as_uint(amax) >> 23) - 127;
+        const int e = min((int)(__float_as_uint(amax) >> 23) - 127, 110);
         const bool some = amax >= 7.888609052210118e-31f;
         up = some ? __uint_as_float((uint32_t)(133 - e) << 23) : 0.f;
         step = some ? __uint_as_float((uint32_t)(121 + e) << 23) : 0.f;

@@ -1309,3 +1309,58 @@ def test_fork_into_a_pipeline_with_another_number_of_units(rs3):
             if p >= 0:
                 n, at = int(length[u]), pipe.w.n_cond * pipe.w.mn
                 assert torch.equal(bits(wide.bank.k_store[u, at:at + n]), bits(pipe.bank.k_store[p, at:at + 180][on]))
+
+
+# ---------------------------------------------------------------------------
+# keys and scores that are no numbers
+# ---------------------------------------------------------------------------
+def eight_bits_of_anything(x):
+    """eight_bits() of the whole definition: a NaN counts as 0, and no step is above 2^104."""
+    x = np.nan_to_num(x.astype(np.float64), nan=0.0, posinf=np.inf, neginf=-np.inf)
+    a = np.abs(x).max(-1)
+    e = np.minimum(np.where(np.isinf(a), 110, np.frexp(np.where(np.isinf(a), 1.0, a))[1] - 1), 110)
+    some = a >= 2.0 ** -100
+    t = np.clip(np.rint(np.ldexp(x, (6 - e)[..., None])), -127, 127)
+    return np.where(some[..., None], t, 0), np.where(some, np.ldexp(1.0, e - 6), 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("U,k_max,rows,n_top", [(1, 5, 640, 20), (1, 5, 640, 3), (160, 9, 640, 20), (160, 9, 640, 4), (1, 5, 40_000, 60),
+                                                (1, 5, 40_000, 1024)])
+def test_digest_and_selection_of_keys_that_are_no_numbers(rs3, dtype, U, k_max, rows, n_top):
+    """Blocks with a NaN, an infinity, means past the largest number and means above 2^111: scores stay finite, so
+    every live block can be chosen, and no entry of a list is left unwritten."""
+    d, mn, nb = 64, 64, rows // 32
+    bank = rs3.Bank(U, 1, d, dtype, mn, 0, -1, rows, 4, 0)
+    st, g = status(), gen(rows + n_top)
+    k = torch.randn((U, nb, 32, d), generator=g, device="cuda").to(DT[dtype])
+    b = torch.arange(nb, device="cuda") % 6
+    k[:, b == 0, 3, 1] = math.nan
+    k[:, b == 1, 7, 2] = -math.inf
+    k[:, b == 2] = -3e38
+    k[:, b == 3, :, 5] = 1e35
+    k[:, b == 4, :, 9] = -1e36
+    bank.k_store.copy_(k.view(U, rows, d))
+    bank.counters[:, 1] = rows                             # as if the ring had been filled
+    dig, step = torch.full((U, 1, nb, d), 77, dtype=torch.int8, device="cuda"), torch.full((U, 1, nb), 0.5, device="cuda")
+    rs3.rs3_bank_digest(bank, 32, -1, dig, step, st)
+    assert int(st) == 0
+    x = k.float().view(U, nb, 4, 8, d)
+    p = x[:, :, 0]
+    for i in range(1, 4):
+        p = p + x[:, :, i]
+    s = ((p[:, :, 0] + p[:, :, 4]) + (p[:, :, 2] + p[:, :, 6])) + ((p[:, :, 1] + p[:, :, 5]) + (p[:, :, 3] + p[:, :, 7]))
+    t, e = eight_bits_of_anything((s / 32).cpu().numpy())
+    assert np.array_equal(dig[:, 0].cpu().numpy(), t.astype(np.int8)) and np.array_equal(step[:, 0].cpu().numpy(), e.astype(np.float32))
+    q = torch.randn((1, mn, d), generator=g, device="cuda").to(DT[dtype])
+    q[0, 1, 3], q[0, 2, 4], q[0, 3] = math.nan, math.inf, math.nan
+    idx = torch.arange(k_max, dtype=torch.int32, device="cuda").expand(U, k_max).contiguous()
+    sel = torch.full((U, 1, k_max, n_top), -5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(U, 1, k_max, nb), dtype=torch.uint8, device="cuda")
+    count, zero = torch.full((U,), k_max, dtype=torch.int32, device="cuda"), torch.zeros(U, dtype=torch.int32, device="cuda")
+    rs3.rs3_block_select(q, dtype, 1, mn, 1, d, zero, idx, count, k_max, bank, 32, dig, step, None, n_top, sel, ws, st)
+    assert int(st) == 0
+    tq, _ = eight_bits_of_anything(q[0, :k_max].float().cpu().numpy())
+    score = (torch.from_numpy(tq).cuda() @ torch.from_numpy(t).cuda().transpose(1, 2)) * torch.from_numpy(e).cuda()[:, None]
+    best = score.argsort(dim=-1, descending=True, stable=True)[..., :n_top].sort(-1).values
+    assert torch.equal(sel[:, 0].long(), best)
