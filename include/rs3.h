@@ -515,7 +515,8 @@ size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_
  * those that sel[u][h][j][0..n_top) lists (as rs3_block_select writes it; entries
  * below 0 are skipped, one at or past the number of blocks latches RS3_EINVAL and
  * is skipped, a block listed twice counts twice).  A query whose blocks hold no
- * live row reads A = 0.  Arguments and results otherwise as rs3_memory_readout;
+ * live row, or whose scores are all minus infinity, reads A = 0; a score that is NaN or plus infinity
+ * makes its query's head NaN.  Arguments and results otherwise as rs3_memory_readout;
  * idx holds distinct cells; a cell outside [0, mn) latches RS3_EINVAL and is
  * skipped, a count outside [0, k_max] latches it and the unit is skipped.
  *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, 16-byte

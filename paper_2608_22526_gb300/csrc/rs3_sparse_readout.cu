@@ -70,6 +70,14 @@ struct Row<float> {
     }
 };
 
+// The larger of two scores, NaN where either is: a maximum that passed over a NaN would drop rows whose scores are all NaN.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 constexpr int GATHER_WARPS = 16;           // at most
 
 // A CTA per (query, head): its warps take the listed blocks in turn.  L lanes hold a row (ITEMS
@@ -167,12 +175,12 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
 #pragma unroll
             for (int f = 0; f < GATHER_FLIGHT; ++f) {
                 if (!live[f]) x[f] = -INFINITY;
-                top = fmaxf(top, x[f]);
+                top = max_nan(top, x[f]);
             }
 #pragma unroll
-            for (int k = L; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-            if (top == -INFINITY) continue;                  // no live row (uniform)
-            const float m1 = fmaxf(m, top), keep = exp2f(m - m1);
+            for (int k = L; k < 32; k <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, k));
+            if (top == -INFINITY) continue;                  // no row that weighs anything (uniform)
+            const float m1 = max_nan(m, top), keep = exp2f(m - m1);
             m = m1;
             l *= keep;
 #pragma unroll
@@ -211,10 +219,10 @@ __global__ void __launch_bounds__(32 * GATHER_WARPS) k_attend_gather(AttendArgs 
     __syncthreads();
     if (threadIdx.x >= s.d / N) return;
     float top = -INFINITY, total = 0.f, y[N];
-    for (int w = 0; w < n_warps; ++w) top = fmaxf(top, s_m[w]);
+    for (int w = 0; w < n_warps; ++w) top = max_nan(top, s_m[w]);
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = 0.f;
-    if (top > -INFINITY) {
+    if (top != -INFINITY) {
         for (int w = 0; w < n_warps; ++w) {
             const float f = exp2f(s_m[w] - top);
             total = fmaf(f, s_l[w], total);
@@ -737,7 +745,7 @@ k_attend_blocks(AttendArgs a, BlockWork w, const __grid_constant__ CUtensorMap t
                         sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
                         if (entry[y] < 0) continue;
                         const int64_t slot = (pair0 + entry[y]) * w.parts + s_item[i].part % w.parts;
-                        if (t == 0) w.ml[slot] = make_float2(mx[y], sum[y]);
+                        if (t == 0) w.ml[slot] = make_float2(sum[y] == sum[y] ? mx[y] : sum[y], sum[y]);   // (NaN for the join)
                         float *dst = w.o + slot * D + 2 * t;
 #pragma unroll
                         for (int x = 0; x < D / 8; ++x)
@@ -939,7 +947,7 @@ __global__ void __launch_bounds__(Fp32Tile<D, PR>::THREADS) k_attend_blocks_fp32
                     const int e = __shfl_sync(0xffffffffu, entry.x, q);
                     if (e < 0) continue;               // (the same for the warp)
                     const int64_t slot = ((int64_t)it.uh * s.k_max * s.n_top + e) * w.parts + it.part % w.parts;
-                    if (lane == 0) w.ml[slot] = make_float2(mx[q], sum[q]);
+                    if (lane == 0) w.ml[slot] = make_float2(sum[q] == sum[q] ? mx[q] : sum[q], sum[q]);     // (NaN for the join)
 #pragma unroll
                     for (int v = 0; v < V4; ++v) {
                         float *dst = w.o + slot * D + 128 * v + COLS * lane;
@@ -1003,7 +1011,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
             }
         float top = m;
 #pragma unroll
-        for (int f = 0; f < F; ++f) top = fmaxf(top, ml[f].x);
+        for (int f = 0; f < F; ++f) top = max_nan(top, ml[f].x);
         if (top == -INFINITY) continue;
         const float keep = exp2f(m - top);
         m = top;
@@ -1022,10 +1030,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
         __syncthreads();
         if (part % G != 0) return;
 #pragma unroll
-        for (int x = 1; x < G; ++x) m = fmaxf(m, s_ml[part + x].x);
+        for (int x = 1; x < G; ++x) m = max_nan(m, s_ml[part + x].x);
         y = make_float4(0.f, 0.f, 0.f, 0.f);
         l = 0.f;
-        if (m > -INFINITY)
+        if (m != -INFINITY)
 #pragma unroll
             for (int x = 0; x < G; ++x) {
                 const float e = exp2f(s_ml[part + x].x - m);
@@ -1035,7 +1043,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_blocks(AttendArgs a, Bloc
             }
     }
     if (!here) return;
-    if (m > -INFINITY) {
+    if (m != -INFINITY) {
         const float inv = 1.f / l;
         y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
     }

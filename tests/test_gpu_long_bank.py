@@ -1364,3 +1364,66 @@ def test_digest_and_selection_of_keys_that_are_no_numbers(rs3, dtype, U, k_max, 
     score = (torch.from_numpy(tq).cuda() @ torch.from_numpy(t).cuda().transpose(1, 2)) * torch.from_numpy(e).cuda()[:, None]
     best = score.argsort(dim=-1, descending=True, stable=True)[..., :n_top].sort(-1).values
     assert torch.equal(sel[:, 0].long(), best)
+
+
+@pytest.mark.parametrize("dtype,H,d,n", [("bf16", 2, 64, 9), ("bf16", 1, 256, 5), ("f32", 2, 64, 9), ("bf16", 2, 64, 300), ("bf16", 1, 256, 300),
+                                         ("f32", 2, 64, 300), ("f32", 2, 256, 300), ("bf16", 2, 32, 300)])
+@pytest.mark.parametrize("block,n_top", [(32, 21), (64, 11)])
+def test_sparse_readout_of_scores_that_are_no_numbers(rs3, dtype, H, d, n, block, n_top):
+    """A NaN key, query or value that counts makes its results NaN, wherever its row lies; a score of minus infinity is a
+    weight of nothing, and queries whose blocks hold no such row are as without them."""
+    b = Built(rs3, U=1, H=H, d=d, dtype=dtype, m=20, n=20, window=-1, ring_frames=8, commits=8, n_ptr=3, seed=n_top)
+    nb = b.bank.blocks(block)
+    q, idx, count, group = queries(b, 1, n, [n])
+    sel = torch.rand((1, H, n, nb), generator=gen(3), device="cuda").argsort(-1)[..., :n_top].to(torch.int32).contiguous()
+    sel[0, :, 1] = 0                                       # two queries of one block each
+    sel[0, :, 2] = 20
+    sel[0, :, 1:3, 1:] = -1
+    sel[0, :, 3, 0] = 27
+    rows = torch.from_numpy(b.places(0)[0]).cuda()
+
+    def read():
+        out = torch.zeros((1, b.mn, b.D), dtype=DT[dtype], device="cuda")
+        run_readout(rs3, b, q, idx, count, group, sel, None, block, 0.0, None, out, 1)
+        assert int(b.st) == 0
+        return out[0, idx[0].long()].view(n, H, d)
+
+    def listed(blocks):                                    # [n, H]: the query's list holds one of them
+        return torch.stack([(sel[0] == x).any(-1) for x in blocks]).any(0).T
+
+    good = read()
+    assert not good.isnan().any()
+    whole = rows[rows // block == 20]
+    one = rows[rows // block == 24][-1:]
+    keys, values = b.bank.k_store.clone(), b.bank.v_store.clone()
+    # every key of a block, and one key of another
+    b.bank.k_store[0, whole] = math.nan
+    b.bank.k_store[0, one, d // 2] = math.nan              # (the first head's)
+    got, hit = read(), listed([20])
+    hit[:, 0] |= listed([24])[:, 0]
+    assert hit.any() and not hit.all() and got[hit].isnan().all() and torch.equal(bits(got[~hit]), bits(good[~hit]))
+    # a value
+    b.bank.k_store.copy_(keys)
+    b.bank.v_store[0, one, 3] = math.nan
+    got, hit = read(), listed([24])[:, 0]
+    assert got[hit, 0, 3].isnan().all()
+    got[:, 0, 3] = good[:, 0, 3]
+    assert torch.equal(bits(got), bits(good))
+    # a query
+    b.bank.v_store.copy_(values)
+    was = q.clone()
+    q[0, idx[0, 3].long(), 1] = math.nan
+    got = read()
+    assert got[3, 0].isnan().all()
+    got[3, 0] = good[3, 0]
+    assert torch.equal(bits(got), bits(good))
+    # scores of minus infinity: a block of them counts for nothing, and a query that reads no other row gets A = 0
+    q.copy_(was)
+    q[0, :, ::d] = q[0, :, ::d].abs() + 1
+    good = read()
+    b.bank.k_store[0, whole] = 0
+    b.bank.k_store[0, whole, ::d] = -math.inf
+    got = read()
+    sel[sel == 20] = -1
+    want = read()
+    assert not got.isnan().any() and not got[2].any() and torch.equal(bits(got), bits(want))
