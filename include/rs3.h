@@ -309,7 +309,8 @@ size_t rs3_bank_copy_workspace_bytes(int U, int64_t keep_stride);
  * `dst` may be `src` itself: unit u with parent[u] = u then stays as it is (with
  * `keep`: RS3_EINVAL), and a parent p of another unit must itself stay as it is
  * (parent[p] = -1, or p without `keep`), else that unit latches RS3_EINVAL.
- * Banks whose storage overlaps otherwise are refused (RS3_EINVAL).
+ * Banks whose storage overlaps otherwise, or is the same in another layout, are
+ * refused (RS3_EINVAL).
  */
 rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, const int32_t *parent,
                          const uint8_t *keep, int64_t keep_stride, void *workspace,

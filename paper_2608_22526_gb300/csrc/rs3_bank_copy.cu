@@ -414,13 +414,18 @@ extern "C" rs3_status rs3_bank_copy(const rs3_bank *dst, const rs3_bank *src, co
     if (keep && workspace_bytes < rs3_bank_copy_workspace_bytes(dst->U, keep_stride)) return RS3_ECAPACITY;
     const int64_t row_bytes = (int64_t)dst->D * (int64_t)elem_bytes(dst->dtype);
     const bool same = dst->k_store == src->k_store && dst->v_store == src->v_store && dst->meta == src->meta;
-    if (same && (dst->U != src->U || dst->rows_per_unit != src->rows_per_unit || dst->max_frames != src->max_frames))
-        return RS3_EINVAL;
+    if (same && (dst->U != src->U || dst->pinned_cap != src->pinned_cap || dst->ring_cap != src->ring_cap || dst->n_ptr != src->n_ptr ||
+                 dst->max_frames != src->max_frames))
+        return RS3_EINVAL;                         // one storage in two layouts
     const int64_t sb = src->U * src->rows_per_unit * row_bytes, db = dst->U * dst->rows_per_unit * row_bytes;
-    if (!same)
+    const int64_t sm = src->U * src->meta_stride, dm = dst->U * dst->meta_stride;
+    if (!same) {
         for (const void *d : {dst->k_store, dst->v_store})
-            if (overlap(d, db, src->k_store, sb) || overlap(d, db, src->v_store, sb)) return RS3_EINVAL;
-    if (!same && overlap(dst->meta, dst->U * dst->meta_stride, src->meta, src->U * src->meta_stride)) return RS3_EINVAL;
+            if (overlap(d, db, src->k_store, sb) || overlap(d, db, src->v_store, sb) || overlap(d, db, src->meta, sm)) return RS3_EINVAL;
+        for (const void *s : {src->k_store, src->v_store})
+            if (overlap(dst->meta, dm, s, sb)) return RS3_EINVAL;
+        if (overlap(dst->meta, dm, src->meta, sm)) return RS3_EINVAL;
+    }
     if (row_bytes > (1 << 20)) return RS3_EUNSUPPORTED;
     CopyArgs a = {};
     a.U = dst->U;

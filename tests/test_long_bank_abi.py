@@ -167,3 +167,19 @@ def test_binding_refuses_tensors_that_are_not_what_the_call_reads(b):
     for t in (torch.zeros(4, 6, 8)[:, :5], torch.zeros(6, 4, 8).transpose(0, 1), torch.zeros(4, 9), torch.zeros(8, 4).T):
         with pytest.raises(ValueError):
             b._rows_of("q", t, 8)
+
+
+def test_copy_refuses_one_storage_in_two_layouts(b):
+    """The same stores and counters, regions of other sizes; counters of one bank inside the rows of the other."""
+    def call(dst, src):
+        return b.lib.rs3_bank_copy(ctypes.byref(dst), ctypes.byref(src), ONE, None, 0, None, 0, ONE, None)
+
+    src = _bank(b)                                         # 64 + 1000 + 4 rows
+    for over in (dict(n_cond=0, ring=1064), dict(ring=1003, n_ptr=1), dict(n_cond=0, ring=1000, n_ptr=68), dict(U=1),
+                 dict(max_frames=19), dict(ring=999)):
+        other = _bank(b, **over)
+        assert call(other, src) == b.RS3_EINVAL and call(src, other) == b.RS3_EINVAL, over
+    far = dict(k=1 << 41, v=1 << 42, meta=1 << 43)
+    inside = (1 << 20) + 4096
+    assert call(_bank(b, k=1 << 41, v=1 << 42, meta=inside), src) == b.RS3_EINVAL
+    assert call(_bank(b, **far), _bank(b, meta=(1 << 42) + 4096)) == b.RS3_EINVAL
