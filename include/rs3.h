@@ -547,8 +547,9 @@ rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int
  *   q, k         device [rows] rows of H*d elements, `stride` elements apart (a
  *                projection that holds queries, keys and values side by side is
  *                read in place)
- *   q_out, k_out device rows `out_stride` elements apart; may be the input itself
- *                with the same stride, and may not overlap it otherwise
+ *   q_out, k_out device rows `out_stride` elements apart; each may be its own input
+ *                with the same stride.  Rows that share a byte with q, k or the other
+ *                result otherwise are refused (RS3_EINVAL): the call's rows go in any order
  *   weight       device fp32 [d] or NULL (ones); 16-byte aligned
  *   keep         device uint8 [rows] or NULL: rows with 0 are neither read nor
  *                written (keys that no commit will store)

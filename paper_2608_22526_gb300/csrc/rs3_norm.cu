@@ -225,6 +225,27 @@ bool norm_side(NormSide &s, const void *x, int64_t rows, int64_t stride, int H, 
     return true;
 }
 
+// Rows of `width` bytes, a_stride and b_stride apart, share no byte: one ends before the other begins, or they are columns
+// of the same rows side by side.
+bool rows_apart(const uint8_t *a, int64_t a_rows, int64_t a_stride, int64_t a_width, const uint8_t *b, int64_t b_rows, int64_t b_stride,
+                int64_t b_width)
+{
+    if (a_rows == 0 || b_rows == 0) return true;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    if (x + (uintptr_t)((a_rows - 1) * a_stride + a_width) <= y || y + (uintptr_t)((b_rows - 1) * b_stride + b_width) <= x) return true;
+    if (a_stride != b_stride) return false;
+    const uintptr_t n = (uintptr_t)a_stride, off = x >= y ? (x - y) % n : (n - (y - x) % n) % n;      // of a's columns behind b's
+    return off >= (uintptr_t)b_width && off + (uintptr_t)a_width <= n;
+}
+
+// No result lies over an operand or the other result, but for its own operand in place.
+bool norm_apart(const NormSide &s, const NormSide &t, int64_t s_width, int64_t t_width)
+{
+    return (s.x == s.y || rows_apart(s.y, s.rows, s.y_stride, s_width, s.x, s.rows, s.x_stride, s_width)) &&
+           rows_apart(s.y, s.rows, s.y_stride, s_width, t.x, t.rows, t.x_stride, t_width) &&
+           rows_apart(s.y, s.rows, s.y_stride, s_width, t.y, t.rows, t.y_stride, t_width);
+}
+
 }  // namespace
 
 extern "C" rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_stride, int Hq, const float *q_weight,
@@ -242,6 +263,8 @@ extern "C" rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_
     if (!norm_side(s[0], q, q_rows, q_stride, Hq, q_weight, q_keep, q_out, q_out_stride, esz, d) ||
         !norm_side(s[1], k, k_rows, k_stride, Hk, k_weight, k_keep, k_out, k_out_stride, esz, d))
         return RS3_EINVAL;
+    const int64_t width[2] = {(int64_t)s[0].H * d * esz, (int64_t)s[1].H * d * esz};
+    if (!norm_apart(s[0], s[1], width[0], width[1]) || !norm_apart(s[1], s[0], width[1], width[0])) return RS3_EINVAL;
     const int pieces = d * esz / 16, items = pieces > 32 ? 2 : 1;
     int L = 1;
     while (L * items < pieces) L <<= 1;

@@ -1427,3 +1427,24 @@ def test_sparse_readout_of_scores_that_are_no_numbers(rs3, dtype, H, d, n, block
     sel[sel == 20] = -1
     want = read()
     assert not got.isnan().any() and not got[2].any() and torch.equal(bits(got), bits(want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_into_columns_of_the_same_rows(rs3, dtype):
+    """Results in other columns of the rows that hold the operands, and in the rows between."""
+    rows, H, d = 37, 2, 64
+    W = H * d
+    x = torch.randn((rows, 4 * W), generator=gen(4), device="cuda").to(DT[dtype])
+    was = x.clone()
+    col = [slice(i * W, (i + 1) * W) for i in range(4)]
+    rs3.rs3_qk_norm_rope(x[:, col[0]], x[:, col[3]], x[:, col[1]], x[:, col[1]], dtype, rows, H, H, d, eps=1e-6)
+    check_norm(x[:, col[3]], *norm_ref(was[:, col[0]].contiguous(), d, None, None, rows, 1e-6), dtype)
+    check_norm(x[:, col[1]], *norm_ref(was[:, col[1]].contiguous(), d, None, None, rows, 1e-6), dtype)
+    assert torch.equal(bits(x[:, col[0]]), bits(was[:, col[0]])) and torch.equal(bits(x[:, col[2]]), bits(was[:, col[2]]))
+    y = torch.randn((2 * rows, W), generator=gen(5), device="cuda").to(DT[dtype])
+    was = y.clone()
+    rs3.rs3_qk_norm_rope(y[::2], y[1::2], y[::2], torch.empty_like(y[::2]), dtype, rows, H, H, d, eps=1e-6)
+    check_norm(y[1::2], *norm_ref(was[::2].contiguous(), d, None, None, rows, 1e-6), dtype)
+    assert torch.equal(bits(y[::2]), bits(was[::2]))
+    with pytest.raises(RuntimeError):
+        rs3.rs3_qk_norm_rope(y[:-1], y[1:], None, None, dtype, rows, H, H, d)

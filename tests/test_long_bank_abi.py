@@ -183,3 +183,26 @@ def test_copy_refuses_one_storage_in_two_layouts(b):
     inside = (1 << 20) + 4096
     assert call(_bank(b, k=1 << 41, v=1 << 42, meta=inside), src) == b.RS3_EINVAL
     assert call(_bank(b, **far), _bank(b, meta=(1 << 42) + 4096)) == b.RS3_EINVAL
+
+
+def _at(n):
+    return ctypes.c_void_p(4096 + n)
+
+
+@pytest.mark.parametrize("over", [
+    # 64 rows of 4 heads of 64 in bf16 are 32 KB: rows of 512 bytes, adjacent or in rows of 1536 (queries, keys, values)
+    dict(qo=_at(16)),                                      # over its input, shifted by a piece
+    dict(qo=_at(512)),                                     # shifted by a row
+    dict(qo=_at(0), qs=512),                               # in place with rows further apart
+    dict(qo=_at(1 << 16), ko=_at(1 << 16)),                # both results in one place
+    dict(qo=_at(1 << 17)),                                 # queries' results over the keys
+    dict(qo=_at((1 << 17) + 32256)),                       # ... over their last row
+    dict(ko=_at(0)),                                       # keys' results over the queries
+    dict(k=_at(0), qo=_at(0)),                             # queries in place, the keys the same tensor
+    dict(q_stride=768, qo=_at(256), qs=768),               # columns that overlap
+    dict(q_stride=768, qo=_at(1280), qs=768),              # ... around the end of a row
+    dict(q_stride=768, k=_at(512), k_stride=768, qo=_at(0), qs=768, ko=_at(768), ks=768)])
+def test_norm_refuses_results_over_other_operands(b, over):
+    a = dict(q=_at(0), qo=_at(1 << 18), k=_at(1 << 17), ko=_at(1 << 19))
+    a.update(over)
+    assert _norm(b, **a) == b.RS3_EINVAL
