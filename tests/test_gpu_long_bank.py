@@ -1448,3 +1448,163 @@ def test_norm_into_columns_of_the_same_rows(rs3, dtype):
     assert torch.equal(bits(y[::2]), bits(was[::2]))
     with pytest.raises(RuntimeError):
         rs3.rs3_qk_norm_rope(y[:-1], y[1:], None, None, dtype, rows, H, H, d)
+
+
+# ---------------------------------------------------------------------------
+# sizes that take several CTAs, turns or operand blocks
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("stride", [20_064, 20_011])
+@pytest.mark.parametrize("keep", [0.0, 0.5, 0.98, 1.0])
+def test_copy_with_a_mask_of_thousands_of_rows(rs3, stride, keep):
+    """Parents of 4096, 4097 and some 20 000 rows: their kept rows are counted by several CTAs, and frames begin and end in
+    either part; aligned and unaligned mask rows."""
+    U, d, mn, frames, n_ptr = 3, 8, 1500, 14, 5
+    src = rs3.Bank(U, 1, d, "bf16", mn, 1, -1, 20_000, 20, n_ptr)
+    g, st = gen(stride), status()
+    for f in range(1 + frames):
+        k, v = (torch.randn((U, mn, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+        n = [[101, 285], [102, 285], [100, 1400]]
+        n = torch.tensor([x[min(f, 1)] for x in n], device="cuda")
+        mask = torch.rand((U, mn), generator=g, device="cuda").argsort(-1).argsort(-1) < n[:, None]
+        rs3.rs3_bank_commit(src, k, v, mask.to(torch.uint8), int(f == 0), st)
+    rs3.rs3_bank_set_pointers(src, *(torch.randn((U, n_ptr, d), generator=g, device="cuda").bfloat16() for _ in range(2)), st)
+    meta, table = rs3.rs3_bank_read_meta(src)
+    assert meta[:, 7].tolist() == [4096, 4097, 19_705]
+    parent = [2, 0, 2, 1]
+    dst = rs3.Bank(4, 1, d, "bf16", mn, 1, -1, 19_700, 14, n_ptr)
+    mask = (torch.rand((4, stride), generator=g, device="cuda") < keep).to(torch.uint8)
+    ws = torch.full((rs3.rs3_bank_copy_workspace_bytes(4, stride),), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(2):                                     # the second call finds the first's workspace and counters
+        rs3.rs3_bank_copy(dst, src, torch.tensor(parent, dtype=torch.int32, device="cuda"), mask, ws, st)
+    assert int(st) == 0 and dst.copies.tolist() == [2] * 4
+    got, got_table = rs3.rs3_bank_read_meta(dst)
+    for u, p in enumerate(parent):
+        cond, ring = int(meta[p, 2]), int(meta[p, 1])      # (heads at 0: nothing was evicted)
+        on = mask[u, :cond + ring + n_ptr] != 0
+        regions = [(torch.arange(cond), 0), (torch.arange(ring) + mn, mn), (torch.arange(n_ptr) + mn + 20_000, mn + 19_700)]
+        at = 0
+        for i, (rows, first) in enumerate(regions):
+            rows = rows.cuda()[on[at:at + rows.numel()]]
+            at += regions[i][0].numel()
+            for a, b in ((src.k_store, dst.k_store), (src.v_store, dst.v_store)):
+                assert torch.equal(bits(b[u, first:first + rows.numel()]), bits(a[p][rows]))
+        upto = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), on.long().cumsum(0)]).cpu().numpy()
+        want = upto[cond + table[p, :frames, 0]] - upto[cond], upto[cond + table[p, :frames].sum(-1)] - upto[cond + table[p, :frames, 0]]
+        assert np.array_equal(got_table[u, :frames, 0], want[0]) and np.array_equal(got_table[u, :frames, 1], want[1])
+        assert got[u].tolist() == [0, int(upto[cond + ring] - upto[cond]), int(upto[cond]), frames, 0, 1, int(upto[-1] - upto[cond + ring]),
+                                   int(upto[-1])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_top", [1, 4])
+@pytest.mark.parametrize("spread,rope", [(127, True), (1, False), (0, False)])
+def test_select_for_many_queries_of_wide_heads(rs3, dtype, n_top, spread, rope):
+    """Heads of 128 with few choices, which a tile of queries takes too: random digests, ties, nothing but ties."""
+    U, H, d, mn, k_max, rows = 80, 1, 128, 256, 150, 5000
+    bank = rs3.Bank(U, H, d, dtype, mn, 0, -1, rows, 4, 0)
+    bank.counters[:, 1] = torch.arange(U, device="cuda") * (rows // U)         # as if the rings had been filled so far
+    st, g, nb = status(), gen(spread + n_top), bank.blocks(32)
+    dig = (torch.randint(-max(1, spread), max(1, spread) + 1, (U, H, nb, d), generator=g, device="cuda") * (spread > 0)).to(torch.int8)
+    step = torch.randint(1, 3, (U, H, nb), generator=g, device="cuda").float() / 64
+    q = torch.randn((1, mn, d), generator=g, device="cuda").to(DT[dtype])
+    idx = torch.stack([torch.randperm(mn, generator=g, device="cuda")[:k_max] for _ in range(U)]).to(torch.int32)
+    count = torch.tensor([k_max - u % 7 for u in range(U)], dtype=torch.int32, device="cuda")
+    zero = torch.zeros(U, dtype=torch.int32, device="cuda")
+    table = rope_table(mn, d) if rope else None
+    sel = torch.full((U, H, k_max, n_top), -5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(rs3.rs3_block_select_workspace_bytes(U, H, k_max, nb), dtype=torch.uint8, device="cuda")
+    rs3.rs3_block_select(q, dtype, 1, mn, H, d, zero, idx, count, k_max, bank, 32, dig, step, table, n_top, sel, ws, st)
+    assert int(st) == 0
+    x = q[0].float().cpu().numpy()
+    if table is not None:
+        t, p = table.cpu().numpy(), x.reshape(mn, d // 2, 2)
+        c, s = t[..., 0], t[..., 1]
+        x = np.stack([p[..., 0] * c - p[..., 1] * s, p[..., 0] * s + p[..., 1] * c], -1).astype(np.float32).reshape(mn, d)
+    tq = torch.from_numpy(eight_bits(x)[0]).cuda()
+    for u in range(U):
+        n, live = int(count[u]), -(-int(bank.counters[u, 1]) // 32)
+        m = min(n_top, live)
+        score = (tq[idx[u, :n].long()] @ dig[u, 0, :live].double().T) * step[u, 0, :live].double()
+        best = score.argsort(dim=-1, descending=True, stable=True)[:, :m].sort(-1).values
+        assert torch.equal(sel[u, 0, :n, :m].long(), best), u
+        assert (sel[u, 0, :n, m:] == -1).all() and (sel[u, 0, n:] == -5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_digest_of_more_blocks_than_a_warp_s_first_turn(rs3, dtype):
+    """A warp looks 32 blocks ahead; units of over 384 blocks give it a second turn, and a third."""
+    U, d, rows = 160, 16, 26_000
+    bank = rs3.Bank(U, 1, d, dtype, 64, 0, -1, rows, 4, 0)
+    st, nb = status(), bank.blocks(32)
+    bank.k_store.normal_(generator=gen(5))
+    bank.counters[:, 0] = 1000                             # as if the rings had been filled: 1000 dead rows, then live ones
+    bank.counters[:, 1] = rows - 7
+    dig, step = torch.full((U, 1, nb, d), 77, dtype=torch.int8, device="cuda"), torch.full((U, 1, nb), 0.5, device="cuda")
+    rs3.rs3_bank_digest(bank, 32, -1, dig, step, st)
+    assert int(st) == 0
+    live = torch.zeros(nb * 32, dtype=torch.bool, device="cuda")
+    live[1000:rows - 7] = True
+    n = live.view(nb, 32).sum(-1).clamp(min=1).float()
+    for u in (0, 77, U - 1):
+        x = torch.zeros((nb * 32, d), device="cuda")
+        x[live] = bank.k_store[u].float()[live[:rows]]
+        x = x.view(nb, 4, 8, d)
+        p = x[:, 0]
+        for i in range(1, 4):
+            p = p + x[:, i]
+        s = ((p[:, 0] + p[:, 4]) + (p[:, 2] + p[:, 6])) + ((p[:, 1] + p[:, 5]) + (p[:, 3] + p[:, 7]))
+        t, e = eight_bits((s / n[:, None]).cpu().numpy())
+        assert np.array_equal(dig[u, 0].cpu().numpy(), t.astype(np.int8)) and np.array_equal(step[u, 0].cpu().numpy(), e.astype(np.float32))
+
+
+def test_captured_frames_read_what_frames_one_by_one_read(rs3):
+    """Frames replayed from a graph leave what the same frames leave when each call is made: results, choices, digests, rows."""
+    pipes, outs = [], []
+    for _ in range(2):
+        pipe, z, mask = small_pipeline()
+        pipe.use_blocks(32, 3)
+        pipe.digest(-1)
+        pipes.append(pipe)
+        outs.append(torch.zeros((2, pipe.w.mn, pipe.w.D), dtype=torch.bfloat16, device="cuda"))
+    k, v = (torch.randn((2, z.shape[1], z.shape[2]), generator=gen(6), device="cuda").bfloat16() for _ in range(2))
+
+    def frame(pipe, out):
+        pipe.select(z, mask)
+        pipe.select_blocks(z)
+        pipe.readout_blocks(z, None, out)
+        pipe.commit(k, v, mask, 0)
+        pipe.digest(1)
+
+    for p, o in zip(pipes, outs):
+        frame(p, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        frame(pipes[0], outs[0])
+    for _ in range(2):
+        graph.replay()
+        frame(pipes[1], outs[1])
+        torch.cuda.synchronize()
+        a, b = pipes
+        assert a.status_code() == 0 and b.status_code() == 0 and outs[1].any()
+        for x, y in ((outs[0], outs[1]), (a.bank.k_store, b.bank.k_store), (a.bank.v_store, b.bank.v_store)):
+            assert torch.equal(bits(x), bits(y))
+        for x, y in ((a.block_digest, b.block_digest), (a.block_step, b.block_step), (a.block_sel, b.block_sel), (a.bank.counters, b.bank.counters)):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 4, 64), ("bf16", 1, 256), ("f32", 2, 64)])
+def test_sparse_readout_repeats_itself(rs3, dtype, H, d):
+    """By block: entries of a block's list come in any order, the result's bits do not depend on it."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=24, n=24, window=-1, ring_frames=8, commits=8, n_ptr=3, seed=2)
+    n, nb = 500, b.bank.blocks(64)
+    q, idx, count, group = queries(b, 1, n, [n, n - 100])
+    sel = torch.rand((2, H, n, nb), generator=gen(3), device="cuda").argsort(-1)[..., :12].to(torch.int32).contiguous()
+    table = rope_table(b.mn, d)
+    first = None
+    for _ in range(5):
+        out = torch.zeros((2, b.mn, b.D), dtype=DT[dtype], device="cuda")
+        run_readout(rs3, b, q, idx, count, group, sel, table, 64, 0.0, None, out, 1)
+        assert int(b.st) == 0
+        first = out if first is None else first
+        assert torch.equal(bits(out), bits(first))
