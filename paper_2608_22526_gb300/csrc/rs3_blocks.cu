@@ -1537,12 +1537,22 @@ extern "C" rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, in
     a.step = step;
     a.sel = sel;
     a.bf16 = dtype == RS3_BF16;
-    // 128 queries to a CTA, where those keep half of the SMs busy and their candidates have room.  Over 990 blocks, 16 choices
-    // (128 queries to a CTA / 16): 64 queries in 32 heads (32 tiles) 38 / 16 us, 709 in 8 heads (48) 40 / 31, 256 in 32
-    // (64) 43 / 40, 384 in 32 (96) 42 / 54, 709 in 32 (192) 57 / 95, with 32 choices 92 / 117.
+    // 128 queries to a CTA, where those are at least one per SM and their candidates have room; the more choices, the more
+    // candidates are cut down again, and the more tiles it takes.  Tiles are counted by k_max, as the counts are on the device.
+    // Heads of 64 with all of k_max kept / with three fifths of it kept, L2 flushed, us (128 queries to a CTA : 16):
+    //   blocks   choices   48 tiles   80, 96             160, 192            240       320, 384             640 (heads of 32)
+    //   990      16        50 : 36    50 : 59, 56 : 37   64 : 101, 62 : 56   64 : 72   101 : 189, 70 : 99   107 : 184
+    //   990      24        62 : 39    62 : 63            78 : 109, 79 : 60   83 : 76   130 : 201, 101 : 105 144 : 193
+    //   990      32        70 : 44    72 : 70, 100 : 48  109 : 126, 111 : 66 117 : 85  165 : 238, 154 : 119 222 : 213
+    //   4 500    16                   183 : 148, 181 : 101  228 : 277, 181 : 185  218 : 263  224 : 353      380 : 690
+    //   4 500    24                   197 : 154          273 : 291, 199 : 193  236 : 273  261 : 369          433 : 720
+    //   4 500    32                   236 : 163, 228 : 116  363 : 310, 236 : 205  302 : 292  361 : 396      566 : 752
+    // Over 325 blocks 160 tiles 31 : 33 (16 choices), 320 tiles 60 : 54 (24).  Heads of 128, 4 choices, 990 blocks: 80 tiles 56 : 42,
+    // 160 tiles 58 : 68, 320 tiles 74 : 115; of 16, 160 tiles, 16 choices 56 : 58; fp32 as bf16.
     const int fixed = (TILE_ROWS + 2 * TILE_COLS) * 2 * (d < 64 ? 64 : d) + 1024, each = TILE_ROWS * 6;
     const int cap = (((106 * 1024 - fixed) / each / 4 - 1) | 1) * 4;       // an odd number of 16 bytes
-    if (2 * (int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS) >= rs3_sm_count() && n_top <= TILE_TOP && cap >= n_top + 48 &&
+    const int64_t tiles = (int64_t)a.s.U * H * ((k_max + TILE_ROWS - 1) / TILE_ROWS);
+    if (4 * tiles >= (int64_t)rs3_sm_count() * (n_top <= 16 ? 4 : n_top <= 24 ? 5 : 10) && n_top <= TILE_TOP && cap >= n_top + 48 &&
         a.s.nb <= 32 * TILE_WORDS) {
         TileArgs p = {a, cap, rs3_get_wait_limit_ns()};
         const size_t smem = (size_t)fixed + (size_t)cap * each;

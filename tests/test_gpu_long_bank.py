@@ -1608,3 +1608,11 @@ def test_sparse_readout_repeats_itself(rs3, dtype, H, d):
         assert int(b.st) == 0
         first = out if first is None else first
         assert torch.equal(bits(out), bits(first))
+
+
+@pytest.mark.parametrize("dtype,H,d,U,k_max,n_top,rows,spread,rope", [
+    ("bf16", 2, 64, 160, 40, 17, 20_000, 127, True), ("f32", 1, 32, 160, 250, 24, 9_000, 2, False), ("bf16", 4, 16, 160, 21, 25, 3_000, 2, True),
+    ("bf16", 4, 64, 160, 33, 32, 9_000, 127, False), ("f32", 4, 64, 160, 9, 32, 900, 0, False)])
+def test_select_for_more_choices_of_many_queries(rs3, dtype, H, d, U, k_max, n_top, rows, spread, rope):
+    """Several tiles of queries per SM, where more than 16 choices go by tiles too."""
+    test_select_for_many_queries(rs3, dtype, H, d, U, k_max, n_top, rows, spread, rope)
