@@ -305,7 +305,9 @@ size_t rs3_bank_copy_workspace_bytes(int U, int64_t keep_stride);
  * Both banks have the same H, d, dtype and mn (else RS3_EINVAL); their pinned,
  * ring, frame and pointer capacities may differ.  Status: RS3_EINVAL for a parent
  * outside [-1, src->U) or a mask row shorter than the parent, RS3_ECAPACITY for
- * rows or frames that do not fit; such a unit is left as it is, others proceed.
+ * rows or frames that do not fit, RS3_EINTERNAL for a parent whose counters are
+ * unsound; such a unit is left as it is, others proceed.  Rows of more than 1 MB are
+ * refused (RS3_EUNSUPPORTED).
  * `dst` may be `src` itself: unit u with parent[u] = u then stays as it is (with
  * `keep`: RS3_EINVAL), and a parent p of another unit must itself stay as it is
  * (parent[p] = -1, or p without `keep`), else that unit latches RS3_EINVAL.
@@ -524,7 +526,9 @@ size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_
  *         aligned; one call at a time
  * Calls with many queries go block by block, in bf16 on the tensor cores: there the
  * softmax's weights are rounded to bf16, and a query that is rotated here is too (a
- * query rotated before, by rs3_qk_norm_rope, has been rounded already).
+ * query rotated before, by rs3_qk_norm_rope, has been rounded already), as in
+ * rs3_memory_readout; calls with few queries keep both in fp32.  The path goes by the
+ * arguments' sizes (U, H, d, k_max, n_top, block), so that the last bits of a result do too.
  * Limits: those of rs3_block_select, without one on the blocks.  RS3_ETIMEOUT as for
  * the readout (rs3_set_wait_limit_ns).
  */

@@ -17,7 +17,6 @@ namespace {
 // ---------------------------------------------------------------------------
 struct DigestArgs {
     BankDev bank;
-    const uint8_t *k_store;
     int8_t *digest;
     float *step;
     int32_t *status;
@@ -922,7 +921,7 @@ constexpr int TILE_WORDS = 512;            // most words of a unit
 
 struct TileArgs {
     SelectArgs a;
-    int32_t cap;               // room for a query's candidates: n_top + 33 at least
+    int32_t cap;               // room for a query's candidates: n_top + 48 at least
     uint64_t wait_ns;          // limit of each wait
 };
 
@@ -1085,7 +1084,7 @@ struct Candidates {
 //                many (ties, or fewer groups than choices), they are cut down and the bound rises.
 // Then the candidates are cut to n_top.  Three warps spread the digests (fp16, 128-byte swizzle) a tile ahead, one issues
 // the products.  Per query this takes a third of k_score_blocks' instructions, but a CTA goes through all of the
-// blocks twice, so it is for calls whose queries fill the SMs: 23 700 queries over 990 blocks 65 us against 93, 757 over
+// blocks twice, so it is for calls whose queries fill the SMs: 23 264 queries over 990 blocks 65 us against 93, 757 over
 // 4 700 the other way round (74 against 46).  A step of 64 blocks takes some 1 600 cycles in the first pass and 2 100 in the
 // second, where a score's predicated stores fill the shared memory's pipe; the digests are there in time.  The maxima take
 // the whole of the warp's part of shared memory: in groups of 16 blocks where 8 have room, 16 choices took 70 us and
@@ -1474,7 +1473,6 @@ extern "C" rs3_status rs3_bank_digest(const rs3_bank *bank, int block, int refre
     if (nb == 0) return RS3_OK;
     DigestArgs a = {};
     a.bank = bank_dev(bank);
-    a.k_store = static_cast<const uint8_t *>(bank->k_store);
     a.digest = digest;
     a.step = step;
     a.status = status;

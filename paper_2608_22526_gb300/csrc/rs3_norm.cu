@@ -126,7 +126,7 @@ k_norm_rope(NormSide q, NormSide k, int mn, int d, float eps, const float *__res
     const uint8_t *src = s.x + row0 * s.x_stride + (head * pieces + lane) * 16;
     uint8_t *dst = s.y + row0 * s.y_stride + (head * pieces + lane) * 16;
     const int64_t x_turn = s.x_stride * mn, y_turn = s.y_stride * mn;
-    // the rows that are kept, a bit for each of this CTA's turns (32 at most): a group's lanes look them up
+    // the rows that are kept, a bit for each of this CTA's turns (NORM_TURNS at most): a group's lanes look them up
     uint32_t kept = 0;
 #pragma unroll
     for (int f = lane; f < NORM_TURNS; f += L) {

@@ -309,7 +309,7 @@ __device__ __forceinline__ uint4 rotate_piece(uint4 v, const float *f)
 // is computed by itself, so the result does not depend on it.  Out of place the launch's other CTAs
 // write out = residual (or zeros) on every cell, and with angles a further few rotate the kept queries once for all
 // of their blocks (in fp32; bf16 queries rounded to bf16 for the tensor cores).  Bound by latency: three cluster barriers and some
-// six dependent loads, 13 us for one head's 24 200 entries over 4 700 blocks and 16 for 32 heads' 379 000 over 990 with
+// six dependent loads, 13 us for one head's 24 200 entries over 4 700 blocks and 16 for 32 heads' 372 000 over 990 with
 // 17 MB passed through; with every CTA going through all of a head's entries for its share of the blocks 18 and 22.
 template <typename T>
 __global__ void __launch_bounds__(LIST_THREADS, 2) k_block_lists(AttendArgs a, BlockWork w, int64_t nvec)
@@ -513,9 +513,12 @@ struct BlockTile {
 // are taken in the order in which adjacent lanes can load 16 bytes of a row), the softmax of its rows in
 // registers, O = P V from those, and (m, l, O) stored for k_join_blocks.  No warp waits for another.
 // mma.sync: a block of a long bank has some 20 queries, so the call is bound by the bytes of K and V, and
-// tiles of 128 rows would be four fifths empty.  23 700 queries of 16 blocks in 32 heads of 64 (18 500 blocks, 303 MB read
-// and 97 MB of results): 75 us, 5.3 TB/s; the loads alone take 60.  757 queries of 32 blocks, one head of 256 (78 MB): 28 us,
-// 21 of them the loads with their start and end.  Seven warps and the producer leave 128 registers (255 at D = 256)
+// tiles of 128 rows would be four fifths empty.  23 264 queries of 16 blocks in 32 heads of 64 (18 538 blocks, 304 MB read
+// and 97 MB of results): 75 us, 5.3 TB/s; the loads alone take 60.  757 queries of 32 blocks, one head of 256 (1 278 blocks, 84 MB): 28 us,
+// 21 of them the loads with their start and end.  The weights are rounded to bf16 for the second product, as the dense
+// readout's are; their sum and every partial result stay fp32.  A weight is off by 2^-8 of itself at most, either way, and a
+// result by less: 7.1e-4 and 7.0e-4 from 64 bits in the two calls above, by its own rounding; fp32 weights give the same.  Seven warps
+// and the producer leave 128 registers (255 at D = 256)
 // where eight and it left 96.
 template <int D, int TR>
 __global__ void __launch_bounds__(BlockTile<D, TR>::THREADS, BlockTile<D, TR>::CTAS)
@@ -967,7 +970,7 @@ __global__ void __launch_bounds__(Fp32Tile<D, PR>::THREADS) k_attend_blocks_fp32
 // their running maximum, eight loads at a time, then the groups are joined:
 //   out = residual + sum_t 2^(m_t - M) O_t / sum_t 2^(m_t - M) l_t
 // Wide heads have few queries and much to load for each; for heads of 64 four groups a query took 33 us where
-// one took 21 (23 700 queries of 16 blocks; 18.5 since the attention leaves its results in L2).
+// one took 21 (23 264 queries of 16 blocks; 18.5 since the attention leaves its results in L2).
 constexpr int JOIN_THREADS = 256;
 
 template <typename T, int D>
@@ -1087,7 +1090,8 @@ WorkLayout work_layout(bool fp32, int64_t U, int64_t H, int64_t d, int64_t k_max
     return l;
 }
 
-// Whether a call's path may be by block, for which its workspace is sized.  Three launches against one, and every row
+// Whether a call's path may be by block, for which its workspace is sized: the kernels by block are built for heads of 64, 128 and
+// 256, and narrower heads are always by query.  Three launches against one, and every row
 // read once against once per query.  bf16, of one bank of 200 frames, blocks of 64 (by block / by query): 4 heads of 64,
 // 64 queries of 4 blocks 14.9 / 9.3 us, 128 of 4 15.5 / 15.4, 64 of 16 16.9 / 16.5, 128 of 16 18.5 / 30, 787 of 16
 // 29 / 129; one head of 256, 16 queries of 4 blocks 16.0 / 21, 64 of 4 17.0 / 22, 787 of 16 33 / 162.
