@@ -508,10 +508,16 @@ rs3_status rs3_block_select(const void *q, rs3_dtype dtype, int G, int mn, int H
                             void *workspace, size_t workspace_bytes, int32_t *status,
                             rs3_stream_t stream);
 
-/* Bytes of device workspace rs3_sparse_readout needs; never falls as U, H, k_max,
- * n_top or n_blocks grows. */
+/* Bytes of device workspace rs3_sparse_readout needs with blocks of any size; never
+ * falls as U, H, k_max, n_top or n_blocks grows. */
 size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks,
                                           rs3_dtype dtype);
+
+/* The same for blocks of `block` rows, of which a unit has n_blocks: enough for calls
+ * with this block, and for calls by block half as much for 32 and 64 rows (a quarter
+ * for 32 and half for 64 in fp32 heads of 128 and 256).  0 for a block that is none. */
+size_t rs3_sparse_readout_block_workspace_bytes(int U, int H, int d, int k_max, int n_top,
+                                                int n_blocks, rs3_dtype dtype, int block);
 
 /*
  * rs3_memory_readout where each query attends to the live rows of its own blocks:
@@ -522,8 +528,9 @@ size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_
  * makes its query's head NaN.  Arguments and results otherwise as rs3_memory_readout;
  * idx holds distinct cells; a cell outside [0, mn) latches RS3_EINVAL and is
  * skipped, a count outside [0, k_max] latches it and the unit is skipped.
- *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, 16-byte
- *         aligned; one call at a time
+ *   workspace device, >= rs3_sparse_readout_workspace_bytes(...) bytes, or
+ *         rs3_sparse_readout_block_workspace_bytes(..., block), 16-byte aligned; one call
+ *         at a time
  * Calls with many queries go block by block, in bf16 on the tensor cores: there the
  * softmax's weights are rounded to bf16, and a query that is rotated here is too (a
  * query rotated before, by rs3_qk_norm_rope, has been rounded already), as in

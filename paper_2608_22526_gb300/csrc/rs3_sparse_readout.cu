@@ -1203,11 +1203,24 @@ rs3_status launch_by_blocks(const AttendArgs &a, bool fp32, void *workspace, cud
 
 }  // namespace
 
-extern "C" size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks, rs3_dtype dtype)
+static size_t readout_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks, rs3_dtype dtype, int block)
 {
     if (U < 1 || H < 1 || d < 1 || k_max < 0 || n_top < 1 || n_blocks < 0) return 0;
     if (dtype != RS3_F32 && dtype != RS3_BF16) return 0;
-    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(dtype == RS3_F32, U, H, d, k_max, n_top, n_blocks, most_parts(dtype == RS3_F32, d)).total : 0);
+    const bool fp32 = dtype == RS3_F32;
+    return 16 + (sized_by_blocks(dtype, U, H, d, k_max, n_top) ? work_layout(fp32, U, H, d, k_max, n_top, n_blocks, block / part_rows(fp32, d, block)).total : 0);
+}
+
+extern "C" size_t rs3_sparse_readout_workspace_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks, rs3_dtype dtype)
+{
+    return readout_bytes(U, H, d, k_max, n_top, n_blocks, dtype, 128);
+}
+
+extern "C" size_t rs3_sparse_readout_block_workspace_bytes(int U, int H, int d, int k_max, int n_top, int n_blocks, rs3_dtype dtype,
+                                                           int block)
+{
+    if (block != 32 && block != 64 && block != 128) return 0;
+    return readout_bytes(U, H, d, k_max, n_top, n_blocks, dtype, block);
 }
 
 extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -1221,7 +1234,7 @@ extern "C" rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, 
     if (r != RS3_OK) return r;
     if (!sel || !out || !workspace || !(scale >= 0.f) || std::isinf(scale)) return RS3_EINVAL;
     if (!rs3_aligned16(out) || !rs3_aligned16(workspace) || (residual && !rs3_aligned16(residual))) return RS3_EINVAL;
-    if (workspace_bytes < rs3_sparse_readout_workspace_bytes(a.s.U, H, d, k_max, n_top, a.s.nb, dtype)) return RS3_ECAPACITY;
+    if (workspace_bytes < readout_bytes(a.s.U, H, d, k_max, n_top, a.s.nb, dtype, block)) return RS3_ECAPACITY;
     const bool blocks = a.s.nb > 0 && by_blocks(a.s, dtype);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     a.k_store = static_cast<const uint8_t *>(bank->k_store);

@@ -137,7 +137,7 @@ class Pipeline:
             self.block_sel = torch.full((w.U, w.H, max(self.k_max, 1), n_top), -1, dtype=torch.int32, device=dev)
             self.ws_blocks = torch.empty(rs3.rs3_block_select_workspace_bytes(w.U, w.H, self.k_max, nb), dtype=torch.uint8,
                                          device=dev)
-            self.ws_sparse = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(w.U, w.H, w.d, self.k_max, n_top, nb, w.dtype),
+            self.ws_sparse = torch.empty(rs3.rs3_sparse_readout_workspace_bytes(w.U, w.H, w.d, self.k_max, n_top, nb, w.dtype, block),
                                          dtype=torch.uint8, device=dev)
 
     def digest(self, refresh: int = 1):

@@ -74,6 +74,7 @@ SIGNATURES = {
     "rs3_block_select_workspace_bytes": (_SZ, [_I, _I, _I, _I]),
     "rs3_block_select": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _P, _P, _SZ, _P, _P]),
     "rs3_sparse_readout_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "rs3_sparse_readout_block_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I, _I, _I, _I]),
     "rs3_sparse_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _I, _P, _I, _P, _P, _P,
                                 ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_qk_norm_rope": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64,
@@ -441,8 +442,11 @@ def rs3_block_select(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group,
 
 
 def rs3_sparse_readout_workspace_bytes(U: int, H: int, d: int, k_max: int, n_top: int, n_blocks: int,
-                                       dtype: str) -> int:
-    return int(lib.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, n_blocks, DTYPES[dtype]))
+                                       dtype: str, block: Optional[int] = None) -> int:
+    """For blocks of any size, or for `block` rows (n_blocks of them), which takes a half or a quarter."""
+    if block is None:
+        return int(lib.rs3_sparse_readout_workspace_bytes(U, H, d, k_max, n_top, n_blocks, DTYPES[dtype]))
+    return int(lib.rs3_sparse_readout_block_workspace_bytes(U, H, d, k_max, n_top, n_blocks, DTYPES[dtype], block))
 
 
 def rs3_sparse_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int,

@@ -1616,3 +1616,21 @@ def test_sparse_readout_repeats_itself(rs3, dtype, H, d):
 def test_select_for_more_choices_of_many_queries(rs3, dtype, H, d, U, k_max, n_top, rows, spread, rope):
     """Several tiles of queries per SM, where more than 16 choices go by tiles too."""
     test_select_for_many_queries(rs3, dtype, H, d, U, k_max, n_top, rows, spread, rope)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("f32", 2, 64), ("f32", 2, 256), ("bf16", 1, 256)])
+@pytest.mark.parametrize("block", [32, 64, 128])
+def test_sparse_readout_stays_inside_the_workspace_of_its_block(rs3, dtype, H, d, block):
+    """By block with the smaller workspace: the same bits, and nothing is written behind it."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=24, n=24, window=-1, ring_frames=8, commits=8, n_ptr=3, seed=2)
+    n, n_top, nb = 500, 14, b.bank.blocks(block)
+    q, idx, count, group = queries(b, 1, n, [n, n - 100])
+    sel = torch.rand((2, H, n, nb), generator=gen(3), device="cuda").argsort(-1)[..., :n_top].to(torch.int32).contiguous()
+    table = rope_table(b.mn, d)
+    want, out = (torch.zeros((2, b.mn, b.D), dtype=DT[dtype], device="cuda") for _ in range(2))
+    run_readout(rs3, b, q, idx, count, group, sel, table, block, 0.0, None, want, 1)
+    size = rs3.rs3_sparse_readout_workspace_bytes(2, H, d, n, n_top, nb, dtype, block)
+    assert size > 1 << 20
+    room = torch.full((size + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+    rs3.rs3_sparse_readout(q, dtype, 1, b.mn, H, d, group, idx, count, n, b.bank, block, sel, n_top, table, None, out, 0.0, room[:size], b.st)
+    assert int(b.st) == 0 and torch.equal(bits(out), bits(want)) and (room[size:] == 0x5a).all()

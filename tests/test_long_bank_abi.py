@@ -206,3 +206,29 @@ def test_norm_refuses_results_over_other_operands(b, over):
     a = dict(q=_at(0), qo=_at(1 << 18), k=_at(1 << 17), ko=_at(1 << 19))
     a.update(over)
     assert _norm(b, **a) == b.RS3_EINVAL
+
+
+def test_readout_workspace_for_one_block_size(b):
+    """No more than for any block, what the call asks for, and never falling."""
+    x = _bank(b, U=3, H=2, mn=1024, ring=20_000, max_frames=40)
+    for dtype, code in (("bf16", 1), ("f32", 0)):
+        for d in (16, 64, 128, 256):
+            x = _bank(b, U=3, H=2, d=d, dtype=dtype, mn=1024, ring=20_000, max_frames=40)
+            for block in (32, 64, 128):
+                nb = b.lib.rs3_bank_blocks(ctypes.byref(x), block)
+                for k_max, n_top in ((4, 2), (700, 16)):
+                    n = b.rs3_sparse_readout_workspace_bytes(3, 2, d, k_max, n_top, nb, dtype, block)
+                    most = b.rs3_sparse_readout_workspace_bytes(3, 2, d, k_max, n_top, nb, dtype)
+                    if d < 64 or k_max == 4:
+                        assert n == most == 16
+                    else:
+                        # partial results in fp32 are nearly all of it: rows of a part in bytes
+                        parts = block // (32 if block == 32 or (dtype == "f32" and d > 64) else 64)
+                        assert parts * 3 * 2 * k_max * n_top * d * 4 < n <= most and (n == most) == (block == 128)
+                    args = [ONE, code, 1, 1024, 2, d, ONE, ONE, ONE, k_max, ctypes.byref(x), block, ONE, n_top, None, None, ONE, 0.0, ONE]
+                    assert b.lib.rs3_sparse_readout(*args, n - 1, ONE, None) == b.RS3_ECAPACITY
+    assert b.rs3_sparse_readout_workspace_bytes(1, 1, 64, 1, 1, 1, "bf16", 16) == 0
+    grow = [(1, 1, 1, 1, 1), (1, 1, 9, 4, 100), (1, 3, 9, 4, 100), (5, 3, 1228, 4, 100), (5, 3, 1228, 32, 5000), (48, 4, 2764, 64, 9000)]
+    for block in (32, 64, 128):
+        sizes = [b.rs3_sparse_readout_workspace_bytes(U, H, 64, k, n, nb, "bf16", block) for U, H, k, n, nb in grow]
+        assert sizes == sorted(sizes) and sizes[0] > 0
