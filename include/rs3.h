@@ -560,7 +560,8 @@ rs3_status rs3_sparse_readout(const void *q, rs3_dtype dtype, int G, int mn, int
  *                read in place)
  *   q_out, k_out device rows `out_stride` elements apart; each may be its own input
  *                with the same stride.  Rows that share a byte with q, k or the other
- *                result otherwise are refused (RS3_EINVAL): the call's rows go in any order
+ *                result otherwise are refused (RS3_EINVAL), as the call's rows go in any
+ *                order, and so are rows of another stride that lie among them
  *   weight       device fp32 [d] or NULL (ones); 16-byte aligned
  *   keep         device uint8 [rows] or NULL: rows with 0 are neither read nor
  *                written (keys that no commit will store)

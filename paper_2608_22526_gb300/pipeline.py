@@ -164,11 +164,12 @@ class Pipeline:
         return self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
 
     def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, into: Optional["Pipeline"] = None) -> "Pipeline":
-        """A pipeline (`into`, or a new one with this one's sizes; `into` may have another number of units) whose unit u holds the rows
-        of this one's unit parent[u], those that keep[u] leaves, and its tracker.  A unit that the copy
-        leaves as it is (`into`'s status tells why) keeps its tracker too.  Digests are
-        not copied: the target's digest(-1) follows.  The copy runs on this pipeline's stream; where `into` has another, it comes after what was issued there, and what is issued
-        there next comes after it."""
+        """A pipeline (`into`, or a new one with this one's sizes; `into` may have another number of units)
+        whose unit u holds the rows of this one's unit parent[u], those that keep[u] leaves, and its
+        tracker.  A unit that the copy leaves as it is (`into`'s status tells why) keeps its tracker
+        too.  Digests are not copied: the target's digest(-1) follows.  The copy runs on this pipeline's
+        stream; where `into` has another, it comes after what was issued there, and what is issued there
+        next comes after it."""
         U = self.w.U if into is None else into.w.U
         if parent.shape != (U,):
             raise ValueError(f"parent: one for each of the {U} units wanted, got {tuple(parent.shape)}")

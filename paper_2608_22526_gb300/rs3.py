@@ -294,7 +294,7 @@ class Bank:
         # per unit, on the device: {head, tail, cond_len, n_frames, oldest, n_cond_frames, ptr_len},
         # int64 [U, 7], a view of the bank's own
         self.counters = self.meta.view(U, -1)[:, :7]
-        # int64 [U], a view too: rises where rs3_bank_copy replaced the unit, not where it left it as it was
+        # int64 [U], a view too (word BM_COPIES): rises where rs3_bank_copy replaced the unit, not where it left it as it was
         self.copies = self.meta.view(U, -1)[:, 9]
 
     def blocks(self, block: int) -> int:
