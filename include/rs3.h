@@ -580,6 +580,107 @@ rs3_status rs3_qk_norm_rope(const void *q, int64_t q_rows, int64_t q_stride, int
                             const float *rope, rs3_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rotary positions from coordinates (Eq. 7)                                 */
+/* ------------------------------------------------------------------------ */
+
+typedef enum { RS3_ROPE_PAIRS = 0, RS3_ROPE_HALVES = 1 } rs3_rope_layout;
+
+/*
+ * How a head turns.  Its first `rot` elements hold rot/2 pairs: (2p, 2p+1), or
+ * (p, p + rot/2); the others stay as they are.  The pairs are shared out among the
+ * coordinates of a position (frame, row, column, say): the first pairs[0] turn with
+ * coordinate 0, and so on.  Pair i of a coordinate with n pairs turns by pos * f radians,
+ *   f = base^(-i/n) * (g + (1 - g) / factor)
+ * with g = 0 (all positions drawn together by `factor`) where context is 0, else
+ *   g = clamp((context * base^(-i/n) / (2 pi) - beta_slow) / (beta_fast - beta_slow), 0, 1):
+ * pairs that turn often over the context trained on keep their frequency, pairs
+ * that turn seldom are slowed.
+ */
+typedef struct {
+    int32_t layout;         /* rs3_rope_layout */
+    int32_t rot;            /* even, 2 <= rot <= d */
+    int32_t axes;           /* coordinates of a position, 1 to 3 */
+    int32_t pairs[3];       /* pairs of each; they add up to rot / 2 */
+    int32_t inverse;        /* 1: turned back (the transpose, a turned row's gradient) */
+    float magnitude;        /* factor of the turned elements */
+    double base;            /* 1 <= base <= 1e12 */
+    double factor;          /* >= 1 */
+    double context;         /* >= 0 */
+    double beta_fast, beta_slow;   /* 0 <= slow < fast, where context > 0 */
+} rs3_rope_spec;
+
+/* Fills layout pairs, rot 0, one axis, base 10000, factor 1, context 0, beta 32 / 1,
+ * magnitude 1; rot and pairs are the caller's. */
+void rs3_default_rope_spec(rs3_rope_spec *spec);
+
+/*
+ * cos_sin[r][p] = magnitude * (cos, sin) of pair p at position r: a table that
+ * rs3_memory_readout, rs3_bank_commit_rope and the other calls with a `rope` argument take
+ * (there rot = d, and pairs are (2p, 2p+1)).
+ *   pos     device int32 [rows][axes], any whole numbers
+ *   cos_sin device fp32 [rows][rot/2][2], 16-byte aligned
+ * Angles are counted in 2^-64 turns: their error is |pos| f 2^-53 and a rounding or two of fp32.
+ */
+rs3_status rs3_rope_table(const int32_t *pos, int64_t rows, const rs3_rope_spec *spec,
+                          float *cos_sin, rs3_stream_t stream);
+
+/*
+ * Every head of every row of q and k (either may be NULL with 0 rows) turned by the row's own
+ * position, in fp32, rounded once; elements past rot are copied.
+ *   q, k, q_out, k_out, strides, keep   as for rs3_qk_norm_rope (in place with the same stride)
+ *   q_pos, k_pos  device int32 [rows][axes]
+ * Limits: d * sizeof(elem) a multiple of 16 (else RS3_EINVAL), d <= 256; strides (in bytes)
+ * multiples of 16.
+ */
+rs3_status rs3_rope_rows(const void *q, int64_t q_rows, int64_t q_stride, int Hq,
+                         const int32_t *q_pos, const uint8_t *q_keep, void *q_out,
+                         int64_t q_out_stride, const void *k, int64_t k_rows, int64_t k_stride,
+                         int Hk, const int32_t *k_pos, const uint8_t *k_keep, void *k_out,
+                         int64_t k_out_stride, rs3_dtype dtype, int d, const rs3_rope_spec *spec,
+                         rs3_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Between two blocks: norms, gate and residual                              */
+/* ------------------------------------------------------------------------ */
+
+typedef enum { RS3_NORM_NONE = 0, RS3_NORM_RMS = 1, RS3_NORM_LAYER = 2 } rs3_norm_kind;
+
+/* norm(v) = n(v) * weight + bias; n(v) = v, v / sqrt(mean(v^2) + eps), or
+ * (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps).  weight, bias: device fp32 [C] or
+ * [U][C], `stride` elements between units (0: one for all); NULL: ones, zeros. */
+typedef struct {
+    int32_t kind;           /* rs3_norm_kind */
+    float eps;              /* >= 0 */
+    const float *weight, *bias;
+    int64_t weight_stride, bias_stride;
+} rs3_norm;
+
+/*
+ * For every unit u and every cell i (of the kept ones, where idx is given):
+ *   x_out[u][i] = alpha * x[u][i] + gate * post(y[u][i])
+ *   h_out[u][i] = pre(x_out[u][i] before its rounding)
+ * what a block (a readout, say) adds to its residual stream, and the input of the next
+ * block.  fp32, each result rounded once; cells that are not kept are neither read nor written.
+ *   y     device [U][mn][C] or NULL (x_out = alpha * x: the entry of a first block)
+ *   x     device [U][mn][C]
+ *   idx, count, k_max  as produced by rs3_select_queries (distinct cells, k_max <= mn), or
+ *         NULL, NULL, 0: every cell
+ *   post, pre   host, may be NULL (as kind RS3_NORM_NONE without weight and bias)
+ *   gate  device fp32 [C], or [U][C] gate_stride elements apart, or NULL (ones)
+ *   x_out, h_out  device [U][mn][C]; one may be NULL.  Each may be x or y itself; they
+ *         overlap nothing otherwise, nor each other (RS3_EINVAL)
+ *   status  device int32 word, may be NULL without idx: RS3_EINVAL for a count outside
+ *         [0, k_max] (the unit is skipped) or a cell outside [0, mn) (skipped)
+ * Limits: C * sizeof(elem) a multiple of 16 (else RS3_EINVAL), C <= 4096, mn <= 16384,
+ * U <= 65535; vectors 16-byte aligned, their strides multiples of 4 and at least C.
+ */
+rs3_status rs3_norm_residual(const void *y, const void *x, rs3_dtype dtype, int U, int mn, int C,
+                             const int32_t *idx, const int32_t *count, int k_max,
+                             const rs3_norm *post, const float *gate, int64_t gate_stride,
+                             float alpha, const rs3_norm *pre, void *x_out, void *h_out,
+                             int32_t *status, rs3_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Write side: keep-set (Sec. 3.2; Eq. 8)                                    */
 /* ------------------------------------------------------------------------ */
 

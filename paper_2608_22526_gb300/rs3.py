@@ -46,6 +46,18 @@ class BankDesc(ctypes.Structure):
                 ("reserved", ctypes.c_uint32)]
 
 
+class RopeSpec(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rot", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * 3), ("inverse", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("context", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("weight_stride", ctypes.c_int64), ("bias_stride", ctypes.c_int64)]
+
+
 # Exported symbols and their signatures (checked against include/rs3.h by the tests)
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -79,6 +91,10 @@ SIGNATURES = {
                                 ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_qk_norm_rope": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64,
                               _I, _I, _I, ctypes.c_float, _P, _P]),
+    "rs3_default_rope_spec": (None, [_P]),
+    "rs3_rope_table": (_I, [_P, _I64, _P, _P, _P]),
+    "rs3_rope_rows": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I, _I, _P, _P]),
+    "rs3_norm_residual": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _I, _P, _P, _I64, ctypes.c_float, _P, _P, _P, _P, _P]),
     "rs3_readout_workspace_bytes": (_SZ, [_I, _I, _I, _I, _I]),
     "rs3_memory_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P,
                                 ctypes.c_float, _P, _SZ, _P, _P]),
@@ -512,6 +528,108 @@ def rs3_qk_norm_rope(q, q_out, k, k_out, dtype: str, mn: int, Hq: int, Hk: int, 
         _want(dev, "rope", rope, torch.float32, mn * d)
     rc = lib.rs3_qk_norm_rope(*sides, DTYPES[dtype], mn, d, float(eps), _ptr(rope), _stream(stream))
     _check(rc, "rs3_qk_norm_rope")
+
+
+# ---------------------------------------------------------------------------
+# rotary positions from coordinates
+# ---------------------------------------------------------------------------
+ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
+
+
+def rope_spec(rot: int, pairs=None, layout: str = "pairs", base: float = 10000.0, factor: float = 1.0, context: float = 0.0,
+              beta_fast: float = 32.0, beta_slow: float = 1.0, magnitude: float = 1.0, inverse: bool = False) -> RopeSpec:
+    """How a head turns: `rot` leading elements, pairs[a] pairs of them with coordinate a (default: all with one)."""
+    s = RopeSpec()
+    lib.rs3_default_rope_spec(ctypes.byref(s))
+    pairs = [rot // 2] if pairs is None else [int(n) for n in pairs]
+    if not 1 <= len(pairs) <= 3:
+        raise ValueError("pairs: one to three coordinates")
+    s.layout, s.rot, s.axes, s.pairs = ROPE_LAYOUTS[layout], rot, len(pairs), (ctypes.c_int32 * 3)(*pairs)
+    s.base, s.factor, s.context, s.beta_fast, s.beta_slow = base, factor, context, beta_fast, beta_slow
+    s.magnitude, s.inverse = magnitude, int(inverse)
+    return s
+
+
+def rs3_rope_table(pos, spec: RopeSpec, cos_sin, stream=None):
+    """(cos, sin) of every pair at the positions pos int32 [rows, axes]: fp32 [rows, rot/2, 2]."""
+    dev = torch.cuda.current_device()
+    _want(dev, "pos", pos, torch.int32, 0)
+    rows = pos.numel() // spec.axes
+    _want(dev, "cos_sin", cos_sin, torch.float32, rows * spec.rot)
+    _check(lib.rs3_rope_table(_ptr(pos), rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
+
+
+def rs3_rope_rows(q, q_out, q_pos, k, k_out, k_pos, dtype: str, Hq: int, Hk: int, d: int, spec: RopeSpec, q_keep=None,
+                  k_keep=None, stream=None):
+    """Every head of q [..., Hq*d] and k [..., Hk*d] (either may be None) turned by its row's
+    position (int32 [rows, axes]).  Rows may be evenly spaced parts of a wider tensor; out may
+    be the input; rows whose keep byte is 0 are neither read nor written."""
+    dev, dt, sides = torch.cuda.current_device(), TORCH_DTYPES[dtype], []
+    for name, x, y, pos, H, keep in (("q", q, q_out, q_pos, Hq, q_keep), ("k", k, k_out, k_pos, Hk, k_keep)):
+        if x is None and y is None:
+            sides += [None, 0, 0, 0, None, None, None, 0]
+            continue
+        _want(dev, name, x, dt, 0)
+        _want(dev, name + "_out", y, dt, 0)
+        (rows, stride), (rows_out, out_stride) = _rows_of(name, x, H * d), _rows_of(name + "_out", y, H * d)
+        if rows != rows_out:
+            raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
+        _want(dev, name + "_pos", pos, torch.int32, rows * spec.axes)
+        if keep is not None:
+            _want(dev, name + "_keep", keep, torch.uint8, rows)
+        sides += [x.data_ptr(), rows, stride, H, _ptr(pos), _ptr(keep), y.data_ptr(), out_stride]
+    rc = lib.rs3_rope_rows(*sides, DTYPES[dtype], d, ctypes.byref(spec), _stream(stream))
+    _check(rc, "rs3_rope_rows")
+
+
+# ---------------------------------------------------------------------------
+# between two blocks: norms, gate and residual
+# ---------------------------------------------------------------------------
+NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
+
+
+def _vector(dev: int, name: str, t, U: int, C: int):
+    """(pointer, elements between units) of a vector fp32 [C] or [U, C]; (None, 0) without one."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) not in ((C,), (U, C)):
+        raise ValueError(f"{name}: [{C}] or [{U}, {C}] wanted, got {tuple(t.shape)}")
+    _want(dev, name, t, torch.float32, C)
+    return _ptr(t), C if t.dim() == 2 else 0
+
+
+def rs3_norm_residual(y, x, x_out, h_out, dtype: str, idx=None, count=None, post: str = "none", post_weight=None,
+                      post_bias=None, gate=None, alpha: float = 1.0, pre: str = "none", pre_weight=None, pre_bias=None,
+                      eps: float = 1e-6, status=None, stream=None):
+    """x_out = alpha x + gate post(y), h_out = pre(x_out) over x, y [U, mn, C], at every cell or
+    at the kept ones (idx int32 [U, k_max], count int32 [U]).  Vectors are fp32 [C] or [U, C]."""
+    dev, dt = torch.cuda.current_device(), TORCH_DTYPES[dtype]
+    if x.dim() != 3:
+        raise ValueError(f"x: [units, cells, channels] wanted, got {tuple(x.shape)}")
+    U, mn, C = x.shape
+    for name, t in (("x", x), ("y", y), ("x_out", x_out), ("h_out", h_out)):
+        if t is not None or name == "x":
+            _want(dev, name, t, dt, U * mn * C)
+    k_max = 0
+    if idx is not None or count is not None:
+        if idx is None or idx.dim() != 2 or idx.shape[0] != U:
+            raise ValueError("idx: one row per unit, with count")
+        k_max = idx.shape[1]
+        _want(dev, "idx", idx, torch.int32, U * k_max)
+        _want(dev, "count", count, torch.int32, U)
+        _want(dev, "status", status, torch.int32, 1)
+    norms = []
+    for name, kind, w, b in (("post", post, post_weight, post_bias), ("pre", pre, pre_weight, pre_bias)):
+        n = Norm()
+        n.kind, n.eps = NORM_KINDS[kind], eps
+        n.weight, n.weight_stride = _vector(dev, name + "_weight", w, U, C)
+        n.bias, n.bias_stride = _vector(dev, name + "_bias", b, U, C)
+        norms.append(n)
+    g, g_stride = _vector(dev, "gate", gate, U, C)
+    rc = lib.rs3_norm_residual(_ptr(y), _ptr(x), DTYPES[dtype], U, mn, C, _ptr(idx), _ptr(count), k_max, ctypes.byref(norms[0]),
+                               g, g_stride, float(alpha), ctypes.byref(norms[1]), _ptr(x_out), _ptr(h_out), _ptr(status),
+                               _stream(stream))
+    _check(rc, "rs3_norm_residual")
 
 
 # ---------------------------------------------------------------------------
