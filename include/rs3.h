@@ -443,6 +443,36 @@ rs3_status rs3_memory_readout_run(const void *q, rs3_dtype dtype, int G, int mn,
                                   rs3_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Read side: a shared prefix                                               */
+/* ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace rs3_shared_readout needs for these banks; never falls as k_max
+ * grows.  0 for an uninitialised bank. */
+size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const rs3_bank *prefix, int k_max);
+
+/*
+ * rs3_memory_readout over two banks: unit u attends to all rows of unit prefix_unit[u] of
+ * `prefix` and to all of its own in `bank`, in one softmax.  Hypotheses that were forked from
+ * a track share its rows this way instead of each holding a copy; the units of one group with the
+ * same prefix unit have each cell's attention over it computed once for all of them.
+ *   bank         the units' own rows (maybe none yet)
+ *   prefix       a bank of the same H, d, dtype and mn; it may be `bank` itself
+ *   prefix_unit  device int32 [U], in [-1, prefix->U); -1: no prefix
+ * Arguments and results otherwise as rs3_memory_readout.  A cell outside [0, mn) latches
+ * RS3_EINVAL and is skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit
+ * out of range latches it and the unit is skipped, and so is one whose counters or whose
+ * prefix's are unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.
+ *   workspace    device, >= rs3_shared_readout_workspace_bytes(...), 16-byte aligned; one call at a time
+ * Limits: those of rs3_memory_readout, for both banks.
+ */
+rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
+                              const int32_t *unit_group, const int32_t *idx, const int32_t *count,
+                              int k_max, const rs3_bank *bank, const rs3_bank *prefix,
+                              const int32_t *prefix_unit, const float *rope, const void *residual,
+                              void *out, float scale, void *workspace, size_t workspace_bytes,
+                              int32_t *status, rs3_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Read side over chosen blocks of a long bank                               */
 /* ------------------------------------------------------------------------ */
 

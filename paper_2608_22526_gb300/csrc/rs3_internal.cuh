@@ -46,7 +46,7 @@ struct RangeSet {           // a unit's bank as <= 4 contiguous row ranges
     int32_t nq;             // query tiles of BM rows
     int32_t cnt;            // kept queries (clamped to k_max)
     int32_t splits;         // KV splits per (head, query tile)
-    int32_t slot_base;      // first partial slot of the unit (-1 if no splits)
+    int32_t slot_base;      // number of the unit's first group, where results stay in partial slots
     int32_t pad[3];
 };
 
@@ -72,7 +72,7 @@ struct ReadoutHeader {
 };
 
 struct ReadoutLayout {      // byte offsets inside the workspace
-    size_t header, cta_items, ranges, items, combine, part_o, part_ml, total;
+    size_t header, cta_items, ranges, items, combine, parts, part_o, part_ml, total;
     int64_t max_items, max_combine, max_slots;
 };
 

@@ -37,8 +37,9 @@ namespace {
 // valid grid or bank has no work.
 __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
 {
-    // every load first (none depends on another), then the checks
-    const int64_t *mu = a.meta + (int64_t)u * a.meta_stride_words;
+    // every load first (none depends on another but a unit's number in the bank), then the checks
+    const int bu = a.bank_unit ? a.bank_unit[u] : u;
+    const int64_t *mu = a.meta + (int64_t)max(bu, 0) * a.meta_stride_words;
     int cnt = a.count[u];
     const int g = a.unit_group[u];
     const int64_t head = mu[BM_HEAD], tail = mu[BM_TAIL], cond = mu[BM_COND_LEN], ptr = mu[BM_PTRLEN];
@@ -55,6 +56,7 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
         if (latch) latch_status(a.status, RS3_EINVAL);
         cnt = 0;
     }
+    if (bu < 0) return rs;                          // reads nothing (nor has queries)
     if (!(head >= 0 && tail >= head && tail - head <= a.ring_cap && cond >= 0 && cond <= a.pinned_cap && ptr >= 0 &&
           ptr <= a.n_ptr)) {
         if (latch) latch_status(a.status, RS3_EINTERNAL);
@@ -73,6 +75,10 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
     }
     rs.start[3] = a.pinned_cap + a.ring_cap;
     rs.len[3] = (int32_t)ptr;
+    if (a.bank_unit) {                              // rows count from unit u's storage
+#pragma unroll
+        for (int r = 0; r < 4; ++r) rs.start[r] += (int64_t)(bu - u) * a.rows_per_unit;
+    }
     return rs;
 }
 
@@ -226,6 +232,11 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
             w.tile_end = (int32_t)t1;
             w.slot = whole ? -1 : 2 * b + (first < 0 ? 0 : 1);
             w.pad = 0;
+            if (whole && a.parts) {
+                const int32_t g = v.gb[u] + gl;
+                w.slot = 2 * a.grid_ctas + g;
+                a.parts[g] = {w.slot, 0, 1, 0};
+            }
             a.items[idx] = w;
             if (first < 0) first = idx;
             last = idx;
@@ -240,6 +251,10 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
                 c.slot0 = w.slot;
                 c.nsplit = (int32_t)(e - b + 1);
                 c.pad[1] = v.cnt[u];
+                if (a.parts) {
+                    a.parts[v.gb[u] + gl] = {c.slot0, b, c.nsplit, 0};
+                    c.nsplit = 0;                   // merged by the caller
+                }
             }
         }
         x += len;
@@ -292,27 +307,16 @@ __device__ __forceinline__ bool two_tiles(const ReadoutArgs &a, const RangeSet &
     return a.d == 64 ? s1 > 1.7f * s2 + (float)a.n_sm : s1 > 1.65f * s2 + 3.75f * (float)a.n_sm;
 }
 
-// Out of place, CTAs 1.. of the launch also write out = residual (or zeros) on
-// every cell: unselected cells equal the residual bit for bit (Eq. 6 S_K), and
-// the copy hides the plan.
-__global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nvec)
+// The plan, by one CTA.
+__device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
 {
-    pdl_wait();
-    if (blockIdx.x > 0) {
-        const uint4 *res = static_cast<const uint4 *>(a.residual);
-        uint4 *out = static_cast<uint4 *>(a.out);
-        for (int64_t i = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + threadIdx.x; i < nvec;
-             i += (int64_t)(gridDim.x - 1) * PLAN_THREADS)
-            out[i] = res ? __ldcs(res + i) : make_uint4(0, 0, 0, 0);
-        return;
-    }
     ReadoutHeader *hdr = a.header;
     // [U+1] tb, [U] wg (int64); [U+1] gb, [U] nt (int32)
     extern __shared__ int64_t s_plan[];
     int64_t *s_tb = s_plan, *s_wg = s_tb + (a.U + 1);
     int32_t *s_gb = reinterpret_cast<int32_t *>(s_wg + a.U), *s_nt = s_gb + (a.U + 1), *s_cnt = s_nt + a.U;
-    __shared__ int s_np, s_nc;
-    if (threadIdx.x == 0) { s_np = 0; s_nc = 0; }
+    __shared__ int s_np, s_nc, s_alone;
+    if (threadIdx.x == 0) { s_np = 0; s_nc = 0; s_alone = 0; }
     RangeSet mine = {};                             // this thread's unit of the first round
     if (threadIdx.x < a.U) mine = unit_ranges(a, threadIdx.x, true);
     struct { int BM, BN, ov, min_chunk; } cfg = {a.BM, a.BN, a.plan_ov, a.min_chunk};
@@ -343,6 +347,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nv
         if (u < a.U) {
             s_tb[u] = off + run;
             s_gb[u] = goff + grun;
+            if (a.parts) a.ranges[u].slot_base = goff + grun;
         }
         run += tot;
         grun += gtot;
@@ -362,8 +367,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nv
     // query tiles on 150 of 152 CTAs: 392 -> 285 us); where it leaves 1 in 64,
     // always.  The line at 48 MB of K and V is a constant fitted on this part, whose L2
     // holds 126 MB; nothing derives it.
-    if (a.U == 1 && a.tensor && grun > 0 && P > grun) {
-        const int64_t idle = P % grun, bytes = (int64_t)s_nt[0] * cfg.BN * a.D * 4;
+    // (Likewise one unit with queries where units share a bank's.)
+    int alone = a.U == 1 ? 0 : -1;
+    if (a.bank_unit && a.U > 1) {
+        for (int u = threadIdx.x; u < a.U; u += blockDim.x)
+            if (s_gb[u + 1] - s_gb[u] == grun) s_alone = u + 1;
+        __syncthreads();
+        alone = s_alone - 1;
+    }
+    if (alone >= 0 && a.tensor && grun > 0 && P > grun) {
+        const int64_t idle = P % grun, bytes = (int64_t)s_nt[alone] * cfg.BN * a.D * 4;
         if (64 * idle <= P || (bytes > ((int64_t)48 << 20) && 8 * idle <= P)) P -= idle;
     }
     PlanView v;
@@ -393,6 +406,32 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nv
         hdr->n_part = s_np;
         hdr->bm = cfg.BM;
     }
+}
+
+// Out of place, the launch's other CTAs also write out = residual (or zeros) on
+// every cell: unselected cells equal the residual bit for bit (Eq. 6 S_K), and
+// the copy hides the plan.
+__device__ __forceinline__ void pass_through(const ReadoutArgs &a, int64_t nvec, int cta, int ctas)
+{
+    const uint4 *res = static_cast<const uint4 *>(a.residual);
+    uint4 *out = static_cast<uint4 *>(a.out);
+    for (int64_t i = (int64_t)cta * PLAN_THREADS + threadIdx.x; i < nvec; i += (int64_t)ctas * PLAN_THREADS)
+        out[i] = res ? __ldcs(res + i) : make_uint4(0, 0, 0, 0);
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nvec)
+{
+    pdl_wait();
+    if (blockIdx.x > 0) pass_through(a, nvec, blockIdx.x - 1, gridDim.x - 1);
+    else plan_cta(a);
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) k_plan_two(const __grid_constant__ ReadoutArgs a, const __grid_constant__ ReadoutArgs b,
+                                                           int64_t nvec)
+{
+    pdl_wait();
+    if (blockIdx.x > 1) pass_through(b, nvec, blockIdx.x - 2, gridDim.x - 2);
+    else plan_cta(blockIdx.x == 0 ? a : b);
 }
 
 // ---------------------------------------------------------------------------
@@ -558,18 +597,16 @@ __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-namespace {
-
 // Bounds of the stream-K plan: item indices < groups + CTAs (group + slice);
 // a CTA has at most two partial items (slots 2b, 2b + 1); at most one merge
 // entry per CTA and per group.
-ReadoutLayout readout_layout(int U, int H, int d, int k_max, const ReadoutPath &p)
+ReadoutLayout rs3_readout_layout(int U, int H, int d, int k_max, const ReadoutPath &p, bool parts)
 {
     const int BM = p.BM, grid = p.grid, part_rows = p.part_rows;
     ReadoutLayout L;
     const int64_t nq = k_max > 0 ? (k_max + BM - 1) / BM : 1;
     const int64_t groups = (int64_t)U * H * nq;
-    L.max_slots = 2 * (int64_t)grid;
+    L.max_slots = 2 * (int64_t)grid + (parts ? (int64_t)U * H * (k_max > 0 ? (k_max + part_rows - 1) / part_rows : 1) : 0);
     L.max_combine = groups < grid ? groups : grid;   // at most one per CTA slice and per group
     L.max_items = groups + grid;
     size_t off = 0;
@@ -583,6 +620,8 @@ ReadoutLayout readout_layout(int U, int H, int d, int k_max, const ReadoutPath &
     off = align_up(off + (size_t)L.max_items * sizeof(WorkItem), 256);
     L.combine = off;
     off = align_up(off + (size_t)L.max_combine * sizeof(CombineItem), 256);
+    L.parts = off;
+    if (parts) off = align_up(off + (size_t)groups * sizeof(GroupParts), 256);
     L.part_o = off;
     off = align_up(off + (size_t)L.max_slots * part_rows * d * 4, 256);
     L.part_ml = off;
@@ -591,9 +630,9 @@ ReadoutLayout readout_layout(int U, int H, int d, int k_max, const ReadoutPath &
     return L;
 }
 
-}  // namespace
-
 namespace {
+ReadoutLayout readout_layout(int U, int H, int d, int k_max, const ReadoutPath &p) { return rs3_readout_layout(U, H, d, k_max, p, false); }
+
 std::atomic<uint64_t> g_wait_ns{1000000000ull};
 }
 
@@ -661,12 +700,9 @@ extern "C" size_t rs3_readout_workspace_bytes(int U, int H, int d, int k_max, rs
     return std::max(readout_layout(U, H, d, k_max, p).total, readout_layout(U, H, d, k_max, floor).total);
 }
 
-rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
-                               const int32_t *unit_group, const int32_t *idx, const int32_t *count,
-                               int k_max, const rs3_bank *bank, const float *rope,
-                               const void *residual, void *out, float scale, void *workspace,
-                               size_t workspace_bytes, int32_t *status, ReadoutArgs *a,
-                               ReadoutPath *path, int64_t *grid_combine)
+rs3_status rs3_readout_check(const void *q, rs3_dtype dtype, int G, int mn, int H, int d, const int32_t *unit_group,
+                             const int32_t *idx, const int32_t *count, int k_max, const rs3_bank *bank, const float *rope,
+                             const void *residual, const void *out, const void *workspace, const int32_t *status)
 {
     if (!q || !unit_group || !idx || !count || !bank || !out || !workspace || !status)
         return RS3_EINVAL;
@@ -680,16 +716,23 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
     if (!rs3_aligned16(q) || !rs3_aligned16(out) || !rs3_aligned16(workspace) ||
         (residual && !rs3_aligned16(residual)) || (rope && !rs3_aligned16(rope)))
         return RS3_EINVAL;
-    const ReadoutPath p = choose_readout_path(dtype, d, bank->U, H, k_max, bank->rows_per_unit, workspace_bytes);
-    const ReadoutLayout L = readout_layout(bank->U, H, d, k_max, p);
-    // work-item indices (group + slice) and item ranges are 32-bit.  The limit
-    // counts 32-row query tiles on the CUDA-core path and 128-row ones on the
-    // tensor cores, at least as many as the kernels have.
+    return RS3_OK;
+}
+
+// work-item indices (group + slice) and item ranges are 32-bit.  The limit
+// counts 32-row query tiles on the CUDA-core path and 128-row ones on the
+// tensor cores, at least as many as the kernels have.
+bool rs3_readout_fits(int U, int H, int k_max, const ReadoutPath &p)
+{
     const int limit_rows = p.kind == 0 ? 32 : 128;
-    const int64_t limit_groups = (int64_t)bank->U * H * (k_max > 0 ? (k_max + limit_rows - 1) / limit_rows : 1);
-    if (limit_groups + p.grid >= ((int64_t)1 << 30)) return RS3_EUNSUPPORTED;
-    if (workspace_bytes < L.total) return RS3_ECAPACITY;
-    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    const int64_t limit_groups = (int64_t)U * H * (k_max > 0 ? (k_max + limit_rows - 1) / limit_rows : 1);
+    return limit_groups + p.grid < ((int64_t)1 << 30);
+}
+
+void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout &L, uint8_t *ws, const void *q, int G, int mn, int H,
+                      int d, const int32_t *unit_group, const int32_t *idx, const int32_t *count, int k_max, int U,
+                      const rs3_bank *bank, const float *rope, const void *residual, void *out, float scale, int32_t *status)
+{
     a->q = q;
     a->k_store = bank->k_store;
     a->v_store = bank->v_store;
@@ -706,7 +749,7 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
     a->residual = residual;
     a->out = out;
     a->status = status;
-    a->U = bank->U;
+    a->U = U;
     a->G = G;
     a->mn = mn;
     a->H = H;
@@ -736,6 +779,26 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
     a->combine = reinterpret_cast<CombineItem *>(ws + L.combine);
     a->part_o = reinterpret_cast<float *>(ws + L.part_o);
     a->part_ml = reinterpret_cast<float *>(ws + L.part_ml);
+    a->bank_unit = nullptr;
+    a->bank_U = bank->U;
+    a->parts = nullptr;
+}
+
+rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
+                               const int32_t *unit_group, const int32_t *idx, const int32_t *count,
+                               int k_max, const rs3_bank *bank, const float *rope,
+                               const void *residual, void *out, float scale, void *workspace,
+                               size_t workspace_bytes, int32_t *status, ReadoutArgs *a,
+                               ReadoutPath *path, int64_t *grid_combine)
+{
+    const rs3_status s = rs3_readout_check(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, residual, out, workspace, status);
+    if (s != RS3_OK) return s;
+    const ReadoutPath p = choose_readout_path(dtype, d, bank->U, H, k_max, bank->rows_per_unit, workspace_bytes);
+    const ReadoutLayout L = readout_layout(bank->U, H, d, k_max, p);
+    if (!rs3_readout_fits(bank->U, H, k_max, p)) return RS3_EUNSUPPORTED;
+    if (workspace_bytes < L.total) return RS3_ECAPACITY;
+    rs3_readout_fill(a, p, L, static_cast<uint8_t *>(workspace), q, G, mn, H, d, unit_group, idx, count, k_max, bank->U, bank, rope,
+                     residual, out, scale, status);
     *path = p;
     *grid_combine = L.max_combine;
     return RS3_OK;
@@ -743,30 +806,52 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
 
 namespace {
 
+// 16-byte pieces of the pass-through (out of place only) and the CTAs for them
+int64_t pass_pieces(const ReadoutArgs &a, rs3_dtype dtype, int64_t &blocks)
+{
+    blocks = 0;
+    if (a.residual == a.out) return 0;
+    const int64_t nvec = (int64_t)a.U * a.mn * a.D * (dtype == RS3_BF16 ? 2 : 4) / 16;
+    blocks = (nvec + PLAN_THREADS - 1) / PLAN_THREADS;
+    const int64_t cap = (int64_t)a.n_sm * 8;
+    if (blocks > cap) blocks = cap;
+    return nvec;
+}
+
+// plan shared memory: unit slot bases and widths (int64), group bases, tiles, kept queries (int32)
+size_t plan_bytes(int U) { return (size_t)(2 * U + 1) * 8 + (size_t)(3 * U + 1) * 4; }
+
 // pass-through of the unselected cells (out of place only) and the plan
 rs3_status launch_plan(const ReadoutArgs &a, cudaStream_t st, rs3_dtype dtype)
 {
-    int64_t nvec = 0, blocks = 0;
-    if (a.residual != a.out) {
-        nvec = (int64_t)a.U * a.mn * a.D * (dtype == RS3_BF16 ? 2 : 4) / 16;
-        blocks = (nvec + PLAN_THREADS - 1) / PLAN_THREADS;
-        const int64_t cap = (int64_t)a.n_sm * 8;
-        if (blocks > cap) blocks = cap;
-    }
-    // plan shared memory: unit slot bases and widths (int64), group bases, tiles, kept queries (int32)
-    const size_t plan_smem = (size_t)(2 * a.U + 1) * 8 + (size_t)(3 * a.U + 1) * 4;
-    if (rs3_kernel_smem((const void *)k_plan, plan_smem) != RS3_OK) return RS3_EUNSUPPORTED;
-    launch_pdl(k_plan, dim3((unsigned)(1 + blocks)), dim3(PLAN_THREADS), plan_smem, st, a, nvec);
+    int64_t blocks;
+    const int64_t nvec = pass_pieces(a, dtype, blocks);
+    if (rs3_kernel_smem((const void *)k_plan, plan_bytes(a.U)) != RS3_OK) return RS3_EUNSUPPORTED;
+    launch_pdl(k_plan, dim3((unsigned)(1 + blocks)), dim3(PLAN_THREADS), plan_bytes(a.U), st, a, nvec);
+    return cudaGetLastError() != cudaSuccess ? RS3_ECUDA : RS3_OK;
+}
+
+}  // namespace
+
+rs3_status rs3_readout_plan_two(const ReadoutArgs &a, const ReadoutArgs &b, rs3_dtype dtype, cudaStream_t st)
+{
+    int64_t blocks;
+    const int64_t nvec = pass_pieces(b, dtype, blocks);
+    const size_t smem = plan_bytes(a.U > b.U ? a.U : b.U);
+    if (rs3_kernel_smem((const void *)k_plan_two, smem) != RS3_OK) return RS3_EUNSUPPORTED;
+    launch_pdl(k_plan_two, dim3((unsigned)(2 + blocks)), dim3(PLAN_THREADS), smem, st, a, b, nvec);
     return cudaGetLastError() != cudaSuccess ? RS3_ECUDA : RS3_OK;
 }
 
 // the attention kernel over the plan in the workspace
-rs3_status launch_run(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st)
+rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st)
 {
     if (p.either) return rs3_launch_either_readout(a, st);
     if (p.kind == 1) return rs3_launch_tc_readout(a, st);
     return rs3_launch_simt_readout(a, dtype, st);
 }
+
+namespace {
 
 // merge of the split-KV partials and their scatter
 rs3_status launch_merge(const ReadoutArgs &a, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
@@ -798,7 +883,7 @@ rs3_status rs3_readout_launch(const ReadoutArgs &a, const ReadoutPath &p,
         if (s != RS3_OK) return s;
     }
     if (phases & RS3_PHASE_RUN) {
-        const rs3_status s = launch_run(a, p, dtype, st);
+        const rs3_status s = rs3_readout_run_launch(a, p, dtype, st);
         if (s != RS3_OK) return s;
     }
     if (phases & RS3_PHASE_MERGE) return launch_merge(a, max_combine, dtype, st);

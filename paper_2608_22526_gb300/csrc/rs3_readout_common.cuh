@@ -7,6 +7,10 @@
 #define RS3_MAX_UNITS 4096  // units per readout call
 #define RS3_PAIR_ITEMS (1 << 30)   // above every item index
 
+struct GroupParts {         // piece 0 of a group is in slot0, piece s >= 1 in slot 2 (slice + s)
+    int32_t slot0, slice, n, pad;
+};
+
 struct ReadoutArgs {
     const void *q;
     const void *k_store;
@@ -39,6 +43,10 @@ struct ReadoutArgs {
     CombineItem *combine;
     float *part_o;          // [slot][BM][d]
     float *part_ml;         // [slot][BM] (m, l) pairs, m in the log2 domain
+    // calls whose units read units of a bank by number, and leave all results in partial slots
+    const int32_t *bank_unit;   // [U] the bank's unit that unit u reads (-1: none); NULL: unit u
+    int bank_U;                 // units of the bank
+    GroupParts *parts;          // [group] its pieces (groups numbered as the plan does); NULL: whole groups are written out
 };
 
 struct ReadoutPath {
@@ -65,6 +73,20 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
                                const void *residual, void *out, float scale, void *workspace,
                                size_t workspace_bytes, int32_t *status, ReadoutArgs *a,
                                ReadoutPath *path, int64_t *grid_combine);
+// The workspace of a path, from `base` on; with `parts`, slots for every group and their table.
+ReadoutLayout rs3_readout_layout(int U, int H, int d, int k_max, const ReadoutPath &p, bool parts);
+// Checks of what readouts of a bank have in common, and the arguments of one over the path and layout.
+rs3_status rs3_readout_check(const void *q, rs3_dtype dtype, int G, int mn, int H, int d, const int32_t *unit_group,
+                             const int32_t *idx, const int32_t *count, int k_max, const rs3_bank *bank, const float *rope,
+                             const void *residual, const void *out, const void *workspace, const int32_t *status);
+bool rs3_readout_fits(int U, int H, int k_max, const ReadoutPath &p);      // its work list's indices
+void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout &L, uint8_t *ws, const void *q, int G, int mn, int H,
+                      int d, const int32_t *unit_group, const int32_t *idx, const int32_t *count, int k_max, int U,
+                      const rs3_bank *bank, const float *rope, const void *residual, void *out, float scale, int32_t *status);
+// The attention kernel over the plan in the workspace.
+rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st);
+// Two plans in one launch, with the second's pass-through.
+rs3_status rs3_readout_plan_two(const ReadoutArgs &first, const ReadoutArgs &second, rs3_dtype dtype, cudaStream_t st);
 // phases of a readout: the attention over the bank (pass-through, plan,
 // readout kernel) and the merge of split-KV partials
 enum { RS3_PHASE_PLAN = 1, RS3_PHASE_RUN = 4, RS3_PHASE_ATTEND = 1 | 4, RS3_PHASE_MERGE = 2 };

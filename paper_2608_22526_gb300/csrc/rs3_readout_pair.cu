@@ -514,7 +514,7 @@ rs3_status launch(const ReadoutArgs &a, cudaStream_t st)
 {
     constexpr int smem = Cfg<DH>::SMEM > tc::Cfg<DH>::SMEM ? Cfg<DH>::SMEM : tc::Cfg<DH>::SMEM;
     if (rs3_kernel_smem((const void *)k_readout_either<DH>, smem) != RS3_OK) return RS3_ECUDA;
-    const int64_t rows = (int64_t)a.U * a.rows_per_unit;
+    const int64_t rows = (int64_t)a.bank_U * a.rows_per_unit;
     if (rows >= (int64_t)1 << 31) return RS3_EUNSUPPORTED;
     CUtensorMap mk, mv;
     if (!make_kv_map(&mk, a.k_store, a.D, rows, tc::Cfg<DH>::BN) || !make_kv_map(&mv, a.v_store, a.D, rows, tc::Cfg<DH>::BN))

@@ -91,6 +91,8 @@ SIGNATURES = {
                                 ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_qk_norm_rope": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64,
                               _I, _I, _I, ctypes.c_float, _P, _P]),
+    "rs3_shared_readout_workspace_bytes": (_SZ, [_P, _P, _I]),
+    "rs3_shared_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_default_rope_spec": (None, [_P]),
     "rs3_rope_table": (_I, [_P, _I64, _P, _P, _P]),
     "rs3_rope_rows": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64, _I, _I, _P, _P]),
@@ -434,6 +436,26 @@ def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope,
         _want(dev, "rope", rope, torch.float32, mn * d)
     _want(dev, "status", status, torch.int32, 1)
     return dev
+
+
+def rs3_shared_readout_workspace_bytes(bank: "Bank", prefix: "Bank", k_max: int) -> int:
+    return int(lib.rs3_shared_readout_workspace_bytes(ctypes.byref(bank.desc), ctypes.byref(prefix.desc), k_max))
+
+
+def rs3_shared_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int, bank: "Bank",
+                       prefix: "Bank", prefix_unit, rope, residual, out, scale: float, workspace, status, stream=None):
+    """rs3_memory_readout over the rows of unit prefix_unit[u] of `prefix` (-1: none) and the unit's own in `bank`."""
+    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    _want_bank(dev, prefix)
+    _want(dev, "prefix_unit", prefix_unit, torch.int32, bank.U)
+    _want_workspace(dev, workspace)
+    if residual is not None:
+        _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    rc = lib.rs3_shared_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
+                                ctypes.byref(bank.desc), ctypes.byref(prefix.desc), _ptr(prefix_unit), _ptr(rope), _ptr(residual),
+                                _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
+    _check(rc, "rs3_shared_readout")
 
 
 def rs3_block_select_workspace_bytes(U: int, H: int, k_max: int, n_blocks: int) -> int:

@@ -1,0 +1,316 @@
+"""Readouts over a shared prefix, and with capped and biased scores, against plain implementations in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_long_bank import DT, HALF, Built, bits, gen, rope_table, status, turned
+
+pytestmark = pytest.mark.gpu
+
+STEP = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def rs3():
+    from paper_2608_22526_gb300 import rs3
+    return rs3
+
+
+def built(rs3, **kw):
+    """A bank whose dead rows hold finite values (large ones: nothing may come of them)."""
+    b = Built(rs3, **kw)
+    for t in (b.bank.k_store, b.bank.v_store):
+        t.copy_(torch.where(t.isnan(), torch.full_like(t, 1000.0), t))
+    return b
+
+
+def frames_of(b, u):
+    """(storage rows of unit u in logical order, the frame of each: its age, F or F + 1)."""
+    rows, lens, (cond, ring, ptr) = b.places(u)
+    F = b.bank.max_frames
+    slot = [F] * cond + [len(lens) - 1 - i for i, n in enumerate(lens) for _ in range(n)] + [F + 1] * ptr
+    return torch.from_numpy(rows).cuda(), torch.tensor(slot, dtype=torch.int64, device="cuda")
+
+
+def keep_sets(U, mn, k_max, counts, seed=17):
+    g = gen(seed)
+    idx = torch.stack([torch.randperm(mn, generator=g, device="cuda")[:k_max].sort().values for _ in range(U)]).to(torch.int32).contiguous()
+    return idx, torch.tensor(counts, dtype=torch.int32, device="cuda")
+
+
+def reference(dtype, H, d, q, idx, counts, group, table, scale, res, shape, rows_of, cap=0.0, bias=None):
+    """(out, tolerance) in 64 bits.  rows_of(u): keys, values [N, D] and the frame of each; bias(u, h): [frames] or None."""
+    bf, half = dtype == "bf16", HALF[dtype]
+    out = torch.zeros(shape, dtype=torch.float64, device="cuda") if res is None else res.double().clone()
+    tol = torch.zeros_like(out)
+    qd = q.double()
+    if table is not None:
+        qd = turned(qd, d, table)
+    for u, n in enumerate(counts):
+        if n == 0:
+            continue
+        k, v, slot = rows_of(u)
+        k, v = k.double(), v.double()
+        cells = idx[u, :n].long()
+        for h in range(H):
+            col = slice(h * d, (h + 1) * d)
+            r = 0.0 if res is None else res[u, cells, col].double()
+            if k.shape[0] == 0:
+                out[u, cells, col] = r
+                tol[u, cells, col] = 0.0
+                continue
+            qq = qd[int(group[u]), cells, col]
+            x = qq @ k[:, col].T * scale
+            terms = qq.abs() @ k[:, col].abs().T * scale
+            # a score: fp32 sums of at most 256 products and its scaling, under 300 half-steps of the terms; a rotated query's
+            # rounding to bf16
+            e = terms * (300 * STEP + (half if bf and table is not None else 0.0))
+            if cap > 0:
+                # |d tanh| <= 1; the change's own error: a power, a sum, a quotient and a product or two, under 32 half-steps of cap
+                x = cap * torch.tanh(x / cap)
+                e = e + 32 * STEP * cap
+            if bias is not None:
+                b = bias(u, h).double()[slot]
+                x = x + b
+                e = e + 8 * STEP * (x.abs() + b.abs().clamp(max=1e30)).nan_to_num(0.0, 0.0, 0.0)
+            top = x.amax(1, keepdim=True)
+            # (a weight is 2^(x - reference): the argument's own rounding, and the reference's, are of their sizes)
+            on = x > -math.inf
+            e = e + 16 * STEP * torch.where(on, x.abs(), 0.0).amax(1, keepdim=True)
+            w = torch.where(on, torch.exp(x - torch.where(top > -math.inf, top, 0.0)), 0.0)
+            total = w.sum(1, keepdim=True)
+            p = w / torch.where(total > 0, total, 1.0)
+            A, size = p @ v[:, col], p @ v[:, col].abs()
+            # a weight's error beside the row's mean error is at most twice the largest one's; far keys weigh by p
+            es = torch.where(on, e, 0.0)
+            share = (p * torch.expm1(2 * es)) @ v[:, col].abs() + (p * torch.expm1(2 * es)).sum(1, keepdim=True) * size
+            out[u, cells, col] = r + A
+            # weights and values: under 300 half-steps, in bf16 a rounding of each weight; then the result's own
+            tol[u, cells, col] = half * (r + A).abs() + (share + size * (300 * STEP + (half if bf else 0.0))) * 1.01 + 1e-30
+    return out, tol
+
+
+# ---------------------------------------------------------------------------
+# a shared prefix
+# ---------------------------------------------------------------------------
+SHAPES = [("bf16", 1, 16), ("bf16", 2, 32), ("bf16", 3, 64), ("bf16", 2, 128), ("bf16", 1, 256), ("f32", 2, 16), ("f32", 1, 32),
+          ("f32", 3, 64), ("f32", 1, 128), ("f32", 2, 256)]
+
+
+def shared_rows(b, p, prefix_unit):
+    def rows(u):
+        at = torch.from_numpy(b.places(u)[0]).cuda()
+        k, v = b.bank.k_store[u][at], b.bank.v_store[u][at]
+        x = int(prefix_unit[u])
+        if x >= 0:
+            pt = torch.from_numpy(p.places(x)[0]).cuda()
+            k, v = torch.cat([p.bank.k_store[x][pt], k]), torch.cat([p.bank.v_store[x][pt], v])
+        return k, v, torch.zeros(k.shape[0], dtype=torch.int64, device="cuda")
+    return rows
+
+
+def run_shared(rs3, b, p, q, G, idx, count, group, prefix_unit, table, scale, res, out, ws=None, stream=None):
+    k_max = idx.shape[1]
+    if ws is None:
+        ws = torch.full((rs3.rs3_shared_readout_workspace_bytes(b.bank, p.bank, k_max),), 255, dtype=torch.uint8, device="cuda")
+    rs3.rs3_shared_readout(q, b.dtype, G, b.mn, b.H, b.d, group, idx, count, k_max, b.bank, p.bank, prefix_unit, table, res, out, scale, ws,
+                           b.st, stream)
+    return ws
+
+
+def shared_case(rs3, b, p, counts, group, prefix, G, residual="none", rope=False, seed=5, k_max=None, scale=0.0):
+    U, mn, D, dtype = b.U, b.mn, b.D, b.dtype
+    g = gen(seed)
+    q = (torch.randn((G, mn, D), generator=g, device="cuda") * 1.2).to(DT[dtype])
+    k_max = max(1, max(counts)) if k_max is None else k_max
+    idx, count = keep_sets(U, mn, k_max, counts, seed)
+    group = torch.tensor(group, dtype=torch.int32, device="cuda")
+    prefix_unit = torch.tensor(prefix, dtype=torch.int32, device="cuda")
+    table = rope_table(mn, b.d) if rope else None
+    x = torch.randn((U, mn, D), generator=g, device="cuda").to(DT[dtype])
+    res = None if residual == "none" else x.clone()
+    out = res if residual == "inplace" else torch.full_like(x, math.nan)
+    want, tol = reference(dtype, b.H, b.d, q, idx, counts, group, table, scale or b.d ** -0.5, None if res is None else x, x.shape,
+                          shared_rows(b, p, prefix_unit))
+    run_shared(rs3, b, p, q, G, idx, count, group, prefix_unit, table, scale, res, out)
+    assert int(b.st) == 0
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
+    return q, idx, count, group, prefix_unit, table, out
+
+
+@pytest.mark.parametrize("dtype,H,d", SHAPES)
+@pytest.mark.parametrize("counts", [[1, 0, 3, 2, 1], [40, 17, 33, 72, 5]])
+@pytest.mark.parametrize("residual,rope", [("none", False), ("inplace", True), ("other", False)])
+def test_shared_readout_matches_64_bits(rs3, dtype, H, d, counts, residual, rope):
+    """Two groups, classes of several units and of one, units without a prefix, without rows of their own, an empty prefix."""
+    b = built(rs3, U=5, H=H, d=d, dtype=dtype, m=8, n=9, window=4, commits=7, n_ptr=5, empty=(1,), seed=2)
+    p = built(rs3, U=3, H=H, d=d, dtype=dtype, m=8, n=9, window=-1, ring_frames=9, commits=9, n_ptr=3, seed=3)
+    rs3.rs3_bank_reset(b.bank, 1)
+    rs3.rs3_bank_reset(p.bank, 2)
+    shared_case(rs3, b, p, counts, [0, 0, 0, 1, 1], [1, 1, 0, 1, 2], 2, residual, rope)
+    shared_case(rs3, b, p, counts, [0, 1, 0, 1, 1], [-1, -1, 2, 0, 0], 2, residual, rope, scale=0.11)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 1, 64), ("bf16", 2, 128), ("bf16", 1, 256), ("f32", 1, 64), ("f32", 1, 256)])
+def test_shared_readout_of_long_prefixes_and_many_queries(rs3, dtype, H, d):
+    """Rows split over many pieces; keep-sets that overlap in part; classes of more tiles than any unit."""
+    b = built(rs3, U=4, H=H, d=d, dtype=dtype, m=32, n=33, window=3, commits=4, n_ptr=0, seed=2)
+    p = built(rs3, U=2, H=H, d=d, dtype=dtype, m=32, n=33, window=-1, ring_frames=24, commits=24, n_ptr=3, seed=3)
+    shared_case(rs3, b, p, [300, 290, 131, 7], [0, 0, 0, 0], [1, 1, 1, 0], 1, "inplace")
+    shared_case(rs3, b, p, [1056, 1056, 1, 129], [0, 0, 1, 1], [0, 0, 1, 1], 2, "none", rope=True)
+    shared_case(rs3, b, p, [3, 2, 1, 1], [0, 0, 0, 0], [0, 0, 0, 0], 1, "other")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_shared_readout_by_pairs_of_query_tiles(rs3, d):
+    """Enough work that the plan takes two query tiles per CTA, for the prefix at least."""
+    H = 512 // d
+    b = built(rs3, U=4, H=H, d=d, dtype="bf16", m=64, n=64, window=2, commits=2, n_ptr=0, seed=2, density=0.3)
+    p = built(rs3, U=1, H=H, d=d, dtype="bf16", m=64, n=64, window=-1, ring_frames=3, commits=3, n_ptr=0, seed=3)
+    shared_case(rs3, b, p, [2500, 1200, 900, 640], [0, 0, 0, 0], [0, 0, 0, 0], 1, "inplace")
+
+
+def test_shared_readout_of_many_units(rs3):
+    """Hundreds of units in classes that lie apart; the grid's last word of cells is a part."""
+    U = 600
+    b = built(rs3, U=U, H=1, d=16, dtype="f32", m=3, n=11, window=1, commits=1, n_ptr=0, n_cond=0, seed=2)
+    p = built(rs3, U=7, H=1, d=16, dtype="f32", m=3, n=11, window=2, commits=2, n_ptr=0, seed=3)
+    shared_case(rs3, b, p, [(5 * u) % 34 for u in range(U)], [u % 3 for u in range(U)], [(u * 7) % 8 - 1 for u in range(U)], 3, "none", k_max=33)
+
+
+def test_shared_readout_of_a_bank_that_is_its_own_prefix(rs3):
+    """Unit 0's rows as the prefix of the others, in one bank; twice the same cell."""
+    b = built(rs3, U=3, H=2, d=64, dtype="bf16", m=8, n=9, window=4, commits=7, n_ptr=5, seed=2)
+    q, idx, count, group, prefix_unit, table, out = shared_case(rs3, b, b, [9, 30, 20], [0, 0, 0], [-1, 0, 0], 1)
+    idx[1, 7] = idx[1, 3]
+    again = torch.full_like(out, math.nan)
+    run_shared(rs3, b, b, q, 1, idx, count, group, prefix_unit, table, 0.0, None, again)
+    same = torch.ones(b.mn, dtype=torch.bool, device="cuda")
+    same[torch.from_numpy(np.setdiff1d(np.arange(b.mn), idx[1].cpu().numpy())).cuda()] = False
+    assert torch.equal(bits(again[0]), bits(out[0])) and not again.isnan().any()
+
+
+def test_shared_readout_of_copies_is_the_memory_readout_of_the_fork(rs3):
+    """What a fork that copies its parent's rows reads, within the tolerance of both."""
+    p = built(rs3, U=1, H=1, d=64, dtype="f32", m=8, n=9, window=-1, ring_frames=9, commits=6, n_ptr=0, seed=3)
+    b = built(rs3, U=4, H=1, d=64, dtype="f32", m=8, n=9, window=-1, ring_frames=3, commits=2, n_ptr=0, n_cond=0, seed=4)
+    q, idx, count, group, prefix_unit, table, out = shared_case(rs3, b, p, [20, 30, 40, 9], [0] * 4, [0] * 4, 1)
+    whole = rs3.Bank(4, 1, 64, "f32", 72, 1, -1, 12 * 72, 12, 0)
+    st = status()
+    rs3.rs3_bank_copy(whole, p.bank, torch.zeros(4, dtype=torch.int32, device="cuda"), None, None, st)
+    for f in range(2):                                     # the children's own frames, once more
+        rows = [b.places(u)[0] for u in range(4)]
+        lens = [b.places(u)[1] for u in range(4)]
+        k, v = (torch.zeros((4, 72, 64), device="cuda") for _ in range(2))
+        mask = torch.zeros((4, 72), dtype=torch.uint8, device="cuda")
+        for u in range(4):
+            at = torch.from_numpy(rows[u][sum(lens[u][:f]):sum(lens[u][:f + 1])]).cuda()
+            k[u, :len(at)], v[u, :len(at)], mask[u, :len(at)] = b.bank.k_store[u][at], b.bank.v_store[u][at], 1
+        rs3.rs3_bank_commit(whole, k, v, mask, 0, st)
+    ref = torch.zeros_like(out)
+    ws = torch.empty(rs3.rs3_readout_workspace_bytes(4, 1, 64, 40, "f32"), dtype=torch.uint8, device="cuda")
+    rs3.rs3_memory_readout(q, "f32", 1, 72, 1, 64, group, idx, count, 40, whole, None, None, ref, 0.0, ws, st)
+    assert int(st) == 0
+    vmax = float(torch.cat([p.bank.v_store[0], b.bank.v_store.view(-1, 64)]).abs().clamp(max=999).max())
+    assert float((out - ref).abs().max()) <= vmax * 2.0 ** -13
+
+
+def test_shared_readout_latches_what_the_device_finds(rs3):
+    b = built(rs3, U=6, H=1, d=64, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    p = built(rs3, U=3, H=1, d=64, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=3)
+    g = gen(1)
+    q = torch.randn((2, 72, 64), generator=g, device="cuda").bfloat16()
+    idx, count = keep_sets(6, 72, 20, [20, 20, 20, 20, 20, 20])
+    good = (torch.tensor([0, 0, 1, 0, 0, 0], dtype=torch.int32, device="cuda"), torch.tensor([0, 0, 0, 1, 2, -1], dtype=torch.int32, device="cuda"))
+    clean = torch.zeros((6, 72, 64), dtype=torch.bfloat16, device="cuda")
+    run_shared(rs3, b, p, q, 2, idx, count, good[0], good[1], None, 0.0, None, clean)
+    assert int(b.st) == 0
+
+    def call(group=good[0], prefix=good[1], idx=idx, count=count):
+        b.st.zero_()
+        res = torch.full((6, 72, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+        out = torch.zeros_like(res)
+        run_shared(rs3, b, p, q, 2, idx, count, group, prefix, None, 0.0, res, out)
+        code = int(b.st)
+        b.st.zero_()
+        return code, out, [bool((out[u] == 5).all()) for u in range(6)]
+
+    def put(t, i, v):
+        t = t.clone()
+        t[i] = v
+        return t
+
+    for bad in (dict(group=put(good[0], 1, 2)), dict(group=put(good[0], 1, -1)), dict(prefix=put(good[1], 1, 3)), dict(prefix=put(good[1], 1, -2)),
+                dict(count=put(count, 1, 21)), dict(count=put(count, 1, -1))):
+        code, out, skipped = call(**bad)
+        assert code == rs3.RS3_EINVAL and skipped == [False, True, False, False, False, False], bad
+    code, out, skipped = call(idx=put(put(idx, (1, 3), -1), (1, 4), 72))
+    assert code == rs3.RS3_EINVAL and not any(skipped)
+    # unsound counters: of a unit, and of a prefix (which skips the units that read it)
+    for store, unit, gone in ((b, 3, [3]), (p, 0, [0, 1, 2])):
+        old = store.bank.counters[unit, 1].clone()
+        store.bank.counters[unit, 1] = -5
+        code, out, skipped = call()
+        store.bank.counters[unit, 1] = old
+        assert code == rs3.RS3_EINTERNAL and skipped == [u in gone for u in range(6)]
+
+
+def test_shared_readout_stays_inside_its_workspace_and_repeats_itself(rs3):
+    for dtype, H, d in (("bf16", 2, 64), ("bf16", 1, 256), ("f32", 1, 32)):
+        b = built(rs3, U=3, H=H, d=d, dtype=dtype, m=16, n=20, window=4, commits=5, n_ptr=0, seed=2)
+        p = built(rs3, U=2, H=H, d=d, dtype=dtype, m=16, n=20, window=4, commits=5, n_ptr=0, seed=3)
+        q, idx, count, group, prefix_unit, table, out = shared_case(rs3, b, p, [320, 200, 90], [0, 0, 0], [1, 1, 0], 1)
+        n = rs3.rs3_shared_readout_workspace_bytes(b.bank, p.bank, idx.shape[1])
+        ws = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+        for _ in range(3):
+            again = torch.full_like(out, math.nan)
+            run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, again, ws[:n])
+            assert torch.equal(bits(again), bits(out))
+        assert (ws[n:] == 77).all()
+        with pytest.raises(rs3.RS3Error) as e:
+            run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, out, ws[:n - 256])
+        assert e.value.code == rs3.RS3_ECAPACITY
+
+
+def test_shared_readout_captured_and_on_another_stream(rs3):
+    b = built(rs3, U=3, H=1, d=64, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    p = built(rs3, U=1, H=1, d=64, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=3)
+    q, idx, count, group, prefix_unit, table, out = shared_case(rs3, b, p, [30, 20, 9], [0, 0, 0], [0, 0, 0], 1)
+    ws = run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, out, ws)
+    b.commit(gen(9))
+    q.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = out.clone()
+    out.zero_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, out, ws, side)
+    side.synchronize()
+    assert torch.equal(bits(got), bits(out)) and (got != 0).any()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256)])
+def test_shared_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3, dtype, d):
+    b = built(rs3, U=3, H=1, d=d, dtype=dtype, m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    p = built(rs3, U=1, H=1, d=d, dtype=dtype, m=8, n=9, window=4, commits=5, n_ptr=0, seed=3)
+    q, idx, count, group, prefix_unit, table, out = shared_case(rs3, b, p, [30, 20, 9], [0, 0, 0], [0, 0, 0], 1)
+    limit = rs3.rs3_get_wait_limit_ns()
+    try:
+        rs3.rs3_set_wait_limit_ns(0)
+        again = torch.zeros_like(out)
+        run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, again)
+        code = int(b.st)
+    finally:
+        rs3.rs3_set_wait_limit_ns(limit)
+    assert code == rs3.RS3_ETIMEOUT
+    b.st.zero_()
+    run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, again)
+    assert int(b.st) == 0 and torch.equal(bits(again), bits(out))
