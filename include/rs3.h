@@ -443,8 +443,42 @@ rs3_status rs3_memory_readout_run(const void *q, rs3_dtype dtype, int G, int mn,
                                   rs3_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
-/* Read side: a shared prefix                                               */
+/* Read side: capped and biased scores, frames left out; a shared prefix      */
 /* ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace rs3_scored_readout needs for this bank; never falls as
+ * k_max grows.  0 for an uninitialised bank. */
+size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max);
+
+/*
+ * rs3_memory_readout whose scores are changed before the softmax, by row j's frame:
+ *   s    = scale * (q~ . k_j)
+ *   s    = cap * tanh(s / cap)                     where cap > 0
+ *   s    = s + frame_bias[u][h][f(j)]              where frame_bias is given
+ * over the rows j whose frame_keep[u][f(j)] is not 0 (all without frame_keep), where f(j)
+ * is, with F = bank->max_frames, the number of newer ring frames (its age, 0 for the newest),
+ * F for a row of a conditioning frame and F + 1 for a pointer row: slopes in the age, learned
+ * biases by distance, windows, frames of another shot left out with the conditioning
+ * frames as the prefix that is always seen.
+ *   cap         0 (none) or in [2^-10, 2^10]
+ *   frame_bias  device fp32 [H][F+2], or [U][H][F+2] bias_stride elements apart
+ *               (bias_stride 0: one for all units), or NULL; finite, or minus infinity (the
+ *               row weighs nothing)
+ *   frame_keep  device uint8 [U][F+2] or NULL.  Rows that are left out are not read as far as
+ *               results go: their bits do not matter
+ * A query with no row left, or whose scores are all minus infinity, reads A = 0; a
+ * score that is NaN or plus infinity makes its query's head NaN.  Arguments and results
+ * otherwise as rs3_memory_readout; idx holds distinct cells; a cell outside [0, mn) latches
+ * RS3_EINVAL and is skipped, a count outside [0, k_max] latches it and the unit is skipped.
+ * In bf16 the softmax's weights are rounded to bf16, and so are queries rotated here.
+ * Limits: those of rs3_memory_readout; U * rows_per_unit < 2^31.
+ */
+rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
+                              const int32_t *unit_group, const int32_t *idx, const int32_t *count,
+                              int k_max, const rs3_bank *bank, float cap, const float *frame_bias,
+                              int64_t bias_stride, const uint8_t *frame_keep, const float *rope,
+                              const void *residual, void *out, float scale, void *workspace,
+                              size_t workspace_bytes, int32_t *status, rs3_stream_t stream);
 
 /* Bytes of device workspace rs3_shared_readout needs for these banks; never falls as k_max
  * grows.  0 for an uninitialised bank. */

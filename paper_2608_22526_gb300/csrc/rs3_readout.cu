@@ -50,7 +50,7 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
     rs.slot_base = -1;
     if (cnt < 0 || cnt > a.k_max) {
         if (latch) latch_status(a.status, RS3_EINVAL);
-        cnt = cnt < 0 ? 0 : a.k_max;
+        cnt = cnt < 0 || a.strict ? 0 : a.k_max;
     }
     if (g < 0 || g >= a.G) {
         if (latch) latch_status(a.status, RS3_EINVAL);
@@ -334,6 +334,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         if (u < a.U) {
             RangeSet rs = u0 > 0 ? unit_ranges(a, u, true) : mine;
             cut_tiles(rs, cfg.BM, cfg.BN);
+            if (a.score.tile_n) rs.n_tiles = a.score.tile_n[u];
             a.ranges[u] = rs;
             s_wg[u] = (int64_t)cfg.ov + rs.n_tiles;
             s_nt[u] = rs.n_tiles;
@@ -524,7 +525,10 @@ __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
                 const float mq = __shfl_sync(0xffffffffu, mv.x, q);
                 wq[q] = (q < c.nsplit && M != -INFINITY) ? exp2f(mq - M) : 0.f;
             }
-            if (cell < 0 || cell >= a.mn) cell = 0;
+            if (cell < 0 || cell >= a.mn) {
+                if (a.strict) continue;
+                cell = 0;
+            }
 #pragma unroll
             for (int cb = 0; cb < 2; ++cb) {
                 const int c4 = lane * 4 + 128 * cb;
@@ -551,7 +555,10 @@ __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
             continue;
         }
         int cell = a.idx[(int64_t)c.u * a.k_max + j];
-        if (cell < 0 || cell >= a.mn) cell = 0;
+        if (cell < 0 || cell >= a.mn) {
+            if (a.strict) continue;
+            cell = 0;
+        }
         float M = -INFINITY;
         for (int s = lane; s < c.nsplit; s += 32) M = fmaxf(M, ml[SLOT_REL(s) * BM].x);
 #pragma unroll
@@ -782,6 +789,8 @@ void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout 
     a->bank_unit = nullptr;
     a->bank_U = bank->U;
     a->parts = nullptr;
+    a->strict = 0;
+    a->score = {};
 }
 
 rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -846,6 +855,7 @@ rs3_status rs3_readout_plan_two(const ReadoutArgs &a, const ReadoutArgs &b, rs3_
 // the attention kernel over the plan in the workspace
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st)
 {
+    if (a.score.tile_n) return p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
     if (p.either) return rs3_launch_either_readout(a, st);
     if (p.kind == 1) return rs3_launch_tc_readout(a, st);
     return rs3_launch_simt_readout(a, dtype, st);

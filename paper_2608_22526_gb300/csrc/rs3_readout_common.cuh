@@ -11,6 +11,27 @@ struct GroupParts {         // piece 0 of a group is in slot0, piece s >= 1 in s
     int32_t slot0, slice, n, pad;
 };
 
+// Scores changed by their row's frame (rs3_scored_readout).
+struct ScoreArgs {
+    const int32_t *tile_n;      // [U] key tiles of rows that are read; NULL: the readout's own tiles
+    const int2 *tiles;          // [U][tile_stride] first row (in the unit's storage) and rows of each
+    const int32_t *row_frame;   // [U][rows_per_unit] entry of the bias table of each live row (where there is a table)
+    const float *bias;          // [H][frames], bias_stride elements between units
+    int64_t bias_stride;
+    int tile_stride, frames;
+    float cap;                  // cap * log2(e)
+    float cap_step;             // 2 log2(e) scale / cap: tanh(x) = 1 - 2 / (1 + e^2x)
+};
+
+// What a readout kernel does to a score: nothing, or a cap and a bias by the row's frame.
+struct PlainScores {
+    static constexpr bool on = false, cap = false, bias = false;
+};
+template <bool CAP, bool BIAS>
+struct FrameScores {
+    static constexpr bool on = true, cap = CAP, bias = BIAS;
+};
+
 struct ReadoutArgs {
     const void *q;
     const void *k_store;
@@ -47,6 +68,8 @@ struct ReadoutArgs {
     const int32_t *bank_unit;   // [U] the bank's unit that unit u reads (-1: none); NULL: unit u
     int bank_U;                 // units of the bank
     GroupParts *parts;          // [group] its pieces (groups numbered as the plan does); NULL: whole groups are written out
+    int strict;                 // counts and cells that are out of range are skipped, not taken for others
+    ScoreArgs score;
 };
 
 struct ReadoutPath {
@@ -85,6 +108,8 @@ void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout 
                       const rs3_bank *bank, const float *rope, const void *residual, void *out, float scale, int32_t *status);
 // The attention kernel over the plan in the workspace.
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st);
+rs3_status rs3_launch_scored_tc(const ReadoutArgs &a, cudaStream_t st);
+rs3_status rs3_launch_scored_simt(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st);
 // Two plans in one launch, with the second's pass-through.
 rs3_status rs3_readout_plan_two(const ReadoutArgs &first, const ReadoutArgs &second, rs3_dtype dtype, cudaStream_t st);
 // phases of a readout: the attention over the bank (pass-through, plan,

@@ -193,8 +193,105 @@ __device__ __forceinline__ uint32_t set_up_tc(const CUtensorMap &tmk, const CUte
     return *tmem_slot;
 }
 
+// Scores of FrameScores: what a softmax warp's columns are biased with, and the tiles that hold them.
+constexpr int SCORE_SMEM = 8 * 64 * 4;
+
+// N scores (raw) of consecutive rows into the softmax's, in the log2 domain; b: their biases in
+// shared memory, log2 domain.
+template <class X, int N>
+__device__ __forceinline__ void change_scores(uint32_t (&sr)[N], const ScoreArgs &s, float sc, const float *b)
+{
+#pragma unroll
+    for (int c0 = 0; c0 < N; c0 += 8) {
+        float x[8], add[8];
+#pragma unroll
+        for (int c = 0; c < 8; c += 4) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if constexpr (X::bias) v = *reinterpret_cast<const float4 *>(b + c0 + c);
+            add[c] = v.x; add[c + 1] = v.y; add[c + 2] = v.z; add[c + 3] = v.w;
+        }
+        if constexpr (X::cap) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] = ex2_approx(__uint_as_float(sr[c0 + c]) * s.cap_step) + 1.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x[c]));
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sr[c0 + c] = __float_as_uint(fmaf(x[c], -2.f * s.cap, s.cap + add[c]));
+        } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sr[c0 + c] = __float_as_uint(fmaf(__uint_as_float(sr[c0 + c]), sc, add[c]));
+        }
+    }
+}
+
+// The rows of one work item that a warp's lanes look up ahead: tile -> rows -> frames -> biases, a
+// tile's each a turn of the loop apart, so that none is waited for.
+template <class X, int SCOLS>
+struct RowsAhead {
+    static constexpr int PER = SCOLS / 32;
+    const int2 *tiles;
+    const int32_t *frame;
+    const float *bias;
+    int col, last;              // first column of the lane; the item's last tile
+    int2 e1, e2, e3;            // tiles j + 1, j + 2, j + 3
+    int f2[PER];                // frames of tile j + 2's rows
+    float b1[PER];              // biases of tile j + 1
+
+    __device__ __forceinline__ int2 entry(int t) const { return __ldg(tiles + min(t, last)); }
+    __device__ __forceinline__ void frames_of(const int2 &e)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) f2[i] = col + 32 * i < e.y ? __ldg(frame + e.x + col + 32 * i) : 0;
+    }
+    __device__ __forceinline__ void biases()
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) b1[i] = __ldg(bias + f2[i]) * 1.4426950408889634f;
+    }
+    __device__ __forceinline__ RowsAhead(const ReadoutArgs &a, const WorkItem &w, int first_col)
+    {
+        tiles = a.score.tiles + (int64_t)w.u * a.score.tile_stride;
+        frame = a.score.row_frame + (int64_t)w.u * a.rows_per_unit;
+        bias = a.score.bias + w.u * a.score.bias_stride + (int64_t)w.h * a.score.frames;
+        col = first_col;
+        last = w.tile_end - 1;
+        if (w.tile_end <= w.tile_begin) return;
+        e1 = entry(w.tile_begin);
+        e2 = entry(w.tile_begin + 1);
+        e3 = entry(w.tile_begin + 2);
+        if constexpr (X::bias) {
+            frames_of(e1);
+            biases();
+            frames_of(e2);
+        }
+    }
+    // On to tile t (the first: w.tile_begin): its rows, its biases into `out`.
+    __device__ __forceinline__ int next(int t, float *out)
+    {
+        const int rows = e1.y;
+        if constexpr (X::bias) {
+            __syncwarp();                                  // the tile before has been read
+#pragma unroll
+            for (int i = 0; i < PER; ++i) out[(threadIdx.x & 31) + 32 * i] = b1[i];
+            __syncwarp();
+            biases();
+            frames_of(e3);
+        }
+        e1 = e2;
+        e2 = e3;
+        e3 = entry(t + 3);
+        return rows;
+    }
+};
+
+template <int SCOLS>
+struct RowsAhead<PlainScores, SCOLS> {
+    __device__ __forceinline__ RowsAhead(const ReadoutArgs &, const WorkItem &, int) {}
+    __device__ __forceinline__ int next(int, float *) { return 0; }
+};
+
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
-template <int DH>
+template <int DH, class X = PlainScores>
 __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
                                            uint32_t tmem, int it_begin, int it_end)
 {
@@ -229,7 +326,8 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 if (!mbar_wait(BAR(b_empty + st), ph ^ 1u, abort_flag, wait_ns)) goto producer_done;
                 int64_t row0;
                 int nvalid;
-                tile_rows(rs, t, BN, row0, nvalid);
+                if constexpr (X::on) row0 = __ldg(&a.score.tiles[(int64_t)w.u * a.score.tile_stride + t].x);
+                else tile_rows(rs, t, BN, row0, nvalid);
                 const int y = (int)((int64_t)w.u * a.rows_per_unit + row0);
                 mbar_expect_tx(BAR(b_full + st), (uint32_t)C::KVBYTES);
 #pragma unroll
@@ -311,6 +409,22 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 ok = mbar_wait_warp(BAR(C::B_VFULL + vs), vph, abort_flag, wait_ns) &&
                      mbar_wait_warp(BAR(C::B_PFULL + pb), pph, abort_flag, wait_ns);
                 if (!ok) break;
+                if constexpr (X::on) {
+                    // rows behind the tile's are another's, or left out: whatever their bits, 0 times them is 0
+                    const int nv = __ldg(&a.score.tiles[(int64_t)w.u * a.score.tile_stride + w.tile_begin + j].y);
+                    if (nv < BN) {
+                        const uint32_t at = sV + vs * C::KVBYTES + (uint32_t)nv * 128u;
+                        const int pieces = (BN - nv) * 8;
+#pragma unroll 1
+                        for (int i = lane; i < pieces; i += 32)
+#pragma unroll
+                            for (int c = 0; c < DH / 64; ++c)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (uint32_t)(c * (BN * 128) + i * 16)), "r"(0)
+                                             : "memory");
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
+                }
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t dvs = dv0 + vs * STAGE16, dps = dp0 + pb * PBUF16;
@@ -380,8 +494,14 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
             const RangeSet *rs = a.ranges + w.u;
             const int n = w.tile_end - w.tile_begin;
             const int jrow = w.qt * BM + r;
-            const bool valid = jrow < __ldg(&rs->cnt);
+            bool valid = jrow < __ldg(&rs->cnt);
             int cell = valid ? a.idx[(int64_t)w.u * a.k_max + jrow] : 0;
+            if constexpr (X::on) {
+                if (cell < 0 || cell >= a.mn) {
+                    latch_status(a.status, RS3_EINVAL);
+                    valid = false;
+                }
+            }
             cell = (cell < 0 || cell >= a.mn) ? 0 : cell;
             if (n > 0) {
                 const int gq = a.unit_group[w.u];
@@ -406,11 +526,16 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 rlen[q] = __ldg(&rs->len[q]);
             }
             float m_run = -INFINITY, l_part = 0.f;
+            RowsAhead<X, SCOLS> ahead(a, w, h * SCOLS + lane);
+            // this warp's columns' biases
+            float *sbias = reinterpret_cast<float *>(gbase + C::OFF_MISC + 16) + (warp - 4) * SCOLS;
             for (int j = 0; j < n; ++j) {
                 const uint32_t tj = tcnt + (uint32_t)j, b = tj & 1u;
                 const bool okw = __all_sync(0xffffffffu, mbar_wait(BAR(C::B_SFULL + b), (tj >> 1) & 1u, abort_flag, wait_ns));
                 int nvt = 0;
-                {
+                if constexpr (X::on) {
+                    nvt = ahead.next(w.tile_begin + j, sbias);
+                } else {
                     int t = w.tile_begin + j;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -420,7 +545,8 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 }
                 const int nv = nvt - h * SCOLS;       // valid columns of this slice (may be <= 0)
                 const uint32_t scol = tl + C::S_COL + (uint32_t)BN * b;
-                const float sc = a.scale_log2;
+                constexpr bool changed = X::cap || X::bias;
+                const float sc = changed ? 1.f : a.scale_log2;
                 uint32_t sr[SCOLS], pk[PCOLS];
                 float rowsum = 0.f;
                 if (okw) {
@@ -431,6 +557,7 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(C::B_SFREE + b));
+                    if constexpr (changed) change_scores<X>(sr, a.score, a.scale_log2, sbias);
                     if (nv < SCOLS) mask_cols(sr, nv);
                 }
                 float *redt = red + (b * NSPLIT) * BM;
@@ -445,7 +572,8 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
 #pragma unroll
                     for (int q = 1; q < NSPLIT; ++q) mrow = fmaxf(mrow, redt[q * BM + r]);
                     m_new = mrow * sc;
-                    rowsum = row_exp(sr, pk, sc, m_new);
+                    // (a row whose scores so far are all -inf has no reference yet: their weights are 0)
+                    rowsum = row_exp(sr, pk, sc, X::bias && m_new == -INFINITY ? 0.f : m_new);
                 } else {
                     // Later tiles take their exps against the running reference.
                     // It moves only if the row max grows past it by more than
@@ -453,8 +581,9 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                     // none, so only rows above that (or a timeout) take the slow
                     // path, together with their quarter: exact maxima exchanged,
                     // exps redone against a moved reference, O rescaled.
-                    if (okw) rowsum = row_exp(sr, pk, sc, m_run);
-                    const bool slow = !(rowsum <= 256.0f);
+                    const bool unset = X::bias && m_run == -INFINITY;
+                    if (okw) rowsum = row_exp(sr, pk, sc, unset ? 0.f : m_run);
+                    const bool slow = unset || !(rowsum <= 256.0f);
                     if (bar_or(bar_id, bar_n, slow || !okw)) {
                         redt[h * BM + r] = okw ? row_max(sr) : -INFINITY;
                         if (!bar_and(bar_id, bar_n, okw)) { ok = false; break; }

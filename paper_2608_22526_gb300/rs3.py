@@ -91,6 +91,9 @@ SIGNATURES = {
                                 ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_qk_norm_rope": (_I, [_P, _I64, _I64, _I, _P, _P, _P, _I64, _P, _I64, _I64, _I, _P, _P, _P, _I64,
                               _I, _I, _I, ctypes.c_float, _P, _P]),
+    "rs3_scored_readout_workspace_bytes": (_SZ, [_P, _I]),
+    "rs3_scored_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, ctypes.c_float, _P, _I64, _P, _P, _P, _P, ctypes.c_float,
+                                _P, _SZ, _P, _P]),
     "rs3_shared_readout_workspace_bytes": (_SZ, [_P, _P, _I]),
     "rs3_shared_readout": (_I, [_P, _I, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, ctypes.c_float, _P, _SZ, _P, _P]),
     "rs3_default_rope_spec": (None, [_P]),
@@ -436,6 +439,37 @@ def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope,
         _want(dev, "rope", rope, torch.float32, mn * d)
     _want(dev, "status", status, torch.int32, 1)
     return dev
+
+
+def rs3_scored_readout_workspace_bytes(bank: "Bank", k_max: int) -> int:
+    return int(lib.rs3_scored_readout_workspace_bytes(ctypes.byref(bank.desc), k_max))
+
+
+def rs3_scored_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int, bank: "Bank", cap: float,
+                       frame_bias, frame_keep, rope, residual, out, scale: float, workspace, status, stream=None):
+    """rs3_memory_readout with scores capped at `cap` (0: not), biased by frame_bias fp32 [H, F+2] or [U, H, F+2], over
+    the frames that frame_keep uint8 [U, F+2] leaves; F = bank.max_frames: ages of ring frames, then conditioning
+    frames, then pointers."""
+    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    F, stride = bank.max_frames, 0
+    if frame_bias is not None:
+        if tuple(frame_bias.shape) not in ((H, F + 2), (bank.U, H, F + 2)):
+            raise ValueError(f"frame_bias: [{H}, {F + 2}] or [{bank.U}, {H}, {F + 2}] wanted, got {tuple(frame_bias.shape)}")
+        _want(dev, "frame_bias", frame_bias, torch.float32, 0)
+        stride = H * (F + 2) if frame_bias.dim() == 3 else 0
+    if frame_keep is not None:
+        if tuple(frame_keep.shape) != (bank.U, F + 2):
+            raise ValueError(f"frame_keep: [{bank.U}, {F + 2}] wanted, got {tuple(frame_keep.shape)}")
+        _want(dev, "frame_keep", frame_keep, torch.uint8, 0)
+    _want_workspace(dev, workspace)
+    if residual is not None:
+        _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
+    rc = lib.rs3_scored_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
+                                ctypes.byref(bank.desc), float(cap), _ptr(frame_bias), stride, _ptr(frame_keep), _ptr(rope),
+                                _ptr(residual), _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status),
+                                _stream(stream))
+    _check(rc, "rs3_scored_readout")
 
 
 def rs3_shared_readout_workspace_bytes(bank: "Bank", prefix: "Bank", k_max: int) -> int:

@@ -314,3 +314,276 @@ def test_shared_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3, dt
     b.st.zero_()
     run_shared(rs3, b, p, q, 1, idx, count, group, prefix_unit, table, 0.0, None, again)
     assert int(b.st) == 0 and torch.equal(bits(again), bits(out))
+
+
+# ---------------------------------------------------------------------------
+# capped and biased scores, frames left out
+# ---------------------------------------------------------------------------
+def run_scored(rs3, b, q, G, idx, count, group, cap, bias, keep, table, scale, res, out, ws=None, stream=None):
+    k_max = idx.shape[1]
+    if ws is None:
+        ws = torch.full((rs3.rs3_scored_readout_workspace_bytes(b.bank, k_max),), 255, dtype=torch.uint8, device="cuda")
+    rs3.rs3_scored_readout(q, b.dtype, G, b.mn, b.H, b.d, group, idx, count, k_max, b.bank, cap, bias, keep, table, res, out, scale, ws,
+                           b.st, stream)
+    return ws
+
+
+def scored_rows(b, keep):
+    def rows(u):
+        at, slot = frames_of(b, u)
+        if keep is not None:
+            on = keep[u][slot] != 0
+            at, slot = at[on], slot[on]
+        return b.bank.k_store[u][at], b.bank.v_store[u][at], slot
+    return rows
+
+
+def scored_case(rs3, b, counts, group, G, cap=0.0, bias=None, keep=None, residual="none", rope=False, seed=5, k_max=None, scale=0.0, qs=1.2):
+    U, mn, D, dtype = b.U, b.mn, b.D, b.dtype
+    g = gen(seed)
+    q = (torch.randn((G, mn, D), generator=g, device="cuda") * qs).to(DT[dtype])
+    k_max = max(1, max(counts)) if k_max is None else k_max
+    idx, count = keep_sets(U, mn, k_max, counts, seed)
+    group = torch.tensor(group, dtype=torch.int32, device="cuda")
+    table = rope_table(mn, b.d) if rope else None
+    x = torch.randn((U, mn, D), generator=g, device="cuda").to(DT[dtype])
+    res = None if residual == "none" else x.clone()
+    out = res if residual == "inplace" else torch.full_like(x, math.nan)
+    of = None if bias is None else lambda u, h: bias[u, h] if bias.dim() == 3 else bias[h]
+    want, tol = reference(dtype, b.H, b.d, q, idx, counts, group, table, scale or b.d ** -0.5, None if res is None else x, x.shape,
+                          scored_rows(b, keep), cap, of)
+    ws = run_scored(rs3, b, q, G, idx, count, group, cap, bias, keep, table, scale, res, out)
+    assert int(b.st) == 0
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
+    return q, idx, count, group, table, out, ws
+
+
+def biases(b, kind, seed=3):
+    F = b.bank.max_frames
+    if kind == "age":
+        age = torch.arange(F + 2, device="cuda").float()
+        age[F:] = 0
+        return (-age[None] * torch.tensor([2.0 ** (-h) for h in range(b.H)], device="cuda")[:, None]).contiguous()
+    if kind == "unit":
+        return torch.randn((b.U, b.H, F + 2), generator=gen(seed), device="cuda") * 2
+    if kind == "holes":                                    # minus infinity for some frames, for all of one head of a unit
+        t = torch.randn((b.U, b.H, F + 2), generator=gen(seed), device="cuda")
+        t = torch.where(torch.rand(t.shape, generator=gen(seed + 1), device="cuda") < 0.5, -math.inf, t)
+        t[0, 0] = -math.inf
+        return t
+    return None
+
+
+def keeps(b, kind, seed=7):
+    F = b.bank.max_frames
+    if kind == "all":
+        return None
+    t = (torch.rand((b.U, F + 2), generator=gen(seed), device="cuda") < 0.5).to(torch.uint8) * 3
+    if kind == "alternate":
+        t[:] = (torch.arange(F + 2, device="cuda") % 2 == 0).to(torch.uint8)
+    if kind == "nothing":
+        t[0] = 0
+    return t
+
+
+def spoil(b, keep):
+    """NaN in every row that is not read."""
+    for u in range(b.U):
+        at, slot = frames_of(b, u)
+        on = torch.zeros(b.bank.rows_per_unit, dtype=torch.bool, device="cuda")
+        on[at if keep is None else at[keep[u][slot] != 0]] = True
+        for t in (b.bank.k_store, b.bank.v_store):
+            t[u, ~on] = math.nan
+
+
+LAYOUTS = [dict(window=4, commits=7, n_ptr=5), dict(window=-1, ring_frames=9, commits=9, n_ptr=3, n_cond=2),
+           dict(window=1, commits=2, n_cond=0, n_ptr=0), dict(window=6, commits=3, n_ptr=0)]
+
+
+@pytest.mark.parametrize("dtype,H,d", SHAPES)
+@pytest.mark.parametrize("counts", [[1, 0, 3], [72, 17, 33]])
+@pytest.mark.parametrize("cap,bias,keep,residual,rope", [(0.0, None, "some", "none", False), (5.0, None, "all", "inplace", True),
+                                                         (0.0, "age", "alternate", "other", False), (2.5, "unit", "nothing", "inplace", False),
+                                                         (30.0, "holes", "some", "none", True), (0.0, "holes", "all", "other", False)])
+def test_scored_readout_matches_64_bits(rs3, dtype, H, d, counts, cap, bias, keep, residual, rope):
+    """Wrapped rings, units without rows, NaN in dead rows and in those that are left out."""
+    b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=8, n=9, empty=(1,), seed=2, **LAYOUTS[(d // 16 + len(residual)) % 4])
+    rs3.rs3_bank_reset(b.bank, 1)
+    kp = keeps(b, keep)
+    spoil(b, kp)
+    scored_case(rs3, b, counts, [0, 1, 0], 2, cap, biases(b, bias), kp, residual, rope, scale=0.2 if rope else 0.0)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 2, 128), ("bf16", 1, 256), ("f32", 1, 64), ("f32", 1, 256), ("bf16", 2, 32)])
+@pytest.mark.parametrize("keep", ["all", "some"])
+def test_scored_readout_of_long_banks(rs3, dtype, H, d, keep):
+    """Rows split over many pieces, hundreds of small frames, many query tiles."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=32, n=33, window=-1, ring_frames=300, commits=290, n_ptr=3, seed=3, density=0.03)
+    kp = keeps(b, keep)
+    spoil(b, kp)
+    scored_case(rs3, b, [300, 7], [0, 0], 1, 8.0, biases(b, "unit"), kp, "inplace")
+    scored_case(rs3, b, [1, 1056], [0, 0], 1, 0.0, biases(b, "age"), kp, "none")
+    c = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=32, n=33, window=5, commits=8, n_ptr=0, seed=3, density=0.9)
+    kp = keeps(c, keep)
+    spoil(c, kp)
+    scored_case(rs3, c, [1056, 513], [0, 1], 2, 8.0, biases(c, "unit"), kp, "other", rope=True)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256), ("f32", 32)])
+def test_scored_readout_of_scores_of_all_sizes(rs3, dtype, d):
+    """Scores far beyond the cap and far below it, biases of thousands, references that move late."""
+    b = Built(rs3, U=2, H=1, d=d, dtype=dtype, m=16, n=17, window=-1, ring_frames=12, commits=12, n_ptr=0, seed=3, scale=6.0)
+    F = b.bank.max_frames
+    spoil(b, None)
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 2.0 ** -10, None, None)
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 2.0 ** 10, None, None, qs=0.01)
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 20.0, None, None, qs=3.0)
+    # the oldest rows are read first: the reference climbs by 100 from frame to frame, or starts at minus infinity
+    climb = -100.0 * torch.arange(F + 2, device="cuda").float()[None]
+    climb[:, F:] = -5000.0
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 10.0, climb.contiguous(), None)
+    late = torch.full((1, F + 2), -math.inf, device="cuda")
+    late[:, 0] = -3000.0
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 0.0, late, None)
+    late[:, 5] = 3000.0
+    scored_case(rs3, b, [100, 40], [0, 0], 1, 3.0, late, None)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 256), ("f32", 2, 64)])
+def test_scored_readout_without_a_change_is_the_memory_readout(rs3, dtype, H, d):
+    b = built(rs3, U=3, H=H, d=d, dtype=dtype, m=16, n=17, window=4, commits=7, n_ptr=5, seed=2)
+    q, idx, count, group, table, out, _ = scored_case(rs3, b, [250, 0, 100], [0, 0, 0], 1, rope=True)
+    ref = torch.full_like(out, math.nan)
+    ws = torch.empty(rs3.rs3_readout_workspace_bytes(3, H, d, 250, dtype), dtype=torch.uint8, device="cuda")
+    rs3.rs3_memory_readout(q, dtype, 1, b.mn, H, d, group, idx, count, 250, b.bank, table, None, ref, 0.0, ws, b.st)
+    vmax = float(b.bank.v_store.float().where(b.bank.v_store.float() < 999, 0.0).abs().max())
+    assert float((out.float() - ref.float()).abs().max()) <= vmax * (2.0 ** -6 if dtype == "bf16" else 2.0 ** -13)
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 1, 64), ("bf16", 1, 256), ("f32", 1, 64)])
+def test_scored_readout_of_scores_that_are_no_numbers(rs3, dtype, H, d):
+    """A key with NaN makes its queries NaN, unless its frame is left out."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    spoil(b, None)
+    at, slot = frames_of(b, 0)
+    b.bank.k_store[0, at[slot == 1][0]] = math.nan
+    q = torch.randn((1, 72, H * d), generator=gen(1), device="cuda").to(DT[dtype])
+    idx, count = keep_sets(2, 72, 30, [30, 30])
+    group = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for cap in (0.0, 4.0):
+        out = torch.zeros((2, 72, H * d), dtype=DT[dtype], device="cuda")
+        run_scored(rs3, b, q, 1, idx, count, group, cap, biases(b, "age"), None, None, 0.0, None, out)
+        assert out[0, idx[0].long()].isnan().all() and not out[1].isnan().any()
+        keep = torch.ones((2, b.bank.max_frames + 2), dtype=torch.uint8, device="cuda")
+        keep[:, 1] = 0
+        out.zero_()
+        run_scored(rs3, b, q, 1, idx, count, group, cap, biases(b, "age"), keep, None, 0.0, None, out)
+        assert not out.isnan().any() and (out[0] != 0).any()
+
+
+def test_scored_readout_latches_what_the_device_finds(rs3):
+    for dtype, d in (("bf16", 64), ("f32", 32)):
+        b = built(rs3, U=4, H=1, d=d, dtype=dtype, m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+        q = torch.randn((2, 72, d), generator=gen(1), device="cuda").to(DT[dtype])
+        idx, count = keep_sets(4, 72, 20, [20] * 4)
+        group = torch.tensor([0, 0, 1, 0], dtype=torch.int32, device="cuda")
+
+        def call(group=group, idx=idx, count=count):
+            b.st.zero_()
+            res = torch.full((4, 72, d), 5.0, dtype=DT[dtype], device="cuda")
+            out = torch.zeros_like(res)
+            run_scored(rs3, b, q, 2, idx, count, group, 9.0, biases(b, "age"), None, None, 0.0, res, out)
+            code = int(b.st)
+            b.st.zero_()
+            return code, out, [bool((out[u] == 5).all()) for u in range(4)]
+
+        def put(t, i, v):
+            t = t.clone()
+            t[i] = v
+            return t
+
+        assert call()[0] == 0
+        for bad in (dict(group=put(group, 1, 2)), dict(group=put(group, 1, -1)), dict(count=put(count, 1, 21)), dict(count=put(count, 1, -1))):
+            code, out, skipped = call(**bad)
+            assert code == rs3.RS3_EINVAL and skipped == [False, True, False, False], bad
+        clean = call()[1]
+        for bad in (-1, 72):
+            code, out, skipped = call(idx=put(idx, (1, 3), bad))
+            gone = torch.zeros(72, dtype=torch.bool, device="cuda")
+            gone[int(idx[1, 3])] = True
+            assert code == rs3.RS3_EINVAL and (out[1, gone] == 5).all() and torch.equal(bits(out[1, ~gone]), bits(clean[1, ~gone]))
+        old = b.bank.counters[3, 1].clone()
+        b.bank.counters[3, 1] = -5
+        code, out, skipped = call()
+        b.bank.counters[3, 1] = old
+        assert code == rs3.RS3_EINTERNAL and skipped == [False, False, False, True]
+
+
+def test_scored_readout_stays_inside_its_workspace_and_repeats_itself(rs3):
+    for dtype, H, d in (("bf16", 2, 64), ("bf16", 1, 256), ("f32", 1, 32)):
+        b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=16, n=20, window=4, commits=5, n_ptr=7, seed=2)
+        kp = keeps(b, "alternate")
+        spoil(b, kp)
+        bias = biases(b, "unit")
+        q, idx, count, group, table, out, _ = scored_case(rs3, b, [320, 200, 90], [0, 0, 0], 1, 6.0, bias, kp)
+        n = rs3.rs3_scored_readout_workspace_bytes(b.bank, idx.shape[1])
+        ws = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+        for _ in range(3):
+            again = torch.full_like(out, math.nan)
+            run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, kp, table, 0.0, None, again, ws[:n])
+            assert torch.equal(bits(again), bits(out))
+        assert (ws[n:] == 77).all()
+        with pytest.raises(rs3.RS3Error) as e:
+            run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, kp, table, 0.0, None, out, ws[:n - 256])
+        assert e.value.code == rs3.RS3_ECAPACITY
+
+
+def test_scored_readout_captured_and_on_another_stream(rs3):
+    b = Built(rs3, U=3, H=1, d=64, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    b.bank.k_store.nan_to_num_(0.0)
+    b.bank.v_store.nan_to_num_(0.0)
+    bias, kp = biases(b, "unit"), keeps(b, "some")
+    q, idx, count, group, table, out, ws = scored_case(rs3, b, [30, 20, 9], [0, 0, 0], 1, 6.0, bias, kp)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, kp, None, 0.0, None, out, ws)
+    b.commit(gen(9))
+    kp[:, :2] = 1
+    bias.add_(0.5)
+    q.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = out.clone()
+    out.zero_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, kp, None, 0.0, None, out, ws, side)
+    side.synchronize()
+    assert torch.equal(bits(got), bits(out)) and (got != 0).any()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_scored_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3, d):
+    b = Built(rs3, U=2, H=1, d=d, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+    spoil(b, None)
+    bias = biases(b, "age")
+    q, idx, count, group, table, out, ws = scored_case(rs3, b, [30, 9], [0, 0], 1, 6.0, bias)
+    limit = rs3.rs3_get_wait_limit_ns()
+    again = torch.zeros_like(out)
+    try:
+        rs3.rs3_set_wait_limit_ns(0)
+        run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, None, None, 0.0, None, again, ws)
+        code = int(b.st)
+    finally:
+        rs3.rs3_set_wait_limit_ns(limit)
+    assert code == rs3.RS3_ETIMEOUT
+    b.st.zero_()
+    again.zero_()
+    run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, None, None, 0.0, None, again, ws)
+    assert int(b.st) == 0 and (again != 0).any()
+    on = torch.zeros_like(again, dtype=torch.bool)
+    for u in range(2):
+        on[u, idx[u, :int(count[u])].long()] = True
+    assert torch.equal(bits(again)[on], bits(out)[on])
