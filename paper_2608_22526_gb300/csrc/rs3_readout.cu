@@ -292,6 +292,7 @@ __device__ __forceinline__ bool two_tiles(const ReadoutArgs &a, const RangeSet &
     for (int u = threadIdx.x; u < a.U; u += PLAN_THREADS) {
         RangeSet rs = u < PLAN_THREADS ? mine : unit_ranges(a, u, false);
         cut_tiles(rs, 128, 128);
+        if (a.score.tile_n) rs.n_tiles = a.score.pair_tile_n[u];
         s1 += (float)rs.nq * (float)rs.n_tiles;
         s2 += (float)((rs.nq + 1) >> 1) * (float)rs.n_tiles;
     }
@@ -334,7 +335,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         if (u < a.U) {
             RangeSet rs = u0 > 0 ? unit_ranges(a, u, true) : mine;
             cut_tiles(rs, cfg.BM, cfg.BN);
-            if (a.score.tile_n) rs.n_tiles = a.score.tile_n[u];
+            if (a.score.tile_n) rs.n_tiles = (pairs ? a.score.pair_tile_n : a.score.tile_n)[u];
             a.ranges[u] = rs;
             s_wg[u] = (int64_t)cfg.ov + rs.n_tiles;
             s_nt[u] = rs.n_tiles;
@@ -855,7 +856,10 @@ rs3_status rs3_readout_plan_two(const ReadoutArgs &a, const ReadoutArgs &b, rs3_
 // the attention kernel over the plan in the workspace
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st)
 {
-    if (a.score.tile_n) return p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
+    if (a.score.tile_n) {
+        if (p.either) return rs3_launch_scored_either(a, st);
+        return p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
+    }
     if (p.either) return rs3_launch_either_readout(a, st);
     if (p.kind == 1) return rs3_launch_tc_readout(a, st);
     return rs3_launch_simt_readout(a, dtype, st);

@@ -15,12 +15,16 @@ struct GroupParts {         // piece 0 of a group is in slot0, piece s >= 1 in s
 struct ScoreArgs {
     const int32_t *tile_n;      // [U] key tiles of rows that are read; NULL: the readout's own tiles
     const int2 *tiles;          // [U][tile_stride] first row (in the unit's storage) and rows of each
+    const int32_t *pair_tile_n; // the same for the kernel with two query tiles
+    const int2 *pair_tiles;
     const int32_t *row_frame;   // [U][rows_per_unit] entry of the bias table of each live row (where there is a table)
     const float *bias;          // [H][frames], bias_stride elements between units
     int64_t bias_stride;
     int tile_stride, frames;
     float cap;                  // cap * log2(e)
     float cap_step;             // 2 log2(e) scale / cap: tanh(x) = 1 - 2 / (1 + e^2x)
+    float cap_half;             // raw scores up to here have |x| <= 1/2, where the polynomial holds
+    float cap_poly[4];          // cap * log2(e) * tanh(x) / raw score, by powers of the raw score's square
 };
 
 // What a readout kernel does to a score: nothing, or a cap and a bias by the row's frame.
@@ -108,6 +112,7 @@ void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout 
                       const rs3_bank *bank, const float *rope, const void *residual, void *out, float scale, int32_t *status);
 // The attention kernel over the plan in the workspace.
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st);
+rs3_status rs3_launch_scored_either(const ReadoutArgs &a, cudaStream_t st);
 rs3_status rs3_launch_scored_tc(const ReadoutArgs &a, cudaStream_t st);
 rs3_status rs3_launch_scored_simt(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st);
 // Two plans in one launch, with the second's pass-through.

@@ -87,6 +87,7 @@ struct Cfg {
     static_assert(KSTK >= 2 && KSTV >= 2 && NBAR <= 64, "K/V stages");
     static_assert(4 * NSPLIT * 32 * 36 * 4 <= NPB * PBYTES, "epilogue staging fits in the P ring");
     static_assert(OCOLS % 32 == 0, "epilogue stages 32 columns at a time");
+    static_assert(OFF_MISC % 16 == 0, "what lies behind is read 16 bytes at a time");
 };
 static_assert(Cfg<256>::SMEM <= 232448 && Cfg<128>::SMEM <= 232448 && Cfg<64>::SMEM <= 232448,
               "shared memory budget");
@@ -193,101 +194,228 @@ __device__ __forceinline__ uint32_t set_up_tc(const CUtensorMap &tmk, const CUte
     return *tmem_slot;
 }
 
-// Scores of FrameScores: what a softmax warp's columns are biased with, and the tiles that hold them.
-constexpr int SCORE_SMEM = 8 * 64 * 4;
-
-// N scores (raw) of consecutive rows into the softmax's, in the log2 domain; b: their biases in
-// shared memory, log2 domain.
-template <class X, int N>
-__device__ __forceinline__ void change_scores(uint32_t (&sr)[N], const ScoreArgs &s, float sc, const float *b)
+// Largest |score| of N.
+template <int N>
+__device__ __forceinline__ float row_size(const uint32_t (&sr)[N])
 {
+    float m[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < N; c += 2)
+        m[c / 2 & 3] = fmaxf(m[c / 2 & 3], fmaxf(fabsf(__uint_as_float(sr[c])), fabsf(__uint_as_float(sr[c + 1]))));
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+// Two columns' scores in place.
+template <int N>
+__device__ __forceinline__ uint64_t get_pair(const uint32_t (&sr)[N], int c)
+{
+    return f2pack(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+}
+template <int N>
+__device__ __forceinline__ void put_pair(uint32_t (&sr)[N], int c, uint64_t v)
+{
+    float lo, hi;
+    f2unpack(v, lo, hi);
+    sr[c] = __float_as_uint(lo);
+    sr[c + 1] = __float_as_uint(hi);
+}
+
+// What the key producer's warp leaves for the softmax beside a tile, in a ring of slots in shared
+// memory: its biases (log2 domain), the number of its rows, and whether one bias holds for all (most
+// tiles lie in one frame).  A slot is written before the tile's K is announced, so whoever has
+// seen its scores sees it.  It is written again R tiles later, when the K stage of that tile
+// has been given back: the S of KST tiles before is done, for which the scores of `behind`
+// tiles before that one had been read, so R >= KST + behind + 1 (everything before those is finished).
+struct TileBias {
+    const float *each;
+    float all;
+    bool same;
+    int rows;
+};
+
+template <class X, int BN, int KST, int BEHIND>
+struct BiasRing {
+    static constexpr int R = KST + BEHIND + 1, SLOT = (X::bias ? BN * 4 : 0) + 16, BYTES = X::on ? R * SLOT : 0;
+    // of the tile with this running number
+    static __device__ __forceinline__ TileBias read(const uint8_t *ring, uint32_t t)
+    {
+        const uint8_t *slot = ring + (t % R) * SLOT;
+        const int4 h = *reinterpret_cast<const int4 *>(slot);
+        return {reinterpret_cast<const float *>(slot + 16), __int_as_float(h.y), h.z != 0, h.x};
+    }
+};
+
+// s * sc + bias
+template <int N>
+__device__ __forceinline__ void bias_scores(uint32_t (&sr)[N], float sc, const TileBias &b)
+{
+    const uint64_t sc2 = f2pack(sc, sc);
+#pragma unroll
+    for (int c = 0; c < N; c += 4) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(b.each + c);
+        put_pair(sr, c, fma2(get_pair(sr, c), sc2, v.x));
+        put_pair(sr, c + 2, fma2(get_pair(sr, c + 2), sc2, v.y));
+    }
+}
+
+// cap tanh(s scale / cap) for |s| <= cap_half: s times a polynomial in s^2.
+template <int N>
+__device__ __forceinline__ void cap_small(uint32_t (&sr)[N], const ScoreArgs &s)
+{
+    uint64_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = f2pack(s.cap_poly[i], s.cap_poly[i]);
+#pragma unroll
+    for (int c0 = 0; c0 < N; c0 += 8) {                                // (sixteen at a time spill)
+        uint64_t z[4], p[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) z[c] = mul2(get_pair(sr, c0 + 2 * c), get_pair(sr, c0 + 2 * c));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) p[c] = fma2(z[c], k[3], k[2]);
+#pragma unroll
+        for (int i = 1; i >= 0; --i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) p[c] = fma2(p[c], z[c], k[i]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) put_pair(sr, c0 + 2 * c, mul2(get_pair(sr, c0 + 2 * c), p[c]));
+    }
+}
+
+// The same for any score: cap - 2 cap / (1 + e^2x).  The reciprocals of four scores are one, of their
+// product, times the others; e^2x is cut at 2^30 (tanh(x) is 1 in fp32 there), so that the product
+// stays finite.
+template <int N>
+__device__ __forceinline__ void cap_any(uint32_t (&sr)[N], const ScoreArgs &s)
+{
+    const uint64_t step2 = f2pack(s.cap_step, s.cap_step), one2 = f2pack(1.f, 1.f), cap2 = f2pack(s.cap, s.cap),
+                   twice2 = f2pack(-2.f * s.cap, -2.f * s.cap);
 #pragma unroll
     for (int c0 = 0; c0 < N; c0 += 8) {
-        float x[8], add[8];
+        float x[8];
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) f2unpack(mul2(get_pair(sr, c0 + c), step2), x[c], x[c + 1]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) asm("min.NaN.f32 %0, %0, %1;" : "+f"(x[c]) : "f"(30.f));      // (a NaN stays one)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[c] = ex2_approx(x[c]);
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) f2unpack(add2(f2pack(x[c], x[c + 1]), one2), x[c], x[c + 1]);
 #pragma unroll
         for (int c = 0; c < 8; c += 4) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if constexpr (X::bias) v = *reinterpret_cast<const float4 *>(b + c0 + c);
-            add[c] = v.x; add[c + 1] = v.y; add[c + 2] = v.z; add[c + 3] = v.w;
-        }
-        if constexpr (X::cap) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[c] = ex2_approx(__uint_as_float(sr[c0 + c]) * s.cap_step) + 1.f;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x[c]));
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sr[c0 + c] = __float_as_uint(fmaf(x[c], -2.f * s.cap, s.cap + add[c]));
-        } else {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) sr[c0 + c] = __float_as_uint(fmaf(__uint_as_float(sr[c0 + c]), sc, add[c]));
+            const float p = x[c] * x[c + 1], r = x[c + 2] * x[c + 3];
+            float i = p * r;
+            asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(i));
+            const float ip = i * r, ir = i * p;
+            put_pair(sr, c0 + c, fma2(f2pack(ip * x[c + 1], ip * x[c]), twice2, cap2));
+            put_pair(sr, c0 + c + 2, fma2(f2pack(ir * x[c + 3], ir * x[c + 2]), twice2, cap2));
         }
     }
 }
 
-// The rows of one work item that a warp's lanes look up ahead: tile -> rows -> frames -> biases, a
-// tile's each a turn of the loop apart, so that none is waited for.
-template <class X, int SCOLS>
+// N scores (raw) of consecutive rows into the softmax's: afterwards a score in the log2 domain is
+// sr * sc + off.  A bias that is the same for all of a tile's columns stays out of the scores.  A warp
+// whose scores are all within half the cap (`size`: the largest |s|) takes the polynomial, on the fp32
+// pipe beside the softmax's powers.  Columns of no row hold zeros (they share a reciprocal with others).
+template <class X, int N>
+__device__ __forceinline__ void change_scores(uint32_t (&sr)[N], const ScoreArgs &s, const TileBias &b, float size, float &sc, float &off)
+{
+    if constexpr (X::cap) {
+        if (__any_sync(0xffffffffu, !(size <= s.cap_half))) cap_any(sr, s);
+        else cap_small(sr, s);
+        sc = 1.f;
+    }
+    off = X::bias && b.same ? b.all : 0.f;
+    if constexpr (X::bias)
+        if (!b.same) {
+            bias_scores(sr, sc, b);
+            sc = 1.f;
+        }
+}
+
+// Rows [nv, BN) of a stage (DH / 64 blocks of BN rows of 128 bytes) become zeros, by a whole warp,
+// for the matrix instructions that it issues next.
+template <int DH, int BN>
+__device__ __forceinline__ void zero_rows(uint32_t stage, int nv)
+{
+    const uint32_t at = stage + (uint32_t)nv * 128u;
+#pragma unroll 1
+    for (int i = threadIdx.x & 31; i < (BN - nv) * 8; i += 32)
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (uint32_t)(c * (BN * 128) + i * 16)), "r"(0) : "memory");
+    fence_proxy_async();
+    __syncwarp();
+}
+
+// The rows of one work item, looked up ahead by the key producer's warp: tile -> rows -> frames ->
+// biases, a turn of its loop each, so that none is waited for.
+template <class X, int BN>
 struct RowsAhead {
-    static constexpr int PER = SCOLS / 32;
+    static constexpr int PER = BN / 32;
     const int2 *tiles;
     const int32_t *frame;
     const float *bias;
-    int col, last;              // first column of the lane; the item's last tile
-    int2 e1, e2, e3;            // tiles j + 1, j + 2, j + 3
-    int f2[PER];                // frames of tile j + 2's rows
-    float b1[PER];              // biases of tile j + 1
+    int last;                   // the item's last tile
+    int2 e1, e2, e3;            // tiles j, j + 1, j + 2
+    int f2[PER];                // frames of tile j + 1's rows: this lane's columns lane, lane + 32, ...
+    float b1[PER];              // biases of tile j
 
     __device__ __forceinline__ int2 entry(int t) const { return __ldg(tiles + min(t, last)); }
     __device__ __forceinline__ void frames_of(const int2 &e)
     {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) f2[i] = col + 32 * i < e.y ? __ldg(frame + e.x + col + 32 * i) : 0;
+        for (int i = 0; i < PER; ++i) {
+            const int col = (int)(threadIdx.x & 31) + 32 * i;
+            f2[i] = __ldg(frame + e.x + min(col, e.y - 1));            // columns behind the tile's rows: as its last row
+        }
     }
     __device__ __forceinline__ void biases()
     {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) b1[i] = __ldg(bias + f2[i]) * 1.4426950408889634f;
+        for (int i = 0; i < PER; ++i) b1[i] = __ldg(bias + f2[i]);
     }
-    __device__ __forceinline__ RowsAhead(const ReadoutArgs &a, const WorkItem &w, int first_col)
+    __device__ __forceinline__ RowsAhead(const ReadoutArgs &a, const int2 *table, const WorkItem &w)
     {
-        tiles = a.score.tiles + (int64_t)w.u * a.score.tile_stride;
-        frame = a.score.row_frame + (int64_t)w.u * a.rows_per_unit;
-        bias = a.score.bias + w.u * a.score.bias_stride + (int64_t)w.h * a.score.frames;
-        col = first_col;
+        tiles = table + (int64_t)w.u * a.score.tile_stride;
         last = w.tile_end - 1;
         if (w.tile_end <= w.tile_begin) return;
         e1 = entry(w.tile_begin);
         e2 = entry(w.tile_begin + 1);
         e3 = entry(w.tile_begin + 2);
         if constexpr (X::bias) {
+            frame = a.score.row_frame + (int64_t)w.u * a.rows_per_unit;
+            bias = a.score.bias + w.u * a.score.bias_stride + (int64_t)w.h * a.score.frames;
             frames_of(e1);
             biases();
             frames_of(e2);
         }
     }
-    // On to tile t (the first: w.tile_begin): its rows, its biases into `out`.
-    __device__ __forceinline__ int next(int t, float *out)
+    // Tile t (the first: w.tile_begin) into its slot; returns its first row.
+    __device__ __forceinline__ int next(int t, uint8_t *slot)
     {
-        const int rows = e1.y;
+        const int2 e = e1;
+        const int lane = threadIdx.x & 31;
+        float all = 0.f;
+        bool same = true;
         if constexpr (X::bias) {
-            __syncwarp();                                  // the tile before has been read
+            all = __shfl_sync(0xffffffffu, b1[0], 0) * 1.4426950408889634f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) out[(threadIdx.x & 31) + 32 * i] = b1[i];
-            __syncwarp();
+            for (int i = 0; i < PER; ++i) {
+                const float v = b1[i] * 1.4426950408889634f;
+                reinterpret_cast<float *>(slot + 16)[lane + 32 * i] = v;
+                same = same && v == all;
+            }
+            same = __all_sync(0xffffffffu, same);
             biases();
             frames_of(e3);
         }
+        if (lane == 0) *reinterpret_cast<int4 *>(slot) = make_int4(e.y, __float_as_int(all), same, 0);
+        __syncwarp();
         e1 = e2;
         e2 = e3;
         e3 = entry(t + 3);
-        return rows;
+        return e.x;
     }
-};
-
-template <int SCOLS>
-struct RowsAhead<PlainScores, SCOLS> {
-    __device__ __forceinline__ RowsAhead(const ReadoutArgs &, const WorkItem &, int) {}
-    __device__ __forceinline__ int next(int, float *) { return 0; }
 };
 
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
@@ -307,7 +435,35 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint64_t wait_ns = a.wait_ns;
 
-    if ((warp == 0 || warp == 2) && lane == 0) {
+    using Ring = BiasRing<X, C::BN, C::KSTK, 2>;             // an S needs the scores of two tiles before read
+    uint8_t *ring = gbase + C::OFF_MISC + 16;
+    if (X::on && warp == 0) {
+        // ------------------------------------------------------------------
+        // TMA producer of the keys, and what the softmax has to know of each tile
+        // ------------------------------------------------------------------
+        uint32_t cnt = 0;
+        bool ok = true;
+        if constexpr (X::on) {
+            for (int it = it_begin; it < it_end && ok; ++it) {
+                const WorkItem w = a.items[it];
+                RowsAhead<X, C::BN> ahead(a, a.score.tiles, w);
+                for (int t = w.tile_begin; t < w.tile_end; ++t, ++cnt) {
+                    const uint32_t st = cnt % KSTK;
+                    ok = mbar_wait_warp(BAR(C::B_KEMPTY + st), ((cnt / KSTK) & 1u) ^ 1u, abort_flag, wait_ns);
+                    if (!ok) break;
+                    const int y = (int)((int64_t)w.u * a.rows_per_unit) + ahead.next(t, ring + (cnt % Ring::R) * Ring::SLOT);
+                    if (lane == 0) {
+                        mbar_expect_tx(BAR(C::B_KFULL + st), (uint32_t)C::KVBYTES);
+#pragma unroll
+                        for (int c = 0; c < DH / 64; ++c)
+                            tma_load_2d(sK + st * C::KVBYTES + c * (BN * 128), &tmk, BAR(C::B_KFULL + st), w.h * DH + c * 64, y);
+                    }
+                }
+            }
+        }
+        if (lane == 0)
+            for (uint32_t k = (cnt > KSTK ? cnt - KSTK : 0); k < cnt; ++k) mbar_drain(BAR(C::B_KFULL + k % KSTK), (k / KSTK) & 1u);
+    } else if ((warp == 0 || warp == 2) && lane == 0) {
         // ------------------------------------------------------------------
         // TMA producers (warp 0: keys, warp 2: values)
         // ------------------------------------------------------------------
@@ -412,18 +568,7 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 if constexpr (X::on) {
                     // rows behind the tile's are another's, or left out: whatever their bits, 0 times them is 0
                     const int nv = __ldg(&a.score.tiles[(int64_t)w.u * a.score.tile_stride + w.tile_begin + j].y);
-                    if (nv < BN) {
-                        const uint32_t at = sV + vs * C::KVBYTES + (uint32_t)nv * 128u;
-                        const int pieces = (BN - nv) * 8;
-#pragma unroll 1
-                        for (int i = lane; i < pieces; i += 32)
-#pragma unroll
-                            for (int c = 0; c < DH / 64; ++c)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + (uint32_t)(c * (BN * 128) + i * 16)), "r"(0)
-                                             : "memory");
-                        fence_proxy_async();
-                        __syncwarp();
-                    }
+                    if (nv < BN) zero_rows<DH, BN>(sV + vs * C::KVBYTES, nv);
                 }
                 tc_fence_after();
                 if (elect_one()) {
@@ -526,15 +671,17 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 rlen[q] = __ldg(&rs->len[q]);
             }
             float m_run = -INFINITY, l_part = 0.f;
-            RowsAhead<X, SCOLS> ahead(a, w, h * SCOLS + lane);
-            // this warp's columns' biases
-            float *sbias = reinterpret_cast<float *>(gbase + C::OFF_MISC + 16) + (warp - 4) * SCOLS;
             for (int j = 0; j < n; ++j) {
                 const uint32_t tj = tcnt + (uint32_t)j, b = tj & 1u;
-                const bool okw = __all_sync(0xffffffffu, mbar_wait(BAR(C::B_SFULL + b), (tj >> 1) & 1u, abort_flag, wait_ns));
                 int nvt = 0;
+                TileBias tb;
+                const bool okw = __all_sync(0xffffffffu, mbar_wait(BAR(C::B_SFULL + b), (tj >> 1) & 1u, abort_flag, wait_ns));
                 if constexpr (X::on) {
-                    nvt = ahead.next(w.tile_begin + j, sbias);
+                    if (okw) {
+                        tb = Ring::read(ring, tj);
+                        tb.each += h * SCOLS;
+                        nvt = tb.rows;
+                    }
                 } else {
                     int t = w.tile_begin + j;
 #pragma unroll
@@ -546,7 +693,7 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                 const int nv = nvt - h * SCOLS;       // valid columns of this slice (may be <= 0)
                 const uint32_t scol = tl + C::S_COL + (uint32_t)BN * b;
                 constexpr bool changed = X::cap || X::bias;
-                const float sc = changed ? 1.f : a.scale_log2;
+                float sc = a.scale_log2, off = 0.f;        // a score in the log2 domain: sr * sc + off
                 uint32_t sr[SCOLS], pk[PCOLS];
                 float rowsum = 0.f;
                 if (okw) {
@@ -557,9 +704,13 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(BAR(C::B_SFREE + b));
-                    if constexpr (changed) change_scores<X>(sr, a.score, a.scale_log2, sbias);
+                    if constexpr (X::cap)                              // (columns of no row share a reciprocal with others)
+                        if (nv < SCOLS) mask_cols(sr, nv, 0u);
+                    if constexpr (changed) change_scores<X>(sr, a.score, tb, X::cap ? row_size(sr) : 0.f, sc, off);
                     if (nv < SCOLS) mask_cols(sr, nv);
                 }
+                const auto scored = [&](float x) { return X::bias ? fmaf(x, sc, off) : x * sc; };
+                const auto against = [&](float m) { return X::bias ? (m == -INFINITY ? 0.f : m) - off : m; };
                 float *redt = red + (b * NSPLIT) * BM;
                 float m_new = m_run;
                 if (j == 0) {
@@ -571,9 +722,9 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                     float mrow = redt[r];
 #pragma unroll
                     for (int q = 1; q < NSPLIT; ++q) mrow = fmaxf(mrow, redt[q * BM + r]);
-                    m_new = mrow * sc;
+                    m_new = scored(mrow);
                     // (a row whose scores so far are all -inf has no reference yet: their weights are 0)
-                    rowsum = row_exp(sr, pk, sc, X::bias && m_new == -INFINITY ? 0.f : m_new);
+                    rowsum = row_exp(sr, pk, sc, against(m_new));
                 } else {
                     // Later tiles take their exps against the running reference.
                     // It moves only if the row max grows past it by more than
@@ -582,7 +733,7 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                     // path, together with their quarter: exact maxima exchanged,
                     // exps redone against a moved reference, O rescaled.
                     const bool unset = X::bias && m_run == -INFINITY;
-                    if (okw) rowsum = row_exp(sr, pk, sc, unset ? 0.f : m_run);
+                    if (okw) rowsum = row_exp(sr, pk, sc, against(m_run));
                     const bool slow = unset || !(rowsum <= 256.0f);
                     if (bar_or(bar_id, bar_n, slow || !okw)) {
                         redt[h * BM + r] = okw ? row_max(sr) : -INFINITY;
@@ -590,9 +741,9 @@ __device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorM
                         float mrow = redt[r];
 #pragma unroll
                         for (int q = 1; q < NSPLIT; ++q) mrow = fmaxf(mrow, redt[q * BM + r]);
-                        if (mrow * sc > m_run + 8.0f) {
-                            m_new = mrow * sc;
-                            rowsum = row_exp(sr, pk, sc, m_new);
+                        if (scored(mrow) > m_run + 8.0f) {
+                            m_new = scored(mrow);
+                            rowsum = row_exp(sr, pk, sc, against(m_new));
                         }
                         const bool grow = m_new != m_run;
                         const float alpha = grow ? ex2_approx(m_run - m_new) : 1.0f;

@@ -25,12 +25,13 @@ struct Stretch { int64_t x, y; };
 struct FramesArgs {
     BankDev bank;
     const uint8_t *keep;        // [U][F + 2] or NULL
-    int32_t *tile_n;            // [U]
-    Stretch *stretch;           // [U][F] first and end ring position of frames that are read and follow one another
-    int4 *runs;                 // [U][F + 4] storage rows of those and of the other regions: (first row, rows, first tile)
-    int2 *tiles;                // [U][tile_stride]
+    int32_t *tile_n;            // [tables][U]
+    Stretch *stretch;           // [tables][U][F] first and end ring position of frames that are read and follow one another
+    int4 *runs;                 // [tables][U][F + 4] storage rows of those and of the other regions: (first row, rows, first tile)
+    int2 *tiles;                // [tables][U][tile_stride]
     int32_t *row_frame;         // [U][rows_per_unit], or NULL without biases
-    int tile_stride, BN;
+    int tile_stride, U, tables;
+    int BN[2];                  // rows of a tile, of either table
 };
 
 constexpr int FRAMES_THREADS = 256;
@@ -97,17 +98,19 @@ struct UnitFrames {
     __device__ __forceinline__ bool ptr_read() const { return !keep || keep[F + 1] != 0; }
 };
 
-__device__ void unit_tiles(const FramesArgs &f, int u)
+__device__ void unit_tiles(const FramesArgs &f, int u, int table)
 {
     const BankDev &b = f.bank;
+    const int BN = f.BN[table];
+    const int64_t slot = (int64_t)table * f.U + u;
     UnitFrames x;
     const bool sound = x.load(b, f.keep, u);
     if (!sound) {                                          // (the plan latches it)
-        if (threadIdx.x == 0) f.tile_n[u] = 0;
+        if (threadIdx.x == 0) f.tile_n[slot] = 0;
         return;
     }
-    Stretch *stretch = f.stretch + (int64_t)u * x.F;
-    int4 *runs = f.runs + (int64_t)u * (x.F + 4);
+    Stretch *stretch = f.stretch + slot * x.F;
+    int4 *runs = f.runs + slot * (x.F + 4);
     // stretches of frames that are read: the first frame of one writes where it begins, the last where it ends
     int n_str = 0;
     for (int i0 = 0; i0 < x.n; i0 += FRAMES_THREADS) {
@@ -127,7 +130,7 @@ __device__ void unit_tiles(const FramesArgs &f, int u)
     __syncthreads();
     // runs of storage rows: the pinned ones, the stretches (cut at the ring's end), the pointers
     int n_runs = 0, n_tiles = 0;
-    const int sh = 31 - __clz(f.BN);
+    const int sh = 31 - __clz(BN);
     for (int k0 = 0; k0 < n_str + 2; k0 += FRAMES_THREADS) {
         const int k = k0 + threadIdx.x;
         int64_t row[2] = {0, 0}, len[2] = {0, 0};
@@ -146,7 +149,7 @@ __device__ void unit_tiles(const FramesArgs &f, int u)
                 len[1] = s.y - s.x - len[0];
             }
         }
-        const int t0 = (int)((len[0] + f.BN - 1) >> sh), t1 = (int)((len[1] + f.BN - 1) >> sh);
+        const int t0 = (int)((len[0] + BN - 1) >> sh), t1 = (int)((len[1] + BN - 1) >> sh);
         int r = (t0 > 0) + (t1 > 0), t = t0 + t1, all_r, all_t;
         scan_two(r, t, all_r, all_t);
         r += n_runs;
@@ -156,9 +159,9 @@ __device__ void unit_tiles(const FramesArgs &f, int u)
         n_runs += all_r;
         n_tiles += all_t;
     }
-    if (threadIdx.x == 0) f.tile_n[u] = n_tiles;
+    if (threadIdx.x == 0) f.tile_n[slot] = n_tiles;
     __syncthreads();
-    int2 *tiles = f.tiles + (int64_t)u * f.tile_stride;
+    int2 *tiles = f.tiles + slot * f.tile_stride;
     for (int t = threadIdx.x; t < n_tiles; t += FRAMES_THREADS) {
         int lo = 0, hi = n_runs;                           // the last run that begins at or before tile t
         while (hi - lo > 1) {
@@ -167,7 +170,7 @@ __device__ void unit_tiles(const FramesArgs &f, int u)
         }
         const int4 r = runs[lo];
         const int at = (t - r.z) << sh;
-        tiles[t] = make_int2(r.x + at, min(f.BN, r.y - at));
+        tiles[t] = make_int2(r.x + at, min(BN, r.y - at));
     }
 }
 
@@ -203,8 +206,9 @@ __global__ void __launch_bounds__(FRAMES_THREADS) k_frames(const __grid_constant
 {
     pdl_wait();
     const int u = blockIdx.y;
-    if (blockIdx.x == 0) unit_tiles(f, u);
-    else unit_rows(f, u, ((int)blockIdx.x - 1) * (FRAMES_THREADS / 32) + ((int)threadIdx.x >> 5), ((int)gridDim.x - 1) * (FRAMES_THREADS / 32));
+    const int x = (int)blockIdx.x - f.tables;
+    if (x < 0) unit_tiles(f, u, (int)blockIdx.x);
+    else unit_rows(f, u, x * (FRAMES_THREADS / 32) + ((int)threadIdx.x >> 5), ((int)gridDim.x - f.tables) * (FRAMES_THREADS / 32));
 }
 
 // Byte offsets in the workspace.
@@ -213,23 +217,25 @@ struct ScoredLayout {
     ReadoutLayout l;
     size_t stretch, runs, tiles, rows, ws, total;
     int64_t tile_stride;
+    int tables;                 // of key tiles: where a head's two kernels have tiles of different rows, two
 };
 
 ScoredLayout scored_layout(const rs3_bank *bank, int k_max)
 {
     const int U = bank->U, F = bank->max_frames;
     ScoredLayout L;
-    // one query tile per CTA: a call of so few queries that the other kernel has no part in it
-    L.path = choose_readout_path((rs3_dtype)bank->dtype, bank->d, U, bank->H, 1, bank->rows_per_unit, SIZE_MAX);
+    L.path = choose_readout_path((rs3_dtype)bank->dtype, bank->d, U, bank->H, k_max, bank->rows_per_unit, SIZE_MAX);
+    L.tables = L.path.either && L.path.BN != 128 ? 2 : 1;
+    const size_t n = (size_t)U * L.tables;
     L.l = rs3_readout_layout(U, bank->H, bank->d, k_max, L.path, false);
     L.tile_stride = bank->rows_per_unit / L.path.BN + F + 4;       // whole tiles, and a part at each run's end
-    size_t off = align_up((size_t)U * 4, 256);
+    size_t off = align_up(n * 4, 256);
     L.stretch = off;
-    off = align_up(off + (size_t)U * F * 16, 256);
+    off = align_up(off + n * F * 16, 256);
     L.runs = off;
-    off = align_up(off + (size_t)U * (F + 4) * 16, 256);
+    off = align_up(off + n * (F + 4) * 16, 256);
     L.tiles = off;
-    off = align_up(off + (size_t)U * L.tile_stride * 8, 256);
+    off = align_up(off + n * L.tile_stride * 8, 256);
     L.rows = off;
     off = align_up(off + (size_t)U * bank->rows_per_unit * 4, 256);
     L.ws = off;
@@ -271,13 +277,18 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     f.tiles = reinterpret_cast<int2 *>(ws + L.tiles);
     f.row_frame = frame_bias ? reinterpret_cast<int32_t *>(ws + L.rows) : nullptr;
     f.tile_stride = (int)L.tile_stride;
-    f.BN = L.path.BN;
+    f.U = bank->U;
+    f.tables = L.tables;
+    f.BN[0] = L.path.BN;
+    f.BN[1] = 128;
     ReadoutArgs a;
     rs3_readout_fill(&a, L.path, L.l, ws + L.ws, q, G, mn, H, d, unit_group, idx, count, k_max, bank->U, bank, rope, residual, out, scale,
                      status);
     a.strict = 1;
     a.score.tile_n = f.tile_n;
     a.score.tiles = f.tiles;
+    a.score.pair_tile_n = f.tile_n + (L.tables - 1) * (int64_t)bank->U;
+    a.score.pair_tiles = f.tiles + (L.tables - 1) * (int64_t)bank->U * L.tile_stride;
     a.score.row_frame = f.row_frame;
     a.score.bias = frame_bias;
     a.score.bias_stride = bias_stride;
@@ -287,8 +298,20 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     a.score.cap = cap * log2e;
     // tensor cores: of a raw score, for e^2x; CUDA cores: of one in the log2 domain, for tanh itself
     if (cap > 0.f) a.score.cap_step = L.path.kind == 1 ? 2.f * a.scale_log2 / cap : 1.f / a.score.cap;
+    if (cap > 0.f) {
+        // tanh(x) / x in x^2 with the least largest relative error over 0 < x <= 1/2 (alternation points found in 64
+        // bits): 5.4e-7, with its roundings 6.2e-7
+        static const double poly[4] = {0.99999945577, -0.33326317936, 0.13190296603, -0.04440222613};
+        const double unit = (double)a.scale_log2 / a.score.cap;
+        a.score.cap_half = (float)(0.5 / unit);
+        double by = unit * a.score.cap;
+        for (int i = 0; i < 4; ++i, by *= unit * unit) {
+            a.score.cap_poly[i] = (float)(poly[i] * by);
+            if (!(std::fabs(a.score.cap_poly[i]) > 1e-30f && std::fabs(a.score.cap_poly[i]) < 1e30f)) a.score.cap_half = -1.f;   // out of range: never
+        }
+    }
     const int row_ctas = frame_bias ? std::min((F + COND_PIECES + 1 + 7) / 8, 32) : 0;
-    launch_pdl(k_frames, dim3((unsigned)(1 + row_ctas), (unsigned)bank->U), dim3(FRAMES_THREADS), 0, st, f);
+    launch_pdl(k_frames, dim3((unsigned)(L.tables + row_ctas), (unsigned)bank->U), dim3(FRAMES_THREADS), 0, st, f);
     if (cudaGetLastError() != cudaSuccess) return RS3_ECUDA;
     return rs3_readout_launch(a, L.path, L.l.max_combine, dtype, st, RS3_PHASE_ATTEND | RS3_PHASE_MERGE);
 }

@@ -1,7 +1,7 @@
 // rs3_scored_tc.cu -- the one-tile tensor-core readout (rs3_readout_tc.cuh) over scores that are
 // capped and biased by their row's frame.  A cap costs a score two instructions of the special-function
-// unit (a power and a reciprocal) beside the softmax's one, and a row's bias is read by its
-// column's threads from shared memory.
+// unit beside the softmax's one at most (change_scores), and the key producer's warp looks the
+// rows' biases up.
 #include "rs3_readout_tc.cuh"
 
 namespace tc {
@@ -18,8 +18,8 @@ k_readout_scored(const ReadoutArgs a, const __grid_constant__ CUtensorMap tmk, c
 template <int DH, class X>
 rs3_status launch_scored(const ReadoutArgs &a, cudaStream_t st)
 {
-    constexpr int smem = Cfg<DH>::SMEM + SCORE_SMEM;
-    static_assert(smem <= 232448 && 8 * Cfg<DH>::SCOLS * 4 <= SCORE_SMEM, "shared memory budget");
+    constexpr int smem = Cfg<DH>::SMEM + BiasRing<X, Cfg<DH>::BN, Cfg<DH>::KSTK, 2>::BYTES;
+    static_assert(smem <= 232448, "shared memory budget");
     if (rs3_kernel_smem((const void *)k_readout_scored<DH, X>, smem) != RS3_OK) return RS3_ECUDA;
     const int64_t rows = (int64_t)a.bank_U * a.rows_per_unit;
     if (rows >= (int64_t)1 << 31) return RS3_EUNSUPPORTED;

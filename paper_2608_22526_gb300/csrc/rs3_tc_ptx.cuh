@@ -405,11 +405,11 @@ __device__ __forceinline__ float row_max(const uint32_t (&sr)[N])
 
 // Scores of keys past a range's end (columns at or past nv) become -inf: p = 0.
 template <int N>
-__device__ __forceinline__ void mask_cols(uint32_t (&sr)[N], int nv)
+__device__ __forceinline__ void mask_cols(uint32_t (&sr)[N], int nv, uint32_t with = 0xff800000u)
 {
 #pragma unroll
     for (int c = 0; c < N; ++c)
-        if (c >= nv) sr[c] = 0xff800000u;
+        if (c >= nv) sr[c] = with;
 }
 
 // p = 2^(s sc - ref) as bf16 pairs; returns their sum.  The scale-and-shift and

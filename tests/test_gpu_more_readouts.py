@@ -167,9 +167,9 @@ def test_shared_readout_of_long_prefixes_and_many_queries(rs3, dtype, H, d):
 @pytest.mark.parametrize("d", [64, 128])
 def test_shared_readout_by_pairs_of_query_tiles(rs3, d):
     """Enough work that the plan takes two query tiles per CTA, for the prefix at least."""
-    H = 512 // d
+    H, frames = 512 // d, 3 if d == 64 else 10
     b = built(rs3, U=4, H=H, d=d, dtype="bf16", m=64, n=64, window=2, commits=2, n_ptr=0, seed=2, density=0.3)
-    p = built(rs3, U=1, H=H, d=d, dtype="bf16", m=64, n=64, window=-1, ring_frames=3, commits=3, n_ptr=0, seed=3)
+    p = built(rs3, U=1, H=H, d=d, dtype="bf16", m=64, n=64, window=-1, ring_frames=frames, commits=frames, n_ptr=0, seed=3)
     shared_case(rs3, b, p, [2500, 1200, 900, 640], [0, 0, 0, 0], [0, 0, 0, 0], 1, "inplace")
 
 
@@ -430,6 +430,17 @@ def test_scored_readout_of_long_banks(rs3, dtype, H, d, keep):
     scored_case(rs3, c, [1056, 513], [0, 1], 2, 8.0, biases(c, "unit"), kp, "other", rope=True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,bias,keep", [(10.0, "unit", "some"), (0.0, "age", "alternate"), (6.0, None, "all"), (0.0, "holes", "all"), (0.0, None, "some")])
+def test_scored_readout_by_pairs_of_query_tiles(rs3, d, cap, bias, keep):
+    """Enough work that the plan takes two query tiles per CTA."""
+    H, frames = 512 // d, 4 if d == 64 else 11
+    b = Built(rs3, U=4, H=H, d=d, dtype="bf16", m=64, n=64, window=-1, ring_frames=frames, commits=frames, n_ptr=3, seed=2, density=0.6)
+    kp = keeps(b, keep)
+    spoil(b, kp)
+    scored_case(rs3, b, [2500, 1200, 129, 640], [0, 0, 0, 0], 1, cap, biases(b, bias), kp, "inplace")
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256), ("f32", 32)])
 def test_scored_readout_of_scores_of_all_sizes(rs3, dtype, d):
     """Scores far beyond the cap and far below it, biases of thousands, references that move late."""
@@ -564,12 +575,15 @@ def test_scored_readout_captured_and_on_another_stream(rs3):
     assert torch.equal(bits(got), bits(out)) and (got != 0).any()
 
 
-@pytest.mark.parametrize("d", [64, 128, 256])
-def test_scored_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3, d):
-    b = Built(rs3, U=2, H=1, d=d, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
+@pytest.mark.parametrize("d,pairs", [(64, False), (128, False), (256, False), (64, True)])
+def test_scored_readout_wait_limit_runs_out_and_the_context_stays_usable(rs3, d, pairs):
+    if pairs:
+        b = Built(rs3, U=2, H=16, d=d, dtype="bf16", m=64, n=64, window=-1, ring_frames=4, commits=4, n_ptr=0, seed=2)
+    else:
+        b = Built(rs3, U=2, H=1, d=d, dtype="bf16", m=8, n=9, window=4, commits=5, n_ptr=0, seed=2)
     spoil(b, None)
     bias = biases(b, "age")
-    q, idx, count, group, table, out, ws = scored_case(rs3, b, [30, 9], [0, 0], 1, 6.0, bias)
+    q, idx, count, group, table, out, ws = scored_case(rs3, b, [2000, 1100] if pairs else [30, 9], [0, 0], 1, 6.0, bias)
     limit = rs3.rs3_get_wait_limit_ns()
     again = torch.zeros_like(out)
     try:
