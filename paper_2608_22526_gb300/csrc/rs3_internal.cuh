@@ -46,7 +46,7 @@ struct RangeSet {           // a unit's bank as <= 4 contiguous row ranges
     int32_t nq;             // query tiles of BM rows
     int32_t cnt;            // kept queries (clamped to k_max)
     int32_t splits;         // KV splits per (head, query tile)
-    int32_t slot_base;      // number of the unit's first group, where results stay in partial slots
+    int32_t first_group;    // number of the unit's first group, where results stay in partial slots
     int32_t pad[3];
 };
 
@@ -68,7 +68,8 @@ struct ReadoutHeader {
     int32_t slices;
     int32_t n_part;         // partial pieces of all split groups
     int32_t bm;             // query rows of an item: which kernel the items are for
-    int32_t pad[27];
+    int32_t n_groups;
+    int32_t pad[26];
 };
 
 struct ReadoutLayout {      // byte offsets inside the workspace

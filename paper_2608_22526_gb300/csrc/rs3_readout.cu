@@ -47,7 +47,7 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
     for (int r = 0; r < 4; ++r) { rs.start[r] = 0; rs.len[r] = 0; rs.tiles[r] = 0; }
     rs.n_tiles = rs.nq = rs.cnt = 0;
     rs.splits = 1;
-    rs.slot_base = -1;
+    rs.first_group = -1;
     if (cnt < 0 || cnt > a.k_max) {
         if (latch) latch_status(a.status, RS3_EINVAL);
         cnt = cnt < 0 || a.strict ? 0 : a.k_max;
@@ -235,7 +235,7 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
             if (whole && a.parts) {
                 const int32_t g = v.gb[u] + gl;
                 w.slot = 2 * a.grid_ctas + g;
-                a.parts[g] = {w.slot, 0, 1, 0};
+                a.parts[g] = {w.slot, 0, 1, u, h, qt, v.cnt[u], 0};
             }
             a.items[idx] = w;
             if (first < 0) first = idx;
@@ -252,7 +252,7 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
                 c.nsplit = (int32_t)(e - b + 1);
                 c.pad[1] = v.cnt[u];
                 if (a.parts) {
-                    a.parts[v.gb[u] + gl] = {c.slot0, b, c.nsplit, 0};
+                    a.parts[v.gb[u] + gl] = {c.slot0, b, c.nsplit, u, h, qt, v.cnt[u], 0};
                     c.nsplit = 0;                   // merged by the caller
                 }
             }
@@ -349,7 +349,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         if (u < a.U) {
             s_tb[u] = off + run;
             s_gb[u] = goff + grun;
-            if (a.parts) a.ranges[u].slot_base = goff + grun;
+            if (a.parts) a.ranges[u].first_group = goff + grun;
         }
         run += tot;
         grun += gtot;
@@ -407,6 +407,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         hdr->slices = v.P;
         hdr->n_part = s_np;
         hdr->bm = cfg.BM;
+        hdr->n_groups = grun;
     }
 }
 

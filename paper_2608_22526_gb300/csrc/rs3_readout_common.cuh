@@ -7,8 +7,9 @@
 #define RS3_MAX_UNITS 4096  // units per readout call
 #define RS3_PAIR_ITEMS (1 << 30)   // above every item index
 
-struct GroupParts {         // piece 0 of a group is in slot0, piece s >= 1 in slot 2 (slice + s)
-    int32_t slot0, slice, n, pad;
+struct GroupParts {         // a group's n pieces: 0 is in slot0, s >= 1 in slot 2 (slice + s); whose they are
+    int32_t slot0, slice, n, u, h, qt;
+    int32_t cnt, pad;       // kept queries of the unit
 };
 
 // Scores changed by their row's frame (rs3_scored_readout).

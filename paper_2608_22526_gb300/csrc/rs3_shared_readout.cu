@@ -13,6 +13,7 @@
 //   k_plan_two    the readout's stream-K plans of the classes over the prefix bank and of the
 //                 units over their own, every result in partial slots
 //   k_readout_*   the readout's kernels over either plan, on the bank each reads
+//   k_merge_prefix  between the two, the classes' pieces: one for each row and head
 //   k_merge_two   log-sum-exp merge of a row's pieces over both banks, and the scatter
 #include "rs3_readout_common.cuh"
 
@@ -32,13 +33,14 @@ struct ShareArgs {
     int U, G, mn, k_max, words, class_stride, prefix_U;
 };
 
-constexpr int SHARE_THREADS = 256;
+constexpr int SHARE_THREADS = 512;
 constexpr int SHARE_WORDS = RS3_MAX_MN / 32;
 
 // The unit's prefix, -1 for none, -2 when its arguments are not sound.
-__device__ __forceinline__ int prefix_of(const ShareArgs &a, int u, int &g)
+__device__ __forceinline__ int prefix_of(const ShareArgs &a, int u, int &g, int &n)
 {
-    const int p = a.prefix_unit[u], n = a.count[u];
+    const int p = a.prefix_unit[u];
+    n = a.count[u];
     g = a.unit_group[u];
     return g < 0 || g >= a.G || n < 0 || n > a.k_max || p < -1 || p >= a.prefix_U ? -2 : p;
 }
@@ -47,50 +49,55 @@ __global__ void __launch_bounds__(SHARE_THREADS) k_classes(const __grid_constant
 {
     pdl_wait();
     __shared__ uint32_t s_bits[SHARE_WORDS];
-    __shared__ int s_list[SHARE_THREADS], s_n, s_first, s_sum[SHARE_THREADS / 32];
+    __shared__ int s_unit[SHARE_THREADS], s_kept[SHARE_THREADS], s_n, s_first, s_sum[SHARE_THREADS / 32];
     const int u = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-    int g, gv;
-    const int p = prefix_of(a, u, g);
+    int g, gv, n, nv;
+    const int p = prefix_of(a, u, g, n);
     if (t == 0) s_first = u;
     for (int w = t; w < a.words; w += SHARE_THREADS) s_bits[w] = 0u;
-    __syncthreads();
-    if (p >= 0)
-        for (int v = t; v < u; v += SHARE_THREADS)
-            if (prefix_of(a, v, gv) == p && gv == g) atomicMin(&s_first, v);
-    __syncthreads();
+    // the class's units, some at a time, and their kept cells; a unit with one before it leaves that to it
+    for (int v0 = 0; p >= 0 && v0 < a.U; v0 += SHARE_THREADS) {
+        if (t == 0) s_n = 0;
+        __syncthreads();
+        const int v = v0 + t;
+        if (v < a.U && prefix_of(a, v, gv, nv) == p && gv == g) {
+            if (v < u) atomicMin(&s_first, v);
+            const int at = atomicAdd(&s_n, 1);
+            s_unit[at] = v;
+            s_kept[at] = nv;
+        }
+        __syncthreads();
+        if (s_first < u) break;
+        const int64_t all = (int64_t)s_n * a.k_max;
+        for (int64_t i = t; i < all; i += 4 * SHARE_THREADS) {
+            int cell[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int64_t at = i + x * SHARE_THREADS;
+                const int m = at < all ? (int)(at / a.k_max) : 0, j = (int)(at - (int64_t)m * a.k_max);
+                cell[x] = at < all && j < s_kept[m] ? __ldg(a.idx + (int64_t)s_unit[m] * a.k_max + j) : INT32_MIN;
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (cell[x] >= 0 && cell[x] < a.mn) atomicOr(&s_bits[cell[x] >> 5], 1u << (cell[x] & 31));
+                else if (cell[x] != INT32_MIN) latch_status(a.status, RS3_EINVAL);
+            }
+        }
+        __syncthreads();                                   // the list is read, the bits are set
+    }
     const bool leads = p >= 0 && s_first == u;
     if (t == 0) {
         if (p == -2) latch_status(a.status, RS3_EINVAL);
-        a.own_count[u] = p == -2 ? 0 : a.count[u];
+        a.own_count[u] = p == -2 ? 0 : n;
         a.leader[u] = p >= 0 ? s_first : -1;
         a.class_group[u] = leads ? g : 0;
         a.class_bank[u] = leads ? p : -1;
         if (!leads) a.class_count[u] = 0;
     }
     if (!leads) return;
-    // the kept cells of the class's units
-    for (int v0 = u; v0 < a.U; v0 += SHARE_THREADS) {
-        if (t == 0) s_n = 0;
-        __syncthreads();
-        const int v = v0 + t;
-        if (v < a.U && prefix_of(a, v, gv) == p && gv == g) s_list[atomicAdd(&s_n, 1)] = v;
-        __syncthreads();
-        const int n = s_n;
-        for (int i = 0; i < n; ++i) {
-            const int w = s_list[i], kept = a.count[w];
-            const int32_t *row = a.idx + (int64_t)w * a.k_max;
-            for (int j = t; j < kept; j += SHARE_THREADS) {
-                const int cell = row[j];
-                if (cell >= 0 && cell < a.mn) atomicOr(&s_bits[cell >> 5], 1u << (cell & 31));
-                else latch_status(a.status, RS3_EINVAL);
-            }
-        }
-        __syncthreads();
-    }
-    // their places: a thread takes two words (512 at most)
-    const int w0 = 2 * t;
-    const uint32_t b0 = w0 < a.words ? s_bits[w0] : 0u, b1 = w0 + 1 < a.words ? s_bits[w0 + 1] : 0u;
-    const int mine = __popc(b0) + __popc(b1);
+    // their places: a thread takes a word (512 at most)
+    uint32_t b = t < a.words ? s_bits[t] : 0u;
+    const int mine = __popc(b);
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -107,16 +114,12 @@ __global__ void __launch_bounds__(SHARE_THREADS) k_classes(const __grid_constant
     }
     if (t == 0) a.class_count[u] = total;
     int32_t *out = a.class_idx + (int64_t)u * a.class_stride;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (w0 + i >= a.words) break;
-        uint32_t b = i ? b1 : b0;
-        a.bits[(int64_t)u * a.words + w0 + i] = b;
-        a.before[(int64_t)u * a.words + w0 + i] = at;
-        for (; b; b &= b - 1u) out[at++] = (w0 + i) * 32 + __ffs(b) - 1;
-    }
+    if (t >= a.words) return;
+    a.bits[(int64_t)u * a.words + t] = b;
+    a.before[(int64_t)u * a.words + t] = at;
+    for (; b; b &= b - 1u) out[at++] = t * 32 + __ffs(b) - 1;
 }
-static_assert(2 * SHARE_THREADS >= SHARE_WORDS, "words of a thread");
+static_assert(SHARE_THREADS >= SHARE_WORDS, "a word each");
 
 // A row's pieces over one bank.
 struct Pieces {
@@ -125,92 +128,200 @@ struct Pieces {
     int64_t step;                          // rows of a slot
     int n, slot0, slice;
     __device__ __forceinline__ int64_t slot(int s) const { return s == 0 ? slot0 : 2 * (int64_t)(slice + s); }
-    __device__ __forceinline__ float2 at(int s) const { return __ldg(ml + slot(s) * step); }
 };
 
-__device__ __forceinline__ Pieces pieces_of(const ReadoutArgs &a, int u, int j, int h)
+__device__ __forceinline__ GroupParts load_parts(const GroupParts *g)
 {
-    const int BM = a.header->bm;
-    const GroupParts g = a.parts[a.ranges[u].slot_base + j / BM * a.H + h];
+    const int4 *p = reinterpret_cast<const int4 *>(g);
+    const int4 a = __ldg(p), b = __ldg(p + 1);
+    return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+constexpr int PREFIX_PIECES = 4;           // more pieces of a class's row than these are merged ahead
+
+// Of row r of a group; `merged`: many pieces have become one, in the first's slot.
+__device__ __forceinline__ Pieces pieces_of(const ReadoutArgs &a, const GroupParts &g, int r, int BM, bool merged)
+{
     Pieces p;
-    p.ml = reinterpret_cast<const float2 *>(a.part_ml) + j % BM;
-    p.o = a.part_o + (int64_t)(j % BM) * a.d;
+    p.ml = reinterpret_cast<const float2 *>(a.part_ml) + r;
+    p.o = a.part_o + (int64_t)r * a.d;
     p.step = BM;
-    p.n = g.n;
+    p.n = merged && g.n > PREFIX_PIECES ? 1 : g.n;
     p.slot0 = g.slot0;
     p.slice = g.slice;
     return p;
 }
 
-// L lanes take a row of one head, four columns each at a time.
-template <typename T, int L>
-__global__ void __launch_bounds__(256) k_merge_two(const __grid_constant__ ReadoutArgs own, const __grid_constant__ ReadoutArgs pre,
-                                                   const __grid_constant__ ShareArgs s)
+// Merges a row's pieces of two lists (the second may be empty).  L lanes take four columns each
+// (twice, for heads of 256); with SPLIT a whole warp takes one row, each L lanes every (32 / L)-th
+// piece, else each L lanes a row of their own (n 0: none).  The pieces' (m, l) are shared out among the
+// row's lanes, and their weights come from the lane that holds their m.  Returns with the columns' sums,
+// not divided by l.  Every lane of the warp calls it.
+template <int L, int CB, bool SPLIT>
+__device__ __forceinline__ void merge_row(const Pieces &p, const Pieces &q, int d, float4 (&acc)[CB], float &M, float &l)
 {
-    pdl_wait();
-    const int lane = threadIdx.x % L;
-    const int64_t rows = (int64_t)own.U * own.k_max * own.H;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; i < rows; i += (int64_t)gridDim.x * (256 / L)) {
-        const int h = (int)(i % own.H);
-        const int64_t r = i / own.H;
-        const int u = (int)(r / own.k_max), j = (int)(r - (int64_t)u * own.k_max);
-        if (j >= own.ranges[u].cnt) continue;              // (0 for a unit that is skipped)
-        const int cell = __ldg(s.idx + r);
-        if (cell < 0 || cell >= own.mn) {
-            if (lane == 0) latch_status(own.status, RS3_EINVAL);
-            continue;
+    constexpr int W = SPLIT ? 32 : L;                      // lanes of a row
+    constexpr int S = W / L, F = 4;                        // sub-groups of a row's lanes; pieces of each in flight
+    const int lane = threadIdx.x % W, sub = lane / L, col = 4 * (lane % L), n = p.n + q.n;
+    const int most = SPLIT ? n : __reduce_max_sync(0xffffffffu, n);
+    const auto ml = [&](int i) { return i < p.n ? __ldcg(p.ml + p.slot(i) * p.step) : __ldcg(q.ml + q.slot(i - p.n) * q.step); };
+    float4 o[F][CB];
+    const auto load = [&](int i0) {                        // pieces i0 + sub, i0 + S + sub, ... of the row
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            const int i = i0 + S * f + sub;
+            const bool in = i < n, first = i < p.n;
+            const int64_t row = first ? p.slot(i) * p.step : q.slot(i - p.n) * q.step;
+            const float *src = (first ? p.o : q.o) + (in ? row * d : 0) + col;
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+                o[f][c] = in ? __ldcg(reinterpret_cast<const float4 *>(src + 128 * c)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const int c = s.leader[u];
-        Pieces p[2];
-        p[0] = pieces_of(own, u, j, h);
-        p[1].n = 0;
-        if (c >= 0) {
-            const int64_t w = (int64_t)c * s.words + (cell >> 5);
-            const int place = s.before[w] + __popc(s.bits[w] & ((1u << (cell & 31)) - 1u));
-            if (place >= pre.ranges[c].cnt) continue;      // (its prefix is unsound)
-            p[1] = pieces_of(pre, c, place, h);
-        }
-        float M = -INFINITY, l = 0.f;
+    };
+    float2 mine = lane < n ? ml(lane) : make_float2(-INFINITY, 0.f);
+    load(0);                                               // (under way while the weights are found)
+    M = mine.x;
+    for (int i = lane + W; i < n; i += W) M = fmaxf(M, ml(i).x);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-            for (int x = 0; x < p[b].n; ++x) M = fmaxf(M, p[b].at(x).x);
-        const float ref = M == -INFINITY ? 0.f : M;
+    for (int x = W / 2; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
+    const float ref = M == -INFINITY ? 0.f : M;
+    l = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-            for (int x = 0; x < p[b].n; ++x) {
-                const float2 v = p[b].at(x);
-                l = fmaf(exp2f(v.x - ref), v.y, l);
-            }
-        const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
-        for (int col = 4 * lane; col < own.d; col += 4 * L) {
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = 0; c < CB; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    static_assert(W % (S * F) == 0, "whole batches");
+    for (int i0 = 0; i0 < most; i0 += W) {
+        if (i0 > 0) mine = i0 + lane < n ? ml(i0 + lane) : make_float2(-INFINITY, 0.f);
+        const float w = exp2f(mine.x - ref);
+        l = fmaf(w, mine.y, l);
+        for (int k0 = 0; k0 < W && i0 + k0 < most; k0 += S * F) {      // (uniform: the shuffles name all lanes)
+            if (i0 + k0 > 0) load(i0 + k0);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll 4
-                for (int x = 0; x < p[b].n; ++x) {
-                    const float wt = exp2f(p[b].at(x).x - ref);
-                    const float4 o = __ldg(reinterpret_cast<const float4 *>(p[b].o + p[b].slot(x) * p[b].step * own.d + col));
-                    acc.x = fmaf(wt, o.x, acc.x);
-                    acc.y = fmaf(wt, o.y, acc.y);
-                    acc.z = fmaf(wt, o.z, acc.z);
-                    acc.w = fmaf(wt, o.w, acc.w);
+            for (int f = 0; f < F; ++f) {
+                const int k = k0 + S * f + sub;
+                float wt = __shfl_sync(0xffffffffu, w, k, W);
+                if (i0 + k >= n) wt = 0.f;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    acc[c].x = fmaf(wt, o[f][c].x, acc[c].x);
+                    acc[c].y = fmaf(wt, o[f][c].y, acc[c].y);
+                    acc[c].z = fmaf(wt, o[f][c].z, acc[c].z);
+                    acc[c].w = fmaf(wt, o[f][c].w, acc[c].w);
                 }
-            const float o4[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-            store_out4<T>(own, u, cell, h * own.d + col, o4);
+            }
         }
+    }
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if constexpr (S > 1) {
+#pragma unroll
+        for (int o = 16; o >= L; o >>= 1)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                acc[c].x += __shfl_xor_sync(0xffffffffu, acc[c].x, o);
+                acc[c].y += __shfl_xor_sync(0xffffffffu, acc[c].y, o);
+                acc[c].z += __shfl_xor_sync(0xffffffffu, acc[c].z, o);
+                acc[c].w += __shfl_xor_sync(0xffffffffu, acc[c].w, o);
+            }
     }
 }
 
-template <typename T>
-void launch_merge(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareArgs &s, cudaStream_t st)
+constexpr int MERGE_THREADS = 256;
+
+// The pieces of the classes' rows become one each, in the first's slot, where there are many: a long
+// prefix is read in a score of pieces, by every unit of the class (eight hypotheses of 750 queries
+// behind 300 000 keys: 19 pieces, the merges 40 us without this, 26 with it).  A warp takes a row of a head.
+template <int L, int CB>
+__global__ void __launch_bounds__(MERGE_THREADS) k_merge_prefix(const __grid_constant__ ReadoutArgs pre)
 {
-    using Kern = void (*)(ReadoutArgs, ReadoutArgs, ShareArgs);
-    const int L = own.d >= 128 ? 32 : own.d / 4;
-    const Kern kern = L == 32 ? k_merge_two<T, 32> : L == 16 ? k_merge_two<T, 16> : L == 8 ? k_merge_two<T, 8> : k_merge_two<T, 4>;
-    int64_t ctas = ((int64_t)own.U * own.k_max * own.H * L + 255) / 256;
-    if (ctas > 16ll * rs3_sm_count()) ctas = 16ll * rs3_sm_count();
-    if (ctas < 1) ctas = 1;
-    launch_pdl(kern, dim3((unsigned)ctas), dim3(256), 0, st, own, pre, s);
+    pdl_wait();
+    const int lane = threadIdx.x & 31, BM = pre.header->bm;
+    const int64_t rows = (int64_t)pre.header->n_groups * BM;
+    for (int64_t i = (int64_t)blockIdx.x * (MERGE_THREADS / 32) + (threadIdx.x >> 5); i < rows; i += (int64_t)gridDim.x * (MERGE_THREADS / 32)) {
+        const GroupParts g = load_parts(pre.parts + i / BM);
+        const int r = (int)(i % BM);
+        if (g.n <= PREFIX_PIECES || g.qt * BM + r >= g.cnt) continue;
+        const Pieces p = pieces_of(pre, g, r, BM, false);
+        Pieces none = p;
+        none.n = 0;
+        float4 acc[CB];
+        float M, l;
+        merge_row<L, CB, true>(p, none, pre.d, acc, M, l);
+        __syncwarp();                                      // the pieces are read before the first's place is written
+        const int64_t row = p.slot0 * p.step;
+        if (lane < L)
+#pragma unroll
+            for (int k = 0; k < CB; ++k)
+                __stcg(reinterpret_cast<float4 *>(const_cast<float *>(p.o) + row * pre.d + 4 * lane + 128 * k), acc[k]);
+        if (lane == 0) __stcg(const_cast<float2 *>(p.ml) + row, make_float2(M, l));
+    }
+}
+
+// A row's pieces over its unit's bank and its one over the prefix, and the scatter.
+template <typename T, int L, int CB>
+__global__ void __launch_bounds__(MERGE_THREADS) k_merge_two(const __grid_constant__ ReadoutArgs own, const __grid_constant__ ReadoutArgs pre,
+                                                             const __grid_constant__ ShareArgs s)
+{
+    pdl_wait();
+    const int lane = threadIdx.x % L, BM = own.header->bm, BMP = pre.header->bm;
+    const int64_t rows = (int64_t)own.header->n_groups * BM;
+    constexpr int PER = MERGE_THREADS / L;                 // rows of a CTA
+    for (int64_t i0 = (int64_t)blockIdx.x * PER; i0 < rows; i0 += (int64_t)gridDim.x * PER) {
+        const int64_t i = i0 + threadIdx.x / L;            // (BM is a multiple of the rows of a warp: all of one group)
+        const GroupParts g = load_parts(own.parts + min(i, rows - 1) / BM);
+        const int r = (int)(i % BM), j = g.qt * BM + r;
+        bool here = i < rows && j < g.cnt;
+        Pieces p = pieces_of(own, g, r, BM, false), q = p;
+        q.n = 0;
+        int cell = 0;
+        if (here) {
+            cell = __ldg(s.idx + (int64_t)g.u * own.k_max + j);
+            if (cell < 0 || cell >= own.mn) {
+                if (lane == 0) latch_status(own.status, RS3_EINVAL);
+                here = false;
+            }
+        }
+        const int c = s.leader[g.u];
+        if (here && c >= 0) {
+            const int64_t w = (int64_t)c * s.words + (cell >> 5);
+            const int place = s.before[w] + __popc(s.bits[w] & ((1u << (cell & 31)) - 1u));
+            const RangeSet *rs = pre.ranges + c;
+            here = place < rs->cnt;                        // (else its prefix is unsound)
+            if (here) q = pieces_of(pre, load_parts(pre.parts + rs->first_group + place / BMP * pre.H + g.h), place % BMP, BMP, true);
+        }
+        if (!here) p.n = q.n = 0;
+        float4 acc[CB];
+        float M, l;
+        merge_row<L, CB, false>(p, q, own.d, acc, M, l);
+        const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+        if (here)
+#pragma unroll
+            for (int k = 0; k < CB; ++k) {
+                const float o4[4] = {acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv};
+                store_out4<T>(own, g.u, cell, g.h * own.d + 4 * lane + 128 * k, o4);
+            }
+    }
+}
+
+template <int L, int CB>
+void launch_merges(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
+{
+    const int64_t rows = (int64_t)own.U * (own.k_max > 0 ? own.k_max : 1) * own.H, per = MERGE_THREADS / (prefix ? 32 : L);
+    const unsigned ctas = (unsigned)std::min<int64_t>((rows + per - 1) / per, 8ll * rs3_sm_count());
+    if (prefix) launch_pdl(k_merge_prefix<L, CB>, dim3(ctas), dim3(MERGE_THREADS), 0, st, pre);
+    else if (dtype == RS3_BF16) launch_pdl(k_merge_two<uint16_t, L, CB>, dim3(ctas), dim3(MERGE_THREADS), 0, st, own, pre, s);
+    else launch_pdl(k_merge_two<float, L, CB>, dim3(ctas), dim3(MERGE_THREADS), 0, st, own, pre, s);
+}
+
+rs3_status launch_merge(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
+{
+    switch (own.d) {
+    case 16: launch_merges<4, 1>(own, pre, s, dtype, st, prefix); break;
+    case 32: launch_merges<8, 1>(own, pre, s, dtype, st, prefix); break;
+    case 64: launch_merges<16, 1>(own, pre, s, dtype, st, prefix); break;
+    case 128: launch_merges<32, 1>(own, pre, s, dtype, st, prefix); break;
+    default: launch_merges<32, 2>(own, pre, s, dtype, st, prefix); break;
+    }
+    return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }
 
 // Byte offsets in the workspace.
@@ -309,8 +420,7 @@ extern "C" rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, 
     if (cudaGetLastError() != cudaSuccess) return RS3_ECUDA;
     if ((s = rs3_readout_plan_two(pre, own, dtype, st)) != RS3_OK) return s;
     if ((s = rs3_readout_run_launch(pre, L.pre, dtype, st)) != RS3_OK) return s;
+    if ((s = launch_merge(own, pre, sh, dtype, st, true)) != RS3_OK) return s;
     if ((s = rs3_readout_run_launch(own, L.own, dtype, st)) != RS3_OK) return s;
-    if (dtype == RS3_BF16) launch_merge<uint16_t>(own, pre, sh, st);
-    else launch_merge<float>(own, pre, sh, st);
-    return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+    return launch_merge(own, pre, sh, dtype, st, false);
 }
