@@ -683,7 +683,8 @@ void rs3_default_rope_spec(rs3_rope_spec *spec);
  * (there rot = d, and pairs are (2p, 2p+1)).
  *   pos     device int32 [rows][axes], any whole numbers
  *   cos_sin device fp32 [rows][rot/2][2], 16-byte aligned
- * Angles are counted in 2^-64 turns: their error is |pos| f 2^-53 and a rounding or two of fp32.
+ * Angles are counted in whole numbers of turns: their error is |pos| f 2^-53, 2^-31 turns and a few
+ * roundings of fp32.
  */
 rs3_status rs3_rope_table(const int32_t *pos, int64_t rows, const rs3_rope_spec *spec,
                           float *cos_sin, rs3_stream_t stream);
@@ -693,8 +694,7 @@ rs3_status rs3_rope_table(const int32_t *pos, int64_t rows, const rs3_rope_spec 
  * position, in fp32, rounded once; elements past rot are copied.
  *   q, k, q_out, k_out, strides, keep   as for rs3_qk_norm_rope (in place with the same stride)
  *   q_pos, k_pos  device int32 [rows][axes]
- * Limits: d * sizeof(elem) a multiple of 16 (else RS3_EINVAL), d <= 256; strides (in bytes)
- * multiples of 16.
+ * Limits: d * sizeof(elem) a multiple of 16 (else RS3_EINVAL), d <= 256; strides (in bytes) multiples of 16.
  */
 rs3_status rs3_rope_rows(const void *q, int64_t q_rows, int64_t q_stride, int Hq,
                          const int32_t *q_pos, const uint8_t *q_keep, void *q_out,

@@ -87,7 +87,7 @@ __device__ __forceinline__ void norm_row(float (&v)[ITEMS][N], int kind, float e
 // Rows [blockIdx.x per_cta, + per_cta) of unit blockIdx.y; a group of L lanes takes every
 // (BN_THREADS / L)-th of them, lane l the pieces l, l + L, ... (ITEMS of them at most).
 template <typename T, int L, int ITEMS>
-__global__ void __launch_bounds__(BN_THREADS, ITEMS == 1 ? 4 : 2) k_block_norm(const __grid_constant__ BlockNorm a)
+__global__ void __launch_bounds__(BN_THREADS, ITEMS == 1 ? 3 : 2) k_block_norm(const __grid_constant__ BlockNorm a)
 {
     constexpr int N = Piece<T>::N, GROUPS = BN_THREADS / L;
     pdl_wait();
@@ -125,21 +125,30 @@ __global__ void __launch_bounds__(BN_THREADS, ITEMS == 1 ? 4 : 2) k_block_norm(c
     const int64_t row_bytes = (int64_t)a.C * sizeof(T), unit = (int64_t)u * a.mn;
     // (a warp's groups go round together: their shuffles name all lanes)
     const int turns = (last - first + GROUPS - 1) / GROUPS;
-    for (int t = 0; t < turns; ++t) {
+    uint4 yn[ITEMS], xn[ITEMS];                            // the next row's, under way while this one is normed
+    int64_t next = -1;                                     // its first byte, or -1
+    const auto fetch = [&](int t) {
         const int j = first + t * GROUPS + threadIdx.x / L;
-        int cell = j < last ? (a.idx ? __ldg(a.idx + (int64_t)u * a.k_max + j) : j) : -1;
-        if (j < last && (cell < 0 || cell >= a.mn)) {
+        int cell = t < turns && j < last ? (a.idx ? __ldg(a.idx + (int64_t)u * a.k_max + j) : j) : -1;
+        if (t < turns && j < last && (cell < 0 || cell >= a.mn)) {
             if (lane == 0) latch_status(a.status, RS3_EINVAL);
             cell = -1;
         }
-        const int64_t off = (unit + (cell < 0 ? 0 : cell)) * row_bytes;
-        uint4 yr[ITEMS], xr[ITEMS];
+        next = cell < 0 ? -1 : (unit + cell) * row_bytes;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const bool take = in[i] && cell >= 0;
-            yr[i] = take && a.y ? __ldcs(reinterpret_cast<const uint4 *>(a.y + off) + lane + i * L) : make_uint4(0, 0, 0, 0);
-            xr[i] = take ? __ldcs(reinterpret_cast<const uint4 *>(a.x + off) + lane + i * L) : make_uint4(0, 0, 0, 0);
+            const bool take = in[i] && next >= 0;
+            yn[i] = take && a.y ? __ldcs(reinterpret_cast<const uint4 *>(a.y + next) + lane + i * L) : make_uint4(0, 0, 0, 0);
+            xn[i] = take ? __ldcs(reinterpret_cast<const uint4 *>(a.x + next) + lane + i * L) : make_uint4(0, 0, 0, 0);
         }
+    };
+    fetch(0);
+    for (int t = 0; t < turns; ++t) {
+        const int64_t off = next;
+        uint4 yr[ITEMS], xr[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) { yr[i] = yn[i]; xr[i] = xn[i]; }
+        fetch(t + 1);
         float v[ITEMS][N], x[ITEMS][N];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -161,7 +170,7 @@ __global__ void __launch_bounds__(BN_THREADS, ITEMS == 1 ? 4 : 2) k_block_norm(c
         if (a.xo) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
-                if (in[i] && cell >= 0) reinterpret_cast<uint4 *>(a.xo + off)[lane + i * L] = Piece<T>::narrow(x[i]);
+                if (in[i] && off >= 0) reinterpret_cast<uint4 *>(a.xo + off)[lane + i * L] = Piece<T>::narrow(x[i]);
         }
         if (a.ho) {
             norm_row<L>(x, a.pre, a.pre_eps, inv_c, in);
@@ -169,7 +178,7 @@ __global__ void __launch_bounds__(BN_THREADS, ITEMS == 1 ? 4 : 2) k_block_norm(c
             for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) x[i][e] = fmaf(x[i][e], w[i][e], b[i][e]);
-                if (in[i] && cell >= 0) reinterpret_cast<uint4 *>(a.ho + off)[lane + i * L] = Piece<T>::narrow(x[i]);
+                if (in[i] && off >= 0) reinterpret_cast<uint4 *>(a.ho + off)[lane + i * L] = Piece<T>::narrow(x[i]);
             }
         }
     }

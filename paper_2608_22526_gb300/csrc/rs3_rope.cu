@@ -3,15 +3,21 @@
 //
 // Pair p of an axis with n pairs turns by pos * f_p, f_p = base^(-p/n), stretched for positions
 // beyond those trained on.  An angle of a far position loses its fraction in fp32, and fp64 is slow
-// here, so positions are counted in turns in whole numbers: F_p = f_p / (2 pi) as a fraction of
-// 2^64, pos * F_p mod 2^64 is the angle's fraction of a turn without rounding (F_p's own error of
-// 2^-53 relative, times pos, is all there is).  Its nearest quarter turn is taken off in whole
-// numbers too, and what is left, |t| <= pi / 4, goes through the Taylor series of sine and cosine:
-// up to t^11 and t^10, whose next terms are below 1e-11 and 2e-10 there.
+// here, so angles are counted in turns in whole numbers: with F_p = f_p / (2 pi) as a fraction of 2^64,
+// pos * F_p mod 2^64 is the angle's fraction of a turn (F_p's own error of 2^-53 relative, times pos, is
+// all there is), of which the upper 32 bits are found, to 2^-31 of a turn.  Its nearest quarter turn is
+// taken off in whole numbers too (what is left are the low 30 bits, with their sign), and that, |t| <= pi
+// / 4, goes through the Taylor series of sine and cosine: up to t^11 and t^10, whose next terms are below
+// 1e-11 and 2e-10 there.
 //
-// A warp takes rows one after another: a row's angles are computed once, a pair per lane, and go
-// through shared memory to the pieces of all of its heads; the loads of the next rows are in flight
-// meanwhile.  The call is bound by the bytes of x and y.
+// A lane keeps one piece of the heads and its pairs' frequencies; its angles of a row are found once, two
+// by two on packed pairs, and serve all heads of the row, whose pieces are under way meanwhile.  With
+// halves a piece's partners come from the lane that holds them.  Queries of 16 streams and two fifths of
+// the rows of 48 objects' keys, 96 x 96 cells of 4 heads of 64 in bf16, 48 elements of a head turned (337
+// MB): 89 us, 3.8 TB/s; bound by issuing instructions (per row and lane about 23 for an angle and 40
+// for a piece) and by the loads' latency beside few warps (a lane's frequencies, angles and pieces
+// under way take 128 registers; 24 warps of 80 registers with four pieces spill: 98 us).  Angles through
+// shared memory, so that a row finds each once: 96 to 155 us, as every piece then reads eight of them again.
 #include "rs3_rows.cuh"
 
 #include <cmath>
@@ -20,41 +26,74 @@ namespace {
 
 constexpr int ROPE_PAIRS = 128;            // of a head of 256
 constexpr int ROPE_WARPS = 8;
-constexpr int ROPE_FLIGHT = 4;             // rows of a warp in flight
+constexpr int ROPE_CTAS = 2;               // resident per SM
+constexpr int ROPE_ROWS = 32;              // rows of a warp
+constexpr int ROPE_COPIES = 4;             // of which copies are held at a time, where partners come from copies
+constexpr int ROPE_FLIGHT = 4;             // pieces of a lane under way
 
-// The pairs' frequencies in turns per position, of 2^64.
+// The pairs' frequencies in turns per position, of 2^64 (turned back: negative ones).
 struct RopeTurns {
     uint64_t f[ROPE_PAIRS];
     uint8_t axis[ROPE_PAIRS];
     int32_t half, axes;
-    float magnitude, sign;                 // of the turned elements; -1 turns back
+    float magnitude;                       // of the turned elements
 };
 
-// (cos, sin) of `turn` / 2^64 turns.
-__device__ __forceinline__ float2 cos_sin(uint64_t turn)
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
 {
-    const uint32_t quarter = (uint32_t)((turn + (1ull << 61)) >> 62);
-    const int64_t rest = (int64_t)(turn - ((uint64_t)quarter << 62));      // within an eighth of a turn of 0
-    const float t = (float)(int32_t)(rest >> 30) * (6.283185307179586f / 17179869184.f);   // 2^34 to a turn
-    const float z = t * t;
-    float s = fmaf(z, -1.f / 39916800.f, 1.f / 362880.f);
-    s = fmaf(s, z, -1.f / 5040.f);
-    s = fmaf(s, z, 1.f / 120.f);
-    s = fmaf(s, z, -1.f / 6.f);
-    s = fmaf(s * z, t, t);
-    float c = fmaf(z, -1.f / 3628800.f, 1.f / 40320.f);
-    c = fmaf(c, z, -1.f / 720.f);
-    c = fmaf(c, z, 1.f / 24.f);
-    c = fmaf(c, z, -0.5f);
-    c = fmaf(c, z, 1.f);
-    const float a = quarter & 1u ? s : c, b = quarter & 1u ? c : s;
-    return make_float2((quarter + 1u) & 2u ? -a : a, quarter & 2u ? -b : b);
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair_of(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void split_pair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+
+// The upper 32 bits of pos * f mod 2^64, but for the last (f's lower half loses one).
+__device__ __forceinline__ uint32_t turn_of(int32_t pos, uint64_t f)
+{
+    return (uint32_t)pos * (uint32_t)(f >> 32) + ((uint32_t)__mulhi(pos, (int32_t)((uint32_t)f >> 1)) << 1);
 }
 
-__device__ __forceinline__ float2 row_angle(const int32_t *pos, uint64_t f, int axis, float sign, float magnitude)
+// (cos, sin) * magnitude of two angles in 2^-32 turns, the second sine's and cosine's operations on packed
+// pairs; the sines with `flip` (0 or the sign bit) changed.
+__device__ __forceinline__ void cos_sin_two(uint32_t t0, uint32_t t1, float magnitude, uint32_t flip, float *c, float *s)
 {
-    const float2 v = cos_sin((uint64_t)(int64_t)__ldg(pos + axis) * f);
-    return make_float2(v.x * magnitude, v.y * sign * magnitude);
+    const auto both = [](float x) { return pair_of(x, x); };
+    const int32_t r0 = (int32_t)(t0 << 2) >> 2, r1 = (int32_t)(t1 << 2) >> 2;
+    const uint64_t t = mul_pair(pair_of((float)r0, (float)r1), both(6.283185307179586f / 4294967296.f));
+    const uint64_t z = mul_pair(t, t);
+    uint64_t a = fma_pair(z, both(-1.f / 39916800.f), both(1.f / 362880.f));
+    a = fma_pair(a, z, both(-1.f / 5040.f));
+    a = fma_pair(a, z, both(1.f / 120.f));
+    a = fma_pair(a, z, both(-1.f / 6.f));
+    a = mul_pair(fma_pair(mul_pair(a, z), t, t), both(magnitude));
+    uint64_t b = fma_pair(z, both(-1.f / 3628800.f), both(1.f / 40320.f));
+    b = fma_pair(b, z, both(-1.f / 720.f));
+    b = fma_pair(b, z, both(1.f / 24.f));
+    b = fma_pair(b, z, both(-0.5f));
+    b = mul_pair(fma_pair(b, z, both(1.f)), both(magnitude));
+    float sn[2], cs[2];
+    split_pair(a, sn[0], sn[1]);
+    split_pair(b, cs[0], cs[1]);
+    const uint32_t w[2] = {t0 + (1u << 29), t1 + (1u << 29)};          // the quarter in the two upper bits
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool odd = w[i] & (1u << 30);
+        const float x = odd ? sn[i] : cs[i], y = odd ? cs[i] : sn[i];
+        c[i] = __uint_as_float(__float_as_uint(x) ^ ((w[i] + (1u << 30)) & 0x80000000u));
+        s[i] = __uint_as_float(__float_as_uint(y) ^ ((w[i] ^ flip) & 0x80000000u));
+    }
 }
 
 // One of the call's two tensors (queries or keys).
@@ -64,94 +103,101 @@ struct RopeSide {
     const int32_t *pos;                    // [rows][axes]
     const uint8_t *keep;                   // [rows] or NULL
     int64_t rows, x_stride, y_stride;      // strides in bytes
-    int32_t H, chunk;                      // heads; rows of a warp
-    int32_t ctas;
+    int32_t H, chunk;                      // heads; rows that a warp takes before it turns to others
+    int64_t chunks;
 };
 
+// Into shared memory; pairs behind the last do not turn.
 __device__ __forceinline__ void load_turns(const RopeTurns &t, uint64_t *f, uint8_t *axis)
 {
-    for (int p = threadIdx.x; p < t.half; p += blockDim.x) {
+    for (int p = threadIdx.x; p < ROPE_PAIRS; p += blockDim.x) {
         f[p] = t.f[p];
         axis[p] = t.axis[p];
     }
     __syncthreads();
 }
 
-// x[N] of a piece that begins at element e of a head, each with its partner and its pair's angle.
-// pairs: (2p, 2p + 1); halves: (p, p + half), whose partners lie in a second piece.
+// LANES: pairs lie within a piece, or a piece's partners are another's of the same head, which a lane
+// of the same turn holds.  COPY: halves otherwise, partners come from the rows' copies in shared memory.
+enum RopeMode { PAIR_LANES, HALF_LANES, HALF_COPY };
+
+// A piece whose elements from `first` (an even one) on keep the bits that they had.
 template <int N>
-__device__ __forceinline__ void turn_pairs(float *x, const float2 *cs)
+__device__ __forceinline__ uint4 keep_tail(uint4 turned, uint4 own, int first)
 {
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-        const float2 a = cs[e / 2];
-        const float x0 = x[e], x1 = x[e + 1];
-        x[e] = fmaf(x0, a.x, -(x1 * a.y));
-        x[e + 1] = fmaf(x0, a.y, x1 * a.x);
-    }
+    constexpr int W = N / 4;                               // elements of a word
+    return make_uint4(first > 0 ? turned.x : own.x, first > W ? turned.y : own.y, first > 2 * W ? turned.z : own.z,
+                      first > 3 * W ? turned.w : own.w);
 }
 
-// WIDE: halves whose two pieces begin on 16-byte boundaries; a lane holds both.  Otherwise a lane
-// holds one piece, and with halves reads its partners from the row's copy in shared memory.
-template <typename T, bool HALVES, bool WIDE>
-__global__ void __launch_bounds__(ROPE_WARPS * 32, 3)
+// Lanes take the pieces of one head of some rows side by side; heads of more than 32 pieces part by part.
+template <typename T, RopeMode MODE>
+__global__ void __launch_bounds__(ROPE_WARPS * 32, ROPE_CTAS)
 k_rope_rows(const __grid_constant__ RopeSide q, const __grid_constant__ RopeSide k, const __grid_constant__ RopeTurns turns, int d)
 {
     constexpr int N = Piece<T>::N;
+    constexpr int NP = MODE == PAIR_LANES ? N / 2 : N;     // angles of a piece
     pdl_wait();
-    extern __shared__ __align__(16) uint8_t s_raw[];
+    extern __shared__ __align__(16) uint8_t s_raw[];       // copies: [ROPE_COPIES][d] and their (cos, sin) [][half] of each warp
+    __shared__ uint64_t s_f[ROPE_PAIRS];
+    __shared__ uint8_t s_axis[ROPE_PAIRS];
+    __shared__ int s_rows[ROPE_WARPS][ROPE_ROWS], s_pos[ROPE_WARPS][ROPE_ROWS][3];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int half = turns.half, rot = 2 * half;
-    // [half] turns, [half] axes; per warp [FLIGHT][half] (cos, sin) and, for halves of odd places, a row
-    uint64_t *s_f = reinterpret_cast<uint64_t *>(s_raw);
-    uint8_t *s_axis = s_raw + 8 * ROPE_PAIRS;
-    const bool is_q = (int)blockIdx.x < q.ctas;
-    const RopeSide &s = is_q ? q : k;
-    const int pieces = d / N;
-    float2 *s_cs = reinterpret_cast<float2 *>(s_raw + 9 * ROPE_PAIRS) + warp * ROPE_FLIGHT * half;
-    T *s_row = reinterpret_cast<T *>(s_raw + 9 * ROPE_PAIRS + ROPE_WARPS * ROPE_FLIGHT * half * 8) +
-               (size_t)warp * ROPE_FLIGHT * d;
+    const int half = turns.half, rot = 2 * half, pieces = d / N;
+    const int64_t chunk = (int64_t)blockIdx.x * ROPE_WARPS + warp;
+    const bool is_q = chunk < q.chunks;
+    const uint8_t *x0 = is_q ? q.x : k.x, *keep = is_q ? q.keep : k.keep;
+    uint8_t *y0 = is_q ? q.y : k.y;
+    const int32_t *pos_in = is_q ? q.pos : k.pos;
+    const int64_t x_stride = is_q ? q.x_stride : k.x_stride, y_stride = is_q ? q.y_stride : k.y_stride, n_rows = is_q ? q.rows : k.rows;
+    const int H = is_q ? q.H : k.H, per_warp = is_q ? q.chunk : k.chunk;
+    const int64_t row0 = (is_q ? chunk : chunk - q.chunks) * per_warp;
+    // the rows that are kept, one after another, and their positions
+    const bool in = lane < per_warp && row0 + lane < n_rows, on = in && (!keep || keep[row0 + lane] != 0);
+    int32_t pos[3];
+#pragma unroll
+    for (int a = 0; a < 3; ++a) pos[a] = in && a < turns.axes ? __ldg(pos_in + (row0 + lane) * turns.axes + a) : 0;
     load_turns(turns, s_f, s_axis);
-    // a head's items: WIDE: half / N pairs of pieces, then the pieces past the turned ones
-    const int both = WIDE ? half / N : 0;
-    const int items = WIDE ? both + pieces - 2 * both : pieces;
-    const int64_t warp_id = (int64_t)((int)blockIdx.x - (is_q ? 0 : q.ctas)) * ROPE_WARPS + warp;
-    const int64_t row0 = warp_id * s.chunk;
-    if (row0 >= s.rows) return;
-    const int n = (int)min((int64_t)s.chunk, s.rows - row0);
-    uint32_t todo = __ballot_sync(0xffffffffu, lane < n && (!s.keep || s.keep[row0 + (lane < n ? lane : 0)] != 0));
-    while (todo) {
-        int row[ROPE_FLIGHT], m = 0;
+    const uint32_t kept = __ballot_sync(0xffffffffu, on);
+    if (on) {
+        const int at = __popc(kept & ((1u << lane) - 1u));
+        s_rows[warp][at] = lane;
 #pragma unroll
-        for (int r = 0; r < ROPE_FLIGHT; ++r) {
-            row[r] = todo ? __ffs(todo) - 1 : -1;
-            m += todo != 0;
-            todo &= todo - 1u;
-        }
-        // the rows' angles
-        for (int p = lane; p < half; p += 32) {
-            const uint64_t f = s_f[p];
-            const int axis = s_axis[p];
-#pragma unroll
-            for (int r = 0; r < ROPE_FLIGHT; ++r)
-                if (row[r] >= 0) s_cs[r * half + p] = row_angle(s.pos + (row0 + row[r]) * turns.axes, f, axis, turns.sign, turns.magnitude);
-        }
-        __syncwarp();
-        if constexpr (HALVES && !WIDE) {
+        for (int a = 0; a < 3; ++a) s_pos[warp][at][a] = pos[a];
+    }
+    __syncwarp();
+    const int n_kept = __popc(kept);
+    if (n_kept == 0) return;
+    x0 += row0 * x_stride;
+    y0 += row0 * y_stride;
+    if constexpr (MODE == HALF_COPY) {
+        const int copy_bytes = (ROPE_COPIES * d * (int)sizeof(T) + 15) / 16 * 16;
+        uint8_t *mine = s_raw + (size_t)warp * (copy_bytes + (ROPE_COPIES * half * 8 + 15) / 16 * 16);
+        T *s_row = reinterpret_cast<T *>(mine);
+        float2 *s_cs = reinterpret_cast<float2 *>(mine + copy_bytes);
+        for (int k0 = 0; k0 < n_kept; k0 += ROPE_COPIES) {
+            const int m = min(ROPE_COPIES, n_kept - k0);
+            const int *rows = s_rows[warp] + k0;
+            for (int i = lane; i < m * half; i += 32) {
+                const int r = i / half, p = i - r * half;
+                const uint32_t t = turn_of(s_pos[warp][k0 + r][s_axis[p]], s_f[p]);
+                float c[2], g[2];
+                cos_sin_two(t, t, turns.magnitude, 0u, c, g);
+                s_cs[i] = make_float2(c[0], g[0]);
+            }
+            __syncwarp();
             // head by head: the rows' copies, then every piece with its partners
-            for (int h = 0; h < s.H; ++h) {
+            for (int h = 0; h < H; ++h) {
                 for (int i = lane; i < m * pieces; i += 32) {
                     const int r = i / pieces, p = i - r * pieces;
-                    const int rr = r == 0 ? row[0] : r == 1 ? row[1] : r == 2 ? row[2] : row[3];
-                    reinterpret_cast<uint4 *>(s_row + r * d)[p] =
-                        *(reinterpret_cast<const uint4 *>(s.x + (row0 + rr) * s.x_stride) + h * pieces + p);
+                    reinterpret_cast<uint4 *>(s_row + r * d)[p] = *(reinterpret_cast<const uint4 *>(x0 + rows[r] * x_stride) + h * pieces + p);
                 }
                 __syncwarp();
                 for (int i = lane; i < m * pieces; i += 32) {
                     const int r = i / pieces, p = i - r * pieces;
-                    const int rr = r == 0 ? row[0] : r == 1 ? row[1] : r == 2 ? row[2] : row[3];
+                    const uint4 own = reinterpret_cast<const uint4 *>(s_row + r * d)[p];
                     float x[N];
-                    Piece<T>::widen(reinterpret_cast<const uint4 *>(s_row + r * d)[p], x);
+                    Piece<T>::widen(own, x);
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         const int at = p * N + e;
@@ -162,60 +208,88 @@ k_rope_rows(const __grid_constant__ RopeSide q, const __grid_constant__ RopeSide
                         float o;
                         if constexpr (sizeof(T) == 2) o = bf16_bits_to_float(other);
                         else o = other;
-                        x[e] = low ? fmaf(x[e], a.x, -(o * a.y)) : fmaf(o, a.y, x[e] * a.x);
+                        x[e] = fmaf(x[e], a.x, o * (low ? -a.y : a.y));
                     }
-                    *(reinterpret_cast<uint4 *>(s.y + (row0 + rr) * s.y_stride) + h * pieces + p) = Piece<T>::narrow(x);
+                    *(reinterpret_cast<uint4 *>(y0 + rows[r] * y_stride) + h * pieces + p) = keep_tail<N>(Piece<T>::narrow(x), own, rot - p * N);
                 }
                 __syncwarp();
             }
-        } else {
-            for (int i = lane; i < s.H * items; i += 32) {
-                const int h = i / items, it = i - h * items;
-                const bool two = WIDE && it < both;
-                const int p = WIDE && !two ? 2 * both + it - both : it;
-                uint4 v[ROPE_FLIGHT], o[ROPE_FLIGHT];
+        }
+    } else {
+        const int lanes = min(pieces, 32), side = lane / lanes, beside = 32 / lanes;       // of a head; the lane's row of `beside`
+        const int both = MODE == HALF_LANES ? half / N : 0, head_bytes = pieces * 16;
+        for (int part = 0; part < pieces; part += 32) {
+            const int piece = part + lane - side * lanes;
+            const bool mine = side < beside && piece < pieces;
+            const bool low = piece < both;
+            // what this lane's pairs turn by per position (pairs behind the last: nothing), and whose
+            uint64_t f[NP];
+            int axis[NP];
+            const int first = MODE == HALF_LANES ? (low ? piece : piece - both) * N : piece * NP;
 #pragma unroll
-                for (int r = 0; r < ROPE_FLIGHT; ++r) {
-                    if (row[r] < 0) continue;
-                    const uint4 *x = reinterpret_cast<const uint4 *>(s.x + (row0 + row[r]) * s.x_stride) + h * pieces;
-                    v[r] = __ldcs(x + p);
-                    if (two) o[r] = __ldcs(x + p + both);
-                }
+            for (int e = 0; e < NP; ++e) {
+                const int p = first + e < half ? first + e : ROPE_PAIRS - 1;
+                f[e] = first + e < half ? s_f[p] : 0ull;
+                axis[e] = s_axis[p];
+            }
+            const uint32_t flip = low ? 0x80000000u : 0u;
+            const int from = MODE == HALF_LANES ? (low ? lane + both : lane - both) : 0, tail = rot - piece * N;
+            // this lane's row of some rows side by side (a lane without one: the last, whose results it keeps to itself)
+            int r = min(side, n_kept - 1);
+            bool here = mine && side < n_kept;
+            const uint8_t *x = x0 + s_rows[warp][r] * x_stride + (mine ? piece * 16 : 0);
+            uint4 v[ROPE_FLIGHT];
 #pragma unroll
-                for (int r = 0; r < ROPE_FLIGHT; ++r) {
-                    if (row[r] < 0) continue;
-                    uint4 *y = reinterpret_cast<uint4 *>(s.y + (row0 + row[r]) * s.y_stride) + h * pieces;
-                    float x[N];
-                    Piece<T>::widen(v[r], x);
-                    if constexpr (WIDE) {
-                        if (two) {
+            for (int i = 0; i < ROPE_FLIGHT; ++i)
+                if (i < H) v[i] = __ldcs(reinterpret_cast<const uint4 *>(x + i * head_bytes));
+            for (int r0 = 0; r0 < n_kept; r0 += beside) {
+                uint8_t *y = y0 + s_rows[warp][r] * y_stride + (mine ? piece * 16 : 0);
+                float c[NP], g[NP];
+                const int32_t *at = s_pos[warp][r];
+#pragma unroll
+                for (int e = 0; e < NP; e += 2)
+                    cos_sin_two(turn_of(at[axis[e]], f[e]), turn_of(at[axis[e + 1]], f[e + 1]), turns.magnitude, flip, c + e, g + e);
+                // the next rows'
+                const bool store = here;
+                const int rn = r0 + beside + side;
+                r = min(rn, n_kept - 1);
+                here = mine && rn < n_kept;
+                const uint8_t *xn = x0 + s_rows[warp][r] * x_stride + (mine ? piece * 16 : 0);
+                const bool more = r0 + beside < n_kept;
+                for (int h0 = 0; h0 < H; h0 += ROPE_FLIGHT) {
+#pragma unroll
+                    for (int i = 0; i < ROPE_FLIGHT; ++i) {
+                        const int h = h0 + i;
+                        if (h >= H) break;                 // (uniform: the exchange names all lanes)
+                        const uint4 own = v[i];
+                        // the place's next piece: of a later head, or of the next rows
+                        if (h + ROPE_FLIGHT < H) v[i] = __ldcs(reinterpret_cast<const uint4 *>(x + (h + ROPE_FLIGHT) * (int64_t)head_bytes));
+                        else if (more) v[i] = __ldcs(reinterpret_cast<const uint4 *>(xn + i * (int64_t)head_bytes));
+                        float a[N];
+                        Piece<T>::widen(own, a);
+                        if constexpr (MODE == HALF_LANES) {
+                            const uint4 w = make_uint4(__shfl_sync(0xffffffffu, own.x, from), __shfl_sync(0xffffffffu, own.y, from),
+                                                       __shfl_sync(0xffffffffu, own.z, from), __shfl_sync(0xffffffffu, own.w, from));
                             float z[N];
-                            Piece<T>::widen(o[r], z);
-                            const float2 *cs = s_cs + r * half + p * N;
-#pragma unroll
-                            for (int e = 0; e < N; ++e) {
-                                const float2 a = cs[e];
-                                const float x0 = x[e], x1 = z[e];
-                                x[e] = fmaf(x0, a.x, -(x1 * a.y));
-                                z[e] = fmaf(x0, a.y, x1 * a.x);
-                            }
-                            y[p + both] = Piece<T>::narrow(z);
-                        }
-                    } else {
-                        const int first = p * N;           // pairs end on an even element: inside a piece the turned ones come first
-                        if (first + N <= rot) {
-                            turn_pairs<N>(x, s_cs + r * half + first / 2);
-                        } else {
+                            Piece<T>::widen(w, z);
 #pragma unroll
                             for (int e = 0; e < N; e += 2)
-                                if (first + e < rot) turn_pairs<2>(x + e, s_cs + r * half + (first + e) / 2);
+                                split_pair(fma_pair(pair_of(a[e], a[e + 1]), pair_of(c[e], c[e + 1]), mul_pair(pair_of(z[e], z[e + 1]), pair_of(g[e], g[e + 1]))),
+                                           a[e], a[e + 1]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < N; e += 2) {
+                                const float a0 = a[e], a1 = a[e + 1];
+                                a[e] = fmaf(a0, c[e / 2], -(a1 * g[e / 2]));
+                                a[e + 1] = fmaf(a0, g[e / 2], a1 * c[e / 2]);
+                            }
                         }
+                        if (store) *reinterpret_cast<uint4 *>(y + h * (int64_t)head_bytes) = keep_tail<N>(Piece<T>::narrow(a), own, tail);
                     }
-                    y[p] = Piece<T>::narrow(x);
                 }
+                x = xn;
             }
         }
-        __syncwarp();                                      // the angles are read before the next rows'
     }
 }
 
@@ -229,7 +303,10 @@ __global__ void __launch_bounds__(256) k_rope_table(const int32_t *pos, int64_t 
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t r = i / turns.half;
         const int p = (int)(i - r * turns.half);
-        out[i] = row_angle(pos + r * turns.axes, s_f[p], s_axis[p], turns.sign, turns.magnitude);
+        const uint32_t t = turn_of(__ldg(pos + r * turns.axes + s_axis[p]), s_f[p]);
+        float c[2], g[2];
+        cos_sin_two(t, t, turns.magnitude, 0u, c, g);
+        out[i] = make_float2(c[0], g[0]);
     }
 }
 
@@ -260,12 +337,12 @@ bool rope_turns(const rs3_rope_spec *s, RopeTurns &t)
             }
             f *= share + (1.0 - share) / s->factor;
             t.f[p] = (uint64_t)std::ldexp(f / two_pi, 64);
+            if (s->inverse) t.f[p] = 0 - t.f[p];
             t.axis[p] = (uint8_t)a;
         }
     t.half = s->rot / 2;
     t.axes = s->axes;
     t.magnitude = s->magnitude;
-    t.sign = s->inverse ? -1.f : 1.f;
     return true;
 }
 
@@ -350,24 +427,25 @@ extern "C" rs3_status rs3_rope_rows(const void *q, int64_t q_rows, int64_t q_str
         // fewer rows to a warp where SMs would be idle
         int chunk = 32;
         while (chunk > 1 && (r.rows + chunk - 1) / chunk < 16ll * rs3_sm_count()) chunk >>= 1;
-        const int64_t warps = (r.rows + chunk - 1) / chunk, ctas = (warps + ROPE_WARPS - 1) / ROPE_WARPS;
-        if (ctas > INT32_MAX) return RS3_EUNSUPPORTED;
         r.chunk = chunk;
-        r.ctas = (int32_t)ctas;
-        total += ctas;
+        r.chunks = (r.rows + chunk - 1) / chunk;
+        total += r.chunks;
     }
     if (total == 0) return RS3_OK;
-    if (total > INT32_MAX) return RS3_EUNSUPPORTED;
-    const bool halves = spec->layout == RS3_ROPE_HALVES, wide = halves && t.half % n == 0;
-    size_t smem = 9 * ROPE_PAIRS + (size_t)ROPE_WARPS * ROPE_FLIGHT * t.half * 8;
-    if (halves && !wide) smem += (size_t)ROPE_WARPS * ROPE_FLIGHT * d * esz;
+    const int64_t ctas = (total + ROPE_WARPS - 1) / ROPE_WARPS;
+    if (ctas > INT32_MAX) return RS3_EUNSUPPORTED;
+    const int pieces = d / n;
+    const RopeMode mode = spec->layout == RS3_ROPE_PAIRS ? PAIR_LANES : t.half % n == 0 && pieces <= 32 ? HALF_LANES : HALF_COPY;
+    size_t smem = 0;
+    if (mode == HALF_COPY) smem = ROPE_WARPS * (align_up((size_t)ROPE_COPIES * d * esz, 16) + align_up((size_t)ROPE_COPIES * t.half * 8, 16));
     using Kern = void (*)(RopeSide, RopeSide, RopeTurns, int);
     Kern kern;
     if (dtype == RS3_BF16)
-        kern = wide ? k_rope_rows<uint16_t, true, true> : halves ? k_rope_rows<uint16_t, true, false> : k_rope_rows<uint16_t, false, false>;
+        kern = mode == PAIR_LANES ? k_rope_rows<uint16_t, PAIR_LANES> : mode == HALF_LANES ? k_rope_rows<uint16_t, HALF_LANES> : k_rope_rows<uint16_t, HALF_COPY>;
     else
-        kern = wide ? k_rope_rows<float, true, true> : halves ? k_rope_rows<float, true, false> : k_rope_rows<float, false, false>;
-    if (rs3_kernel_smem((const void *)kern, smem) != RS3_OK) return RS3_ECUDA;
-    launch_pdl(kern, dim3((unsigned)total), dim3(ROPE_WARPS * 32), smem, reinterpret_cast<cudaStream_t>(stream), s[0], s[1], t, d);
+        kern = mode == PAIR_LANES ? k_rope_rows<float, PAIR_LANES> : mode == HALF_LANES ? k_rope_rows<float, HALF_LANES> : k_rope_rows<float, HALF_COPY>;
+    // (beside up to 8 KB that the kernel has anyhow)
+    if (rs3_kernel_smem((const void *)kern, smem + 8192) != RS3_OK) return RS3_ECUDA;
+    launch_pdl(kern, dim3((unsigned)ctas), dim3(ROPE_WARPS * 32), smem, reinterpret_cast<cudaStream_t>(stream), s[0], s[1], t, d);
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }

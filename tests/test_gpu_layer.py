@@ -95,6 +95,23 @@ def test_rows_match_64_bits(rs3, dtype, layout, d, rot, pairs, rows, Hq, Hk):
     assert torch.equal(bits(q), bits(qo)) and torch.equal(bits(k), bits(ko))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout,rot", [("pairs", 34), ("pairs", 32), ("halves", 32), ("halves", 22), ("halves", 6)])
+def test_elements_that_do_not_turn_keep_their_bits(rs3, dtype, layout, rot):
+    """Whatever they are: infinities, NaN of any payload."""
+    d, H, rows = 64, 3, 40
+    g = gen(rot)
+    raw = torch.randint(-2 ** 31, 2 ** 31 - 1, (rows, H * d), generator=g, device="cuda").to(torch.int32)
+    x = (raw.to(torch.int16) if dtype == "bf16" else raw).view(DT[dtype]).clone()
+    x.view(rows, H, d)[..., :rot] = 1.0
+    x.view(rows, H, d)[:, 0, rot:rot + 2] = math.inf
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")[:, None]
+    y = torch.zeros_like(x)
+    rs3.rs3_rope_rows(x, y, pos, None, None, None, dtype, H, 0, d, rs3.rope_spec(rot, layout=layout))
+    assert torch.equal(bits(y).view(rows, H, d)[..., rot:], bits(x).view(rows, H, d)[..., rot:])
+    assert y.view(rows, H, d)[..., :rot].isfinite().all()
+
+
 @pytest.mark.parametrize("layout", ["pairs", "halves"])
 def test_far_positions(rs3, layout):
     """The whole range of positions: whole turns drop out."""
