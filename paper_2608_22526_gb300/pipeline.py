@@ -159,6 +159,63 @@ class Pipeline:
                                self.bank, self.block, self.block_sel, self.n_top, rope, residual, out, scale,
                                self.ws_sparse, self.status, self.stream)
 
+    # -- a memory-attention layer around the readout ----------------------------
+    def use_scores(self, cap: float = 0.0, frame_bias: Optional[torch.Tensor] = None,
+                   frame_keep: Optional[torch.Tensor] = None):
+        """How readout_scored() changes its scores: capped at `cap` (0: not), biased by frame_bias [H, F+2] or
+        [U, H, F+2], over the frames that frame_keep uint8 [U, F+2] leaves (ages of ring frames, F =
+        bank.max_frames of them, then conditioning frames, then pointers).  The tensors are read by every call."""
+        self.cap, self.frame_bias, self.frame_keep = cap, frame_bias, frame_keep
+        if not hasattr(self, "ws_scored"):
+            with torch.cuda.stream(self.stream):           # (made in the order of the calls that use it)
+                self.ws_scored = torch.empty(rs3.rs3_scored_readout_workspace_bytes(self.bank, self.k_max), dtype=torch.uint8,
+                                             device=self.device)
+
+    def readout_scored(self, q: torch.Tensor, residual: Optional[torch.Tensor], out: torch.Tensor,
+                       rope: Optional[torch.Tensor] = None, scale: float = 0.0):
+        """readout() with the scores of use_scores()."""
+        w = self.w
+        rs3.rs3_scored_readout(q, w.dtype, w.G, w.mn, w.H, w.d, self.unit_group, self.idx, self.count, self.k_max, self.bank,
+                               self.cap, self.frame_bias, self.frame_keep, rope, residual, out, scale, self.ws_scored,
+                               self.status, self.stream)
+
+    def share(self, prefix: "Pipeline", prefix_unit: torch.Tensor):
+        """readout_shared() reads unit prefix_unit[u] (int32 [U], -1: none) of `prefix`'s bank before each unit's own rows:
+        what fork() would copy, read in place."""
+        self.prefix, self.prefix_unit = prefix, prefix_unit
+        with torch.cuda.stream(self.stream):
+            self.ws_shared = torch.empty(rs3.rs3_shared_readout_workspace_bytes(self.bank, prefix.bank, self.k_max),
+                                         dtype=torch.uint8, device=self.device)
+
+    def readout_shared(self, q: torch.Tensor, residual: Optional[torch.Tensor], out: torch.Tensor,
+                       rope: Optional[torch.Tensor] = None, scale: float = 0.0):
+        """readout() over the rows of share()'s prefix and the own ones.  Where the prefix has another stream, the call
+        comes after what was issued there, and what is issued there next (a commit, say) comes after it."""
+        w = self.w
+        here, there = self._on(), self.prefix._on()
+        if there != here:
+            here.wait_stream(there)
+        rs3.rs3_shared_readout(q, w.dtype, w.G, w.mn, w.H, w.d, self.unit_group, self.idx, self.count, self.k_max, self.bank,
+                               self.prefix.bank, self.prefix_unit, rope, residual, out, scale, self.ws_shared, self.status,
+                               self.stream)
+        if there != here:
+            there.wait_stream(here)
+
+    def rotate(self, q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], q_pos: Optional[torch.Tensor],
+               k: Optional[torch.Tensor], k_out: Optional[torch.Tensor], k_pos: Optional[torch.Tensor],
+               spec: rs3.RopeSpec, k_keep: Optional[torch.Tensor] = None):
+        """The frame's query and key heads turned by their positions (int32 [rows, axes]): what readout() and commit()
+        then take without a table.  k_keep: the commit's mask."""
+        w = self.w
+        rs3.rs3_rope_rows(q, q_out, q_pos, k, k_out, k_pos, w.dtype, w.H, w.H, w.d, spec, k_keep=k_keep, stream=self.stream)
+
+    def norm_residual(self, y: Optional[torch.Tensor], x: torch.Tensor, x_out: Optional[torch.Tensor],
+                      h_out: Optional[torch.Tensor], **norms):
+        """x_out = alpha x + gate post(y), h_out = pre(x_out) at the kept cells of every unit (rs3_norm_residual)."""
+        # (idx has a column where nothing is ever kept; its counts are 0 then)
+        rs3.rs3_norm_residual(y, x, x_out, h_out, self.w.dtype, idx=self.idx, count=self.count, status=self.status,
+                              stream=self.stream, **norms)
+
     def _on(self):
         """The stream of this pipeline's calls."""
         return self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
