@@ -169,6 +169,15 @@ def _want(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int):
     if t.dtype != dtype or t.numel() < numel:
         raise ValueError(f"{name}: at least {numel} elements of {dtype} wanted, got {tuple(t.shape)} of {t.dtype}")
 
+
+def _arg(dev: int, name: str, t: Optional[torch.Tensor], dtype, numel: int) -> int:
+    """The pointer of a contiguous tensor of at least `numel` elements of this type on device `dev`, the current one."""
+    if t is None or t.dtype is not dtype or t.numel() < numel or t.get_device() != dev or not t.is_contiguous():
+        _want(dev, name, t, dtype, numel)
+        return _ptr(t)
+    return t.data_ptr()
+
+
 def _want_bank(dev: int, bank: "Bank"):
     """A bank whose storage is on device `dev`."""
     if bank.k_store.get_device() != dev:
@@ -451,22 +460,22 @@ def rs3_scored_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
     the frames that frame_keep uint8 [U, F+2] leaves; F = bank.max_frames: ages of ring frames, then conditioning
     frames, then pointers."""
     dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
-    F, stride = bank.max_frames, 0
+    F, stride, bias_ptr, keep_ptr = bank.max_frames, 0, None, None
     if frame_bias is not None:
         if tuple(frame_bias.shape) not in ((H, F + 2), (bank.U, H, F + 2)):
             raise ValueError(f"frame_bias: [{H}, {F + 2}] or [{bank.U}, {H}, {F + 2}] wanted, got {tuple(frame_bias.shape)}")
-        _want(dev, "frame_bias", frame_bias, torch.float32, 0)
+        bias_ptr = _arg(dev, "frame_bias", frame_bias, torch.float32, 0)
         stride = H * (F + 2) if frame_bias.dim() == 3 else 0
     if frame_keep is not None:
         if tuple(frame_keep.shape) != (bank.U, F + 2):
             raise ValueError(f"frame_keep: [{bank.U}, {F + 2}] wanted, got {tuple(frame_keep.shape)}")
-        _want(dev, "frame_keep", frame_keep, torch.uint8, 0)
+        keep_ptr = _arg(dev, "frame_keep", frame_keep, torch.uint8, 0)
     _want_workspace(dev, workspace)
     if residual is not None:
         _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
     _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
     rc = lib.rs3_scored_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
-                                ctypes.byref(bank.desc), float(cap), _ptr(frame_bias), stride, _ptr(frame_keep), _ptr(rope),
+                                ctypes.byref(bank.desc), float(cap), bias_ptr, stride, keep_ptr, _ptr(rope),
                                 _ptr(residual), _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status),
                                 _stream(stream))
     _check(rc, "rs3_scored_readout")
@@ -630,10 +639,8 @@ def rs3_rope_rows(q, q_out, q_pos, k, k_out, k_pos, dtype: str, Hq: int, Hk: int
         (rows, stride), (rows_out, out_stride) = _rows_of(name, x, H * d), _rows_of(name + "_out", y, H * d)
         if rows != rows_out:
             raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
-        _want(dev, name + "_pos", pos, torch.int32, rows * spec.axes)
-        if keep is not None:
-            _want(dev, name + "_keep", keep, torch.uint8, rows)
-        sides += [x.data_ptr(), rows, stride, H, _ptr(pos), _ptr(keep), y.data_ptr(), out_stride]
+        sides += [x.data_ptr(), rows, stride, H, _arg(dev, name + "_pos", pos, torch.int32, rows * spec.axes),
+                  None if keep is None else _arg(dev, name + "_keep", keep, torch.uint8, rows), y.data_ptr(), out_stride]
     rc = lib.rs3_rope_rows(*sides, DTYPES[dtype], d, ctypes.byref(spec), _stream(stream))
     _check(rc, "rs3_rope_rows")
 
@@ -648,10 +655,18 @@ def _vector(dev: int, name: str, t, U: int, C: int):
     """(pointer, elements between units) of a vector fp32 [C] or [U, C]; (None, 0) without one."""
     if t is None:
         return None, 0
-    if tuple(t.shape) not in ((C,), (U, C)):
-        raise ValueError(f"{name}: [{C}] or [{U}, {C}] wanted, got {tuple(t.shape)}")
-    _want(dev, name, t, torch.float32, C)
-    return _ptr(t), C if t.dim() == 2 else 0
+    shape = t.shape
+    if not (shape[-1:] == (C,) and (len(shape) == 1 or (len(shape) == 2 and shape[0] == U))):
+        raise ValueError(f"{name}: [{C}] or [{U}, {C}] wanted, got {tuple(shape)}")
+    return _arg(dev, name, t, torch.float32, C), C if len(shape) == 2 else 0
+
+
+def _norm(dev: int, name: str, kind: str, eps: float, weight, bias, U: int, C: int):
+    if kind == "none" and weight is None and bias is None:
+        return None
+    w, w_stride = _vector(dev, name + "_weight", weight, U, C)
+    b, b_stride = _vector(dev, name + "_bias", bias, U, C)
+    return ctypes.byref(Norm(NORM_KINDS[kind], eps, w, b, w_stride, b_stride))
 
 
 def rs3_norm_residual(y, x, x_out, h_out, dtype: str, idx=None, count=None, post: str = "none", post_weight=None,
@@ -663,28 +678,20 @@ def rs3_norm_residual(y, x, x_out, h_out, dtype: str, idx=None, count=None, post
     if x.dim() != 3:
         raise ValueError(f"x: [units, cells, channels] wanted, got {tuple(x.shape)}")
     U, mn, C = x.shape
-    for name, t in (("x", x), ("y", y), ("x_out", x_out), ("h_out", h_out)):
-        if t is not None or name == "x":
-            _want(dev, name, t, dt, U * mn * C)
-    k_max = 0
+    n = U * mn * C
+    grids = [None if t is None else _arg(dev, name, t, dt, n) for name, t in (("y", y), ("x", x), ("x_out", x_out), ("h_out", h_out))]
+    k_max, idx_ptr, count_ptr = 0, None, None
     if idx is not None or count is not None:
         if idx is None or idx.dim() != 2 or idx.shape[0] != U:
             raise ValueError("idx: one row per unit, with count")
         k_max = idx.shape[1]
-        _want(dev, "idx", idx, torch.int32, U * k_max)
-        _want(dev, "count", count, torch.int32, U)
+        idx_ptr, count_ptr = _arg(dev, "idx", idx, torch.int32, 0), _arg(dev, "count", count, torch.int32, U)
         _want(dev, "status", status, torch.int32, 1)
-    norms = []
-    for name, kind, w, b in (("post", post, post_weight, post_bias), ("pre", pre, pre_weight, pre_bias)):
-        n = Norm()
-        n.kind, n.eps = NORM_KINDS[kind], eps
-        n.weight, n.weight_stride = _vector(dev, name + "_weight", w, U, C)
-        n.bias, n.bias_stride = _vector(dev, name + "_bias", b, U, C)
-        norms.append(n)
     g, g_stride = _vector(dev, "gate", gate, U, C)
-    rc = lib.rs3_norm_residual(_ptr(y), _ptr(x), DTYPES[dtype], U, mn, C, _ptr(idx), _ptr(count), k_max, ctypes.byref(norms[0]),
-                               g, g_stride, float(alpha), ctypes.byref(norms[1]), _ptr(x_out), _ptr(h_out), _ptr(status),
-                               _stream(stream))
+    rc = lib.rs3_norm_residual(grids[0], grids[1], DTYPES[dtype], U, mn, C, idx_ptr, count_ptr, k_max,
+                               _norm(dev, "post", post, eps, post_weight, post_bias, U, C), g, g_stride, float(alpha),
+                               _norm(dev, "pre", pre, eps, pre_weight, pre_bias, U, C), grids[2], grids[3],
+                               _ptr(status), _stream(stream))
     _check(rc, "rs3_norm_residual")
 
 
