@@ -24,6 +24,7 @@
 #include <atomic>
 #include <cmath>
 #include <initializer_list>
+#include <type_traits>
 
 #include "rs3_readout_common.cuh"
 
@@ -35,11 +36,15 @@ namespace {
 // A unit's part of the plan: kept queries and the bank's row ranges, without tiles.
 // What is wrong with its inputs is latched by the calls with `latch`; a unit without a
 // valid grid or bank has no work.
-__device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
+template <class Args>
+__device__ RangeSet unit_ranges(const Args &a, int u, bool latch)
 {
+    constexpr bool more = std::is_same<Args, ReadoutMore>::value;
     // every load first (none depends on another but a unit's number in the bank), then the checks
-    const int bu = a.bank_unit ? a.bank_unit[u] : u;
-    const int64_t *mu = a.meta + (int64_t)max(bu, 0) * a.meta_stride_words;
+    int bu = u;
+    if constexpr (more)
+        if (a.bank_unit) bu = a.bank_unit[u];
+    const int64_t *mu = a.meta + (int64_t)(more ? max(bu, 0) : u) * a.meta_stride_words;
     int cnt = a.count[u];
     const int g = a.unit_group[u];
     const int64_t head = mu[BM_HEAD], tail = mu[BM_TAIL], cond = mu[BM_COND_LEN], ptr = mu[BM_PTRLEN];
@@ -50,13 +55,14 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
     rs.first_group = -1;
     if (cnt < 0 || cnt > a.k_max) {
         if (latch) latch_status(a.status, RS3_EINVAL);
-        cnt = cnt < 0 || a.strict ? 0 : a.k_max;
+        cnt = cnt < 0 ? 0 : a.k_max;
+        if constexpr (more) cnt = 0;
     }
     if (g < 0 || g >= a.G) {
         if (latch) latch_status(a.status, RS3_EINVAL);
         cnt = 0;
     }
-    if (bu < 0) return rs;                          // reads nothing (nor has queries)
+    if (more && bu < 0) return rs;                  // reads nothing (nor has queries)
     if (!(head >= 0 && tail >= head && tail - head <= a.ring_cap && cond >= 0 && cond <= a.pinned_cap && ptr >= 0 &&
           ptr <= a.n_ptr)) {
         if (latch) latch_status(a.status, RS3_EINTERNAL);
@@ -75,7 +81,7 @@ __device__ RangeSet unit_ranges(const ReadoutArgs &a, int u, bool latch)
     }
     rs.start[3] = a.pinned_cap + a.ring_cap;
     rs.len[3] = (int32_t)ptr;
-    if (a.bank_unit) {                              // rows count from unit u's storage
+    if constexpr (more) {                           // rows count from unit u's storage
 #pragma unroll
         for (int r = 0; r < 4; ++r) rs.start[r] += (int64_t)(bu - u) * a.rows_per_unit;
     }
@@ -196,7 +202,8 @@ __device__ __forceinline__ void locate(const PlanView &v, int64_t x, int &u, int
 
 // Writes slice b's items and its item range; returns its merge entry in c
 // (nsplit 0: none) and its partial pieces in n_part.
-__device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &n_part, CombineItem &c)
+template <class Args>
+__device__ void plan_slice(const Args &a, const PlanView &v, int b, int &n_part, CombineItem &c)
 {
     const int64_t lo = slice_start(v, b), hi = slice_start(v, b + 1);
     int64_t first = -1, last = -1;
@@ -232,11 +239,12 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
             w.tile_end = (int32_t)t1;
             w.slot = whole ? -1 : 2 * b + (first < 0 ? 0 : 1);
             w.pad = 0;
-            if (whole && a.parts) {
-                const int32_t g = v.gb[u] + gl;
-                w.slot = 2 * a.grid_ctas + g;
-                a.parts[g] = {w.slot, 0, 1, u, h, qt, v.cnt[u], 0};
-            }
+            if constexpr (std::is_same<Args, ReadoutMore>::value)
+                if (whole && a.parts) {
+                    const int32_t g = v.gb[u] + gl;
+                    w.slot = 2 * a.grid_ctas + g;
+                    a.parts[g] = {w.slot, 0, 1, u, h, qt, v.cnt[u], 0};
+                }
             a.items[idx] = w;
             if (first < 0) first = idx;
             last = idx;
@@ -251,10 +259,11 @@ __device__ void plan_slice(const ReadoutArgs &a, const PlanView &v, int b, int &
                 c.slot0 = w.slot;
                 c.nsplit = (int32_t)(e - b + 1);
                 c.pad[1] = v.cnt[u];
-                if (a.parts) {
-                    a.parts[v.gb[u] + gl] = {c.slot0, b, c.nsplit, u, h, qt, v.cnt[u], 0};
-                    c.nsplit = 0;                   // merged by the caller
-                }
+                if constexpr (std::is_same<Args, ReadoutMore>::value)
+                    if (a.parts) {
+                        a.parts[v.gb[u] + gl] = {c.slot0, b, c.nsplit, u, h, qt, v.cnt[u], 0};
+                        c.nsplit = 0;               // merged by the caller
+                    }
             }
         }
         x += len;
@@ -284,7 +293,8 @@ constexpr int PLAN_THREADS = 256;
 // the choice is within 9% of the better one, and right beyond that: one object's 3
 // to 7 tiles per head 15.6 us against 25.2 with pairs, 16 objects 260 against 165.
 // `mine` is this thread's unit of the first round.  Every thread of the CTA calls it.
-__device__ __forceinline__ bool two_tiles(const ReadoutArgs &a, const RangeSet &mine)
+template <class Args>
+__device__ __forceinline__ bool two_tiles(const Args &a, const RangeSet &mine)
 {
     __shared__ float s_sum[2][PLAN_THREADS / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -292,7 +302,8 @@ __device__ __forceinline__ bool two_tiles(const ReadoutArgs &a, const RangeSet &
     for (int u = threadIdx.x; u < a.U; u += PLAN_THREADS) {
         RangeSet rs = u < PLAN_THREADS ? mine : unit_ranges(a, u, false);
         cut_tiles(rs, 128, 128);
-        if (a.score.tile_n) rs.n_tiles = a.score.pair_tile_n[u];
+        if constexpr (std::is_same<Args, ReadoutMore>::value)
+            if (a.score.tile_n) rs.n_tiles = a.score.pair_tile_n[u];
         s1 += (float)rs.nq * (float)rs.n_tiles;
         s2 += (float)((rs.nq + 1) >> 1) * (float)rs.n_tiles;
     }
@@ -309,8 +320,10 @@ __device__ __forceinline__ bool two_tiles(const ReadoutArgs &a, const RangeSet &
 }
 
 // The plan, by one CTA.
-__device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
+template <class Args>
+__device__ __forceinline__ void plan_cta(const Args &a)
 {
+    constexpr bool more = std::is_same<Args, ReadoutMore>::value;
     ReadoutHeader *hdr = a.header;
     // [U+1] tb, [U] wg (int64); [U+1] gb, [U] nt (int32)
     extern __shared__ int64_t s_plan[];
@@ -335,7 +348,8 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         if (u < a.U) {
             RangeSet rs = u0 > 0 ? unit_ranges(a, u, true) : mine;
             cut_tiles(rs, cfg.BM, cfg.BN);
-            if (a.score.tile_n) rs.n_tiles = (pairs ? a.score.pair_tile_n : a.score.tile_n)[u];
+            if constexpr (more)
+                if (a.score.tile_n) rs.n_tiles = (pairs ? a.score.pair_tile_n : a.score.tile_n)[u];
             a.ranges[u] = rs;
             s_wg[u] = (int64_t)cfg.ov + rs.n_tiles;
             s_nt[u] = rs.n_tiles;
@@ -349,7 +363,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         if (u < a.U) {
             s_tb[u] = off + run;
             s_gb[u] = goff + grun;
-            if (a.parts) a.ranges[u].first_group = goff + grun;
+            if constexpr (more) a.ranges[u].first_group = goff + grun;
         }
         run += tot;
         grun += gtot;
@@ -371,12 +385,13 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
     // holds 126 MB; nothing derives it.
     // (Likewise one unit with queries where units share a bank's.)
     int alone = a.U == 1 ? 0 : -1;
-    if (a.bank_unit && a.U > 1) {
-        for (int u = threadIdx.x; u < a.U; u += blockDim.x)
-            if (s_gb[u + 1] - s_gb[u] == grun) s_alone = u + 1;
-        __syncthreads();
-        alone = s_alone - 1;
-    }
+    if constexpr (more)
+        if (a.bank_unit && a.U > 1) {
+            for (int u = threadIdx.x; u < a.U; u += blockDim.x)
+                if (s_gb[u + 1] - s_gb[u] == grun) s_alone = u + 1;
+            __syncthreads();
+            alone = s_alone - 1;
+        }
     if (alone >= 0 && a.tensor && grun > 0 && P > grun) {
         const int64_t idle = P % grun, bytes = (int64_t)s_nt[alone] * cfg.BN * a.D * 4;
         if (64 * idle <= P || (bytes > ((int64_t)48 << 20) && 8 * idle <= P)) P -= idle;
@@ -407,7 +422,7 @@ __device__ __forceinline__ void plan_cta(const ReadoutArgs &a)
         hdr->slices = v.P;
         hdr->n_part = s_np;
         hdr->bm = cfg.BM;
-        hdr->n_groups = grun;
+        if constexpr (more) hdr->n_groups = grun;
     }
 }
 
@@ -422,14 +437,15 @@ __device__ __forceinline__ void pass_through(const ReadoutArgs &a, int64_t nvec,
         out[i] = res ? __ldcs(res + i) : make_uint4(0, 0, 0, 0);
 }
 
-__global__ void __launch_bounds__(PLAN_THREADS) k_plan(ReadoutArgs a, int64_t nvec)
+template <class Args>
+__global__ void __launch_bounds__(PLAN_THREADS) k_plan(Args a, int64_t nvec)
 {
     pdl_wait();
     if (blockIdx.x > 0) pass_through(a, nvec, blockIdx.x - 1, gridDim.x - 1);
     else plan_cta(a);
 }
 
-__global__ void __launch_bounds__(PLAN_THREADS) k_plan_two(const __grid_constant__ ReadoutArgs a, const __grid_constant__ ReadoutArgs b,
+__global__ void __launch_bounds__(PLAN_THREADS) k_plan_two(const __grid_constant__ ReadoutMore a, const __grid_constant__ ReadoutMore b,
                                                            int64_t nvec)
 {
     pdl_wait();
@@ -458,7 +474,8 @@ __device__ __forceinline__ void store_out1(const uint16_t *res, uint16_t *out, i
     out[off] = float_to_bf16_bits((res ? bf16_bits_to_float(res[off]) : 0.f) + o);
 }
 
-template <typename T, int E>
+// With STRICT, rows of cells that are none are skipped.
+template <typename T, int E, bool STRICT>
 __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
 {
     pdl_wait();
@@ -528,7 +545,7 @@ __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
                 wq[q] = (q < c.nsplit && M != -INFINITY) ? exp2f(mq - M) : 0.f;
             }
             if (cell < 0 || cell >= a.mn) {
-                if (a.strict) continue;
+                if constexpr (STRICT) continue;
                 cell = 0;
             }
 #pragma unroll
@@ -558,7 +575,7 @@ __global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
         }
         int cell = a.idx[(int64_t)c.u * a.k_max + j];
         if (cell < 0 || cell >= a.mn) {
-            if (a.strict) continue;
+            if constexpr (STRICT) continue;
             cell = 0;
         }
         float M = -INFINITY;
@@ -788,11 +805,7 @@ void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout 
     a->combine = reinterpret_cast<CombineItem *>(ws + L.combine);
     a->part_o = reinterpret_cast<float *>(ws + L.part_o);
     a->part_ml = reinterpret_cast<float *>(ws + L.part_ml);
-    a->bank_unit = nullptr;
     a->bank_U = bank->U;
-    a->parts = nullptr;
-    a->strict = 0;
-    a->score = {};
 }
 
 rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
@@ -833,18 +846,19 @@ int64_t pass_pieces(const ReadoutArgs &a, rs3_dtype dtype, int64_t &blocks)
 size_t plan_bytes(int U) { return (size_t)(2 * U + 1) * 8 + (size_t)(3 * U + 1) * 4; }
 
 // pass-through of the unselected cells (out of place only) and the plan
-rs3_status launch_plan(const ReadoutArgs &a, cudaStream_t st, rs3_dtype dtype)
+template <class Args>
+rs3_status launch_plan(const Args &a, cudaStream_t st, rs3_dtype dtype)
 {
     int64_t blocks;
     const int64_t nvec = pass_pieces(a, dtype, blocks);
-    if (rs3_kernel_smem((const void *)k_plan, plan_bytes(a.U)) != RS3_OK) return RS3_EUNSUPPORTED;
-    launch_pdl(k_plan, dim3((unsigned)(1 + blocks)), dim3(PLAN_THREADS), plan_bytes(a.U), st, a, nvec);
+    if (rs3_kernel_smem((const void *)k_plan<Args>, plan_bytes(a.U)) != RS3_OK) return RS3_EUNSUPPORTED;
+    launch_pdl(k_plan<Args>, dim3((unsigned)(1 + blocks)), dim3(PLAN_THREADS), plan_bytes(a.U), st, a, nvec);
     return cudaGetLastError() != cudaSuccess ? RS3_ECUDA : RS3_OK;
 }
 
 }  // namespace
 
-rs3_status rs3_readout_plan_two(const ReadoutArgs &a, const ReadoutArgs &b, rs3_dtype dtype, cudaStream_t st)
+rs3_status rs3_readout_plan_two(const ReadoutMore &a, const ReadoutMore &b, rs3_dtype dtype, cudaStream_t st)
 {
     int64_t blocks;
     const int64_t nvec = pass_pieces(b, dtype, blocks);
@@ -857,10 +871,6 @@ rs3_status rs3_readout_plan_two(const ReadoutArgs &a, const ReadoutArgs &b, rs3_
 // the attention kernel over the plan in the workspace
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st)
 {
-    if (a.score.tile_n) {
-        if (p.either) return rs3_launch_scored_either(a, st);
-        return p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
-    }
     if (p.either) return rs3_launch_either_readout(a, st);
     if (p.kind == 1) return rs3_launch_tc_readout(a, st);
     return rs3_launch_simt_readout(a, dtype, st);
@@ -869,6 +879,7 @@ rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs
 namespace {
 
 // merge of the split-KV partials and their scatter
+template <bool STRICT>
 rs3_status launch_merge(const ReadoutArgs &a, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
 {
     // one warp per (partial row, 64-column chunk; 32 for d < 64)
@@ -879,16 +890,24 @@ rs3_status launch_merge(const ReadoutArgs &a, int64_t max_combine, rs3_dtype dty
     if (cblocks > ccap) cblocks = ccap;
     if (cblocks < 1) cblocks = 1;
     if (dtype == RS3_BF16) {
-        if (ce == 2) launch_pdl(k_combine<uint16_t, 2>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
-        else launch_pdl(k_combine<uint16_t, 1>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
+        if (ce == 2) launch_pdl(k_combine<uint16_t, 2, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
+        else launch_pdl(k_combine<uint16_t, 1, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
     } else {
-        if (ce == 2) launch_pdl(k_combine<float, 2>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
-        else launch_pdl(k_combine<float, 1>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
+        if (ce == 2) launch_pdl(k_combine<float, 2, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
+        else launch_pdl(k_combine<float, 1, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
     }
     return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
 }
 
 }  // namespace
+
+rs3_status rs3_scored_launch(const ReadoutMore &a, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
+{
+    rs3_status s = launch_plan(a, st, dtype);
+    if (s != RS3_OK) return s;
+    s = p.either ? rs3_launch_scored_either(a, st) : p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
+    return s != RS3_OK ? s : launch_merge<true>(a, max_combine, dtype, st);
+}
 
 rs3_status rs3_readout_launch(const ReadoutArgs &a, const ReadoutPath &p,
                               int64_t max_combine, rs3_dtype dtype, cudaStream_t st, int phases)
@@ -901,7 +920,7 @@ rs3_status rs3_readout_launch(const ReadoutArgs &a, const ReadoutPath &p,
         const rs3_status s = rs3_readout_run_launch(a, p, dtype, st);
         if (s != RS3_OK) return s;
     }
-    if (phases & RS3_PHASE_MERGE) return launch_merge(a, max_combine, dtype, st);
+    if (phases & RS3_PHASE_MERGE) return launch_merge<false>(a, max_combine, dtype, st);
     return RS3_OK;
 }
 

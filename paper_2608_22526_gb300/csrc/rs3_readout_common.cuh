@@ -69,12 +69,26 @@ struct ReadoutArgs {
     CombineItem *combine;
     float *part_o;          // [slot][BM][d]
     float *part_ml;         // [slot][BM] (m, l) pairs, m in the log2 domain
-    // calls whose units read units of a bank by number, and leave all results in partial slots
+    int bank_U;             // units of the bank
+};
+
+// The arguments of the calls whose plan or scores are not the plain readout's.
+struct ReadoutMore : ReadoutArgs {
+    // units that read units of a bank by number, and leave all results in partial slots
     const int32_t *bank_unit;   // [U] the bank's unit that unit u reads (-1: none); NULL: unit u
-    int bank_U;                 // units of the bank
     GroupParts *parts;          // [group] its pieces (groups numbered as the plan does); NULL: whole groups are written out
-    int strict;                 // counts and cells that are out of range are skipped, not taken for others
+    // changed scores (counts and cells that are out of range are skipped, not taken for others)
     ScoreArgs score;
+};
+
+// What a kernel takes for a kind of scores.
+template <class X>
+struct ReadoutOf {
+    using Args = ReadoutMore;
+};
+template <>
+struct ReadoutOf<PlainScores> {
+    using Args = ReadoutArgs;
 };
 
 struct ReadoutPath {
@@ -113,11 +127,13 @@ void rs3_readout_fill(ReadoutArgs *a, const ReadoutPath &p, const ReadoutLayout 
                       const rs3_bank *bank, const float *rope, const void *residual, void *out, float scale, int32_t *status);
 // The attention kernel over the plan in the workspace.
 rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs3_dtype dtype, cudaStream_t st);
-rs3_status rs3_launch_scored_either(const ReadoutArgs &a, cudaStream_t st);
-rs3_status rs3_launch_scored_tc(const ReadoutArgs &a, cudaStream_t st);
-rs3_status rs3_launch_scored_simt(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st);
+rs3_status rs3_launch_scored_either(const ReadoutMore &a, cudaStream_t st);
+rs3_status rs3_launch_scored_tc(const ReadoutMore &a, cudaStream_t st);
+rs3_status rs3_launch_scored_simt(const ReadoutMore &a, rs3_dtype dtype, cudaStream_t st);
+// A readout over changed scores.
+rs3_status rs3_scored_launch(const ReadoutMore &a, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype, cudaStream_t st);
 // Two plans in one launch, with the second's pass-through.
-rs3_status rs3_readout_plan_two(const ReadoutArgs &first, const ReadoutArgs &second, rs3_dtype dtype, cudaStream_t st);
+rs3_status rs3_readout_plan_two(const ReadoutMore &first, const ReadoutMore &second, rs3_dtype dtype, cudaStream_t st);
 // phases of a readout: the attention over the bank (pass-through, plan,
 // readout kernel) and the merge of split-KV partials
 enum { RS3_PHASE_PLAN = 1, RS3_PHASE_RUN = 4, RS3_PHASE_ATTEND = 1 | 4, RS3_PHASE_MERGE = 2 };

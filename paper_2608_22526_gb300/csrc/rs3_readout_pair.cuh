@@ -150,7 +150,7 @@ struct TileWalk {
 // Items [it_begin, it_end) of the plan, in a CTA that is set up for the one-tile
 // kernel (set_up_tc): its tensor memory serves, its barriers make room.
 template <int DH, class X = PlainScores>
-__device__ __forceinline__ void readout_pair(const ReadoutArgs &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
+__device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
                                              uint32_t tmem, int it_begin, int it_end)
 {
     using C = Cfg<DH, X>;
@@ -568,7 +568,7 @@ __device__ __forceinline__ void readout_pair(const ReadoutArgs &a, const CUtenso
 // The kernel that the plan chose, on the same threads.
 template <int DH, class X = PlainScores>
 __global__ void __launch_bounds__(NTHREADS, 1)
-k_readout_either(const ReadoutArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
+k_readout_either(const typename ReadoutOf<X>::Args a, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
 {
     static_assert(NTHREADS == tc::Cfg<DH>::NTHREADS, "one launch for both");
     // set up for the one-tile kernel, whose calls are the short ones
@@ -580,7 +580,7 @@ k_readout_either(const ReadoutArgs a, const __grid_constant__ CUtensorMap tmk, c
 }
 
 template <int DH, class X = PlainScores>
-rs3_status launch(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
 {
     constexpr int one = tc::Cfg<DH>::SMEM + BiasRing<X, tc::Cfg<DH>::BN, tc::Cfg<DH>::KSTK, 2>::BYTES, smem = Cfg<DH, X>::SMEM > one ? Cfg<DH, X>::SMEM : one;
     if (rs3_kernel_smem((const void *)k_readout_either<DH, X>, smem) != RS3_OK) return RS3_ECUDA;

@@ -135,7 +135,7 @@ struct Tiles {
 };
 
 template <typename T, int D, class X>
-__global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(ReadoutArgs a)
+__global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(typename ReadoutOf<X>::Args a)
 {
     using C = Cfg<D>;
     constexpr int TM = C::TM, RW = C::RW, BM = C::BM, LD = C::LD, PLD = C::PLD, KC = C::KC, KG = C::KG,
@@ -162,7 +162,8 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(ReadoutA
         const T *Vb = static_cast<const T *>(a.v_store) + (int64_t)w.u * a.rows_per_unit * a.D + w.h * D;
         __syncthreads();                                     // the previous item's last tile has been read
         const Tiles tiles(rs);
-        const int2 *tab = X::on ? a.score.tiles + (int64_t)w.u * a.score.tile_stride : nullptr;
+        const int2 *tab = nullptr;
+        if constexpr (X::on) tab = a.score.tiles + (int64_t)w.u * a.score.tile_stride;
         auto tile_row = [&](int t, int &nvalid) -> int64_t {
             if constexpr (X::on) {
                 const int2 e = __ldg(tab + t);
@@ -307,8 +308,10 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(ReadoutA
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        s[i][j] = (X::cap ? a.score.cap * tanhf(s[i][j] * a.score.cap_step) : s[i][j]) + add[j];
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (X::cap) s[i][j] = a.score.cap * tanhf(s[i][j] * a.score.cap_step);
+                        s[i][j] += add[j];
+                    }
             }
             if (nv < BN) {
 #pragma unroll
@@ -447,7 +450,7 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(ReadoutA
 }
 
 template <typename T, int D, class X>
-rs3_status launch(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
 {
     if (rs3_kernel_smem((const void *)k_readout_simt<T, D, X>, Cfg<D>::SMEM) != RS3_OK) return RS3_ECUDA;
     launch_pdl(k_readout_simt<T, D, X>, dim3((unsigned)a.grid_ctas), dim3(NW * 32), Cfg<D>::SMEM, st, a);

@@ -374,7 +374,7 @@ struct RowsAhead {
 #pragma unroll
         for (int i = 0; i < PER; ++i) b1[i] = __ldg(bias + f2[i]);
     }
-    __device__ __forceinline__ RowsAhead(const ReadoutArgs &a, const int2 *table, const WorkItem &w)
+    __device__ __forceinline__ RowsAhead(const ReadoutMore &a, const int2 *table, const WorkItem &w)
     {
         tiles = table + (int64_t)w.u * a.score.tile_stride;
         last = w.tile_end - 1;
@@ -420,7 +420,7 @@ struct RowsAhead {
 
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
 template <int DH, class X = PlainScores>
-__device__ __forceinline__ void readout_tc(const ReadoutArgs &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
+__device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
                                            uint32_t tmem, int it_begin, int it_end)
 {
     using C = Cfg<DH>;

@@ -5,7 +5,7 @@
 namespace {
 
 template <int DH>
-rs3_status launch_width(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch_width(const ReadoutMore &a, cudaStream_t st)
 {
     using namespace tc::pair;
     const bool cap = a.score.cap > 0.f, bias = a.score.bias != nullptr;
@@ -15,7 +15,7 @@ rs3_status launch_width(const ReadoutArgs &a, cudaStream_t st)
 
 }  // namespace
 
-rs3_status rs3_launch_scored_either(const ReadoutArgs &a, cudaStream_t st)
+rs3_status rs3_launch_scored_either(const ReadoutMore &a, cudaStream_t st)
 {
     switch (a.d) {
     case 64: return launch_width<64>(a, st);

@@ -281,10 +281,9 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     f.tables = L.tables;
     f.BN[0] = L.path.BN;
     f.BN[1] = 128;
-    ReadoutArgs a;
+    ReadoutMore a = {};
     rs3_readout_fill(&a, L.path, L.l, ws + L.ws, q, G, mn, H, d, unit_group, idx, count, k_max, bank->U, bank, rope, residual, out, scale,
                      status);
-    a.strict = 1;
     a.score.tile_n = f.tile_n;
     a.score.tiles = f.tiles;
     a.score.pair_tile_n = f.tile_n + (L.tables - 1) * (int64_t)bank->U;
@@ -313,5 +312,5 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     const int row_ctas = frame_bias ? std::min((F + COND_PIECES + 1 + 7) / 8, 32) : 0;
     launch_pdl(k_frames, dim3((unsigned)(L.tables + row_ctas), (unsigned)bank->U), dim3(FRAMES_THREADS), 0, st, f);
     if (cudaGetLastError() != cudaSuccess) return RS3_ECUDA;
-    return rs3_readout_launch(a, L.path, L.l.max_combine, dtype, st, RS3_PHASE_ATTEND | RS3_PHASE_MERGE);
+    return rs3_scored_launch(a, L.path, L.l.max_combine, dtype, st);
 }

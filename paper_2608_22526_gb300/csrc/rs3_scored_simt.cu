@@ -5,7 +5,7 @@
 namespace {
 
 template <typename T, int D>
-rs3_status launch_scored(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch_scored(const ReadoutMore &a, cudaStream_t st)
 {
     const bool cap = a.score.cap > 0.f, bias = a.score.bias != nullptr;
     if (cap) return bias ? launch<T, D, FrameScores<true, true>>(a, st) : launch<T, D, FrameScores<true, false>>(a, st);
@@ -14,7 +14,7 @@ rs3_status launch_scored(const ReadoutArgs &a, cudaStream_t st)
 
 }  // namespace
 
-rs3_status rs3_launch_scored_simt(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st)
+rs3_status rs3_launch_scored_simt(const ReadoutMore &a, rs3_dtype dtype, cudaStream_t st)
 {
     if (dtype == RS3_BF16) {                 // the other widths have a tensor-core tile
         switch (a.d) {

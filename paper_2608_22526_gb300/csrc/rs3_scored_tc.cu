@@ -8,7 +8,7 @@ namespace tc {
 
 template <int DH, class X>
 __global__ void __launch_bounds__(Cfg<DH>::NTHREADS, 1)
-k_readout_scored(const ReadoutArgs a, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
+k_readout_scored(const ReadoutMore a, const __grid_constant__ CUtensorMap tmk, const __grid_constant__ CUtensorMap tmv)
 {
     const uint32_t tmem = set_up_tc<DH>(tmk, tmv);
     pdl_wait();                      // the plan
@@ -16,7 +16,7 @@ k_readout_scored(const ReadoutArgs a, const __grid_constant__ CUtensorMap tmk, c
 }
 
 template <int DH, class X>
-rs3_status launch_scored(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch_scored(const ReadoutMore &a, cudaStream_t st)
 {
     constexpr int smem = Cfg<DH>::SMEM + BiasRing<X, Cfg<DH>::BN, Cfg<DH>::KSTK, 2>::BYTES;
     static_assert(smem <= 232448, "shared memory budget");
@@ -30,7 +30,7 @@ rs3_status launch_scored(const ReadoutArgs &a, cudaStream_t st)
 }
 
 template <int DH>
-rs3_status launch_width(const ReadoutArgs &a, cudaStream_t st)
+rs3_status launch_width(const ReadoutMore &a, cudaStream_t st)
 {
     const bool cap = a.score.cap > 0.f, bias = a.score.bias != nullptr;
     if (cap) return bias ? launch_scored<DH, FrameScores<true, true>>(a, st) : launch_scored<DH, FrameScores<true, false>>(a, st);
@@ -39,7 +39,7 @@ rs3_status launch_width(const ReadoutArgs &a, cudaStream_t st)
 
 }  // namespace tc
 
-rs3_status rs3_launch_scored_tc(const ReadoutArgs &a, cudaStream_t st)
+rs3_status rs3_launch_scored_tc(const ReadoutMore &a, cudaStream_t st)
 {
     switch (a.d) {
     case 64: return tc::launch_width<64>(a, st);

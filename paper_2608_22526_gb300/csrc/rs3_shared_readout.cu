@@ -140,7 +140,7 @@ __device__ __forceinline__ GroupParts load_parts(const GroupParts *g)
 constexpr int PREFIX_PIECES = 4;           // more pieces of a class's row than these are merged ahead
 
 // Of row r of a group; `merged`: many pieces have become one, in the first's slot.
-__device__ __forceinline__ Pieces pieces_of(const ReadoutArgs &a, const GroupParts &g, int r, int BM, bool merged)
+__device__ __forceinline__ Pieces pieces_of(const ReadoutMore &a, const GroupParts &g, int r, int BM, bool merged)
 {
     Pieces p;
     p.ml = reinterpret_cast<const float2 *>(a.part_ml) + r;
@@ -231,7 +231,7 @@ constexpr int MERGE_THREADS = 256;
 // prefix is read in a score of pieces, by every unit of the class (eight hypotheses of 750 queries
 // behind 300 000 keys: 19 pieces, the merges 40 us without this, 26 with it).  A warp takes a row of a head.
 template <int L, int CB>
-__global__ void __launch_bounds__(MERGE_THREADS) k_merge_prefix(const __grid_constant__ ReadoutArgs pre)
+__global__ void __launch_bounds__(MERGE_THREADS) k_merge_prefix(const __grid_constant__ ReadoutMore pre)
 {
     pdl_wait();
     const int lane = threadIdx.x & 31, BM = pre.header->bm;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_merge_prefix(const __grid_con
 
 // A row's pieces over its unit's bank and its one over the prefix, and the scatter.
 template <typename T, int L, int CB>
-__global__ void __launch_bounds__(MERGE_THREADS) k_merge_two(const __grid_constant__ ReadoutArgs own, const __grid_constant__ ReadoutArgs pre,
+__global__ void __launch_bounds__(MERGE_THREADS) k_merge_two(const __grid_constant__ ReadoutMore own, const __grid_constant__ ReadoutMore pre,
                                                              const __grid_constant__ ShareArgs s)
 {
     pdl_wait();
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) k_merge_two(const __grid_consta
 }
 
 template <int L, int CB>
-void launch_merges(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
+void launch_merges(const ReadoutMore &own, const ReadoutMore &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
 {
     const int64_t rows = (int64_t)own.U * (own.k_max > 0 ? own.k_max : 1) * own.H, per = MERGE_THREADS / (prefix ? 32 : L);
     const unsigned ctas = (unsigned)std::min<int64_t>((rows + per - 1) / per, 8ll * rs3_sm_count());
@@ -312,7 +312,7 @@ void launch_merges(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareAr
     else launch_pdl(k_merge_two<float, L, CB>, dim3(ctas), dim3(MERGE_THREADS), 0, st, own, pre, s);
 }
 
-rs3_status launch_merge(const ReadoutArgs &own, const ReadoutArgs &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
+rs3_status launch_merge(const ReadoutMore &own, const ReadoutMore &pre, const ShareArgs &s, rs3_dtype dtype, cudaStream_t st, bool prefix)
 {
     switch (own.d) {
     case 16: launch_merges<4, 1>(own, pre, s, dtype, st, prefix); break;
@@ -408,7 +408,7 @@ extern "C" rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, 
     sh.words = L.n_words;
     sh.class_stride = L.class_stride;
     sh.prefix_U = prefix->U;
-    ReadoutArgs own, pre;
+    ReadoutMore own = {}, pre = {};
     rs3_readout_fill(&own, L.own, L.own_l, ws + L.own_ws, q, G, mn, H, d, unit_group, idx, sh.own_count, k_max, U, bank, rope, residual,
                      out, scale, status);
     own.parts = reinterpret_cast<GroupParts *>(ws + L.own_ws + L.own_l.parts);
