@@ -19,6 +19,13 @@
  *                                                closed masks onto the grid
  *   front end (Sec. 3.1)   rs3_seed_from_masks -- seed box of Eq. 1 from
  *                                                pixel masks, down_s
+ * around the readout of a memory-attention layer (no counterpart in the paper),
+ *   rs3_scored_readout     -- the readout with capped scores, biases by a row's frame,
+ *                             and frames left out
+ *   rs3_shared_readout     -- the readout of units that share the rows they were forked from
+ *   rs3_rope_table, rs3_rope_rows
+ *                          -- rotary positions (Eq. 7) from coordinates
+ *   rs3_norm_residual      -- the norms before and behind a block, its gate and residual
  * and, for banks of hundreds of frames (no counterpart in the paper),
  *   rs3_qk_norm_rope       -- RMS norm of query and key heads, rotated (Eq. 7)
  *   rs3_bank_copy          -- units copied, forked and compacted
@@ -462,14 +469,16 @@ size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max);
  * frames as the prefix that is always seen.
  *   cap         0 (none) or in [2^-10, 2^10]
  *   frame_bias  device fp32 [H][F+2], or [U][H][F+2] bias_stride elements apart
- *               (bias_stride 0: one for all units), or NULL; finite, or minus infinity (the
- *               row weighs nothing)
+ *               (bias_stride 0: one for all units), or NULL.  Minus infinity and all below
+ *               -1e30 (a type's lowest value, say): the row weighs nothing
  *   frame_keep  device uint8 [U][F+2] or NULL.  Rows that are left out are not read as far as
  *               results go: their bits do not matter
- * A query with no row left, or whose scores are all minus infinity, reads A = 0; a
+ * A query with no row left, or whose rows all weigh nothing, reads A = 0; a changed
  * score that is NaN or plus infinity makes its query's head NaN.  Arguments and results
  * otherwise as rs3_memory_readout; idx holds distinct cells; a cell outside [0, mn) latches
  * RS3_EINVAL and is skipped, a count outside [0, k_max] latches it and the unit is skipped.
+ *   workspace   device, >= rs3_scored_readout_workspace_bytes(bank, k_max) bytes, 16-byte
+ *               aligned; one call at a time
  * In bf16 the softmax's weights are rounded to bf16, and so are queries rotated here.
  * Limits: those of rs3_memory_readout; U * rows_per_unit < 2^31.
  */
@@ -492,8 +501,8 @@ size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const rs3_bank *
  *   bank         the units' own rows (maybe none yet)
  *   prefix       a bank of the same H, d, dtype and mn; it may be `bank` itself
  *   prefix_unit  device int32 [U], in [-1, prefix->U); -1: no prefix
- * Arguments and results otherwise as rs3_memory_readout.  A cell outside [0, mn) latches
- * RS3_EINVAL and is skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit
+ * Arguments and results otherwise as rs3_memory_readout; idx holds distinct cells (twice
+ * the same one is fine out of place).  A cell outside [0, mn) latches RS3_EINVAL and is skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit
  * out of range latches it and the unit is skipped, and so is one whose counters or whose
  * prefix's are unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.
  *   workspace    device, >= rs3_shared_readout_workspace_bytes(...), 16-byte aligned; one call at a time

@@ -28,6 +28,9 @@ struct ScoreArgs {
     float cap_poly[4];          // cap * log2(e) * tanh(x) / raw score, by powers of the raw score's square
 };
 
+// A frame's bias in the log2 domain; one below any that a score could show beside counts as minus infinity.
+__device__ __forceinline__ float log2_bias(float b) { return b < -1e30f ? -INFINITY : b * 1.4426950408889634f; }
+
 // What a readout kernel does to a score: nothing, or a cap and a bias by the row's frame.
 struct PlainScores {
     static constexpr bool on = false, cap = false, bias = false;

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(typename
                 const float *bias = a.score.bias + w.u * a.score.bias_stride + (int64_t)w.h * a.score.frames;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (tk + 8 * j < nv) add[j] = __ldg(bias + __ldg(frame + tk + 8 * j)) * 1.4426950408889634f;
+                    if (tk + 8 * j < nv) add[j] = log2_bias(__ldg(bias + __ldg(frame + tk + 8 * j)));
             }
             cp_async_wait();
             __syncthreads();                                 // tile t is in; every warp has read tile t - 1

@@ -398,10 +398,10 @@ struct RowsAhead {
         float all = 0.f;
         bool same = true;
         if constexpr (X::bias) {
-            all = __shfl_sync(0xffffffffu, b1[0], 0) * 1.4426950408889634f;
+            all = log2_bias(__shfl_sync(0xffffffffu, b1[0], 0));
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const float v = b1[i] * 1.4426950408889634f;
+                const float v = log2_bias(b1[i]);
                 reinterpret_cast<float *>(slot + 16)[lane + 32 * i] = v;
                 same = same && v == all;
             }

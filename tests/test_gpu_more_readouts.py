@@ -1,5 +1,6 @@
 """Readouts over a shared prefix, and with capped and biased scores, against plain implementations in 64 bits."""
 import math
+import types
 
 import numpy as np
 import pytest
@@ -459,6 +460,50 @@ def test_scored_readout_of_scores_of_all_sizes(rs3, dtype, d):
     scored_case(rs3, b, [100, 40], [0, 0], 1, 0.0, late, None)
     late[:, 5] = 3000.0
     scored_case(rs3, b, [100, 40], [0, 0], 1, 3.0, late, None)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256), ("f32", 32)])
+@pytest.mark.parametrize("lowest", [-3.4028234663852886e38, -math.inf])
+def test_scored_readout_masked_by_the_lowest_value(rs3, dtype, d, lowest):
+    """Frames that a bias of the type's lowest value masks weigh nothing, and a query with no other reads 0."""
+    b = Built(rs3, U=2, H=2, d=d, dtype=dtype, m=8, n=9, window=4, commits=5, n_ptr=3, seed=2)
+    spoil(b, None)
+    bias = torch.zeros((2, 2, b.bank.max_frames + 2), device="cuda")
+    bias[0, 0], bias[1, 1, 1:] = lowest, lowest
+    same = torch.where(bias < -1e30, -math.inf, bias)
+    q = torch.randn((1, 72, 2 * d), generator=gen(1), device="cuda").to(DT[dtype])
+    idx, count = keep_sets(2, 72, 40, [40, 40])
+    group = torch.zeros(2, dtype=torch.int32, device="cuda")
+    outs = []
+    for t in (bias, same):
+        out = torch.zeros((2, 72, 2 * d), dtype=DT[dtype], device="cuda")
+        run_scored(rs3, b, q, 1, idx, count, group, 7.0, t, None, None, 0.0, None, out)
+        outs.append(out)
+    assert torch.equal(bits(outs[0]), bits(outs[1])) and not outs[0].isnan().any()
+    assert (outs[0][0, :, :d] == 0).all() and (outs[0][0, idx[0].long(), d:] != 0).any() and (outs[0][1, idx[1].long(), d:] != 0).any()
+    want, tol = reference(dtype, 2, d, q, idx, [40, 40], group, None, d ** -0.5, None, outs[0].shape, scored_rows(b, None), 7.0, lambda u, h: same[u, h])
+    assert ((outs[0].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,H,d", [("bf16", 4, 64), ("f32", 1, 128)])
+def test_readouts_of_rows_past_32_bit_offsets(rs3, dtype, H, d):
+    """A bank whose ring and pointers begin past 2^31 elements."""
+    D = H * d
+    n_cond = -(-(1 << 31) // (D * 16384)) + 3
+    b = types.SimpleNamespace(rs3=rs3, U=1, H=H, d=d, D=D, dtype=dtype, mn=16384, st=status())
+    b.bank = rs3.Bank(1, H, d, dtype, b.mn, n_cond, 2, 2 * b.mn, 2, 7)
+    b.places = lambda u, bank=None: Built.places(b, u, bank)
+    assert b.bank.pinned_cap * D > 1 << 31
+    g = gen(5)
+    for f in range(4):
+        k, v = (torch.randn((1, b.mn, D), generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+        mask = (torch.rand((1, b.mn), generator=g, device="cuda") < 0.02).to(torch.uint8)
+        rs3.rs3_bank_commit(b.bank, k, v, mask, int(f == 0), b.st)
+    rs3.rs3_bank_set_pointers(b.bank, *(torch.randn((1, 7, D), generator=g, device="cuda").to(DT[dtype]) for _ in range(2)), b.st)
+    bias = torch.randn((H, 4), generator=g, device="cuda")
+    keep = torch.tensor([[1, 1, 0, 1]], dtype=torch.uint8, device="cuda")
+    scored_case(rs3, b, [150], [0], 1, 9.0, bias, keep)
+    shared_case(rs3, b, b, [150], [0], [0], 1)
 
 
 @pytest.mark.parametrize("dtype,H,d", [("bf16", 2, 64), ("bf16", 1, 256), ("f32", 2, 64)])
