@@ -15,6 +15,8 @@
 //   k_readout_*   the readout's kernels over either plan, on the bank each reads
 //   k_merge_prefix  between the two, the classes' pieces: one for each row and head
 //   k_merge_two   log-sum-exp merge of a row's pieces over both banks, and the scatter
+// Eight hypotheses of some 750 queries behind 300 000 rows of 256, six frames of their own: 255 us, of
+// which the attention over the prefix 187 (what it would take for each hypothesis), over the own rows 33.
 #include "rs3_readout_common.cuh"
 
 #include <algorithm>
