@@ -476,7 +476,8 @@ size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max);
  * A query with no row left, or whose rows all weigh nothing, reads A = 0; a changed
  * score that is NaN or plus infinity makes its query's head NaN.  Arguments and results
  * otherwise as rs3_memory_readout; idx holds distinct cells; a cell outside [0, mn) latches
- * RS3_EINVAL and is skipped, a count outside [0, k_max] latches it and the unit is skipped.
+ * RS3_EINVAL and is skipped, a count outside [0, k_max] latches it and the unit is skipped, and so
+ * is a unit whose counters or frames are unsound (RS3_EINTERNAL).
  *   workspace   device, >= rs3_scored_readout_workspace_bytes(bank, k_max) bytes, 16-byte
  *               aligned; one call at a time
  * In bf16 the softmax's weights are rounded to bf16, and so are queries rotated here.

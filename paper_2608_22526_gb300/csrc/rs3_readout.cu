@@ -47,6 +47,9 @@ __device__ RangeSet unit_ranges(const Args &a, int u, bool latch)
     const int64_t *mu = a.meta + (int64_t)(more ? max(bu, 0) : u) * a.meta_stride_words;
     int cnt = a.count[u];
     const int g = a.unit_group[u];
+    int tiles = 0;
+    if constexpr (more)
+        if (a.score.tile_n) tiles = a.score.tile_n[u];
     const int64_t head = mu[BM_HEAD], tail = mu[BM_TAIL], cond = mu[BM_COND_LEN], ptr = mu[BM_PTRLEN];
     RangeSet rs;
     for (int r = 0; r < 4; ++r) { rs.start[r] = 0; rs.len[r] = 0; rs.tiles[r] = 0; }
@@ -61,6 +64,10 @@ __device__ RangeSet unit_ranges(const Args &a, int u, bool latch)
     if (g < 0 || g >= a.G) {
         if (latch) latch_status(a.status, RS3_EINVAL);
         cnt = 0;
+    }
+    if (tiles < 0) {                                // what the frames' table found unsound
+        if (latch) latch_status(a.status, RS3_EINTERNAL);
+        return rs;
     }
     if (more && bu < 0) return rs;                  // reads nothing (nor has queries)
     if (!(head >= 0 && tail >= head && tail - head <= a.ring_cap && cond >= 0 && cond <= a.pinned_cap && ptr >= 0 &&
@@ -303,7 +310,7 @@ __device__ __forceinline__ bool two_tiles(const Args &a, const RangeSet &mine)
         RangeSet rs = u < PLAN_THREADS ? mine : unit_ranges(a, u, false);
         cut_tiles(rs, 128, 128);
         if constexpr (std::is_same<Args, ReadoutMore>::value)
-            if (a.score.tile_n) rs.n_tiles = a.score.pair_tile_n[u];
+            if (a.score.tile_n) rs.n_tiles = max(a.score.pair_tile_n[u], 0);
         s1 += (float)rs.nq * (float)rs.n_tiles;
         s2 += (float)((rs.nq + 1) >> 1) * (float)rs.n_tiles;
     }
@@ -349,7 +356,7 @@ __device__ __forceinline__ void plan_cta(const Args &a)
             RangeSet rs = u0 > 0 ? unit_ranges(a, u, true) : mine;
             cut_tiles(rs, cfg.BM, cfg.BN);
             if constexpr (more)
-                if (a.score.tile_n) rs.n_tiles = (pairs ? a.score.pair_tile_n : a.score.tile_n)[u];
+                if (a.score.tile_n) rs.n_tiles = max((pairs ? a.score.pair_tile_n : a.score.tile_n)[u], 0);
             a.ranges[u] = rs;
             s_wg[u] = (int64_t)cfg.ov + rs.n_tiles;
             s_nt[u] = rs.n_tiles;

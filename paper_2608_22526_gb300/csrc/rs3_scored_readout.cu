@@ -27,7 +27,7 @@ struct Stretch { int64_t x, y; };
 struct FramesArgs {
     BankDev bank;
     const uint8_t *keep;        // [U][F + 2] or NULL
-    int32_t *tile_n;            // [tables][U]
+    int32_t *tile_n;            // [tables][U]; -1: counters or frames that are unsound
     Stretch *stretch;           // [tables][U][F] first and end ring position of frames that are read and follow one another
     int4 *runs;                 // [tables][U][F + 4] storage rows of those and of the other regions: (first row, rows, first tile)
     int2 *tiles;                // [tables][U][tile_stride]
@@ -88,6 +88,14 @@ struct UnitFrames {
         oldest = (int)first;
         return true;
     }
+    // The frames in their order fill [head, tail) without gap or overlap: of the i-th oldest, it begins where
+    // the one before it ends (the first at the head), and the last ends at the tail.
+    __device__ __forceinline__ bool follows(int i) const
+    {
+        const int s = oldest + i < F ? oldest + i : oldest + i - F, before = s > 0 ? s - 1 : F - 1;
+        const int64_t a = off[s], l = len[s], from = i == 0 ? head : off[before] + len[before];
+        return a == from && a >= head && a <= tail && l >= 0 && l <= tail - a && (i + 1 < n || l == tail - a);
+    }
     // of the i-th oldest frame
     __device__ __forceinline__ bool read(int i) const { return !keep || keep[n - 1 - i] != 0; }
     __device__ __forceinline__ void span(int i, int64_t &a, int64_t &e) const
@@ -106,17 +114,18 @@ __device__ void unit_tiles(const FramesArgs &f, int u, int table)
     const int BN = f.BN[table];
     const int64_t slot = (int64_t)table * f.U + u;
     UnitFrames x;
-    const bool sound = x.load(b, f.keep, u);
-    if (!sound) {                                          // (the plan latches it)
-        if (threadIdx.x == 0) f.tile_n[slot] = 0;
+    if (!x.load(b, f.keep, u)) {                           // (the plan latches it)
+        if (threadIdx.x == 0) f.tile_n[slot] = -1;
         return;
     }
     Stretch *stretch = f.stretch + slot * x.F;
     int4 *runs = f.runs + slot * (x.F + 4);
     // stretches of frames that are read: the first frame of one writes where it begins, the last where it ends
     int n_str = 0;
+    bool gap = x.n == 0 && x.head != x.tail;
     for (int i0 = 0; i0 < x.n; i0 += FRAMES_THREADS) {
         const int i = i0 + threadIdx.x;
+        gap = gap || (i < x.n && !x.follows(i));
         const bool on = i < x.n && x.read(i), begins = on && (i == 0 || !x.read(i - 1)), ends = on && (i == x.n - 1 || !x.read(i + 1));
         int before = begins, none = 0, all, zero;
         scan_two(before, none, all, zero);
@@ -129,7 +138,11 @@ __device__ void unit_tiles(const FramesArgs &f, int u, int table)
         }
         n_str += all;
     }
-    __syncthreads();
+    // (the tables hold frames that fill the ring's rows, no more, and rows between frames have no bias)
+    if (__syncthreads_or(gap)) {
+        if (threadIdx.x == 0) f.tile_n[slot] = -1;
+        return;
+    }
     // runs of storage rows: the pinned ones, the stretches (cut at the ring's end), the pointers
     int n_runs = 0, n_tiles = 0;
     const int sh = 31 - __clz(BN);

@@ -576,6 +576,38 @@ def test_scored_readout_latches_what_the_device_finds(rs3):
         assert code == rs3.RS3_EINTERNAL and skipped == [False, False, False, True]
 
 
+def test_scored_readout_skips_units_whose_frames_do_not_fill_the_ring(rs3):
+    """Frames that overlap, leave rows between them, or are more than the table holds: the unit is skipped, nothing past its
+    tables is written."""
+    for dtype, H, d, bias in (("bf16", 1, 64, "age"), ("bf16", 1, 256, "unit"), ("f32", 1, 32, None)):
+        b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=16, n=20, window=6, commits=8, n_ptr=0, seed=2)
+        b.bank.k_store.nan_to_num_(0.0)
+        b.bank.v_store.nan_to_num_(0.0)
+        words = b.bank.meta.view(3, -1)
+        kp, bias = keeps(b, "alternate"), biases(b, bias)
+        q, idx, count, group, table, out, _ = scored_case(rs3, b, [40, 300, 200], [0, 0, 0], 1, 6.0, bias, kp)
+        n, F, good = rs3.rs3_scored_readout_workspace_bytes(b.bank, idx.shape[1]), b.bank.max_frames, words.clone()
+        off, length = 16, 16 + F
+        head, tail, oldest = int(good[1, 0]), int(good[1, 1]), int(good[1, 4])
+        wide = {off + i: head for i in range(F)} | {length + i: tail - head for i in range(F)}
+        second = (oldest + 1) % F
+        for change in (wide, {3: F + 1}, {3: -1}, {4: F}, {4: -1}, {3: 0}, {off + second: int(good[1, off + second]) + 1},
+                       {length + second: int(good[1, length + second]) - 1}, {length + second: -1}, {off + oldest: head - 1},
+                       {off + oldest: -(2 ** 62)}, {length + oldest: 2 ** 62}):
+            for word, value in change.items():
+                words[1, word] = value
+            ws = torch.full((n + 65536,), 77, dtype=torch.uint8, device="cuda")
+            again = torch.full_like(out, 5.0)
+            b.st.zero_()
+            run_scored(rs3, b, q, 1, idx, count, group, 6.0, bias, kp, table, 0.0, again, again, ws[:n])
+            code = int(b.st)
+            b.st.zero_()
+            words.copy_(good)
+            assert code == rs3.RS3_EINTERNAL, change
+            assert (again[1] == 5).all() and not (again[0] == 5).all() and not (again[2] == 5).all(), change
+            assert (ws[n:] == 77).all()
+
+
 def test_scored_readout_stays_inside_its_workspace_and_repeats_itself(rs3):
     for dtype, H, d in (("bf16", 2, 64), ("bf16", 1, 256), ("f32", 1, 32)):
         b = Built(rs3, U=3, H=H, d=d, dtype=dtype, m=16, n=20, window=4, commits=5, n_ptr=7, seed=2)
