@@ -6,6 +6,9 @@
 
 #define RS3_MAX_UNITS 4096  // units per readout call
 #define RS3_PAIR_ITEMS (1 << 30)   // above every item index
+// Scores in the log2 domain whose weights 2^s can be summed as they are: 2^80, a million of them and values up to 2^26 stay
+// within fp32's (and bf16's) 2^127, and 2^-80 leaves 2^-46 to values.
+#define RS3_BOUNDED 80.f
 
 struct GroupParts {         // a group's n pieces: 0 is in slot0, s >= 1 in slot 2 (slice + s); whose they are
     int32_t slot0, slice, n, u, h, qt;
@@ -22,6 +25,7 @@ struct ScoreArgs {
     const float *bias;          // [H][frames], bias_stride elements between units
     int64_t bias_stride;
     int tile_stride, frames;
+    int bounded;                // the cap holds scores within 2^+-RS3_BOUNDED: weights need no reference beside the biases'
     float cap;                  // cap * log2(e)
     float cap_step;             // 2 log2(e) scale / cap: tanh(x) = 1 - 2 / (1 + e^2x)
     float cap_half;             // raw scores up to here have |x| <= 1/2, where the polynomial holds

@@ -392,6 +392,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
         const uint32_t scol = tl + C::S_COL + (uint32_t)(BN * q), pcol = tl + C::P_COL + C::P_STEP * q;
         const uint32_t ocol = tl + C::O_COL + (uint32_t)(DH * q);
         constexpr bool changed = X::cap || X::bias;
+        const bool bounded = X::cap && bounded_scores(a);
         uint32_t tq = 0, passed = 0;                                   // tiles of this query tile; of all items so far
         int q_loaded = -1;                                             // item whose query rows are in shared memory
         // kept row of item w: its cell, or -1
@@ -429,7 +430,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 int nv = X::on ? 0 : walk.next();
                 ok = mbar_wait_warp(BAR(C::B_SFULL + q), tj & 1u, abort_flag, wait_ns);
                 if (!ok) break;
-                TileBias tb;
+                TileBias tb = {};
                 if constexpr (X::on) {
                     tb = C::Ring::read(gbase + C::OFF_BIAS, tile0 + (uint32_t)j);
                     nv = tb.rows;
@@ -446,11 +447,26 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 }
                 if constexpr (X::cap)                                  // (columns of no row share a reciprocal with others)
                     if (nv < BN) mask_cols(sr, nv, 0u);
-                if constexpr (changed) change_scores<X>(sr, a.score, tb, X::cap ? row_size(sr) : 0.f, sc, off);
-                if (nv < BN) mask_cols(sr, nv);
+                const float size = X::cap ? row_size(sr) : 0.f;
+                bool fused = false;
+                if constexpr (X::cap)
+                    fused = bounded && nv >= BN && (!X::bias || tb.same) && !__any_sync(0xffffffffu, !(size <= a.score.cap_half));
+                if (fused) {
+                    off = X::bias ? tb.all : 0.f;
+                } else {
+                    if constexpr (changed) change_scores<X>(sr, a.score, tb, size, sc, off);
+                    if (nv < BN) mask_cols(sr, nv);
+                }
                 // The reference moves at the first tile, and when a score passes it by
-                // more than 2^8; O (complete up to tile j - 1) and l follow it.
-                const float top = row_max(sr), mt = X::bias ? fmaf(top, sc, off) : top * sc;
+                // more than 2^8; O (complete up to tile j - 1) and l follow it.  Scores that a cap
+                // bounds need none but their biases'.
+                float mt;
+                if (X::cap && bounded) {
+                    mt = X::bias ? tb.top : 0.f;
+                } else {
+                    const float top = row_max(sr);
+                    mt = X::bias ? fmaf(top, sc, off) : top * sc;
+                }
                 if (j == 0) {
                     m_run = mt;
                 } else if (__any_sync(0xffffffffu, mt > m_run + 8.0f)) {
@@ -471,8 +487,8 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                     l_run *= alpha;
                     m_run = m_new;
                 }
-                const float sum = row_exp(sr, pk, sc, X::bias ? (m_run == -INFINITY ? 0.f : m_run) - off : m_run);
-                l_run += sum;
+                const float ref = X::bias ? (m_run == -INFINITY ? 0.f : m_run) - off : m_run;
+                l_run += weights<X>(fused, sr, pk, a, sc, ref);
                 if (C::PSEP && j > 0) {                                // P_q(j - 1) has been read
                     ok = mbar_wait_warp(BAR(C::B_PVDONE + q), (tj - 1u) & 1u, abort_flag, wait_ns);
                     if (!ok) break;

@@ -228,7 +228,7 @@ __device__ __forceinline__ void put_pair(uint32_t (&sr)[N], int c, uint64_t v)
 // tiles before that one had been read, so R >= KST + behind + 1 (everything before those is finished).
 struct TileBias {
     const float *each;
-    float all;
+    float all, top;             // the first's; the largest
     bool same;
     int rows;
 };
@@ -241,7 +241,7 @@ struct BiasRing {
     {
         const uint8_t *slot = ring + (t % R) * SLOT;
         const int4 h = *reinterpret_cast<const int4 *>(slot);
-        return {reinterpret_cast<const float *>(slot + 16), __int_as_float(h.y), h.z != 0, h.x};
+        return {reinterpret_cast<const float *>(slot + 16), __int_as_float(h.y), __int_as_float(h.w), h.z != 0, h.x};
     }
 };
 
@@ -312,6 +312,41 @@ __device__ __forceinline__ void cap_any(uint32_t (&sr)[N], const ScoreArgs &s)
     }
 }
 
+// 2^(cap tanh(s scale / cap) - ref) as bf16 pairs, for |s| <= cap_half; returns their sum.
+template <int N>
+__device__ __forceinline__ float capped_exp(const uint32_t (&sr)[N], uint32_t *pk, const ScoreArgs &s, float ref)
+{
+    const uint64_t nref2 = f2pack(-ref, -ref);
+    uint64_t k[4], acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = f2pack(s.cap_poly[i], s.cap_poly[i]);
+#pragma unroll
+    for (int c0 = 0; c0 < N; c0 += 8) {
+        uint64_t z[4], p[4];
+        float x[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) z[c] = mul2(get_pair(sr, c0 + 2 * c), get_pair(sr, c0 + 2 * c));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) p[c] = fma2(z[c], k[3], k[2]);
+#pragma unroll
+        for (int i = 1; i >= 0; --i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) p[c] = fma2(p[c], z[c], k[i]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) f2unpack(fma2(get_pair(sr, c0 + 2 * c), p[c], nref2), x[2 * c], x[2 * c + 1]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[c] = ex2_approx(x[c]);
+#pragma unroll
+        for (int c = 0; c < 8; c += 2) {
+            acc[c / 2] = add2(acc[c / 2], f2pack(x[c], x[c + 1]));
+            pk[(c0 + c) / 2] = pack_bf16x2(x[c], x[c + 1]);
+        }
+    }
+    float a, b;
+    f2unpack(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), a, b);
+    return a + b;
+}
+
 // N scores (raw) of consecutive rows into the softmax's: afterwards a score in the log2 domain is
 // sr * sc + off.  A bias that is the same for all of a tile's columns stays out of the scores.  A warp
 // whose scores are all within half the cap (`size`: the largest |s|) takes the polynomial, on the fp32
@@ -334,6 +369,15 @@ __device__ __forceinline__ void change_scores(uint32_t (&sr)[N], const ScoreArgs
             bias_scores(sr, sc, b);
             sc = 1.f;
         }
+}
+
+// A tile's weights: of raw scores that its cap takes to 2^+-RS3_BOUNDED (`fused`), or of changed ones.
+template <class X, int N, class Args>
+__device__ __forceinline__ float weights(bool fused, const uint32_t (&sr)[N], uint32_t *pk, const Args &a, float sc, float ref)
+{
+    if constexpr (X::cap)
+        if (fused) return capped_exp(sr, pk, a.score, ref);
+    return row_exp(sr, pk, sc, ref);
 }
 
 // Rows [nv, BN) of a stage (DH / 64 blocks of BN rows of 128 bytes) become zeros, by a whole warp,
@@ -399,21 +443,26 @@ struct RowsAhead {
     {
         const int2 e = e1;
         const int lane = threadIdx.x & 31;
-        float all = 0.f;
+        float all = 0.f, top = 0.f;
         bool same = true;
         if constexpr (X::bias) {
             all = log2_bias(__shfl_sync(0xffffffffu, b1[0], 0));
+            top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const float v = log2_bias(b1[i]);
                 reinterpret_cast<float *>(slot + 16)[lane + 32 * i] = v;
                 same = same && v == all;
+                top = fmaxf(top, v);
             }
             same = __all_sync(0xffffffffu, same);
+            if (!same)
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             biases();
             frames_of(e3);
         }
-        if (lane == 0) *reinterpret_cast<int4 *>(slot) = make_int4(e.y, __float_as_int(all), same, 0);
+        if (lane == 0) *reinterpret_cast<int4 *>(slot) = make_int4(e.y, __float_as_int(all), same, __float_as_int(top));
         __syncwarp();
         e1 = e2;
         e2 = e3;
@@ -421,6 +470,9 @@ struct RowsAhead {
         return e.x;
     }
 };
+
+__device__ __forceinline__ bool bounded_scores(const ReadoutArgs &) { return false; }
+__device__ __forceinline__ bool bounded_scores(const ReadoutMore &a) { return a.score.bounded != 0; }
 
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
 template <int DH, class X = PlainScores>
@@ -675,10 +727,36 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 rlen[q] = __ldg(&rs->len[q]);
             }
             float m_run = -INFINITY, l_part = 0.f;
+            // Scores that a cap bounds need no reference but their biases' (the same for all rows), so the slices
+            // have nothing to agree on before the item's end; a slice whose wait ran out goes there idle.
+            const bool bounded = X::cap && bounded_scores(a);
+            bool alive = true;
+            const auto rescale = [&](uint32_t tp, float alpha) {
+                // O must hold tile j-1 before its rows are rescaled; on
+                // a timeout the rescale is skipped and the next tile's
+                // barrier takes every slice out
+                const bool there = __all_sync(0xffffffffu, mbar_wait(BAR(C::B_PVDONE + tp % C::NPB), (tp / C::NPB) & 1u, abort_flag, wait_ns));
+                if (there) {
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c16 = 0; c16 < OCOLS / 16; ++c16) {
+                        uint32_t o[16];
+                        const uint32_t ta = tl + (uint32_t)(h * OCOLS) + 16u * c16;
+                        tmem_ld16(ta, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        tmem_st16(ta, o);
+                    }
+                }
+                return there;
+            };
             for (int j = 0; j < n; ++j) {
+                if (bounded && !alive) break;
                 const uint32_t tj = tcnt + (uint32_t)j, b = tj & 1u;
                 int nvt = 0;
-                TileBias tb;
+                TileBias tb = {};
                 const bool okw = __all_sync(0xffffffffu, mbar_wait(BAR(C::B_SFULL + b), (tj >> 1) & 1u, abort_flag, wait_ns));
                 if constexpr (X::on) {
                     if (okw) {
@@ -700,6 +778,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 float sc = a.scale_log2, off = 0.f;        // a score in the log2 domain: sr * sc + off
                 uint32_t sr[SCOLS], pk[PCOLS];
                 float rowsum = 0.f;
+                bool fused = false;
                 if (okw) {
                     tc_fence_after();
                     tmem_ld_cols<SCOLS>(scol + (uint32_t)(h * SCOLS), sr);
@@ -710,14 +789,33 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                     if (lane == 0) mbar_arrive(BAR(C::B_SFREE + b));
                     if constexpr (X::cap)                              // (columns of no row share a reciprocal with others)
                         if (nv < SCOLS) mask_cols(sr, nv, 0u);
-                    if constexpr (changed) change_scores<X>(sr, a.score, tb, X::cap ? row_size(sr) : 0.f, sc, off);
-                    if (nv < SCOLS) mask_cols(sr, nv);
+                    const float size = X::cap ? row_size(sr) : 0.f;
+                    if constexpr (X::cap)
+                        fused = bounded && nv >= SCOLS && (!X::bias || tb.same) && !__any_sync(0xffffffffu, !(size <= a.score.cap_half));
+                    if (fused) {
+                        off = X::bias ? tb.all : 0.f;
+                    } else {
+                        if constexpr (changed) change_scores<X>(sr, a.score, tb, size, sc, off);
+                        if (nv < SCOLS) mask_cols(sr, nv);
+                    }
                 }
                 const auto scored = [&](float x) { return X::bias ? fmaf(x, sc, off) : x * sc; };
                 const auto against = [&](float m) { return X::bias ? (m == -INFINITY ? 0.f : m) - off : m; };
                 float *redt = red + (b * NSPLIT) * BM;
                 float m_new = m_run;
-                if (j == 0) {
+                if (X::cap && bounded) {
+                    if (!okw) { alive = false; break; }
+                    const float top = X::bias ? tb.top : 0.f;
+                    if (j == 0) {
+                        m_new = top;
+                    } else if (top > m_run + 8.0f) {
+                        m_new = top;
+                        const float alpha = ex2_approx(m_run - m_new);
+                        alive = rescale(tj - 1u, alpha);
+                        l_part *= alpha;
+                    }
+                    rowsum = weights<X>(fused, sr, pk, a, sc, against(m_new));
+                } else if (j == 0) {
                     // the first tile of an item sets the reference: the row max
                     // over the slices (the scale is positive, so it is applied
                     // to the max of the raw scores)
@@ -751,27 +849,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                         }
                         const bool grow = m_new != m_run;
                         const float alpha = grow ? ex2_approx(m_run - m_new) : 1.0f;
-                        if (__any_sync(0xffffffffu, grow)) {
-                            // O must hold tile j-1 before its rows are rescaled; on
-                            // a timeout the rescale is skipped and the next tile's
-                            // barrier takes every slice out
-                            const uint32_t tp = tj - 1u;
-                            if (__all_sync(0xffffffffu, mbar_wait(BAR(C::B_PVDONE + tp % C::NPB),
-                                                                  (tp / C::NPB) & 1u, abort_flag, wait_ns))) {
-                                tc_fence_after();
-#pragma unroll 1
-                                for (int c16 = 0; c16 < OCOLS / 16; ++c16) {
-                                    uint32_t o[16];
-                                    const uint32_t ta = tl + (uint32_t)(h * OCOLS) + 16u * c16;
-                                    tmem_ld16(ta, o);
-                                    tmem_wait_ld();
-#pragma unroll
-                                    for (int e = 0; e < 16; ++e)
-                                        o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                                    tmem_st16(ta, o);
-                                }
-                            }
-                        }
+                        if (__any_sync(0xffffffffu, grow)) rescale(tj - 1u, alpha);
                         l_part *= alpha;
                     }
                 }
@@ -791,6 +869,8 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                                      "r"(pk[4 * cc + 1]), "r"(pk[4 * cc + 2]), "r"(pk[4 * cc + 3]) : "memory");
                     }
                     fence_proxy_async();
+                } else {
+                    alive = false;
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -804,7 +884,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                                                                    (tlast / C::NPB) & 1u, abort_flag, wait_ns));
                 float *redl = red + (2 * NSPLIT) * BM;
                 redl[h * BM + r] = l_part;
-                if (!bar_and(bar_id, bar_n, okw)) { ok = false; break; }
+                if (!bar_and(bar_id, bar_n, okw && (alive || !bounded))) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < NSPLIT; ++q) l_run += redl[q * BM + r];

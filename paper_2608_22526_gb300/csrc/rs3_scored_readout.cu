@@ -310,6 +310,7 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     a.score.frames = F + 2;
     const float log2e = 1.4426950408889634f;
     a.score.cap = cap * log2e;
+    a.score.bounded = cap > 0.f && a.score.cap <= RS3_BOUNDED;
     // tensor cores: of a raw score, for e^2x; CUDA cores: of one in the log2 domain, for tanh itself
     if (cap > 0.f) a.score.cap_step = L.path.kind == 1 ? 2.f * a.scale_log2 / cap : 1.f / a.score.cap;
     if (cap > 0.f) {
