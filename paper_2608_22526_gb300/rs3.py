@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -569,6 +570,13 @@ def _rows_of(name: str, t: torch.Tensor, width: int):
     return rows, (width if step is None else step)
 
 
+def _rows_arg(dev: int, name: str, t, dt, width: int):
+    """(rows, elements between rows, pointer) of a tensor [..., width] of this type on device `dev`."""
+    if t is None or t.dtype is not dt or t.get_device() != dev:
+        _want(dev, name, t, dt, 0)
+    return *_rows_of(name, t, width), t.data_ptr()
+
+
 def rs3_qk_norm_rope(q, q_out, k, k_out, dtype: str, mn: int, Hq: int, Hk: int, d: int, q_weight=None,
                      k_weight=None, eps: float = 1e-6, rope=None, q_keep=None, k_keep=None, stream=None):
     """RMS norm of every head of q [..., Hq*d] and k [..., Hk*d] (either may be None),
@@ -624,24 +632,28 @@ def rs3_rope_table(pos, spec: RopeSpec, cos_sin, stream=None):
     _check(lib.rs3_rope_table(_ptr(pos), rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
 
 
+def _rope_side(dev: int, name: str, x, y, dt, H: int, d: int, pos, axes: int, keep):
+    """What rs3_rope_rows takes for the queries or the keys."""
+    if x is None and y is None:
+        return None, 0, 0, 0, None, None, None, 0
+    width = H * d
+    rows, stride, x_ptr = _rows_arg(dev, name, x, dt, width)
+    rows_out, out_stride, y_ptr = _rows_arg(dev, name + "_out", y, dt, width)
+    if rows != rows_out:
+        raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
+    return (x_ptr, rows, stride, H, _arg(dev, name + "_pos", pos, torch.int32, rows * axes),
+            None if keep is None else _arg(dev, name + "_keep", keep, torch.uint8, rows), y_ptr, out_stride)
+
+
 def rs3_rope_rows(q, q_out, q_pos, k, k_out, k_pos, dtype: str, Hq: int, Hk: int, d: int, spec: RopeSpec, q_keep=None,
                   k_keep=None, stream=None):
     """Every head of q [..., Hq*d] and k [..., Hk*d] (either may be None) turned by its row's
     position (int32 [rows, axes]).  Rows may be evenly spaced parts of a wider tensor; out may
     be the input; rows whose keep byte is 0 are neither read nor written."""
-    dev, dt, sides = torch.cuda.current_device(), TORCH_DTYPES[dtype], []
-    for name, x, y, pos, H, keep in (("q", q, q_out, q_pos, Hq, q_keep), ("k", k, k_out, k_pos, Hk, k_keep)):
-        if x is None and y is None:
-            sides += [None, 0, 0, 0, None, None, None, 0]
-            continue
-        _want(dev, name, x, dt, 0)
-        _want(dev, name + "_out", y, dt, 0)
-        (rows, stride), (rows_out, out_stride) = _rows_of(name, x, H * d), _rows_of(name + "_out", y, H * d)
-        if rows != rows_out:
-            raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
-        sides += [x.data_ptr(), rows, stride, H, _arg(dev, name + "_pos", pos, torch.int32, rows * spec.axes),
-                  None if keep is None else _arg(dev, name + "_keep", keep, torch.uint8, rows), y.data_ptr(), out_stride]
-    rc = lib.rs3_rope_rows(*sides, DTYPES[dtype], d, ctypes.byref(spec), _stream(stream))
+    dev, dt, axes = torch.cuda.current_device(), TORCH_DTYPES[dtype], spec.axes
+    rc = lib.rs3_rope_rows(*_rope_side(dev, "q", q, q_out, dt, Hq, d, q_pos, axes, q_keep),
+                           *_rope_side(dev, "k", k, k_out, dt, Hk, d, k_pos, axes, k_keep), DTYPES[dtype], d, ctypes.byref(spec),
+                           _stream(stream))
     _check(rc, "rs3_rope_rows")
 
 
@@ -655,18 +667,23 @@ def _vector(dev: int, name: str, t, U: int, C: int):
     """(pointer, elements between units) of a vector fp32 [C] or [U, C]; (None, 0) without one."""
     if t is None:
         return None, 0
-    shape = t.shape
-    if not (shape[-1:] == (C,) and (len(shape) == 1 or (len(shape) == 2 and shape[0] == U))):
-        raise ValueError(f"{name}: [{C}] or [{U}, {C}] wanted, got {tuple(shape)}")
-    return _arg(dev, name, t, torch.float32, C), C if len(shape) == 2 else 0
+    n = t.numel()
+    if n == C and t.dim() == 1:
+        return _arg(dev, name, t, torch.float32, C), 0
+    if n != U * C or tuple(t.shape) != (U, C):
+        raise ValueError(f"{name}: [{C}] or [{U}, {C}] wanted, got {tuple(t.shape)}")
+    return _arg(dev, name, t, torch.float32, C), C
+
+
+_norm_bytes = struct.Struct("ifNNqq").pack                 # a Norm, without its object
 
 
 def _norm(dev: int, name: str, kind: str, eps: float, weight, bias, U: int, C: int):
-    if kind == "none" and weight is None and bias is None:
-        return None
+    if weight is None and bias is None:
+        return None if kind == "none" else _norm_bytes(NORM_KINDS[kind], eps, 0, 0, 0, 0)
     w, w_stride = _vector(dev, name + "_weight", weight, U, C)
     b, b_stride = _vector(dev, name + "_bias", bias, U, C)
-    return ctypes.byref(Norm(NORM_KINDS[kind], eps, w, b, w_stride, b_stride))
+    return _norm_bytes(NORM_KINDS[kind], eps, w or 0, b or 0, w_stride, b_stride)
 
 
 def rs3_norm_residual(y, x, x_out, h_out, dtype: str, idx=None, count=None, post: str = "none", post_weight=None,
@@ -679,19 +696,20 @@ def rs3_norm_residual(y, x, x_out, h_out, dtype: str, idx=None, count=None, post
         raise ValueError(f"x: [units, cells, channels] wanted, got {tuple(x.shape)}")
     U, mn, C = x.shape
     n = U * mn * C
-    grids = [None if t is None else _arg(dev, name, t, dt, n) for name, t in (("y", y), ("x", x), ("x_out", x_out), ("h_out", h_out))]
-    k_max, idx_ptr, count_ptr = 0, None, None
+    k_max, idx_ptr, count_ptr, status_ptr = 0, None, None, None
     if idx is not None or count is not None:
         if idx is None or idx.dim() != 2 or idx.shape[0] != U:
             raise ValueError("idx: one row per unit, with count")
         k_max = idx.shape[1]
         idx_ptr, count_ptr = _arg(dev, "idx", idx, torch.int32, 0), _arg(dev, "count", count, torch.int32, U)
-        _want(dev, "status", status, torch.int32, 1)
+        status_ptr = _arg(dev, "status", status, torch.int32, 1)
     g, g_stride = _vector(dev, "gate", gate, U, C)
-    rc = lib.rs3_norm_residual(grids[0], grids[1], DTYPES[dtype], U, mn, C, idx_ptr, count_ptr, k_max,
-                               _norm(dev, "post", post, eps, post_weight, post_bias, U, C), g, g_stride, float(alpha),
-                               _norm(dev, "pre", pre, eps, pre_weight, pre_bias, U, C), grids[2], grids[3],
-                               _ptr(status), _stream(stream))
+    rc = lib.rs3_norm_residual(None if y is None else _arg(dev, "y", y, dt, n), _arg(dev, "x", x, dt, n), DTYPES[dtype], U, mn, C,
+                               idx_ptr, count_ptr, k_max, _norm(dev, "post", post, eps, post_weight, post_bias, U, C), g, g_stride,
+                               alpha, _norm(dev, "pre", pre, eps, pre_weight, pre_bias, U, C),
+                               None if x_out is None else _arg(dev, "x_out", x_out, dt, n),
+                               None if h_out is None else _arg(dev, "h_out", h_out, dt, n),
+                               status_ptr, _stream(stream))
     _check(rc, "rs3_norm_residual")
 
 
