@@ -109,12 +109,15 @@ struct ReadoutPath {
 // the path of a call over banks of this many rows with this workspace (INT64_MAX and
 // SIZE_MAX: the path that any workspace is sized for)
 ReadoutPath choose_readout_path(rs3_dtype dtype, int d, int U, int H, int k_max, int64_t bank_rows, size_t workspace_bytes);
+// The CUDA-core path `p` with fewer query rows to a CTA, and whether a call has too few of them for `p`.
+ReadoutPath rs3_few_rows(ReadoutPath p, int d);
+bool rs3_has_few_rows(const ReadoutPath &p, int U, int H, int d, int k_max, int64_t bank_rows);
 bool rs3_tc_supported(int d);
 int rs3_tc_block_n(int d);
 rs3_status rs3_launch_tc_readout(const ReadoutArgs &a, cudaStream_t st);
 rs3_status rs3_launch_either_readout(const ReadoutArgs &a, cudaStream_t st);   // d = 64, 128
 // CUDA-core path: rows and keys of a tile and resident CTAs per SM, for a head width
-void rs3_simt_tile(int d, int &bm, int &bn, int &ctas_per_sm);
+void rs3_simt_tile(int d, bool few, int &bm, int &bn, int &ctas_per_sm);
 rs3_status rs3_launch_simt_readout(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st);
 rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
                                const int32_t *unit_group, const int32_t *idx, const int32_t *count,

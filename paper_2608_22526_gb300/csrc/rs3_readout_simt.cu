@@ -1,16 +1,27 @@
 // rs3_readout_simt.cu -- the CUDA-core readout (rs3_readout_simt.cuh) over plain scores.
 #include "rs3_readout_simt.cuh"
 
-void rs3_simt_tile(int d, int &bm, int &bn, int &ctas_per_sm)
+namespace {
+
+template <int ROWS>
+void tile(int d, int &bm, int &ctas_per_sm)
+{
+    switch (d) {
+    case 16: bm = Cfg<16, ROWS>::BM; ctas_per_sm = Cfg<16, ROWS>::CTAS; break;
+    case 32: bm = Cfg<32, ROWS>::BM; ctas_per_sm = Cfg<32, ROWS>::CTAS; break;
+    case 64: bm = Cfg<64, ROWS>::BM; ctas_per_sm = Cfg<64, ROWS>::CTAS; break;
+    case 128: bm = Cfg<128, ROWS>::BM; ctas_per_sm = Cfg<128, ROWS>::CTAS; break;
+    default: bm = Cfg<256, ROWS>::BM; ctas_per_sm = Cfg<256, ROWS>::CTAS; break;
+    }
+}
+
+}  // namespace
+
+void rs3_simt_tile(int d, bool few, int &bm, int &bn, int &ctas_per_sm)
 {
     bn = BN;
-    switch (d) {
-    case 16: bm = Cfg<16>::BM; ctas_per_sm = Cfg<16>::CTAS; break;
-    case 32: bm = Cfg<32>::BM; ctas_per_sm = Cfg<32>::CTAS; break;
-    case 64: bm = Cfg<64>::BM; ctas_per_sm = Cfg<64>::CTAS; break;
-    case 128: bm = Cfg<128>::BM; ctas_per_sm = Cfg<128>::CTAS; break;
-    default: bm = Cfg<256>::BM; ctas_per_sm = Cfg<256>::CTAS; break;
-    }
+    if (few) tile<FEW>(d, bm, ctas_per_sm);
+    else tile<0>(d, bm, ctas_per_sm);
 }
 
 rs3_status rs3_launch_simt_readout(const ReadoutArgs &a, rs3_dtype dtype, cudaStream_t st)

@@ -35,9 +35,12 @@ namespace {
 constexpr int BN = 32;              // keys per tile
 constexpr int NW = 4;               // warps per CTA
 
-template <int D>
+constexpr int FEW = 2;              // rows per lane where there are few (rs3_has_few_rows)
+
+// ROWS: rows per lane, or 0 for as many as the registers hold.
+template <int D, int ROWS = 0>
 struct Cfg {
-    static constexpr int TM = D <= 128 ? 8 : 4;      // rows per lane
+    static constexpr int TM = ROWS ? ROWS : D <= 128 ? 8 : 4;      // rows per lane
     static constexpr int RW = 4 * TM;                // rows per warp
     static constexpr int BM = NW * RW;
     static constexpr int LD = D + 4;                 // row stride in shared memory (floats)
@@ -50,7 +53,7 @@ struct Cfg {
     static constexpr int VW = TC < 4 ? TC : 4;       // columns per load
     static constexpr int NJ = TC / VW;
     static constexpr int SMEM = 4 * (BM * LD + 2 * 2 * BN * LD + BM * PLD);
-    static constexpr int CTAS = SMEM <= 113 * 1024 ? 2 : 1;   // resident per SM
+    static constexpr int CTAS = ROWS && SMEM <= 56 * 1024 ? 4 : SMEM <= 113 * 1024 ? 2 : 1;   // resident per SM
 };
 
 using tc::fma2;
@@ -134,12 +137,12 @@ struct Tiles {
     }
 };
 
-template <typename T, int D, class X>
-__global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(typename ReadoutOf<X>::Args a)
+template <typename T, int D, class X, int ROWS>
+__global__ void __launch_bounds__(NW * 32, Cfg<D, ROWS>::CTAS) k_readout_simt(typename ReadoutOf<X>::Args a)
 {
-    using C = Cfg<D>;
+    using C = Cfg<D, ROWS>;
     constexpr int TM = C::TM, RW = C::RW, BM = C::BM, LD = C::LD, PLD = C::PLD, KC = C::KC, KG = C::KG,
-                  TC = C::TC, VW = C::VW, NJ = C::NJ;
+                  TC = C::TC, VW = C::VW, NJ = C::NJ, QR = TM < 4 ? TM : 4;
     pdl_wait();
     extern __shared__ __align__(16) float sm[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tr = (lane & 1) | (lane >> 4) << 1,
@@ -275,17 +278,17 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(typename
 #pragma unroll
                         for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const ulonglong2 *>(kp + 8 * j * LD + k);
 #pragma unroll
-                        for (int i0 = 0; i0 < TM; i0 += 4) {
-                            ulonglong2 qv[4];
+                        for (int i0 = 0; i0 < TM; i0 += QR) {
+                            ulonglong2 qv[QR];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
+                            for (int i = 0; i < QR; ++i)
                                 qv[i] = *reinterpret_cast<const ulonglong2 *>(qp + 4 * (i0 + i) * LD + k);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
+                            for (int i = 0; i < QR; ++i)
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) acc[i0 + i][j] = fma2(qv[i].x, kv[j].x, acc[i0 + i][j]);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
+                            for (int i = 0; i < QR; ++i)
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) acc[i0 + i][j] = fma2(qv[i].y, kv[j].y, acc[i0 + i][j]);
                         }
@@ -449,12 +452,19 @@ __global__ void __launch_bounds__(NW * 32, Cfg<D>::CTAS) k_readout_simt(typename
     }
 }
 
+template <typename T, int D, class X, int ROWS>
+rs3_status launch_rows(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
+{
+    if (rs3_kernel_smem((const void *)k_readout_simt<T, D, X, ROWS>, Cfg<D, ROWS>::SMEM) != RS3_OK) return RS3_ECUDA;
+    launch_pdl(k_readout_simt<T, D, X, ROWS>, dim3((unsigned)a.grid_ctas), dim3(NW * 32), Cfg<D, ROWS>::SMEM, st, a);
+    return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+}
+
+// The kernel whose rows the path's items have.
 template <typename T, int D, class X>
 rs3_status launch(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
 {
-    if (rs3_kernel_smem((const void *)k_readout_simt<T, D, X>, Cfg<D>::SMEM) != RS3_OK) return RS3_ECUDA;
-    launch_pdl(k_readout_simt<T, D, X>, dim3((unsigned)a.grid_ctas), dim3(NW * 32), Cfg<D>::SMEM, st, a);
-    return cudaGetLastError() == cudaSuccess ? RS3_OK : RS3_ECUDA;
+    return a.BM == Cfg<D, FEW>::BM ? launch_rows<T, D, X, FEW>(a, st) : launch_rows<T, D, X, 0>(a, st);
 }
 
 }  // namespace

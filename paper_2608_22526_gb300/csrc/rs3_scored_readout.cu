@@ -235,11 +235,16 @@ struct ScoredLayout {
     int tables;                 // of key tiles: where a head's two kernels have tiles of different rows, two
 };
 
-ScoredLayout scored_layout(const rs3_bank *bank, int k_max)
+ReadoutPath scored_path(const rs3_bank *bank, int k_max)
+{
+    return choose_readout_path((rs3_dtype)bank->dtype, bank->d, bank->U, bank->H, k_max, bank->rows_per_unit, SIZE_MAX);
+}
+
+ScoredLayout scored_layout(const rs3_bank *bank, int k_max, const ReadoutPath &path)
 {
     const int U = bank->U, F = bank->max_frames;
     ScoredLayout L;
-    L.path = choose_readout_path((rs3_dtype)bank->dtype, bank->d, U, bank->H, k_max, bank->rows_per_unit, SIZE_MAX);
+    L.path = path;
     L.tables = L.path.either && L.path.BN != 128 ? 2 : 1;
     const size_t n = (size_t)U * L.tables;
     L.l = rs3_readout_layout(U, bank->H, bank->d, k_max, L.path, false);
@@ -263,7 +268,9 @@ ScoredLayout scored_layout(const rs3_bank *bank, int k_max)
 extern "C" size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max)
 {
     if (!bank || bank->magic != RS3_BANK_MAGIC || k_max < 0) return 0;
-    return scored_layout(bank, k_max).total;
+    const ReadoutPath p = scored_path(bank, k_max);        // (a call of fewer queries may take the other one)
+    const size_t n = scored_layout(bank, k_max, p).total;
+    return p.kind == 0 ? std::max(n, scored_layout(bank, k_max, rs3_few_rows(p, bank->d)).total) : n;
 }
 
 extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d, const int32_t *unit_group,
@@ -278,9 +285,11 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
     const int F = bank->max_frames;
     if (frame_bias && ((reinterpret_cast<uintptr_t>(frame_bias) & 3u) || (bias_stride != 0 && bias_stride < (int64_t)H * (F + 2)))) return RS3_EINVAL;
     if ((int64_t)bank->U * bank->rows_per_unit >= (int64_t)1 << 31) return RS3_EUNSUPPORTED;
-    const ScoredLayout L = scored_layout(bank, k_max);
-    if (!rs3_readout_fits(bank->U, H, k_max, L.path)) return RS3_EUNSUPPORTED;
-    if (workspace_bytes < L.total) return RS3_ECAPACITY;
+    ReadoutPath path = scored_path(bank, k_max);
+    if (!rs3_readout_fits(bank->U, H, k_max, path)) return RS3_EUNSUPPORTED;
+    if (workspace_bytes < rs3_scored_readout_workspace_bytes(bank, k_max)) return RS3_ECAPACITY;
+    if (rs3_has_few_rows(path, bank->U, H, d, k_max, bank->rows_per_unit)) path = rs3_few_rows(path, d);
+    const ScoredLayout L = scored_layout(bank, k_max, path);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     FramesArgs f = {};

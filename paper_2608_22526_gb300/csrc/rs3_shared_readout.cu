@@ -337,13 +337,18 @@ struct ShareLayout {
 // Queries of a class: no more than cells, nor than its units keep.
 int class_stride(int U, int mn, int k_max) { return (int)std::min<int64_t>(mn, (int64_t)U * k_max); }
 
-ShareLayout share_layout(const rs3_bank *bank, const rs3_bank *prefix, int k_max)
+// `few`: of the paths with fewer query rows to a CTA, where there are such (1: yes, 0: no, -1: as the calls have them)
+ShareLayout share_layout(const rs3_bank *bank, const rs3_bank *prefix, int k_max, int few)
 {
     const rs3_dtype dtype = (rs3_dtype)bank->dtype;
     const int U = bank->U, H = bank->H, d = bank->d;
     ShareLayout L;
     L.own = choose_readout_path(dtype, d, U, H, k_max, bank->rows_per_unit, SIZE_MAX);
     L.pre = choose_readout_path(dtype, d, U, H, k_max, prefix->rows_per_unit, SIZE_MAX);
+    if (L.own.kind == 0) {
+        if (few < 0 ? rs3_has_few_rows(L.own, U, H, d, k_max, bank->rows_per_unit) : few) L.own = rs3_few_rows(L.own, d);
+        if (few < 0 ? rs3_has_few_rows(L.pre, U, H, d, k_max, prefix->rows_per_unit) : few) L.pre = rs3_few_rows(L.pre, d);
+    }
     // the classes' tiles together are no more than their units' (a sum's ceiling is no more than the sum of ceilings)
     L.own_l = rs3_readout_layout(U, H, d, k_max, L.own, true);
     L.pre_l = rs3_readout_layout(U, H, d, k_max, L.pre, true);
@@ -368,7 +373,9 @@ bool bank_known(const rs3_bank *b) { return b && b->magic == RS3_BANK_MAGIC; }
 extern "C" size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const rs3_bank *prefix, int k_max)
 {
     if (!bank_known(bank) || !bank_known(prefix) || k_max < 0) return 0;
-    return share_layout(bank, prefix, k_max).total;
+    // (each part's is the larger of both paths': a call of fewer queries may take the other one)
+    const ShareLayout a = share_layout(bank, prefix, k_max, 0), b = share_layout(bank, prefix, k_max, 1);
+    return a.own_ws + align_up(std::max(a.own_l.total, b.own_l.total), 256) + std::max(a.pre_l.total, b.pre_l.total);
 }
 
 extern "C" rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d, const int32_t *unit_group,
@@ -382,9 +389,9 @@ extern "C" rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, 
     if (!bank_known(prefix) || !prefix->meta || !prefix->k_store || !prefix->v_store || !prefix_unit) return RS3_EINVAL;
     if (prefix->dtype != bank->dtype || prefix->H != H || prefix->d != d || bank->mn != mn || prefix->mn != mn || k_max > mn) return RS3_EINVAL;
     if (prefix->U > RS3_MAX_UNITS) return RS3_EUNSUPPORTED;
-    const ShareLayout L = share_layout(bank, prefix, k_max);
+    const ShareLayout L = share_layout(bank, prefix, k_max, -1);
     if (!rs3_readout_fits(bank->U, H, k_max, L.own) || !rs3_readout_fits(bank->U, H, k_max, L.pre)) return RS3_EUNSUPPORTED;
-    if (workspace_bytes < L.total) return RS3_ECAPACITY;
+    if (workspace_bytes < rs3_shared_readout_workspace_bytes(bank, prefix, k_max)) return RS3_ECAPACITY;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int U = bank->U;

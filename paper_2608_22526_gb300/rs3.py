@@ -451,6 +451,20 @@ def _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope,
     return dev
 
 
+def _read_args(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int, bank: "Bank", rope, residual, out,
+               workspace, status):
+    """What the readouts of scores or of a prefix have in common, checked: (device, arguments up to the bank, those from
+    rope to out, the workspace's and the status)."""
+    dev, dt, U, grid = torch.cuda.current_device(), TORCH_DTYPES[dtype], bank.U, mn * H * d
+    _want_bank(dev, bank)
+    _want_workspace(dev, workspace)
+    head = (_arg(dev, "q", q, dt, G * grid), DTYPES[dtype], G, mn, H, d, _arg(dev, "unit_group", unit_group, torch.int32, U),
+            _arg(dev, "idx", idx, torch.int32, U * k_max), _arg(dev, "count", count, torch.int32, U), k_max, ctypes.byref(bank.desc))
+    to = (None if rope is None else _arg(dev, "rope", rope, torch.float32, mn * d),
+          None if residual is None else _arg(dev, "residual", residual, dt, U * grid), _arg(dev, "out", out, dt, U * grid))
+    return dev, head, to, (_ptr(workspace), _bytes(workspace), _arg(dev, "status", status, torch.int32, 1))
+
+
 def rs3_scored_readout_workspace_bytes(bank: "Bank", k_max: int) -> int:
     return int(lib.rs3_scored_readout_workspace_bytes(ctypes.byref(bank.desc), k_max))
 
@@ -460,7 +474,7 @@ def rs3_scored_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
     """rs3_memory_readout with scores capped at `cap` (0: not), biased by frame_bias fp32 [H, F+2] or [U, H, F+2], over
     the frames that frame_keep uint8 [U, F+2] leaves; F = bank.max_frames: ages of ring frames, then conditioning
     frames, then pointers."""
-    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    dev, head, to, tail = _read_args(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, residual, out, workspace, status)
     F, stride, bias_ptr, keep_ptr = bank.max_frames, 0, None, None
     if frame_bias is not None:
         if tuple(frame_bias.shape) not in ((H, F + 2), (bank.U, H, F + 2)):
@@ -471,14 +485,7 @@ def rs3_scored_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_grou
         if tuple(frame_keep.shape) != (bank.U, F + 2):
             raise ValueError(f"frame_keep: [{bank.U}, {F + 2}] wanted, got {tuple(frame_keep.shape)}")
         keep_ptr = _arg(dev, "frame_keep", frame_keep, torch.uint8, 0)
-    _want_workspace(dev, workspace)
-    if residual is not None:
-        _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
-    _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
-    rc = lib.rs3_scored_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
-                                ctypes.byref(bank.desc), float(cap), bias_ptr, stride, keep_ptr, _ptr(rope),
-                                _ptr(residual), _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status),
-                                _stream(stream))
+    rc = lib.rs3_scored_readout(*head, float(cap), bias_ptr, stride, keep_ptr, *to, float(scale), *tail, _stream(stream))
     _check(rc, "rs3_scored_readout")
 
 
@@ -489,16 +496,10 @@ def rs3_shared_readout_workspace_bytes(bank: "Bank", prefix: "Bank", k_max: int)
 def rs3_shared_readout(q, dtype: str, G: int, mn: int, H: int, d: int, unit_group, idx, count, k_max: int, bank: "Bank",
                        prefix: "Bank", prefix_unit, rope, residual, out, scale: float, workspace, status, stream=None):
     """rs3_memory_readout over the rows of unit prefix_unit[u] of `prefix` (-1: none) and the unit's own in `bank`."""
-    dev = _want_read(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, status)
+    dev, head, to, tail = _read_args(q, dtype, G, mn, H, d, unit_group, idx, count, k_max, bank, rope, residual, out, workspace, status)
     _want_bank(dev, prefix)
-    _want(dev, "prefix_unit", prefix_unit, torch.int32, bank.U)
-    _want_workspace(dev, workspace)
-    if residual is not None:
-        _want(dev, "residual", residual, TORCH_DTYPES[dtype], bank.U * mn * H * d)
-    _want(dev, "out", out, TORCH_DTYPES[dtype], bank.U * mn * H * d)
-    rc = lib.rs3_shared_readout(_ptr(q), DTYPES[dtype], G, mn, H, d, _ptr(unit_group), _ptr(idx), _ptr(count), k_max,
-                                ctypes.byref(bank.desc), ctypes.byref(prefix.desc), _ptr(prefix_unit), _ptr(rope), _ptr(residual),
-                                _ptr(out), float(scale), _ptr(workspace), _bytes(workspace), _ptr(status), _stream(stream))
+    rc = lib.rs3_shared_readout(*head, ctypes.byref(prefix.desc), _arg(dev, "prefix_unit", prefix_unit, torch.int32, bank.U), *to,
+                                float(scale), *tail, _stream(stream))
     _check(rc, "rs3_shared_readout")
 
 
