@@ -462,6 +462,57 @@ def test_scored_readout_of_scores_of_all_sizes(rs3, dtype, d):
     scored_case(rs3, b, [100, 40], [0, 0], 1, 3.0, late, None)
 
 
+@pytest.mark.parametrize("dtype,H,d,m", [("bf16", 2, 64, 16), ("bf16", 1, 128, 16), ("bf16", 1, 256, 16), ("bf16", 8, 64, 64), ("bf16", 4, 128, 80),
+                                         ("f32", 1, 64, 16)])
+@pytest.mark.parametrize("cap", [55.0, 55.5, 200.0])
+def test_scored_readout_of_rows_at_either_end_of_the_cap(rs3, dtype, H, d, m, cap):
+    """Rows whose scores are all near minus the cap, all near the cap, some of either, and within half of it, on both sides of
+    the largest cap whose weights need no running maximum; biases that lift and sink frames by more than the cap."""
+    b = Built(rs3, U=2, H=H, d=d, dtype=dtype, m=m, n=m, window=4 if m == 16 else 8, commits=6 if m == 16 else 8, n_ptr=3, seed=5, density=0.7)
+    spoil(b, None)
+    b.bank.k_store.abs_()
+    U, mn, D = 2, b.mn, b.D
+    counts = [mn // 2, mn - 1]
+    idx, count = keep_sets(U, mn, mn, counts, 6)
+    g = gen(8)
+    q = torch.randn((1, mn, D), generator=g, device="cuda").abs() * 8.0
+    kind = torch.arange(mn, device="cuda")[None, :, None] // 32 % 4
+    mixed = torch.randn((1, mn, D), generator=g, device="cuda")
+    q = torch.where(kind == 0, -q, torch.where(kind == 1, q, torch.where(kind == 2, 20.0 * mixed, mixed))).to(DT[dtype])
+    group = torch.zeros(2, dtype=torch.int32, device="cuda")
+    unit = biases(b, "unit") * 60.0
+    for bias in (None, unit, torch.where(torch.rand(unit.shape, generator=g, device="cuda") < 0.3, -math.inf, unit)):
+        out = torch.full((U, mn, D), math.nan, dtype=DT[dtype], device="cuda")
+        want, tol = reference(dtype, H, d, q, idx, counts, group, None, d ** -0.5, None, out.shape, scored_rows(b, None), cap,
+                              None if bias is None else lambda u, h: bias[u, h])
+        run_scored(rs3, b, q, 1, idx, count, group, cap, bias, None, None, 0.0, None, out)
+        assert int(b.st) == 0
+        err = (out.double() - want).abs()
+        assert (err <= tol).all(), (float((err - tol).max()), float(err.max()))
+        assert tol.max() < 1.0
+
+
+@pytest.mark.parametrize("dtype,H,d", [("f32", 4, 64), ("f32", 8, 32), ("f32", 8, 16), ("f32", 4, 256), ("bf16", 8, 16), ("bf16", 8, 32)])
+def test_readouts_of_whole_query_tiles_on_the_cuda_cores(rs3, dtype, H, d):
+    """Enough queries and keys that a CTA takes its largest query tile, and calls with a few of either on the same workspace."""
+    U, counts = 8, [300, 1, 0, 129, 128, 300, 257, 64]
+    b = Built(rs3, U=U, H=H, d=d, dtype=dtype, m=30, n=30, window=2, commits=3, n_ptr=5, seed=4)
+    BM, ctas = (64, 1) if d == 256 else (128, 2)
+    assert U * H * -(-300 // BM) * (b.bank.rows_per_unit // 32) >= 16 * ctas * torch.cuda.get_device_properties(0).multi_processor_count
+    kp, bias = keeps(b, "some"), biases(b, "unit")
+    spoil(b, kp)
+    scored_case(rs3, b, counts, [0, 1] * 4, 2, 9.0, bias, kp, "inplace")
+    q, idx, count, group, table, out, ws = scored_case(rs3, b, counts, [0] * U, 1, 0.0, None, kp, "none", rope=True, k_max=300)
+    few, first = torch.full_like(out, math.nan), idx[:, :20].contiguous()
+    run_scored(rs3, b, q, 1, first, count.clamp(max=20), group, 0.0, None, kp, table, 0.0, None, few, ws)
+    assert int(b.st) == 0
+    want, tol = reference(dtype, H, d, q, first, [min(n, 20) for n in counts], group, table, d ** -0.5, None, out.shape, scored_rows(b, kp))
+    assert ((few.double() - want).abs() <= tol).all()
+    c = built(rs3, U=U, H=H, d=d, dtype=dtype, m=30, n=30, window=2, commits=3, n_ptr=5, seed=4)
+    p = built(rs3, U=2, H=H, d=d, dtype=dtype, m=30, n=30, window=3, commits=3, n_ptr=0, seed=6)
+    shared_case(rs3, c, p, counts, [0] * U, [0, 0, 1, 1, 1, 0, -1, 1], 1, "other")
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256), ("f32", 32)])
 @pytest.mark.parametrize("lowest", [-3.4028234663852886e38, -math.inf])
 def test_scored_readout_masked_by_the_lowest_value(rs3, dtype, d, lowest):
