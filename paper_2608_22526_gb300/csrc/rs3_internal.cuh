@@ -69,7 +69,8 @@ struct ReadoutHeader {
     int32_t n_part;         // partial pieces of all split groups
     int32_t bm;             // query rows of an item: which kernel the items are for
     int32_t n_groups;
-    int32_t pad[26];
+    int32_t passed;         // words of cells that have been passed through so far (where that is left to the kernels behind)
+    int32_t pad[25];
 };
 
 struct ReadoutLayout {      // byte offsets inside the workspace

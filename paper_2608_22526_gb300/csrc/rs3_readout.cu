@@ -429,7 +429,10 @@ __device__ __forceinline__ void plan_cta(const Args &a)
         hdr->slices = v.P;
         hdr->n_part = s_np;
         hdr->bm = cfg.BM;
-        if constexpr (more) hdr->n_groups = grun;
+        if constexpr (more) {
+            hdr->n_groups = grun;
+            hdr->passed = 0;
+        }
     }
 }
 
@@ -481,11 +484,13 @@ __device__ __forceinline__ void store_out1(const uint16_t *res, uint16_t *out, i
     out[off] = float_to_bf16_bits((res ? bf16_bits_to_float(res[off]) : 0.f) + o);
 }
 
-// With STRICT, rows of cells that are none are skipped.
+// With STRICT, rows of cells that are none are skipped, and cells that have not been passed through yet are.
 template <typename T, int E, bool STRICT>
-__global__ void __launch_bounds__(256) k_combine(ReadoutArgs a)
+__global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRICT, ReadoutMore, ReadoutArgs>::type a)
 {
     pdl_wait();
+    if constexpr (STRICT && sizeof(T) == 2)
+        if (a.kept) pass_cells(a, nullptr);
     constexpr int CW = 32 * E;                      // columns per warp
     const int d = a.d;
     // chunked tasks only when the groups are split more than four ways on
@@ -860,10 +865,10 @@ rs3_status rs3_readout_prepare(const void *q, rs3_dtype dtype, int G, int mn, in
 namespace {
 
 // 16-byte pieces of the pass-through (out of place only) and the CTAs for them
-int64_t pass_pieces(const ReadoutArgs &a, rs3_dtype dtype, int64_t &blocks)
+int64_t pass_pieces(const ReadoutArgs &a, bool later, rs3_dtype dtype, int64_t &blocks)
 {
     blocks = 0;
-    if (a.residual == a.out) return 0;
+    if (a.residual == a.out || later) return 0;
     const int64_t nvec = (int64_t)a.U * a.mn * a.D * (dtype == RS3_BF16 ? 2 : 4) / 16;
     blocks = (nvec + PLAN_THREADS - 1) / PLAN_THREADS;
     const int64_t cap = (int64_t)a.n_sm * 8;
@@ -879,7 +884,9 @@ template <class Args>
 rs3_status launch_plan(const Args &a, cudaStream_t st, rs3_dtype dtype)
 {
     int64_t blocks;
-    const int64_t nvec = pass_pieces(a, dtype, blocks);
+    bool later = false;
+    if constexpr (std::is_same<Args, ReadoutMore>::value) later = a.kept != nullptr;
+    const int64_t nvec = pass_pieces(a, later, dtype, blocks);
     if (rs3_kernel_smem((const void *)k_plan<Args>, plan_bytes(a.U)) != RS3_OK) return RS3_EUNSUPPORTED;
     launch_pdl(k_plan<Args>, dim3((unsigned)(1 + blocks)), dim3(PLAN_THREADS), plan_bytes(a.U), st, a, nvec);
     return cudaGetLastError() != cudaSuccess ? RS3_ECUDA : RS3_OK;
@@ -890,7 +897,7 @@ rs3_status launch_plan(const Args &a, cudaStream_t st, rs3_dtype dtype)
 rs3_status rs3_readout_plan_two(const ReadoutMore &a, const ReadoutMore &b, rs3_dtype dtype, cudaStream_t st)
 {
     int64_t blocks;
-    const int64_t nvec = pass_pieces(b, dtype, blocks);
+    const int64_t nvec = pass_pieces(b, false, dtype, blocks);
     const size_t smem = plan_bytes(a.U > b.U ? a.U : b.U);
     if (rs3_kernel_smem((const void *)k_plan_two, smem) != RS3_OK) return RS3_EUNSUPPORTED;
     launch_pdl(k_plan_two, dim3((unsigned)(2 + blocks)), dim3(PLAN_THREADS), smem, st, a, b, nvec);
@@ -909,7 +916,7 @@ namespace {
 
 // merge of the split-KV partials and their scatter
 template <bool STRICT>
-rs3_status launch_merge(const ReadoutArgs &a, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
+rs3_status launch_merge(const typename std::conditional<STRICT, ReadoutMore, ReadoutArgs>::type &a, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
 {
     // one warp per (partial row, 64-column chunk; 32 for d < 64)
     const int ce = a.d >= 64 ? 2 : 1;
@@ -918,6 +925,8 @@ rs3_status launch_merge(const ReadoutArgs &a, int64_t max_combine, rs3_dtype dty
     const int64_t ccap = (int64_t)a.n_sm * 16;
     if (cblocks > ccap) cblocks = ccap;
     if (cblocks < 1) cblocks = 1;
+    if constexpr (STRICT)
+        if (a.kept) cblocks = std::max(cblocks, (int64_t)a.n_sm * 8);
     if (dtype == RS3_BF16) {
         if (ce == 2) launch_pdl(k_combine<uint16_t, 2, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);
         else launch_pdl(k_combine<uint16_t, 1, STRICT>, dim3((unsigned)cblocks), dim3(256), 0, st, a);

@@ -84,9 +84,46 @@ struct ReadoutMore : ReadoutArgs {
     // units that read units of a bank by number, and leave all results in partial slots
     const int32_t *bank_unit;   // [U] the bank's unit that unit u reads (-1: none); NULL: unit u
     GroupParts *parts;          // [group] its pieces (groups numbered as the plan does); NULL: whole groups are written out
+    // cells that are not kept are passed through (out = residual, or zeros) beside the attention and behind it, not by
+    // the plan's launch: a bit for each kept cell, 32 to a word, [U][words].  NULL: by the plan's launch
+    const uint32_t *kept;
+    int words;
     // changed scores (counts and cells that are out of range are skipped, not taken for others)
     ScoreArgs score;
 };
+
+// The pass-through of rows of bf16 by one warp, 32 cells of a unit at a time, until all are taken, or *done.
+__device__ __forceinline__ void pass_cells(const ReadoutMore &a, const volatile int *done)
+{
+    constexpr int F = 8;                                    // 16-byte pieces of a lane under way
+    const int lane = threadIdx.x & 31, n = a.U * a.words, vecs = a.D / 8;
+    const uint4 *res = static_cast<const uint4 *>(a.residual);
+    uint4 *out = static_cast<uint4 *>(a.out);
+    while (true) {
+        int c = n;
+        if (lane == 0 && !(done && *done)) c = atomicAdd(&a.header->passed, 1);
+        c = __shfl_sync(0xffffffffu, c, 0);
+        if (c >= n || c < 0) return;
+        const int u = c / a.words, cell0 = 32 * (c - u * a.words);
+        // (a unit that is skipped is passed through as a whole)
+        const uint32_t kept = __ldg(&a.ranges[u].cnt) > 0 ? __ldg(a.kept + c) : 0u;
+        const int total = min(32, a.mn - cell0) * vecs;
+        const int64_t at = ((int64_t)u * a.mn + cell0) * vecs;
+        for (int i0 = lane; i0 < total; i0 += 32 * F) {
+            uint4 v[F];
+            bool in[F];
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const int i = i0 + 32 * f;
+                in[f] = i < total && !(kept >> (i / vecs) & 1u);
+                v[f] = in[f] && res ? __ldcs(res + at + i) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+                if (in[f]) out[at + i0 + 32 * f] = v[f];
+        }
+    }
+}
 
 // What a kernel takes for a kind of scores.
 template <class X>

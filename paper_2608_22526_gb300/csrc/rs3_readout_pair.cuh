@@ -50,12 +50,14 @@ constexpr int BN = 128;             // keys per tile
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int NTHREADS = 384;
 
+constexpr int PASS_BUFS = 3, PASS_BYTES = 4096;
+
 template <int DH, class X>
 struct Cfg {
     static constexpr int KVBYTES = BN * DH * 2;              // one K (or V) stage
     static constexpr int QBYTES = BQ * DH * 2;               // one query tile
-    // (the slots of the biases take a stage or less)
-    static constexpr int BIAS_MOST = X::bias ? 9 * (BN * 4 + 16) : X::on ? 9 * 16 : 0;
+    // (the slots of the biases and the buffers behind them take a stage)
+    static constexpr int BIAS_MOST = X::on ? 9 * (BN * 4 + 16) : 0;
     static constexpr int NKV = (232448 - 1024 - 512 - BIAS_MOST - 2 * QBYTES) / KVBYTES;
     static constexpr int KSTK = (NKV + 1) / 2, KSTV = NKV / 2;
     using Ring = BiasRing<X, BN, KSTK, 1>;                   // an S needs the scores of the tile before read
@@ -77,7 +79,8 @@ struct Cfg {
     static constexpr int B_DRAIN = B_QFULL + 12, NBAR = B_QFULL + 13;
     static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
     static constexpr int OFF_BIAS = OFF_MISC + 16 + (NBAR & 1 ? 8 : 0);
-    static constexpr int SMEM = OFF_BIAS + Ring::BYTES + 1024;      // + alignment slack
+    static constexpr int OFF_PASS = OFF_BIAS + Ring::BYTES;  // what cells are passed through
+    static constexpr int SMEM = OFF_PASS + (X::on ? PASS_BUFS * (PASS_BYTES + 8) : 0) + 1024;      // + alignment slack
     static_assert(OFF_BIAS % 16 == 0, "biases are read 16 bytes at a time");
     static_assert(S_COL + 2 * BN <= TMEM_COLS && P_COL + P_STEP + BN / 2 <= TMEM_COLS, "TMEM budget");
     static_assert(KSTK >= 2 && KSTV >= 2 && SMEM <= 232448 && NBAR * 8 + 16 <= 512, "shared memory budget");
@@ -147,6 +150,73 @@ struct TileWalk {
     }
 };
 
+// The pass-through (pass_cells) by bulk copies, which a warp beside the softmax's can issue without taking their slots:
+// runs of cells that are not kept, mostly whole words, in pieces through the ring of buffers at `bufs`.  With the
+// same copies by the warp's own loads and stores the attention was 100 us longer (48 objects of 96 x 96 cells).
+__device__ __forceinline__ void pass_runs(const ReadoutMore &a, uint32_t bufs, int lane, const volatile int *done, volatile int *abort_flag,
+                                          uint64_t wait_ns)
+{
+    const uint32_t bars = bufs + PASS_BUFS * PASS_BYTES;
+    const int n = a.U * a.words;
+    const int64_t row = 2 * (int64_t)a.D;
+    const uint8_t *res = static_cast<const uint8_t *>(a.residual);
+    uint8_t *out = static_cast<uint8_t *>(a.out);
+    if (!res) {                                             // zeros from the first buffer
+        for (int i = lane; i < PASS_BYTES / 16; i += 32) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(bufs + 16u * i), "r"(0) : "memory");
+        fence_proxy_async();
+        __syncwarp();
+    }
+    if (lane != 0) return;
+    const auto put = [&](int64_t at, uint32_t bytes, uint32_t buf) {
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(out + at), "r"(bufs + buf * PASS_BYTES), "r"(bytes) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    };
+    uint32_t loaded = 0, stored = 0, last_bytes = 0;        // pieces; the last one that is loaded is not stored yet
+    int64_t last_at = 0;
+    bool ok = true;
+    const auto finish = [&]() {                             // the piece before
+        if (stored == loaded) return;
+        ok = mbar_wait(bars + 8u * (stored % PASS_BUFS), (stored / PASS_BUFS) & 1u, abort_flag, wait_ns);
+        if (!ok) return;
+        put(last_at, last_bytes, stored % PASS_BUFS);
+        ++stored;
+    };
+    while (ok && !*done) {
+        const int c = atomicAdd(&a.header->passed, 1);
+        if (c >= n || c < 0) break;
+        const int u = c / a.words, cell0 = 32 * (c - u * a.words), m = min(32, a.mn - cell0);
+        uint32_t left = ~(__ldg(&a.ranges[u].cnt) > 0 ? __ldg(a.kept + c) : 0u) & (m == 32 ? ~0u : (1u << m) - 1u);
+        while (left && ok) {
+            const int first = __ffs(left) - 1;
+            const uint32_t from = left >> first;
+            const int len = ~from ? __ffs(~from) - 1 : 32;  // (the bits above the word are zeros, so a run ends there)
+            left = first + len < 32 ? left & (~0u << (first + len)) : 0u;
+            int64_t at = ((int64_t)u * a.mn + cell0 + first) * row;
+            for (int64_t rest = len * row; rest > 0 && ok; rest -= PASS_BYTES, at += PASS_BYTES) {
+                const uint32_t bytes = (uint32_t)min(rest, (int64_t)PASS_BYTES);
+                if (!res) {
+                    put(at, bytes, 0);
+                    asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory");
+                    continue;
+                }
+                // its buffer's last piece has been stored: all but the latest one have
+                asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                const uint32_t b = loaded % PASS_BUFS, bar = bars + 8u * b;
+                mbar_expect_tx(bar, bytes);
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(bufs + b * PASS_BYTES), "l"(res + at), "r"(bytes), "r"(bar) : "memory");
+                finish();
+                ++loaded;
+                last_at = at;
+                last_bytes = bytes;
+            }
+        }
+    }
+    if (ok) finish();
+    for (; stored < loaded; ++stored) mbar_drain(bars + 8u * (stored % PASS_BUFS), (stored / PASS_BUFS) & 1u);
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
 // Items [it_begin, it_end) of the plan, in a CTA that is set up for the one-tile
 // kernel (set_up_tc): its tensor memory serves, its barriers make room.
 template <int DH, class X = PlainScores>
@@ -162,7 +232,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
     uint8_t *gbase = smem_raw + (base - raw);
     const uint32_t sQ = base + C::OFF_Q, sK = base + C::OFF_K, sV = base + C::OFF_V;
     const uint32_t bars = base + C::OFF_BAR;
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + C::OFF_MISC);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + C::OFF_MISC), *done_flag = abort_flag + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #define BAR(i) (bars + 8u * (uint32_t)(i))
 
@@ -186,6 +256,9 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
         }
         mbar_init(BAR(C::B_DRAIN), 2);
         *abort_flag = 0;
+        *done_flag = 0;
+        if (X::on)
+            for (int i = 0; i < PASS_BUFS; ++i) mbar_init(base + C::OFF_PASS + PASS_BUFS * PASS_BYTES + 8u * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async();
     }
@@ -381,6 +454,12 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 tc_commit(BAR(C::B_DRAIN));
                 mbar_drain(BAR(C::B_DRAIN), 0);
             }
+        } else if (X::on && warp == 3) {
+            // ------------------------------------------------------------------
+            // cells that are not kept, while the others work
+            // ------------------------------------------------------------------
+            if constexpr (X::on)
+                if (a.kept) pass_runs(a, base + C::OFF_PASS, lane, done_flag, abort_flag, wait_ns);
         }
     } else {
         // ----------------------------------------------------------------------
@@ -569,6 +648,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
             if (w.slot >= 0 && cell >= 0)
                 reinterpret_cast<float2 *>(a.part_ml)[(int64_t)w.slot * 2 * BQ + q * BQ + r] = make_float2(m_run, l_run);
         }
+        if (X::on && q == 0 && w4 == 0 && lane == 0) *done_flag = 1;
     }
 
     tc_fence_before();

@@ -32,8 +32,11 @@ struct FramesArgs {
     int4 *runs;                 // [tables][U][F + 4] storage rows of those and of the other regions: (first row, rows, first tile)
     int2 *tiles;                // [tables][U][tile_stride]
     int32_t *row_frame;         // [U][rows_per_unit], or NULL without biases
-    int tile_stride, U, tables;
+    int tile_stride, U, tables, row_ctas;
     int BN[2];                  // rows of a tile, of either table
+    const int32_t *idx, *count; // kept queries [U][k_max]
+    uint32_t *kept;             // [U][words] a bit for each of their cells, or NULL
+    int k_max, mn, words;
 };
 
 constexpr int FRAMES_THREADS = 256;
@@ -217,21 +220,37 @@ __device__ void unit_rows(const FramesArgs &f, int u, int warp, int warps)
     }
 }
 
+__device__ void unit_kept(const FramesArgs &f, int u)
+{
+    __shared__ uint32_t s_bits[RS3_MAX_MN / 32];
+    for (int w = threadIdx.x; w < f.words; w += FRAMES_THREADS) s_bits[w] = 0u;
+    __syncthreads();
+    const int n = f.count[u];
+    for (int j = threadIdx.x; j < n && n <= f.k_max; j += FRAMES_THREADS) {
+        const int cell = __ldg(f.idx + (int64_t)u * f.k_max + j);
+        if (cell >= 0 && cell < f.mn) atomicOr(&s_bits[cell >> 5], 1u << (cell & 31));
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < f.words; w += FRAMES_THREADS) f.kept[(int64_t)u * f.words + w] = s_bits[w];
+}
+
 __global__ void __launch_bounds__(FRAMES_THREADS) k_frames(const __grid_constant__ FramesArgs f)
 {
     pdl_wait();
     const int u = blockIdx.y;
     const int x = (int)blockIdx.x - f.tables;
     if (x < 0) unit_tiles(f, u, (int)blockIdx.x);
-    else unit_rows(f, u, x * (FRAMES_THREADS / 32) + ((int)threadIdx.x >> 5), ((int)gridDim.x - f.tables) * (FRAMES_THREADS / 32));
+    else if (x < f.row_ctas) unit_rows(f, u, x * (FRAMES_THREADS / 32) + ((int)threadIdx.x >> 5), f.row_ctas * (FRAMES_THREADS / 32));
+    else unit_kept(f, u);
 }
 
 // Byte offsets in the workspace.
 struct ScoredLayout {
     ReadoutPath path;
     ReadoutLayout l;
-    size_t stretch, runs, tiles, rows, ws, total;
+    size_t stretch, runs, tiles, rows, kept, ws, total;
     int64_t tile_stride;
+    int words;                  // of 32 cells
     int tables;                 // of key tiles: where a head's two kernels have tiles of different rows, two
 };
 
@@ -258,6 +277,9 @@ ScoredLayout scored_layout(const rs3_bank *bank, int k_max, const ReadoutPath &p
     off = align_up(off + n * L.tile_stride * 8, 256);
     L.rows = off;
     off = align_up(off + (size_t)U * bank->rows_per_unit * 4, 256);
+    L.kept = off;
+    L.words = (bank->mn + 31) / 32;
+    if (L.path.either) off = align_up(off + (size_t)U * L.words * 4, 256);
     L.ws = off;
     L.total = off + L.l.total;
     return L;
@@ -334,8 +356,21 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
             if (!(std::fabs(a.score.cap_poly[i]) > 1e-30f && std::fabs(a.score.cap_poly[i]) < 1e30f)) a.score.cap_half = -1.f;   // out of range: never
         }
     }
-    const int row_ctas = frame_bias ? std::min((F + COND_PIECES + 1 + 7) / 8, 32) : 0;
-    launch_pdl(k_frames, dim3((unsigned)(L.tables + row_ctas), (unsigned)bank->U), dim3(FRAMES_THREADS), 0, st, f);
+    // Out of place, calls of much work leave the cells that are not kept to a warp that the attention has to spare,
+    // and what that has not reached to the merge (48 objects of 96 x 96 cells, 453 MB: 1 137 us, 1 187 where the
+    // plan's launch passes them through)
+    if (L.path.either && residual != out && mn == bank->mn) {
+        f.kept = reinterpret_cast<uint32_t *>(ws + L.kept);
+        a.kept = f.kept;
+        a.words = L.words;
+    }
+    f.idx = idx;
+    f.count = count;
+    f.k_max = k_max;
+    f.mn = mn;
+    f.words = L.words;
+    f.row_ctas = frame_bias ? std::min((F + COND_PIECES + 1 + 7) / 8, 32) : 0;
+    launch_pdl(k_frames, dim3((unsigned)(L.tables + f.row_ctas + (f.kept ? 1 : 0)), (unsigned)bank->U), dim3(FRAMES_THREADS), 0, st, f);
     if (cudaGetLastError() != cudaSuccess) return RS3_ECUDA;
     return rs3_scored_launch(a, L.path, L.l.max_combine, dtype, st);
 }

@@ -442,6 +442,58 @@ def test_scored_readout_by_pairs_of_query_tiles(rs3, d, cap, bias, keep):
     scored_case(rs3, b, [2500, 1200, 129, 640], [0, 0, 0, 0], 1, cap, biases(b, bias), kp, "inplace")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("residual", ["none", "other"])
+@pytest.mark.parametrize("counts", [[2500, 1200, 129, 0], [70, 3, 0, 1], [0, 0, 0, 0], [4095, 4095, 4095, 4095]])
+def test_scored_readout_of_much_work_passes_the_other_cells_through(rs3, d, residual, counts):
+    """Out of place: cells that are not kept are the residual's bit for bit, or zeros, whichever kernel reaches them; the
+    grid's last word of cells is a part; few queries leave all of it to the merge."""
+    H, frames = 512 // d, 4 if d == 64 else 11
+    b = Built(rs3, U=4, H=H, d=d, dtype="bf16", m=63, n=65, window=-1, ring_frames=frames, commits=frames, n_ptr=3, seed=2, density=0.6)
+    spoil(b, None)
+    for _ in range(2):
+        scored_case(rs3, b, counts, [0, 0, 0, 0], 1, 6.0, biases(b, "age"), None, residual, k_max=4095)
+
+
+def test_scored_readout_of_much_work_passes_skipped_units_through(rs3):
+    """A unit whose group, count or frames are unsound, or whose cells are partly none, is the residual there."""
+    b = Built(rs3, U=4, H=8, d=64, dtype="bf16", m=63, n=65, window=-1, ring_frames=4, commits=4, n_ptr=3, seed=2, density=0.6)
+    spoil(b, None)
+    counts = [2500, 1200, 900, 640]
+    q, idx, count, group, _, clean, ws = scored_case(rs3, b, counts, [0] * 4, 1, 6.0, None, None, "none", k_max=4095)
+    res = torch.randn(clean.shape, generator=gen(3), device="cuda").bfloat16()
+    words = b.bank.meta.view(4, -1)
+    good = words.clone()
+    for what in ("group", "count", "tail", "frame", "cell"):
+        g, c, i = group.clone(), count.clone(), idx.clone()
+        if what == "group":
+            g[1] = 1
+        elif what == "count":
+            c[1] = 4096
+        elif what == "tail":
+            words[1, 1] = -5
+        elif what == "frame":
+            words[1, 16] += 1
+        else:
+            i[1, 3], i[1, 4] = -1, 4095
+        out = torch.full_like(clean, math.nan)
+        run_scored(rs3, b, q, 1, i, c, g, 6.0, None, None, None, 0.0, res, out, ws)
+        code = int(b.st)
+        b.st.zero_()
+        words.copy_(good)
+        assert code == (rs3.RS3_EINTERNAL if what in ("tail", "frame") else rs3.RS3_EINVAL), what
+        assert not out.isnan().any(), what
+        if what != "cell":
+            assert torch.equal(bits(out[1]), bits(res[1])), what
+        for u, n in enumerate(counts):
+            other = torch.ones(b.mn, dtype=torch.bool, device="cuda")
+            other[idx[u, :n].long()] = False
+            assert torch.equal(bits(out[u, other]), bits(res[u, other])), (what, u)
+        if what == "cell":
+            gone = idx[1, 3:5].long()
+            assert torch.equal(bits(out[1, gone]), bits(res[1, gone]))
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 256), ("f32", 32)])
 def test_scored_readout_of_scores_of_all_sizes(rs3, dtype, d):
     """Scores far beyond the cap and far below it, biases of thousands, references that move late."""
