@@ -25,6 +25,7 @@
 // the low bits a key load took four shared-memory passes instead of two, and
 // P stored twice per value in place of a move per value doubled its loads;
 // together 260 us.
+// Calls of few queries and keys, or of heads of 128, may take FEW rows per lane instead (rs3_has_few_rows).
 #pragma once
 
 #include "rs3_readout_common.cuh"

@@ -6,14 +6,15 @@
 // A frame that is left out costs nothing: its rows lie in no key tile.  Launches:
 //   k_frames       a CTA per unit: frames that are read and follow one another make runs of storage
 //                  rows (cut at the ring's end), the runs make a table of key tiles; with biases,
-//                  other CTAs write each row's frame beside it
+//                  other CTAs write each row's frame beside it; out of place, one more a bit per kept cell
 //   k_plan, k_readout_*, k_combine   the readout's, over the table
-// The kernels are the readout's own with a score's change compiled in.  Per tile, a softmax
-// warp's lanes have looked up their columns' biases three tiles ahead (tile, frame, bias, a turn
-// each).  V rows of a tile that belong to no live row are zeroed in shared memory, so that
-// nothing comes of what they hold.  Eight objects of one 64 x 64 grid (7 frames, heads of 256, 46 GFLOP):
-// 76 us capped and biased, 60 with neither (the plain readout 58); 174 000 of 302 000 rows of a video after
-// a cut: 127 us, 200 over all rows.
+// The kernels are the readout's own with a score's change compiled in.  The key producer's warp looks
+// the biases of a tile's rows up ahead (tile, frames, biases, a turn of its loop each) and leaves them beside K.
+// Scores that a cap of 55 or less bounds need no running maximum (RS3_BOUNDED): weights are taken against the largest bias
+// so far, the same for all rows, and cap and power are one pass.  V rows of a tile that belong to no
+// live row are zeroed in shared memory, so that nothing comes of what they hold.  Eight objects of one 64 x 64 grid
+// (7 frames, heads of 256, 46 GFLOP), in place: 68 us capped and biased, 65 capped, 66 biased, 59 with neither (the
+// plain readout 58); 174 000 of 302 000 rows of a video after a cut: 127 us, 200 over all rows.
 #include "rs3_readout_common.cuh"
 #include "rs3_bank.cuh"
 

@@ -1,7 +1,7 @@
 // rs3_scored_tc.cu -- the one-tile tensor-core readout (rs3_readout_tc.cuh) over scores that are
-// capped and biased by their row's frame.  A cap costs a score two instructions of the special-function
-// unit beside the softmax's one at most (change_scores), and the key producer's warp looks the
-// rows' biases up.
+// capped and biased by their row's frame.  A cap costs a score four fp32 operations beside the softmax's two
+// within half of it, else a power and a quarter of a reciprocal (change_scores), and the key producer's warp
+// looks the rows' biases up.
 #include "rs3_readout_tc.cuh"
 
 namespace tc {
