@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
 {
     pdl_wait();
     if constexpr (STRICT && sizeof(T) == 2)
-        if (a.kept) pass_cells(a, nullptr);
+        if (a.kept) pass_cells(a);
     constexpr int CW = 32 * E;                      // columns per warp
     const int d = a.d;
     // chunked tasks only when the groups are split more than four ways on

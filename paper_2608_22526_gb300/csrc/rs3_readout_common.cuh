@@ -92,8 +92,8 @@ struct ReadoutMore : ReadoutArgs {
     ScoreArgs score;
 };
 
-// The pass-through of rows of bf16 by one warp, 32 cells of a unit at a time, until all are taken, or *done.
-__device__ __forceinline__ void pass_cells(const ReadoutMore &a, const volatile int *done)
+// What is left of the pass-through of rows of bf16, by one warp, 32 cells of a unit at a time.
+__device__ __forceinline__ void pass_cells(const ReadoutMore &a)
 {
     constexpr int F = 8;                                    // 16-byte pieces of a lane under way
     const int lane = threadIdx.x & 31, n = a.U * a.words, vecs = a.D / 8;
@@ -101,7 +101,8 @@ __device__ __forceinline__ void pass_cells(const ReadoutMore &a, const volatile 
     uint4 *out = static_cast<uint4 *>(a.out);
     while (true) {
         int c = n;
-        if (lane == 0 && !(done && *done)) c = atomicAdd(&a.header->passed, 1);
+        // (mostly nothing is: thousands of warps would wait for one another's sums)
+        if (lane == 0 && __ldcg(&a.header->passed) < n) c = atomicAdd(&a.header->passed, 1);
         c = __shfl_sync(0xffffffffu, c, 0);
         if (c >= n || c < 0) return;
         const int u = c / a.words, cell0 = 32 * (c - u * a.words);
