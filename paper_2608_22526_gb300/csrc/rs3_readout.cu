@@ -26,7 +26,7 @@
 #include <initializer_list>
 #include <type_traits>
 
-#include "rs3_readout_common.cuh"
+#include "rs3_frames.cuh"
 
 namespace {
 
@@ -453,6 +453,24 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_plan(Args a, int64_t nvec)
     pdl_wait();
     if (blockIdx.x > 0) pass_through(a, nvec, blockIdx.x - 1, gridDim.x - 1);
     else plan_cta(a);
+}
+
+// The plan of one unit's readout over changed scores, after its frames' tables.
+__global__ void __launch_bounds__(PLAN_THREADS) k_plan_one(const __grid_constant__ ReadoutMore a, const __grid_constant__ frames::FramesArgs f,
+                                                           int64_t nvec)
+{
+    static_assert(PLAN_THREADS == frames::FRAMES_THREADS, "one launch for both");
+    pdl_wait();
+    const int x = (int)blockIdx.x - 1;
+    if (x >= f.rest_ctas) {
+        pass_through(a, nvec, x - f.rest_ctas, (int)gridDim.x - 1 - f.rest_ctas);
+    } else if (x >= 0) {
+        frames::unit_rest(f, 0, x);
+    } else {
+        for (int t = 0; t < f.tables; ++t) frames::unit_tiles(f, 0, t);
+        __syncthreads();                                   // the tables' lengths are read by other threads
+        plan_cta(a);
+    }
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS) k_plan_two(const __grid_constant__ ReadoutMore a, const __grid_constant__ ReadoutMore b,
@@ -939,9 +957,18 @@ rs3_status launch_merge(const typename std::conditional<STRICT, ReadoutMore, Rea
 
 }  // namespace
 
-rs3_status rs3_scored_launch(const ReadoutMore &a, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype, cudaStream_t st)
+rs3_status rs3_scored_launch(const ReadoutMore &a, const frames::FramesArgs *one, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype,
+                             cudaStream_t st)
 {
-    rs3_status s = launch_plan(a, st, dtype);
+    rs3_status s = RS3_OK;
+    if (one) {
+        int64_t blocks;
+        const int64_t nvec = pass_pieces(a, a.kept != nullptr, dtype, blocks);
+        launch_pdl(k_plan_one, dim3((unsigned)(1 + one->rest_ctas + blocks)), dim3(PLAN_THREADS), plan_bytes(1), st, a, *one, nvec);
+        if (cudaGetLastError() != cudaSuccess) s = RS3_ECUDA;
+    } else {
+        s = launch_plan(a, st, dtype);
+    }
     if (s != RS3_OK) return s;
     s = p.either ? rs3_launch_scored_either(a, st) : p.kind == 1 ? rs3_launch_scored_tc(a, st) : rs3_launch_scored_simt(a, dtype, st);
     return s != RS3_OK ? s : launch_merge<true>(a, max_combine, dtype, st);

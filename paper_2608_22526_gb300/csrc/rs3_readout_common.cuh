@@ -178,8 +178,9 @@ rs3_status rs3_readout_run_launch(const ReadoutArgs &a, const ReadoutPath &p, rs
 rs3_status rs3_launch_scored_either(const ReadoutMore &a, cudaStream_t st);
 rs3_status rs3_launch_scored_tc(const ReadoutMore &a, cudaStream_t st);
 rs3_status rs3_launch_scored_simt(const ReadoutMore &a, rs3_dtype dtype, cudaStream_t st);
-// A readout over changed scores.
-rs3_status rs3_scored_launch(const ReadoutMore &a, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype, cudaStream_t st);
+// A readout over changed scores; `one`: of a single unit, whose frames are still to be gone through.
+namespace frames { struct FramesArgs; }
+rs3_status rs3_scored_launch(const ReadoutMore &a, const frames::FramesArgs *one, const ReadoutPath &p, int64_t max_combine, rs3_dtype dtype, cudaStream_t st);
 // Two plans in one launch, with the second's pass-through.
 rs3_status rs3_readout_plan_two(const ReadoutMore &first, const ReadoutMore &second, rs3_dtype dtype, cudaStream_t st);
 // phases of a readout: the attention over the bank (pass-through, plan,
