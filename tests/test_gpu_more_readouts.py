@@ -442,6 +442,38 @@ def test_scored_readout_by_pairs_of_query_tiles(rs3, d, cap, bias, keep):
     scored_case(rs3, b, [2500, 1200, 129, 640], [0, 0, 0, 0], 1, cap, biases(b, bias), kp, "inplace")
 
 
+@pytest.mark.parametrize("dtype,H,d", SHAPES)
+@pytest.mark.parametrize("cap,bias,keep,residual", [(0.0, None, "some", "none"), (5.0, "age", "all", "inplace"), (0.0, "unit", "alternate", "other"),
+                                                    (30.0, "holes", "nothing", "none")])
+def test_scored_readout_of_one_unit(rs3, dtype, H, d, cap, bias, keep, residual):
+    for layout in LAYOUTS:
+        b = Built(rs3, U=1, H=H, d=d, dtype=dtype, m=8, n=9, seed=2, **layout)
+        kp = keeps(b, keep)
+        spoil(b, kp)
+        scored_case(rs3, b, [33], [1], 2, cap, biases(b, bias), kp, residual)
+        scored_case(rs3, b, [0], [0], 1, cap, biases(b, bias), kp, residual, k_max=5)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("residual", ["inplace", "other"])
+def test_scored_readout_of_one_unit_of_much_work(rs3, d, residual):
+    """Two tables of key tiles, two query tiles per CTA, hundreds of frames."""
+    b = Built(rs3, U=1, H=1024 // d, d=d, dtype="bf16", m=63, n=65, window=-1, ring_frames=300, commits=290, n_ptr=3, seed=2, density=0.1,
+              ring=126000)
+    kp = keeps(b, "some")
+    spoil(b, kp)
+    scored_case(rs3, b, [3000], [0], 1, 10.0, biases(b, "unit"), kp, residual)
+    words, good = b.bank.meta, b.bank.meta.clone()
+    q, idx, count, group, _, out, ws = scored_case(rs3, b, [300], [0], 1, 10.0, None, kp, "none", k_max=3000)
+    for word, value in ((16 + 100, int(words[16 + 100]) + 1), (3, 301), (1, -5)):
+        words[word] = value
+        again = torch.full_like(out, 5.0)
+        run_scored(rs3, b, q, 1, idx, count, group, 10.0, None, kp, None, 0.0, again, again, ws)
+        words.copy_(good)
+        assert int(b.st) == rs3.RS3_EINTERNAL and (again == 5).all()
+        b.st.zero_()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("residual", ["none", "other"])
 @pytest.mark.parametrize("counts", [[2500, 1200, 129, 0], [70, 3, 0, 1], [0, 0, 0, 0], [4095, 4095, 4095, 4095]])
