@@ -506,10 +506,12 @@ size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const rs3_bank *
  *   prefix       a bank of the same H, d, dtype and mn; it may be `bank` itself
  *   prefix_unit  device int32 [U], in [-1, prefix->U); -1: no prefix
  * Arguments and results otherwise as rs3_memory_readout; idx holds distinct cells (twice
- * the same one is fine out of place).  A cell outside [0, mn) latches RS3_EINVAL and is skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit
- * out of range latches it and the unit is skipped, and so is one whose counters or whose
- * prefix's are unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.
- *   workspace    device, >= rs3_shared_readout_workspace_bytes(...), 16-byte aligned; one call at a time
+ * the same one is fine out of place).  A cell outside [0, mn) latches RS3_EINVAL and is
+ * skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit out of range
+ * latches it and the unit is skipped, and so is one whose counters or whose prefix's are
+ * unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.
+ *   workspace    device, >= rs3_shared_readout_workspace_bytes(...) bytes, 16-byte aligned;
+ *                one call at a time
  * Limits: those of rs3_memory_readout, for both banks.
  */
 rs3_status rs3_shared_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
