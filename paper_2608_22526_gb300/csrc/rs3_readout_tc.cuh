@@ -749,6 +749,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                             o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
                         tmem_st16(ta, o);
                     }
+                    tmem_wait_st();                                    // (another warp's P V adds to them after PFULL)
                 }
                 return there;
             };
