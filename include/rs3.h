@@ -482,9 +482,9 @@ size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max);
  *               aligned; one call at a time
  * In bf16 the softmax's weights are rounded to bf16, and so are queries rotated here.
  * Limits: those of rs3_memory_readout; U * rows_per_unit < 2^31.  In bf16 with a cap of 55 or less,
- * weights are e^s as they are (but for the biases), so a head's rows times their largest value times
- * e^cap stay below 3e38 (a million rows: values up to 4e8 at a cap of 55, 7e23 at 20), and what is
- * below 1e-38 e^cap in a value may be lost.
+ * weights are e^s against the largest bias so far, or one that is up to 5.5 lower, so a head's rows times
+ * their largest value times e^cap stay below 1e36 (a million rows: values up to 1e6 at a cap of 55, 2e21 at
+ * 20), and what is below 1e-38 e^cap in a value may be lost.
  */
 rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d,
                               const int32_t *unit_group, const int32_t *idx, const int32_t *count,

@@ -6,8 +6,8 @@
 
 #define RS3_MAX_UNITS 4096  // units per readout call
 #define RS3_PAIR_ITEMS (1 << 30)   // above every item index
-// Scores in the log2 domain whose weights 2^s can be summed as they are: 2^80, a million of them and values up to 2^26 stay
-// within fp32's (and bf16's) 2^127, and 2^-80 leaves 2^-46 to values.
+// Scores in the log2 domain whose weights 2^s can be summed as they are: 2^80, the 2^8 that biases may rise by before the
+// reference follows, a million of them and values up to 2^18 stay within fp32's (and bf16's) 2^127, and 2^-80 leaves 2^-46 to values.
 #define RS3_BOUNDED 80.f
 
 struct GroupParts {         // a group's n pieces: 0 is in slot0, s >= 1 in slot 2 (slice + s); whose they are

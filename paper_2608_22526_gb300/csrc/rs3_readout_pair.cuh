@@ -470,7 +470,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
         const uint32_t tl = tmem + ((uint32_t)(32 * w4) << 16);       // this warp's TMEM lanes
         const uint32_t scol = tl + C::S_COL + (uint32_t)(BN * q), pcol = tl + C::P_COL + C::P_STEP * q;
         const uint32_t ocol = tl + C::O_COL + (uint32_t)(DH * q);
-        constexpr bool changed = X::cap || X::bias;
+        constexpr bool changed = X::cap || X::bias, lifted = X::cap && X::bias;
         const bool bounded = X::cap && bounded_scores(a);
         uint32_t tq = 0, passed = 0;                                   // tiles of this query tile; of all items so far
         int q_loaded = -1;                                             // item whose query rows are in shared memory
@@ -550,7 +550,9 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                     m_run = mt;
                 } else if (__any_sync(0xffffffffu, mt > m_run + 8.0f)) {
                     // (a row whose scores so far are all -inf has no reference yet: their weights are 0)
-                    const float m_new = fmaxf(m_run, mt), alpha = X::bias && m_new == -INFINITY ? 1.f : ex2_approx(m_run - m_new);
+                    const float m_new = fmaxf(m_run, mt);
+                    // (with a cap and biases in two steps, bounded or not)
+                    const float alpha = X::bias && m_new == -INFINITY ? 1.f : lifted ? half_way(m_run, m_new) : ex2_approx(m_run - m_new);
                     ok = mbar_wait_warp(BAR(C::B_PVDONE + q), (tj - 1u) & 1u, abort_flag, wait_ns);
                     if (!ok) break;
                     tc_fence_after();
@@ -560,10 +562,11 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                         tmem_ld16(ocol + (uint32_t)c, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                        for (int e = 0; e < 16; ++e)
+                            o[e] = __float_as_uint(lifted ? __uint_as_float(o[e]) * alpha * alpha : __uint_as_float(o[e]) * alpha);
                         tmem_st16(ocol + (uint32_t)c, o);
                     }
-                    l_run *= alpha;
+                    l_run = lifted ? l_run * alpha * alpha : l_run * alpha;
                     m_run = m_new;
                 }
                 const float ref = X::bias ? (m_run == -INFINITY ? 0.f : m_run) - off : m_run;
@@ -598,7 +601,10 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 tc_fence_after();
             }
             tq += (uint32_t)n;
-            const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+            // what the sums are multiplied by: whole rows by 1 / l, pieces of bounded scores by a power of two
+            float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+            if constexpr (lifted)
+                if (w.slot >= 0) inv = bounded ? piece_step(m_run, l_run) : 1.f;
             const int64_t ooff = ((int64_t)w.u * a.mn + cell) * a.D + w.h * DH;
             float *po = a.part_o + ((int64_t)w.slot * 2 * BQ + q * BQ + r) * DH;
 #pragma unroll 1
@@ -626,6 +632,10 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 }
                 if (cell < 0) continue;
                 if (w.slot >= 0) {                                     // split-KV partial (fp32, unnormalised)
+                    if constexpr (lifted) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+                    }
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         __stcg(reinterpret_cast<float4 *>(po + c0) + k,

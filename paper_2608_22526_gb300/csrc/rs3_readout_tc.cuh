@@ -474,6 +474,23 @@ struct RowsAhead {
 __device__ __forceinline__ bool bounded_scores(const ReadoutArgs &) { return false; }
 __device__ __forceinline__ bool bounded_scores(const ReadoutMore &a) { return a.score.bounded != 0; }
 
+// What bounded scores are summed against is the largest bias, not the largest score: sums against a low bias may weigh more
+// than those against one that is 2^160 higher.  So (1) sums follow a reference in two steps, each the square root of the
+// factor, which alone may be below what fp32 holds;
+__device__ __forceinline__ float half_way(float from, float to) { return ex2_approx(0.5f * (from - to)); }
+
+// (2) a piece of a row is left with its l in [1, 2), for the merge goes by m alone: returns the power of two
+// that its sums take (1 where l is none: no weight, or no number).
+__device__ __forceinline__ float piece_step(float &m, float &l)
+{
+    if (!(l > 0.f && l < INFINITY)) return 1.f;
+    const int e = min((__float_as_int(l) >> 23) - 127, 126);
+    const float step = __int_as_float((127 - e) << 23);
+    m += (float)e;
+    l *= step;
+    return step;
+}
+
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
 template <int DH, class X = PlainScores>
 __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a, const CUtensorMap &tmk, const CUtensorMap &tmv,
@@ -730,8 +747,9 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
             // Scores that a cap bounds need no reference but their biases' (the same for all rows), so the slices
             // have nothing to agree on before the item's end; a slice whose wait ran out goes there idle.
             const bool bounded = X::cap && bounded_scores(a);
+            constexpr bool lifted = X::cap && X::bias;
             bool alive = true;
-            const auto rescale = [&](uint32_t tp, float alpha) {
+            const auto rescale = [&](uint32_t tp, float alpha) {      // with a cap and biases by alpha twice
                 // O must hold tile j-1 before its rows are rescaled; on
                 // a timeout the rescale is skipped and the next tile's
                 // barrier takes every slice out
@@ -746,7 +764,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                         tmem_wait_ld();
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
-                            o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                            o[e] = __float_as_uint(lifted ? __uint_as_float(o[e]) * alpha * alpha : __uint_as_float(o[e]) * alpha);
                         tmem_st16(ta, o);
                     }
                     tmem_wait_st();                                    // (another warp's P V adds to them after PFULL)
@@ -811,9 +829,9 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                         m_new = top;
                     } else if (top > m_run + 8.0f) {
                         m_new = top;
-                        const float alpha = ex2_approx(m_run - m_new);
+                        const float alpha = half_way(m_run, m_new);      // (without biases it never comes here)
                         alive = rescale(tj - 1u, alpha);
-                        l_part *= alpha;
+                        l_part = l_part * alpha * alpha;
                     }
                     rowsum = weights<X>(fused, sr, pk, a, sc, against(m_new));
                 } else if (j == 0) {
@@ -849,9 +867,9 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                             rowsum = row_exp(sr, pk, sc, against(m_new));
                         }
                         const bool grow = m_new != m_run;
-                        const float alpha = grow ? ex2_approx(m_run - m_new) : 1.0f;
+                        const float alpha = grow ? (lifted ? half_way(m_run, m_new) : ex2_approx(m_run - m_new)) : 1.0f;
                         if (__any_sync(0xffffffffu, grow)) rescale(tj - 1u, alpha);
-                        l_part *= alpha;
+                        l_part = lifted ? l_part * alpha * alpha : l_part * alpha;
                     }
                 }
                 l_part += rowsum;
@@ -891,7 +909,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 for (int q = 0; q < NSPLIT; ++q) l_run += redl[q * BM + r];
             }
             tcnt += (uint32_t)n;
-            const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+            float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
             if (w.slot >= 0) {
                 // split-KV partial (fp32, unnormalised): 32 columns at a time are
                 // staged through shared memory so that each store instruction
@@ -899,6 +917,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 // warp's part of the P ring, idle from the item's last PV (waited
                 // for above) until the next item's first P, which no warp writes
                 // before every warp has passed this epilogue (QFULL).
+                if constexpr (lifted) inv = bounded ? piece_step(m_run, l_run) : 1.f;
                 float *stg = reinterpret_cast<float *>(gbase + C::OFF_P) + (warp - 4) * (32 * 36);
                 float *pdst = a.part_o + ((int64_t)w.slot * BM + 32 * q4) * DH + h * OCOLS;
 #pragma unroll 1
@@ -910,6 +929,10 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+                    if constexpr (lifted) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
                     }
                     __syncwarp();
 #pragma unroll
