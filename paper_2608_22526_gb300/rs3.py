@@ -624,13 +624,24 @@ def rope_spec(rot: int, pairs=None, layout: str = "pairs", base: float = 10000.0
     return s
 
 
+def _positions(dev: int, name: str, pos, axes: int, rows: Optional[int] = None) -> int:
+    """The pointer of positions int32 [..., axes], as many as `rows` where that is known.  With one axis its extent may be
+    left out, of a list where rows is not known."""
+    at = _arg(dev, name, pos, torch.int32, 0)
+    if pos.shape[-1:] != (axes,) and not (axes == 1 and (pos.dim() == 1 or rows is not None)):
+        raise ValueError(f"{name}: int32 [rows, {axes}] wanted, got {tuple(pos.shape)}")
+    if rows is not None and pos.numel() != rows * axes:
+        raise ValueError(f"{name}: {rows} positions of {axes} wanted, got {tuple(pos.shape)}")
+    return at
+
+
 def rs3_rope_table(pos, spec: RopeSpec, cos_sin, stream=None):
     """(cos, sin) of every pair at the positions pos int32 [rows, axes]: fp32 [rows, rot/2, 2]."""
     dev = torch.cuda.current_device()
-    _want(dev, "pos", pos, torch.int32, 0)
+    at = _positions(dev, "pos", pos, spec.axes)
     rows = pos.numel() // spec.axes
     _want(dev, "cos_sin", cos_sin, torch.float32, rows * spec.rot)
-    _check(lib.rs3_rope_table(_ptr(pos), rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
+    _check(lib.rs3_rope_table(at, rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
 
 
 def _rope_side(dev: int, name: str, x, y, dt, H: int, d: int, pos, axes: int, keep):
@@ -642,7 +653,7 @@ def _rope_side(dev: int, name: str, x, y, dt, H: int, d: int, pos, axes: int, ke
     rows_out, out_stride, y_ptr = _rows_arg(dev, name + "_out", y, dt, width)
     if rows != rows_out:
         raise ValueError(f"{name}_out has {rows_out} rows, {name} {rows}")
-    return (x_ptr, rows, stride, H, _arg(dev, name + "_pos", pos, torch.int32, rows * axes),
+    return (x_ptr, rows, stride, H, _positions(dev, name + "_pos", pos, axes, rows),
             None if keep is None else _arg(dev, name + "_keep", keep, torch.uint8, rows), y_ptr, out_stride)
 
 
