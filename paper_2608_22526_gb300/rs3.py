@@ -624,24 +624,25 @@ def rope_spec(rot: int, pairs=None, layout: str = "pairs", base: float = 10000.0
     return s
 
 
-def _positions(dev: int, name: str, pos, axes: int, rows: Optional[int] = None) -> int:
-    """The pointer of positions int32 [..., axes], as many as `rows` where that is known.  With one axis its extent may be
-    left out, of a list where rows is not known."""
-    at = _arg(dev, name, pos, torch.int32, 0)
-    if pos.shape[-1:] != (axes,) and not (axes == 1 and (pos.dim() == 1 or rows is not None)):
-        raise ValueError(f"{name}: int32 [rows, {axes}] wanted, got {tuple(pos.shape)}")
-    if rows is not None and pos.numel() != rows * axes:
-        raise ValueError(f"{name}: {rows} positions of {axes} wanted, got {tuple(pos.shape)}")
-    return at
+def _positions(dev: int, name: str, pos, axes: int, rows: int) -> int:
+    """The pointer of positions int32 [..., axes] of so many rows; with one axis its extent may be left out."""
+    if (pos is None or pos.dtype is not torch.int32 or pos.numel() != rows * axes or (axes != 1 and pos.size(-1) != axes)
+            or pos.get_device() != dev or not pos.is_contiguous()):
+        _want(dev, name, pos, torch.int32, 0)
+        _ptr(pos)
+        raise ValueError(f"{name}: int32 [{rows}, {axes}] wanted, got {tuple(pos.shape)}")
+    return pos.data_ptr()
 
 
 def rs3_rope_table(pos, spec: RopeSpec, cos_sin, stream=None):
     """(cos, sin) of every pair at the positions pos int32 [rows, axes]: fp32 [rows, rot/2, 2]."""
     dev = torch.cuda.current_device()
-    at = _positions(dev, "pos", pos, spec.axes)
+    _want(dev, "pos", pos, torch.int32, 0)
+    if pos.shape[-1:] != (spec.axes,) and not (spec.axes == 1 and pos.dim() == 1):
+        raise ValueError(f"pos: int32 [rows, {spec.axes}] wanted, got {tuple(pos.shape)}")
     rows = pos.numel() // spec.axes
     _want(dev, "cos_sin", cos_sin, torch.float32, rows * spec.rot)
-    _check(lib.rs3_rope_table(at, rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
+    _check(lib.rs3_rope_table(_ptr(pos), rows, ctypes.byref(spec), _ptr(cos_sin), _stream(stream)), "rs3_rope_table")
 
 
 def _rope_side(dev: int, name: str, x, y, dt, H: int, d: int, pos, axes: int, keep):
