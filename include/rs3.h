@@ -681,11 +681,11 @@ typedef struct {
     int32_t axes;           /* coordinates of a position, 1 to 3 */
     int32_t pairs[3];       /* pairs of each; they add up to rot / 2 */
     int32_t inverse;        /* 1: turned back (the transpose, a turned row's gradient) */
-    float magnitude;        /* factor of the turned elements */
+    float magnitude;        /* factor of the turned elements, |magnitude| < 1e30 */
     double base;            /* 1 <= base <= 1e12 */
-    double factor;          /* >= 1 */
-    double context;         /* >= 0 */
-    double beta_fast, beta_slow;   /* 0 <= slow < fast, where context > 0 */
+    double factor;          /* 1 <= factor <= 1e9 */
+    double context;         /* 0 <= context <= 1e12 */
+    double beta_fast, beta_slow;   /* 0 <= slow < fast <= 1e12, where context > 0 */
 } rs3_rope_spec;
 
 /* Fills layout pairs, rot 0, one axis, base 10000, factor 1, context 0, beta 32 / 1,
@@ -698,7 +698,7 @@ void rs3_default_rope_spec(rs3_rope_spec *spec);
  * (there rot = d, and pairs are (2p, 2p+1)).
  *   pos     device int32 [rows][axes], any whole numbers
  *   cos_sin device fp32 [rows][rot/2][2], 16-byte aligned
- * Angles are counted in whole numbers of turns: their error is |pos| f 2^-53, 2^-31 turns and a few
+ * Angles are counted in whole numbers of turns: at any position they are within 2^-30 turns and a few
  * roundings of fp32.
  */
 rs3_status rs3_rope_table(const int32_t *pos, int64_t rows, const rs3_rope_spec *spec,

@@ -4,8 +4,10 @@
 // Pair p of an axis with n pairs turns by pos * f_p, f_p = base^(-p/n), stretched for positions
 // beyond those trained on.  An angle of a far position loses its fraction in fp32, and fp64 is slow
 // here, so angles are counted in turns in whole numbers: with F_p = f_p / (2 pi) as a fraction of 2^64,
-// pos * F_p mod 2^64 is the angle's fraction of a turn (F_p's own error of 2^-53 relative, times pos, is
-// all there is), of which the upper 32 bits are found, to 2^-31 of a turn.  Its nearest quarter turn is
+// pos * F_p mod 2^64 is the angle's fraction of a turn, of which the upper 32 bits are found.  The host has f_p in pairs of
+// doubles (100 bits; in one, the ramp of a stretch alone can cost a dozen of the 53), so F_p is off by its rounding, 2^-65,
+// the lower bit that turn_of drops and what it cuts off are 2^-64 and 2^-31: |pos| (2^-65 + 2^-64) + 2^-31 is
+// below 2^-30 of a turn.  Its nearest quarter turn is
 // taken off in whole numbers too (what is left are the low 30 bits, with their sign), and that, |t| <= pi
 // / 4, goes through the Taylor series of sine and cosine: up to t^11 and t^10, whose next terms are below
 // 1e-11 and 2e-10 there.
@@ -310,6 +312,56 @@ __global__ void __launch_bounds__(256) k_rope_table(const int32_t *pos, int64_t 
     }
 }
 
+// A number as the sum of two doubles, the second at most half a last place of the first: some 100 bits.  Sums and products by
+// the error-free transformations of Knuth and Dekker (the product's with a fused multiply-add).
+struct Two {
+    double hi, lo;
+};
+
+Two two_sum(double a, double b)
+{
+    const double s = a + b, v = s - a;
+    return {s, (a - (s - v)) + (b - v)};
+}
+
+Two operator+(Two a, Two b)
+{
+    const Two s = two_sum(a.hi, b.hi);
+    return two_sum(s.hi, s.lo + (a.lo + b.lo));
+}
+
+Two operator-(Two a, Two b) { return a + Two{-b.hi, -b.lo}; }
+
+Two operator*(Two a, Two b)
+{
+    const double p = a.hi * b.hi, e = std::fma(a.hi, b.hi, -p);
+    return two_sum(p, e + (a.hi * b.lo + a.lo * b.hi));
+}
+
+Two operator/(Two a, Two b)
+{
+    const double q = a.hi / b.hi;
+    const Two r = a - b * Two{q, 0.0};
+    const double c = r.hi / b.hi;
+    return two_sum(q, c) + Two{(r - b * Two{c, 0.0}).hi / b.hi, 0.0};
+}
+
+Two power(Two x, int n)
+{
+    Two y = {1.0, 0.0};
+    for (; n > 0; n >>= 1, x = x * x)
+        if (n & 1) y = y * x;
+    return y;
+}
+
+// base^(-1/n): a step of Newton's iteration from the value in one double, whose error of 2^-52 or so it squares.
+Two root_of(double base, int n)
+{
+    const double r = std::pow(base, -1.0 / n);
+    const Two off = power({r, 0.0}, n) * Two{base, 0.0} - Two{1.0, 0.0};
+    return two_sum(r, -r * off.hi / n);
+}
+
 // The pairs' turns; false when the description is not what the header asks for.
 bool rope_turns(const rs3_rope_spec *s, RopeTurns &t)
 {
@@ -325,21 +377,29 @@ bool rope_turns(const rs3_rope_spec *s, RopeTurns &t)
     }
     if (sum != s->rot / 2) return false;
     if (s->rot > 2 * ROPE_PAIRS) return true;              // (the caller tells that it is not supported)
-    const double two_pi = 6.283185307179586476925;
+    const Two per_turn = {0x1.45f306dc9c883p-3, -0x1.6b01ec5417056p-57};       // 1 / (2 pi)
+    const Two one = {1.0, 0.0}, slow = {s->beta_slow, 0.0}, part = one / Two{s->factor, 0.0};
+    const Two slope = s->context > 0.0 ? one / two_sum(s->beta_fast, -s->beta_slow) : one;
     int p = 0;
-    for (int a = 0; a < s->axes; ++a)
-        for (int i = 0; i < s->pairs[a]; ++i, ++p) {
-            double f = std::pow(s->base, -(double)i / (double)s->pairs[a]);
-            double share = 0.0;                            // of the frequency as trained
+    for (int a = 0; a < s->axes; ++a) {
+        const Two step = s->pairs[a] > 1 ? root_of(s->base, s->pairs[a]) : one;
+        Two f = per_turn;                                  // pair i: base^(-i/n) / (2 pi)
+        for (int i = 0; i < s->pairs[a]; ++i, ++p, f = f * step) {
+            Two turn = f * part;
             if (s->context > 0.0) {
-                share = (s->context * f / two_pi - s->beta_slow) / (s->beta_fast - s->beta_slow);
-                share = share < 0.0 ? 0.0 : share > 1.0 ? 1.0 : share;
+                Two share = (f * Two{s->context, 0.0} - slow) * slope;          // of the frequency as trained
+                if (share.hi >= 1.0) share = one;
+                if (share.hi > 0.0) turn = f * share + turn * (one - share);
             }
-            f *= share + (1.0 - share) / s->factor;
-            t.f[p] = (uint64_t)std::ldexp(f / two_pi, 64);
+            // (below 2^62, and what lies behind its whole number within some hundreds)
+            const double hi = turn.hi * 0x1p64;
+            const int64_t whole = (int64_t)hi;
+            const double rest = turn.lo * 0x1p64 + (hi - (double)whole);
+            t.f[p] = (uint64_t)(whole + (int64_t)(rest < 0.0 ? rest - 0.5 : rest + 0.5));
             if (s->inverse) t.f[p] = 0 - t.f[p];
             t.axis[p] = (uint8_t)a;
         }
+    }
     t.half = s->rot / 2;
     t.axes = s->axes;
     t.magnitude = s->magnitude;
