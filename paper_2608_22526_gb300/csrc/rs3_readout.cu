@@ -760,7 +760,7 @@ ReadoutPath rs3_few_rows(ReadoutPath p, int d)
 bool rs3_has_few_rows(const ReadoutPath &p, int U, int H, int d, int k_max, int64_t bank_rows)
 {
     if (p.kind != 0) return false;
-    return d == 128 || (double)U * H * ((k_max + p.BM - 1) / p.BM) * ((double)bank_rows / p.BN + 1.0) < 16.0 * p.grid;
+    return rs3_always_few_rows(d) || (double)U * H * ((k_max + p.BM - 1) / p.BM) * ((double)bank_rows / p.BN + 1.0) < 16.0 * p.grid;
 }
 
 // What the preferred path of this call needs, and no less than a call of fewer

@@ -147,9 +147,11 @@ struct ReadoutPath {
 // the path of a call over banks of this many rows with this workspace (INT64_MAX and
 // SIZE_MAX: the path that any workspace is sized for)
 ReadoutPath choose_readout_path(rs3_dtype dtype, int d, int U, int H, int k_max, int64_t bank_rows, size_t workspace_bytes);
-// The CUDA-core path `p` with fewer query rows to a CTA, and whether a call has too few of them for `p`.
+// The CUDA-core path `p` with fewer query rows to a CTA, and whether a call has too few of them for `p`; heads whose calls
+// always have.
 ReadoutPath rs3_few_rows(ReadoutPath p, int d);
 bool rs3_has_few_rows(const ReadoutPath &p, int U, int H, int d, int k_max, int64_t bank_rows);
+constexpr bool rs3_always_few_rows(int d) { return d == 128; }
 bool rs3_tc_supported(int d);
 int rs3_tc_block_n(int d);
 rs3_status rs3_launch_tc_readout(const ReadoutArgs &a, cudaStream_t st);

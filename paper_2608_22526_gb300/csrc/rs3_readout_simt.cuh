@@ -465,7 +465,8 @@ rs3_status launch_rows(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
 template <typename T, int D, class X>
 rs3_status launch(const typename ReadoutOf<X>::Args &a, cudaStream_t st)
 {
-    return a.BM == Cfg<D, FEW>::BM ? launch_rows<T, D, X, FEW>(a, st) : launch_rows<T, D, X, 0>(a, st);
+    if constexpr (X::on && rs3_always_few_rows(D)) return launch_rows<T, D, X, FEW>(a, st);
+    else return a.BM == Cfg<D, FEW>::BM ? launch_rows<T, D, X, FEW>(a, st) : launch_rows<T, D, X, 0>(a, st);
 }
 
 }  // namespace

@@ -80,8 +80,8 @@ extern "C" size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k
 {
     if (!bank || bank->magic != RS3_BANK_MAGIC || k_max < 0) return 0;
     const ReadoutPath p = scored_path(bank, k_max);        // (a call of fewer queries may take the other one)
-    const size_t n = scored_layout(bank, k_max, p).total;
-    return p.kind == 0 ? std::max(n, scored_layout(bank, k_max, rs3_few_rows(p, bank->d)).total) : n;
+    const size_t few = p.kind == 0 ? scored_layout(bank, k_max, rs3_few_rows(p, bank->d)).total : 0;
+    return few && rs3_always_few_rows(bank->d) ? few : std::max(few, scored_layout(bank, k_max, p).total);
 }
 
 extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, int mn, int H, int d, const int32_t *unit_group,

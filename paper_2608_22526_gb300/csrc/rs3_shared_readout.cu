@@ -374,7 +374,7 @@ extern "C" size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const
 {
     if (!bank_known(bank) || !bank_known(prefix) || k_max < 0) return 0;
     // (each part's is the larger of both paths': a call of fewer queries may take the other one)
-    const ShareLayout a = share_layout(bank, prefix, k_max, 0), b = share_layout(bank, prefix, k_max, 1);
+    const ShareLayout a = share_layout(bank, prefix, k_max, rs3_always_few_rows(bank->d)), b = share_layout(bank, prefix, k_max, 1);
     return a.own_ws + align_up(std::max(a.own_l.total, b.own_l.total), 256) + std::max(a.pre_l.total, b.pre_l.total);
 }
 
