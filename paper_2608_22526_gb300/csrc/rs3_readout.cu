@@ -502,6 +502,13 @@ __device__ __forceinline__ void store_out1(const uint16_t *res, uint16_t *out, i
     out[off] = float_to_bf16_bits((res ? bf16_bits_to_float(res[off]) : 0.f) + o);
 }
 
+// A piece whose scores were summed against its largest score (or one up to 2^8 lower) weighs about 2^m.  One whose bounded
+// scores were summed against its largest bias (`lifted`) weighs 2^m l, with l anywhere within 2^+-108, so M is the largest
+// of m + log2 l there, to a power of two.  Its m are counted from the largest first: biases may be large and alike (a
+// mask of -1e9 for all rows).  2^(m - M) l is below 2; a factor 2^(m - M) that fp32 holds to 2^-150 only is off by 2^-42
+// of the row.
+__device__ __forceinline__ float log2_floor(float l) { return l > 0.f && l < INFINITY ? (float)((__float_as_int(l) >> 23) - 127) : 0.f; }
+
 // With STRICT, rows of cells that are none are skipped, and cells that have not been passed through yet are.
 template <typename T, int E, bool STRICT>
 __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRICT, ReadoutMore, ReadoutArgs>::type a)
@@ -519,6 +526,8 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
     const int64_t n_tasks = (int64_t)n_comb * BM * chunks;
     const int lane = threadIdx.x & 31;
     const float2 *pm = reinterpret_cast<const float2 *>(a.part_ml);
+    bool lifted = false;
+    if constexpr (STRICT && sizeof(T) == 2) lifted = a.tensor && a.score.bounded && a.score.bias;
     for (int64_t task = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; task < n_tasks;
          task += ((int64_t)gridDim.x * blockDim.x) >> 5) {
         const int64_t gr = task / chunks;
@@ -536,6 +545,18 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
         const float2 *ml = pm + 2 * b0 * BM + r;                 // piece s at ml[slot_rel(s) BM]
         const int64_t sstride = (int64_t)BM * d;                 // one slot
 #define SLOT_REL(s_) (2 * (int64_t)(s_) + ((s_) == 0 ? d0 : 0))
+        float m0 = 0.f;                                          // what the m of lifted pieces are counted from
+        const auto lift = [&](float M) {                         // the largest m -> of what the pieces weigh
+            m0 = fabsf(M) < INFINITY ? M : 0.f;                  // (plus infinity stays what it is)
+            M = -INFINITY;
+            for (int s = lane; s < c.nsplit; s += 32) {
+                const float2 v = ml[SLOT_REL(s) * BM];
+                M = fmaxf(M, (v.x - m0) + log2_floor(v.y));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+            return M;
+        };
         if (!chunked) {
             // One round trip for the row's cell, the pieces' (m, l) pairs (lane
             // s holds piece s) and the first MP pieces' partial columns (lanes
@@ -558,12 +579,13 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
             for (int s = lane + 32; s < c.nsplit; s += 32) M = fmaxf(M, ml[SLOT_REL(s) * BM].x);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+            if (lifted) M = lift(M);
             float L = 0.f;
             if (M != -INFINITY) {
-                if (lane < c.nsplit) L = exp2f(mv.x - M) * mv.y;
+                if (lane < c.nsplit) L = exp2f(mv.x - m0 - M) * mv.y;
                 for (int s = lane + 32; s < c.nsplit; s += 32) {
                     const float2 v = ml[SLOT_REL(s) * BM];
-                    L += exp2f(v.x - M) * v.y;
+                    L += exp2f(v.x - m0 - M) * v.y;
                 }
             }
             L = warp_sum(L);
@@ -572,7 +594,7 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
 #pragma unroll
             for (int q = 0; q < MP; ++q) {
                 const float mq = __shfl_sync(0xffffffffu, mv.x, q);
-                wq[q] = (q < c.nsplit && M != -INFINITY) ? exp2f(mq - M) : 0.f;
+                wq[q] = (q < c.nsplit && M != -INFINITY) ? exp2f(mq - m0 - M) : 0.f;
             }
             if (cell < 0 || cell >= a.mn) {
                 if constexpr (STRICT) continue;
@@ -591,7 +613,7 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
                     acc.w = fmaf(wq[q], pf[q][cb].w, acc.w);
                 }
                 for (int s = MP; s < c.nsplit; ++s) {
-                    const float ws = M == -INFINITY ? 0.f : exp2f(ml[SLOT_REL(s) * BM].x - M);
+                    const float ws = M == -INFINITY ? 0.f : exp2f(ml[SLOT_REL(s) * BM].x - m0 - M);
                     const float4 po = __ldcs(reinterpret_cast<const float4 *>(base + SLOT_REL(s) * sstride + c4));
                     acc.x = fmaf(ws, po.x, acc.x);
                     acc.y = fmaf(ws, po.y, acc.y);
@@ -612,11 +634,12 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
         for (int s = lane; s < c.nsplit; s += 32) M = fmaxf(M, ml[SLOT_REL(s) * BM].x);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        if (lifted) M = lift(M);
         float L = 0.f;
         if (M != -INFINITY)
             for (int s = lane; s < c.nsplit; s += 32) {
                 const float2 v = ml[SLOT_REL(s) * BM];
-                L += exp2f(v.x - M) * v.y;
+                L += exp2f(v.x - m0 - M) * v.y;
             }
         L = warp_sum(L);
         const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -628,7 +651,7 @@ __global__ void __launch_bounds__(256) k_combine(typename std::conditional<STRIC
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll 8
         for (int s = 0; s < c.nsplit; ++s) {
-            const float ws = M == -INFINITY ? 0.f : exp2f(ml[SLOT_REL(s) * BM].x - M);
+            const float ws = M == -INFINITY ? 0.f : exp2f(ml[SLOT_REL(s) * BM].x - m0 - M);
             if constexpr (E == 2) {
                 const float2 po = __ldcs(reinterpret_cast<const float2 *>(base + SLOT_REL(s) * sstride));
                 acc[0] = fmaf(ws, po.x, acc[0]);

@@ -601,10 +601,7 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 tc_fence_after();
             }
             tq += (uint32_t)n;
-            // what the sums are multiplied by: whole rows by 1 / l, pieces of bounded scores by a power of two
-            float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
-            if constexpr (lifted)
-                if (w.slot >= 0) inv = bounded ? piece_step(m_run, l_run) : 1.f;
+            const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
             const int64_t ooff = ((int64_t)w.u * a.mn + cell) * a.D + w.h * DH;
             float *po = a.part_o + ((int64_t)w.slot * 2 * BQ + q * BQ + r) * DH;
 #pragma unroll 1
@@ -632,10 +629,6 @@ __device__ __forceinline__ void readout_pair(const typename ReadoutOf<X>::Args &
                 }
                 if (cell < 0) continue;
                 if (w.slot >= 0) {                                     // split-KV partial (fp32, unnormalised)
-                    if constexpr (lifted) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
-                    }
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         __stcg(reinterpret_cast<float4 *>(po + c0) + k,

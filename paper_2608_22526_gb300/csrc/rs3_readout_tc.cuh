@@ -475,21 +475,9 @@ __device__ __forceinline__ bool bounded_scores(const ReadoutArgs &) { return fal
 __device__ __forceinline__ bool bounded_scores(const ReadoutMore &a) { return a.score.bounded != 0; }
 
 // What bounded scores are summed against is the largest bias, not the largest score: sums against a low bias may weigh more
-// than those against one that is 2^160 higher.  So (1) sums follow a reference in two steps, each the square root of the
-// factor, which alone may be below what fp32 holds;
+// than those against one that is 2^160 higher.  So sums follow a reference in two steps, each the square root of the
+// factor, which alone may be below what fp32 holds; pieces are merged by what they weigh (k_combine).
 __device__ __forceinline__ float half_way(float from, float to) { return ex2_approx(0.5f * (from - to)); }
-
-// (2) a piece of a row is left with its l in [1, 2), for the merge goes by m alone: returns the power of two
-// that its sums take (1 where l is none: no weight, or no number).
-__device__ __forceinline__ float piece_step(float &m, float &l)
-{
-    if (!(l > 0.f && l < INFINITY)) return 1.f;
-    const int e = min((__float_as_int(l) >> 23) - 127, 126);
-    const float step = __int_as_float((127 - e) << 23);
-    m += (float)e;
-    l *= step;
-    return step;
-}
 
 // Items [it_begin, it_end) of the plan, this CTA's slice; frees the tensor memory.
 template <int DH, class X = PlainScores>
@@ -909,7 +897,7 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 for (int q = 0; q < NSPLIT; ++q) l_run += redl[q * BM + r];
             }
             tcnt += (uint32_t)n;
-            float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+            const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
             if (w.slot >= 0) {
                 // split-KV partial (fp32, unnormalised): 32 columns at a time are
                 // staged through shared memory so that each store instruction
@@ -917,7 +905,6 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                 // warp's part of the P ring, idle from the item's last PV (waited
                 // for above) until the next item's first P, which no warp writes
                 // before every warp has passed this epilogue (QFULL).
-                if constexpr (lifted) inv = bounded ? piece_step(m_run, l_run) : 1.f;
                 float *stg = reinterpret_cast<float *>(gbase + C::OFF_P) + (warp - 4) * (32 * 36);
                 float *pdst = a.part_o + ((int64_t)w.slot * BM + 32 * q4) * DH + h * OCOLS;
 #pragma unroll 1
@@ -929,10 +916,6 @@ __device__ __forceinline__ void readout_tc(const typename ReadoutOf<X>::Args &a,
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = 0u;
-                    }
-                    if constexpr (lifted) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
                     }
                     __syncwarp();
 #pragma unroll

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_long_bank import DT, Built, gen
+from test_gpu_long_bank import DT, Built, bits, gen
 from test_gpu_more_readouts import frames_of, keep_sets, reference, run_scored, scored_rows, spoil
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,40 @@ def test_values_as_large_as_the_limit_allows(rs3, H, d, m, counts):
     bias = torch.tensor([0.0, -1.8, -3.6, -5.4, -0.1], device="cuda").repeat(H, 1).contiguous()
     out = check(rs3, b, q, counts, 55.0, bias)
     assert out[0].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype,U,H,d,m,ring_frames,counts", SHAPES[:8])
+@pytest.mark.parametrize("offset", [-1e9, -1e5, 12345.0, 1e9])
+def test_an_offset_of_all_biases_changes_nothing(rs3, dtype, U, H, d, m, ring_frames, counts, offset):
+    """All frames masked by the same finite number, scores at either end of the cap: the weights are the scores' own."""
+    b, q = saturated(rs3, dtype, U, H, d, m, ring_frames, 9, range(0, ring_frames, 3))
+    idx, count = keep_sets(U, b.mn, max(counts), counts, 7)
+    group = torch.zeros(U, dtype=torch.int32, device="cuda")
+    outs = []
+    for value in (0.0, offset):
+        bias = torch.full((H, ring_frames + 2), value, device="cuda")
+        outs.append(torch.zeros((U, b.mn, b.D), dtype=DT[dtype], device="cuda"))
+        run_scored(rs3, b, q, 1, idx, count, group, 55.0, bias, None, None, 0.0, None, outs[-1])
+    assert int(b.st) == 0
+    assert torch.equal(bits(outs[0]), bits(outs[1])) and (outs[0] != 0).any()
+
+
+@pytest.mark.parametrize("dtype,U,H,d,m,ring_frames,counts", SHAPES)
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_a_bias_that_is_no_number_makes_its_queries_none(rs3, dtype, U, H, d, m, ring_frames, counts, value):
+    """Plus infinity and NaN reach the result from whichever piece they are in, of the head and unit that they belong to."""
+    b, q = saturated(rs3, dtype, U, H, d, m, ring_frames, 10, [0])
+    idx, count = keep_sets(U, b.mn, max(counts), counts, 7)
+    group = torch.zeros(U, dtype=torch.int32, device="cuda")
+    for frame in (0, ring_frames // 2, ring_frames, ring_frames + 1):
+        bias = torch.zeros((U, H, ring_frames + 2), device="cuda")
+        bias[0, H - 1, frame] = value
+        bias[:, :, 1] = -math.inf
+        out = torch.zeros((U, b.mn, b.D), dtype=DT[dtype], device="cuda")
+        run_scored(rs3, b, q, 1, idx, count, group, 55.0, bias, None, None, 0.0, None, out)
+        assert int(b.st) == 0
+        cells = idx[0, :counts[0]].long()
+        # (of three frames, the middle one's value gives way to minus infinity)
+        assert out[0, cells, (H - 1) * d:].isnan().all() == (frame != 1), frame
+        out[0, cells, (H - 1) * d:] = 0.0
+        assert out.isfinite().all(), frame
