@@ -467,10 +467,11 @@ size_t rs3_scored_readout_workspace_bytes(const rs3_bank *bank, int k_max);
  * F for a row of a conditioning frame and F + 1 for a pointer row: slopes in the age, learned
  * biases by distance, windows, frames of another shot left out with the conditioning
  * frames as the prefix that is always seen.
- *   cap         0 (none) or in [2^-10, 2^10]
+ *   cap         0 (none) or in [2^-10, 2^10].  A capped score is within 2e-6 of the cap (32 roundings
+ *               of fp32): at 1024 a weight is off by 2e-3, half of a rounding to bf16
  *   frame_bias  device fp32 [H][F+2], or [U][H][F+2] bias_stride elements apart
- *               (bias_stride 0: one for all units), or NULL.  Minus infinity and all below
- *               -1e30 (a type's lowest value, say): the row weighs nothing
+ *               (bias_stride 0: one for all units), or NULL; at most 1e30.  Minus infinity and all
+ *               below -1e30 (a type's lowest value, say): the row weighs nothing
  *   frame_keep  device uint8 [U][F+2] or NULL.  Rows that are left out are not read as far as
  *               results go: their bits do not matter
  * A query with no row left, or whose rows all weigh nothing, reads A = 0; a changed
@@ -509,7 +510,9 @@ size_t rs3_shared_readout_workspace_bytes(const rs3_bank *bank, const rs3_bank *
  * the same one is fine out of place).  A cell outside [0, mn) latches RS3_EINVAL and is
  * skipped; a count outside [0, k_max], a group outside [0, G) or a prefix unit out of range
  * latches it and the unit is skipped, and so is one whose counters or whose prefix's are
- * unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.
+ * unsound (RS3_EINTERNAL).  k_max <= mn = bank->mn.  As in rs3_memory_readout, and other than in
+ * rs3_scored_readout, rows that are live no longer (evicted ones) are read beside live ones, with
+ * weight 0: what they hold is finite, in a prefix for all of its units.
  *   workspace    device, >= rs3_shared_readout_workspace_bytes(...) bytes, 16-byte aligned;
  *                one call at a time
  * Limits: those of rs3_memory_readout, for both banks.

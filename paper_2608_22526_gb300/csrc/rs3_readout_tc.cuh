@@ -353,8 +353,8 @@ __device__ __forceinline__ float capped_exp(const uint32_t (&sr)[N], uint32_t *p
 // pipe beside the softmax's powers.  Columns of no row hold zeros (they share a reciprocal with others).
 // 48 objects of four heads of 64 on 96 x 96 cells, 135 000 tiles of 128 x 128 scores, capped and biased, in
 // place: the call takes 2 100 us with a reciprocal for each score, 1 530 with one for four (and two query tiles
-// per CTA), 1 250 with the polynomial and the biases looked up by the producer's warp instead of the softmax's, 1 107
-// without a running maximum (capped_exp); beyond half the cap 1 562; without a cap 736, plain scores 691.
+// per CTA), 1 250 with the polynomial and the biases looked up by the producer's warp instead of the softmax's, 1 084
+// without a running maximum (capped_exp); beyond half the cap 1 565; without a cap 738, plain scores 688.
 template <class X, int N>
 __device__ __forceinline__ void change_scores(uint32_t (&sr)[N], const ScoreArgs &s, const TileBias &b, float size, float &sc, float &off)
 {

@@ -14,8 +14,9 @@
 // Scores that a cap of 55 or less bounds need no running maximum (RS3_BOUNDED): weights are taken against the largest bias
 // so far, the same for all rows, and cap and power are one pass.  V rows of a tile that belong to no
 // live row are zeroed in shared memory, so that nothing comes of what they hold.  Eight objects of one 64 x 64 grid
-// (7 frames, heads of 256, 46 GFLOP), in place: 68 us capped and biased, 65 capped, 66 biased, 59 with neither (the
-// plain readout 58); 174 000 of 302 000 rows of a video after a cut: 127 us, 200 over all rows.
+// (7 frames, heads of 256, 46 GFLOP), in place, the call alone: 68 us capped and biased, 65 capped, 63 to 72 biased (as
+// biases move the running maximum), 59 with neither (the plain readout 57); 174 000 of 302 000 rows of a video after a
+// cut: 125 us, 194 over all rows.
 #include "rs3_frames.cuh"
 
 #include <algorithm>
@@ -146,8 +147,8 @@ extern "C" rs3_status rs3_scored_readout(const void *q, rs3_dtype dtype, int G, 
         }
     }
     // Out of place, calls of much work leave the cells that are not kept to a warp that the attention has to spare,
-    // and what that has not reached to the merge (48 objects of 96 x 96 cells, 453 MB: 1 137 us, 1 187 where the
-    // plan's launch passes them through)
+    // and what that has not reached to the merge (48 objects of 96 x 96 cells, 453 MB: 45 us less than where the
+    // plan's launch passes them through, 1 158 us then)
     if (L.path.either && residual != out && mn == bank->mn) {
         f.kept = reinterpret_cast<uint32_t *>(ws + L.kept);
         a.kept = f.kept;
