@@ -379,7 +379,7 @@ bool rope_turns(const rs3_rope_spec *s, RopeTurns &t)
     if (s->rot > 2 * ROPE_PAIRS) return true;              // (the caller tells that it is not supported)
     const Two per_turn = {0x1.45f306dc9c883p-3, -0x1.6b01ec5417056p-57};       // 1 / (2 pi)
     const Two one = {1.0, 0.0}, slow = {s->beta_slow, 0.0}, part = one / Two{s->factor, 0.0};
-    const Two slope = s->context > 0.0 ? one / two_sum(s->beta_fast, -s->beta_slow) : one;
+    const Two ramp = two_sum(s->beta_fast, -s->beta_slow), slope = s->context > 0.0 ? one / ramp : one;
     int p = 0;
     for (int a = 0; a < s->axes; ++a) {
         const Two step = s->pairs[a] > 1 ? root_of(s->base, s->pairs[a]) : one;
@@ -387,9 +387,9 @@ bool rope_turns(const rs3_rope_spec *s, RopeTurns &t)
         for (int i = 0; i < s->pairs[a]; ++i, ++p, f = f * step) {
             Two turn = f * part;
             if (s->context > 0.0) {
-                Two share = (f * Two{s->context, 0.0} - slow) * slope;          // of the frequency as trained
-                if (share.hi >= 1.0) share = one;
-                if (share.hi > 0.0) turn = f * share + turn * (one - share);
+                const Two up = f * Two{s->context, 0.0} - slow, share = up * slope;       // of the frequency as trained
+                if (up.hi >= ramp.hi) turn = f;            // (a ramp may be too short for its slope)
+                else if (up.hi > 0.0) turn = f * share + turn * (one - share);
             }
             // (below 2^62, and what lies behind its whole number within some hundreds)
             const double hi = turn.hi * 0x1p64;

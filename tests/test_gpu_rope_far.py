@@ -33,7 +33,8 @@ def turns(n, base, factor, context, fast, slow):
 
 SPECS = [dict(rot=64, base=10000.0, factor=3.0), dict(rot=64, base=10000.0, factor=8.0, context=64.0), dict(rot=256, base=1e12),
          dict(rot=64, base=10000.0, factor=8.0, context=1e7, beta_slow=1.185e6, beta_fast=1.195e6),
-         dict(rot=32, base=500000.0, factor=1e6, context=1e5, beta_slow=7000.0, beta_fast=7010.0), dict(rot=2, base=1.0), dict(rot=16, base=1.0, factor=7.0)]
+         dict(rot=32, base=500000.0, factor=1e6, context=1e5, beta_slow=7000.0, beta_fast=7010.0), dict(rot=2, base=1.0), dict(rot=16, base=1.0, factor=7.0),
+         dict(rot=16, base=100.0, factor=2.0, context=64.0, beta_slow=0.0, beta_fast=1e-310)]
 
 
 @pytest.mark.parametrize("spec", SPECS)
